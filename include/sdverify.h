@@ -90,6 +90,17 @@ typedef struct {
                                     i itself or an ancestor of i (sd_tree_prepare)   */
 } sd_batch;
 
+/* Element type of a matrix of logits. */
+typedef enum { SD_F32 = 0, SD_BF16 = 1 } sd_dtype;
+
+/* Sampling parameters of M rows; every pointer is a dev array [M] or NULL (nobody uses it). */
+typedef struct {
+    const float *inv_temp;       /* 1 / temperature, at least 1e-6; +infinity: the first entry alone (NULL: 1) */
+    const int32_t *top_k;        /* the k first entries; below 1 or above V - 1: all                           */
+    const float *top_p;          /* shortest prefix with this share of their mass; 1 and above: all            */
+    const float *min_p;          /* entries with this share of the largest probability; 0 and below: all       */
+} sd_sampling;
+
 /* Library version (major*100 + minor). */
 int sd_version(void);
 
@@ -459,6 +470,102 @@ sd_status sd_lmhead_accept_sampled_compact(const sd_batch *batch, const void *hi
 sd_status sd_draft_feature_attention(const void *qp, const void *k, const void *v,
                                      int32_t S, int32_t L, int32_t Q, int32_t H, int32_t D,
                                      float scale, void *out, void *stream);
+
+/*
+ * Rows of logits.  The calls below read a matrix of logits as sd_lmhead_stats_logits keeps it, or as a draft model's own head
+ * produces it:
+ *   logits : dev, f32 or bf16 (`dtype`, an sd_dtype), row r starts at element r * ld (ld >= V: rows of a padded vocabulary
+ *            or of a larger matrix; only the base has to be 16-byte aligned), 1 <= V <= 262144
+ * Entries of a row stand in the order (logit descending, index ascending).  Entries of minus infinity, and NaN, are masked: they are
+ * in no list and have no mass.  A mask's lowest finite value is an ordinary logit.  M rows, up to 2^24; M = 0 does nothing.
+ * The small arrays of these calls (one or a few values per row) need the alignment of their elements only.
+ */
+
+/*
+ * The K first entries of every row (Sec. 3.1.3: what a draft learns from is the target's distribution, of which the first tokens
+ * carry nearly all; Sec. 1: a tree's next level is grown from a node's best candidates), with the row's log-sum-exp.
+ *   values : dev f32 [M][K], in order; minus infinity where a row has fewer unmasked entries
+ *   index  : dev int32 [M][K], their places; -1 there
+ *   lse    : NULL, or dev f32 [M]: log sum_v exp(logits[r][v] * inv_temp); minus infinity for a row without an unmasked entry
+ *   1 <= K <= 1024, inv_temp > 0
+ * Every logit is read once.
+ */
+sd_status sd_top_logits(const void *logits, int32_t dtype, int64_t ld, int32_t M, int32_t V, int32_t K,
+                        float inv_temp, float *values, int32_t *index, float *lse,
+                        int32_t *dev_status, void *stream);
+
+/*
+ * Tokens drawn from every row at a temperature behind top-k, top-p and min-p (Sec. 1: drafts that are sampled; the acceptance calls
+ * take the tokens, their probabilities and the distributions that they were drawn from).  Of row r with z = logits * inv_temp[r]:
+ *   the top_k[r] first entries stay; of those the shortest prefix whose mass (exp z) is at least top_p[r] times theirs, one
+ *   entry at least; of those the ones with exp(z - largest) >= min_p[r].  p = softmax(z) over what stays.
+ *   draw n: the first token, in vocabulary order, at which the cumulative mass exceeds u[r][n] times the total.
+ * Arguments that may be NULL are marked; all random numbers are inputs.
+ *   u         : dev f32 [M][N] in [0,1); another number stores SD_ERR_INVALID_ARG and draws -1
+ *   tokens    : dev int32 [M][N]; -1 for a row in which nothing is unmasked (its other outputs: 0, lse minus infinity)
+ *   prob      : dev f32 [M][N] or NULL: p of the drawn token (sd_accept_chain_sampled's q_tok)
+ *   probs     : dev f32 [M][V] or NULL: p of the whole row (sd_accept_tree_sampled_q's q_rows); not `logits`
+ *   lse       : dev f32 [M] or NULL: log of the mass that stays
+ *   1 <= N <= 64
+ * An inv_temp below 1e-6 or NaN stores SD_ERR_INVALID_ARG (the row counts as masked).  Masses and their sums are held in 64 bits,
+ * so that borders and draws are those of exact arithmetic but for sums within about 1e-10 of a border.  Scaled logits beyond
+ * 2^29 count as 2^29.
+ */
+sd_status sd_sample_logits(const void *logits, int32_t dtype, int64_t ld, int32_t M, int32_t V,
+                           const sd_sampling *how, const float *u, int32_t N,
+                           int32_t *tokens, float *prob, float *probs, float *lse,
+                           int32_t *dev_status, void *stream);
+
+/*
+ * The same temperature and filters as a transformation of the target's rows, for verification against the filtered target
+ * (Sec. 1, lossless validation: what is compared with is the distribution that the target would be sampled from).
+ *   out  : dev f32 [M][V]: logits * inv_temp[r] of what stays (finite: products stop at f32's range), minus infinity elsewhere; may be `logits` itself where that
+ *          is f32 with ld = V
+ *   lse  : dev f32 [M]: log sum exp of out's row (minus infinity if nothing is unmasked)
+ *   kept : dev int32 [M] or NULL: how many entries stay
+ * out and lse are what sd_accept_tree_sampled_q and sd_accept_chain_sampled take as logits and lse, with inv_temp = 1 there: the
+ * temperatures, which may differ from row to row, are in them.  (An infinite inv_temp scales by 1.)
+ */
+sd_status sd_filter_logits(const void *logits, int32_t dtype, int64_t ld, int32_t M, int32_t V,
+                           const sd_sampling *how, float *out, float *lse, int32_t *kept,
+                           int32_t *dev_status, void *stream);
+
+/*
+ * The draft's training loss (Sec. 3.1.3, L = KL(p_target || p_draft) + lambda CE(argmax p_target)) from the target's K first
+ * logits, and its gradient.  Student row z = logits[r], s = softmax(z * inv_temp); the target's entries (t, i):
+ *   top_lse NULL : p = softmax of t * inv_temp over the row's entries;  kl[r] = sum_k p_k (log p_k - log s[i_k])
+ *   top_lse given: p_k = exp(t_k * inv_temp - top_lse[r]), and what is missing from 1, p_rest, stands against the student's mass outside
+ *                  the entries, s_rest:  kl[r] = sum_k p_k (log p_k - log s[i_k]) + p_rest (log p_rest - log s_rest)
+ *                  (no such term where p_rest <= 0 or s_rest = 0)
+ *   ce[r] = log sum_v exp z[v] - z[label[r]]                                                    (at temperature 1)
+ *   grad[r][v] = dloss[r] * d(kl_weight * kl[r] + ce_weight * ce[r]) / d z[v]
+ * top_val, top_idx : dev f32, int32 [M][K], 1 <= K <= 1024, as sd_top_logits leaves them.  An index below 0 is no entry (a
+ *             token outside the draft's vocabulary: its mass belongs to the rest); the same index twice adds up
+ * top_lse   : dev f32 [M] or NULL, with the same inv_temp
+ * label     : dev int32 [M] or NULL; below 0: the row has no cross-entropy (ce 0)
+ * kl, ce    : dev f32 [M]; ce may be NULL where label is
+ * stats     : NULL, or dev f32 [M][4] that sd_distill_grad reads
+ * dloss     : NULL (1), or dev f32 [M], the rows' weights in what is minimised; a row of weight 0 has gradient 0
+ * grad      : NULL (the loss alone), or dev [M][V] of the logits' type, rows grad_ld apart; may be `logits` itself (grad_ld = ld)
+ * A row without entries has kl 0.  An index or label of V or more stores SD_ERR_BOUNDS and is left out.  Logits of minus infinity
+ * are allowed (kl is infinite where the target gives one mass); NaN, or a row of minus infinity alone, gives NaN.  With the gradient
+ * in the same call the logits are read once.
+ */
+sd_status sd_distill_loss(const void *logits, int32_t dtype, int64_t ld, int32_t M, int32_t V,
+                          const float *top_val, const int32_t *top_idx, int32_t K, const float *top_lse,
+                          const int32_t *label, float inv_temp, float kl_weight, float ce_weight,
+                          float *kl, float *ce, float *stats, const float *dloss, void *grad, int64_t grad_ld,
+                          int32_t *dev_status, void *stream);
+
+/*
+ * The gradient of sd_distill_loss in a call of its own, where the rows' weights are known only behind the loss.  Arguments as
+ * there; stats as sd_distill_loss left them for the same rows.
+ */
+sd_status sd_distill_grad(const void *logits, int32_t dtype, int64_t ld, int32_t M, int32_t V,
+                          const float *top_val, const int32_t *top_idx, int32_t K, const float *top_lse,
+                          const int32_t *label, float inv_temp, float kl_weight, float ce_weight,
+                          const float *stats, const float *dloss, void *grad, int64_t grad_ld,
+                          int32_t *dev_status, void *stream);
 
 #ifdef __cplusplus
 }

@@ -32,11 +32,16 @@ ATTENTION_LAYERS_PER_LAUNCH = 32   # sd_verify_attention_layers: layers sharing 
 KERNELS_PER_TAIL = 2               # sd_lmhead_accept_compact: LM-head tiles + fused tail kernel
 KERNELS_PER_LMHEAD = 2         # tiles + cross-slab reduce
 KERNELS_PER_SAMPLED_TAIL = 2       # sd_lmhead_accept_sampled_compact: LM-head tiles + one cluster kernel
+KERNELS_PER_ROWS_CALL = 1          # each of the calls on rows of logits
+
+SD_F32 = 0                     # sd_dtype
+SD_BF16 = 1
 
 EXPORTS = ["sd_version", "sd_status_string", "sd_workspace_bytes", "sd_tree_prepare",
            "sd_verify_attention", "sd_verify_attention_layers", "sd_lmhead_argmax", "sd_lmhead_argmax_static", "sd_accept_tree",
            "sd_compact_kv", "sd_lmhead_accept_compact", "sd_lmhead_stats", "sd_accept_tree_sampled", "sd_lmhead_accept_sampled_compact", "sd_accept_chain_sampled", "sd_lmhead_stats_logits", "sd_accept_tree_sampled_q",
-           "sd_draft_feature_attention"]
+           "sd_draft_feature_attention",
+           "sd_top_logits", "sd_sample_logits", "sd_filter_logits", "sd_distill_loss", "sd_distill_grad"]
 
 
 class sd_kv_layer(C.Structure):
@@ -48,6 +53,10 @@ class sd_batch(C.Structure):
                 ("D", C.c_int32), ("block_size", C.c_int32), ("max_blocks_per_seq", C.c_int32),
                 ("block_table", C.c_void_p), ("len", C.c_void_p), ("n_nodes", C.c_void_p),
                 ("parents", C.c_void_p), ("anc_mask", C.c_void_p)]
+
+
+class sd_sampling(C.Structure):
+    _fields_ = [("inv_temp", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p), ("min_p", C.c_void_p)]
 
 
 def _load(path: str = LIB_PATH) -> C.CDLL:
@@ -117,6 +126,18 @@ def _load(path: str = LIB_PATH) -> C.CDLL:
     lib.sd_draft_feature_attention.restype = C.c_int
     lib.sd_draft_feature_attention.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32,
                                                C.c_int32, C.c_int32, C.c_float, C.c_void_p, C.c_void_p]
+    rows = [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int32]
+    lib.sd_top_logits.restype = C.c_int
+    lib.sd_top_logits.argtypes = rows + [C.c_int32, C.c_float] + [C.c_void_p] * 5
+    lib.sd_sample_logits.restype = C.c_int
+    lib.sd_sample_logits.argtypes = rows + [C.c_void_p, C.c_void_p, C.c_int32] + [C.c_void_p] * 6
+    lib.sd_filter_logits.restype = C.c_int
+    lib.sd_filter_logits.argtypes = rows + [C.c_void_p] * 6
+    teacher = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_float, C.c_float, C.c_float]
+    lib.sd_distill_loss.restype = C.c_int
+    lib.sd_distill_loss.argtypes = rows + teacher + [C.c_void_p] * 5 + [C.c_int64, C.c_void_p, C.c_void_p]
+    lib.sd_distill_grad.restype = C.c_int
+    lib.sd_distill_grad.argtypes = rows + teacher + [C.c_void_p] * 3 + [C.c_int64, C.c_void_p, C.c_void_p]
     return lib
 
 
@@ -357,3 +378,106 @@ def sd_draft_feature_attention(qp, k, v, H: int, scale: float, out, stream=None)
     Q, D = qp.shape
     S, L, _ = k.shape
     _check(_n.sd_draft_feature_attention(qp, k, v, S, L, Q, H, D, scale, out, stream))
+
+
+# ------------------------------------------------------------------ rows of logits
+_DTYPES = {torch.float32: SD_F32, torch.bfloat16: SD_BF16}
+
+
+def _rows(t):
+    """(address, dtype, row stride, rows, columns) of a matrix of logits; rows may lie further apart than they are long."""
+    M, V = t.shape
+    assert t.is_cuda and t.dtype in _DTYPES, "logits are float32 or bfloat16 CUDA tensors"
+    assert t.get_device() == torch.cuda.current_device(), "logits lie on another device than the current one"
+    ld = t.stride(0) if M > 1 else max(t.stride(0), V)
+    assert (t.stride(1) == 1 or V == 1) and ld >= V, "a row's logits must be contiguous, rows must not overlap"
+    return t.data_ptr(), _DTYPES[t.dtype], ld, M, V
+
+
+def _shaped(t, shape, dtype=torch.float32):
+    if t is not None:
+        assert t.shape == shape and t.dtype == dtype, f"expected {dtype} {shape}, got {t.dtype} {tuple(t.shape)}"
+
+
+class Sampling:
+    """Owns the per-row arrays named by the C struct ``sd_sampling`` (each a sequence or tensor of M values, or None)."""
+
+    def __init__(self, inv_temp=None, top_k=None, top_p=None, min_p=None, device="cuda"):
+        to = lambda a, t: None if a is None else torch.as_tensor(a, dtype=t).contiguous().to(torch.device(device))
+        self.inv_temp, self.top_p, self.min_p = to(inv_temp, torch.float32), to(top_p, torch.float32), to(min_p, torch.float32)
+        self.top_k = to(top_k, torch.int32)
+        have = [t for t in (self.inv_temp, self.top_k, self.top_p, self.min_p) if t is not None]
+        assert all(t.dim() == 1 and t.shape == have[0].shape for t in have), "one value per row in each array"
+        self.M = have[0].numel() if have else None
+        self.c = sd_sampling(_ptr(self.inv_temp), _ptr(self.top_k), _ptr(self.top_p), _ptr(self.min_p))
+
+
+def sd_top_logits(logits, inv_temp: float, values, index, lse, status, stream=None) -> None:
+    """The K first entries of every row of logits [M,V] (values, index [M,K]) and lse [M] (or None) at inv_temp."""
+    x, dtype, ld, M, V = _rows(logits)
+    K = values.size(1)
+    _shaped(values, (M, K))
+    _shaped(index, (M, K), torch.int32)
+    _shaped(lse, (M,))
+    _check(_n.sd_top_logits(x, dtype, ld, M, V, K, inv_temp, values, index, lse, status, stream))
+
+
+def sd_sample_logits(logits, how: Sampling, u, tokens, prob, probs, lse, status, stream=None) -> None:
+    """N tokens per row drawn with the uniforms u [M,N]: tokens [M,N], their probabilities prob [M,N] (or None), the filtered
+    distributions probs [M,V] (or None) and the log of the mass that stays, lse [M] (or None)."""
+    x, dtype, ld, M, V = _rows(logits)
+    N = u.size(1)
+    assert how.M is None or how.M == M, "one set of sampling parameters per row"
+    _shaped(u, (M, N))
+    _shaped(tokens, (M, N), torch.int32)
+    _shaped(prob, (M, N))
+    _shaped(probs, (M, V))
+    _shaped(lse, (M,))
+    _check(_n.sd_sample_logits(x, dtype, ld, M, V, _at(how.c), u, N, tokens, prob, probs, lse, status, stream))
+
+
+def sd_filter_logits(logits, how: Sampling, out, lse, kept, status, stream=None) -> None:
+    """out [M,V] (f32; may be f32 logits themselves) = logits * inv_temp where the filters let them stay, minus infinity elsewhere; lse [M];
+    kept [M] (or None).  sd_accept_tree_sampled_q and sd_accept_chain_sampled take out and lse with inv_temp = 1."""
+    x, dtype, ld, M, V = _rows(logits)
+    assert how.M is None or how.M == M, "one set of sampling parameters per row"
+    _shaped(out, (M, V))
+    _shaped(lse, (M,))
+    _shaped(kept, (M,), torch.int32)
+    _check(_n.sd_filter_logits(x, dtype, ld, M, V, _at(how.c), out, lse, kept, status, stream))
+
+
+def _distill_args(logits, top_val, top_idx, top_lse, label, dloss, grad, stats):
+    x, dtype, ld, M, V = _rows(logits)
+    K = top_val.size(1)
+    _shaped(top_val, (M, K))
+    _shaped(top_idx, (M, K), torch.int32)
+    _shaped(top_lse, (M,))
+    _shaped(label, (M,), torch.int32)
+    _shaped(dloss, (M,))
+    _shaped(stats, (M, 4))
+    g, g_ld = None, V
+    if grad is not None:
+        g, g_dtype, g_ld, g_M, g_V = _rows(grad)
+        assert (g_dtype, g_M, g_V) == (dtype, M, V), "the gradient has the logits' type and shape"
+    return x, dtype, ld, M, V, K, g, g_ld
+
+
+def sd_distill_loss(logits, top_val, top_idx, top_lse, label, inv_temp: float, kl_weight: float, ce_weight: float, kl, ce, stats,
+                    dloss, grad, status, stream=None) -> None:
+    """KL from the target's first logits (top_val, top_idx [M,K], top_lse [M] or None: sd_top_logits) to the student's rows, kl [M], and
+    cross-entropy with label [M] (or None), ce [M].  With grad (the logits' type and shape, or the logits themselves): the gradient of
+    sum_r dloss[r] (kl_weight kl[r] + ce_weight ce[r]) too.  stats [M,4] (or None): for sd_distill_grad."""
+    x, dtype, ld, M, V, K, g, g_ld = _distill_args(logits, top_val, top_idx, top_lse, label, dloss, grad, stats)
+    _shaped(kl, (M,))
+    _shaped(ce, (M,))
+    _check(_n.sd_distill_loss(x, dtype, ld, M, V, top_val, top_idx, K, top_lse, label, inv_temp, kl_weight, ce_weight, kl, ce, stats,
+                              dloss, g, g_ld, status, stream))
+
+
+def sd_distill_grad(logits, top_val, top_idx, top_lse, label, inv_temp: float, kl_weight: float, ce_weight: float, stats, dloss, grad,
+                    status, stream=None) -> None:
+    """The gradient of sd_distill_loss in a call of its own, from the stats that it left."""
+    x, dtype, ld, M, V, K, g, g_ld = _distill_args(logits, top_val, top_idx, top_lse, label, dloss, grad, stats)
+    _check(_n.sd_distill_grad(x, dtype, ld, M, V, top_val, top_idx, K, top_lse, label, inv_temp, kl_weight, ce_weight, stats, dloss,
+                              g, g_ld, status, stream))

@@ -2,6 +2,7 @@
 #include "common.cuh"
 
 #include <atomic>
+#include <math.h>
 #include <stdlib.h>
 #include <string.h>
 #include <unistd.h>
@@ -58,6 +59,33 @@ sd_status check_geometry(const sd_batch* bt, bool need_pointers) {
 }
 
 bool ok_ptr(const void* p) { return p && aligned16(p); }
+bool ok_4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+sd_status check_rows(const void* logits, int32_t dtype, int64_t ld, int32_t M, int32_t V) {
+    if (M < 0 || V < 1 || ld < V) return SD_ERR_INVALID_ARG;
+    if (dtype != SD_F32 && dtype != SD_BF16) return SD_ERR_UNSUPPORTED;
+    if (V > 262144 || M > (1 << 24)) return SD_ERR_UNSUPPORTED;
+    if (M > 0 && !ok_ptr(logits)) return SD_ERR_INVALID_ARG;
+    return SD_OK;
+}
+bool ok_sampling(const sd_sampling* how) {
+    return how && ok_4(how->inv_temp) && ok_4(how->top_k) && ok_4(how->top_p) && ok_4(how->min_p);
+}
+// the arguments that the two distillation calls share
+sd_status check_distill(const void* logits, int32_t dtype, int64_t ld, int32_t M, int32_t V, const float* top_val, const int32_t* top_idx,
+                        int32_t K, const float* top_lse, const int32_t* label, float inv_temp, const float* dloss, const void* grad,
+                        int64_t grad_ld, const int32_t* dev_status) {
+    const sd_status s = check_rows(logits, dtype, ld, M, V);
+    if (s != SD_OK) return s;
+    if (K < 1 || !(inv_temp > 0.f) || !(inv_temp < INFINITY)) return SD_ERR_INVALID_ARG;
+    if (K > 1024) return SD_ERR_UNSUPPORTED;
+    if (M == 0) return SD_OK;
+    if (!top_val || !top_idx || !dev_status) return SD_ERR_INVALID_ARG;
+    if (!ok_4(top_val) || !ok_4(top_idx) || !ok_4(top_lse) || !ok_4(label) || !ok_4(dloss)) return SD_ERR_INVALID_ARG;
+    if (grad && (!aligned16(grad) || grad_ld < V)) return SD_ERR_INVALID_ARG;
+    if (grad == logits && grad_ld != ld) return SD_ERR_INVALID_ARG;
+    return SD_OK;
+}
 
 }  // namespace
 
@@ -292,6 +320,65 @@ sd_status sd_draft_feature_attention(const void* qp, const void* k, const void* 
     if (S < 1 || L < 1 || Q < 1 || H < 1 || !(scale > 0.f)) return SD_ERR_INVALID_ARG;
     if (D != H * 128 || L > 32 || Q > 8) return SD_ERR_UNSUPPORTED;
     return launch_draft_feature_attention(qp, k, v, S, L, Q, H, scale, out, static_cast<cudaStream_t>(stream));
+}
+
+sd_status sd_top_logits(const void* logits, int32_t dtype, int64_t ld, int32_t M, int32_t V, int32_t K, float inv_temp,
+                        float* values, int32_t* index, float* lse, int32_t* dev_status, void* stream) {
+    const sd_status s = check_rows(logits, dtype, ld, M, V);
+    if (s != SD_OK) return s;
+    if (K < 1 || !(inv_temp > 0.f) || !(inv_temp < INFINITY)) return SD_ERR_INVALID_ARG;
+    if (K > 1024) return SD_ERR_UNSUPPORTED;
+    if (M == 0) return SD_OK;
+    if (!values || !index || !ok_4(values) || !ok_4(index) || !ok_4(lse) || !dev_status) return SD_ERR_INVALID_ARG;
+    return launch_top_logits(logits, dtype, ld, M, V, K, inv_temp, values, index, lse, static_cast<cudaStream_t>(stream));
+}
+
+sd_status sd_sample_logits(const void* logits, int32_t dtype, int64_t ld, int32_t M, int32_t V, const sd_sampling* how,
+                           const float* u, int32_t N, int32_t* tokens, float* prob, float* probs, float* lse,
+                           int32_t* dev_status, void* stream) {
+    const sd_status s = check_rows(logits, dtype, ld, M, V);
+    if (s != SD_OK) return s;
+    if (!ok_sampling(how) || N < 1) return SD_ERR_INVALID_ARG;
+    if (N > 64) return SD_ERR_UNSUPPORTED;
+    if (M == 0) return SD_OK;
+    if (!u || !tokens || !dev_status) return SD_ERR_INVALID_ARG;
+    if (!ok_4(u) || !ok_4(tokens) || !ok_4(prob) || !ok_4(lse) || (probs && !aligned16(probs)) || probs == logits) return SD_ERR_INVALID_ARG;
+    return launch_sample(logits, dtype, ld, M, V, *how, u, N, tokens, prob, probs, false, lse, nullptr, dev_status,
+                         static_cast<cudaStream_t>(stream));
+}
+
+sd_status sd_filter_logits(const void* logits, int32_t dtype, int64_t ld, int32_t M, int32_t V, const sd_sampling* how,
+                           float* out, float* lse, int32_t* kept, int32_t* dev_status, void* stream) {
+    const sd_status s = check_rows(logits, dtype, ld, M, V);
+    if (s != SD_OK) return s;
+    if (!ok_sampling(how)) return SD_ERR_INVALID_ARG;
+    if (M == 0) return SD_OK;
+    if (!ok_ptr(out) || !lse || !ok_4(lse) || !ok_4(kept) || !dev_status) return SD_ERR_INVALID_ARG;
+    if (out == logits && (dtype != SD_F32 || ld != V)) return SD_ERR_INVALID_ARG;
+    return launch_sample(logits, dtype, ld, M, V, *how, nullptr, 0, nullptr, nullptr, out, true, lse, kept, dev_status,
+                         static_cast<cudaStream_t>(stream));
+}
+
+sd_status sd_distill_loss(const void* logits, int32_t dtype, int64_t ld, int32_t M, int32_t V, const float* top_val,
+                          const int32_t* top_idx, int32_t K, const float* top_lse, const int32_t* label, float inv_temp,
+                          float kl_weight, float ce_weight, float* kl, float* ce, float* stats, const float* dloss, void* grad,
+                          int64_t grad_ld, int32_t* dev_status, void* stream) {
+    const sd_status s = check_distill(logits, dtype, ld, M, V, top_val, top_idx, K, top_lse, label, inv_temp, dloss, grad, grad_ld, dev_status);
+    if (s != SD_OK || M == 0) return s;
+    if (!kl || !ok_4(kl) || (label && !ce) || !ok_4(ce) || (stats && !aligned16(stats))) return SD_ERR_INVALID_ARG;
+    return launch_distill_loss(DistillCall{logits, ld, V, top_val, top_idx, K, top_lse, label, inv_temp, kl_weight, ce_weight, kl, ce, stats, dloss,
+                                           grad, grad_ld, dev_status}, dtype, M, static_cast<cudaStream_t>(stream));
+}
+
+sd_status sd_distill_grad(const void* logits, int32_t dtype, int64_t ld, int32_t M, int32_t V, const float* top_val,
+                          const int32_t* top_idx, int32_t K, const float* top_lse, const int32_t* label, float inv_temp,
+                          float kl_weight, float ce_weight, const float* stats, const float* dloss, void* grad, int64_t grad_ld,
+                          int32_t* dev_status, void* stream) {
+    const sd_status s = check_distill(logits, dtype, ld, M, V, top_val, top_idx, K, top_lse, label, inv_temp, dloss, grad, grad_ld, dev_status);
+    if (s != SD_OK || M == 0) return s;
+    if (!grad || !ok_ptr(stats)) return SD_ERR_INVALID_ARG;
+    return launch_distill_grad(DistillCall{logits, ld, V, top_val, top_idx, K, top_lse, label, inv_temp, kl_weight, ce_weight, nullptr, nullptr,
+                                           const_cast<float*>(stats), dloss, grad, grad_ld, dev_status}, dtype, M, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

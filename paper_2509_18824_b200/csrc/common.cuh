@@ -158,4 +158,18 @@ sd_status launch_lmhead_accept_sampled_compact(const sd_batch& bt, const void* h
                                                int32_t* out_tok, int32_t* new_len, void* ws, size_t ws_bytes,
                                                int32_t* dev_status, cudaStream_t st);
 
+// rows of logits (sample.cu, distill.cu)
+sd_status launch_top_logits(const void* logits, int dtype, long long ld, int M, int V, int K, float inv_temp, float* values, int32_t* index,
+                            float* lse, cudaStream_t st);
+sd_status launch_sample(const void* logits, int dtype, long long ld, int M, int V, const sd_sampling& how, const float* u, int N, int32_t* tokens,
+                        float* prob, float* dense, bool scaled, float* lse, int32_t* kept, int32_t* dev_status, cudaStream_t st);
+struct DistillCall {
+    const void* logits; long long ld; int V;
+    const float* top_val; const int32_t* top_idx; int K; const float* top_lse; const int32_t* label;
+    float inv_temp, kl_weight, ce_weight;
+    float *kl, *ce, *stats; const float* dloss; void* grad; long long grad_ld; int32_t* status;
+};
+sd_status launch_distill_loss(const DistillCall& call, int dtype, int M, cudaStream_t st);
+sd_status launch_distill_grad(const DistillCall& call, int dtype, int M, cudaStream_t st);
+
 }  // namespace sdv

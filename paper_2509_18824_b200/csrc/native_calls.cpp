@@ -59,6 +59,12 @@ template <> struct Convert<int32_t> {
         return !PyErr_Occurred();
     }
 };
+template <> struct Convert<int64_t> {
+    static bool get(const Arg& a, int64_t* out) {
+        *out = PyLong_AsLongLong(a.obj);
+        return !PyErr_Occurred();
+    }
+};
 template <> struct Convert<float> {
     static bool get(const Arg& a, float* out) {
         *out = static_cast<float>(PyFloat_AsDouble(a.obj));
@@ -109,7 +115,8 @@ PyMethodDef kMethods[] = {
     SD_METHOD(sd_lmhead_argmax), SD_METHOD(sd_lmhead_argmax_static), SD_METHOD(sd_accept_tree), SD_METHOD(sd_compact_kv),
     SD_METHOD(sd_lmhead_accept_compact), SD_METHOD(sd_lmhead_stats), SD_METHOD(sd_lmhead_stats_logits),
     SD_METHOD(sd_accept_tree_sampled), SD_METHOD(sd_accept_chain_sampled), SD_METHOD(sd_accept_tree_sampled_q),
-    SD_METHOD(sd_lmhead_accept_sampled_compact), SD_METHOD(sd_draft_feature_attention), {nullptr, nullptr, 0, nullptr}};
+    SD_METHOD(sd_lmhead_accept_sampled_compact), SD_METHOD(sd_draft_feature_attention), SD_METHOD(sd_top_logits),
+    SD_METHOD(sd_sample_logits), SD_METHOD(sd_filter_logits), SD_METHOD(sd_distill_loss), SD_METHOD(sd_distill_grad), {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_sdnative", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,199 @@
+// Rows of logits: 16-byte vectors of a row that may start anywhere, masses in 64 bits, the order of a row's entries, and the
+// block-wide steps (sums, scans, sorting) that the kernels on rows share.
+#pragma once
+#include "common.cuh"
+#include "sm100.cuh"
+
+namespace sdv {
+namespace rows {
+
+constexpr int kThreads = 512;          // threads of a CTA of sample.cu
+constexpr int kWarps = kThreads / 32;
+constexpr float kLog2e = 1.4426950408889634f;
+
+// ---------------------------------------------------------------- a row as 16-byte vectors
+// Vector 0 is the aligned one that holds the row's first entry; `lead` entries of it lie in front of the row, and the last
+// one may reach behind the row.  Those two are put together from single entries, so that nothing outside the row is read.
+template <typename T>
+struct Row {
+    static constexpr int kE = 16 / (int)sizeof(T);
+    const T* p;
+    const uint4* vec;
+    int lead, V, nvec, full0, full1;
+    __device__ __forceinline__ Row(const void* base, long long ld, long long r, int V_) : p(static_cast<const T*>(base) + r * ld), V(V_) {
+        const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+        vec = reinterpret_cast<const uint4*>(a & ~(uintptr_t)15);
+        lead = (int)((a & 15) / sizeof(T));
+        nvec = (lead + V + kE - 1) / kE;
+        full0 = lead ? 1 : 0;
+        full1 = (lead + V) / kE;
+    }
+    static __device__ __forceinline__ uint4 nothing() {                            // entries of minus infinity
+        const uint32_t w = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+        return make_uint4(w, w, w, w);
+    }
+    __device__ __forceinline__ uint4 edge(int i) const {
+        const uint4 r = nothing();
+        uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+            const int v = i * kE + e - lead;
+            if (v < 0 || v >= V) continue;
+            if constexpr (sizeof(T) == 4) w[e] = __float_as_uint(__ldcg(reinterpret_cast<const float*>(p) + v));
+            else {
+                const uint32_t h = __ldcg(reinterpret_cast<const unsigned short*>(p) + v);
+                w[e >> 1] = (e & 1) ? ((w[e >> 1] & 0xffffu) | (h << 16)) : ((w[e >> 1] & 0xffff0000u) | h);
+            }
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    // (through L2, never the read-only path: a filter's output may be the row itself)
+    __device__ __forceinline__ uint4 load(int i) const { return i >= full0 && i < full1 ? __ldcg(vec + i) : edge(i); }
+    static __device__ __forceinline__ void unpack(const uint4& r, float (&x)[kE]) {
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int e = 0; e < kE; ++e) {
+            if constexpr (sizeof(T) == 4) x[e] = __uint_as_float(w[e]);
+            else x[e] = (e & 1) ? bf16hi(w[e >> 1]) : bf16lo(w[e >> 1]);
+        }
+    }
+    __device__ __forceinline__ float at(int v) const {
+        if constexpr (sizeof(T) == 4) return __ldcg(reinterpret_cast<const float*>(p) + v);
+        else return __uint_as_float((uint32_t)__ldcg(reinterpret_cast<const unsigned short*>(p) + v) << 16);
+    }
+};
+
+// 2^x, to about 2^-22 of it
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// ---------------------------------------------------------------- masses
+// mass(x) = 2^(x c - ref) with c = inv_temp log2 e and a whole number ref, in 64 bits: which token a uniform number falls on, and
+// where a sum passes top_p of another, must not depend on the rounding of single masses (with 2^-24 in each of 152064 equal masses
+// one draw in forty thousand would).  2^f for |f| <= 1/2 is its Taylor series up to f^9 (the rest is below 7e-12 of it); ref
+// being whole, sums taken with different ones are brought together exactly.  Scaled logits beyond 2^29 count as 2^29.
+struct Scale {
+    double c;
+    float lim;
+    __device__ __forceinline__ explicit Scale(float inv_temp) : c((double)inv_temp * 1.4426950408889634073599) {
+        lim = (float)fmin(536870912.0 / c, 3.4028234663852886e38);
+    }
+    __device__ __forceinline__ double clamped(float x) const { return (double)fminf(fmaxf(x, -lim), lim) * c; }
+    __device__ __forceinline__ int whole(float x) const { return __double2int_rn(clamped(x)); }
+    __device__ __forceinline__ double mass(float x, int ref) const {
+        const double t = clamped(x);
+        const double big = 6755399441055744.0;                                     // 1.5 * 2^52: adding it rounds to a whole number
+        const double r = t + big;
+        const int n = __double2loint(r);
+        const double f = t - (r - big);
+        double p = 1.0178086009239699e-07;                                         // (ln 2)^k / k!, k = 9 .. 0
+        p = fma(p, f, 1.3215486790144309e-06);
+        p = fma(p, f, 1.5252733804059841e-05);
+        p = fma(p, f, 1.5403530393381609e-04);
+        p = fma(p, f, 1.3333558146428443e-03);
+        p = fma(p, f, 9.6181291076284772e-03);
+        p = fma(p, f, 5.5504108664821580e-02);
+        p = fma(p, f, 2.4022650695910072e-01);
+        p = fma(p, f, 6.9314718055994531e-01);
+        p = fma(p, f, 1.0);
+        const int e = n - ref;
+        if (!(x > -INFINITY) || e < -1000) return 0.0;                             // masked entries and NaN have none
+        return __hiloint2double(__double2hiint(p) + (e << 20), __double2loint(p));
+    }
+};
+// v * 2^e
+__device__ __forceinline__ double times_pow2(double v, int e) {
+    if (e < -1000) return 0.0;
+    return v * __hiloint2double((1023 + min(e, 1000)) << 20, 0);
+}
+
+// ---------------------------------------------------------------- the order of a row's entries
+// Entries stand in the order (logit descending, index ascending); the smaller key comes first.  Zeros of both signs are equal.
+__device__ __forceinline__ uint64_t order_key(float x, int index) {
+    const uint32_t u = __float_as_uint(x + 0.f);
+    const uint32_t up = u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u);
+    return ((uint64_t)(~up) << 32) | (uint32_t)index;
+}
+__device__ __forceinline__ float key_logit(uint64_t key) {
+    const uint32_t up = ~(uint32_t)(key >> 32);
+    return __uint_as_float(up ^ ((up >> 31) ? 0x80000000u : 0xffffffffu));
+}
+__device__ __forceinline__ int key_index(uint64_t key) { return (int)(uint32_t)key; }
+
+// ---------------------------------------------------------------- clusters of one to eight CTAs
+__device__ __forceinline__ void sync_parts(int parts) {
+    if (parts == 1) { __syncthreads(); return; }
+    sm100::cluster_arrive_release();
+    sm100::cluster_wait_acquire();
+}
+// the same variable of shared memory in CTA `rank` of the cluster
+template <typename P>
+__device__ __forceinline__ P* of_rank(P* mine, int rank) {
+    uint64_t r;
+    asm volatile("mapa.u64 %0, %1, %2;" : "=l"(r) : "l"(reinterpret_cast<uint64_t>(mine)), "r"(rank));
+    return reinterpret_cast<P*>(r);
+}
+
+// ---------------------------------------------------------------- block-wide steps
+template <typename S>
+__device__ __forceinline__ S warp_add(S v) {
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    return v;
+}
+__device__ __forceinline__ float warp_fmax(float v) {
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
+    return v;
+}
+
+// Inclusive sums of a[0..n), n <= 2 * kThreads, in place and in a fixed order.  `tmp`: kWarps values.
+template <typename S>
+__device__ void block_scan(S* a, int n, S* tmp) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, i = 2 * tid;
+    __syncthreads();
+    const S x = i < n ? a[i] : S(0), y = i + 1 < n ? a[i + 1] : S(0);
+    S s = x + y;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const S o = __shfl_up_sync(0xffffffffu, s, d);
+        if (lane >= d) s += o;
+    }
+    if (lane == 31) tmp[warp] = s;
+    __syncthreads();
+    S before = S(0);
+    for (int w = 0; w < warp; ++w) before += tmp[w];
+    const S own = __shfl_up_sync(0xffffffffu, s, 1);
+    if (lane > 0) before += own;
+    if (i < n) a[i] = before + x;
+    if (i + 1 < n) a[i + 1] = before + x + y;
+    __syncthreads();
+}
+
+// a[0..n) in ascending order; n <= 1024, room for the next power of two.
+static __device__ __noinline__ void block_sort(uint64_t* a, int n) {
+    const int tid = threadIdx.x;
+    int size = 32;
+    while (size < n) size <<= 1;
+    __syncthreads();
+    for (int i = n + tid; i < size; i += kThreads) a[i] = ~0ull;
+    __syncthreads();
+    for (int k = 2; k <= size; k <<= 1) {
+        for (int j = k >> 1; j >= 1; j >>= 1) {
+            if (tid < size / 2) {
+                const int i = 2 * tid - (tid & (j - 1)), o = i + j;
+                const uint64_t x = a[i], y = a[o];
+                if ((x > y) == ((i & k) == 0)) { a[i] = y; a[o] = x; }
+            }
+            if (j > 32) __syncthreads();                                           // (32 pairs of j <= 32 stay within a warp's 64 entries)
+            else __syncwarp();
+        }
+        __syncthreads();
+    }
+}
+
+}  // namespace rows
+}  // namespace sdv
