@@ -11,6 +11,37 @@ constexpr int kThreads = 512;          // threads of a CTA of sample.cu
 constexpr int kWarps = kThreads / 32;
 constexpr float kLog2e = 1.4426950408889634f;
 
+// ---------------------------------------------------------------- arithmetic
+// 2^x, to about 2^-22 of it
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Two 32-bit operations in one instruction
+struct Pair { float x, y; };
+__device__ __forceinline__ uint64_t as_u64(Pair a) { uint64_t r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a.x), "f"(a.y)); return r; }
+__device__ __forceinline__ Pair as_pair(uint64_t v) { Pair a; asm("mov.b64 {%0, %1}, %2;" : "=f"(a.x), "=f"(a.y) : "l"(v)); return a; }
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(as_u64(a)), "l"(as_u64(b)), "l"(as_u64(c)));
+    return as_pair(d);
+}
+__device__ __forceinline__ Pair add2(Pair a, Pair b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(as_u64(a)), "l"(as_u64(b)));
+    return as_pair(d);
+}
+__device__ __forceinline__ Pair ex2(Pair a) { return Pair{ex2(a.x), ex2(a.y)}; }
+
+// largest over the warp (NaN left out), by one reduction of integers that are ordered as the values are
+__device__ __forceinline__ float warp_largest(float v) {
+    const int i = __float_as_int(fmaxf(v, -INFINITY));
+    const int m = __reduce_max_sync(0xffffffffu, i ^ ((i >> 31) & 0x7fffffff));
+    return __int_as_float(m ^ ((m >> 31) & 0x7fffffff));
+}
+
 // ---------------------------------------------------------------- a row as 16-byte vectors
 // Vector 0 is the aligned one that holds the row's first entry; `lead` entries of it lie in front of the row, and the last
 // one may reach behind the row.  Those two are put together from single entries, so that nothing outside the row is read.
@@ -57,18 +88,28 @@ struct Row {
             else x[e] = (e & 1) ? bf16hi(w[e >> 1]) : bf16lo(w[e >> 1]);
         }
     }
+    // the vector's entries two by two
+    static __device__ __forceinline__ void pairs(const uint4& r, Pair (&x)[kE / 2]) {
+        float f[kE];
+        unpack(r, f);
+#pragma unroll
+        for (int e = 0; e < kE / 2; ++e) x[e] = Pair{f[2 * e], f[2 * e + 1]};
+    }
+    // largest entry of a vector and `m` (NaN left out)
+    static __device__ __forceinline__ float largest(const uint4& r, float m) {
+        if constexpr (sizeof(T) == 4) {
+            return fmaxf(fmaxf(fmaxf(__uint_as_float(r.x), __uint_as_float(r.y)), fmaxf(__uint_as_float(r.z), __uint_as_float(r.w))), m);
+        } else {
+            const auto h = [](uint32_t w) { return *reinterpret_cast<const __nv_bfloat162*>(&w); };
+            const __nv_bfloat162 t = __hmax2(__hmax2(h(r.x), h(r.y)), __hmax2(h(r.z), h(r.w)));
+            return fmaxf(fmaxf(__low2float(t), __high2float(t)), m);
+        }
+    }
     __device__ __forceinline__ float at(int v) const {
         if constexpr (sizeof(T) == 4) return __ldcg(reinterpret_cast<const float*>(p) + v);
         else return __uint_as_float((uint32_t)__ldcg(reinterpret_cast<const unsigned short*>(p) + v) << 16);
     }
 };
-
-// 2^x, to about 2^-22 of it
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 
 // ---------------------------------------------------------------- masses
 // mass(x) = 2^(x c - ref) with c = inv_temp log2 e and a whole number ref, in 64 bits: which token a uniform number falls on, and
