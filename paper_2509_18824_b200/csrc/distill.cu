@@ -1,151 +1,71 @@
 // The draft's training loss on rows of logits [M][V] and its gradient (sd_distill_loss, sd_distill_grad).
 //
-// Memory-bound: a row is read once and, with the gradient, written once.  For that a cluster of CTAs holds the whole row in its
-// shared memory (bulk copies; 152064 bf16 are eight slices of 38 KB, five of which share an SM at different stages), so that
-// the gradient, which needs the row's sums, is formed from there.  One exchange between the CTAs: largest logit, sums, and the
-// entries' part of the loss.  Which entries of a slice the target lists is a bitmap, one byte of which goes with each vector; their
-// gradients (and the label's) are written over the others' afterwards, by one thread each.
+// Memory-bound: a row is read once and, with the gradient, written once.  Persistent clusters of `parts` CTAs take a row at a time,
+// each CTA a slice of it, in pieces of 28 KB through a ring of slots.  Fourteen warps sum up the exponentials of a piece; what a row
+// needs but once is done by four more, so that it does not stand in their way:
+//   copy     issues the pieces' copies as slots become free
+//   entries  prepares the next row's list: probabilities, places in the slice
+//   pick     takes the listed logits (and the label's) out of a piece that has arrived and puts minus infinity in their place: the others'
+//            sums are then those of the rest, without a question per entry (and without the cancellation of a difference)
+//   join     brings the warps' sums together, and with stores that report to a barrier the CTAs', and writes the losses
+// With the gradient a slice's pieces stay in their slots until the sums are known, the gradient is formed from there, and the next
+// row's pieces follow into the slots one by one; the listed entries' gradients (and the label's) are written over the others' afterwards.
+// (One row per cluster, all warps doing everything, a bitmap of the listed entries: 4096 rows of 152064 bf16 790 us.)
+#include <type_traits>
 #include "rows.cuh"
 
 namespace sdv {
 namespace rows {
 
-constexpr int kDistillThreads = 256;
-constexpr int kDistillWarps = kDistillThreads / 32;
-constexpr int kPieces = 4;             // copies of a slice, each with a barrier of its own
+constexpr int kSumWarps = 14;
+constexpr int kSumThreads = kSumWarps * 32;
+constexpr int kDistillThreads = kSumThreads + 128;
+enum { kCopyWarp = kSumWarps, kEntryWarp, kPickWarp, kJoinWarp };
+constexpr int kPieceVecs = 4 * kSumThreads;                // vectors of a piece: four per thread
+constexpr int kMaxSlots = 6;           // of 28 KB
+enum { kLoss, kLossGrad, kGrad };      // what a launch computes
 
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar, uint64_t policy) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;"
                  ::"r"(sm100::smem_u32(dst)), "l"(src), "r"(bytes), "r"(sm100::smem_u32(bar)), "l"(policy) : "memory");
 }
+// barrier of the fourteen warps, with the disjunction of what they bring
+__device__ __forceinline__ bool sum_warps_or(bool v) {
+    uint32_t r;
+    asm volatile("{\n .reg .pred p, q;\n setp.ne.b32 p, %1, 0;\n barrier.cta.red.or.pred q, 1, %2, p;\n selp.u32 %0, 1, 0, q;\n}\n"
+                 : "=r"(r) : "r"((uint32_t)v), "n"(kSumThreads) : "memory");
+    return r != 0;
+}
 
 // Exponentials are taken as 2^(x c - R) with R = rint(top c), a whole number: x c - R is one instruction with one rounding (of a small
 // number where it matters), and sums with different R are brought together exactly.
-//
-// What the CTAs of a row tell each other: for each warp its largest logit and, with its R, the sums of 2^(x c - R) outside
-// and among the entries and of 2^(x log2 e - R); and the CTA's part of sum p (log p - z inv_temp), and the label's logit where
-// it lies in its slice.
-struct Published {
-    float4 warp[kDistillWarps];
-    double entries;
-    float label;
-};
-
-// The row's factors: largest logit, and what an exponential is multiplied with at the entries, elsewhere, and for the cross-entropy
-struct RowFactors { float top, listed, tail, one, label_z; };
-
-struct DistillShared {
-    uint64_t bar[kPieces];
-    int abort_flag, dup, label_listed, any;
-    float wf[kDistillWarps];
-    double wd[kDistillWarps];
-    double we[kDistillWarps];
-    Published pub;
-    RowFactors row;
-};
-
-__device__ __forceinline__ double block_add(DistillShared& sh, double v) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    v = warp_add(v);
-    __syncthreads();
-    if (lane == 0) sh.wd[warp] = v;
-    __syncthreads();
-    v = 0.0;
-#pragma unroll
-    for (int w = 0; w < kDistillWarps; ++w) v += sh.wd[w];
-    return v;
-}
-__device__ __forceinline__ float block_max(DistillShared& sh, float v) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    v = warp_largest(v);
-    __syncthreads();
-    if (lane == 0) sh.wf[warp] = v;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kDistillWarps; ++w) v = fmaxf(v, sh.wf[w]);
-    return v;
-}
-
 __device__ __forceinline__ float whole_power(float top, float c) { return top > -INFINITY ? rintf(top * c) : 0.f; }
 
-// The target's entries of one row as the kernels keep them in shared memory: probability and place in this CTA's slice (entries
-// from the slice's first one on; -1: elsewhere, or no entry), and the slice's bitmap.
-struct Entries {
-    double* p;
-    int* at;
-    uint32_t* bits;
-    double log_norm;                   // log p = t inv_temp - log_norm
-};
-// `first`: index in the row of the slice's first entry (negative where the row starts inside vector 0); `count`: entries of the slice.
-// Leaves the warps' sums of p in sh.wd; the caller's barrier settles everything but log_norm.
-__device__ __forceinline__ void load_entries(DistillShared& sh, Entries& en, const DistillCall& a, long long r, int first, int count, bool report) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const float* val = a.top_val + r * a.K;
-    const int32_t* idx = a.top_idx + r * a.K;
-    const int label = a.label ? __ldg(a.label + r) : -1;
-    int i0 = -1;                                                                   // the thread's first entry (most calls have no more)
-    float t0 = 0.f;
-    if (tid < a.K) { i0 = __ldg(idx + tid); t0 = __ldg(val + tid); }
-    if (a.top_lse) en.log_norm = (double)__ldg(a.top_lse + r);
-    const int words = (count + 31) / 32;
-    for (int i = tid; i < words; i += kDistillThreads) en.bits[i] = 0;
-    if (tid == 0) { sh.dup = 0; sh.label_listed = 0; sh.any = 0; }
-    __syncthreads();
-    if (!a.top_lse) {                                                              // the entries' own soft-max
-        float top = -INFINITY;
-        for (int k = tid; k < a.K; k += kDistillThreads) {
-            const int i = k == tid ? i0 : __ldg(idx + k);
-            if (i >= 0 && i < a.V) top = fmaxf(top, k == tid ? t0 : __ldg(val + k));
-        }
-        top = block_max(sh, top);
-        double norm = 0.0;
-        for (int k = tid; k < a.K; k += kDistillThreads) {
-            const int i = k == tid ? i0 : __ldg(idx + k);
-            if (i >= 0 && i < a.V) norm += exp(((double)(k == tid ? t0 : __ldg(val + k)) - (double)top) * (double)a.inv_temp);
-        }
-        norm = block_add(sh, norm);
-        en.log_norm = (double)top * (double)a.inv_temp + log(norm);
-        __syncthreads();                                                           // (sh.wd is written again below)
-    }
-    double mass = 0.0;
-    if (warp * 32 < a.K) {
-        for (int k = tid; k < a.K; k += kDistillThreads) {
-            const int i = k == tid ? i0 : __ldg(idx + k), at = i - first;
-            const bool there = i >= 0 && i < a.V, here = there && at >= 0 && at < count;
-            const double p = there ? exp((double)(k == tid ? t0 : __ldg(val + k)) * (double)a.inv_temp - en.log_norm) : 0.0;
-            mass += p;
-            en.p[k] = p;
-            en.at[k] = here ? at : -1;
-            if (there) sh.any = 1;
-            if (i >= a.V && report) set_status(a.status, SD_ERR_BOUNDS);
-            if (here) {
-                if (i == label) sh.label_listed = 1;
-                const uint32_t bit = 1u << (at & 31);
-                if (atomicOr(&en.bits[at >> 5], bit) & bit) sh.dup = 1;
-            }
-        }
-        __syncwarp();
-        mass = warp_add(mass);
-    }
-    if (lane == 0) sh.wd[warp] = mass;
-}
+// What a CTA tells the others of its row: its largest logit and, with its R, the sums of 2^(x c - R) outside and among the
+// entries and of 2^(x log2 e - R1); its part of sum p z; the label's logit where it lies in its slice.
+struct __align__(16) Message { float top, label, rest, listed, sum1, pad; double entries; };
+static_assert(sizeof(Message) == 32, "two stores of 16 bytes");
 
-// Gradient factors of a row, with dloss and the weights: an entry x outside the list gets tail * 2^(x c - R) + one *
-// 2^(x log2 e - R1), at temperature 1 in one term.
-struct Factors {
-    float top_c, top_e, c;             // R, R1
-    float listed, tail, one;           // `listed` stands for `tail` at the listed entries
-    float per_p, per_label;            // what a listed entry's p, and the label, take away
-    bool two;
-    __device__ __forceinline__ float plain(float x) const {
-        const float e = ex2(fmaf(x, c, -top_c));
-        return two ? fmaf(one, ex2(fmaf(x, kLog2e, -top_e)), tail * e) : tail * e;
-    }
-    __device__ __forceinline__ float entry(float x) const {
-        const float e = ex2(fmaf(x, c, -top_c));
-        return two ? fmaf(one, ex2(fmaf(x, kLog2e, -top_e)), listed * e) : listed * e;
-    }
+struct RowInfo {                       // prepared ahead
+    double mass, plogp;                // sums of p and p log p
+    float weight;                      // dloss
+    int label, any;
 };
+struct RowFactors { float top, listed, tail, one; };           // what an exponential is multiplied with at the entries, elsewhere, for the cross-entropy
+
+struct DistillShared {
+    uint64_t full[kMaxSlots], picked[kMaxSlots], free_[kMaxSlots];
+    uint64_t info_full[2], info_free[2], sums_full[2], row_ready[2], told[2];
+    int abort_flag;
+    RowInfo info[2];
+    float4 sums[2][kSumWarps + 1];     // the warps' (largest logit, sum outside the entries, 0, sum at temperature 1); the listed entries'
+    double part[2];                    // sum of p z
+    float label_z[2];
+    int dup[2], label_listed[2];
+    Message msg[2][8];
+    RowFactors row[2];
+};
+
 template <typename T>
 __device__ __forceinline__ void store_one(void* row, long long v, float g) {
     if constexpr (sizeof(T) == 4) static_cast<float*>(row)[v] = g;
@@ -167,300 +87,564 @@ __device__ __forceinline__ uint4 pack(const float (&g)[Row<T>::kE]) {
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// The gradient of vectors [v0, v1) of a row.  load(i): vector i; at(j): entry j of the slice; listed_at(k, j): the same for the list's
-// k-th entry, and label_z the label's logit, as they were before anything was written (the gradient may take the logits' place)
-template <typename T, typename L, typename A, typename B>
-__device__ __forceinline__ void write_gradient(DistillShared& sh, const DistillCall& a, const Entries& en, const Row<T>& row, long long r, int v0, int v1,
-                                               const Factors& f, bool zero, L load, A at, B listed_at, float label_z) {
-    constexpr int E = Row<T>::kE;
-    const int tid = threadIdx.x;
-    T* grad = static_cast<T*>(a.grad) + r * a.grad_ld;
-    const int first = v0 * E - row.lead;
-    if (((reinterpret_cast<uintptr_t>(grad) ^ reinterpret_cast<uintptr_t>(row.p)) & 15) == 0) {
-        uint4* out = reinterpret_cast<uint4*>(reinterpret_cast<uintptr_t>(grad) & ~(uintptr_t)15);
-#pragma unroll 4
-        for (int i = v0 + tid; i < v1; i += kDistillThreads) {
-            float g[E];
-            if (zero) {
-#pragma unroll
-                for (int e = 0; e < E; ++e) g[e] = 0.f;
-            } else {
-                Pair x[E / 2];
-                Row<T>::pairs(load(i), x);
-#pragma unroll
-                for (int e = 0; e < E / 2; ++e) {
-                    const Pair w = ex2(fma2(x[e], Pair{f.c, f.c}, Pair{-f.top_c, -f.top_c}));
-                    Pair o{f.tail * w.x, f.tail * w.y};
-                    if (f.two) o = fma2(Pair{f.one, f.one}, ex2(fma2(x[e], Pair{kLog2e, kLog2e}, Pair{-f.top_e, -f.top_e})), o);
-                    g[2 * e] = o.x;
-                    g[2 * e + 1] = o.y;
-                }
-            }
-            if (i >= row.full0 && i < row.full1) out[i] = pack<T>(g);
-            else
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const int v = i * E + e - row.lead;
-                    if (v >= 0 && v < a.V) store_one<T>(grad, v, g[e]);
-                }
-        }
-    } else {                                                                       // rows that start at different places in their 16 bytes
-        const int lo = max(0, first), hi = min(a.V, v1 * E - row.lead);
-        for (int v = lo + tid; v < hi; v += kDistillThreads) store_one<T>(grad, v, zero ? 0.f : f.plain(at(v - first)));
-    }
-    if (zero) return;
-    __syncthreads();                                                               // over what has just been written
-    const int label = a.label ? a.label[r] : -1;
-    for (int k = tid; k < a.K; k += kDistillThreads) {
-        const int j = en.at[k];
-        if (j < 0) continue;
-        double p = en.p[k];
-        if (sh.dup) {                                                              // the same index twice somewhere: all of its masses
-            p = 0.0;
-            for (int q = 0; q < a.K; ++q) p += en.at[q] == j ? en.p[q] : 0.0;
-        }
-        float g = f.entry(listed_at(k, j)) - f.per_p * (float)p;
-        if (j + first == label) g -= f.per_label;
-        store_one<T>(grad, j + first, g);
-    }
-    if (tid == 0 && label >= 0 && label < a.V && !sh.label_listed) {
-        const int j = label - first;
-        if (j >= 0 && j < (v1 - v0) * E) store_one<T>(grad, label, f.plain(label_z) - f.per_label);
-    }
-}
 
-__device__ __forceinline__ Factors factors_of(const DistillCall& a, float g, bool has_label, float top, float listed, float tail, float one) {
-    Factors f;
-    f.c = a.inv_temp * kLog2e;
-    f.top_c = whole_power(top, f.c);
-    f.top_e = whole_power(top, kLog2e);
-    f.per_p = g * a.kl_weight * a.inv_temp;
-    f.listed = f.per_p * listed;
-    f.tail = f.per_p * tail;
-    f.per_label = has_label ? g * a.ce_weight : 0.f;
-    f.one = f.per_label != 0.f ? f.per_label * one : 0.f;
-    f.two = a.inv_temp != 1.f && f.one != 0.f;
-    if (!f.two) { f.listed += f.one; f.tail += f.one; }
-    return f;
-}
+// Gradient factors of a row, with dloss and the weights: an entry x outside the list gets tail * 2^(x c - R) + one *
+// 2^(x log2 e - R1), at temperature 1 in one term.
+struct Factors {
+    float r_c, r_e, c;                 // R, R1
+    float listed, tail, one;           // `listed` stands for `tail` at the listed entries
+    float per_p, per_label;            // what a listed entry's p, and the label, take away
+    bool two;
+    __device__ __forceinline__ Factors(const DistillCall& a, const RowFactors& rf, float g, bool has_label) {
+        c = a.inv_temp * kLog2e;
+        r_c = whole_power(rf.top, c);
+        r_e = whole_power(rf.top, kLog2e);
+        per_p = g * a.kl_weight * a.inv_temp;
+        listed = per_p * rf.listed;
+        tail = per_p * rf.tail;
+        per_label = has_label ? g * a.ce_weight : 0.f;
+        one = per_label != 0.f ? per_label * rf.one : 0.f;
+        two = a.inv_temp != 1.f && one != 0.f;
+        if (!two) { listed += one; tail += one; }
+    }
+    __device__ __forceinline__ float at(float x, float factor) const {
+        const float e = factor * ex2(fmaf(x, c, -r_c));
+        return two ? fmaf(one, ex2(fmaf(x, kLog2e, -r_e)), e) : e;
+    }
+    template <typename T, bool TWO>
+    __device__ __forceinline__ void vector(const uint4& raw, float (&g)[Row<T>::kE]) const {
+        Pair x[Row<T>::kE / 2];
+        Row<T>::pairs(raw, x);
+#pragma unroll
+        for (int e = 0; e < Row<T>::kE / 2; ++e) {
+            const Pair w = ex2(fma2(x[e], Pair{c, c}, Pair{-r_c, -r_c}));
+            Pair o{tail * w.x, tail * w.y};
+            if constexpr (TWO) o = fma2(Pair{one, one}, ex2(fma2(x[e], Pair{kLog2e, kLog2e}, Pair{-r_e, -r_e})), o);
+            g[2 * e] = o.x;
+            g[2 * e + 1] = o.y;
+        }
+    }
+};
 
+// One row's slice as a CTA sees it
 template <typename T>
-__global__ void __launch_bounds__(kDistillThreads)
-distill_loss_kernel(DistillCall a, int parts, int per, int withheld, long long wait_cycles) {
+struct SliceOf {
+    static constexpr int E = Row<T>::kE;
+    Row<T> row;
+    int v0, v1, first, pieces;         // vectors [v0, v1); index in the row of the first one's first entry (negative where the row starts inside it)
+    __device__ __forceinline__ SliceOf(const DistillCall& a, long long r, int rank, int per) : row(a.logits, a.ld, r, a.V) {
+        v0 = min(row.nvec, rank * per);
+        v1 = min(row.nvec, v0 + per);
+        first = v0 * E - row.lead;
+        pieces = (v1 - v0 + kPieceVecs - 1) / kPieceVecs;
+    }
+};
+
+// Lists of one row in shared memory: probabilities, logits, places in the slice (-1: elsewhere, or no entry; with kAgain: a place that
+// another entry of the list has too, and answers for)
+constexpr int kAgain = 1 << 30;
+struct Lists { double* p; float* z; int* at; };
+
+// By one warp: the entries of row r.
+template <typename T>
+__device__ __forceinline__ void prepare_entries(RowInfo& info, const Lists& li, const DistillCall& a, long long r, const SliceOf<T>& sl, bool report) {
+    const int lane = threadIdx.x & 31;
+    const float* val = a.top_val + r * a.K;
+    const int32_t* idx = a.top_idx + r * a.K;
+    const int count = (sl.v1 - sl.v0) * SliceOf<T>::E;
+    const int label = a.label ? __ldcg(a.label + r) : -1;
+    const float weight = a.dloss ? __ldcg(a.dloss + r) : 1.f;
+    const float t_lse = a.top_lse ? __ldcg(a.top_lse + r) : 0.f;
+    double log_norm = (double)t_lse;
+    if (!a.top_lse) {                                                              // the entries' own soft-max
+        float top = -INFINITY;
+        for (int k = lane; k < a.K; k += 32) {
+            const int i = __ldcg(idx + k);
+            if (i >= 0 && i < a.V) top = fmaxf(top, __ldcg(val + k));
+        }
+        top = warp_largest(top);
+        double norm = 0.0;
+        for (int k = lane; k < a.K; k += 32) {
+            const int i = __ldcg(idx + k);
+            if (i >= 0 && i < a.V) norm += exp(((double)__ldcg(val + k) - (double)top) * (double)a.inv_temp);
+        }
+        norm = warp_add(norm);
+        log_norm = (double)top * (double)a.inv_temp + log(norm);
+    }
+    double mass = 0.0, plogp = 0.0;
+    bool any = false;
+    for (int k = lane; k < a.K; k += 32) {
+        const int i = __ldcg(idx + k), at = i - sl.first;
+        const bool there = i >= 0 && i < a.V, here = there && at >= 0 && at < count;
+        const double log_p = there ? (double)__ldcg(val + k) * (double)a.inv_temp - log_norm : -INFINITY, p = exp(log_p);
+        mass += p;
+        if (p != 0.0) plogp += p * log_p;
+        li.p[k] = p;
+        li.at[k] = here ? at : -1;
+        any = any || there;
+        if (i >= a.V && report) set_status(a.status, SD_ERR_BOUNDS);
+    }
+    mass = warp_add(mass);
+    plogp = warp_add(plogp);
+    any = __any_sync(0xffffffffu, any);
+    if (lane == 0) info = RowInfo{mass, plogp, weight, label, any};
+    __syncwarp();
+}
+
+template <typename T, int MODE>
+__global__ void __launch_bounds__(kDistillThreads, 2)
+distill_kernel(DistillCall a, long long units, int parts, int per, int slots, int withheld, long long wait_cycles) {
     using namespace sm100;
+    using Sl = SliceOf<T>;
     constexpr int E = Row<T>::kE;
-    extern __shared__ __align__(16) uint4 slice[];
+    using Number = std::conditional_t<sizeof(T) == 4, uint32_t, uint16_t>;
+    extern __shared__ __align__(16) uint4 ring[];
     __shared__ DistillShared sh;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     if (tid == 0) {
         sh.abort_flag = 0;
-        for (int q = 0; q < kPieces; ++q) mbar_init(&sh.bar[q], 1);
+        for (int q = 0; q < slots; ++q) { mbar_init(&sh.full[q], 1); mbar_init(&sh.picked[q], 1); mbar_init(&sh.free_[q], kSumWarps); }
+        for (int q = 0; q < 2; ++q) { mbar_init(&sh.info_full[q], 1); mbar_init(&sh.info_free[q], kSumWarps + 1 + (MODE != kGrad)); mbar_init(&sh.told[q], 1); }
+        for (int q = 0; q < 2; ++q) { mbar_init(&sh.sums_full[q], MODE == kGrad ? 1 : kSumWarps + 1); mbar_init(&sh.row_ready[q], 1); }
         fence_barrier_init();
     }
-    __syncthreads();
+    const bool talk = MODE != kGrad && parts > 1;                                  // CTAs of a cluster share a row (else every unit is its own)
+    const int rank = talk ? (int)cluster_ctarank() : 0;
+    if (talk) sync_parts(parts); else __syncthreads();
     begin_dependent(a.logits, a.top_val, a.top_idx, a.top_lse, a.label, a.kl, a.ce, a.stats, a.dloss, a.grad, a.status);
-    const long long r = blockIdx.x / parts;
-    const int rank = parts == 1 ? 0 : (int)cluster_ctarank();
-    const Row<T> row(a.logits, a.ld, r, a.V);
-    const int v0 = min(row.nvec, rank * per), v1 = min(row.nvec, v0 + per);
-    // (a piece is whole rounds of the threads: a warp then sums up the vectors of which it has taken the largest entry)
-    const int piece = (per + kPieces * kDistillThreads - 1) / (kPieces * kDistillThreads) * kDistillThreads;
-    if (tid == 0) {
-        const uint64_t pol = policy_evict_first();
-        for (int q = 0; q < kPieces; ++q) {
-            const int i0 = max(row.full0, min(v1, v0 + q * piece)), i1 = min(row.full1, min(v1, v0 + (q + 1) * piece));
-            const uint32_t bytes = i1 > i0 ? (uint32_t)(i1 - i0) * 16 : 0;
-            mbar_arrive_expect_tx(&sh.bar[q], bytes + withheld);
-            if (bytes) bulk_load(slice + (i0 - v0), row.vec + i0, bytes, &sh.bar[q], pol);
-        }
-    }
-    if (tid == 32 && row.full0 > 0 && v0 == 0 && v1 > 0) slice[0] = row.edge(0);
-    if (tid == 64 && row.nvec - 1 >= max(row.full0, row.full1) && row.nvec - 1 >= v0 && row.nvec - 1 < v1) slice[row.nvec - 1 - v0] = row.edge(row.nvec - 1);
-
-    Entries en;
-    en.p = reinterpret_cast<double*>(slice + per);
-    en.at = reinterpret_cast<int*>(en.p + a.K);
-    en.bits = reinterpret_cast<uint32_t*>(en.at + a.K);
-    const int first = v0 * E - row.lead;
-    load_entries(sh, en, a, r, first, (v1 - v0) * E, rank == 0);
-
-    __syncthreads();
-    // ---- largest logit of the warp's vectors, as they come in
-    const float c = a.inv_temp * kLog2e;
-    float top = -INFINITY;
-    bool ok = true;
-    for (int q = 0; q < kPieces; ++q) {
-        ok = mbar_wait(&sh.bar[q], 0, &sh.abort_flag, wait_cycles) && ok;
-        const int i1 = min(v1, v0 + (q + 1) * piece);
-        for (int i = v0 + q * piece + tid; i < i1; i += kDistillThreads) top = Row<T>::largest(slice[i - v0], top);
-    }
-    top = warp_largest(top);
-    // ---- sums relative to it
-    const int label = a.label ? __ldg(a.label + r) : -1;
-    const bool has_label = label >= 0 && label < a.V;
-    const bool two = has_label && a.inv_temp != 1.f, rest_too = a.top_lse != nullptr;
-    const float r_c = whole_power(top, c), r_e = whole_power(top, kLog2e);
-    const Pair c2{c, c}, from_c{-r_c, -r_c}, e2{kLog2e, kLog2e}, from_e{-r_e, -r_e};
-    Pair s{0.f, 0.f}, t{0.f, 0.f}, s1{0.f, 0.f};
-    float s_listed = 0.f;
-    const uint8_t* bytes = reinterpret_cast<const uint8_t*>(en.bits);
-#pragma unroll 2
-    for (int j = tid; j < v1 - v0; j += kDistillThreads) {
-        Pair x[E / 2], w[E / 2];
-        Row<T>::pairs(slice[j], x);
-        const uint32_t mask = E == 8 ? bytes[j] : (bytes[j >> 1] >> ((j & 1) * 4)) & 15u;
-        if (two) {
-#pragma unroll
-            for (int e = 0; e < E / 2; ++e) s1 = add2(s1, ex2(fma2(x[e], e2, from_e)));
-        }
-#pragma unroll
-        for (int e = 0; e < E / 2; ++e) w[e] = ex2(fma2(x[e], c2, from_c));
-        if (mask != 0 && rest_too) {
-#pragma unroll
-            for (int e = 0; e < E / 2; ++e) {
-                if (mask >> (2 * e) & 1) { s_listed += w[e].x; w[e].x = 0.f; }
-                if (mask >> (2 * e + 1) & 1) { s_listed += w[e].y; w[e].y = 0.f; }
-            }
-        }
-#pragma unroll
-        for (int e = 0; e < E / 2; e += 2) { s = add2(s, w[e]); t = add2(t, w[e + 1]); }
-    }
-    const T* entries = reinterpret_cast<const T*>(slice);
-    const auto at = [&](int j) {
-        if constexpr (sizeof(T) == 4) return (float)entries[j];
-        else return __uint_as_float((uint32_t)entries[j] << 16);
+    // units: rows for a cluster; slices where every CTA stands alone
+    const long long step = talk ? gridDim.x / parts : gridDim.x, start = talk ? blockIdx.x / parts : blockIdx.x;
+    const auto row_of = [&](long long u) { return MODE == kGrad ? u / parts : u; };
+    const auto rank_of = [&](long long u) { return MODE == kGrad ? (int)(u % parts) : rank; };
+    const auto lists_of = [&](int b) {
+        Lists li;
+        double* base = reinterpret_cast<double*>(ring + slots * kPieceVecs);
+        li.p = base + b * a.K;
+        base += 2 * a.K;
+        li.at = reinterpret_cast<int*>(base) + b * a.K;
+        li.z = reinterpret_cast<float*>(base + a.K) + b * a.K;
+        return li;
     };
-    double part = 0.0;
-    if (warp * 32 < a.K) {
-        for (int k = tid; k < a.K; k += kDistillThreads) {
-            const int j = en.at[k];
-            const double p = en.p[k];
-            if (j >= 0 && p != 0.0) part += p * ((double)__ldg(a.top_val + r * a.K + k) * (double)a.inv_temp - en.log_norm - (double)at(j) * (double)a.inv_temp);
-        }
-        __syncwarp();
-        part = warp_add(part);
-    }
-    {
-        const float rest = warp_add((s.x + s.y) + (t.x + t.y)), listed = rest_too ? warp_add(s_listed) : 0.f, sum1 = two ? warp_add(s1.x + s1.y) : 0.f;
-        if (lane == 0) { sh.pub.warp[warp] = make_float4(top, rest, listed, sum1); sh.we[warp] = part; }
-    }
-    __syncthreads();
-    if (tid == 0) {
-        const int j = label - first;
-        double all = 0.0;
-#pragma unroll
-        for (int w = 0; w < kDistillWarps; ++w) all += sh.we[w];
-        sh.pub.entries = all;
-        sh.pub.label = has_label && j >= 0 && j < (v1 - v0) * E ? at(j) : 0.f;
-    }
-    sync_parts(parts);
+    bool ok = true;
 
-    // ---- the row's: one warp brings the parts together
-    if (warp == 0) {
-        float4 w[2];
-        float most = -INFINITY;
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            const int i = lane + q * 32, rk = i / kDistillWarps;
-            w[q] = rk < parts ? *of_rank(&sh.pub.warp[i % kDistillWarps], rk) : make_float4(-INFINITY, 0.f, 0.f, 0.f);
-            most = fmaxf(most, w[q].x);
+    if (warp == kEntryWarp) {
+        long long n = 0;
+        for (long long u = start; u < units; u += step, ++n) {
+            const int b = (int)(n & 1);
+            ok = mbar_wait_warp(&sh.info_free[b], (uint32_t)((n >> 1) & 1) ^ 1u, &sh.abort_flag, wait_cycles);
+            if (!ok) break;
+            const Sl sl(a, row_of(u), rank_of(u), per);
+            prepare_entries<T>(sh.info[b], lists_of(b), a, row_of(u), sl, rank_of(u) == 0);
+            if (lane == 0) mbar_arrive(&sh.info_full[b]);
         }
-        double entries_part = lane < parts ? *of_rank(&sh.pub.entries, lane) : 0.0;
-        float z_label = lane < parts ? *of_rank(&sh.pub.label, lane) : 0.f;
-        double mass = lane < kDistillWarps ? sh.wd[lane] : 0.0;
-        most = warp_largest(most);
-        const float r_row = whole_power(most, c), r_row1 = whole_power(most, kLog2e);
-        double rest = 0.0, sum = 0.0, sum1 = 0.0;
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            const bool some = w[q].x > -INFINITY;
-            const double f = some ? times_pow2(1.0, (int)fmaxf(whole_power(w[q].x, c) - r_row, -2000.f)) : 1.0;
-            rest += (double)w[q].y * f;
-            sum += ((double)w[q].y + (double)w[q].z) * f;
-            if (two) sum1 += (double)w[q].w * (some ? times_pow2(1.0, (int)fmaxf(whole_power(w[q].x, kLog2e) - r_row1, -2000.f)) : 1.0);
-        }
-        rest = warp_add(rest);
-        sum = warp_add(sum);
-        sum1 = two ? warp_add(sum1) : sum;
-        // (R belongs to the power with c as 32 bits hold it: log sum = R ln 2 + log(sum), but for top's own rounding)
-        const double lse = (double)most * (double)a.inv_temp + log(sum) - ((double)most * (double)c - (double)r_row) * 0.69314718055994530942;
-        const double lse1 = two ? (double)most + log(sum1) - ((double)most * (double)kLog2e - (double)r_row1) * 0.69314718055994530942 : lse;
-        entries_part = warp_add(entries_part);
-        mass = warp_add(mass);
-        z_label = warp_add(z_label);
-        const bool any = sh.any != 0;
-        const double p_rest = rest_too ? 1.0 - mass : 0.0, s_rest = rest / sum;
-        const bool has_rest = p_rest > 0.0 && rest > 0.0;
-        const double all_p = has_rest ? 1.0 : (any ? mass : 0.0);
-        const double tail = all_p - (has_rest ? p_rest / s_rest : 0.0);
-        if (lane == 0) {
-            sh.row = RowFactors{most, (float)(all_p / sum), (float)(tail / sum), (float)(1.0 / sum1), z_label};
-            if (rank == 0) {
-                double kl = any ? entries_part + mass * lse : 0.0;
-                if (has_rest && any) kl += p_rest * (log(p_rest) - log(s_rest));
-                a.kl[r] = (float)kl;
-                if (a.ce) a.ce[r] = has_label ? (float)(lse1 - (double)z_label) : 0.f;
-                if (a.stats) reinterpret_cast<float4*>(a.stats)[r] = make_float4(sh.row.top, sh.row.listed, sh.row.tail, sh.row.one);
-                if (label >= a.V) set_status(a.status, SD_ERR_BOUNDS);
+    } else if (warp == kCopyWarp) {
+        const uint64_t pol = policy_evict_first();
+        long long cnt = 0;
+        for (long long u = start; u < units && ok; u += step) {
+            const Sl sl(a, row_of(u), rank_of(u), per);
+            int slot = (int)(cnt % slots);
+            for (int q = 0; q < sl.pieces && ok; ++q, ++cnt) {
+                ok = mbar_wait_warp(&sh.free_[slot], (uint32_t)((cnt / slots) & 1) ^ 1u, &sh.abort_flag, wait_cycles);
+                if (!ok) break;
+                uint4* dst = ring + slot * kPieceVecs;
+                const int a0 = sl.v0 + q * kPieceVecs, a1 = min(sl.v1, a0 + kPieceVecs);
+                const int i0 = max(sl.row.full0, a0), i1 = min(sl.row.full1, a1);
+                // (what lies in the slot from ordinary stores stands behind the copy that comes)
+                fence_proxy_async_smem();
+                if (lane == 1 && sl.row.full0 > 0 && a0 == 0) dst[0] = sl.row.edge(0);
+                const int e = sl.row.nvec - 1;
+                if (lane == 2 && e >= max(sl.row.full0, sl.row.full1) && e >= a0 && e < a1) dst[e - a0] = sl.row.edge(e);
+                __syncwarp();
+                if (lane == 0) {
+                    const uint32_t bytes = i1 > i0 ? (uint32_t)(i1 - i0) * 16 : 0;
+                    mbar_arrive_expect_tx(&sh.full[slot], bytes + withheld);
+                    if (bytes) bulk_load(dst + (i0 - a0), sl.row.vec + i0, bytes, &sh.full[slot], pol);
+                }
+                __syncwarp();
+                if (++slot == slots) slot = 0;
             }
         }
+    } else if (warp == kPickWarp) {
+        const float c = a.inv_temp * kLog2e;
+        const bool rest_too = a.top_lse != nullptr;
+        long long cnt = 0, n = 0;
+        for (long long u = start; u < units && ok; u += step, ++n) {
+            const int b = (int)(n & 1);
+            const Sl sl(a, row_of(u), rank_of(u), per);
+            const Lists li = lists_of(b);
+            ok = mbar_wait_warp(&sh.info_full[b], (uint32_t)((n >> 1) & 1), &sh.abort_flag, wait_cycles);
+            const int label = sh.info[b].label, lj = label - sl.first;
+            const bool has_label = label >= 0 && label < a.V;
+            float label_z = 0.f;
+            double part = 0.0;
+            bool dup = false, label_listed = false;
+            int slot = (int)(cnt % slots);
+            for (int q = 0; q < sl.pieces && ok; ++q, ++cnt) {
+                ok = mbar_wait_warp(&sh.full[slot], (uint32_t)((cnt / slots) & 1), &sh.abort_flag, wait_cycles);
+                if (!ok) break;
+                T* entries = reinterpret_cast<T*>(ring + slot * kPieceVecs);
+                const int e0 = q * kPieceVecs * E, e1 = min(e0 + kPieceVecs * E, (sl.v1 - sl.v0) * E);
+                const auto value = [&](int j) {
+                    if constexpr (sizeof(T) == 4) return (float)entries[j - e0];
+                    else return __uint_as_float((uint32_t)entries[j - e0] << 16);
+                };
+                if (has_label && lj >= e0 && lj < e1) label_z = value(lj);
+                const auto here = [&](int k) { const int j = li.at[k]; return j >= e0 && j < e1; };
+                for (int k = lane; k < a.K; k += 32) {
+                    if (!here(k)) continue;
+                    const float z = value(li.at[k]);
+                    const double p = li.p[k];
+                    li.z[k] = z;
+                    label_listed = label_listed || li.at[k] == lj;
+                    if (p != 0.0) part += p * (double)z;
+                }
+                // the same place twice?  Every entry leaves its number there; one of them finds it again.
+                __syncwarp();
+                for (int k = lane; k < a.K; k += 32)
+                    if (here(k)) reinterpret_cast<Number*>(entries)[li.at[k] - e0] = (Number)k;
+                __syncwarp();
+                uint32_t again = 0;                                                // (K is at most 1024: a bit per round)
+                for (int k = lane; k < a.K; k += 32)
+                    if (here(k) && reinterpret_cast<Number*>(entries)[li.at[k] - e0] != (Number)k) again |= 1u << (k >> 5);
+                __syncwarp();
+                for (int k = lane; k < a.K; k += 32)
+                    if (here(k)) {
+                        const uint32_t z = __float_as_uint(MODE != kGrad && rest_too ? -INFINITY : li.z[k]);
+                        reinterpret_cast<Number*>(entries)[li.at[k] - e0] = (Number)(sizeof(T) == 4 ? z : z >> 16);
+                    }
+                __syncwarp();
+                if (again) {
+                    dup = true;
+                    for (int k = lane; k < a.K; k += 32) if (again >> (k >> 5) & 1) li.at[k] |= kAgain;
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh.picked[slot]);
+                if (++slot == slots) slot = 0;
+            }
+            if (!ok) break;
+            dup = __any_sync(0xffffffffu, dup);
+            label_listed = __any_sync(0xffffffffu, label_listed);
+            if constexpr (MODE != kGrad) {
+                // the listed entries' own sum, every index once
+                float top = -INFINITY, sum = 0.f, sum1 = 0.f;
+                if (rest_too) {
+                    const auto counts = [&](int k) { const int j = li.at[k]; return j >= 0 && j < kAgain; };
+                    for (int k = lane; k < a.K; k += 32) if (counts(k)) top = fmaxf(top, li.z[k]);
+                    top = warp_largest(top);
+                    const float r_c = whole_power(top, c), r_e = whole_power(top, kLog2e);
+                    for (int k = lane; k < a.K; k += 32)
+                        if (counts(k)) {
+                            sum += ex2(fmaf(li.z[k], c, -r_c));
+                            sum1 += ex2(fmaf(li.z[k], kLog2e, -r_e));
+                        }
+                    sum = warp_add(sum);
+                    sum1 = warp_add(sum1);
+                }
+                part = warp_add(part);
+                // (the loss alone: the sums of two rows before have been taken over)
+                ok = mbar_wait_warp(&sh.row_ready[b], (uint32_t)((n >> 1) & 1) ^ 1u, &sh.abort_flag, wait_cycles);
+                if (lane == 0) { sh.sums[b][kSumWarps] = make_float4(top, 0.f, sum, sum1); sh.part[b] = part; }
+            }
+            if (lane == 0) { sh.label_z[b] = label_z; sh.dup[b] = dup; sh.label_listed[b] = label_listed; }
+            __syncwarp();
+            if (lane == 0) { mbar_arrive(&sh.sums_full[b]); mbar_arrive(&sh.info_free[b]); }
+        }
+    } else if (warp == kJoinWarp) {
+        const float c = a.inv_temp * kLog2e;
+        const bool rest_too = a.top_lse != nullptr;
+        const auto weigh = [](float own, float all, float cc) {                    // 2^(R - the row's R)
+            return own > -INFINITY ? ex2(whole_power(own, cc) - whole_power(all, cc)) : 1.f;
+        };
+        long long n = 0;
+        if constexpr (MODE != kGrad)
+        for (long long r = start; r < units && ok; r += step, ++n) {
+            const int b = (int)(n & 1);
+            const uint32_t ph = (uint32_t)((n >> 1) & 1);
+            ok = mbar_wait_warp(&sh.info_full[b], ph, &sh.abort_flag, wait_cycles) && mbar_wait_warp(&sh.sums_full[b], ph, &sh.abort_flag, wait_cycles);
+            if (!ok) break;
+            const RowInfo& info = sh.info[b];
+            const int label = info.label;
+            const bool has_label = label >= 0 && label < a.V, two = has_label && a.inv_temp != 1.f;
+            const float4 w = lane <= kSumWarps ? sh.sums[b][lane] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+            double entries = sh.part[b];
+            float label_z = sh.label_z[b], most = warp_largest(w.x);
+            const float f = weigh(w.x, most, c);
+            float rest = warp_add(w.y * f), listed = rest_too ? warp_add(w.z * f) : 0.f, sum1 = two ? warp_add(w.w * weigh(w.x, most, kLog2e)) : 0.f;
+            if (talk) {
+                const Message mine{most, label_z, rest, listed, sum1, 0.f, entries};
+                if (lane == rank) {
+                    sh.msg[b][rank] = mine;
+                    mbar_arrive_expect_tx(&sh.told[b], (parts - 1) * (uint32_t)sizeof(Message));
+                } else if (lane < parts) {
+                    const uint32_t to = map_dsmem(smem_u32(&sh.msg[b][rank]), lane), bar = map_dsmem(smem_u32(&sh.told[b]), lane);
+                    st_async_v4(to, __float_as_uint(most), __float_as_uint(label_z), __float_as_uint(rest), __float_as_uint(listed), bar);
+                    st_async_v4(to + 16, __float_as_uint(sum1), 0u, (uint32_t)__double2loint(entries), (uint32_t)__double2hiint(entries), bar);
+                }
+                ok = mbar_wait_cluster(&sh.told[b], ph, &sh.abort_flag, wait_cycles);
+                ok = __all_sync(0xffffffffu, ok);
+                Message o{-INFINITY, 0.f, 0.f, 0.f, 0.f, 0.f, 0.0};
+                if (lane < parts) o = sh.msg[b][lane];
+                most = warp_largest(o.top);
+                const float g = weigh(o.top, most, c);
+                rest = warp_add(o.rest * g);
+                listed = rest_too ? warp_add(o.listed * g) : 0.f;
+                if (two) sum1 = warp_add(o.sum1 * weigh(o.top, most, kLog2e));
+                entries = o.entries;
+                label_z = o.label;
+            }
+            const float sum = rest + listed;
+            if (!two) sum1 = sum;
+            const double p_rest = rest_too ? 1.0 - info.mass : 0.0;
+            const bool has_rest = p_rest > 0.0 && rest > 0.f;
+            const float all_p = has_rest ? 1.f : (info.any ? (float)info.mass : 0.f);
+            // tail / sum = (all_p - p_rest / s_rest) / sum with s_rest = rest / sum
+            const float inv = 1.f / sum, tail = has_rest ? inv - (float)p_rest / rest : all_p * inv;
+            const RowFactors rf{most, all_p * inv, tail, two ? 1.f / sum1 : inv};
+            if (lane == 0) { sh.row[b] = rf; mbar_arrive(&sh.row_ready[b]); }
+            if (rank == 0) {
+                if (talk) { entries = warp_add(entries); label_z = warp_add(label_z); }
+                // lane 0: kl; lane 1: ce.  (R belongs to the power with c as 32 bits hold it: log sum = R ln 2 + log(sum), but for c's rounding)
+                const float cc = lane == 0 ? c : kLog2e;
+                const double it = lane == 0 ? (double)a.inv_temp : 1.0;
+                if (lane < 2) {
+                    const double lse = (double)most * it + log((double)(lane == 0 ? sum : sum1)) - ((double)most * (double)cc - (double)whole_power(most, cc)) * 0.69314718055994530942;
+                    if (lane == 0) {
+                        double kl = info.any ? info.plogp - entries * it + info.mass * lse : 0.0;
+                        if (has_rest && info.any) kl += p_rest * log(p_rest * (double)sum / (double)rest);
+                        a.kl[r] = (float)kl;
+                        if (a.stats) reinterpret_cast<float4*>(a.stats)[r] = make_float4(rf.top, rf.listed, rf.tail, rf.one);
+                        if (label >= a.V) set_status(a.status, SD_ERR_BOUNDS);
+                    } else if (a.ce) {
+                        a.ce[r] = has_label ? (float)(lse - (double)label_z) : 0.f;
+                    }
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh.info_free[b]);
+        }
+    } else {
+        const float c = a.inv_temp * kLog2e;
+        const Pair c2{c, c}, e2{kLog2e, kLog2e};
+        long long cnt = 0;
+        long long n = 0;
+        for (long long u = start; u < units; u += step, ++n) {
+            const int b = (int)(n & 1);
+            const long long r = row_of(u);
+            const Sl sl(a, r, rank_of(u), per);
+            const Lists li = lists_of(b);
+            ok = mbar_wait(&sh.info_full[b], (uint32_t)((n >> 1) & 1), &sh.abort_flag, wait_cycles) && ok;
+            const RowInfo& info = sh.info[b];
+            const int label = info.label;
+            const bool has_label = label >= 0 && label < a.V;
+            const bool two = MODE != kGrad && has_label && a.inv_temp != 1.f;
+            const long long cnt0 = cnt;
+            int slot = (int)(cnt % slots);
+            const int slot0 = slot;
+
+            // ---- sums of the pieces as they come in
+            float top = -INFINITY, r_c = 0.f, r_e = 0.f;                           // top: of the lane's entries; the R's are the warp's
+            Pair s{0.f, 0.f}, t{0.f, 0.f}, s1{0.f, 0.f};
+            bool begun = false;
+            for (int q = 0; MODE != kGrad && q < sl.pieces; ++q, ++cnt) {
+                ok = mbar_wait(&sh.picked[slot], (uint32_t)((cnt / slots) & 1), &sh.abort_flag, wait_cycles) && ok;
+                const uint4* src = ring + slot * kPieceVecs;
+                const int len = min(kPieceVecs, sl.v1 - sl.v0 - q * kPieceVecs);
+                uint4 raw[4];
+                float m = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int i = tid + j * kSumThreads;
+                    raw[j] = i < len ? src[i] : Row<T>::nothing();
+                    m = Row<T>::largest(raw[j], m);
+                }
+                // R is that of the first pieces' largest logit until one comes that is 2^32 times as much (exponentials of up to that
+                // size are added as exactly)
+                if (__any_sync(0xffffffffu, m > -INFINITY && (!begun || m * c - r_c > 32.f || m * kLog2e - r_e > 32.f))) {
+                    const float most = warp_largest(fmaxf(top, m));
+                    const float n_c = whole_power(most, c), n_e = whole_power(most, kLog2e);
+                    const float f = ex2(r_c - n_c), f1 = ex2(r_e - n_e);
+                    if (begun) { s = Pair{s.x * f, s.y * f}; t = Pair{t.x * f, t.y * f}; s1 = Pair{s1.x * f1, s1.y * f1}; }
+                    r_c = n_c;
+                    r_e = n_e;
+                    begun = true;
+                }
+                top = fmaxf(top, m);
+                const Pair from_c{-r_c, -r_c}, from_e{-r_e, -r_e};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    Pair x[E / 2];
+                    Row<T>::pairs(raw[j], x);
+#pragma unroll
+                    for (int e = 0; e < E / 2; e += 2) {
+                        s = add2(s, ex2(fma2(x[e], c2, from_c)));
+                        t = add2(t, ex2(fma2(x[e + 1], c2, from_c)));
+                    }
+                    if (two) {
+#pragma unroll
+                        for (int e = 0; e < E / 2; ++e) s1 = add2(s1, ex2(fma2(x[e], e2, from_e)));
+                    }
+                }
+                if (MODE == kLoss) {
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sh.free_[slot]);
+                }
+                if (++slot == slots) slot = 0;
+            }
+
+            RowFactors rf;
+            if constexpr (MODE != kGrad) {
+                // (handed on relative to the R of the largest logit: the join takes a sum's R from that)
+                const float most = warp_largest(top);
+                const float rest = warp_add((s.x + s.y) + (t.x + t.y)) * ex2(r_c - whole_power(most, c));
+                const float sum1 = two ? warp_add(s1.x + s1.y) * ex2(r_e - whole_power(most, kLog2e)) : 0.f;
+                // (the loss alone: the sums of two rows before have been taken over)
+                if (MODE == kLoss) ok = mbar_wait(&sh.row_ready[b], (uint32_t)((n >> 1) & 1) ^ 1u, &sh.abort_flag, wait_cycles) && ok;
+                if (lane == 0) sh.sums[b][warp] = make_float4(most, rest, 0.f, sum1);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh.sums_full[b]);
+                if constexpr (MODE == kLossGrad) {
+                    ok = mbar_wait(&sh.row_ready[b], (uint32_t)((n >> 1) & 1), &sh.abort_flag, wait_cycles) && ok;
+                    rf = sh.row[b];
+                }
+            } else {
+                const float4 st = __ldcg(reinterpret_cast<const float4*>(a.stats) + r);
+                rf = RowFactors{st.x, st.y, st.z, st.w};
+                if (label >= a.V && tid == 0 && rank_of(u) == 0) set_status(a.status, SD_ERR_BOUNDS);
+            }
+
+            // ---- the gradient, piece by piece
+            if constexpr (MODE != kLoss) {
+                const float weight = info.weight;
+                const bool zero = weight == 0.f;
+                const Factors f(a, rf, weight, has_label);
+                T* grad = static_cast<T*>(a.grad) + r * a.grad_ld;
+                const bool same = ((reinterpret_cast<uintptr_t>(grad) ^ reinterpret_cast<uintptr_t>(sl.row.p)) & 15) == 0;
+                uint4* out = reinterpret_cast<uint4*>(reinterpret_cast<uintptr_t>(grad) & ~(uintptr_t)15);
+                slot = slot0;
+                cnt = cnt0;
+                for (int q = 0; q < sl.pieces; ++q, ++cnt) {
+                    if (MODE == kGrad) ok = mbar_wait(&sh.picked[slot], (uint32_t)((cnt / slots) & 1), &sh.abort_flag, wait_cycles) && ok;
+                    const uint4* src = ring + slot * kPieceVecs;
+                    const int len = min(kPieceVecs, sl.v1 - sl.v0 - q * kPieceVecs), a0 = sl.v0 + q * kPieceVecs;
+                    const auto one = [&](int i, auto kind) {                       // vector i of the piece
+                        constexpr int kind_of = decltype(kind)::value;             // 0: weight 0, 1: one exponential per entry, 2: two
+                        float g[E];
+                        if constexpr (kind_of == 0) {
+#pragma unroll
+                            for (int e = 0; e < E; ++e) g[e] = 0.f;
+                        } else f.template vector<T, kind_of == 2>(src[i], g);
+                        const int v = a0 + i;
+                        if (same && v >= sl.row.full0 && v < sl.row.full1) out[v] = pack<T>(g);
+                        else
+#pragma unroll
+                            for (int e = 0; e < E; ++e) {
+                                const int at = v * E + e - sl.row.lead;
+                                if (at >= 0 && at < a.V) store_one<T>(grad, at, g[e]);
+                            }
+                    };
+                    const auto all = [&](auto kind) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const int i = tid + j * kSumThreads;
+                            if (i < len) one(i, kind);
+                        }
+                    };
+                    if (zero) all(std::integral_constant<int, 0>{});
+                    else if (f.two) all(std::integral_constant<int, 2>{});
+                    else all(std::integral_constant<int, 1>{});
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sh.free_[slot]);
+                    if (++slot == slots) slot = 0;
+                }
+                // over what has just been written
+                if (MODE == kGrad) ok = mbar_wait(&sh.sums_full[b], (uint32_t)((n >> 1) & 1), &sh.abort_flag, wait_cycles) && ok;
+                ok = !sum_warps_or(!ok);                                           // (all fourteen come here in every row, whatever they waited for)
+                if (!zero) {
+                    for (int k = tid; k < a.K; k += kSumThreads) {
+                        const int j = li.at[k];
+                        if (j < 0 || j >= kAgain) continue;
+                        double p = li.p[k];
+                        if (sh.dup[b]) {                                           // the same index twice somewhere: all of its masses
+                            p = 0.0;
+                            for (int x = 0; x < a.K; ++x) p += li.at[x] >= 0 && (li.at[x] & ~kAgain) == j ? li.p[x] : 0.0;
+                        }
+                        float g = f.at(li.z[k], f.listed) - f.per_p * (float)p;
+                        if (j + sl.first == label) g -= f.per_label;
+                        store_one<T>(grad, j + sl.first, g);
+                    }
+                    const int lj = label - sl.first;
+                    if (tid == kSumThreads - 1 && has_label && !sh.label_listed[b] && lj >= 0 && lj < (sl.v1 - sl.v0) * E)
+                        store_one<T>(grad, label, f.at(sh.label_z[b], f.tail) - f.per_label);
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh.info_free[b]);
+            if (!ok) break;
+        }
     }
+    if (!ok) set_status(a.status, SD_ERR_TIMEOUT);                                 // a copy, or another CTA's sums, did not come
     __syncwarp();
-    if (parts > 1) cluster_arrive_relaxed();                                       // this CTA has read the others' (the wait is at the end)
-    if (a.grad) {
-        const float g = a.dloss ? __ldg(a.dloss + r) : 1.f;
-        __syncthreads();
-        const RowFactors rf = sh.row;
-        const Factors f = factors_of(a, g, has_label, rf.top, rf.listed, rf.tail, rf.one);
-        write_gradient<T>(sh, a, en, row, r, v0, v1, f, g == 0.f, [&](int i) { return slice[i - v0]; }, at, [&](int, int j) { return at(j); }, rf.label_z);
-    }
-    if (parts > 1) cluster_wait_acquire();
-    if (!ok) {                                                                     // a copy did not come
-        set_status(a.status, SD_ERR_TIMEOUT);
-        unwind_pause();
-    }
+    if (talk) sync_parts(parts);                                                   // nobody leaves while another CTA may still send to it
+    if (!ok || *reinterpret_cast<volatile int*>(&sh.abort_flag)) unwind_pause();
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kDistillThreads)
-distill_grad_kernel(DistillCall a, int parts, int per) {
-    constexpr int E = Row<T>::kE;
-    extern __shared__ __align__(16) uint4 lists[];
-    __shared__ DistillShared sh;
-    begin_dependent(a.logits, a.top_val, a.top_idx, a.top_lse, a.label, a.stats, a.dloss, a.grad, a.status);
-    const long long r = blockIdx.x / parts;
-    const int part = (int)(blockIdx.x - r * parts);
-    const Row<T> row(a.logits, a.ld, r, a.V);
-    const int v0 = min(row.nvec, part * per), v1 = min(row.nvec, v0 + per);
-    const int first = v0 * E - row.lead;
-    Entries en;
-    en.p = reinterpret_cast<double*>(lists);
-    en.at = reinterpret_cast<int*>(en.p + a.K);
-    float* z = reinterpret_cast<float*>(en.at + a.K);                              // the listed logits, and the label's, read before they are overwritten
-    en.bits = reinterpret_cast<uint32_t*>(z + a.K + 1);
-    load_entries(sh, en, a, r, first, (v1 - v0) * E, part == 0);
-    __syncthreads();
-    const int label = a.label ? a.label[r] : -1;
-    const bool has_label = label >= 0 && label < a.V;
-    for (int k = threadIdx.x; k < a.K; k += kDistillThreads) z[k] = en.at[k] >= 0 ? row.at(en.at[k] + first) : 0.f;
-    if (threadIdx.x == 0) {
-        const bool here = has_label && label >= first && label < first + (v1 - v0) * E;
-        z[a.K] = here ? row.at(label) : 0.f;
-        if (label >= a.V && part == 0) set_status(a.status, SD_ERR_BOUNDS);
-    }
-    __syncthreads();
-    const float4 st = reinterpret_cast<const float4*>(a.stats)[r];
-    const float g = a.dloss ? a.dloss[r] : 1.f;
-    const Factors f = factors_of(a, g, has_label, st.x, st.y, st.z, st.w);
-    write_gradient<T>(sh, a, en, row, r, v0, v1, f, g == 0.f, [&](int i) { return row.load(i); }, [&](int j) { return row.at(j + first); },
-                      [&](int k, int) { return z[k]; }, z[a.K]);
-}
-
-// CTAs per row: slices of at most 40 KB while eight are enough for that, and more of them where the rows leave SMs idle
-static int loss_parts(int M, int nvec, int sms) {
+// CTAs per row: slices of at most three pieces where eight CTAs are enough for that, and more of them where the rows leave SMs idle
+static int distill_parts(int M, int nvec, int sms) {
     int parts = 1;
-    while (parts < 8 && ((nvec + parts - 1) / parts * 16 > 40 * 1024 || ((long long)M * parts * 2 <= sms && nvec / (parts * 2) >= kDistillThreads))) parts *= 2;
+    while (parts < 8 && ((nvec + parts - 1) / parts > 3 * kPieceVecs || ((long long)M * parts <= sms && nvec / (parts * 2) >= kSumThreads))) parts *= 2;
     return parts;
+}
+
+// Clusters of this kernel that are on the GPU at once, asked once per kind of launch.  (Which GPCs have how many SMs decides: with one cluster
+// more, its rows would begin when all the others' are done.)
+template <typename Kernel>
+static int resident_clusters(Kernel* kern, int dev, int cluster, int smem) {
+    struct Known { const void* kern; int dev, cluster, smem, n; };
+    static thread_local Known known[32];
+    static thread_local int next = 0;
+    for (const Known& k : known)
+        if (k.kern == reinterpret_cast<const void*>(kern) && k.dev == dev && k.cluster == cluster && k.smem == smem) return k.n;
+    int n = 0;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(cluster);
+    cfg.blockDim = dim3(kDistillThreads);
+    cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = cluster;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cluster > 1) {
+        if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess) return 0;
+    } else {
+        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kern, kDistillThreads, smem) != cudaSuccess) return 0;
+        n *= sm_count(dev);
+    }
+    if (n < 1) return 0;
+    known[next++ % 32] = Known{reinterpret_cast<const void*>(kern), dev, cluster, smem, n};
+    return n;
+}
+
+template <typename T, int MODE>
+static sd_status launch_distill(const DistillCall& call, int M, cudaStream_t st) {
+    const int nvec = (int)(((long long)call.V * (int)sizeof(T) + 15) / 16) + 1;                // (a row may lie across one vector more)
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return SD_ERR_CUDA;
+    const int sms = sm_count(dev), parts = distill_parts(M, nvec, sms), per = (nvec + parts - 1) / parts;
+    const int pieces = (per + kPieceVecs - 1) / kPieceVecs, slots = pieces > 3 ? pieces : 3;
+    const int smem = slots * kPieceVecs * 16 + 2 * call.K * 16;
+    auto kern = distill_kernel<T, MODE>;
+    if (slots > kMaxSlots || !allow_dynamic_smem(kern, smem)) return SD_ERR_CUDA;
+    const int cluster = MODE == kGrad ? 1 : parts;
+    const long long units = MODE == kGrad ? (long long)M * parts : M;
+    const int resident = resident_clusters(kern, dev, cluster, smem);
+    if (resident < 1) return SD_ERR_CUDA;
+    const long long clusters = units < resident ? units : resident;
+    const TestKnobs knobs = test_knobs();
+    return launch_dependent(kern, dim3((unsigned)(clusters * cluster)), kDistillThreads, smem, cluster, st, call, units, parts, per, slots,
+                            knobs.withhold ? 16 : 0, knobs.wait_cycles);
 }
 
 }  // namespace rows
@@ -468,24 +652,12 @@ static int loss_parts(int M, int nvec, int sms) {
 using namespace rows;
 
 sd_status launch_distill_loss(const DistillCall& call, int dtype, int M, cudaStream_t st) {
-    const int elem = dtype == SD_F32 ? 4 : 2, nvec = (call.V * elem + 15) / 16 + 1;            // (a row may lie across one vector more)
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return SD_ERR_CUDA;
-    const int parts = loss_parts(M, nvec, sm_count(dev)), per = (nvec + parts - 1) / parts;
-    const int smem = per * 16 + call.K * 12 + (per * (16 / elem) + 31) / 32 * 4;
-    auto kern = dtype == SD_F32 ? distill_loss_kernel<float> : distill_loss_kernel<uint16_t>;
-    if (!allow_dynamic_smem(kern, smem)) return SD_ERR_CUDA;
-    const TestKnobs knobs = test_knobs();
-    return launch_dependent(kern, dim3((unsigned)M * parts), kDistillThreads, smem, parts, st, call, parts, per, knobs.withhold ? 16 : 0, knobs.wait_cycles);
+    if (call.grad) return dtype == SD_F32 ? launch_distill<float, kLossGrad>(call, M, st) : launch_distill<uint16_t, kLossGrad>(call, M, st);
+    return dtype == SD_F32 ? launch_distill<float, kLoss>(call, M, st) : launch_distill<uint16_t, kLoss>(call, M, st);
 }
 
 sd_status launch_distill_grad(const DistillCall& call, int dtype, int M, cudaStream_t st) {
-    const int elem = dtype == SD_F32 ? 4 : 2, nvec = (call.V * elem + 15) / 16 + 1;
-    const int parts = (nvec + 2047) / 2048, per = (nvec + parts - 1) / parts;
-    const int smem = call.K * 16 + 4 + (per * (16 / elem) + 31) / 32 * 4;
-    auto kern = dtype == SD_F32 ? distill_grad_kernel<float> : distill_grad_kernel<uint16_t>;
-    if (!allow_dynamic_smem(kern, smem)) return SD_ERR_CUDA;
-    return launch_dependent(kern, dim3((unsigned)M * parts), kDistillThreads, smem, 1, st, call, parts, per);
+    return dtype == SD_F32 ? launch_distill<float, kGrad>(call, M, st) : launch_distill<uint16_t, kGrad>(call, M, st);
 }
 
 }  // namespace sdv
