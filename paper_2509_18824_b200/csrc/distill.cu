@@ -23,6 +23,7 @@ constexpr int kDistillThreads = kSumThreads + 128;
 enum { kCopyWarp = kSumWarps, kEntryWarp, kPickWarp, kJoinWarp };
 constexpr int kPieceVecs = 4 * kSumThreads;                // vectors of a piece: four per thread
 constexpr int kMaxSlots = 6;           // of 28 KB
+constexpr int kMaxLists = 4;           // rows whose entries are at hand: as many are prepared ahead
 enum { kLoss, kLossGrad, kGrad };      // what a launch computes
 
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar, uint64_t policy) {
@@ -55,13 +56,13 @@ struct RowFactors { float top, listed, tail, one; };           // what an expone
 
 struct DistillShared {
     uint64_t full[kMaxSlots], picked[kMaxSlots], free_[kMaxSlots];
-    uint64_t info_full[2], info_free[2], sums_full[2], row_ready[2], told[2];
+    uint64_t info_full[kMaxLists], info_free[kMaxLists], sums_full[kMaxLists], row_ready[2], told[2];
     int abort_flag;
-    RowInfo info[2];
+    RowInfo info[kMaxLists];
+    float label_z[kMaxLists];
+    int dup[kMaxLists], label_listed[kMaxLists];
     float4 sums[2][kSumWarps + 1];     // the warps' (largest logit, sum outside the entries, 0, sum at temperature 1); the listed entries'
     double part[2];                    // sum of p z
-    float label_z[2];
-    int dup[2], label_listed[2];
     Message msg[2][8];
     RowFactors row[2];
 };
@@ -145,28 +146,43 @@ struct SliceOf {
 constexpr int kAgain = 1 << 30;
 struct Lists { double* p; float* z; int* at; };
 
+// A row's list as it lies in memory, the lane's first two entries of it (the others are loaded when they are needed)
+struct RawList {
+    const float* val;
+    const int32_t* idx;
+    int label, i0, i1;
+    float weight, t_lse, t0, t1;
+    __device__ __forceinline__ RawList(const DistillCall& a, long long r) : val(a.top_val + r * a.K), idx(a.top_idx + r * a.K) {
+        const int lane = threadIdx.x & 31;
+        i0 = lane < a.K ? __ldcg(idx + lane) : -1;
+        t0 = lane < a.K ? __ldcg(val + lane) : 0.f;
+        i1 = lane + 32 < a.K ? __ldcg(idx + lane + 32) : -1;
+        t1 = lane + 32 < a.K ? __ldcg(val + lane + 32) : 0.f;
+        label = a.label ? __ldcg(a.label + r) : -1;
+        weight = a.dloss ? __ldcg(a.dloss + r) : 1.f;
+        t_lse = a.top_lse ? __ldcg(a.top_lse + r) : 0.f;
+    }
+    __device__ __forceinline__ int index(int k) const { return k < 32 ? i0 : (k < 64 ? i1 : __ldcg(idx + k)); }
+    __device__ __forceinline__ float logit(int k) const { return k < 32 ? t0 : (k < 64 ? t1 : __ldcg(val + k)); }
+};
+
 // By one warp: the entries of row r.
 template <typename T>
-__device__ __forceinline__ void prepare_entries(RowInfo& info, const Lists& li, const DistillCall& a, long long r, const SliceOf<T>& sl, bool report) {
+__device__ __forceinline__ void prepare_entries(RowInfo& info, const Lists& li, const DistillCall& a, long long r, const RawList& raw, const SliceOf<T>& sl, bool report) {
     const int lane = threadIdx.x & 31;
-    const float* val = a.top_val + r * a.K;
-    const int32_t* idx = a.top_idx + r * a.K;
     const int count = (sl.v1 - sl.v0) * SliceOf<T>::E;
-    const int label = a.label ? __ldcg(a.label + r) : -1;
-    const float weight = a.dloss ? __ldcg(a.dloss + r) : 1.f;
-    const float t_lse = a.top_lse ? __ldcg(a.top_lse + r) : 0.f;
-    double log_norm = (double)t_lse;
+    double log_norm = (double)raw.t_lse;
     if (!a.top_lse) {                                                              // the entries' own soft-max
         float top = -INFINITY;
         for (int k = lane; k < a.K; k += 32) {
-            const int i = __ldcg(idx + k);
-            if (i >= 0 && i < a.V) top = fmaxf(top, __ldcg(val + k));
+            const int i = raw.index(k);
+            if (i >= 0 && i < a.V) top = fmaxf(top, raw.logit(k));
         }
         top = warp_largest(top);
         double norm = 0.0;
         for (int k = lane; k < a.K; k += 32) {
-            const int i = __ldcg(idx + k);
-            if (i >= 0 && i < a.V) norm += exp(((double)__ldcg(val + k) - (double)top) * (double)a.inv_temp);
+            const int i = raw.index(k);
+            if (i >= 0 && i < a.V) norm += exp(((double)raw.logit(k) - (double)top) * (double)a.inv_temp);
         }
         norm = warp_add(norm);
         log_norm = (double)top * (double)a.inv_temp + log(norm);
@@ -174,26 +190,26 @@ __device__ __forceinline__ void prepare_entries(RowInfo& info, const Lists& li, 
     double mass = 0.0, plogp = 0.0;
     bool any = false;
     for (int k = lane; k < a.K; k += 32) {
-        const int i = __ldcg(idx + k), at = i - sl.first;
-        const bool there = i >= 0 && i < a.V, here = there && at >= 0 && at < count;
-        const double log_p = there ? (double)__ldcg(val + k) * (double)a.inv_temp - log_norm : -INFINITY, p = exp(log_p);
+        const int i = raw.index(k), at = i - sl.first;
+        const bool there = i >= 0 && i < a.V;
+        const double log_p = there ? (double)raw.logit(k) * (double)a.inv_temp - log_norm : -INFINITY, p = exp(log_p);
         mass += p;
         if (p != 0.0) plogp += p * log_p;
         li.p[k] = p;
-        li.at[k] = here ? at : -1;
+        li.at[k] = there && at >= 0 && at < count ? at : -1;
         any = any || there;
         if (i >= a.V && report) set_status(a.status, SD_ERR_BOUNDS);
     }
     mass = warp_add(mass);
     plogp = warp_add(plogp);
     any = __any_sync(0xffffffffu, any);
-    if (lane == 0) info = RowInfo{mass, plogp, weight, label, any};
+    if (lane == 0) info = RowInfo{mass, plogp, raw.weight, raw.label, any};
     __syncwarp();
 }
 
 template <typename T, int MODE>
 __global__ void __launch_bounds__(kDistillThreads, 2)
-distill_kernel(DistillCall a, long long units, int parts, int per, int slots, int withheld, long long wait_cycles) {
+distill_kernel(DistillCall a, long long units, int parts, int per, int slots, int list_bits, int withheld, long long wait_cycles) {
     using namespace sm100;
     using Sl = SliceOf<T>;
     constexpr int E = Row<T>::kE;
@@ -204,8 +220,8 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
     if (tid == 0) {
         sh.abort_flag = 0;
         for (int q = 0; q < slots; ++q) { mbar_init(&sh.full[q], 1); mbar_init(&sh.picked[q], 1); mbar_init(&sh.free_[q], kSumWarps); }
-        for (int q = 0; q < 2; ++q) { mbar_init(&sh.info_full[q], 1); mbar_init(&sh.info_free[q], kSumWarps + 1 + (MODE != kGrad)); mbar_init(&sh.told[q], 1); }
-        for (int q = 0; q < 2; ++q) { mbar_init(&sh.sums_full[q], MODE == kGrad ? 1 : kSumWarps + 1); mbar_init(&sh.row_ready[q], 1); }
+        for (int q = 0; q < kMaxLists; ++q) { mbar_init(&sh.info_full[q], 1); mbar_init(&sh.info_free[q], kSumWarps + 1 + (MODE != kGrad)); mbar_init(&sh.sums_full[q], MODE == kGrad ? 1 : kSumWarps + 1); }
+        for (int q = 0; q < 2; ++q) { mbar_init(&sh.told[q], 1); mbar_init(&sh.row_ready[q], 1); }
         fence_barrier_init();
     }
     const bool talk = MODE != kGrad && parts > 1;                                  // CTAs of a cluster share a row (else every unit is its own)
@@ -220,21 +236,26 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
         Lists li;
         double* base = reinterpret_cast<double*>(ring + slots * kPieceVecs);
         li.p = base + b * a.K;
-        base += 2 * a.K;
+        base += a.K << list_bits;
         li.at = reinterpret_cast<int*>(base) + b * a.K;
-        li.z = reinterpret_cast<float*>(base + a.K) + b * a.K;
+        li.z = reinterpret_cast<float*>(base) + (a.K << list_bits) + b * a.K;
         return li;
     };
+    // the n-th unit's list, and the phase of its barriers; sums alternate between two places
+    const auto list_of = [&](long long n) { return (int)(n & ((1 << list_bits) - 1)); };
+    const auto phase_of = [&](long long n) { return (uint32_t)((n >> list_bits) & 1); };
     bool ok = true;
 
     if (warp == kEntryWarp) {
         long long n = 0;
         for (long long u = start; u < units; u += step, ++n) {
-            const int b = (int)(n & 1);
-            ok = mbar_wait_warp(&sh.info_free[b], (uint32_t)((n >> 1) & 1) ^ 1u, &sh.abort_flag, wait_cycles);
+            const int b = list_of(n);
+            const long long r = row_of(u);
+            const Sl sl(a, r, rank_of(u), per);
+            const RawList raw(a, r);                                               // (under way while the place is waited for)
+            ok = mbar_wait_warp(&sh.info_free[b], phase_of(n) ^ 1u, &sh.abort_flag, wait_cycles);
             if (!ok) break;
-            const Sl sl(a, row_of(u), rank_of(u), per);
-            prepare_entries<T>(sh.info[b], lists_of(b), a, row_of(u), sl, rank_of(u) == 0);
+            prepare_entries<T>(sh.info[b], lists_of(b), a, r, raw, sl, rank_of(u) == 0);
             if (lane == 0) mbar_arrive(&sh.info_full[b]);
         }
     } else if (warp == kCopyWarp) {
@@ -269,10 +290,10 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
         const bool rest_too = a.top_lse != nullptr;
         long long cnt = 0, n = 0;
         for (long long u = start; u < units && ok; u += step, ++n) {
-            const int b = (int)(n & 1);
+            const int b = list_of(n), h = (int)(n & 1);
             const Sl sl(a, row_of(u), rank_of(u), per);
             const Lists li = lists_of(b);
-            ok = mbar_wait_warp(&sh.info_full[b], (uint32_t)((n >> 1) & 1), &sh.abort_flag, wait_cycles);
+            ok = mbar_wait_warp(&sh.info_full[b], phase_of(n), &sh.abort_flag, wait_cycles);
             const int label = sh.info[b].label, lj = label - sl.first;
             const bool has_label = label >= 0 && label < a.V;
             float label_z = 0.f;
@@ -342,8 +363,8 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
                 }
                 part = warp_add(part);
                 // (the loss alone: the sums of two rows before have been taken over)
-                ok = mbar_wait_warp(&sh.row_ready[b], (uint32_t)((n >> 1) & 1) ^ 1u, &sh.abort_flag, wait_cycles);
-                if (lane == 0) { sh.sums[b][kSumWarps] = make_float4(top, 0.f, sum, sum1); sh.part[b] = part; }
+                ok = mbar_wait_warp(&sh.row_ready[h], (uint32_t)((n >> 1) & 1) ^ 1u, &sh.abort_flag, wait_cycles);
+                if (lane == 0) { sh.sums[h][kSumWarps] = make_float4(top, 0.f, sum, sum1); sh.part[h] = part; }
             }
             if (lane == 0) { sh.label_z[b] = label_z; sh.dup[b] = dup; sh.label_listed[b] = label_listed; }
             __syncwarp();
@@ -358,32 +379,32 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
         long long n = 0;
         if constexpr (MODE != kGrad)
         for (long long r = start; r < units && ok; r += step, ++n) {
-            const int b = (int)(n & 1);
+            const int b = list_of(n), h = (int)(n & 1);
             const uint32_t ph = (uint32_t)((n >> 1) & 1);
-            ok = mbar_wait_warp(&sh.info_full[b], ph, &sh.abort_flag, wait_cycles) && mbar_wait_warp(&sh.sums_full[b], ph, &sh.abort_flag, wait_cycles);
+            ok = mbar_wait_warp(&sh.info_full[b], phase_of(n), &sh.abort_flag, wait_cycles) && mbar_wait_warp(&sh.sums_full[b], phase_of(n), &sh.abort_flag, wait_cycles);
             if (!ok) break;
             const RowInfo& info = sh.info[b];
             const int label = info.label;
             const bool has_label = label >= 0 && label < a.V, two = has_label && a.inv_temp != 1.f;
-            const float4 w = lane <= kSumWarps ? sh.sums[b][lane] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
-            double entries = sh.part[b];
+            const float4 w = lane <= kSumWarps ? sh.sums[h][lane] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+            double entries = sh.part[h];
             float label_z = sh.label_z[b], most = warp_largest(w.x);
             const float f = weigh(w.x, most, c);
             float rest = warp_add(w.y * f), listed = rest_too ? warp_add(w.z * f) : 0.f, sum1 = two ? warp_add(w.w * weigh(w.x, most, kLog2e)) : 0.f;
             if (talk) {
                 const Message mine{most, label_z, rest, listed, sum1, 0.f, entries};
                 if (lane == rank) {
-                    sh.msg[b][rank] = mine;
-                    mbar_arrive_expect_tx(&sh.told[b], (parts - 1) * (uint32_t)sizeof(Message));
+                    sh.msg[h][rank] = mine;
+                    mbar_arrive_expect_tx(&sh.told[h], (parts - 1) * (uint32_t)sizeof(Message));
                 } else if (lane < parts) {
-                    const uint32_t to = map_dsmem(smem_u32(&sh.msg[b][rank]), lane), bar = map_dsmem(smem_u32(&sh.told[b]), lane);
+                    const uint32_t to = map_dsmem(smem_u32(&sh.msg[h][rank]), lane), bar = map_dsmem(smem_u32(&sh.told[h]), lane);
                     st_async_v4(to, __float_as_uint(most), __float_as_uint(label_z), __float_as_uint(rest), __float_as_uint(listed), bar);
                     st_async_v4(to + 16, __float_as_uint(sum1), 0u, (uint32_t)__double2loint(entries), (uint32_t)__double2hiint(entries), bar);
                 }
-                ok = mbar_wait_cluster(&sh.told[b], ph, &sh.abort_flag, wait_cycles);
+                ok = mbar_wait_cluster(&sh.told[h], ph, &sh.abort_flag, wait_cycles);
                 ok = __all_sync(0xffffffffu, ok);
                 Message o{-INFINITY, 0.f, 0.f, 0.f, 0.f, 0.f, 0.0};
-                if (lane < parts) o = sh.msg[b][lane];
+                if (lane < parts) o = sh.msg[h][lane];
                 most = warp_largest(o.top);
                 const float g = weigh(o.top, most, c);
                 rest = warp_add(o.rest * g);
@@ -400,7 +421,7 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
             // tail / sum = (all_p - p_rest / s_rest) / sum with s_rest = rest / sum
             const float inv = 1.f / sum, tail = has_rest ? inv - (float)p_rest / rest : all_p * inv;
             const RowFactors rf{most, all_p * inv, tail, two ? 1.f / sum1 : inv};
-            if (lane == 0) { sh.row[b] = rf; mbar_arrive(&sh.row_ready[b]); }
+            if (lane == 0) { sh.row[h] = rf; mbar_arrive(&sh.row_ready[h]); }
             if (rank == 0) {
                 if (talk) { entries = warp_add(entries); label_z = warp_add(label_z); }
                 // lane 0: kl; lane 1: ce.  (R belongs to the power with c as 32 bits hold it: log sum = R ln 2 + log(sum), but for c's rounding)
@@ -428,11 +449,11 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
         long long cnt = 0;
         long long n = 0;
         for (long long u = start; u < units; u += step, ++n) {
-            const int b = (int)(n & 1);
+            const int b = list_of(n), h = (int)(n & 1);
             const long long r = row_of(u);
             const Sl sl(a, r, rank_of(u), per);
             const Lists li = lists_of(b);
-            ok = mbar_wait(&sh.info_full[b], (uint32_t)((n >> 1) & 1), &sh.abort_flag, wait_cycles) && ok;
+            ok = mbar_wait(&sh.info_full[b], phase_of(n), &sh.abort_flag, wait_cycles) && ok;
             const RowInfo& info = sh.info[b];
             const int label = info.label;
             const bool has_label = label >= 0 && label < a.V;
@@ -498,13 +519,13 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
                 const float rest = warp_add((s.x + s.y) + (t.x + t.y)) * ex2(r_c - whole_power(most, c));
                 const float sum1 = two ? warp_add(s1.x + s1.y) * ex2(r_e - whole_power(most, kLog2e)) : 0.f;
                 // (the loss alone: the sums of two rows before have been taken over)
-                if (MODE == kLoss) ok = mbar_wait(&sh.row_ready[b], (uint32_t)((n >> 1) & 1) ^ 1u, &sh.abort_flag, wait_cycles) && ok;
-                if (lane == 0) sh.sums[b][warp] = make_float4(most, rest, 0.f, sum1);
+                if (MODE == kLoss) ok = mbar_wait(&sh.row_ready[h], (uint32_t)((n >> 1) & 1) ^ 1u, &sh.abort_flag, wait_cycles) && ok;
+                if (lane == 0) sh.sums[h][warp] = make_float4(most, rest, 0.f, sum1);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sh.sums_full[b]);
                 if constexpr (MODE == kLossGrad) {
-                    ok = mbar_wait(&sh.row_ready[b], (uint32_t)((n >> 1) & 1), &sh.abort_flag, wait_cycles) && ok;
-                    rf = sh.row[b];
+                    ok = mbar_wait(&sh.row_ready[h], (uint32_t)((n >> 1) & 1), &sh.abort_flag, wait_cycles) && ok;
+                    rf = sh.row[h];
                 }
             } else {
                 const float4 st = __ldcg(reinterpret_cast<const float4*>(a.stats) + r);
@@ -557,7 +578,7 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
                     if (++slot == slots) slot = 0;
                 }
                 // over what has just been written
-                if (MODE == kGrad) ok = mbar_wait(&sh.sums_full[b], (uint32_t)((n >> 1) & 1), &sh.abort_flag, wait_cycles) && ok;
+                if (MODE == kGrad) ok = mbar_wait(&sh.sums_full[b], phase_of(n), &sh.abort_flag, wait_cycles) && ok;
                 ok = !sum_warps_or(!ok);                                           // (all fourteen come here in every row, whatever they waited for)
                 if (!zero) {
                     for (int k = tid; k < a.K; k += kSumThreads) {
@@ -634,7 +655,8 @@ static sd_status launch_distill(const DistillCall& call, int M, cudaStream_t st)
     if (cudaGetDevice(&dev) != cudaSuccess) return SD_ERR_CUDA;
     const int sms = sm_count(dev), parts = distill_parts(M, nvec, sms), per = (nvec + parts - 1) / parts;
     const int pieces = (per + kPieceVecs - 1) / kPieceVecs, slots = pieces > 3 ? pieces : 3;
-    const int smem = slots * kPieceVecs * 16 + 2 * call.K * 16;
+    const int list_bits = call.K <= 256 ? 2 : 1;                                   // four rows' lists, or two long ones'
+    const int smem = slots * kPieceVecs * 16 + (call.K * 16 << list_bits);
     auto kern = distill_kernel<T, MODE>;
     if (slots > kMaxSlots || !allow_dynamic_smem(kern, smem)) return SD_ERR_CUDA;
     const int cluster = MODE == kGrad ? 1 : parts;
@@ -643,7 +665,7 @@ static sd_status launch_distill(const DistillCall& call, int M, cudaStream_t st)
     if (resident < 1) return SD_ERR_CUDA;
     const long long clusters = units < resident ? units : resident;
     const TestKnobs knobs = test_knobs();
-    return launch_dependent(kern, dim3((unsigned)(clusters * cluster)), kDistillThreads, smem, cluster, st, call, units, parts, per, slots,
+    return launch_dependent(kern, dim3((unsigned)(clusters * cluster)), kDistillThreads, smem, cluster, st, call, units, parts, per, slots, list_bits,
                             knobs.withhold ? 16 : 0, knobs.wait_cycles);
 }
 
