@@ -50,7 +50,7 @@ static_assert(sizeof(Message) == 32, "two stores of 16 bytes");
 struct RowInfo {                       // prepared ahead
     double mass, plogp;                // sums of p and p log p
     float weight;                      // dloss
-    int label, any;
+    int label, any, count;             // count: entries that lie in this CTA's slice
 };
 struct RowFactors { float top, listed, tail, one; };           // what an exponential is multiplied with at the entries, elsewhere, for the cross-entropy
 
@@ -141,8 +141,8 @@ struct SliceOf {
     }
 };
 
-// Lists of one row in shared memory: probabilities, logits, places in the slice (-1: elsewhere, or no entry; with kAgain: a place that
-// another entry of the list has too, and answers for)
+// Lists of one row in shared memory, the entries in this CTA's slice: probabilities, logits, places in the slice (with kAgain: a place
+// that another entry of the list has too, and answers for)
 constexpr int kAgain = 1 << 30;
 struct Lists { double* p; float* z; int* at; };
 
@@ -189,21 +189,27 @@ __device__ __forceinline__ void prepare_entries(RowInfo& info, const Lists& li, 
     }
     double mass = 0.0, plogp = 0.0;
     bool any = false;
-    for (int k = lane; k < a.K; k += 32) {
-        const int i = raw.index(k), at = i - sl.first;
-        const bool there = i >= 0 && i < a.V;
+    int n = 0;
+    for (int k0 = 0; k0 < a.K; k0 += 32) {
+        const int k = k0 + lane, i = k < a.K ? raw.index(k) : -1, at = i - sl.first;
+        const bool there = i >= 0 && i < a.V, here = there && at >= 0 && at < count;
         const double log_p = there ? (double)raw.logit(k) * (double)a.inv_temp - log_norm : -INFINITY, p = exp(log_p);
         mass += p;
         if (p != 0.0) plogp += p * log_p;
-        li.p[k] = p;
-        li.at[k] = there && at >= 0 && at < count ? at : -1;
+        const uint32_t all = __ballot_sync(0xffffffffu, here);
+        if (here) {
+            const int to = n + __popc(all & ((1u << lane) - 1));
+            li.p[to] = p;
+            li.at[to] = at;
+        }
+        n += __popc(all);
         any = any || there;
         if (i >= a.V && report) set_status(a.status, SD_ERR_BOUNDS);
     }
     mass = warp_add(mass);
     plogp = warp_add(plogp);
     any = __any_sync(0xffffffffu, any);
-    if (lane == 0) info = RowInfo{mass, plogp, raw.weight, raw.label, any};
+    if (lane == 0) info = RowInfo{mass, plogp, raw.weight, raw.label, any, n};
     __syncwarp();
 }
 
@@ -296,67 +302,90 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
             ok = mbar_wait_warp(&sh.info_full[b], phase_of(n), &sh.abort_flag, wait_cycles);
             const int label = sh.info[b].label, lj = label - sl.first;
             const bool has_label = label >= 0 && label < a.V;
+            const int count = sh.info[b].count;
+            const bool away = MODE != kGrad && rest_too;                           // minus infinity takes a listed logit's place
             float label_z = 0.f;
             double part = 0.0;
             bool dup = false, label_listed = false;
+            // the lane's first entry (a slice has rarely more than 32)
+            const int j0 = ok && lane < count ? li.at[lane] : -1;
+            const double p0 = j0 >= 0 ? li.p[lane] : 0.0;
+            float z0 = 0.f;
+            bool again0 = false;
             int slot = (int)(cnt % slots);
             for (int q = 0; q < sl.pieces && ok; ++q, ++cnt) {
                 ok = mbar_wait_warp(&sh.full[slot], (uint32_t)((cnt / slots) & 1), &sh.abort_flag, wait_cycles);
                 if (!ok) break;
-                T* entries = reinterpret_cast<T*>(ring + slot * kPieceVecs);
+                Number* piece = reinterpret_cast<Number*>(ring + slot * kPieceVecs);
                 const int e0 = q * kPieceVecs * E, e1 = min(e0 + kPieceVecs * E, (sl.v1 - sl.v0) * E);
-                const auto value = [&](int j) {
-                    if constexpr (sizeof(T) == 4) return (float)entries[j - e0];
-                    else return __uint_as_float((uint32_t)entries[j - e0] << 16);
-                };
+                const auto value = [&](int j) { return __uint_as_float(sizeof(T) == 4 ? (uint32_t)piece[j - e0] : (uint32_t)piece[j - e0] << 16); };
+                const auto put = [&](int j, float z) { piece[j - e0] = (Number)(sizeof(T) == 4 ? __float_as_uint(z) : __float_as_uint(z) >> 16); };
                 if (has_label && lj >= e0 && lj < e1) label_z = value(lj);
-                const auto here = [&](int k) { const int j = li.at[k]; return j >= e0 && j < e1; };
-                for (int k = lane; k < a.K; k += 32) {
-                    if (!here(k)) continue;
-                    const float z = value(li.at[k]);
-                    const double p = li.p[k];
-                    li.z[k] = z;
-                    label_listed = label_listed || li.at[k] == lj;
-                    if (p != 0.0) part += p * (double)z;
-                }
-                // the same place twice?  Every entry leaves its number there; one of them finds it again.
-                __syncwarp();
-                for (int k = lane; k < a.K; k += 32)
-                    if (here(k)) reinterpret_cast<Number*>(entries)[li.at[k] - e0] = (Number)k;
-                __syncwarp();
-                uint32_t again = 0;                                                // (K is at most 1024: a bit per round)
-                for (int k = lane; k < a.K; k += 32)
-                    if (here(k) && reinterpret_cast<Number*>(entries)[li.at[k] - e0] != (Number)k) again |= 1u << (k >> 5);
-                __syncwarp();
-                for (int k = lane; k < a.K; k += 32)
-                    if (here(k)) {
-                        const uint32_t z = __float_as_uint(MODE != kGrad && rest_too ? -INFINITY : li.z[k]);
-                        reinterpret_cast<Number*>(entries)[li.at[k] - e0] = (Number)(sizeof(T) == 4 ? z : z >> 16);
+                // The same place twice?  Every entry leaves its number there; one of them finds it again.
+                const bool here0 = j0 >= e0 && j0 < e1;
+                if (count <= 32) {
+                    if (__any_sync(0xffffffffu, here0)) {
+                        if (here0) z0 = value(j0);
+                        __syncwarp();
+                        if (here0) piece[j0 - e0] = (Number)lane;
+                        __syncwarp();
+                        again0 = again0 || (here0 && piece[j0 - e0] != (Number)lane);
+                        __syncwarp();
+                        if (here0) put(j0, away ? -INFINITY : z0);
+                        __syncwarp();
                     }
-                __syncwarp();
-                if (again) {
-                    dup = true;
-                    for (int k = lane; k < a.K; k += 32) if (again >> (k >> 5) & 1) li.at[k] |= kAgain;
+                } else {
+                    const auto here = [&](int k) { const int j = li.at[k]; return j >= e0 && j < e1; };
+                    for (int k = lane; k < count; k += 32)
+                        if (here(k)) li.z[k] = value(li.at[k]);
+                    __syncwarp();
+                    for (int k = lane; k < count; k += 32)
+                        if (here(k)) piece[li.at[k] - e0] = (Number)k;
+                    __syncwarp();
+                    uint32_t again = 0;                                            // (at most 1024 entries: a bit per round)
+                    for (int k = lane; k < count; k += 32)
+                        if (here(k) && piece[li.at[k] - e0] != (Number)k) again |= 1u << (k >> 5);
+                    __syncwarp();
+                    for (int k = lane; k < count; k += 32)
+                        if (here(k)) put(li.at[k], away ? -INFINITY : li.z[k]);
+                    __syncwarp();
+                    if (again) {
+                        dup = true;
+                        for (int k = lane; k < count; k += 32) if (again >> (k >> 5) & 1) li.at[k] |= kAgain;
+                    }
                 }
-                __syncwarp();
                 if (lane == 0) mbar_arrive(&sh.picked[slot]);
                 if (++slot == slots) slot = 0;
             }
             if (!ok) break;
+            if (count <= 32) {
+                dup = again0;
+                label_listed = j0 >= 0 && j0 == lj;
+                part = p0 != 0.0 ? p0 * (double)z0 : 0.0;
+                if (j0 >= 0) li.z[lane] = z0;
+                if (again0) li.at[lane] = j0 | kAgain;
+            } else {
+                for (int k = lane; k < count; k += 32) {
+                    label_listed = label_listed || (li.at[k] & ~kAgain) == lj;
+                    if (li.p[k] != 0.0) part += li.p[k] * (double)li.z[k];
+                }
+            }
             dup = __any_sync(0xffffffffu, dup);
             label_listed = __any_sync(0xffffffffu, label_listed);
             if constexpr (MODE != kGrad) {
-                // the listed entries' own sum, every index once
+                // the listed entries' own sums, every index once
                 float top = -INFINITY, sum = 0.f, sum1 = 0.f;
                 if (rest_too) {
-                    const auto counts = [&](int k) { const int j = li.at[k]; return j >= 0 && j < kAgain; };
-                    for (int k = lane; k < a.K; k += 32) if (counts(k)) top = fmaxf(top, li.z[k]);
+                    const auto counts = [&](int k) { return k < 32 ? j0 >= 0 && !again0 : li.at[k] < kAgain; };
+                    const auto logit = [&](int k) { return count <= 32 ? z0 : li.z[k]; };
+                    if (count > 32) again0 = j0 >= 0 && li.at[lane] >= kAgain;
+                    for (int k = lane; k < count; k += 32) if (counts(k)) top = fmaxf(top, logit(k));
                     top = warp_largest(top);
                     const float r_c = whole_power(top, c), r_e = whole_power(top, kLog2e);
-                    for (int k = lane; k < a.K; k += 32)
+                    for (int k = lane; k < count; k += 32)
                         if (counts(k)) {
-                            sum += ex2(fmaf(li.z[k], c, -r_c));
-                            sum1 += ex2(fmaf(li.z[k], kLog2e, -r_e));
+                            sum += ex2(fmaf(logit(k), c, -r_c));
+                            sum1 += ex2(fmaf(logit(k), kLog2e, -r_e));
                         }
                     sum = warp_add(sum);
                     sum1 = warp_add(sum1);
@@ -581,13 +610,13 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
                 if (MODE == kGrad) ok = mbar_wait(&sh.sums_full[b], phase_of(n), &sh.abort_flag, wait_cycles) && ok;
                 ok = !sum_warps_or(!ok);                                           // (all fourteen come here in every row, whatever they waited for)
                 if (!zero) {
-                    for (int k = tid; k < a.K; k += kSumThreads) {
+                    for (int k = tid; k < info.count; k += kSumThreads) {
                         const int j = li.at[k];
-                        if (j < 0 || j >= kAgain) continue;
+                        if (j >= kAgain) continue;
                         double p = li.p[k];
                         if (sh.dup[b]) {                                           // the same index twice somewhere: all of its masses
                             p = 0.0;
-                            for (int x = 0; x < a.K; ++x) p += li.at[x] >= 0 && (li.at[x] & ~kAgain) == j ? li.p[x] : 0.0;
+                            for (int x = 0; x < info.count; ++x) p += (li.at[x] & ~kAgain) == j ? li.p[x] : 0.0;
                         }
                         float g = f.at(li.z[k], f.listed) - f.per_p * (float)p;
                         if (j + sl.first == label) g -= f.per_label;
