@@ -47,6 +47,13 @@ __device__ __forceinline__ float whole_power(float top, float c) { return top > 
 struct __align__(16) Message { float top, label, rest, listed, sum1, pad; double entries; };
 static_assert(sizeof(Message) == 32, "two stores of 16 bytes");
 
+// A place in the ring of slots and the phase of its barriers
+struct Turn {
+    int slot = 0;
+    uint32_t phase = 0;
+    __device__ __forceinline__ void next(int slots) { if (++slot == slots) { slot = 0; phase ^= 1u; } }
+};
+
 struct RowInfo {                       // prepared ahead
     double mass, plogp;                // sums of p and p log p
     float weight;                      // dloss
@@ -266,12 +273,12 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
         }
     } else if (warp == kCopyWarp) {
         const uint64_t pol = policy_evict_first();
-        long long cnt = 0;
+        Turn at;
         for (long long u = start; u < units && ok; u += step) {
             const Sl sl(a, row_of(u), rank_of(u), per);
-            int slot = (int)(cnt % slots);
-            for (int q = 0; q < sl.pieces && ok; ++q, ++cnt) {
-                ok = mbar_wait_warp(&sh.free_[slot], (uint32_t)((cnt / slots) & 1) ^ 1u, &sh.abort_flag, wait_cycles);
+            for (int q = 0; q < sl.pieces && ok; ++q, at.next(slots)) {
+                const int slot = at.slot;
+                ok = mbar_wait_warp(&sh.free_[slot], at.phase ^ 1u, &sh.abort_flag, wait_cycles);
                 if (!ok) break;
                 uint4* dst = ring + slot * kPieceVecs;
                 const int a0 = sl.v0 + q * kPieceVecs, a1 = min(sl.v1, a0 + kPieceVecs);
@@ -288,13 +295,13 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
                     if (bytes) bulk_load(dst + (i0 - a0), sl.row.vec + i0, bytes, &sh.full[slot], pol);
                 }
                 __syncwarp();
-                if (++slot == slots) slot = 0;
             }
         }
     } else if (warp == kPickWarp) {
         const float c = a.inv_temp * kLog2e;
         const bool rest_too = a.top_lse != nullptr;
-        long long cnt = 0, n = 0;
+        Turn at;
+        long long n = 0;
         for (long long u = start; u < units && ok; u += step, ++n) {
             const int b = list_of(n), h = (int)(n & 1);
             const Sl sl(a, row_of(u), rank_of(u), per);
@@ -312,9 +319,9 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
             const double p0 = j0 >= 0 ? li.p[lane] : 0.0;
             float z0 = 0.f;
             bool again0 = false;
-            int slot = (int)(cnt % slots);
-            for (int q = 0; q < sl.pieces && ok; ++q, ++cnt) {
-                ok = mbar_wait_warp(&sh.full[slot], (uint32_t)((cnt / slots) & 1), &sh.abort_flag, wait_cycles);
+            for (int q = 0; q < sl.pieces && ok; ++q, at.next(slots)) {
+                const int slot = at.slot;
+                ok = mbar_wait_warp(&sh.full[slot], at.phase, &sh.abort_flag, wait_cycles);
                 if (!ok) break;
                 Number* piece = reinterpret_cast<Number*>(ring + slot * kPieceVecs);
                 const int e0 = q * kPieceVecs * E, e1 = min(e0 + kPieceVecs * E, (sl.v1 - sl.v0) * E);
@@ -355,7 +362,6 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
                     }
                 }
                 if (lane == 0) mbar_arrive(&sh.picked[slot]);
-                if (++slot == slots) slot = 0;
             }
             if (!ok) break;
             if (count <= 32) {
@@ -475,7 +481,7 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
     } else {
         const float c = a.inv_temp * kLog2e;
         const Pair c2{c, c}, e2{kLog2e, kLog2e};
-        long long cnt = 0;
+        Turn at;
         long long n = 0;
         for (long long u = start; u < units; u += step, ++n) {
             const int b = list_of(n), h = (int)(n & 1);
@@ -487,16 +493,15 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
             const int label = info.label;
             const bool has_label = label >= 0 && label < a.V;
             const bool two = MODE != kGrad && has_label && a.inv_temp != 1.f;
-            const long long cnt0 = cnt;
-            int slot = (int)(cnt % slots);
-            const int slot0 = slot;
+            const Turn at0 = at;
 
             // ---- sums of the pieces as they come in
             float top = -INFINITY, r_c = 0.f, r_e = 0.f;                           // top: of the lane's entries; the R's are the warp's
             Pair s{0.f, 0.f}, t{0.f, 0.f}, s1{0.f, 0.f};
             bool begun = false;
-            for (int q = 0; MODE != kGrad && q < sl.pieces; ++q, ++cnt) {
-                ok = mbar_wait(&sh.picked[slot], (uint32_t)((cnt / slots) & 1), &sh.abort_flag, wait_cycles) && ok;
+            for (int q = 0; MODE != kGrad && q < sl.pieces; ++q, at.next(slots)) {
+                const int slot = at.slot;
+                ok = mbar_wait(&sh.picked[slot], at.phase, &sh.abort_flag, wait_cycles) && ok;
                 const uint4* src = ring + slot * kPieceVecs;
                 const int len = min(kPieceVecs, sl.v1 - sl.v0 - q * kPieceVecs);
                 uint4 raw[4];
@@ -520,25 +525,28 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
                 }
                 top = fmaxf(top, m);
                 const Pair from_c{-r_c, -r_c}, from_e{-r_e, -r_e};
+                const auto add = [&](auto both) {                                  // (two loops: as one, the second exponentials were issued in either case)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    Pair x[E / 2];
-                    Row<T>::pairs(raw[j], x);
+                    for (int j = 0; j < 4; ++j) {
+                        Pair x[E / 2];
+                        Row<T>::pairs(raw[j], x);
 #pragma unroll
-                    for (int e = 0; e < E / 2; e += 2) {
-                        s = add2(s, ex2(fma2(x[e], c2, from_c)));
-                        t = add2(t, ex2(fma2(x[e + 1], c2, from_c)));
+                        for (int e = 0; e < E / 2; e += 2) {
+                            s = add2(s, ex2(fma2(x[e], c2, from_c)));
+                            t = add2(t, ex2(fma2(x[e + 1], c2, from_c)));
+                        }
+                        if constexpr (decltype(both)::value) {
+#pragma unroll
+                            for (int e = 0; e < E / 2; ++e) s1 = add2(s1, ex2(fma2(x[e], e2, from_e)));
+                        }
                     }
-                    if (two) {
-#pragma unroll
-                        for (int e = 0; e < E / 2; ++e) s1 = add2(s1, ex2(fma2(x[e], e2, from_e)));
-                    }
-                }
+                };
+                if (two) add(std::true_type{});
+                else add(std::false_type{});
                 if (MODE == kLoss) {
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&sh.free_[slot]);
                 }
-                if (++slot == slots) slot = 0;
             }
 
             RowFactors rf;
@@ -570,10 +578,10 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
                 T* grad = static_cast<T*>(a.grad) + r * a.grad_ld;
                 const bool same = ((reinterpret_cast<uintptr_t>(grad) ^ reinterpret_cast<uintptr_t>(sl.row.p)) & 15) == 0;
                 uint4* out = reinterpret_cast<uint4*>(reinterpret_cast<uintptr_t>(grad) & ~(uintptr_t)15);
-                slot = slot0;
-                cnt = cnt0;
-                for (int q = 0; q < sl.pieces; ++q, ++cnt) {
-                    if (MODE == kGrad) ok = mbar_wait(&sh.picked[slot], (uint32_t)((cnt / slots) & 1), &sh.abort_flag, wait_cycles) && ok;
+                at = at0;
+                for (int q = 0; q < sl.pieces; ++q, at.next(slots)) {
+                    const int slot = at.slot;
+                    if (MODE == kGrad) ok = mbar_wait(&sh.picked[slot], at.phase, &sh.abort_flag, wait_cycles) && ok;
                     const uint4* src = ring + slot * kPieceVecs;
                     const int len = min(kPieceVecs, sl.v1 - sl.v0 - q * kPieceVecs), a0 = sl.v0 + q * kPieceVecs;
                     const auto one = [&](int i, auto kind) {                       // vector i of the piece
@@ -604,7 +612,6 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
                     else all(std::integral_constant<int, 1>{});
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&sh.free_[slot]);
-                    if (++slot == slots) slot = 0;
                 }
                 // over what has just been written
                 if (MODE == kGrad) ok = mbar_wait(&sh.sums_full[b], phase_of(n), &sh.abort_flag, wait_cycles) && ok;
