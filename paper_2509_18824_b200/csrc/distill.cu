@@ -1,7 +1,7 @@
 // The draft's training loss on rows of logits [M][V] and its gradient (sd_distill_loss, sd_distill_grad).
 //
 // Memory-bound: a row is read once and, with the gradient, written once.  Persistent clusters of `parts` CTAs take a row at a time,
-// each CTA a slice of it, in pieces of 28 KB through a ring of slots.  Fourteen warps sum up the exponentials of a piece; what a row
+// each CTA a slice of it, in pieces of 21 KB through a ring of slots.  Fourteen warps sum up the exponentials of a piece; what a row
 // needs but once is done by four more, so that it does not stand in their way:
 //   copy     issues the pieces' copies as slots become free
 //   entries  prepares the next row's list: probabilities, places in the slice
@@ -21,8 +21,9 @@ constexpr int kSumWarps = 14;
 constexpr int kSumThreads = kSumWarps * 32;
 constexpr int kDistillThreads = kSumThreads + 128;
 enum { kCopyWarp = kSumWarps, kEntryWarp, kPickWarp, kJoinWarp };
-constexpr int kPieceVecs = 4 * kSumThreads;                // vectors of a piece: four per thread
-constexpr int kMaxSlots = 6;           // of 28 KB
+constexpr int kPerThread = 3;
+constexpr int kPieceVecs = kPerThread * kSumThreads;       // vectors of a piece
+constexpr int kSlots = 5, kMaxSlots = 8;                   // of 21 KB
 constexpr int kMaxLists = 4;           // rows whose entries are at hand: as many are prepared ahead
 enum { kLoss, kLossGrad, kGrad };      // what a launch computes
 
@@ -504,10 +505,10 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
                 ok = mbar_wait(&sh.picked[slot], at.phase, &sh.abort_flag, wait_cycles) && ok;
                 const uint4* src = ring + slot * kPieceVecs;
                 const int len = min(kPieceVecs, sl.v1 - sl.v0 - q * kPieceVecs);
-                uint4 raw[4];
+                uint4 raw[kPerThread];
                 float m = -INFINITY;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
+                for (int j = 0; j < kPerThread; ++j) {
                     const int i = tid + j * kSumThreads;
                     raw[j] = i < len ? src[i] : Row<T>::nothing();
                     m = Row<T>::largest(raw[j], m);
@@ -527,7 +528,8 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
                 const Pair from_c{-r_c, -r_c}, from_e{-r_e, -r_e};
                 const auto add = [&](auto both) {                                  // (two loops: as one, the second exponentials were issued in either case)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
+                    for (int j = 0; j < kPerThread; ++j) {
+                        if (warp * 32 + j * kSumThreads >= len) break;             // (nothing for the whole warp)
                         Pair x[E / 2];
                         Row<T>::pairs(raw[j], x);
 #pragma unroll
@@ -602,7 +604,7 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
                     };
                     const auto all = [&](auto kind) {
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
+                        for (int j = 0; j < kPerThread; ++j) {
                             const int i = tid + j * kSumThreads;
                             if (i < len) one(i, kind);
                         }
@@ -645,10 +647,10 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
     if (!ok || *reinterpret_cast<volatile int*>(&sh.abort_flag)) unwind_pause();
 }
 
-// CTAs per row: slices of at most three pieces where eight CTAs are enough for that, and more of them where the rows leave SMs idle
+// CTAs per row: slices of at most four pieces (a slot is left for the next row) where eight CTAs are enough for that, and more of them where the rows leave SMs idle
 static int distill_parts(int M, int nvec, int sms) {
     int parts = 1;
-    while (parts < 8 && ((nvec + parts - 1) / parts > 3 * kPieceVecs || ((long long)M * parts <= sms && nvec / (parts * 2) >= kSumThreads))) parts *= 2;
+    while (parts < 8 && ((nvec + parts - 1) / parts > (kSlots - 1) * kPieceVecs || ((long long)M * parts <= sms && nvec / (parts * 2) >= kSumThreads))) parts *= 2;
     return parts;
 }
 
@@ -690,7 +692,7 @@ static sd_status launch_distill(const DistillCall& call, int M, cudaStream_t st)
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return SD_ERR_CUDA;
     const int sms = sm_count(dev), parts = distill_parts(M, nvec, sms), per = (nvec + parts - 1) / parts;
-    const int pieces = (per + kPieceVecs - 1) / kPieceVecs, slots = pieces > 3 ? pieces : 3;
+    const int pieces = (per + kPieceVecs - 1) / kPieceVecs, slots = pieces > kSlots ? pieces : kSlots;
     const int list_bits = call.K <= 256 ? 2 : 1;                                   // four rows' lists, or two long ones'
     const int smem = slots * kPieceVecs * 16 + (call.K * 16 << list_bits);
     auto kern = distill_kernel<T, MODE>;
