@@ -548,7 +548,8 @@ sd_status sd_filter_logits(const void *logits, int32_t dtype, int64_t ld, int32_
  * dloss     : NULL (1), or dev f32 [M], the rows' weights in what is minimised; a row of weight 0 has gradient 0
  * grad      : NULL (the loss alone), or dev [M][V] of the logits' type, rows grad_ld apart; may be `logits` itself (grad_ld = ld)
  * A row without entries has kl 0.  An index or label of V or more stores SD_ERR_BOUNDS and is left out.  Logits of minus infinity
- * are allowed (kl is infinite where the target gives one mass); NaN, or a row of minus infinity alone, gives NaN.  With the gradient
+ * are allowed (kl is infinite where the target gives one mass); NaN, a row of minus infinity alone, or one whose
+ * largest |logit * inv_temp| is beyond 1e38 gives NaN.  With the gradient
  * in the same call the logits are read once.
  */
 sd_status sd_distill_loss(const void *logits, int32_t dtype, int64_t ld, int32_t M, int32_t V,

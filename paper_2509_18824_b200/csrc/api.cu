@@ -330,7 +330,7 @@ sd_status sd_top_logits(const void* logits, int32_t dtype, int64_t ld, int32_t M
     if (K > 1024) return SD_ERR_UNSUPPORTED;
     if (M == 0) return SD_OK;
     if (!values || !index || !ok_4(values) || !ok_4(index) || !ok_4(lse) || !dev_status) return SD_ERR_INVALID_ARG;
-    return launch_top_logits(logits, dtype, ld, M, V, K, inv_temp, values, index, lse, static_cast<cudaStream_t>(stream));
+    return launch_top_logits(logits, dtype, ld, M, V, K, inv_temp, values, index, lse, dev_status, static_cast<cudaStream_t>(stream));
 }
 
 sd_status sd_sample_logits(const void* logits, int32_t dtype, int64_t ld, int32_t M, int32_t V, const sd_sampling* how,

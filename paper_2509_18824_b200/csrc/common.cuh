@@ -160,7 +160,7 @@ sd_status launch_lmhead_accept_sampled_compact(const sd_batch& bt, const void* h
 
 // rows of logits (sample.cu, distill.cu)
 sd_status launch_top_logits(const void* logits, int dtype, long long ld, int M, int V, int K, float inv_temp, float* values, int32_t* index,
-                            float* lse, cudaStream_t st);
+                            float* lse, int32_t* dev_status, cudaStream_t st);
 sd_status launch_sample(const void* logits, int dtype, long long ld, int M, int V, const sd_sampling& how, const float* u, int N, int32_t* tokens,
                         float* prob, float* dense, bool scaled, float* lse, int32_t* kept, int32_t* dev_status, cudaStream_t st);
 struct DistillCall {

@@ -33,6 +33,11 @@ __device__ __forceinline__ Pair add2(Pair a, Pair b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(as_u64(a)), "l"(as_u64(b)));
     return as_pair(d);
 }
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(as_u64(a)), "l"(as_u64(b)));
+    return as_pair(d);
+}
 __device__ __forceinline__ Pair ex2(Pair a) { return Pair{ex2(a.x), ex2(a.y)}; }
 
 // largest over the warp (NaN left out), by one reduction of integers that are ordered as the values are
@@ -191,30 +196,32 @@ __device__ __forceinline__ float warp_fmax(float v) {
     return v;
 }
 
-// Inclusive sums of a[0..n), n <= 2 * kThreads, in place and in a fixed order.  `tmp`: kWarps values.
+// Inclusive sums of a[0..n), n <= kListMax, in place and in a fixed order.  `tmp`: kWarps values.
+constexpr int kListMax = 2 * kThreads;
 template <typename S>
-__device__ void block_scan(S* a, int n, S* tmp) {
+static __device__ __noinline__ void block_scan(S* a, int n, S* tmp) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, i = 2 * tid;
     __syncthreads();
-    const S x = i < n ? a[i] : S(0), y = i + 1 < n ? a[i + 1] : S(0);
-    S s = x + y;
+    const S x = i < n ? a[i] : S(0), y = x + (i + 1 < n ? a[i + 1] : S(0));
+    S incl = y;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
-        const S o = __shfl_up_sync(0xffffffffu, s, d);
-        if (lane >= d) s += o;
+        const S o = __shfl_up_sync(0xffffffffu, incl, d);
+        if (lane >= d) incl += o;
     }
-    if (lane == 31) tmp[warp] = s;
+    if (lane == 31) tmp[warp] = incl;
     __syncthreads();
     S before = S(0);
-    for (int w = 0; w < warp; ++w) before += tmp[w];
-    const S own = __shfl_up_sync(0xffffffffu, s, 1);
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) before += w < warp ? tmp[w] : S(0);
+    const S own = __shfl_up_sync(0xffffffffu, incl, 1);
     if (lane > 0) before += own;
     if (i < n) a[i] = before + x;
-    if (i + 1 < n) a[i + 1] = before + x + y;
+    if (i + 1 < n) a[i + 1] = before + y;
     __syncthreads();
 }
 
-// a[0..n) in ascending order; n <= 1024, room for the next power of two.
+// a[0..n) in ascending order; n <= kListMax, room for the next power of two.
 static __device__ __noinline__ void block_sort(uint64_t* a, int n) {
     const int tid = threadIdx.x;
     int size = 32;

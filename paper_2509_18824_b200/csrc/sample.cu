@@ -1,70 +1,145 @@
 // Top logits, filtered sampling and filtered logits of rows [M][V] (sd_top_logits, sd_sample_logits, sd_filter_logits).
 //
-// One cluster of `parts` CTAs per row; every warp reads one consecutive piece of it.  A row is read once: a warp keeps what its
-// lanes see above a threshold that only rises (at least `keep` entries are known to reach it), so that of 152064 entries a few
-// hundred ever enter the list in shared memory, and where the row's whole mass is needed it is summed up beside that, one sum
-// per chunk of kU * 32 vectors.  The lists meet in the first CTA, are cut to the `keep` first entries in order and sorted; on
-// the sorted list top-k, top-p and min-p are prefix lengths.  Only where a border lies behind the listed entries (flat rows)
-// the row is read again (it is in L2 by then): histograms of counts and masses, over the cluster's CTAs, narrow the border down to
-// one entry.  The draw is by inverse CDF in vocabulary order: over the list, or over the chunks' sums and then one chunk.
+// One cluster of `parts` CTAs per row, each with a slice of it in its shared memory (bulk copies; 152064 f32 are eight slices of
+// 76 KB, two of which share an SM): a row is read once, and passed over as often as it takes.  Which entries stay is decided on a
+// list of some hundred entries that the first CTA collects and sorts:
+//   top-k up to kFewK   entries that reach the k-th largest of 128 groups' largest logits
+//   other borders       histograms of the row in bins of a sixteenth of a factor of two below its largest logit, counts and (to 1e-4)
+//                       masses: the bins in which the borders lie are listed, and if there are few, all that is above them
+// With all kept entries listed, the borders are prefix lengths of the sorted list and the draws are among its entries.  Otherwise (flat
+// rows) the list gives the last entry that stays, and the mass above the listed bins is summed up, in 64 bits, chunk by chunk (32 * kU
+// consecutive vectors); a draw looks up the chunk and then the entry.  Lists that overflow (thousands of nearly equal logits) are
+// narrowed down by further histograms over the keys.
+// (Lists kept in a single pass over global memory, with a threshold that rises, took three times as long: their cutting and their
+// barriers, 12 of 30 us for one row, and for flat rows four passes through L2.)
 #include <limits.h>
 #include "rows.cuh"
 
 namespace sdv {
 namespace rows {
 
-constexpr int kKeepMax = 1024;         // entries of a sorted list
-constexpr int kCap = 8192;             // entries that a CTA's list holds before it is cut
-constexpr int kU = 4;                  // vectors in flight per lane
-constexpr int kMaxChunks = 1024;       // of a row: 2^18 entries in chunks of 512, and one broken one for each of 128 warps
+constexpr int kFewK = 112;             // of 128 groups: with k near 128 the threshold would be the least of them, and the list long
+constexpr int kGroups = 128;
+constexpr int kU = 4;                  // vectors per lane and chunk
+constexpr int kMaxChunks = 128;        // of a CTA
 constexpr int kBins = 1024;
-
-struct Plan {                          // what the first CTA found out about its row
-    int kind;                          // kNone: no entry left; kList: the kept entries are listed; kWide: they are not
-    int n;                             // entries kept (kList)
-    int ref;
-    float top;                         // largest logit
-    double total;                      // mass of the kept entries (kList)
-};
-enum { kNone, kList, kWide };
+constexpr int kPieces = 4;             // copies of a slice: four warps' vectors each
+constexpr int kComparePairs = 96;      // kept entries up to which the draw compares all pairs instead of sorting again
+constexpr double kUnit = 8796093022208.0;          // 2^43: masses as whole numbers
+enum { kNone, kList, kWide };          // no entry left; the kept entries are listed; they are those up to a border
 
 struct RowShared {
+    uint64_t bar[kPieces];
+    int abort_flag;
     uint32_t n;                        // entries in the list
-    float thr;                         // a logit that at least `keep` entries seen so far reach
-    uint64_t thr_key;                  // and the key of the last of them, where it is known
     uint32_t hist[256];
     uint64_t sel_prefix;
     uint32_t sel_left;
     int sel_done;
-    float wmax[kWarps], wsum[kWarps];
+    float wtop[kWarps], wsum[kWarps];
     int wcnt[kWarps];
-    float cta_top, cta_sum;
-    int cta_count;
     double tmp_d[kWarps];
     uint64_t tmp_u[kWarps];
-    uint64_t lo[kWarps], hi[kWarps], cta_lo, cta_hi;
+    uint64_t lo[kWarps], hi[kWarps];
+    float groups[kGroups];
+    float thr;
     struct { uint32_t bin, n; uint64_t count, mass; } pick;      // a bin, the entries in it, and what stands in front of it
+    int found[64];                     // draws
+    // what the CTAs of a row read of each other
+    float group_top[kGroups], cta_top, cta_sum;
+    uint32_t cta_n;
+    uint64_t cta_lo, cta_hi;
+    double cta_mid;
+    int cta_count;
+    double chunk[kMaxChunks];          // sums of this CTA's chunks
+    uint64_t list[kListMax];
+    union {
+        struct { uint32_t count[kBins], mass[kBins]; } bins;     // of this CTA
+        uint64_t other[kListMax];
+    };
+    // what the first CTA tells the others
+    int kind, kept;
     uint64_t border, border_mass;
-    Plan plan;
-    double chunk[kMaxChunks];          // sums of this CTA's chunks, relative to 2^chunk_ref
-    int chunk_ref[kMaxChunks];
-    double all[kMaxChunks];            // the row's
+    double total;
+    // the row's, in every CTA: bins, or in the first one chunks or the list's masses, as inclusive sums
+    union { double all[kListMax]; uint64_t all_u[kListMax]; };
+    uint32_t all_count[kBins];
+};
+
+// ---------------------------------------------------------------- a slice of a row
+template <typename T>
+struct Slice {
+    static constexpr int E = Row<T>::kE;
+    Row<T> row;
+    uint4* data;
+    int parts, rank, per, v0, nv, first, seg, iters;       // first: index in the row of the slice's first entry (negative where the row starts inside it)
+    __device__ __forceinline__ Slice(const void* base, long long ld, long long r, int V, int parts_, int rank_, uint4* data_)
+        : row(base, ld, r, V), data(data_), parts(parts_), rank(rank_) {
+        per = (row.nvec + parts - 1) / parts;
+        v0 = min(row.nvec, rank * per);
+        nv = min(row.nvec, v0 + per) - v0;
+        first = v0 * E - row.lead;
+        seg = (per + kWarps - 1) / kWarps;                                         // a warp's consecutive vectors (the same in all parts)
+        iters = (seg + 32 * kU - 1) / (32 * kU);                                   // its chunks
+    }
+    __device__ __forceinline__ void copy(RowShared& sh, int withheld) const {      // by the whole CTA; the caller's barrier settles the edges
+        const int tid = threadIdx.x;
+        if (tid == 0) {
+            const uint64_t pol = sm100::policy_evict_first();
+            for (int q = 0; q < kPieces; ++q) {
+                const int a0 = v0 + min(nv, q * (kWarps / kPieces) * seg), a1 = v0 + min(nv, (q + 1) * (kWarps / kPieces) * seg);
+                const int i0 = max(row.full0, a0), i1 = min(row.full1, a1);
+                const uint32_t bytes = i1 > i0 ? (uint32_t)(i1 - i0) * 16 : 0;
+                sm100::mbar_arrive_expect_tx(&sh.bar[q], bytes + withheld);
+                if (bytes)
+                    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;"
+                                 ::"r"(sm100::smem_u32(data + (i0 - v0))), "l"(row.vec + i0), "r"(bytes), "r"(sm100::smem_u32(&sh.bar[q])), "l"(pol) : "memory");
+            }
+        }
+        if (tid == 32 && row.full0 > 0 && v0 == 0 && nv > 0) data[0] = row.edge(0);
+        const int e = row.nvec - 1;
+        if (tid == 64 && e >= max(row.full0, row.full1) && e >= v0 && e < v0 + nv) data[e - v0] = row.edge(e);
+    }
+    // f(logit, index) for every entry that is not masked
+    template <typename F>
+    __device__ __forceinline__ void each(F f) const {
+#pragma unroll 2
+        for (int i = (int)threadIdx.x; i < nv; i += kThreads) {
+            float x[E];
+            Row<T>::unpack(data[i], x);
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (x[e] > -INFINITY) f(x[e], first + i * E + e);
+        }
+    }
+    // the chunk that entry `index` of the row belongs to, counted over the parts
+    __device__ __forceinline__ int chunk_of(int index) const {
+        const int v = (index + row.lead) / E, q = v / per, i = v - q * per, w = i / seg;
+        return (q * kWarps + w) * iters + (i - w * seg) / (32 * kU);
+    }
 };
 
 // ---------------------------------------------------------------- cutting a list down
-// Leaves the `keep` first of buf[0..n) in buf[0..keep), in any order, and their last key in thr_key (keep < n <= kCap).  Radix
-// selection from the highest bit in which the keys differ.
-__device__ void cut_list(RowShared& sh, uint64_t* buf, int n, int keep) {
+// Leaves the `keep` first of buf[0..n) in buf[0..keep), in any order (keep < n <= kListMax).  Radix selection from the highest bit
+// in which the keys differ.
+__device__ __noinline__ void cut_list(RowShared& sh, uint64_t* buf, int n, int keep) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    constexpr int kPer = kListMax / kThreads;
     __syncthreads();
-    uint64_t lo = ~0ull, hi = 0;
-    for (int i = tid; i < n; i += kThreads) { const uint64_t k = buf[i]; lo = min(lo, k); hi = max(hi, k); }
+    uint64_t mine[kPer], lo = ~0ull, hi = 0;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        const int i = tid + j * kThreads;
+        mine[j] = i < n ? buf[i] : ~0ull;
+        if (i < n) { lo = min(lo, mine[j]); hi = max(hi, mine[j]); }
+    }
 #pragma unroll
     for (int d = 16; d >= 1; d >>= 1) {
         lo = min(lo, __shfl_xor_sync(0xffffffffu, lo, d));
         hi = max(hi, __shfl_xor_sync(0xffffffffu, hi, d));
     }
     if (lane == 0) { sh.lo[warp] = lo; sh.hi[warp] = hi; }
+    if (tid < 256) sh.hist[tid] = 0;
     __syncthreads();
     for (int w = 0; w < kWarps; ++w) { lo = min(lo, sh.lo[w]); hi = max(hi, sh.hi[w]); }
     // keys agree above bit `shift`; [prefix, prefix + 2^shift) holds the entry looked for
@@ -75,12 +150,9 @@ __device__ void cut_list(RowShared& sh, uint64_t* buf, int n, int keep) {
     while (shift > 0) {
         const int step = min(8, shift);
         const int down = shift - step;
-        if (tid < 256) sh.hist[tid] = 0;
-        __syncthreads();
-        for (int i = tid; i < n; i += kThreads) {
-            const uint64_t k = buf[i];
-            if (shift == 64 || (k >> shift) == (prefix >> shift)) atomicAdd(&sh.hist[(k >> down) & ((1u << step) - 1)], 1u);
-        }
+#pragma unroll
+        for (int j = 0; j < kPer; ++j)
+            if (tid + j * kThreads < n && (shift == 64 || (mine[j] >> shift) == (prefix >> shift))) atomicAdd(&sh.hist[(mine[j] >> down) & ((1u << step) - 1)], 1u);
         __syncthreads();
         if (warp == 0) {
             uint32_t s = 0;
@@ -107,203 +179,61 @@ __device__ void cut_list(RowShared& sh, uint64_t* buf, int n, int keep) {
         shift = down;
         last = prefix | (down == 0 ? 0 : (~0ull >> (64 - down)));
         if (sh.sel_done) break;
+        if (tid < 256) sh.hist[tid] = 0;
         __syncthreads();
     }
     // keys are distinct (the index is part of them): exactly `keep` are at or below `last`
-    constexpr int kPer = kCap / kThreads;
-    uint64_t mine[kPer];
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-        const int i = tid + j * kThreads;
-        mine[j] = i < n ? buf[i] : ~0ull;
-    }
-    __syncthreads();
     if (tid == 0) sh.n = 0;
     __syncthreads();
-    uint64_t worst = 0;
 #pragma unroll
     for (int j = 0; j < kPer; ++j)
-        if (mine[j] <= last && mine[j] != ~0ull) {
-            const uint32_t at = atomicAdd(&sh.n, 1u);
-            if (at < (uint32_t)kCap) buf[at] = mine[j];
-            worst = max(worst, mine[j]);
-        }
-#pragma unroll
-    for (int d = 16; d >= 1; d >>= 1) worst = max(worst, __shfl_xor_sync(0xffffffffu, worst, d));
-    if (lane == 0) sh.hi[warp] = worst;
-    __syncthreads();
-    if (tid == 0) {
-        for (int w = 1; w < kWarps; ++w) worst = max(worst, sh.hi[w]);
-        sh.thr_key = worst;
-        sh.thr = key_logit(worst);
-    }
+        if (tid + j * kThreads < n && mine[j] <= last) buf[atomicAdd(&sh.n, 1u)] = mine[j];
     __syncthreads();
 }
 
-// ---------------------------------------------------------------- the first pass
-// This CTA's part of the row: the entries that may be among its `keep` first ones into buf, the largest logit, and either the
-// chunks' masses (need_mass) or (LSE) the sum of exp((x - largest) inv_temp).
+// ---------------------------------------------------------------- largest logits
+// Waits for the slice; the largest logit of every group (4 * parts lanes) and of the CTA, and with LSE the sum of
+// 2^((x - cta_top) c).  Returns whether the copies came.
 template <typename T, bool LSE>
-__device__ void scan_part(RowShared& sh, uint64_t* buf, const Row<T>& row, int v0, int v1, int seg, int iters, int keep, bool need_mass,
-                          const Scale& sc, float c32) {
-    constexpr int E = Row<T>::kE;
+__device__ __forceinline__ bool first_pass(RowShared& sh, const Slice<T>& sl, float c, long long wait_cycles) {
+    constexpr int E = Slice<T>::E;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int w0 = min(v1, v0 + warp * seg), w1 = min(v1, w0 + seg);
-    if (tid == 0) { sh.n = 0; sh.thr = -INFINITY; sh.thr_key = ~0ull; }
-    __syncthreads();
-    float thr = -INFINITY, top = -INFINITY, sum = 0.f;
-    uint64_t thr_key = ~0ull;
-    uint32_t bound = 0;                                                            // entries in the list, at most
-    for (int it = 0; it < iters; ++it) {
-        uint4 raw[kU];
-#pragma unroll
-        for (int u = 0; u < kU; ++u) {
-            const int i = w0 + (it * kU + u) * 32 + lane;
-            raw[u] = i < w1 ? row.load(i) : Row<T>::nothing();
-        }
-        float m_lo = -INFINITY, m_hi = -INFINITY;                                  // largest of either half
-#pragma unroll
-        for (int u = 0; u < kU; ++u) {
-            float x[E];
-            Row<T>::unpack(raw[u], x);
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                if (u < kU / 2) m_lo = fmaxf(m_lo, x[e]);
-                else m_hi = fmaxf(m_hi, x[e]);
-            }
-        }
-        const float vmax = fmaxf(m_lo, m_hi);
-        if constexpr (LSE) {
-            const float now = fmaxf(top, vmax);
-            if (now > -INFINITY) {
-                sum *= ex2((top - now) * c32);
-#pragma unroll
-                for (int u = 0; u < kU; ++u) {
-                    float x[E];
-                    Row<T>::unpack(raw[u], x);
-#pragma unroll
-                    for (int e = 0; e < E; ++e) sum += ex2((fmaxf(x[e], -INFINITY) - now) * c32);
-                }
-            }
-        } else if (need_mass) {
-            const int ref = __reduce_max_sync(0xffffffffu, vmax > -INFINITY ? sc.whole(vmax) : INT_MIN);
-            double s = 0.0;
-            if (ref != INT_MIN) {
-#pragma unroll
-                for (int u = 0; u < kU; ++u) {
-                    float x[E];
-                    Row<T>::unpack(raw[u], x);
-#pragma unroll
-                    for (int e = 0; e < E; ++e) s += sc.mass(x[e], ref);
-                }
-                s = warp_add(s);
-            }
-            if (lane == 0) { sh.chunk[warp * iters + it] = s; sh.chunk_ref[warp * iters + it] = ref; }
-        }
-        top = fmaxf(top, vmax);
-        if (keep == 0) continue;
-        if (it == 0) {
-            // a first threshold: the least of as many groups' largest entries as there are entries to keep
-            float g = keep > kThreads ? fminf(m_lo, m_hi) : vmax;
-            for (int d = 1; d < 32 && (kThreads >> __ffs(d)) >= keep; d <<= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, d));
-#pragma unroll
-            for (int d = 16; d >= 1; d >>= 1) g = fminf(g, __shfl_xor_sync(0xffffffffu, g, d));
-            if (lane == 0) sh.wmax[warp] = g;
-            __syncthreads();
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) g = fminf(g, sh.wmax[w]);
-            thr = g;
-        }
-        bool any = vmax >= thr && vmax > -INFINITY;
-        uint32_t threads = __syncthreads_count(any);
-        bool one_by_one = false;
-        if (bound + threads * (kU * E) > (uint32_t)kCap) {
-            bound = sh.n;                                                          // (nothing is added until all have seen it)
-            __syncthreads();
-            if (bound > (uint32_t)max(2 * keep, 512) || bound + threads * (kU * E) > (uint32_t)kCap) {
-                if (bound > (uint32_t)keep) {
-                    cut_list(sh, buf, bound, keep);
-                    bound = keep;
-                    thr = sh.thr;
-                    thr_key = sh.thr_key;
-                    any = vmax >= thr && vmax > -INFINITY;
-                    threads = __syncthreads_count(any);
-                }
-                one_by_one = bound + threads * (kU * E) > (uint32_t)kCap;
-            }
-        }
-        if (threads == 0) continue;
-#pragma unroll
-        for (int u = 0; u < kU; ++u) {
-            if (any) {
-                float x[E];
-                Row<T>::unpack(raw[u], x);
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (x[e] >= thr && x[e] > -INFINITY) {
-                        const uint64_t key = order_key(x[e], (w0 + (it * kU + u) * 32 + lane) * E + e - row.lead);
-                        if (key <= thr_key) {
-                            const uint32_t at = atomicAdd(&sh.n, 1u);
-                            if (at < (uint32_t)kCap) buf[at] = key;
-                        }
-                    }
-            }
-            if (one_by_one) {                                                      // at most kThreads * E more each time
-                __syncthreads();
-                bound = sh.n;
-                __syncthreads();
-                if (bound > (uint32_t)(kCap - kThreads * E)) {
-                    cut_list(sh, buf, bound, keep);
-                    bound = keep;
-                    thr = sh.thr;
-                    thr_key = sh.thr_key;
-                }
-            }
-        }
-        if (!one_by_one) bound += threads * (kU * E);
-    }
-    // the CTA's largest logit, and sum
-    const float wtop = warp_fmax(top);
-    __syncthreads();
-    if (lane == 0) sh.wmax[warp] = wtop;
-    __syncthreads();
-    float all = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) all = fmaxf(all, sh.wmax[w]);
+    const bool ok = sm100::mbar_wait_warp(&sh.bar[warp / (kWarps / kPieces)], 0, &sh.abort_flag, wait_cycles);
+    const int w0 = min(sl.nv, warp * sl.seg), w1 = min(sl.nv, w0 + sl.seg);
+    float top = -INFINITY;
+#pragma unroll 4
+    for (int i = w0 + lane; i < w1; i += 32) top = Row<T>::largest(sl.data[i], top);
+    float g = top;
+    for (int d = 1; d < 4 * sl.parts; d <<= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, d));
+    if (lane % (4 * sl.parts) == 0) sh.group_top[tid / (4 * sl.parts)] = g;
+    top = warp_largest(top);
+    float s = 0.f;
     if constexpr (LSE) {
-        sum = top > -INFINITY ? sum * ex2((top - all) * c32) : 0.f;
-        sum = warp_add(sum);
-        if (lane == 0) sh.wsum[warp] = sum;
-        __syncthreads();
-        float s = 0.f;
+        const float from = top > -INFINITY ? top : 0.f;
+        Pair a{0.f, 0.f}, b{0.f, 0.f};
+#pragma unroll 2
+        for (int i = w0 + lane; i < w1; i += 32) {
+            Pair x[E / 2];
+            Row<T>::pairs(sl.data[i], x);
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) s += sh.wsum[w];
-        if (tid == 0) sh.cta_sum = s;
+            for (int e = 0; e < E / 2; e += 2) {
+                a = add2(a, ex2(mul2(add2(Pair{fmaxf(x[e].x, -INFINITY), fmaxf(x[e].y, -INFINITY)}, Pair{-from, -from}), Pair{c, c})));
+                b = add2(b, ex2(mul2(add2(Pair{fmaxf(x[e + 1].x, -INFINITY), fmaxf(x[e + 1].y, -INFINITY)}, Pair{-from, -from}), Pair{c, c})));
+            }
+        }
+        s = warp_add((a.x + a.y) + (b.x + b.y));
     }
-    if (tid == 0) sh.cta_top = all;
+    if (lane == 0) { sh.wtop[warp] = top; sh.wsum[warp] = s; }
     __syncthreads();
-}
-
-// The lists of all parts into the first CTA's, cut to the `keep` first entries and sorted (a list that travels holds at most
-// kCap / parts entries).  Returns the entries there are (in the first CTA).
-__device__ int meet(RowShared& sh, uint64_t* buf, int parts, int rank, int keep) {
-    const int tid = threadIdx.x;
-    __syncthreads();
-    const uint32_t have = sh.n;
-    if (have > (uint32_t)(kCap / parts) || (parts == 1 && have > (uint32_t)kKeepMax)) cut_list(sh, buf, min(have, (uint32_t)kCap), keep);
-    sync_parts(parts);
-    if (rank != 0) return 0;
-    int n = sh.n;
-    for (int r = 1; r < parts; ++r) {
-        const int more = *of_rank(&sh.n, r);
-        const uint64_t* from = of_rank(buf, r);
-        for (int i = tid; i < more; i += kThreads) buf[n + i] = from[i];
-        n += more;
+    if (warp == 0) {
+        const float t = lane < kWarps ? sh.wtop[lane] : -INFINITY, most = warp_largest(t);
+        if constexpr (LSE) {
+            s = lane < kWarps && t > -INFINITY ? sh.wsum[lane] * ex2((t - most) * c) : 0.f;
+            s = warp_add(s);
+        }
+        if (lane == 0) { sh.cta_top = most; sh.cta_sum = s; }
     }
-    __syncthreads();
-    if (n > kKeepMax) { cut_list(sh, buf, n, keep); n = keep; }
-    block_sort(buf, n);
-    return min(n, keep);
+    return ok;
 }
 
 // Largest logit over the parts (behind a sync_parts).
@@ -313,17 +243,59 @@ __device__ __forceinline__ float top_of_parts(RowShared& sh, int parts) {
     return top;
 }
 
-// The chunks of all parts as inclusive sums in sh.all, relative to 2^ref (behind a sync_parts).  Returns how many.
-__device__ int scan_chunks(RowShared& sh, int parts, int per_part, int ref) {
-    const int n = parts * per_part;
-    for (int i = threadIdx.x; i < n; i += kThreads) {
-        const int r = i / per_part, at = i - r * per_part;
-        const double s = *of_rank(&sh.chunk[at], r);
-        const int e = *of_rank(&sh.chunk_ref[at], r);
-        sh.all[i] = e == INT_MIN ? 0.0 : times_pow2(s, e - ref);
+// The k-th largest of the groups' largest logits, k <= kGroups: at least k entries reach it (behind a sync_parts).
+__device__ __forceinline__ float kth_group(RowShared& sh, int parts, int k) {
+    const int tid = threadIdx.x;
+    if (tid < kGroups) {
+        const int each = kGroups / parts;
+        sh.groups[tid] = *of_rank(&sh.group_top[tid % each], tid / each);
     }
-    block_scan(sh.all, n, sh.tmp_d);
+    __syncthreads();
+    if (tid < kGroups) {
+        const float mine = sh.groups[tid];
+        int before = 0;
+#pragma unroll 8
+        for (int g = 0; g < kGroups; ++g) before += sh.groups[g] > mine || (sh.groups[g] == mine && g < tid);
+        if (before == k - 1) sh.thr = mine;
+    }
+    __syncthreads();
+    return sh.thr;
+}
+
+// ---------------------------------------------------------------- lists
+// Entries that `wanted` names into this CTA's list; cta_n counts them, also those that find no room.
+template <typename T, typename F>
+__device__ __forceinline__ void list_entries(RowShared& sh, const Slice<T>& sl, F wanted) {
+    if (threadIdx.x == 0) sh.cta_n = 0;
+    __syncthreads();
+    sl.each([&](float x, int index) {
+        if (!wanted(x, index)) return;
+        const uint32_t at = atomicAdd(&sh.cta_n, 1u);
+        if (at < (uint32_t)kListMax) sh.list[at] = order_key(x, index);
+    });
+}
+// how many entries all parts have listed (behind a sync_parts)
+__device__ __forceinline__ uint32_t listed(RowShared& sh, int parts) {
+    uint32_t n = 0;
+    for (int r = 0; r < parts; ++r) n += *of_rank(&sh.cta_n, r);
     return n;
+}
+// All parts' entries into the first CTA's list (by the first CTA; they fit)
+__device__ void collect(RowShared& sh, int parts) {
+    int n = sh.cta_n;
+    for (int r = 1; r < parts; ++r) {
+        const int more = *of_rank(&sh.cta_n, r);
+        const uint64_t* from = of_rank(sh.list, r);
+        for (int i = threadIdx.x; i < more; i += kThreads) sh.list[n + i] = from[i];
+        n += more;
+    }
+    __syncthreads();
+}
+// The first CTA's list of n entries sorted, cut to the `keep` first ones where that is worth a pass; returns how many there are.
+__device__ int sort_list(RowShared& sh, int n, int keep) {
+    if (n > keep && n > 64) { cut_list(sh, sh.list, n, keep); n = keep; }
+    block_sort(sh.list, n);
+    return min(n, keep);
 }
 
 // first i with a[i] > t (n: none) or, with `or_equal`, a[i] >= t; a ascending
@@ -338,203 +310,177 @@ __device__ __forceinline__ int first_above(const S* a, int n, S t, bool or_equal
     return lo;
 }
 
+// ---------------------------------------------------------------- histograms
+// Bins of a sixteenth of a factor of two, counted from the largest logit; what is further off than 2^-64 shares the last.
+struct LinearBins {
+    float top, per_bin;
+    __device__ __forceinline__ LinearBins(float top_, const Scale& sc) : top(top_), per_bin((float)fmin(16.0 * sc.c, 3.0e38)) {}
+    __device__ __forceinline__ float distance(float x) const { return fminf((top - x) * per_bin, (float)(kBins - 1)); }
+    __device__ __forceinline__ int of(float x) const { return (int)distance(x); }
+};
+
+// Counts and masses of the row's bins, as inclusive sums in every CTA: all_count, and (masses) all, as multiples of the largest
+// entry's mass.  A bin's mass is summed up in units of 2^-16 of its upper end, in 32 bits (a slice has at most 2^15 + 8 entries): to
+// 2e-5 of it.  The last bin counts without mass.
 template <typename T>
-struct Part {                          // this CTA's share of a row
-    Row<T> row;
-    int parts, rank, v0, v1, seg, iters;
-    __device__ __forceinline__ Part(const void* base, long long ld, long long r, int V, int parts_, int rank_) : row(base, ld, r, V), parts(parts_), rank(rank_) {
-        const int per = (row.nvec + parts - 1) / parts;
-        v0 = min(row.nvec, rank * per);
-        v1 = min(row.nvec, v0 + per);
-        seg = (per + kWarps - 1) / kWarps;                                         // (the same in all parts: chunks are numbered alike)
-        iters = (seg + 32 * kU - 1) / (32 * kU);
-    }
-    template <typename F>
-    __device__ __forceinline__ void each(F f) const {                              // f(logit, index), entries of minus infinity and NaN left out
-        constexpr int E = Row<T>::kE;
-        for (int i = v0 + (int)threadIdx.x; i < v1; i += kThreads) {
-            const uint4 raw = row.load(i);
-            float x[E];
-            Row<T>::unpack(raw, x);
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (x[e] > -INFINITY) f(x[e], i * E + e - row.lead);
-        }
-    }
-};
-
-// ---------------------------------------------------------------- flat rows: the border by histograms
-// Counts and masses (2^-43 of 2^ref as the unit; whole numbers, so that the order of additions is of no matter) of
-// kBins bins, in buf; merged over the parts into inclusive sums.
-struct Bins {
-    uint32_t* count; uint64_t* mass;               // this CTA's
-    uint64_t* sum_count; uint64_t* sum_mass;       // of all parts
-    __device__ __forceinline__ explicit Bins(uint64_t* buf)
-        : count(reinterpret_cast<uint32_t*>(buf)), mass(buf + kBins / 2), sum_count(buf + 3 * kBins / 2), sum_mass(buf + 5 * kBins / 2) {}
-};
-constexpr int kListAt = 4096;                      // where lists start in buf while the bins are in use
-static_assert(7 * kBins / 2 <= kListAt && kListAt + kKeepMax <= kCap, "bins, then a list");
-
-__device__ __forceinline__ uint64_t unit_mass(const Scale& sc, float x, int ref) { return (uint64_t)(sc.mass(x, ref) * 8796093022208.0 + 0.5); }
-
-// bin_of(x, index): the entry's bin, or -1
-template <typename T, typename F>
-__device__ void fill_bins(RowShared& sh, const Bins& b, const Part<T>& part, bool masses, const Scale& sc, int ref, F bin_of) {
-    const int tid = threadIdx.x;
-    sync_parts(part.parts);                        // (nobody reads the bins any more)
-    for (int i = tid; i < kBins; i += kThreads) { b.count[i] = 0; b.mass[i] = 0; }
-    __syncthreads();
-    part.each([&](float x, int index) {
-        const int bin = bin_of(x, index);
-        if (bin < 0) return;
-        atomicAdd(&b.count[bin], 1u);
-        if (masses) atomicAdd(reinterpret_cast<unsigned long long*>(&b.mass[bin]), (unsigned long long)unit_mass(sc, x, ref));
-    });
-    sync_parts(part.parts);
-    for (int i = tid; i < kBins; i += kThreads) {
-        uint64_t c = 0, m = 0;
-        for (int r = 0; r < part.parts; ++r) {
-            c += *of_rank(&b.count[i], r);
-            if (masses) m += *of_rank(&b.mass[i], r);
-        }
-        b.sum_count[i] = c;
-        b.sum_mass[i] = m;
-    }
-    block_scan(b.sum_count, kBins, sh.tmp_u);
-    block_scan(b.sum_mass, kBins, sh.tmp_u);
-}
-
-// The bin in which the counts (or masses) reach `target`, at least 1 and at most their sum.
-__device__ void pick_bin(RowShared& sh, const Bins& b, bool by_mass, uint64_t target) {
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        const uint64_t* sums = by_mass ? b.sum_mass : b.sum_count;
-        const int bin = min(first_above(sums, kBins, target, true), kBins - 1);
-        sh.pick.bin = bin;
-        sh.pick.count = bin ? b.sum_count[bin - 1] : 0;
-        sh.pick.mass = bin ? b.sum_mass[bin - 1] : 0;
-        sh.pick.n = (uint32_t)(b.sum_count[bin] - sh.pick.count);
-    }
-    __syncthreads();
-}
-
-// The last entry, in order, of the shortest prefix whose count (or mass) is at least `target`: its key, and the mass up to and
-// with it.  The bins hold the row's linear histogram with pick_bin's answer in sh.pick; they are used up.
-template <typename T, typename F>
-__device__ void find_border(RowShared& sh, uint64_t* buf, const Bins& b, const Part<T>& part, bool by_mass, bool masses, uint64_t target,
-                            const Scale& sc, int ref, F linear_bin, uint64_t* border, uint64_t* border_mass) {
+__device__ void fill_bins(RowShared& sh, const Slice<T>& sl, bool masses, const LinearBins& lin) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int bin = sh.pick.bin;
-    uint64_t before_n = sh.pick.count, before_m = sh.pick.mass;
-    uint32_t n = sh.pick.n;
-    uint64_t lo = 0, hi = ~0ull;                   // and among the bin's entries those with keys in [lo, hi]
-    if (n > (uint32_t)kKeepMax) {
-        // more than a list holds: equal or nearly equal logits.  The range of the keys, then bins of equal widths in it.
-        uint64_t l = ~0ull, h = 0;
-        part.each([&](float x, int index) {
-            if (linear_bin(x) != bin) return;
-            const uint64_t k = order_key(x, index);
-            l = min(l, k);
-            h = max(h, k);
+    sync_parts(sl.parts);                          // (nobody reads the last ones any more)
+    for (int i = tid; i < kBins; i += kThreads) { sh.bins.count[i] = 0; sh.bins.mass[i] = 0; }
+    __syncthreads();
+    if (masses)
+        sl.each([&](float x, int) {
+            const float d = lin.distance(x);
+            const int bin = (int)d;
+            atomicAdd(&sh.bins.count[bin], 1u);
+            if (bin < kBins - 1) atomicAdd(&sh.bins.mass[bin], (uint32_t)fmaf(ex2(((float)bin - d) * 0.0625f), 65536.f, 0.5f));
         });
+    else
+        sl.each([&](float x, int) { atomicAdd(&sh.bins.count[lin.of(x)], 1u); });
+    sync_parts(sl.parts);
+    for (int i = tid; i < kBins; i += kThreads) {
+        uint32_t c = 0;
+        double m = 0.0;
+        for (int r = 0; r < sl.parts; ++r) {
+            c += *of_rank(&sh.bins.count[i], r);
+            if (masses) m += (double)*of_rank(&sh.bins.mass[i], r);
+        }
+        sh.all_count[i] = c;
+        sh.all[i] = m * (double)exp2f((float)i * -0.0625f) * (1.0 / 65536.0);
+    }
+    if (masses) block_scan(sh.all, kBins, sh.tmp_d);
+    // the counts: two per thread
+    __syncthreads();
+    const uint32_t x = sh.all_count[2 * tid], y = x + sh.all_count[2 * tid + 1];
+    uint32_t incl = y;
 #pragma unroll
-        for (int d = 16; d >= 1; d >>= 1) {
-            l = min(l, __shfl_xor_sync(0xffffffffu, l, d));
-            h = max(h, __shfl_xor_sync(0xffffffffu, h, d));
-        }
-        if (lane == 0) { sh.lo[warp] = l; sh.hi[warp] = h; }
-        __syncthreads();
-        if (tid == 0) {
-            for (int w = 1; w < kWarps; ++w) { l = min(l, sh.lo[w]); h = max(h, sh.hi[w]); }
-            sh.cta_lo = l;
-            sh.cta_hi = h;
-        }
-        sync_parts(part.parts);
-        lo = ~0ull;
-        hi = 0;
-        for (int r = 0; r < part.parts; ++r) { lo = min(lo, *of_rank(&sh.cta_lo, r)); hi = max(hi, *of_rank(&sh.cta_hi, r)); }
-        while (n > (uint32_t)kKeepMax) {           // (keys differ: a range of up to kBins keys leaves one entry to a bin)
-            const int bits = 64 - __clzll((long long)(hi - lo));
-            const int shift = max(0, bits - 10);
-            fill_bins(sh, b, part, masses, sc, ref, [&](float x, int index) {
-                if (linear_bin(x) != bin) return -1;
-                const uint64_t k = order_key(x, index);
-                return k >= lo && k <= hi ? (int)((k - lo) >> shift) : -1;
-            });
-            pick_bin(sh, b, by_mass, target - (by_mass ? before_m : before_n));
-            before_n += sh.pick.count;
-            before_m += sh.pick.mass;
-            n = sh.pick.n;
-            lo += (uint64_t)sh.pick.bin << shift;
-            hi = lo + ((1ull << shift) - 1);
-        }
+    for (int d = 1; d < 32; d <<= 1) {
+        const uint32_t o = __shfl_up_sync(0xffffffffu, incl, d);
+        if (lane >= d) incl += o;
     }
-    // the few that are left: listed, sorted, and counted or summed up
-    uint64_t* list = buf + kListAt;
+    if (lane == 31) sh.wcnt[warp] = incl;
     __syncthreads();
-    if (tid == 0) sh.n = 0;
+    uint32_t before = incl - y;
+    for (int w = 0; w < warp; ++w) before += sh.wcnt[w];
+    sh.all_count[2 * tid] = before + x;
+    sh.all_count[2 * tid + 1] = before + y;
     __syncthreads();
-    part.each([&](float x, int index) {
-        if (linear_bin(x) != bin) return;
-        const uint64_t k = order_key(x, index);
-        if (k >= lo && k <= hi) {
-            const uint32_t at = atomicAdd(&sh.n, 1u);
-            if (at < (uint32_t)kKeepMax) list[at] = k;
-        }
+}
+
+// ---------------------------------------------------------------- the general search for a border
+// For rows whose border bin holds more than a list does (equal or nearly equal logits): whole-number counts or masses (2^-43 of 2^ref
+// as the unit) in bins over ranges of keys, until a list holds what is left.  Slow (a pass and two barriers of the cluster per round of
+// ten bits), and right for everything.
+template <typename T, typename F>
+__device__ void key_bins(RowShared& sh, const Slice<T>& sl, bool by_mass, const Scale& sc, int ref, F bin_of) {
+    const int tid = threadIdx.x;
+    sync_parts(sl.parts);
+    for (int i = tid; i < kBins; i += kThreads) sh.other[i] = 0;
+    __syncthreads();
+    sl.each([&](float x, int index) {
+        const int bin = bin_of(x, index);
+        if (bin >= 0) atomicAdd(reinterpret_cast<unsigned long long*>(&sh.other[bin]), by_mass ? (unsigned long long)(sc.mass(x, ref) * kUnit + 0.5) : 1ull);
     });
-    sync_parts(part.parts);
-    if (part.rank == 0) {
-        int m = min(sh.n, (uint32_t)kKeepMax);
-        for (int r = 1; r < part.parts; ++r) {
-            const int more = min(*of_rank(&sh.n, r), (uint32_t)(kKeepMax - m));
-            const uint64_t* from = of_rank(list, r);
-            for (int i = tid; i < more; i += kThreads) list[m + i] = from[i];
-            m += more;
-        }
-        block_sort(list, m);
-        uint64_t* sums = b.sum_mass;               // (its histogram is not needed any more)
-        for (int i = tid; i < m; i += kThreads) sums[i] = unit_mass(sc, key_logit(list[i]), ref);
-        block_scan(sums, m, sh.tmp_u);
-        if (tid == 0) {
-            int j = by_mass ? first_above(sums, m, target - before_m, true) : (int)(target - before_n) - 1;
-            j = max(0, min(j, m - 1));
-            sh.border = list[j];
-            sh.border_mass = before_m + sums[j];
-        }
+    sync_parts(sl.parts);
+    for (int i = tid; i < kBins; i += kThreads) {
+        uint64_t c = 0;
+        for (int r = 0; r < sl.parts; ++r) c += *of_rank(&sh.other[i], r);
+        sh.all_u[i] = c;
     }
-    sync_parts(part.parts);
-    *border = *of_rank(&sh.border, 0);
-    *border_mass = *of_rank(&sh.border_mass, 0);
+    block_scan(sh.all_u, kBins, sh.tmp_u);
+}
+// The key of the last entry, in order, of the shortest prefix whose count (or mass) is at least `target`, and the count or mass with it.
+// share: take target as that share of the sum over the keys up to `upto` instead.
+template <typename T>
+__device__ void search_border(RowShared& sh, const Slice<T>& sl, bool by_mass, uint64_t target, double share, uint64_t upto, const Scale& sc, int ref,
+                              uint64_t* border) {
+    const int tid = threadIdx.x;
+    uint64_t lo = 0, hi = upto, before = 0;
+    bool first = true;
+    while (true) {
+        const int bits = hi == lo ? 0 : 64 - __clzll((long long)(hi - lo)), shift = max(0, bits - 10);
+        key_bins(sh, sl, by_mass, sc, ref, [&](float x, int index) {
+            const uint64_t k = order_key(x, index);
+            return k >= lo && k <= hi ? (int)((k - lo) >> shift) : -1;
+        });
+        if (first && share >= 0.0) target = max((uint64_t)1, (uint64_t)ceil(share * (double)sh.all_u[kBins - 1]));
+        first = false;
+        const int bin = min(first_above(sh.all_u, kBins, target - before, true), kBins - 1);
+        before += bin ? sh.all_u[bin - 1] : 0;
+        lo += (uint64_t)bin << shift;
+        hi = lo + (shift ? (1ull << shift) - 1 : 0);
+        if (shift == 0) break;                     // one key
+    }
+    *border = lo;
 }
 
 // ---------------------------------------------------------------- top logits
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 2)
-top_kernel(const void* logits, long long ld, int V, int parts, int K, float inv_temp, float* values, int32_t* index, float* lse) {
-    extern __shared__ __align__(16) uint64_t buf[];
+top_kernel(const void* logits, long long ld, int V, int parts, int K, float inv_temp, float* values, int32_t* index, float* lse, int32_t* status,
+           int withheld, long long wait_cycles) {
+    extern __shared__ __align__(16) uint4 data[];
     __shared__ RowShared sh;
-    begin_dependent(logits, values, index, lse);
+    const int tid = threadIdx.x;
+    if (tid == 0) {
+        sh.abort_flag = 0;
+        for (int q = 0; q < kPieces; ++q) sm100::mbar_init(&sh.bar[q], 1);
+        sm100::fence_barrier_init();
+    }
+    __syncthreads();
+    begin_dependent(logits, values, index, lse, status);
     const long long r = blockIdx.x / parts;
     const int rank = parts == 1 ? 0 : (int)sm100::cluster_ctarank();
-    const Part<T> part(logits, ld, r, V, parts, rank);
-    const float c32 = inv_temp * kLog2e;
-    scan_part<T, true>(sh, buf, part.row, part.v0, part.v1, part.seg, part.iters, K, false, Scale(1.f), c32);
-    const int n = meet(sh, buf, parts, rank, K);
-    if (rank == 0) {
-        for (int i = threadIdx.x; i < K; i += kThreads) {
-            values[r * K + i] = i < n ? key_logit(buf[i]) : -INFINITY;
-            index[r * K + i] = i < n ? key_index(buf[i]) : -1;
+    const Slice<T> sl(logits, ld, r, V, parts, rank, data);
+    sl.copy(sh, withheld);
+    __syncthreads();
+    const float c = inv_temp * kLog2e;
+    const bool ok = first_pass<T, true>(sh, sl, c, wait_cycles);
+    sync_parts(parts);
+    const float top = top_of_parts(sh, parts);
+    uint32_t n = kListMax + 1;
+    if (K <= kFewK) {
+        const float thr = kth_group(sh, parts, K);
+        list_entries(sh, sl, [&](float x, int) { return x >= thr; });
+        sync_parts(parts);
+        n = listed(sh, parts);
+    }
+    if (n > (uint32_t)kListMax && top > -INFINITY) {
+        const LinearBins lin(top, Scale(1.f));
+        fill_bins(sh, sl, false, lin);
+        const int bin = min(first_above(sh.all_count, kBins, (uint32_t)K, true), kBins - 1);
+        n = sh.all_count[bin];
+        if (n <= (uint32_t)kListMax) {
+            list_entries(sh, sl, [&](float x, int) { return lin.of(x) <= bin; });
+        } else {
+            uint64_t border = ~0ull;
+            if (sh.all_count[kBins - 1] > (uint32_t)K) search_border(sh, sl, false, (uint64_t)K, -1.0, ~0ull, Scale(1.f), 0, &border);
+            sync_parts(parts);
+            list_entries(sh, sl, [&](float x, int i) { return order_key(x, i) <= border; });
         }
-        if (lse && threadIdx.x == 0) {
-            const float top = top_of_parts(sh, parts);
+        sync_parts(parts);
+    }
+    if (rank == 0) {
+        int have = 0;
+        if (top > -INFINITY) {
+            collect(sh, parts);
+            have = sort_list(sh, min(listed(sh, parts), (uint32_t)kListMax), K);
+        }
+        for (int i = tid; i < K; i += kThreads) {
+            values[r * K + i] = i < have ? key_logit(sh.list[i]) : -INFINITY;
+            index[r * K + i] = i < have ? key_index(sh.list[i]) : -1;
+        }
+        if (lse && tid == kThreads - 1) {
             float s = 0.f;
             for (int q = 0; q < parts; ++q) {
                 const float t = *of_rank(&sh.cta_top, q);
-                if (t > -INFINITY) s += *of_rank(&sh.cta_sum, q) * ex2((t - top) * c32);
+                if (t > -INFINITY) s += *of_rank(&sh.cta_sum, q) * ex2((t - top) * c);
             }
-            lse[r] = top > -INFINITY && top < INFINITY ? (float)((double)top * inv_temp + log((double)s)) : top;
+            lse[r] = top > -INFINITY && top < INFINITY ? (float)((double)top * (double)inv_temp + log((double)s)) : top;
         }
     }
+    if (!ok) { set_status(status, SD_ERR_TIMEOUT); sm100::unwind_pause(); }
+    __syncwarp();
     if (parts > 1) sync_parts(parts);                                              // nobody leaves while the first CTA reads
 }
 
@@ -545,27 +491,65 @@ struct SampleCall {
     const float* u; int N; int32_t* tokens; float* prob;       // draws (N = 0: none)
     float* dense; bool scaled;                                 // [M][V]: probabilities, or (scaled) the kept logits times inv_temp
     float* lse; int32_t* kept; int32_t* status;
+    int withheld; long long wait_cycles;
 };
 
-// The entry of a chunk at which the mass in vocabulary order exceeds `over`; kept(x, index): whether an entry counts.  A warp
-// calls it.  Sums that fall short by rounding end at the last entry with mass.
+// Sums of the slice's chunks, relative to 2^ref, of the entries that `in` names; f sees every entry and its mass.
+template <typename T, typename I, typename F>
+__device__ __forceinline__ void sum_chunks(RowShared& sh, const Slice<T>& sl, const Scale& sc, int ref, I in, F f) {
+    constexpr int E = Slice<T>::E;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int w0 = min(sl.nv, warp * sl.seg), w1 = min(sl.nv, w0 + sl.seg);
+    for (int c = 0; c < sl.iters; ++c) {
+        double s = 0.0, t = 0.0;
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+            const int i = w0 + (c * kU + u) * 32 + lane;
+            if (i >= w1) break;
+            float x[E];
+            Row<T>::unpack(sl.data[i], x);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const double m = sc.mass(x[e], ref);
+                f(x[e], sl.first + i * E + e, m);
+                (e & 1 ? t : s) += in(x[e], m) ? m : 0.0;
+            }
+        }
+        s = warp_add(s + t);
+        if (lane == 0) sh.chunk[warp * sl.iters + c] = s;
+    }
+}
+
+// The entry of a chunk at which the mass in vocabulary order exceeds `over`; kept(x, index, mass): whether an entry counts.  A warp
+// calls it; the chunk may lie in another CTA's slice.  Sums that fall short by rounding end at the last entry with mass.
 template <typename T, typename F>
-__device__ int chunk_crossing(const Part<T>& part, int warp_of, int it, double over, const Scale& sc, int ref, F kept, double* its_mass) {
-    constexpr int E = Row<T>::kE;
-    const int lane = threadIdx.x & 31;
-    const int w0 = min(part.v1, part.v0 + warp_of * part.seg), w1 = min(part.v1, w0 + part.seg);
+__device__ int chunk_crossing(const Slice<T>& sl, int g, double over, const Scale& sc, int ref, F kept, double* its_mass) {
+    constexpr int E = Slice<T>::E;
+    const int lane = threadIdx.x & 31, per_part = kWarps * sl.iters, q = g / per_part, at = g - q * per_part, w = at / sl.iters, c = at - w * sl.iters;
+    const uint4* data = sl.parts > 1 ? of_rank(sl.data, q) : sl.data;
+    const int v0 = min(sl.row.nvec, q * sl.per), nv = min(sl.row.nvec, v0 + sl.per) - v0, first = v0 * E - sl.row.lead;
+    const int w0 = min(nv, w * sl.seg), w1 = min(nv, w0 + sl.seg);
+    uint4 raw[kU];
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+        const int i = w0 + (c * kU + u) * 32 + lane;
+        raw[u] = i < w1 ? data[i] : Row<T>::nothing();
+    }
     double before = 0.0, last_mass = 0.0;
     int last = -1;
+#pragma unroll 1
     for (int u = 0; u < kU; ++u) {
-        const int i = w0 + (it * kU + u) * 32 + lane;
-        const uint4 raw = i < w1 ? part.row.load(i) : Row<T>::nothing();
+        const int i = w0 + (c * kU + u) * 32 + lane;
+        uint4 now = raw[0];
+#pragma unroll
+        for (int j = 1; j < kU; ++j) if (u == j) now = raw[j];
         float x[E];
-        Row<T>::unpack(raw, x);
+        Row<T>::unpack(now, x);
         double m[E], s = 0.0;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const int index = i * E + e - part.row.lead;
-            m[e] = x[e] > -INFINITY && kept(x[e], index) ? sc.mass(x[e], ref) : 0.0;
+            m[e] = sc.mass(x[e], ref);
+            if (!kept(x[e], first + i * E + e, m[e])) m[e] = 0.0;
             s += m[e];
         }
         double incl = s;
@@ -583,7 +567,7 @@ __device__ int chunk_crossing(const Part<T>& part, int warp_of, int it, double o
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             run += m[e];
-            if (m[e] > 0.0 && !crossed) { found = i * E + e - part.row.lead; found_mass = m[e]; crossed = run > over; }
+            if (m[e] > 0.0 && !crossed) { found = first + i * E + e; found_mass = m[e]; crossed = run > over; }
         }
         if (over_here | with_mass) {
             const int src = over_here ? __ffs(over_here) - 1 : 31 - __clz(with_mass);
@@ -614,244 +598,411 @@ __device__ void fill_floats(float* dst, int n, float value) {
     if (tid < n - lead - vecs * 4) dst[lead + vecs * 4 + tid] = value;
 }
 
+// Draws among the `kept` first entries of the sorted list (by the first CTA; sh.all: the list's masses as inclusive sums)
+__device__ void draw_from_list(RowShared& sh, const SampleCall& a, long long r, const Scale& sc, int ref, int kept) {
+    const int tid = threadIdx.x;
+    const auto report = [&](int i, bool fine, int token, double share) {
+        if (!fine) set_status(a.status, SD_ERR_INVALID_ARG);
+        a.tokens[r * a.N + i] = fine ? token : -1;
+        if (a.prob) a.prob[r * a.N + i] = fine ? (float)share : 0.f;
+    };
+    if (kept <= kComparePairs) {
+        // every entry sums up the masses of those in front of it in the vocabulary; of the entries past the mark the first is drawn
+        const double total = sh.all[kept - 1];
+        double* mass = reinterpret_cast<double*>(sh.other);
+        double mine = 0.0, cum = 0.0;
+        if (tid < kept) mass[tid] = mine = sc.mass(key_logit(sh.list[tid]), ref);
+        if (tid < a.N) sh.found[tid] = INT_MAX;
+        __syncthreads();
+        int index = 0;
+        if (tid < kept) {
+            index = key_index(sh.list[tid]);
+#pragma unroll 4
+            for (int j = 0; j < kept; ++j) cum += key_index(sh.list[j]) <= index ? mass[j] : 0.0;
+            for (int i = 0; i < a.N; ++i)
+                if (mine > 0.0 && cum > (double)a.u[r * a.N + i] * total) atomicMin(&sh.found[i], index);
+        }
+        __syncthreads();
+        // rounding may leave all sums at or below the mark: the last entry with mass then
+        for (int i = 0; i < a.N; ++i) {
+            const float u = a.u[r * a.N + i];
+            const bool fine = u >= 0.f && u < 1.f, none = sh.found[i] == INT_MAX;
+            if (none) {
+                int last = tid < kept && mine > 0.0 ? index : -1;
+                last = __reduce_max_sync(0xffffffffu, last);
+                if ((tid & 31) == 0) sh.wcnt[tid >> 5] = last;
+                __syncthreads();
+                for (int w = 0; w < kWarps; ++w) last = max(last, sh.wcnt[w]);
+                __syncthreads();
+                if (tid == 0) sh.found[i] = last;
+                __syncthreads();
+            }
+            if (fine ? tid < kept && index == sh.found[i] : tid == 0) report(i, fine, index, sc.mass(key_logit(sh.list[tid < kept ? tid : 0]), ref) / total);
+        }
+        __syncthreads();
+        return;
+    }
+    // the kept entries in vocabulary order, and where the uniform numbers fall among them
+    uint64_t* by_index = sh.other;
+    for (int i = tid; i < kept; i += kThreads) by_index[i] = ((uint64_t)(uint32_t)key_index(sh.list[i]) << 32) | (uint32_t)i;
+    block_sort(by_index, kept);
+    for (int i = tid; i < kept; i += kThreads) sh.all[i] = sc.mass(key_logit(sh.list[(uint32_t)by_index[i]]), ref);
+    block_scan(sh.all, kept, sh.tmp_d);
+    for (int i = tid; i < a.N; i += kThreads) {
+        const float u = a.u[r * a.N + i];
+        const double total = sh.all[kept - 1];
+        int at = first_above(sh.all, kept, (double)u * total, false);
+        while (at >= kept || (at > 0 && !(sh.all[at] > sh.all[at - 1]))) --at;       // (none above: the last with mass)
+        report(i, u >= 0.f && u < 1.f, (int)(by_index[at] >> 32), sc.mass(key_logit(sh.list[(uint32_t)by_index[at]]), ref) / total);
+    }
+}
+
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 2)
 sample_kernel(SampleCall a) {
-    extern __shared__ __align__(16) uint64_t buf[];
+    extern __shared__ __align__(16) uint4 data[];
     __shared__ RowShared sh;
-    begin_dependent(a.logits, a.inv_temp, a.top_k, a.top_p, a.min_p, a.u, a.tokens, a.prob, a.dense, a.lse, a.kept, a.status);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (tid == 0) {
+        sh.abort_flag = 0;
+        for (int q = 0; q < kPieces; ++q) sm100::mbar_init(&sh.bar[q], 1);
+        sm100::fence_barrier_init();
+    }
+    __syncthreads();
+    begin_dependent(a.logits, a.inv_temp, a.top_k, a.top_p, a.min_p, a.u, a.tokens, a.prob, a.dense, a.lse, a.kept, a.status);
     const int parts = a.parts, V = a.V;
     const long long r = blockIdx.x / parts;
     const int rank = parts == 1 ? 0 : (int)sm100::cluster_ctarank();
-    const Part<T> part(a.logits, a.ld, r, V, parts, rank);
+    const Slice<T> sl(a.logits, a.ld, r, V, parts, rank, data);
+    sl.copy(sh, a.withheld);
 
     // ---- what the row asks for
     float it = a.inv_temp ? a.inv_temp[r] : 1.f;
     int k = a.top_k ? a.top_k[r] : 0;
-    const float p = a.top_p ? a.top_p[r] : 1.f;
+    float p = a.top_p ? a.top_p[r] : 1.f;
     float mp = a.min_p ? a.min_p[r] : 0.f;
     const bool bad = !(it >= 1e-6f);
     if (bad || it > 3.4e38f) { if (!bad) k = 1; it = 1.f; }                        // infinite: the first entry alone
     if (k >= V) k = 0;
     const bool by_k = k >= 1, by_p = p < 1.f, by_mp = mp > 0.f;
+    p = fmaxf(p, 0.f);
     mp = by_mp ? fminf(mp, 1.f) : 0.f;
-    const bool short_k = by_k && k <= kKeepMax;
-    const int keep = short_k ? k : (by_k || by_p || by_mp ? kKeepMax : 0);
-    const bool need_mass = !short_k;
     const Scale sc(it);
+    __syncthreads();
 
-    scan_part<T, false>(sh, buf, part.row, part.v0, part.v1, part.seg, part.iters, keep, need_mass, sc, 0.f);
-    const int n = meet(sh, buf, parts, rank, keep);                                // (keep = 0: only the parts' meeting)
-
-    if (rank == 0) {
-        const float top = bad ? -INFINITY : top_of_parts(sh, parts);
-        const int ref = top > -INFINITY ? sc.whole(top) : 0;
-        double total = 0.0;
-        int kept = -1;
-        if (top > -INFINITY) {
-            double* sums = sh.all;
-            if (need_mass) {
-                const int chunks = scan_chunks(sh, parts, kWarps * part.iters, ref);
-                total = sh.all[chunks - 1];
-                __syncthreads();
-            }
-            if (keep) {
-                const bool whole = short_k || n < keep;                            // every entry that can stay is listed
-                for (int i = tid; i < n; i += kThreads) sums[i] = sc.mass(key_logit(buf[i]), ref);
-                block_scan(sums, n, sh.tmp_d);
-                const int in_k = by_k ? min(k, n) : n;
-                // the listed entries whose mass min_p lets pass: a prefix
-                int in_mp = n;
-                if (by_mp) {
-                    const double least = (double)mp * sc.mass(top, ref);
-                    int lo = 0, hi = n;
-                    while (lo < hi) {
-                        const int mid = (lo + hi) >> 1;
-                        if (sc.mass(key_logit(buf[mid]), ref) < least) hi = mid; else lo = mid + 1;
-                    }
-                    in_mp = lo;
-                }
-                if (whole) {
-                    kept = in_k;
-                    if (by_p) kept = min(kept, first_above(sums, in_k, (double)p * sums[in_k - 1], true) + 1);
-                    kept = min(kept, in_mp);
-                } else {
-                    // entries may follow behind the list
-                    const bool known = !(by_p && by_k);                            // (the mass of the k first ones is not at hand)
-                    int len = n + 1;
-                    if (by_p && !by_k) {
-                        const int at = first_above(sums, n, (double)p * total, true);
-                        if (at < n) len = at + 1;
-                    }
-                    if (in_mp < n) len = min(len, in_mp);
-                    if (known && len <= n) kept = len;
-                }
-                if (kept >= 0) { kept = max(kept, 1); total = sums[kept - 1]; }
-            }
-        }
-        __syncthreads();
-        if (tid == 0) sh.plan = Plan{!(top > -INFINITY) ? kNone : (kept >= 0 ? kList : kWide), kept, ref, top, total};
-    }
+    const bool ok = first_pass<T, false>(sh, sl, 0.f, a.wait_cycles);
     sync_parts(parts);
-    const Plan plan = *of_rank(&sh.plan, 0);
+    const float top = bad ? -INFINITY : top_of_parts(sh, parts);
+    const int ref = top > -INFINITY ? sc.whole(top) : 0;
+    const double top_mass = sc.mass(top, ref), least = (double)mp * top_mass;
     float* dense = a.dense ? a.dense + r * (long long)V : nullptr;
     const int per = ((V + parts - 1) / parts + 3) & ~3;                            // this CTA's share of the output row
     const int o0 = min(V, rank * per), o1 = min(V, o0 + per);
 
-    if (plan.kind == kNone) {
-        if (dense) fill_floats(dense + o0, o1 - o0, a.scaled ? -INFINITY : 0.f);
+    int kind = kNone;
+    uint64_t border = ~0ull;                                                       // kWide: the key of the last entry that stays
+    double total = 0.0;
+    int kept = 0;
+    if (top > -INFINITY) {
+        kind = kWide;
+        bool summed = false;                                                       // sh.chunk has what the draws need, but for the listed entries
+        bool narrow = false;                                                       // the list has all that can stay
+        // ---- the list
+        if (by_k && k <= kFewK) {
+            const float thr = kth_group(sh, parts, k);
+            list_entries(sh, sl, [&](float x, int) { return x >= thr; });
+            sync_parts(parts);
+            narrow = listed(sh, parts) <= (uint32_t)kListMax;
+        }
+        if (!narrow && (by_k || by_p)) {
+            const LinearBins lin(top, sc);
+            fill_bins(sh, sl, by_p, lin);
+            const int n_all = sh.all_count[kBins - 1];
+            const bool cut_k = by_k && k < n_all;
+            // bin of the k-th entry; bins between which the border of top_p must lie: masses are known to 2e-5, and M, the mass of the
+            // k first entries, to that of the k-th's bin
+            const int bk = cut_k ? min(first_above(sh.all_count, kBins, (uint32_t)k, true), kBins - 1) : kBins - 1;
+            int b_lo = bk, b_hi = bk;
+            if (by_p) {
+                const double m_lo = cut_k && bk > 0 ? sh.all[bk - 1] : (cut_k ? 1.0 : sh.all[bk]), m_hi = sh.all[bk];
+                b_lo = min(first_above(sh.all, kBins, (double)p * m_lo * (1.0 - 1e-4), true), bk);
+                b_hi = min(first_above(sh.all, kBins, (double)p * m_hi * (1.0 + 1e-4), true), bk);
+            }
+            const int end = by_p ? b_hi : bk;
+            if (sh.all_count[end] <= (uint32_t)kListMax && (cut_k || by_p) && (!(cut_k && by_p) || sh.all_count[bk] <= (uint32_t)kListMax)) {
+                // everything down to the border is few: listed (with top-k and top-p, down to the k-th)
+                const int down = cut_k ? bk : end;
+                __syncthreads();
+                list_entries(sh, sl, [&](float x, int) { return lin.of(x) <= down; });
+                if (!cut_k) {                                                      // top_p of the whole row: its mass
+                    sum_chunks(sh, sl, sc, ref, [](float, double) { return true; }, [](float, int, double) {});
+                    summed = true;
+                }
+                sync_parts(parts);
+                narrow = true;
+            } else if (cut_k || by_p) {
+                // flat: the borders' bins are listed, what is above them is summed up
+                int m_lo = b_lo;                                                   // the listed bins start here
+                bool p_counts = by_p;
+                if (by_mp) {
+                    // min_p's border: above, among or below the listed bins
+                    const double d = -16.0 * log2((double)mp);
+                    const int bm = (int)fmin(d, (double)(kBins - 1));
+                    if (bm + 1 < b_lo) { p_counts = false; m_lo = -1; }
+                    else m_lo = min(m_lo, max(0, bm - 1));
+                }
+                if (m_lo >= 0) {
+                    const int n_above = m_lo ? sh.all_count[m_lo - 1] : 0, above_k = cut_k && bk ? sh.all_count[bk - 1] : 0;
+                    const int to = p_counts ? b_hi : bk;
+                    const uint32_t n_list = sh.all_count[to] - n_above + (cut_k && bk > to ? sh.all_count[bk] - above_k : 0);
+                    if (n_list <= (uint32_t)kListMax) {
+                        if (tid == 0) sh.cta_n = 0;
+                        __syncthreads();
+                        double mid = 0.0;
+                        sum_chunks(sh, sl, sc, ref, [&](float x, double) { return lin.of(x) < m_lo; },
+                                   [&](float x, int index, double m) {
+                                       const int b = x > -INFINITY ? lin.of(x) : kBins;
+                                       if (b == kBins) return;
+                                       if ((b >= m_lo && b <= to) || (cut_k && b == bk)) {
+                                           const uint32_t at = atomicAdd(&sh.cta_n, 1u);
+                                           if (at < (uint32_t)kListMax) sh.list[at] = order_key(x, index);
+                                       } else if (b > to && (!cut_k || b < bk)) mid += m;
+                                   });
+                        mid = warp_add(mid);
+                        if (lane == 0) sh.tmp_d[warp] = mid;
+                        __syncthreads();
+                        if (tid == 0) {
+                            for (int w = 1; w < kWarps; ++w) mid += sh.tmp_d[w];
+                            sh.cta_mid = mid;
+                        }
+                        sync_parts(parts);
+                        if (rank == 0) {
+                            // masses above the listed bins, chunk by chunk; the listed entries in order
+                            collect(sh, parts);
+                            const int n = min(n_list, (uint32_t)kListMax), per_part = kWarps * sl.iters, chunks = parts * per_part;
+                            block_sort(sh.list, n);
+                            double above = 0.0;
+                            mid = 0.0;
+                            for (int q = 0; q < parts; ++q) mid += *of_rank(&sh.cta_mid, q);
+                            for (int i = tid; i < chunks; i += kThreads) above += *of_rank(&sh.chunk[i % per_part], i / per_part);
+                            above = warp_add(above);
+                            __syncthreads();
+                            if (lane == 0) sh.tmp_d[warp] = above;
+                            __syncthreads();
+                            above = 0.0;
+                            for (int w = 0; w < kWarps; ++w) above += sh.tmp_d[w];
+                            for (int i = tid; i < n; i += kThreads) sh.all[i] = sc.mass(key_logit(sh.list[i]), ref);
+                            block_scan(sh.all, n, sh.tmp_d);
+                            // how many of the list belong to the k first; the listed ones in front of the k-th's bin stand before them
+                            int len = n;
+                            const int in_bk = cut_k ? sh.all_count[bk] - above_k : 0;                // (0: no top-k)
+                            const bool apart = cut_k && bk > to;
+                            if (cut_k) len = (apart ? n - in_bk : above_k - n_above) + (k - above_k);
+                            len = min(len, n);
+                            if (p_counts) {
+                                const double listed_mass = len ? sh.all[len - 1] : 0.0;
+                                const double m_k = above + listed_mass + mid;
+                                const int span = apart ? n - in_bk : len;                            // the border of top_p is not among the k-th's bin alone
+                                len = min(len, min(first_above(sh.all, span, (double)p * m_k - above, true) + 1, span));
+                            }
+                            if (by_mp) {
+                                int l = 0, h = len;
+                                while (l < h) {
+                                    const int m = (l + h) >> 1;
+                                    if (sc.mass(key_logit(sh.list[m]), ref) < least) h = m; else l = m + 1;
+                                }
+                                len = l;
+                            }
+                            if (tid == 0) {
+                                sh.border = len ? sh.list[len - 1] : 0;                              // (none of the list: all above its bins)
+                                sh.kept = n_above + len;
+                                if (!len) sh.border = sh.list[0] - 1;
+                                sh.total = above + (len ? sh.all[len - 1] : 0.0);
+                            }
+                            // the draws' chunks: with the listed entries that stay
+                            __syncthreads();
+                            if (a.N) {
+                                const int stays = len;
+                                for (int i = tid; i < kBins; i += kThreads) sh.other[i] = 0;
+                                __syncthreads();
+                                for (int i = tid; i < stays; i += kThreads)
+                                    atomicAdd(reinterpret_cast<unsigned long long*>(&sh.other[sl.chunk_of(key_index(sh.list[i]))]),
+                                              (unsigned long long)(sc.mass(key_logit(sh.list[i]), ref) * kUnit + 0.5));
+                                __syncthreads();
+                                for (int i = tid; i < chunks; i += kThreads)
+                                    sh.all[i] = *of_rank(&sh.chunk[i % per_part], i / per_part) + (double)sh.other[i] / kUnit;
+                                block_scan(sh.all, chunks, sh.tmp_d);
+                            }
+                        }
+                        sync_parts(parts);
+                        border = *of_rank(&sh.border, 0);
+                        kept = *of_rank(&sh.kept, 0);
+                        total = *of_rank(&sh.total, 0);
+                        kind = -1;                                                 // (done: borders, count and mass are known)
+                    } else {
+                        // more than a list holds in the borders' bins
+                        if (cut_k) search_border(sh, sl, false, (uint64_t)k, -1.0, ~0ull, sc, ref, &border);
+                        if (p_counts) search_border(sh, sl, true, 0, (double)p, border, sc, ref, &border);
+                    }
+                }
+            }
+        } else if (!narrow && by_mp) {
+            // min_p alone: the entries that stay, listed if they are few
+            const float d = (float)(-log2((double)mp) * 1.0001 / sc.c), from = top - d - fabsf(top) * 1e-6f - d * 1e-4f;
+            list_entries(sh, sl, [&](float x, int) { return x >= from && sc.mass(x, ref) >= least; });
+            sync_parts(parts);
+            narrow = listed(sh, parts) <= (uint32_t)kListMax;
+        }
+
+        // ---- the row is decided on the list
+        if (narrow) {
+            if (rank == 0) {
+                collect(sh, parts);
+                int n = listed(sh, parts);
+                n = sort_list(sh, n, by_k ? min(k, kListMax) : kListMax);
+                double all = 0.0;
+                if (summed) {
+                    const int per_part = kWarps * sl.iters, chunks = parts * per_part;
+                    for (int i = tid; i < chunks; i += kThreads) all += *of_rank(&sh.chunk[i % per_part], i / per_part);
+                    all = warp_add(all);
+                    if (lane == 0) sh.tmp_d[warp] = all;
+                    __syncthreads();
+                    all = 0.0;
+                    for (int w = 0; w < kWarps; ++w) all += sh.tmp_d[w];
+                    __syncthreads();
+                }
+                for (int i = tid; i < n; i += kThreads) sh.all[i] = sc.mass(key_logit(sh.list[i]), ref);
+                block_scan(sh.all, n, sh.tmp_d);
+                int len = n;
+                if (by_p) len = min(len, first_above(sh.all, len, (double)p * (summed ? all : sh.all[len - 1]), true) + 1);
+                if (by_mp) {
+                    int l = 0, h = len;
+                    while (l < h) {
+                        const int m = (l + h) >> 1;
+                        if (sc.mass(key_logit(sh.list[m]), ref) < least) h = m; else l = m + 1;
+                    }
+                    len = l;
+                }
+                len = max(len, 1);
+                if (tid == 0) { sh.kept = len; sh.total = sh.all[len - 1]; }
+            }
+            kind = kList;
+        } else if (kind == kWide) {
+            // ---- everything up to a border (or all, or by min_p): its mass chunk by chunk
+            int cnt = 0;
+            const uint64_t last = border;
+            if (last == ~0ull && !by_mp && !a.kept) {
+                sum_chunks(sh, sl, sc, ref, [](float, double) { return true; }, [](float, int, double) {});
+            } else {
+                constexpr int E = Slice<T>::E;
+                const int w0 = min(sl.nv, warp * sl.seg), w1 = min(sl.nv, w0 + sl.seg);
+                for (int c = 0; c < sl.iters; ++c) {
+                    double s = 0.0;
+                    for (int u = 0; u < kU; ++u) {
+                        const int i = w0 + (c * kU + u) * 32 + lane;
+                        if (i >= w1) break;
+                        float x[E];
+                        Row<T>::unpack(sl.data[i], x);
+#pragma unroll
+                        for (int e = 0; e < E; ++e) {
+                            const double m = sc.mass(x[e], ref);
+                            if (x[e] > -INFINITY && order_key(x[e], sl.first + i * E + e) <= last && m >= least) { s += m; ++cnt; }
+                        }
+                    }
+                    s = warp_add(s);
+                    if (lane == 0) sh.chunk[warp * sl.iters + c] = s;
+                }
+                cnt = warp_add(cnt);
+                if (lane == 0) sh.wcnt[warp] = cnt;
+                __syncthreads();
+                if (tid == 0) {
+                    for (int w = 1; w < kWarps; ++w) cnt += sh.wcnt[w];
+                    sh.cta_count = cnt;
+                }
+            }
+            sync_parts(parts);
+            if (rank == 0) {
+                const int per_part = kWarps * sl.iters, chunks = parts * per_part;
+                for (int i = tid; i < chunks; i += kThreads) sh.all[i] = *of_rank(&sh.chunk[i % per_part], i / per_part);
+                block_scan(sh.all, chunks, sh.tmp_d);
+                if (tid == 0) {
+                    sh.total = sh.all[chunks - 1];
+                    cnt = 0;
+                    if (a.kept) for (int q = 0; q < parts; ++q) cnt += *of_rank(&sh.cta_count, q);
+                    sh.kept = cnt;
+                }
+                __syncthreads();
+            }
+        }
+        if (kind == -1) kind = kWide;
+    }
+
+    // ---- outputs
+    if (dense && kind != kWide) fill_floats(dense + o0, o1 - o0, a.scaled ? -INFINITY : 0.f);
+    if (kind == kNone) {
         if (rank == 0) {
             if (bad && tid == 0) set_status(a.status, SD_ERR_INVALID_ARG);
             for (int i = tid; i < a.N; i += kThreads) { a.tokens[r * a.N + i] = -1; if (a.prob) a.prob[r * a.N + i] = 0.f; }
             if (tid == 0) { if (a.lse) a.lse[r] = -INFINITY; if (a.kept) a.kept[r] = 0; }
         }
-        if (parts > 1) sync_parts(parts);
-        return;
-    }
-    if (plan.kind == kList) {
-        if (dense) {
-            fill_floats(dense + o0, o1 - o0, a.scaled ? -INFINITY : 0.f);
-            sync_parts(parts);                                                     // all parts are filled before entries go in
-        }
+    } else {
+        if (dense) sync_parts(parts);                                              // all parts are filled before entries go in; the total is known
+        else __syncthreads();
+        if (dense) { total = *of_rank(&sh.total, 0); }
         if (rank == 0) {
-            if (dense)
-                for (int i = tid; i < plan.n; i += kThreads) {
-                    const float x = key_logit(buf[i]);
-                    dense[key_index(buf[i])] = a.scaled ? scaled_logit(x, it) : (float)(sc.mass(x, plan.ref) / plan.total);
-                }
-            if (tid == 0) {
-                if (a.lse) a.lse[r] = log_mass(sc, plan.top, it, plan.ref, plan.total);
-                if (a.kept) a.kept[r] = plan.n;
+            total = sh.total;
+            kept = sh.kept;
+            if (tid == kThreads - 1) {
+                if (a.lse) a.lse[r] = log_mass(sc, top, it, ref, total);
+                if (a.kept) a.kept[r] = kept;
             }
-            if (a.N) {
-                // the kept entries in vocabulary order, and where the uniform numbers fall among them
-                uint64_t* by_index = buf + kListAt;
-                for (int i = tid; i < plan.n; i += kThreads) by_index[i] = ((uint64_t)(uint32_t)key_index(buf[i]) << 32) | (uint32_t)i;
-                block_sort(by_index, plan.n);
-                for (int i = tid; i < plan.n; i += kThreads) sh.all[i] = sc.mass(key_logit(buf[(uint32_t)by_index[i]]), plan.ref);
-                block_scan(sh.all, plan.n, sh.tmp_d);
-                for (int i = tid; i < a.N; i += kThreads) {
-                    const float u = a.u[r * a.N + i];
-                    const double total = sh.all[plan.n - 1];
-                    int at = first_above(sh.all, plan.n, (double)u * total, false);
-                    while (at >= plan.n || (at > 0 && !(sh.all[at] > sh.all[at - 1]))) --at;       // (none above: the last with mass)
-                    const bool fine = u >= 0.f && u < 1.f;
-                    if (!fine) set_status(a.status, SD_ERR_INVALID_ARG);
-                    a.tokens[r * a.N + i] = fine ? (int)(by_index[at] >> 32) : -1;
-                    if (a.prob) a.prob[r * a.N + i] = fine ? (float)(sc.mass(key_logit(buf[(uint32_t)by_index[at]]), plan.ref) / total) : 0.f;
-                }
-            }
-        }
-        if (parts > 1) sync_parts(parts);
-        return;
-    }
-
-    // ---- the kept entries are not all listed: borders by histograms, where there is one, then the kept mass chunk by chunk
-    const int ref = plan.ref;
-    uint64_t border = ~0ull;
-    if (by_k || by_p) {
-        // bins of a sixteenth of a factor of two, counted from the largest logit; what is further off than 2^-64 shares the last
-        const float per_bin = (float)fmin(16.0 * sc.c, 3.0e38), top = plan.top;
-        const auto linear_bin = [&](float x) { return (int)fminf((top - x) * per_bin, (float)(kBins - 1)); };
-        const Bins b(buf);
-        fill_bins(sh, b, part, by_p, sc, ref, [&](float x, int) { return linear_bin(x); });
-        uint64_t mass_k = b.sum_mass[kBins - 1];
-        const uint64_t count = b.sum_count[kBins - 1];
-        if (by_k && (uint64_t)k < count) {
-            pick_bin(sh, b, false, (uint64_t)k);
-            find_border(sh, buf, b, part, false, by_p, (uint64_t)k, sc, ref, linear_bin, &border, &mass_k);
-            if (by_p) fill_bins(sh, b, part, true, sc, ref, [&](float x, int) { return linear_bin(x); });
-        }
-        if (by_p) {
-            uint64_t target = (uint64_t)ceil((double)fmaxf(p, 0.f) * (double)mass_k), last, last_mass;
-            target = max((uint64_t)1, min(target, mass_k));
-            pick_bin(sh, b, true, target);
-            find_border(sh, buf, b, part, true, true, target, sc, ref, linear_bin, &last, &last_mass);
-            border = min(border, last);
-        }
-    }
-    const double least = by_mp ? (double)mp * sc.mass(plan.top, ref) : 0.0;
-    const auto stays = [&](float x, int index) { return order_key(x, index) <= border && (!by_mp || sc.mass(x, ref) >= least); };
-    const bool everything = border == ~0ull && !by_mp;
-    if (!everything || a.kept) {
-        // (chunk sums of the first pass are this CTA's own until here; the first CTA has read them)
-        constexpr int E = Row<T>::kE;
-        const int w0 = min(part.v1, part.v0 + warp * part.seg), w1 = min(part.v1, w0 + part.seg);
-        int cnt = 0;
-        for (int c = 0; c < part.iters; ++c) {
-            double s = 0.0;
-#pragma unroll
-            for (int u = 0; u < kU; ++u) {
-                const int i = w0 + (c * kU + u) * 32 + lane;
-                const uint4 raw = i < w1 ? part.row.load(i) : Row<T>::nothing();
-                float x[E];
-                Row<T>::unpack(raw, x);
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (x[e] > -INFINITY && order_key(x[e], i * E + e - part.row.lead) <= border) {
-                        const double mass = sc.mass(x[e], ref);
-                        if (!by_mp || mass >= least) { s += mass; ++cnt; }
+            if (kind == kList) {
+                if (dense)
+                    for (int i = tid; i < kept; i += kThreads) {
+                        const float x = key_logit(sh.list[i]);
+                        dense[key_index(sh.list[i])] = a.scaled ? scaled_logit(x, it) : (float)(sc.mass(x, ref) / total);
                     }
+                if (a.N) draw_from_list(sh, a, r, sc, ref, kept);
+            } else {
+                const int chunks = parts * kWarps * sl.iters;
+                for (int d = warp; d < a.N; d += kWarps) {                         // a warp per draw
+                    const float u = a.u[r * a.N + d];
+                    const bool fine = u >= 0.f && u < 1.f;
+                    int token = -1;
+                    double mass = 0.0;
+                    if (fine) {
+                        const double target = (double)u * sh.all[chunks - 1];
+                        int g = first_above(sh.all, chunks, target, false);
+                        while (g >= chunks || (g > 0 && !(sh.all[g] > sh.all[g - 1]))) --g;
+                        token = chunk_crossing(sl, g, target - (g ? sh.all[g - 1] : 0.0), sc, ref,
+                                               [&](float x, int index, double m) { return x > -INFINITY && order_key(x, index) <= border && m >= least; }, &mass);
+                    } else if (lane == 0) set_status(a.status, SD_ERR_INVALID_ARG);
+                    if (lane == 0) { a.tokens[r * a.N + d] = token; if (a.prob) a.prob[r * a.N + d] = (float)(mass / total); }
+                }
             }
-            s = warp_add(s);
-            if (lane == 0) { sh.chunk[warp * part.iters + c] = s; sh.chunk_ref[warp * part.iters + c] = ref; }
         }
-        cnt = warp_add(cnt);
-        if (lane == 0) sh.wcnt[warp] = cnt;
-        __syncthreads();
-        if (tid == 0) {
-            cnt = 0;
-            for (int w = 0; w < kWarps; ++w) cnt += sh.wcnt[w];
-            sh.cta_count = cnt;
-        }
-    }
-    sync_parts(parts);
-    const int chunks = scan_chunks(sh, parts, kWarps * part.iters, ref);
-    const double total = sh.all[chunks - 1];
-    if (rank == 0 && tid == 0) {
-        if (a.lse) a.lse[r] = log_mass(sc, plan.top, it, ref, total);
-        if (a.kept) {
-            int all = 0;
-            for (int q = 0; q < parts; ++q) all += *of_rank(&sh.cta_count, q);
-            a.kept[r] = all;
+        if (dense && kind == kWide) {
+            const float c32 = (float)sc.c, at_top = (float)(top_mass / total);
+            const T* entries = reinterpret_cast<const T*>(data);
+            const int lo = max(0, sl.first), hi = min(V, sl.first + sl.nv * Slice<T>::E);
+            for (int v = lo + tid; v < hi; v += kThreads) {
+                float x;
+                if constexpr (sizeof(T) == 4) x = (float)entries[v - sl.first];
+                else x = __uint_as_float((uint32_t)entries[v - sl.first] << 16);
+                const bool in = x > -INFINITY && order_key(x, v) <= border && (!by_mp || sc.mass(x, ref) >= least);
+                dense[v] = a.scaled ? (in ? scaled_logit(x, it) : -INFINITY) : (in ? at_top * exp2f((x - top) * c32) : 0.f);
+            }
         }
     }
-    for (int d = warp; d < a.N; d += kWarps) {                                     // a warp per draw, in the CTA whose part it falls into
-        const float u = a.u[r * a.N + d];
-        if (!(u >= 0.f && u < 1.f)) {
-            if (rank == 0 && lane == 0) { set_status(a.status, SD_ERR_INVALID_ARG); a.tokens[r * a.N + d] = -1; if (a.prob) a.prob[r * a.N + d] = 0.f; }
-            continue;
-        }
-        const double target = (double)u * total;
-        int g = first_above(sh.all, chunks, target, false);
-        while (g >= chunks || (g > 0 && !(sh.all[g] > sh.all[g - 1]))) --g;
-        const int per_part = kWarps * part.iters;
-        if (g / per_part != rank) continue;
-        const int at = g - rank * per_part;
-        double mass = 0.0;
-        const int token = chunk_crossing(part, at / part.iters, at % part.iters, target - (g ? sh.all[g - 1] : 0.0), sc, ref, stays, &mass);
-        if (lane == 0) { a.tokens[r * a.N + d] = token; if (a.prob) a.prob[r * a.N + d] = (float)(mass / total); }
-    }
-    sync_parts(parts);                                                             // the last reading of other CTAs' memory, and of the row for draws
-    if (dense) {
-        const float top = plan.top, c32 = (float)sc.c, at_top = (float)(sc.mass(top, ref) / total);
-        for (int v = o0 + tid; v < o1; v += kThreads) {
-            const float x = part.row.at(v);
-            const bool in = x > -INFINITY && stays(x, v);
-            dense[v] = a.scaled ? (in ? scaled_logit(x, it) : -INFINITY) : (in ? at_top * exp2f((x - top) * c32) : 0.f);
-        }
-    }
+    if (!ok) { set_status(a.status, SD_ERR_TIMEOUT); sm100::unwind_pause(); }
+    __syncwarp();
+    if (parts > 1) sync_parts(parts);                                              // nobody leaves while another CTA reads
 }
 
-// CTAs per row: as many as leave every warp a few vectors, while all of them fit on the GPU at once
-static int parts_for(int M, int V, int elem) {
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return 1;
-    const long long slots = 2ll * sm_count(dev);
-    const int vecs = (int)(((long long)V * elem + 15) / 16);
+// CTAs per row: slices of at most 80 KB while eight are enough for that, and more of them where the rows leave SMs idle
+static int parts_for(int M, int nvec, int sms) {
     int parts = 1;
-    while (parts < 8 && (long long)M * parts * 2 <= slots && vecs / (parts * 2) >= kThreads) parts *= 2;
+    while (parts < 8 && ((nvec + parts - 1) / parts > 5120 || ((long long)M * parts * 2 <= sms && nvec / (parts * 2) >= kThreads))) parts *= 2;
     return parts;
 }
 
@@ -860,20 +1011,30 @@ static int parts_for(int M, int V, int elem) {
 using namespace rows;
 
 sd_status launch_top_logits(const void* logits, int dtype, long long ld, int M, int V, int K, float inv_temp, float* values, int32_t* index,
-                            float* lse, cudaStream_t st) {
-    const int parts = parts_for(M, V, dtype == SD_F32 ? 4 : 2);
+                            float* lse, int32_t* dev_status, cudaStream_t st) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return SD_ERR_CUDA;
+    const int nvec = (int)(((long long)V * (dtype == SD_F32 ? 4 : 2) + 15) / 16) + 1;
+    const int parts = parts_for(M, nvec, sm_count(dev)), smem = (nvec + parts - 1) / parts * 16;
     auto kern = dtype == SD_F32 ? top_kernel<float> : top_kernel<uint16_t>;
-    if (!allow_dynamic_smem(kern, kCap * 8)) return SD_ERR_CUDA;
-    return launch_dependent(kern, dim3((unsigned)M * parts), kThreads, kCap * 8, parts, st, logits, ld, V, parts, K, inv_temp, values, index, lse);
+    if (!allow_dynamic_smem(kern, smem)) return SD_ERR_CUDA;
+    const TestKnobs knobs = test_knobs();
+    return launch_dependent(kern, dim3((unsigned)M * parts), kThreads, smem, parts, st, logits, ld, V, parts, K, inv_temp, values, index, lse, dev_status,
+                            knobs.withhold ? 16 : 0, knobs.wait_cycles);
 }
 
 sd_status launch_sample(const void* logits, int dtype, long long ld, int M, int V, const sd_sampling& how, const float* u, int N, int32_t* tokens,
                         float* prob, float* dense, bool scaled, float* lse, int32_t* kept, int32_t* dev_status, cudaStream_t st) {
-    const int parts = parts_for(M, V, dtype == SD_F32 ? 4 : 2);
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return SD_ERR_CUDA;
+    const int nvec = (int)(((long long)V * (dtype == SD_F32 ? 4 : 2) + 15) / 16) + 1;
+    const int parts = parts_for(M, nvec, sm_count(dev)), smem = (nvec + parts - 1) / parts * 16;
     auto kern = dtype == SD_F32 ? sample_kernel<float> : sample_kernel<uint16_t>;
-    if (!allow_dynamic_smem(kern, kCap * 8)) return SD_ERR_CUDA;
-    const SampleCall call{logits, ld, V, parts, how.inv_temp, how.top_k, how.top_p, how.min_p, u, N, tokens, prob, dense, scaled, lse, kept, dev_status};
-    return launch_dependent(kern, dim3((unsigned)M * parts), kThreads, kCap * 8, parts, st, call);
+    if (!allow_dynamic_smem(kern, smem)) return SD_ERR_CUDA;
+    const TestKnobs knobs = test_knobs();
+    const SampleCall call{logits, ld, V, parts, how.inv_temp, how.top_k, how.top_p, how.min_p, u, N, tokens, prob, dense, scaled, lse, kept, dev_status,
+                          knobs.withhold ? 16 : 0, knobs.wait_cycles};
+    return launch_dependent(kern, dim3((unsigned)M * parts), kThreads, smem, parts, st, call);
 }
 
 }  // namespace sdv
