@@ -129,25 +129,37 @@ struct Scale {
     }
     __device__ __forceinline__ double clamped(float x) const { return (double)fminf(fmaxf(x, -lim), lim) * c; }
     __device__ __forceinline__ int whole(float x) const { return __double2int_rn(clamped(x)); }
-    __device__ __forceinline__ double mass(float x, int ref) const {
-        const double t = clamped(x);
+    // N masses side by side: their chains of multiply-adds hide one another's latency
+    template <int N>
+    __device__ __forceinline__ void masses(const float (&x)[N], int ref, double (&m)[N]) const {
         const double big = 6755399441055744.0;                                     // 1.5 * 2^52: adding it rounds to a whole number
-        const double r = t + big;
-        const int n = __double2loint(r);
-        const double f = t - (r - big);
-        double p = 1.0178086009239699e-07;                                         // (ln 2)^k / k!, k = 9 .. 0
-        p = fma(p, f, 1.3215486790144309e-06);
-        p = fma(p, f, 1.5252733804059841e-05);
-        p = fma(p, f, 1.5403530393381609e-04);
-        p = fma(p, f, 1.3333558146428443e-03);
-        p = fma(p, f, 9.6181291076284772e-03);
-        p = fma(p, f, 5.5504108664821580e-02);
-        p = fma(p, f, 2.4022650695910072e-01);
-        p = fma(p, f, 6.9314718055994531e-01);
-        p = fma(p, f, 1.0);
-        const int e = n - ref;
-        if (!(x > -INFINITY) || e < -1000) return 0.0;                             // masked entries and NaN have none
-        return __hiloint2double(__double2hiint(p) + (e << 20), __double2loint(p));
+        constexpr double kC[10] = {1.0, 6.9314718055994531e-01, 2.4022650695910072e-01, 5.5504108664821580e-02, 9.6181291076284772e-03,
+                                   1.3333558146428443e-03, 1.5403530393381609e-04, 1.5252733804059841e-05, 1.3215486790144309e-06,
+                                   1.0178086009239699e-07};                        // (ln 2)^k / k!
+        double f[N];
+        int e[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const double t = clamped(x[j]), r = t + big;
+            e[j] = __double2loint(r) - ref;
+            f[j] = t - (r - big);
+            m[j] = kC[9];
+        }
+#pragma unroll
+        for (int k = 8; k >= 0; --k)
+#pragma unroll
+            for (int j = 0; j < N; ++j) m[j] = fma(m[j], f[j], kC[k]);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const bool none = !(x[j] > -INFINITY) || e[j] < -1000;                 // masked entries and NaN have none
+            m[j] = __hiloint2double(none ? 0 : __double2hiint(m[j]) + (e[j] << 20), none ? 0 : __double2loint(m[j]));
+        }
+    }
+    __device__ __forceinline__ double mass(float x, int ref) const {
+        const float a[1] = {x};
+        double m[1];
+        masses(a, ref, m);
+        return m[0];
     }
 };
 // v * 2^e
@@ -181,6 +193,13 @@ __device__ __forceinline__ P* of_rank(P* mine, int rank) {
     uint64_t r;
     asm volatile("mapa.u64 %0, %1, %2;" : "=l"(r) : "l"(reinterpret_cast<uint64_t>(mine)), "r"(rank));
     return reinterpret_cast<P*>(r);
+}
+
+// the same variable of every part, part r's in lane r (0 in the others)
+template <typename P>
+__device__ __forceinline__ P of_parts(P* mine, int parts) {
+    const int lane = threadIdx.x & 31;
+    return lane < parts ? *of_rank(mine, lane) : P(0);
 }
 
 // ---------------------------------------------------------------- block-wide steps
@@ -221,9 +240,23 @@ static __device__ __noinline__ void block_scan(S* a, int n, S* tmp) {
     __syncthreads();
 }
 
-// a[0..n) in ascending order; n <= kListMax, room for the next power of two.
+// a[0..n) in ascending order; n <= kListMax, room for the next power of two.  Distinct keys.
+constexpr int kRankSort = 160;         // up to which every key counts those in front of it (128 keys: 0.5 us, the network 0.9)
 static __device__ __noinline__ void block_sort(uint64_t* a, int n) {
     const int tid = threadIdx.x;
+    if (n <= kRankSort) {
+        __syncthreads();
+        const uint64_t mine = tid < n ? a[tid] : 0;
+        int at = 0;
+        if (tid < n) {
+#pragma unroll 8
+            for (int j = 0; j < n; ++j) at += a[j] < mine;
+        }
+        __syncthreads();
+        if (tid < n) a[at] = mine;
+        __syncthreads();
+        return;
+    }
     int size = 32;
     while (size < n) size <<= 1;
     __syncthreads();

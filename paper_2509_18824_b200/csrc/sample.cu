@@ -238,9 +238,8 @@ __device__ __forceinline__ bool first_pass(RowShared& sh, const Slice<T>& sl, fl
 
 // Largest logit over the parts (behind a sync_parts).
 __device__ __forceinline__ float top_of_parts(RowShared& sh, int parts) {
-    float top = -INFINITY;
-    for (int r = 0; r < parts; ++r) top = fmaxf(top, *of_rank(&sh.cta_top, r));
-    return top;
+    const float top = of_parts(&sh.cta_top, parts);
+    return warp_largest((threadIdx.x & 31) < parts ? top : -INFINITY);
 }
 
 // The k-th largest of the groups' largest logits, k <= kGroups: at least k entries reach it (behind a sync_parts).
@@ -276,24 +275,28 @@ __device__ __forceinline__ void list_entries(RowShared& sh, const Slice<T>& sl, 
 }
 // how many entries all parts have listed (behind a sync_parts)
 __device__ __forceinline__ uint32_t listed(RowShared& sh, int parts) {
-    uint32_t n = 0;
-    for (int r = 0; r < parts; ++r) n += *of_rank(&sh.cta_n, r);
-    return n;
+    return __reduce_add_sync(0xffffffffu, of_parts(&sh.cta_n, parts));
 }
-// All parts' entries into the first CTA's list (by the first CTA; they fit)
-__device__ void collect(RowShared& sh, int parts) {
-    int n = sh.cta_n;
-    for (int r = 1; r < parts; ++r) {
-        const int more = *of_rank(&sh.cta_n, r);
+// All parts' entries into the first CTA's list (by the first CTA; they fit): two warps for each part
+__device__ __forceinline__ void collect(RowShared& sh, int parts) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = warp >> 1;
+    const uint32_t n = of_parts(&sh.cta_n, parts);
+    uint32_t upto = n;
+#pragma unroll
+    for (int d = 1; d < 8; d <<= 1) {
+        const uint32_t o = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= d) upto += o;
+    }
+    const int more = __shfl_sync(0xffffffffu, n, r), at = __shfl_sync(0xffffffffu, upto, r) - more;
+    if (r > 0 && r < parts) {
         const uint64_t* from = of_rank(sh.list, r);
-        for (int i = threadIdx.x; i < more; i += kThreads) sh.list[n + i] = from[i];
-        n += more;
+        for (int i = lane + (warp & 1) * 32; i < more; i += 64) sh.list[at + i] = from[i];
     }
     __syncthreads();
 }
 // The first CTA's list of n entries sorted, cut to the `keep` first ones where that is worth a pass; returns how many there are.
 __device__ int sort_list(RowShared& sh, int n, int keep) {
-    if (n > keep && n > 64) { cut_list(sh, sh.list, n, keep); n = keep; }
+    if (n > keep && n > kRankSort) { cut_list(sh, sh.list, n, keep); n = keep; }
     block_sort(sh.list, n);
     return min(n, keep);
 }
@@ -502,17 +505,18 @@ __device__ __forceinline__ void sum_chunks(RowShared& sh, const Slice<T>& sl, co
     const int w0 = min(sl.nv, warp * sl.seg), w1 = min(sl.nv, w0 + sl.seg);
     for (int c = 0; c < sl.iters; ++c) {
         double s = 0.0, t = 0.0;
-#pragma unroll
+#pragma unroll 1
         for (int u = 0; u < kU; ++u) {
             const int i = w0 + (c * kU + u) * 32 + lane;
-            if (i >= w1) break;
+            if (i - lane >= w1) break;
             float x[E];
-            Row<T>::unpack(sl.data[i], x);
+            double m[E];
+            Row<T>::unpack(i < w1 ? sl.data[i] : Row<T>::nothing(), x);
+            sc.masses(x, ref, m);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const double m = sc.mass(x[e], ref);
-                f(x[e], sl.first + i * E + e, m);
-                (e & 1 ? t : s) += in(x[e], m) ? m : 0.0;
+                f(x[e], sl.first + i * E + e, m[e]);
+                (e & 1 ? t : s) += in(x[e], m[e]) ? m[e] : 0.0;
             }
         }
         s = warp_add(s + t);
@@ -535,23 +539,41 @@ __device__ int chunk_crossing(const Slice<T>& sl, int g, double over, const Scal
         const int i = w0 + (c * kU + u) * 32 + lane;
         raw[u] = i < w1 ? data[i] : Row<T>::nothing();
     }
-    double before = 0.0, last_mass = 0.0;
-    int last = -1;
-#pragma unroll 1
-    for (int u = 0; u < kU; ++u) {
-        const int i = w0 + (c * kU + u) * 32 + lane;
-        uint4 now = raw[0];
-#pragma unroll
-        for (int j = 1; j < kU; ++j) if (u == j) now = raw[j];
+    const auto masses_of = [&](const uint4& now, int u, double (&m)[E]) {
         float x[E];
         Row<T>::unpack(now, x);
-        double m[E], s = 0.0;
+        sc.masses(x, ref, m);
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            m[e] = sc.mass(x[e], ref);
-            if (!kept(x[e], first + i * E + e, m[e])) m[e] = 0.0;
-            s += m[e];
-        }
+        for (int e = 0; e < E; ++e) if (!kept(x[e], first + (w0 + (c * kU + u) * 32 + lane) * E + e, m[e])) m[e] = 0.0;
+    };
+    // the sums of the kU steps, and in which of them the mark is passed (else the last with mass)
+    double sum[kU];
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+        double m[E], s = 0.0;
+        masses_of(raw[u], u, m);
+#pragma unroll
+        for (int e = 0; e < E; ++e) s += m[e];
+        sum[u] = warp_add(s);
+    }
+    double before = 0.0, run = 0.0;
+    int step = -1;
+    bool passed = false;
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+        if (!passed && sum[u] > 0.0) { step = u; before = run; passed = run + sum[u] > over; }
+        run += sum[u];
+    }
+    int last = -1;
+    double last_mass = 0.0;
+    if (step >= 0) {
+        uint4 now = raw[0];
+#pragma unroll
+        for (int j = 1; j < kU; ++j) if (step == j) now = raw[j];
+        double m[E], s = 0.0;
+        masses_of(now, step, m);
+#pragma unroll
+        for (int e = 0; e < E; ++e) s += m[e];
         double incl = s;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -562,20 +584,17 @@ __device__ int chunk_crossing(const Slice<T>& sl, int g, double over, const Scal
         const uint32_t with_mass = __ballot_sync(0xffffffffu, s > 0.0);
         // within the lane: the first entry at which the sum exceeds `over`, else the last with mass
         int found = -1;
-        double found_mass = 0.0, run = before + (incl - s);
+        double found_mass = 0.0;
         bool crossed = false;
+        run = before + (incl - s);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             run += m[e];
-            if (m[e] > 0.0 && !crossed) { found = first + i * E + e; found_mass = m[e]; crossed = run > over; }
+            if (m[e] > 0.0 && !crossed) { found = first + (w0 + (c * kU + step) * 32 + lane) * E + e; found_mass = m[e]; crossed = run > over; }
         }
-        if (over_here | with_mass) {
-            const int src = over_here ? __ffs(over_here) - 1 : 31 - __clz(with_mass);
-            last = __shfl_sync(0xffffffffu, found, src);
-            last_mass = __shfl_sync(0xffffffffu, found_mass, src);
-            if (over_here) break;
-        }
-        before += __shfl_sync(0xffffffffu, incl, 31);
+        const int src = over_here ? __ffs(over_here) - 1 : 31 - __clz(with_mass);
+        last = __shfl_sync(0xffffffffu, found, src);
+        last_mass = __shfl_sync(0xffffffffu, found_mass, src);
     }
     *its_mass = last_mass;
     return last;
