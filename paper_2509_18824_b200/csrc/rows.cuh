@@ -127,7 +127,7 @@ struct Scale {
     __device__ __forceinline__ explicit Scale(float inv_temp) : c((double)inv_temp * 1.4426950408889634073599) {
         lim = (float)fmin(536870912.0 / c, 3.4028234663852886e38);
     }
-    __device__ __forceinline__ double clamped(float x) const { return (double)fminf(fmaxf(x, -lim), lim) * c; }
+    __device__ __forceinline__ double clamped(float x) const { return __dmul_rn((double)fminf(fmaxf(x, -lim), lim), c); }
     __device__ __forceinline__ int whole(float x) const { return __double2int_rn(clamped(x)); }
     // N masses side by side: their chains of multiply-adds hide one another's latency
     template <int N>
@@ -140,9 +140,10 @@ struct Scale {
         int e[N];
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            const double t = clamped(x[j]), r = t + big;
+            // (single roundings: the same entry has the same mass wherever it is computed, to the last bit)
+            const double t = clamped(x[j]), r = __dadd_rn(t, big);
             e[j] = __double2loint(r) - ref;
-            f[j] = t - (r - big);
+            f[j] = __dsub_rn(t, __dsub_rn(r, big));
             m[j] = kC[9];
         }
 #pragma unroll
@@ -182,10 +183,13 @@ __device__ __forceinline__ float key_logit(uint64_t key) {
 __device__ __forceinline__ int key_index(uint64_t key) { return (int)(uint32_t)key; }
 
 // ---------------------------------------------------------------- clusters of one to eight CTAs
+// (Not the aligned form of the barrier: what stands in front of it is code in which a warp's lanes part, loops with a condition per
+// entry, and an aligned barrier that a warp reaches in pieces is an illegal instruction.)
 __device__ __forceinline__ void sync_parts(int parts) {
     if (parts == 1) { __syncthreads(); return; }
-    sm100::cluster_arrive_release();
-    sm100::cluster_wait_acquire();
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
 }
 // the same variable of shared memory in CTA `rank` of the cluster
 template <typename P>

@@ -47,7 +47,7 @@ struct RowShared {
     int found[64];                     // draws
     // what the CTAs of a row read of each other
     float group_top[kGroups], cta_top, cta_sum;
-    uint32_t cta_n;
+    uint32_t cta_n, cta_m;             // entries in list, in other
     uint64_t cta_lo, cta_hi;
     double cta_mid;
     int cta_count;
@@ -64,6 +64,7 @@ struct RowShared {
     // the row's, in every CTA: bins, or in the first one chunks or the list's masses, as inclusive sums
     union { double all[kListMax]; uint64_t all_u[kListMax]; };
     uint32_t all_count[kBins];
+    uint32_t scan_count[kWarps];
 };
 
 // ---------------------------------------------------------------- a slice of a row
@@ -110,6 +111,19 @@ struct Slice {
 #pragma unroll
             for (int e = 0; e < E; ++e)
                 if (x[e] > -INFINITY) f(x[e], first + i * E + e);
+        }
+    }
+    // f(logit, index) for every entry from `thr` on
+    template <typename F>
+    __device__ __forceinline__ void each_from(float thr, F f) const {
+#pragma unroll 4
+        for (int i = (int)threadIdx.x; i < nv; i += kThreads) {
+            if (!(Row<T>::largest(data[i], -INFINITY) >= thr)) continue;
+            float x[E];
+            Row<T>::unpack(data[i], x);
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (x[e] >= thr && x[e] > -INFINITY) f(x[e], first + i * E + e);
         }
     }
     // the chunk that entry `index` of the row belongs to, counted over the parts
@@ -250,13 +264,14 @@ __device__ __forceinline__ float kth_group(RowShared& sh, int parts, int k) {
         sh.groups[tid] = *of_rank(&sh.group_top[tid % each], tid / each);
     }
     __syncthreads();
-    if (tid < kGroups) {
-        const float mine = sh.groups[tid];
-        int before = 0;
+    const int g = tid >> 2;                                                        // four threads count for a group
+    const float mine = sh.groups[g];
+    int before = 0;
 #pragma unroll 8
-        for (int g = 0; g < kGroups; ++g) before += sh.groups[g] > mine || (sh.groups[g] == mine && g < tid);
-        if (before == k - 1) sh.thr = mine;
-    }
+    for (int j = tid & 3; j < kGroups; j += 4) before += sh.groups[j] > mine || (sh.groups[j] == mine && j < g);
+    before += __shfl_xor_sync(0xffffffffu, before, 1);
+    before += __shfl_xor_sync(0xffffffffu, before, 2);
+    if (before == k - 1) sh.thr = mine;
     __syncthreads();
     return sh.thr;
 }
@@ -273,14 +288,23 @@ __device__ __forceinline__ void list_entries(RowShared& sh, const Slice<T>& sl, 
         if (at < (uint32_t)kListMax) sh.list[at] = order_key(x, index);
     });
 }
+template <typename T>
+__device__ __forceinline__ void list_from(RowShared& sh, const Slice<T>& sl, float thr) {
+    if (threadIdx.x == 0) sh.cta_n = 0;
+    __syncthreads();
+    sl.each_from(thr, [&](float x, int index) {
+        const uint32_t at = atomicAdd(&sh.cta_n, 1u);
+        if (at < (uint32_t)kListMax) sh.list[at] = order_key(x, index);
+    });
+}
 // how many entries all parts have listed (behind a sync_parts)
 __device__ __forceinline__ uint32_t listed(RowShared& sh, int parts) {
     return __reduce_add_sync(0xffffffffu, of_parts(&sh.cta_n, parts));
 }
-// All parts' entries into the first CTA's list (by the first CTA; they fit): two warps for each part
-__device__ __forceinline__ void collect(RowShared& sh, int parts) {
+// All parts' entries into the first CTA's list (by the first CTA; they fit): two warps for each part.  Returns how many.
+__device__ __forceinline__ int collect(uint64_t* list, uint32_t* count, int parts) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = warp >> 1;
-    const uint32_t n = of_parts(&sh.cta_n, parts);
+    const uint32_t n = of_parts(count, parts);
     uint32_t upto = n;
 #pragma unroll
     for (int d = 1; d < 8; d <<= 1) {
@@ -289,15 +313,16 @@ __device__ __forceinline__ void collect(RowShared& sh, int parts) {
     }
     const int more = __shfl_sync(0xffffffffu, n, r), at = __shfl_sync(0xffffffffu, upto, r) - more;
     if (r > 0 && r < parts) {
-        const uint64_t* from = of_rank(sh.list, r);
-        for (int i = lane + (warp & 1) * 32; i < more; i += 64) sh.list[at + i] = from[i];
+        const uint64_t* from = of_rank(list, r);
+        for (int i = lane + (warp & 1) * 32; i < more && at + i < kListMax; i += 64) list[at + i] = from[i];
     }
     __syncthreads();
+    return min((int)__shfl_sync(0xffffffffu, upto, 7), kListMax);
 }
-// The first CTA's list of n entries sorted, cut to the `keep` first ones where that is worth a pass; returns how many there are.
-__device__ int sort_list(RowShared& sh, int n, int keep) {
-    if (n > keep && n > kRankSort) { cut_list(sh, sh.list, n, keep); n = keep; }
-    block_sort(sh.list, n);
+// A list of n entries sorted, cut to the `keep` first ones where that is worth a pass; returns how many there are.
+__device__ int sort_list(RowShared& sh, uint64_t* list, int n, int keep) {
+    if (n > keep && n > kRankSort) { cut_list(sh, list, n, keep); n = keep; }
+    block_sort(list, n);
     return min(n, keep);
 }
 
@@ -314,46 +339,71 @@ __device__ __forceinline__ int first_above(const S* a, int n, S t, bool or_equal
 }
 
 // ---------------------------------------------------------------- histograms
-// Bins of a sixteenth of a factor of two, counted from the largest logit; what is further off than 2^-64 shares the last.
+// kBins bins of equal widths in the logarithm, counted from the largest logit: of a sixteenth of a factor of two (what is further off
+// than 2^-64 shares the last), or, where those are too coarse, of a window of them.
 struct LinearBins {
-    float top, per_bin;
-    __device__ __forceinline__ LinearBins(float top_, const Scale& sc) : top(top_), per_bin((float)fmin(16.0 * sc.c, 3.0e38)) {}
-    __device__ __forceinline__ float distance(float x) const { return fminf((top - x) * per_bin, (float)(kBins - 1)); }
-    __device__ __forceinline__ int of(float x) const { return (int)distance(x); }
+    float top, per_bin, offset, octaves;           // octaves: a bin's width in powers of two
+    bool window;
+    __device__ __forceinline__ LinearBins(float top_, const Scale& sc) : top(top_), per_bin((float)fmin(16.0 * sc.c, 3.0e38)), offset(0.f), octaves(0.0625f), window(false) {}
+    __device__ __forceinline__ void zoom(int from, int to) {                       // to bins from .. to of the coarse ones
+        const float f = (float)kBins / (float)(to - from + 1);
+        per_bin *= f;
+        octaves /= f;
+        offset = (float)from * f;
+        window = true;
+    }
+    // (single roundings throughout: a bin's entries are counted in one place and listed in another, and the compiler may fuse a product
+    // with a difference in one of them and not in the other)
+    __device__ __forceinline__ float distance(float x) const {
+        const float d = __fmul_rn(__fsub_rn(top, x), per_bin);
+        return window ? fminf(fmaxf(__fsub_rn(d, offset), -1.f), (float)kBins) : fminf(d, (float)(kBins - 1));
+    }
+    __device__ __forceinline__ int of(float x) const { return (int)floorf(distance(x)); }       // -1, kBins: in front of, behind the window
+    __device__ __forceinline__ float at(double octaves_off) const {                // where something so far below the largest entry falls
+        return (float)fmin(fmax(octaves_off / (double)octaves - (double)offset, -1.0e6), 1.0e6);
+    }
 };
 
-// Counts and masses of the row's bins, as inclusive sums in every CTA: all_count, and (masses) all, as multiples of the largest
-// entry's mass.  A bin's mass is summed up in units of 2^-16 of its upper end, in 32 bits (a slice has at most 2^15 + 8 entries): to
-// 2e-5 of it.  The last bin counts without mass.
+// Counts and masses of the row's bins, in every CTA: all_count and (masses) all, inclusive sums that begin with the given ones; masses
+// as multiples of the largest entry's.  A bin's mass is summed up in units of 2^-16 of its upper end, in 32 bits (a slice has at
+// most 2^15 + 8 entries): to 2e-5 of it.  (The last coarse bin counts without mass.)  Every CTA adds up its share of the bins over the parts
+// and hands it to all.
 template <typename T>
-__device__ void fill_bins(RowShared& sh, const Slice<T>& sl, bool masses, const LinearBins& lin) {
+__device__ void fill_bins(RowShared& sh, const Slice<T>& sl, bool masses, const LinearBins& lin, uint32_t count0, double mass0) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    sync_parts(sl.parts);                          // (nobody reads the last ones any more)
     for (int i = tid; i < kBins; i += kThreads) { sh.bins.count[i] = 0; sh.bins.mass[i] = 0; }
     __syncthreads();
-    if (masses)
-        sl.each([&](float x, int) {
-            const float d = lin.distance(x);
-            const int bin = (int)d;
-            atomicAdd(&sh.bins.count[bin], 1u);
-            if (bin < kBins - 1) atomicAdd(&sh.bins.mass[bin], (uint32_t)fmaf(ex2(((float)bin - d) * 0.0625f), 65536.f, 0.5f));
-        });
-    else
-        sl.each([&](float x, int) { atomicAdd(&sh.bins.count[lin.of(x)], 1u); });
+    sl.each([&](float x, int) {
+        const float d = lin.distance(x), b = floorf(d);
+        const int bin = (int)b;
+        if (bin < 0 || bin >= kBins) return;
+        atomicAdd(&sh.bins.count[bin], 1u);
+        if (masses && (lin.window || bin < kBins - 1)) atomicAdd(&sh.bins.mass[bin], (uint32_t)fmaf(ex2((b - d) * lin.octaves), 65536.f, 0.5f));
+    });
     sync_parts(sl.parts);
-    for (int i = tid; i < kBins; i += kThreads) {
-        uint32_t c = 0;
-        double m = 0.0;
-        for (int r = 0; r < sl.parts; ++r) {
-            c += *of_rank(&sh.bins.count[i], r);
-            if (masses) m += (double)*of_rank(&sh.bins.mass[i], r);
+    const int share = kBins / sl.parts;
+    for (int j = tid; j < share; j += kThreads) {
+        const int i = sl.rank * share + j;
+        uint32_t c[8], m[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+            c[r] = r < sl.parts ? *of_rank(&sh.bins.count[i], r) : 0;
+            m[r] = masses && r < sl.parts ? *of_rank(&sh.bins.mass[i], r) : 0;
         }
-        sh.all_count[i] = c;
-        sh.all[i] = m * (double)exp2f((float)i * -0.0625f) * (1.0 / 65536.0);
+        uint32_t count = 0;
+        double mass = 0.0;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) { count += c[r]; mass += (double)m[r]; }
+        mass *= (double)exp2f(-((float)i + lin.offset) * lin.octaves) * (1.0 / 65536.0);
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+            if (r < sl.parts) {
+                *of_rank(&sh.all_count[i], r) = count;
+                *of_rank(&sh.all[i], r) = mass;
+            }
     }
+    sync_parts(sl.parts);
     if (masses) block_scan(sh.all, kBins, sh.tmp_d);
-    // the counts: two per thread
-    __syncthreads();
     const uint32_t x = sh.all_count[2 * tid], y = x + sh.all_count[2 * tid + 1];
     uint32_t incl = y;
 #pragma unroll
@@ -361,12 +411,13 @@ __device__ void fill_bins(RowShared& sh, const Slice<T>& sl, bool masses, const 
         const uint32_t o = __shfl_up_sync(0xffffffffu, incl, d);
         if (lane >= d) incl += o;
     }
-    if (lane == 31) sh.wcnt[warp] = incl;
+    if (lane == 31) sh.scan_count[warp] = incl;
     __syncthreads();
-    uint32_t before = incl - y;
-    for (int w = 0; w < warp; ++w) before += sh.wcnt[w];
+    uint32_t before = incl - y + count0;
+    for (int w = 0; w < warp; ++w) before += sh.scan_count[w];
     sh.all_count[2 * tid] = before + x;
     sh.all_count[2 * tid + 1] = before + y;
+    if (masses && mass0 != 0.0) { sh.all[2 * tid] += mass0; sh.all[2 * tid + 1] += mass0; }
     __syncthreads();
 }
 
@@ -397,7 +448,6 @@ __device__ void key_bins(RowShared& sh, const Slice<T>& sl, bool by_mass, const 
 template <typename T>
 __device__ void search_border(RowShared& sh, const Slice<T>& sl, bool by_mass, uint64_t target, double share, uint64_t upto, const Scale& sc, int ref,
                               uint64_t* border) {
-    const int tid = threadIdx.x;
     uint64_t lo = 0, hi = upto, before = 0;
     bool first = true;
     while (true) {
@@ -442,32 +492,60 @@ top_kernel(const void* logits, long long ld, int V, int parts, int K, float inv_
     sync_parts(parts);
     const float top = top_of_parts(sh, parts);
     uint32_t n = kListMax + 1;
+    bool two_lists = false;
     if (K <= kFewK) {
         const float thr = kth_group(sh, parts, K);
-        list_entries(sh, sl, [&](float x, int) { return x >= thr; });
+        list_from(sh, sl, thr);
         sync_parts(parts);
         n = listed(sh, parts);
     }
     if (n > (uint32_t)kListMax && top > -INFINITY) {
-        const LinearBins lin(top, Scale(1.f));
-        fill_bins(sh, sl, false, lin);
-        const int bin = min(first_above(sh.all_count, kBins, (uint32_t)K, true), kBins - 1);
-        n = sh.all_count[bin];
-        if (n <= (uint32_t)kListMax) {
-            list_entries(sh, sl, [&](float x, int) { return lin.of(x) <= bin; });
-        } else {
-            uint64_t border = ~0ull;
-            if (sh.all_count[kBins - 1] > (uint32_t)K) search_border(sh, sl, false, (uint64_t)K, -1.0, ~0ull, Scale(1.f), 0, &border);
+        // the bin of the K-th entry; where it is too full, that bin in finer ones
+        LinearBins lin(top, Scale(1.f));
+        fill_bins(sh, sl, false, lin, 0, 0.0);
+        const uint32_t n_all = sh.all_count[kBins - 1];
+        uint32_t before = 0;
+        int bin = min(first_above(sh.all_count, kBins, (uint32_t)K, true), kBins - 1);
+        if (n_all > (uint32_t)K && sh.all_count[bin] - (bin ? sh.all_count[bin - 1] : 0) > (uint32_t)kListMax && bin < kBins - 1) {
+            before = bin ? sh.all_count[bin - 1] : 0;
+            lin.zoom(bin, bin);
+            __syncthreads();
+            fill_bins(sh, sl, false, lin, before, 0.0);
+            bin = min(first_above(sh.all_count, kBins, (uint32_t)K, true), kBins - 1);
+        }
+        // what stands in front of the bin (fewer than K) and the bin's own entries, listed apart; thousands of equal logits there are
+        // searched for the K-th's key
+        if (bin) before = sh.all_count[bin - 1];
+        uint64_t border = ~0ull;
+        if (sh.all_count[bin] - before > (uint32_t)kListMax) {
+            if (n_all > (uint32_t)K) search_border(sh, sl, false, (uint64_t)K, -1.0, ~0ull, Scale(1.f), 0, &border);
             sync_parts(parts);
             list_entries(sh, sl, [&](float x, int i) { return order_key(x, i) <= border; });
+        } else {
+            if (tid == 0) { sh.cta_n = 0; sh.cta_m = 0; }
+            __syncthreads();
+            sl.each([&](float x, int index) {
+                const int b = lin.of(x);
+                if (b > bin) return;
+                uint64_t* to = b < bin ? sh.list : sh.other;
+                const uint32_t at = atomicAdd(b < bin ? &sh.cta_n : &sh.cta_m, 1u);
+                if (at < (uint32_t)kListMax) to[at] = order_key(x, index);
+            });
+            two_lists = true;
         }
         sync_parts(parts);
     }
     if (rank == 0) {
         int have = 0;
         if (top > -INFINITY) {
-            collect(sh, parts);
-            have = sort_list(sh, min(listed(sh, parts), (uint32_t)kListMax), K);
+            have = min(collect(sh.list, &sh.cta_n, parts), kListMax);
+            if (two_lists) {
+                const int more = collect(sh.other, &sh.cta_m, parts), take = max(0, min(K - have, more));
+                sort_list(sh, sh.other, more, max(1, take));
+                for (int i = tid; i < take; i += kThreads) sh.list[have + i] = sh.other[i];
+                have += take;
+            }
+            have = sort_list(sh, sh.list, have, K);
         }
         for (int i = tid; i < K; i += kThreads) {
             values[r * K + i] = i < have ? key_logit(sh.list[i]) : -INFINITY;
@@ -729,26 +807,59 @@ sample_kernel(SampleCall a) {
         // ---- the list
         if (by_k && k <= kFewK) {
             const float thr = kth_group(sh, parts, k);
-            list_entries(sh, sl, [&](float x, int) { return x >= thr; });
+            list_from(sh, sl, thr);
             sync_parts(parts);
             narrow = listed(sh, parts) <= (uint32_t)kListMax;
         }
         if (!narrow && (by_k || by_p)) {
-            const LinearBins lin(top, sc);
-            fill_bins(sh, sl, by_p, lin);
-            const int n_all = sh.all_count[kBins - 1];
-            const bool cut_k = by_k && k < n_all;
-            // bin of the k-th entry; bins between which the border of top_p must lie: masses are known to 2e-5, and M, the mass of the
-            // k first entries, to that of the k-th's bin
-            const int bk = cut_k ? min(first_above(sh.all_count, kBins, (uint32_t)k, true), kBins - 1) : kBins - 1;
-            int b_lo = bk, b_hi = bk;
-            if (by_p) {
-                const double m_lo = cut_k && bk > 0 ? sh.all[bk - 1] : (cut_k ? 1.0 : sh.all[bk]), m_hi = sh.all[bk];
-                b_lo = min(first_above(sh.all, kBins, (double)p * m_lo * (1.0 - 1e-4), true), bk);
-                b_hi = min(first_above(sh.all, kBins, (double)p * m_hi * (1.0 + 1e-4), true), bk);
+            LinearBins lin(top, sc);
+            fill_bins(sh, sl, by_p, lin, 0, 0.0);
+            const uint32_t n_all = sh.all_count[kBins - 1];
+            const double m_all = sh.all[kBins - 1];
+            const bool cut_k = by_k && (uint32_t)k < n_all;
+            uint32_t count0 = 0;                                                   // what stands in front of the bins
+            double mass0 = 0.0;
+            int bk, b_lo, b_hi, m_lo;
+            bool p_counts;
+            uint32_t n_list, n_down;
+            const auto count_to = [&](int b) { return b >= 0 ? sh.all_count[b] : count0; };
+            const auto mass_to = [&](int b) { return b >= 0 ? sh.all[b] : mass0; };
+            const auto find = [&]() {
+                // bin of the k-th entry; bins between which the border of top_p must lie: masses are known to 2e-5, and M, the mass
+                // of the k first entries, to that of the k-th's bin
+                bk = cut_k ? min(first_above(sh.all_count, kBins, (uint32_t)k, true), kBins - 1) : kBins - 1;
+                b_lo = b_hi = bk;
+                if (by_p) {
+                    const double lo = cut_k ? fmax(mass_to(bk - 1), 1.0) : m_all, hi = cut_k ? mass_to(bk) : m_all;
+                    b_lo = min(first_above(sh.all, kBins, (double)p * lo * (1.0 - 1e-4), true), bk);
+                    b_hi = min(first_above(sh.all, kBins, (double)p * hi * (1.0 + 1e-4), true), bk);
+                }
+                // min_p's border: above, among or below the listed bins
+                m_lo = b_lo;
+                p_counts = by_p;
+                if (by_mp) {
+                    const int bm = (int)floorf(lin.at(-log2((double)mp)));
+                    if (bm + 1 < b_lo) { p_counts = false; m_lo = -1; }
+                    else m_lo = min(m_lo, max(0, bm - 1));
+                }
+                const int to = p_counts ? b_hi : bk;
+                n_list = count_to(to) - count_to(max(m_lo, 0) - 1) + (cut_k && bk > to ? count_to(bk) - count_to(bk - 1) : 0);
+                n_down = count_to(cut_k ? bk : b_hi);                              // all down to the border
+            };
+            find();
+            if ((cut_k || by_p) && m_lo >= 0 && n_list > (uint32_t)kListMax && n_down > (uint32_t)kListMax) {
+                const int from = m_lo, to = max(bk * cut_k, b_hi);
+                if (to < kBins - 1) {
+                    count0 = count_to(from - 1);
+                    mass0 = mass_to(from - 1);
+                    lin.zoom(from, to);
+                    __syncthreads();
+                    fill_bins(sh, sl, by_p, lin, count0, mass0);
+                    find();
+                }
             }
             const int end = by_p ? b_hi : bk;
-            if (sh.all_count[end] <= (uint32_t)kListMax && (cut_k || by_p) && (!(cut_k && by_p) || sh.all_count[bk] <= (uint32_t)kListMax)) {
+            if ((cut_k || by_p) && n_down <= (uint32_t)kListMax) {
                 // everything down to the border is few: listed (with top-k and top-p, down to the k-th)
                 const int down = cut_k ? bk : end;
                 __syncthreads();
@@ -761,27 +872,17 @@ sample_kernel(SampleCall a) {
                 narrow = true;
             } else if (cut_k || by_p) {
                 // flat: the borders' bins are listed, what is above them is summed up
-                int m_lo = b_lo;                                                   // the listed bins start here
-                bool p_counts = by_p;
-                if (by_mp) {
-                    // min_p's border: above, among or below the listed bins
-                    const double d = -16.0 * log2((double)mp);
-                    const int bm = (int)fmin(d, (double)(kBins - 1));
-                    if (bm + 1 < b_lo) { p_counts = false; m_lo = -1; }
-                    else m_lo = min(m_lo, max(0, bm - 1));
-                }
                 if (m_lo >= 0) {
-                    const int n_above = m_lo ? sh.all_count[m_lo - 1] : 0, above_k = cut_k && bk ? sh.all_count[bk - 1] : 0;
+                    const int n_above = count_to(m_lo - 1), above_k = cut_k ? count_to(bk - 1) : 0, in_bk = cut_k ? (int)count_to(bk) - above_k : 0;
                     const int to = p_counts ? b_hi : bk;
-                    const uint32_t n_list = sh.all_count[to] - n_above + (cut_k && bk > to ? sh.all_count[bk] - above_k : 0);
                     if (n_list <= (uint32_t)kListMax) {
                         if (tid == 0) sh.cta_n = 0;
                         __syncthreads();
                         double mid = 0.0;
                         sum_chunks(sh, sl, sc, ref, [&](float x, double) { return lin.of(x) < m_lo; },
                                    [&](float x, int index, double m) {
-                                       const int b = x > -INFINITY ? lin.of(x) : kBins;
-                                       if (b == kBins) return;
+                                       if (!(x > -INFINITY)) return;
+                                       const int b = lin.of(x);
                                        if ((b >= m_lo && b <= to) || (cut_k && b == bk)) {
                                            const uint32_t at = atomicAdd(&sh.cta_n, 1u);
                                            if (at < (uint32_t)kListMax) sh.list[at] = order_key(x, index);
@@ -797,8 +898,7 @@ sample_kernel(SampleCall a) {
                         sync_parts(parts);
                         if (rank == 0) {
                             // masses above the listed bins, chunk by chunk; the listed entries in order
-                            collect(sh, parts);
-                            const int n = min(n_list, (uint32_t)kListMax), per_part = kWarps * sl.iters, chunks = parts * per_part;
+                            const int n = collect(sh.list, &sh.cta_n, parts), per_part = kWarps * sl.iters, chunks = parts * per_part;
                             block_sort(sh.list, n);
                             double above = 0.0;
                             mid = 0.0;
@@ -814,7 +914,6 @@ sample_kernel(SampleCall a) {
                             block_scan(sh.all, n, sh.tmp_d);
                             // how many of the list belong to the k first; the listed ones in front of the k-th's bin stand before them
                             int len = n;
-                            const int in_bk = cut_k ? sh.all_count[bk] - above_k : 0;                // (0: no top-k)
                             const bool apart = cut_k && bk > to;
                             if (cut_k) len = (apart ? n - in_bk : above_k - n_above) + (k - above_k);
                             len = min(len, n);
@@ -832,10 +931,10 @@ sample_kernel(SampleCall a) {
                                 }
                                 len = l;
                             }
+                            if (n != (int)n_list) set_status(a.status, SD_ERR_BOUNDS);               // (counted and listed alike, or something is wrong)
                             if (tid == 0) {
-                                sh.border = len ? sh.list[len - 1] : 0;                              // (none of the list: all above its bins)
+                                sh.border = len ? sh.list[len - 1] : sh.list[0] - 1;                 // (none of the list: all above its bins)
                                 sh.kept = n_above + len;
-                                if (!len) sh.border = sh.list[0] - 1;
                                 sh.total = above + (len ? sh.all[len - 1] : 0.0);
                             }
                             // the draws' chunks: with the listed entries that stay
@@ -844,9 +943,12 @@ sample_kernel(SampleCall a) {
                                 const int stays = len;
                                 for (int i = tid; i < kBins; i += kThreads) sh.other[i] = 0;
                                 __syncthreads();
-                                for (int i = tid; i < stays; i += kThreads)
-                                    atomicAdd(reinterpret_cast<unsigned long long*>(&sh.other[sl.chunk_of(key_index(sh.list[i]))]),
-                                              (unsigned long long)(sc.mass(key_logit(sh.list[i]), ref) * kUnit + 0.5));
+                                for (int i = tid; i < stays; i += kThreads) {
+                                    const int id = sl.chunk_of(key_index(sh.list[i]));
+                                    if (id >= 0 && id < chunks)
+                                        atomicAdd(reinterpret_cast<unsigned long long*>(&sh.other[id]), (unsigned long long)(sc.mass(key_logit(sh.list[i]), ref) * kUnit + 0.5));
+                                    else set_status(a.status, SD_ERR_BOUNDS);
+                                }
                                 __syncthreads();
                                 for (int i = tid; i < chunks; i += kThreads)
                                     sh.all[i] = *of_rank(&sh.chunk[i % per_part], i / per_part) + (double)sh.other[i] / kUnit;
@@ -855,8 +957,7 @@ sample_kernel(SampleCall a) {
                         }
                         sync_parts(parts);
                         border = *of_rank(&sh.border, 0);
-                        kept = *of_rank(&sh.kept, 0);
-                        total = *of_rank(&sh.total, 0);
+                                        total = *of_rank(&sh.total, 0);
                         kind = -1;                                                 // (done: borders, count and mass are known)
                     } else {
                         // more than a list holds in the borders' bins
@@ -875,10 +976,9 @@ sample_kernel(SampleCall a) {
 
         // ---- the row is decided on the list
         if (narrow) {
+            if (dense) fill_floats(dense + o0, o1 - o0, a.scaled ? -INFINITY : 0.f);
             if (rank == 0) {
-                collect(sh, parts);
-                int n = listed(sh, parts);
-                n = sort_list(sh, n, by_k ? min(k, kListMax) : kListMax);
+                int n = collect(sh.list, &sh.cta_n, parts);
                 double all = 0.0;
                 if (summed) {
                     const int per_part = kWarps * sl.iters, chunks = parts * per_part;
@@ -888,8 +988,10 @@ sample_kernel(SampleCall a) {
                     __syncthreads();
                     all = 0.0;
                     for (int w = 0; w < kWarps; ++w) all += sh.tmp_d[w];
-                    __syncthreads();
                 }
+                // the other CTAs' parts of the output are filled, and they are not needed any more
+                sync_parts(parts);
+                n = sort_list(sh, sh.list, n, by_k ? min(k, kListMax) : kListMax);
                 for (int i = tid; i < n; i += kThreads) sh.all[i] = sc.mass(key_logit(sh.list[i]), ref);
                 block_scan(sh.all, n, sh.tmp_d);
                 int len = n;
@@ -903,7 +1005,10 @@ sample_kernel(SampleCall a) {
                     len = l;
                 }
                 len = max(len, 1);
-                if (tid == 0) { sh.kept = len; sh.total = sh.all[len - 1]; }
+                kept = len;
+                total = sh.all[len - 1];
+            } else {
+                sync_parts(parts);
             }
             kind = kList;
         } else if (kind == kWide) {
@@ -957,50 +1062,54 @@ sample_kernel(SampleCall a) {
     }
 
     // ---- outputs
-    if (dense && kind != kWide) fill_floats(dense + o0, o1 - o0, a.scaled ? -INFINITY : 0.f);
     if (kind == kNone) {
+        if (dense) fill_floats(dense + o0, o1 - o0, a.scaled ? -INFINITY : 0.f);
         if (rank == 0) {
             if (bad && tid == 0) set_status(a.status, SD_ERR_INVALID_ARG);
             for (int i = tid; i < a.N; i += kThreads) { a.tokens[r * a.N + i] = -1; if (a.prob) a.prob[r * a.N + i] = 0.f; }
             if (tid == 0) { if (a.lse) a.lse[r] = -INFINITY; if (a.kept) a.kept[r] = 0; }
         }
-    } else {
-        if (dense) sync_parts(parts);                                              // all parts are filled before entries go in; the total is known
-        else __syncthreads();
-        if (dense) { total = *of_rank(&sh.total, 0); }
-        if (rank == 0) {
-            total = sh.total;
-            kept = sh.kept;
+        if (parts > 1) sync_parts(parts);
+    } else if (kind == kList) {
+        if (rank == 0) {                                                           // (alone by now)
             if (tid == kThreads - 1) {
                 if (a.lse) a.lse[r] = log_mass(sc, top, it, ref, total);
                 if (a.kept) a.kept[r] = kept;
             }
-            if (kind == kList) {
-                if (dense)
-                    for (int i = tid; i < kept; i += kThreads) {
-                        const float x = key_logit(sh.list[i]);
-                        dense[key_index(sh.list[i])] = a.scaled ? scaled_logit(x, it) : (float)(sc.mass(x, ref) / total);
-                    }
-                if (a.N) draw_from_list(sh, a, r, sc, ref, kept);
-            } else {
-                const int chunks = parts * kWarps * sl.iters;
-                for (int d = warp; d < a.N; d += kWarps) {                         // a warp per draw
-                    const float u = a.u[r * a.N + d];
-                    const bool fine = u >= 0.f && u < 1.f;
-                    int token = -1;
-                    double mass = 0.0;
-                    if (fine) {
-                        const double target = (double)u * sh.all[chunks - 1];
-                        int g = first_above(sh.all, chunks, target, false);
-                        while (g >= chunks || (g > 0 && !(sh.all[g] > sh.all[g - 1]))) --g;
-                        token = chunk_crossing(sl, g, target - (g ? sh.all[g - 1] : 0.0), sc, ref,
-                                               [&](float x, int index, double m) { return x > -INFINITY && order_key(x, index) <= border && m >= least; }, &mass);
-                    } else if (lane == 0) set_status(a.status, SD_ERR_INVALID_ARG);
-                    if (lane == 0) { a.tokens[r * a.N + d] = token; if (a.prob) a.prob[r * a.N + d] = (float)(mass / total); }
+            if (dense)
+                for (int i = tid; i < kept; i += kThreads) {
+                    const float x = key_logit(sh.list[i]);
+                    dense[key_index(sh.list[i])] = a.scaled ? scaled_logit(x, it) : (float)(sc.mass(x, ref) / total);
                 }
+            if (a.N) draw_from_list(sh, a, r, sc, ref, kept);
+        }
+    } else {
+        if (dense) sync_parts(parts);                                              // the total is known
+        else __syncthreads();
+        if (dense) total = *of_rank(&sh.total, 0);
+        if (rank == 0) {
+            total = sh.total;
+            if (tid == kThreads - 1) {
+                if (a.lse) a.lse[r] = log_mass(sc, top, it, ref, total);
+                if (a.kept) a.kept[r] = sh.kept;
+            }
+            const int chunks = parts * kWarps * sl.iters;
+            for (int d = warp; d < a.N; d += kWarps) {                             // a warp per draw
+                const float u = a.u[r * a.N + d];
+                const bool fine = u >= 0.f && u < 1.f;
+                int token = -1;
+                double mass = 0.0;
+                if (fine) {
+                    const double target = (double)u * sh.all[chunks - 1];
+                    int g = first_above(sh.all, chunks, target, false);
+                    while (g >= chunks || (g > 0 && !(sh.all[g] > sh.all[g - 1]))) --g;
+                    token = chunk_crossing(sl, g, target - (g ? sh.all[g - 1] : 0.0), sc, ref,
+                                           [&](float x, int index, double m) { return x > -INFINITY && order_key(x, index) <= border && m >= least; }, &mass);
+                } else if (lane == 0) set_status(a.status, SD_ERR_INVALID_ARG);
+                if (lane == 0) { a.tokens[r * a.N + d] = token; if (a.prob) a.prob[r * a.N + d] = (float)(mass / total); }
             }
         }
-        if (dense && kind == kWide) {
+        if (dense) {
             const float c32 = (float)sc.c, at_top = (float)(top_mass / total);
             const T* entries = reinterpret_cast<const T*>(data);
             const int lo = max(0, sl.first), hi = min(V, sl.first + sl.nv * Slice<T>::E);
@@ -1012,10 +1121,10 @@ sample_kernel(SampleCall a) {
                 dense[v] = a.scaled ? (in ? scaled_logit(x, it) : -INFINITY) : (in ? at_top * exp2f((x - top) * c32) : 0.f);
             }
         }
+        __syncwarp();
+        if (parts > 1) sync_parts(parts);                                          // nobody leaves while another CTA reads
     }
     if (!ok) { set_status(a.status, SD_ERR_TIMEOUT); sm100::unwind_pause(); }
-    __syncwarp();
-    if (parts > 1) sync_parts(parts);                                              // nobody leaves while another CTA reads
 }
 
 // CTAs per row: slices of at most 80 KB while eight are enough for that, and more of them where the rows leave SMs idle
