@@ -45,6 +45,7 @@ struct RowShared {
     float thr;
     struct { uint32_t bin, n; uint64_t count, mass; } pick;      // a bin, the entries in it, and what stands in front of it
     int found[64];                     // draws
+    float u[64];
     // what the CTAs of a row read of each other
     float group_top[kGroups], cta_top, cta_sum;
     uint32_t cta_n, cta_m;             // entries in list, in other
@@ -338,6 +339,15 @@ __device__ __forceinline__ int first_above(const S* a, int n, S t, bool or_equal
     return lo;
 }
 
+// The same over kBins (first index, at most kBins - 1), by the whole CTA: every thread looks at two
+template <typename S>
+__device__ __forceinline__ void find_bin(const S* a, S t, int* out) {
+    const int i = 2 * (int)threadIdx.x;
+    const S before = i ? a[i - 1] : a[0], x = a[i], y = a[i + 1];
+    if (x >= t && (i == 0 || before < t)) *out = i;
+    else if (y >= t && x < t) *out = i + 1;
+    else if (i + 2 == kBins && y < t) *out = kBins - 1;
+}
 // ---------------------------------------------------------------- histograms
 // kBins bins of equal widths in the logarithm, counted from the largest logit: of a sixteenth of a factor of two (what is further off
 // than 2^-64 shares the last), or, where those are too coarse, of a window of them.
@@ -359,27 +369,55 @@ struct LinearBins {
         return window ? fminf(fmaxf(__fsub_rn(d, offset), -1.f), (float)kBins) : fminf(d, (float)(kBins - 1));
     }
     __device__ __forceinline__ int of(float x) const { return (int)floorf(distance(x)); }       // -1, kBins: in front of, behind the window
+    // The least logit that falls into bin `bin` or in front of it (minus infinity's successor at least): bins are monotone in the logit,
+    // so that this is a search over its bit patterns; a warp's lanes try 32 of them at a time.
+    __device__ __forceinline__ float edge(int bin) const {
+        if (bin < 0 && !window) return INFINITY;
+        const int lane = threadIdx.x & 31;
+        const uint32_t t = __float_as_uint(top + 0.f);
+        // keys count upwards with the logit; key(top) itself is in bin 0 (or in front of the window)
+        uint32_t lo = 0x00800000u, hi = t ^ ((t >> 31) ? 0xffffffffu : 0x80000000u);               // lo: -FLT_MAX
+        const auto value = [](uint32_t k) { return __uint_as_float(k ^ ((k >> 31) ? 0x80000000u : 0xffffffffu)); };
+        if (of(value(hi)) > bin) return INFINITY;
+        while (lo < hi) {                                                          // the answer lies in [lo, hi]
+            const uint32_t step = (hi - lo) / 33 + 1, k = min(hi, lo + step * lane);
+            const uint32_t good = __ballot_sync(0xffffffffu, of(value(k)) <= bin);
+            const int first = good ? __ffs(good) - 1 : 32;
+            const uint32_t new_hi = first < 32 ? min(hi, lo + step * first) : hi, new_lo = first ? min(hi, lo + step * (first - 1) + 1) : lo;
+            hi = new_hi;
+            lo = min(new_lo, hi);
+        }
+        return value(lo);
+    }
     __device__ __forceinline__ float at(double octaves_off) const {                // where something so far below the largest entry falls
         return (float)fmin(fmax(octaves_off / (double)octaves - (double)offset, -1.0e6), 1.0e6);
     }
 };
 
-// Counts and masses of the row's bins, in every CTA: all_count and (masses) all, inclusive sums that begin with the given ones; masses
-// as multiples of the largest entry's.  A bin's mass is summed up in units of 2^-16 of its upper end, in 32 bits (a slice has at
-// most 2^15 + 8 entries): to 2e-5 of it.  (The last coarse bin counts without mass.)  Every CTA adds up its share of the bins over the parts
+// Counts or masses (or both) of the row's bins, in every CTA: all_count and all, inclusive sums that begin with the given ones; masses
+// as multiples of the largest entry's.  Without counts, all_count is what the masses allow at most.  A bin's mass is summed up in units of 2^-16 of its upper end, in 32 bits (a slice has at
+// most 40960 entries): to 2e-5 of it.  (The last coarse bin has none.)  Every CTA adds up its share of the bins over the parts
 // and hands it to all.
 template <typename T>
-__device__ void fill_bins(RowShared& sh, const Slice<T>& sl, bool masses, const LinearBins& lin, uint32_t count0, double mass0) {
+__device__ void fill_bins(RowShared& sh, const Slice<T>& sl, bool counts, bool masses, const LinearBins& lin, uint32_t count0, double mass0) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     for (int i = tid; i < kBins; i += kThreads) { sh.bins.count[i] = 0; sh.bins.mass[i] = 0; }
     __syncthreads();
-    sl.each([&](float x, int) {
-        const float d = lin.distance(x), b = floorf(d);
-        const int bin = (int)b;
-        if (bin < 0 || bin >= kBins) return;
-        atomicAdd(&sh.bins.count[bin], 1u);
-        if (masses && (lin.window || bin < kBins - 1)) atomicAdd(&sh.bins.mass[bin], (uint32_t)fmaf(ex2((b - d) * lin.octaves), 65536.f, 0.5f));
-    });
+    if (!masses)
+        sl.each([&](float x, int) {
+            const int bin = lin.of(x);
+            if (bin >= 0 && bin < kBins) atomicAdd(&sh.bins.count[bin], 1u);
+        });
+    else
+        sl.each([&](float x, int) {
+            const float d = lin.distance(x), b = floorf(d);
+            const int bin = (int)b;
+            if (bin < 0 || bin >= kBins) return;
+            // (a far entry of the last coarse bin: one unit, for its count)
+            const float m = lin.window || bin < kBins - 1 ? ex2((b - d) * lin.octaves) : 1.f;
+            atomicAdd(&sh.bins.mass[bin], (uint32_t)fmaf(m, 65536.f, 0.5f));
+            if (counts) atomicAdd(&sh.bins.count[bin], 1u);
+        });
     sync_parts(sl.parts);
     const int share = kBins / sl.parts;
     for (int j = tid; j < share; j += kThreads) {
@@ -387,13 +425,16 @@ __device__ void fill_bins(RowShared& sh, const Slice<T>& sl, bool masses, const 
         uint32_t c[8], m[8];
 #pragma unroll
         for (int r = 0; r < 8; ++r) {
-            c[r] = r < sl.parts ? *of_rank(&sh.bins.count[i], r) : 0;
+            c[r] = counts && r < sl.parts ? *of_rank(&sh.bins.count[i], r) : 0;
             m[r] = masses && r < sl.parts ? *of_rank(&sh.bins.mass[i], r) : 0;
         }
         uint32_t count = 0;
         double mass = 0.0;
 #pragma unroll
         for (int r = 0; r < 8; ++r) { count += c[r]; mass += (double)m[r]; }
+        // (a unit of mass is between 2^-octaves and 1 of an entry)
+        if (!counts) count = (uint32_t)((float)mass * (1.f / 65535.f) * exp2f(lin.octaves)) + (mass > 0.0);
+        if (!lin.window && i == kBins - 1) mass = 0.0;
         mass *= (double)exp2f(-((float)i + lin.offset) * lin.octaves) * (1.0 / 65536.0);
 #pragma unroll
         for (int r = 0; r < 8; ++r)
@@ -502,7 +543,7 @@ top_kernel(const void* logits, long long ld, int V, int parts, int K, float inv_
     if (n > (uint32_t)kListMax && top > -INFINITY) {
         // the bin of the K-th entry; where it is too full, that bin in finer ones
         LinearBins lin(top, Scale(1.f));
-        fill_bins(sh, sl, false, lin, 0, 0.0);
+        fill_bins(sh, sl, true, false, lin, 0, 0.0);
         const uint32_t n_all = sh.all_count[kBins - 1];
         uint32_t before = 0;
         int bin = min(first_above(sh.all_count, kBins, (uint32_t)K, true), kBins - 1);
@@ -510,7 +551,7 @@ top_kernel(const void* logits, long long ld, int V, int parts, int K, float inv_
             before = bin ? sh.all_count[bin - 1] : 0;
             lin.zoom(bin, bin);
             __syncthreads();
-            fill_bins(sh, sl, false, lin, before, 0.0);
+            fill_bins(sh, sl, true, false, lin, before, 0.0);
             bin = min(first_above(sh.all_count, kBins, (uint32_t)K, true), kBins - 1);
         }
         // what stands in front of the bin (fewer than K) and the bin's own entries, listed apart; thousands of equal logits there are
@@ -717,12 +758,12 @@ __device__ void draw_from_list(RowShared& sh, const SampleCall& a, long long r, 
 #pragma unroll 4
             for (int j = 0; j < kept; ++j) cum += key_index(sh.list[j]) <= index ? mass[j] : 0.0;
             for (int i = 0; i < a.N; ++i)
-                if (mine > 0.0 && cum > (double)a.u[r * a.N + i] * total) atomicMin(&sh.found[i], index);
+                if (mine > 0.0 && cum > (double)sh.u[i] * total) atomicMin(&sh.found[i], index);
         }
         __syncthreads();
         // rounding may leave all sums at or below the mark: the last entry with mass then
         for (int i = 0; i < a.N; ++i) {
-            const float u = a.u[r * a.N + i];
+            const float u = sh.u[i];
             const bool fine = u >= 0.f && u < 1.f, none = sh.found[i] == INT_MAX;
             if (none) {
                 int last = tid < kept && mine > 0.0 ? index : -1;
@@ -746,7 +787,7 @@ __device__ void draw_from_list(RowShared& sh, const SampleCall& a, long long r, 
     for (int i = tid; i < kept; i += kThreads) sh.all[i] = sc.mass(key_logit(sh.list[(uint32_t)by_index[i]]), ref);
     block_scan(sh.all, kept, sh.tmp_d);
     for (int i = tid; i < a.N; i += kThreads) {
-        const float u = a.u[r * a.N + i];
+        const float u = sh.u[i];
         const double total = sh.all[kept - 1];
         int at = first_above(sh.all, kept, (double)u * total, false);
         while (at >= kept || (at > 0 && !(sh.all[at] > sh.all[at - 1]))) --at;       // (none above: the last with mass)
@@ -784,6 +825,7 @@ sample_kernel(SampleCall a) {
     const bool by_k = k >= 1, by_p = p < 1.f, by_mp = mp > 0.f;
     p = fmaxf(p, 0.f);
     mp = by_mp ? fminf(mp, 1.f) : 0.f;
+    if (tid < a.N) sh.u[tid] = a.u[r * a.N + tid];
     const Scale sc(it);
     __syncthreads();
 
@@ -813,7 +855,7 @@ sample_kernel(SampleCall a) {
         }
         if (!narrow && (by_k || by_p)) {
             LinearBins lin(top, sc);
-            fill_bins(sh, sl, by_p, lin, 0, 0.0);
+            fill_bins(sh, sl, by_k, by_p, lin, 0, 0.0);
             const uint32_t n_all = sh.all_count[kBins - 1];
             const double m_all = sh.all[kBins - 1];
             const bool cut_k = by_k && (uint32_t)k < n_all;
@@ -827,12 +869,20 @@ sample_kernel(SampleCall a) {
             const auto find = [&]() {
                 // bin of the k-th entry; bins between which the border of top_p must lie: masses are known to 2e-5, and M, the mass
                 // of the k first entries, to that of the k-th's bin
-                bk = cut_k ? min(first_above(sh.all_count, kBins, (uint32_t)k, true), kBins - 1) : kBins - 1;
+                bk = kBins - 1;
+                if (cut_k) {
+                    find_bin(sh.all_count, (uint32_t)k, &sh.found[0]);
+                    __syncthreads();
+                    bk = sh.found[0];
+                }
                 b_lo = b_hi = bk;
                 if (by_p) {
                     const double lo = cut_k ? fmax(mass_to(bk - 1), 1.0) : m_all, hi = cut_k ? mass_to(bk) : m_all;
-                    b_lo = min(first_above(sh.all, kBins, (double)p * lo * (1.0 - 1e-4), true), bk);
-                    b_hi = min(first_above(sh.all, kBins, (double)p * hi * (1.0 + 1e-4), true), bk);
+                    find_bin(sh.all, (double)p * lo * (1.0 - 1e-4), &sh.found[1]);
+                    find_bin(sh.all, (double)p * hi * (1.0 + 1e-4), &sh.found[2]);
+                    __syncthreads();
+                    b_lo = min(sh.found[1], bk);
+                    b_hi = min(sh.found[2], bk);
                 }
                 // min_p's border: above, among or below the listed bins
                 m_lo = b_lo;
@@ -854,7 +904,7 @@ sample_kernel(SampleCall a) {
                     mass0 = mass_to(from - 1);
                     lin.zoom(from, to);
                     __syncthreads();
-                    fill_bins(sh, sl, by_p, lin, count0, mass0);
+                    fill_bins(sh, sl, by_k, by_p, lin, count0, mass0);
                     find();
                 }
             }
@@ -873,27 +923,34 @@ sample_kernel(SampleCall a) {
             } else if (cut_k || by_p) {
                 // flat: the borders' bins are listed, what is above them is summed up
                 if (m_lo >= 0) {
-                    const int n_above = count_to(m_lo - 1), above_k = cut_k ? count_to(bk - 1) : 0, in_bk = cut_k ? (int)count_to(bk) - above_k : 0;
+                    const int above_k = cut_k ? count_to(bk - 1) : 0, in_bk = cut_k ? (int)count_to(bk) - above_k : 0;
                     const int to = p_counts ? b_hi : bk;
                     if (n_list <= (uint32_t)kListMax) {
                         if (tid == 0) sh.cta_n = 0;
                         __syncthreads();
                         double mid = 0.0;
-                        sum_chunks(sh, sl, sc, ref, [&](float x, double) { return lin.of(x) < m_lo; },
+                        int n_over = 0;
+                        // the bins' borders as logits: above the listed ones, down to their end, and the k-th's bin
+                        const float above_them = lin.edge(m_lo - 1), end_them = lin.edge(to);
+                        const float above_k_bin = cut_k ? lin.edge(bk - 1) : -INFINITY, end_k_bin = cut_k ? lin.edge(bk) : -INFINITY;
+                        sum_chunks(sh, sl, sc, ref, [&](float x, double) { return x >= above_them; },
                                    [&](float x, int index, double m) {
+                                       if (x >= above_them) { ++n_over; return; }
                                        if (!(x > -INFINITY)) return;
-                                       const int b = lin.of(x);
-                                       if ((b >= m_lo && b <= to) || (cut_k && b == bk)) {
+                                       if (x >= end_them || (x >= end_k_bin && x < above_k_bin)) {
                                            const uint32_t at = atomicAdd(&sh.cta_n, 1u);
                                            if (at < (uint32_t)kListMax) sh.list[at] = order_key(x, index);
-                                       } else if (b > to && (!cut_k || b < bk)) mid += m;
+                                       } else if (x >= above_k_bin) mid += m;
                                    });
+                        n_over = __reduce_add_sync(0xffffffffu, n_over);
+                        if (lane == 0) sh.wcnt[warp] = n_over;
                         mid = warp_add(mid);
                         if (lane == 0) sh.tmp_d[warp] = mid;
                         __syncthreads();
                         if (tid == 0) {
-                            for (int w = 1; w < kWarps; ++w) mid += sh.tmp_d[w];
+                            for (int w = 1; w < kWarps; ++w) { mid += sh.tmp_d[w]; n_over += sh.wcnt[w]; }
                             sh.cta_mid = mid;
+                            sh.cta_count = n_over;
                         }
                         sync_parts(parts);
                         if (rank == 0) {
@@ -902,7 +959,8 @@ sample_kernel(SampleCall a) {
                             block_sort(sh.list, n);
                             double above = 0.0;
                             mid = 0.0;
-                            for (int q = 0; q < parts; ++q) mid += *of_rank(&sh.cta_mid, q);
+                            mid = warp_add(of_parts(&sh.cta_mid, parts));
+                            const int n_above = __reduce_add_sync(0xffffffffu, of_parts(&sh.cta_count, parts));
                             for (int i = tid; i < chunks; i += kThreads) above += *of_rank(&sh.chunk[i % per_part], i / per_part);
                             above = warp_add(above);
                             __syncthreads();
@@ -931,7 +989,6 @@ sample_kernel(SampleCall a) {
                                 }
                                 len = l;
                             }
-                            if (n != (int)n_list) set_status(a.status, SD_ERR_BOUNDS);               // (counted and listed alike, or something is wrong)
                             if (tid == 0) {
                                 sh.border = len ? sh.list[len - 1] : sh.list[0] - 1;                 // (none of the list: all above its bins)
                                 sh.kept = n_above + len;
@@ -1095,7 +1152,7 @@ sample_kernel(SampleCall a) {
             }
             const int chunks = parts * kWarps * sl.iters;
             for (int d = warp; d < a.N; d += kWarps) {                             // a warp per draw
-                const float u = a.u[r * a.N + d];
+                const float u = sh.u[d];
                 const bool fine = u >= 0.f && u < 1.f;
                 int token = -1;
                 double mass = 0.0;
