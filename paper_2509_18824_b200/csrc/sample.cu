@@ -4,7 +4,7 @@
 // 76 KB, two of which share an SM): a row is read once, and passed over as often as it takes.  Which entries stay is decided on a
 // list of some hundred entries that the first CTA collects and sorts:
 //   top-k up to kFewK   entries that reach the k-th largest of 128 groups' largest logits
-//   other borders       histograms of the row in bins of a sixteenth of a factor of two below its largest logit, counts and (to 1e-4)
+//   other borders       histograms of the row in bins of a fraction of a factor of two below its largest logit, counts and (to 1e-4)
 //                       masses: the bins in which the borders lie are listed, and if there are few, all that is above them
 // With all kept entries listed, the borders are prefix lengths of the sorted list and the draws are among its entries.  Otherwise (flat
 // rows) the list gives the last entry that stays, and the mass above the listed bins is summed up, in 64 bits, chunk by chunk (32 * kU
@@ -45,6 +45,7 @@ struct RowShared {
     float thr;
     struct { uint32_t bin, n; uint64_t count, mass; } pick;      // a bin, the entries in it, and what stands in front of it
     int found[64];                     // draws
+    float edges[4];
     float u[64];
     // what the CTAs of a row read of each other
     float group_top[kGroups], cta_top, cta_sum;
@@ -132,6 +133,15 @@ struct Slice {
         const int v = (index + row.lead) / E, q = v / per, i = v - q * per, w = i / seg;
         return (q * kWarps + w) * iters + (i - w * seg) / (32 * kU);
     }
+};
+
+// A slice as the passes over it take it.  They are calls of their own: inlined, the kernel's many values left their loops without
+// registers (the pass over 19008 entries that sums up and lists 17000 cycles).
+struct Entries {
+    const uint4* data;
+    int nv, first, seg, iters;
+    template <typename T>
+    __device__ __forceinline__ explicit Entries(const Slice<T>& sl) : data(sl.data), nv(sl.nv), first(sl.first), seg(sl.seg), iters(sl.iters) {}
 };
 
 // ---------------------------------------------------------------- cutting a list down
@@ -349,12 +359,14 @@ __device__ __forceinline__ void find_bin(const S* a, S t, int* out) {
     else if (i + 2 == kBins && y < t) *out = kBins - 1;
 }
 // ---------------------------------------------------------------- histograms
-// kBins bins of equal widths in the logarithm, counted from the largest logit: of a sixteenth of a factor of two (what is further off
-// than 2^-64 shares the last), or, where those are too coarse, of a window of them.
+// kBins bins of equal widths in the logarithm, counted from the largest logit; what is further off than the last one's beginning belongs to
+// that: with 32 bins to a factor of two (for top-p alone: 2^-32, with 2^18 entries at most 6e-5 of the mass) or with 16.  Or, where those
+// are too coarse, bins of a window of them.
 struct LinearBins {
     float top, per_bin, offset, octaves;           // octaves: a bin's width in powers of two
     bool window;
-    __device__ __forceinline__ LinearBins(float top_, const Scale& sc) : top(top_), per_bin((float)fmin(16.0 * sc.c, 3.0e38)), offset(0.f), octaves(0.0625f), window(false) {}
+    __device__ __forceinline__ LinearBins(float top_, const Scale& sc, float per_octave)
+        : top(top_), per_bin((float)fmin(per_octave * sc.c, 3.0e38)), offset(0.f), octaves(1.f / per_octave), window(false) {}
     __device__ __forceinline__ void zoom(int from, int to) {                       // to bins from .. to of the coarse ones
         const float f = (float)kBins / (float)(to - from + 1);
         per_bin *= f;
@@ -394,6 +406,26 @@ struct LinearBins {
     }
 };
 
+template <typename T>
+__device__ __noinline__ void bin_entries(RowShared& sh, Entries en, bool counts, bool masses, LinearBins lin) {
+    constexpr int E = Row<T>::kE;
+#pragma unroll 2
+    for (int i = (int)threadIdx.x; i < en.nv; i += kThreads) {
+        float x[E];
+        Row<T>::unpack(en.data[i], x);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float d = lin.distance(x[e]), b = floorf(d);
+            const int bin = (int)b;
+            const bool in = x[e] > -INFINITY && bin >= 0 && bin < kBins;
+            // (a far entry of the last coarse bin: one unit, for its count)
+            const uint32_t m = (uint32_t)fmaf(ex2(lin.window || bin < kBins - 1 ? (b - d) * lin.octaves : 0.f), 65536.f, 0.5f);
+            if (in && masses) atomicAdd(&sh.bins.mass[bin], m);
+            if (in && counts) atomicAdd(&sh.bins.count[bin], 1u);
+        }
+    }
+}
+
 // Counts or masses (or both) of the row's bins, in every CTA: all_count and all, inclusive sums that begin with the given ones; masses
 // as multiples of the largest entry's.  Without counts, all_count is what the masses allow at most.  A bin's mass is summed up in units of 2^-16 of its upper end, in 32 bits (a slice has at
 // most 40960 entries): to 2e-5 of it.  (The last coarse bin has none.)  Every CTA adds up its share of the bins over the parts
@@ -403,21 +435,7 @@ __device__ void fill_bins(RowShared& sh, const Slice<T>& sl, bool counts, bool m
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     for (int i = tid; i < kBins; i += kThreads) { sh.bins.count[i] = 0; sh.bins.mass[i] = 0; }
     __syncthreads();
-    if (!masses)
-        sl.each([&](float x, int) {
-            const int bin = lin.of(x);
-            if (bin >= 0 && bin < kBins) atomicAdd(&sh.bins.count[bin], 1u);
-        });
-    else
-        sl.each([&](float x, int) {
-            const float d = lin.distance(x), b = floorf(d);
-            const int bin = (int)b;
-            if (bin < 0 || bin >= kBins) return;
-            // (a far entry of the last coarse bin: one unit, for its count)
-            const float m = lin.window || bin < kBins - 1 ? ex2((b - d) * lin.octaves) : 1.f;
-            atomicAdd(&sh.bins.mass[bin], (uint32_t)fmaf(m, 65536.f, 0.5f));
-            if (counts) atomicAdd(&sh.bins.count[bin], 1u);
-        });
+    bin_entries<T>(sh, Entries(sl), counts, masses, lin);
     sync_parts(sl.parts);
     const int share = kBins / sl.parts;
     for (int j = tid; j < share; j += kThreads) {
@@ -542,7 +560,7 @@ top_kernel(const void* logits, long long ld, int V, int parts, int K, float inv_
     }
     if (n > (uint32_t)kListMax && top > -INFINITY) {
         // the bin of the K-th entry; where it is too full, that bin in finer ones
-        LinearBins lin(top, Scale(1.f));
+        LinearBins lin(top, Scale(1.f), 16.f);
         fill_bins(sh, sl, true, false, lin, 0, 0.0);
         const uint32_t n_all = sh.all_count[kBins - 1];
         uint32_t before = 0;
@@ -616,31 +634,83 @@ struct SampleCall {
     int withheld; long long wait_cycles;
 };
 
-// Sums of the slice's chunks, relative to 2^ref, of the entries that `in` names; f sees every entry and its mass.
-template <typename T, typename I, typename F>
-__device__ __forceinline__ void sum_chunks(RowShared& sh, const Slice<T>& sl, const Scale& sc, int ref, I in, F f) {
-    constexpr int E = Slice<T>::E;
+// Sums of the slice's chunks, relative to 2^ref: of all entries, or (LIST) of those from `above` on, while the entries from `end` to `above`
+// and from `end_k` to `above_k` are listed; returns the thread's share of the mass of the others from `above_k` on, and counts the ones above.
+template <typename T, bool LIST>
+__device__ __noinline__ double sum_chunks(RowShared& sh, Entries en, Scale sc, int ref, float above, float end, float above_k, float end_k, int* n_above) {
+    constexpr int E = Row<T>::kE;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int w0 = min(sl.nv, warp * sl.seg), w1 = min(sl.nv, w0 + sl.seg);
-    for (int c = 0; c < sl.iters; ++c) {
+    const int w0 = min(en.nv, warp * en.seg), w1 = min(en.nv, w0 + en.seg);
+    double mid = 0.0;
+    int over = 0;
+    for (int c = 0; c < en.iters; ++c) {
         double s = 0.0, t = 0.0;
 #pragma unroll 1
         for (int u = 0; u < kU; ++u) {
             const int i = w0 + (c * kU + u) * 32 + lane;
             if (i - lane >= w1) break;
             float x[E];
-            double m[E];
-            Row<T>::unpack(i < w1 ? sl.data[i] : Row<T>::nothing(), x);
-            sc.masses(x, ref, m);
+            Row<T>::unpack(i < w1 ? en.data[i] : Row<T>::nothing(), x);
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                f(x[e], sl.first + i * E + e, m[e]);
-                (e & 1 ? t : s) += in(x[e], m[e]) ? m[e] : 0.0;
+            for (int h = 0; h < E; h += 4) {
+                const float y[4] = {x[h], x[h + 1], x[h + 2], x[h + 3]};
+                double m[4];
+                sc.masses(y, ref, m);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if constexpr (LIST) {
+                        const bool up = y[e] >= above, here = !up && y[e] > -INFINITY && (y[e] >= end || (y[e] >= end_k && y[e] < above_k));
+                        over += up;
+                        (e & 1 ? t : s) += up ? m[e] : 0.0;
+                        mid += !up && !here && y[e] >= above_k ? m[e] : 0.0;
+                        if (here) {
+                            const uint32_t at = atomicAdd(&sh.cta_n, 1u);
+                            if (at < (uint32_t)kListMax) sh.list[at] = order_key(y[e], en.first + i * E + h + e);
+                        }
+                    } else {
+                        (e & 1 ? t : s) += m[e];
+                    }
+                }
             }
         }
         s = warp_add(s + t);
-        if (lane == 0) sh.chunk[warp * sl.iters + c] = s;
+        if (lane == 0) sh.chunk[warp * en.iters + c] = s;
     }
+    if constexpr (LIST) *n_above = over;
+    return mid;
+}
+// The same of the entries up to the key `last` with a mass of at least `least`, counted in n_above
+template <typename T>
+__device__ __noinline__ void sum_kept(RowShared& sh, Entries en, Scale sc, int ref, uint64_t last, double least, int* kept) {
+    constexpr int E = Row<T>::kE;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int w0 = min(en.nv, warp * en.seg), w1 = min(en.nv, w0 + en.seg);
+    int cnt = 0;
+    for (int c = 0; c < en.iters; ++c) {
+        double s = 0.0;
+#pragma unroll 1
+        for (int u = 0; u < kU; ++u) {
+            const int i = w0 + (c * kU + u) * 32 + lane;
+            if (i - lane >= w1) break;
+            float x[E];
+            Row<T>::unpack(i < w1 ? en.data[i] : Row<T>::nothing(), x);
+#pragma unroll
+            for (int h = 0; h < E; h += 4) {
+                const float y[4] = {x[h], x[h + 1], x[h + 2], x[h + 3]};
+                double m[4];
+                sc.masses(y, ref, m);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const bool in = y[e] > -INFINITY && order_key(y[e], en.first + i * E + h + e) <= last && m[e] >= least;
+                    s += in ? m[e] : 0.0;
+                    cnt += in;
+                }
+            }
+        }
+        s = warp_add(s);
+        if (lane == 0) sh.chunk[warp * en.iters + c] = s;
+    }
+    *kept = cnt;
 }
 
 // The entry of a chunk at which the mass in vocabulary order exceeds `over`; kept(x, index, mass): whether an entry counts.  A warp
@@ -854,10 +924,10 @@ sample_kernel(SampleCall a) {
             narrow = listed(sh, parts) <= (uint32_t)kListMax;
         }
         if (!narrow && (by_k || by_p)) {
-            LinearBins lin(top, sc);
+            LinearBins lin(top, sc, by_k ? 16.f : 32.f);
             fill_bins(sh, sl, by_k, by_p, lin, 0, 0.0);
             const uint32_t n_all = sh.all_count[kBins - 1];
-            const double m_all = sh.all[kBins - 1];
+            const double m_all = sh.all[kBins - 1], m_far = (double)(n_all - sh.all_count[kBins - 2]) * exp2(-(double)lin.octaves * (kBins - 1));
             const bool cut_k = by_k && (uint32_t)k < n_all;
             uint32_t count0 = 0;                                                   // what stands in front of the bins
             double mass0 = 0.0;
@@ -867,8 +937,8 @@ sample_kernel(SampleCall a) {
             const auto count_to = [&](int b) { return b >= 0 ? sh.all_count[b] : count0; };
             const auto mass_to = [&](int b) { return b >= 0 ? sh.all[b] : mass0; };
             const auto find = [&]() {
-                // bin of the k-th entry; bins between which the border of top_p must lie: masses are known to 2e-5, and M, the mass
-                // of the k first entries, to that of the k-th's bin
+                // bin of the k-th entry; bins between which the border of top_p must lie: masses are known to 2e-5 (2^-17 from the units,
+                // 3e-6 from a distance in 32 bits) and to what the last bin may hold, and M, the mass of the k first entries, to that of the k-th's bin
                 bk = kBins - 1;
                 if (cut_k) {
                     find_bin(sh.all_count, (uint32_t)k, &sh.found[0]);
@@ -877,9 +947,9 @@ sample_kernel(SampleCall a) {
                 }
                 b_lo = b_hi = bk;
                 if (by_p) {
-                    const double lo = cut_k ? fmax(mass_to(bk - 1), 1.0) : m_all, hi = cut_k ? mass_to(bk) : m_all;
-                    find_bin(sh.all, (double)p * lo * (1.0 - 1e-4), &sh.found[1]);
-                    find_bin(sh.all, (double)p * hi * (1.0 + 1e-4), &sh.found[2]);
+                    const double lo = cut_k ? fmax(mass_to(bk - 1), 1.0) : m_all, hi = (cut_k ? mass_to(bk) : m_all) + m_far;
+                    find_bin(sh.all, (double)p * lo * (1.0 - 4e-5), &sh.found[1]);
+                    find_bin(sh.all, (double)p * hi * (1.0 + 4e-5), &sh.found[2]);
                     __syncthreads();
                     b_lo = min(sh.found[1], bk);
                     b_hi = min(sh.found[2], bk);
@@ -915,7 +985,7 @@ sample_kernel(SampleCall a) {
                 __syncthreads();
                 list_entries(sh, sl, [&](float x, int) { return lin.of(x) <= down; });
                 if (!cut_k) {                                                      // top_p of the whole row: its mass
-                    sum_chunks(sh, sl, sc, ref, [](float, double) { return true; }, [](float, int, double) {});
+                    sum_chunks<T, false>(sh, Entries(sl), sc, ref, 0.f, 0.f, 0.f, 0.f, nullptr);
                     summed = true;
                 }
                 sync_parts(parts);
@@ -928,20 +998,16 @@ sample_kernel(SampleCall a) {
                     if (n_list <= (uint32_t)kListMax) {
                         if (tid == 0) sh.cta_n = 0;
                         __syncthreads();
-                        double mid = 0.0;
                         int n_over = 0;
-                        // the bins' borders as logits: above the listed ones, down to their end, and the k-th's bin
-                        const float above_them = lin.edge(m_lo - 1), end_them = lin.edge(to);
-                        const float above_k_bin = cut_k ? lin.edge(bk - 1) : -INFINITY, end_k_bin = cut_k ? lin.edge(bk) : -INFINITY;
-                        sum_chunks(sh, sl, sc, ref, [&](float x, double) { return x >= above_them; },
-                                   [&](float x, int index, double m) {
-                                       if (x >= above_them) { ++n_over; return; }
-                                       if (!(x > -INFINITY)) return;
-                                       if (x >= end_them || (x >= end_k_bin && x < above_k_bin)) {
-                                           const uint32_t at = atomicAdd(&sh.cta_n, 1u);
-                                           if (at < (uint32_t)kListMax) sh.list[at] = order_key(x, index);
-                                       } else if (x >= above_k_bin) mid += m;
-                                   });
+                        // the bins' borders as logits: above the listed ones, down to their end, and the k-th's bin (a warp each)
+                        if (warp < 4) {
+                            const float e = warp < 2 || cut_k ? lin.edge(warp == 0 ? m_lo - 1 : warp == 1 ? to : warp == 2 ? bk - 1 : bk) : -INFINITY;
+                            if (lane == 0) sh.edges[warp] = e;
+                        }
+                        __syncthreads();
+                        const float above_them = sh.edges[0], end_them = sh.edges[1], above_k_bin = sh.edges[2], end_k_bin = sh.edges[3];
+                        // (without top-k, above_k_bin is minus infinity and nothing lies below it)
+                        double mid = sum_chunks<T, true>(sh, Entries(sl), sc, ref, above_them, end_them, above_k_bin, end_k_bin, &n_over);
                         n_over = __reduce_add_sync(0xffffffffu, n_over);
                         if (lane == 0) sh.wcnt[warp] = n_over;
                         mid = warp_add(mid);
@@ -1073,26 +1139,9 @@ sample_kernel(SampleCall a) {
             int cnt = 0;
             const uint64_t last = border;
             if (last == ~0ull && !by_mp && !a.kept) {
-                sum_chunks(sh, sl, sc, ref, [](float, double) { return true; }, [](float, int, double) {});
+                sum_chunks<T, false>(sh, Entries(sl), sc, ref, 0.f, 0.f, 0.f, 0.f, nullptr);
             } else {
-                constexpr int E = Slice<T>::E;
-                const int w0 = min(sl.nv, warp * sl.seg), w1 = min(sl.nv, w0 + sl.seg);
-                for (int c = 0; c < sl.iters; ++c) {
-                    double s = 0.0;
-                    for (int u = 0; u < kU; ++u) {
-                        const int i = w0 + (c * kU + u) * 32 + lane;
-                        if (i >= w1) break;
-                        float x[E];
-                        Row<T>::unpack(sl.data[i], x);
-#pragma unroll
-                        for (int e = 0; e < E; ++e) {
-                            const double m = sc.mass(x[e], ref);
-                            if (x[e] > -INFINITY && order_key(x[e], sl.first + i * E + e) <= last && m >= least) { s += m; ++cnt; }
-                        }
-                    }
-                    s = warp_add(s);
-                    if (lane == 0) sh.chunk[warp * sl.iters + c] = s;
-                }
+                sum_kept<T>(sh, Entries(sl), sc, ref, last, least, &cnt);
                 cnt = warp_add(cnt);
                 if (lane == 0) sh.wcnt[warp] = cnt;
                 __syncthreads();
