@@ -100,6 +100,19 @@ struct Row {
 #pragma unroll
         for (int e = 0; e < kE / 2; ++e) x[e] = Pair{f[2 * e], f[2 * e + 1]};
     }
+    static __device__ __forceinline__ uint4 without_nan(const uint4& r) {           // minus infinity instead
+        if constexpr (sizeof(T) == 4) {
+            const auto f = [](uint32_t w) { return __float_as_uint(fmaxf(__uint_as_float(w), -INFINITY)); };
+            return make_uint4(f(r.x), f(r.y), f(r.z), f(r.w));
+        } else {
+            const auto f = [](uint32_t w) {
+                const uint32_t none = 0xff80ff80u;
+                const __nv_bfloat162 m = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&w), *reinterpret_cast<const __nv_bfloat162*>(&none));
+                return *reinterpret_cast<const uint32_t*>(&m);
+            };
+            return make_uint4(f(r.x), f(r.y), f(r.z), f(r.w));
+        }
+    }
     // largest entry of a vector and `m` (NaN left out)
     static __device__ __forceinline__ float largest(const uint4& r, float m) {
         if constexpr (sizeof(T) == 4) {

@@ -484,8 +484,8 @@ __device__ void fill_bins(RowShared& sh, const Slice<T>& sl, bool counts, bool m
 // For rows whose border bin holds more than a list does (equal or nearly equal logits): whole-number counts or masses (2^-43 of 2^ref
 // as the unit) in bins over ranges of keys, until a list holds what is left.  Slow (a pass and two barriers of the cluster per round of
 // ten bits), and right for everything.
-template <typename T, typename F>
-__device__ void key_bins(RowShared& sh, const Slice<T>& sl, bool by_mass, const Scale& sc, int ref, F bin_of) {
+template <typename S, typename F>
+__device__ void key_bins(RowShared& sh, const S& sl, bool by_mass, const Scale& sc, int ref, F bin_of) {
     const int tid = threadIdx.x;
     sync_parts(sl.parts);
     for (int i = tid; i < kBins; i += kThreads) sh.other[i] = 0;
@@ -504,8 +504,8 @@ __device__ void key_bins(RowShared& sh, const Slice<T>& sl, bool by_mass, const 
 }
 // The key of the last entry, in order, of the shortest prefix whose count (or mass) is at least `target`, and the count or mass with it.
 // share: take target as that share of the sum over the keys up to `upto` instead.
-template <typename T>
-__device__ void search_border(RowShared& sh, const Slice<T>& sl, bool by_mass, uint64_t target, double share, uint64_t upto, const Scale& sc, int ref,
+template <typename S>
+__device__ __noinline__ void search_border(RowShared& sh, const S& sl, bool by_mass, uint64_t target, double share, uint64_t upto, const Scale& sc, int ref,
                               uint64_t* border) {
     uint64_t lo = 0, hi = upto, before = 0;
     bool first = true;
@@ -622,6 +622,204 @@ top_kernel(const void* logits, long long ld, int V, int parts, int K, float inv_
     if (!ok) { set_status(status, SD_ERR_TIMEOUT); sm100::unwind_pause(); }
     __syncwarp();
     if (parts > 1) sync_parts(parts);                                              // nobody leaves while the first CTA reads
+}
+
+// ---------------------------------------------------------------- top logits of many rows
+// Where there are enough rows to fill the GPU, a CTA takes one at a time, in pieces through a ring of slots that it refills as it goes:
+// first for the groups' largest logits and the sum, then, from L2 (300 rows are at most 180 MB, 152064 bf16 90 MB), for the entries that
+// reach the threshold.  The next row's pieces are under way while a row's list is sorted.  (Clusters that hold a row in shared
+// memory, 4096 rows of 152064 bf16: 740 us; most of a CTA's time went into what a row needs but once.)
+constexpr int kStreamVecs = 2 * kThreads;          // a piece: two vectors per thread
+constexpr int kStreamSlots = 5;
+
+// a whole row where it lies in memory, for the general search
+template <typename T>
+struct RowInMemory {
+    Row<T> row;
+    int parts = 1;
+    __device__ __forceinline__ explicit RowInMemory(const Row<T>& r) : row(r) {}
+    template <typename F>
+    __device__ __forceinline__ void each(F f) const {
+        constexpr int E = Row<T>::kE;
+        for (int i = (int)threadIdx.x; i < row.nvec; i += kThreads) {
+            float x[E];
+            Row<T>::unpack(row.load(i), x);
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (x[e] > -INFINITY) f(x[e], i * E + e - row.lead);
+        }
+    }
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads, 2)
+top_stream_kernel(const void* logits, long long ld, int V, int M, int pieces, int K, float inv_temp, float* values, int32_t* index, float* lse,
+                  int32_t* status, int withheld, long long wait_cycles) {
+    using namespace sm100;
+    constexpr int E = Row<T>::kE;
+    extern __shared__ __align__(16) uint4 ring[];
+    __shared__ RowShared sh;
+    __shared__ uint64_t full[kStreamSlots], free_[kStreamSlots];
+    const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+    if (tid == 0) {
+        sh.abort_flag = 0;
+        for (int q = 0; q < kStreamSlots; ++q) { mbar_init(&full[q], 1); mbar_init(&free_[q], kWarps); }
+        fence_barrier_init();
+    }
+    __syncthreads();
+    begin_dependent(logits, values, index, lse, status);
+    const float c = inv_temp * kLog2e;
+    // the next piece to be copied (thread 0's business)
+    int in_piece = 0, in_pass = 0;
+    long long in_row = blockIdx.x;
+    const uint64_t keep_pol = policy_evict_last(), drop_pol = policy_evict_first();
+    bool ok = true;
+    const auto issue = [&](int in_slot) {                                          // by thread 0; the slot is free
+        if (in_row >= M) return;
+        const Row<T> row(logits, ld, in_row, V);
+        uint4* dst = ring + in_slot * kStreamVecs;
+        const int a0 = min(row.nvec, in_piece * kStreamVecs), a1 = min(row.nvec, a0 + kStreamVecs);
+        const int i0 = max(row.full0, a0), i1 = min(row.full1, a1);
+        const uint32_t bytes = i1 > i0 ? (uint32_t)(i1 - i0) * 16 : 0;
+        fence_proxy_async_smem();                                                  // (edges that were stored into the slot stand behind the copy)
+        if (a0 == 0 && row.full0 > 0) dst[0] = row.edge(0);
+        const int e = row.nvec - 1;
+        if (e >= max(row.full0, row.full1) && e >= a0 && e < a1) dst[e - a0] = row.edge(e);
+        mbar_arrive_expect_tx(&full[in_slot], bytes + withheld);
+        if (bytes)
+            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;"
+                         ::"r"(smem_u32(dst + (i0 - a0))), "l"(row.vec + i0), "r"(bytes), "r"(smem_u32(&full[in_slot])), "l"(in_pass ? drop_pol : keep_pol) : "memory");
+        if (++in_piece == pieces) {
+            in_piece = 0;
+            if (++in_pass == 2) { in_pass = 0; in_row += gridDim.x; }
+        }
+    };
+    if (tid == 0) for (int q = 0; q < kStreamSlots; ++q) issue(q);
+    int slot = 0, left = 0;                                                        // left: the slot of the piece before
+    uint32_t phase = 0, left_phase = 0;
+    bool first = true;
+    // In front of a piece, the slot of the one before it is filled again: by now all warps have mostly left it.
+    const auto refill = [&]() {
+        if (!first) {
+            if (warp == 0) {
+                ok = mbar_wait_warp(&free_[left], left_phase, &sh.abort_flag, wait_cycles) && ok;
+                if (lane == 0 && ok) issue(left);
+                __syncwarp();
+            }
+            if (++left == kStreamSlots) { left = 0; left_phase ^= 1u; }
+        }
+        first = false;
+    };
+    for (long long r = blockIdx.x; r < M; r += gridDim.x) {
+        const Row<T> row(logits, ld, r, V);
+        // ---- the groups' largest logits, and the sum of 2^((x - from) c)
+        float top = -INFINITY, from = 0.f;
+        Pair a{0.f, 0.f}, b{0.f, 0.f};
+        bool begun = false;
+        for (int q = 0; q < pieces; ++q) {
+            refill();
+            ok = mbar_wait(&full[slot], phase, &sh.abort_flag, wait_cycles) && ok;
+            const uint4* src = ring + slot * kStreamVecs;
+            const int len = min(kStreamVecs, row.nvec - q * kStreamVecs);
+            uint4 raw[2];
+            float m = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int i = tid + j * kThreads;
+                raw[j] = i < len ? src[i] : Row<T>::nothing();
+                m = Row<T>::largest(raw[j], m);
+            }
+            if (__any_sync(0xffffffffu, m > -INFINITY && (!begun || (m - from) * c > 32.f))) {
+                const float now = warp_largest(fmaxf(top, m));
+                if (begun) {
+                    const float f = ex2((from - now) * c);
+                    a = Pair{a.x * f, a.y * f};
+                    b = Pair{b.x * f, b.y * f};
+                }
+                from = now;
+                begun = true;
+            }
+            top = fmaxf(top, m);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                if (warp * 32 + j * kThreads >= len) break;
+                Pair x[E / 2];
+                Row<T>::pairs(Row<T>::without_nan(raw[j]), x);
+#pragma unroll
+                for (int e = 0; e < E / 2; e += 2) {
+                    a = add2(a, ex2(mul2(add2(x[e], Pair{-from, -from}), Pair{c, c})));
+                    b = add2(b, ex2(mul2(add2(x[e + 1], Pair{-from, -from}), Pair{c, c})));
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&free_[slot]);
+            if (++slot == kStreamSlots) { slot = 0; phase ^= 1u; }
+        }
+        float g = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 2));
+        if ((lane & 3) == 0) sh.group_top[tid >> 2] = g;
+        const float sum = warp_add((a.x + a.y) + (b.x + b.y));
+        top = warp_largest(top);
+        if (lane == 0) { sh.wtop[warp] = top; sh.wsum[warp] = sum; sh.groups[warp] = from; }
+        if (tid == 0) sh.cta_n = 0;
+        __syncthreads();
+        const float wtop = lane < kWarps ? sh.wtop[lane] : -INFINITY, most = warp_largest(wtop);
+        if (lse && warp == kWarps - 1) {
+            float s = lane < kWarps && wtop > -INFINITY ? sh.wsum[lane] * ex2((sh.groups[lane] - most) * c) : 0.f;
+            s = warp_add(s);
+            if (lane == 0) lse[r] = most > -INFINITY && most < INFINITY ? (float)((double)most * (double)inv_temp + log((double)s)) : most;
+        }
+        __syncthreads();                                                           // (groups is written again)
+        const float thr = kth_group(sh, 1, K);
+        // ---- the entries that reach the threshold
+        for (int q = 0; q < pieces; ++q) {
+            refill();
+            ok = mbar_wait(&full[slot], phase, &sh.abort_flag, wait_cycles) && ok;
+            const uint4* src = ring + slot * kStreamVecs;
+            const int len = min(kStreamVecs, row.nvec - q * kStreamVecs);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int i = tid + j * kThreads;
+                if (i >= len) break;
+                const uint4 raw = src[i];
+                if (!(Row<T>::largest(raw, -INFINITY) >= thr)) continue;
+                float x[E];
+                Row<T>::unpack(raw, x);
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (x[e] >= thr && x[e] > -INFINITY) {
+                        const uint32_t at = atomicAdd(&sh.cta_n, 1u);
+                        if (at < (uint32_t)kListMax) sh.list[at] = order_key(x[e], (q * kStreamVecs + i) * E + e - row.lead);
+                    }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&free_[slot]);
+            if (++slot == kStreamSlots) { slot = 0; phase ^= 1u; }
+        }
+        if (__syncthreads_or(!ok)) { ok = false; break; }
+        int n = sh.cta_n;
+        if (n > kListMax) {                                                        // (thousands of equal logits: the K-th's key is searched for)
+            const RowInMemory<T> all(row);
+            uint64_t border = ~0ull;
+            search_border(sh, all, false, (uint64_t)K, -1.0, ~0ull, Scale(1.f), 0, &border);
+            if (tid == 0) sh.cta_n = 0;
+            __syncthreads();
+            all.each([&](float x, int i) {
+                if (order_key(x, i) > border) return;
+                const uint32_t at = atomicAdd(&sh.cta_n, 1u);
+                if (at < (uint32_t)kListMax) sh.list[at] = order_key(x, i);
+            });
+            __syncthreads();
+            n = min(sh.cta_n, (uint32_t)kListMax);
+        }
+        n = sort_list(sh, sh.list, n, K);
+        for (int i = tid; i < K; i += kThreads) {
+            values[r * K + i] = i < n ? key_logit(sh.list[i]) : -INFINITY;
+            index[r * K + i] = i < n ? key_index(sh.list[i]) : -1;
+        }
+        __syncthreads();
+    }
+    if (!ok) { set_status(status, SD_ERR_TIMEOUT); unwind_pause(); }
 }
 
 // ---------------------------------------------------------------- sampling and filtering
@@ -1240,6 +1438,8 @@ static int parts_for(int M, int nvec, int sms) {
     return parts;
 }
 
+static int stream_rows(int sms) { return sms / 2; }
+
 }  // namespace rows
 
 using namespace rows;
@@ -1249,10 +1449,18 @@ sd_status launch_top_logits(const void* logits, int dtype, long long ld, int M, 
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return SD_ERR_CUDA;
     const int nvec = (int)(((long long)V * (dtype == SD_F32 ? 4 : 2) + 15) / 16) + 1;
+    const TestKnobs knobs = test_knobs();
+    if (K <= kFewK && M >= stream_rows(sm_count(dev))) {
+        auto kern = dtype == SD_F32 ? top_stream_kernel<float> : top_stream_kernel<uint16_t>;
+        constexpr int smem = kStreamSlots * kStreamVecs * 16;
+        if (!allow_dynamic_smem(kern, smem)) return SD_ERR_CUDA;
+        const int ctas = 2 * sm_count(dev), pieces = (nvec + kStreamVecs - 1) / kStreamVecs;
+        return launch_dependent(kern, dim3((unsigned)(M < ctas ? M : ctas)), kThreads, smem, 1, st, logits, ld, V, M, pieces, K, inv_temp, values, index, lse,
+                                dev_status, knobs.withhold ? 16 : 0, knobs.wait_cycles);
+    }
     const int parts = parts_for(M, nvec, sm_count(dev)), smem = (nvec + parts - 1) / parts * 16;
     auto kern = dtype == SD_F32 ? top_kernel<float> : top_kernel<uint16_t>;
     if (!allow_dynamic_smem(kern, smem)) return SD_ERR_CUDA;
-    const TestKnobs knobs = test_knobs();
     return launch_dependent(kern, dim3((unsigned)M * parts), kThreads, smem, parts, st, logits, ld, V, parts, K, inv_temp, values, index, lse, dev_status,
                             knobs.withhold ? 16 : 0, knobs.wait_cycles);
 }
