@@ -625,12 +625,12 @@ top_kernel(const void* logits, long long ld, int V, int parts, int K, float inv_
 }
 
 // ---------------------------------------------------------------- top logits of many rows
-// Where there are enough rows to fill the GPU, a CTA takes one at a time, in pieces through a ring of slots that it refills as it goes:
-// first for the groups' largest logits and the sum, then, from L2 (300 rows are at most 180 MB, 152064 bf16 90 MB), for the entries that
-// reach the threshold.  The next row's pieces are under way while a row's list is sorted.  (Clusters that hold a row in shared
-// memory, 4096 rows of 152064 bf16: 740 us; most of a CTA's time went into what a row needs but once.)
-constexpr int kStreamVecs = 2 * kThreads;          // a piece: two vectors per thread
-constexpr int kStreamSlots = 5;
+// Where there are enough rows to fill the GPU, a CTA takes one at a time, twice over: first for the groups' largest logits and the
+// sum, then, mostly from L2, for the entries that reach the threshold.  Every warp has a sixteenth of the row and loads four vectors per
+// lane ahead of those that it works on, the next pass's and row's first ones too: no warp waits for another within a pass.  (Clusters
+// that hold a row in shared memory, 4096 rows of 152064 bf16: 740 us; a ring of copies for all warps of a CTA 580; one for every warp 850.)
+constexpr int kStreamLane = 4;                     // vectors per lane and step
+constexpr int kStreamVecs = kStreamLane * 32;
 
 // a whole row where it lies in memory, for the general search
 template <typename T>
@@ -653,82 +653,39 @@ struct RowInMemory {
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 2)
-top_stream_kernel(const void* logits, long long ld, int V, int M, int pieces, int K, float inv_temp, float* values, int32_t* index, float* lse,
-                  int32_t* status, int withheld, long long wait_cycles) {
-    using namespace sm100;
+top_stream_kernel(const void* logits, long long ld, int V, int M, int steps, int K, float inv_temp, float* values, int32_t* index, float* lse) {
     constexpr int E = Row<T>::kE;
-    extern __shared__ __align__(16) uint4 ring[];
     __shared__ RowShared sh;
-    __shared__ uint64_t full[kStreamSlots], free_[kStreamSlots];
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
-    if (tid == 0) {
-        sh.abort_flag = 0;
-        for (int q = 0; q < kStreamSlots; ++q) { mbar_init(&full[q], 1); mbar_init(&free_[q], kWarps); }
-        fence_barrier_init();
-    }
-    __syncthreads();
-    begin_dependent(logits, values, index, lse, status);
+    begin_dependent(logits, values, index, lse);
     const float c = inv_temp * kLog2e;
-    // the next piece to be copied (thread 0's business)
-    int in_piece = 0, in_pass = 0;
-    long long in_row = blockIdx.x;
-    const uint64_t keep_pol = policy_evict_last(), drop_pol = policy_evict_first();
-    bool ok = true;
-    const auto issue = [&](int in_slot) {                                          // by thread 0; the slot is free
-        if (in_row >= M) return;
-        const Row<T> row(logits, ld, in_row, V);
-        uint4* dst = ring + in_slot * kStreamVecs;
-        const int a0 = min(row.nvec, in_piece * kStreamVecs), a1 = min(row.nvec, a0 + kStreamVecs);
-        const int i0 = max(row.full0, a0), i1 = min(row.full1, a1);
-        const uint32_t bytes = i1 > i0 ? (uint32_t)(i1 - i0) * 16 : 0;
-        fence_proxy_async_smem();                                                  // (edges that were stored into the slot stand behind the copy)
-        if (a0 == 0 && row.full0 > 0) dst[0] = row.edge(0);
-        const int e = row.nvec - 1;
-        if (e >= max(row.full0, row.full1) && e >= a0 && e < a1) dst[e - a0] = row.edge(e);
-        mbar_arrive_expect_tx(&full[in_slot], bytes + withheld);
-        if (bytes)
-            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;"
-                         ::"r"(smem_u32(dst + (i0 - a0))), "l"(row.vec + i0), "r"(bytes), "r"(smem_u32(&full[in_slot])), "l"(in_pass ? drop_pol : keep_pol) : "memory");
-        if (++in_piece == pieces) {
-            in_piece = 0;
-            if (++in_pass == 2) { in_pass = 0; in_row += gridDim.x; }
+    const int w0 = warp * steps * kStreamVecs;                                     // the warp's first vector
+    uint4 ahead[kStreamLane];
+    const auto fetch = [&](const Row<T>& row, int q) {                             // step q of the warp's part
+        const int i0 = w0 + q * kStreamVecs;
+        if (i0 >= row.full0 && i0 + kStreamVecs <= row.full1) {
+#pragma unroll
+            for (int j = 0; j < kStreamLane; ++j) ahead[j] = __ldcg(row.vec + i0 + j * 32 + lane);
+        } else {
+#pragma unroll
+            for (int j = 0; j < kStreamLane; ++j) ahead[j] = i0 + j * 32 + lane < row.nvec ? row.load(i0 + j * 32 + lane) : Row<T>::nothing();
         }
     };
-    if (tid == 0) for (int q = 0; q < kStreamSlots; ++q) issue(q);
-    int slot = 0, left = 0;                                                        // left: the slot of the piece before
-    uint32_t phase = 0, left_phase = 0;
-    bool first = true;
-    // In front of a piece, the slot of the one before it is filled again: by now all warps have mostly left it.
-    const auto refill = [&]() {
-        if (!first) {
-            if (warp == 0) {
-                ok = mbar_wait_warp(&free_[left], left_phase, &sh.abort_flag, wait_cycles) && ok;
-                if (lane == 0 && ok) issue(left);
-                __syncwarp();
-            }
-            if (++left == kStreamSlots) { left = 0; left_phase ^= 1u; }
-        }
-        first = false;
-    };
+    if (blockIdx.x < M) fetch(Row<T>(logits, ld, blockIdx.x, V), 0);
     for (long long r = blockIdx.x; r < M; r += gridDim.x) {
         const Row<T> row(logits, ld, r, V);
         // ---- the groups' largest logits, and the sum of 2^((x - from) c)
         float top = -INFINITY, from = 0.f;
         Pair a{0.f, 0.f}, b{0.f, 0.f};
         bool begun = false;
-        for (int q = 0; q < pieces; ++q) {
-            refill();
-            ok = mbar_wait(&full[slot], phase, &sh.abort_flag, wait_cycles) && ok;
-            const uint4* src = ring + slot * kStreamVecs;
-            const int len = min(kStreamVecs, row.nvec - q * kStreamVecs);
-            uint4 raw[2];
+        for (int q = 0; q < steps; ++q) {
+            uint4 raw[kStreamLane];
             float m = -INFINITY;
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int i = tid + j * kThreads;
-                raw[j] = i < len ? src[i] : Row<T>::nothing();
-                m = Row<T>::largest(raw[j], m);
-            }
+            for (int j = 0; j < kStreamLane; ++j) raw[j] = ahead[j];
+            fetch(row, q + 1 < steps ? q + 1 : 0);                                 // (behind the last one, the second pass's first)
+#pragma unroll
+            for (int j = 0; j < kStreamLane; ++j) m = Row<T>::largest(raw[j], m);
             if (__any_sync(0xffffffffu, m > -INFINITY && (!begun || (m - from) * c > 32.f))) {
                 const float now = warp_largest(fmaxf(top, m));
                 if (begun) {
@@ -741,8 +698,8 @@ top_stream_kernel(const void* logits, long long ld, int V, int M, int pieces, in
             }
             top = fmaxf(top, m);
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                if (warp * 32 + j * kThreads >= len) break;
+            for (int j = 0; j < kStreamLane; ++j) {
+                if (w0 + q * kStreamVecs + j * 32 >= row.nvec) break;
                 Pair x[E / 2];
                 Row<T>::pairs(Row<T>::without_nan(raw[j]), x);
 #pragma unroll
@@ -751,9 +708,6 @@ top_stream_kernel(const void* logits, long long ld, int V, int M, int pieces, in
                     b = add2(b, ex2(mul2(add2(x[e + 1], Pair{-from, -from}), Pair{c, c})));
                 }
             }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&free_[slot]);
-            if (++slot == kStreamSlots) { slot = 0; phase ^= 1u; }
         }
         float g = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 2));
@@ -772,31 +726,26 @@ top_stream_kernel(const void* logits, long long ld, int V, int M, int pieces, in
         __syncthreads();                                                           // (groups is written again)
         const float thr = kth_group(sh, 1, K);
         // ---- the entries that reach the threshold
-        for (int q = 0; q < pieces; ++q) {
-            refill();
-            ok = mbar_wait(&full[slot], phase, &sh.abort_flag, wait_cycles) && ok;
-            const uint4* src = ring + slot * kStreamVecs;
-            const int len = min(kStreamVecs, row.nvec - q * kStreamVecs);
+        for (int q = 0; q < steps; ++q) {
+            uint4 raw[kStreamLane];
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int i = tid + j * kThreads;
-                if (i >= len) break;
-                const uint4 raw = src[i];
-                if (!(Row<T>::largest(raw, -INFINITY) >= thr)) continue;
+            for (int j = 0; j < kStreamLane; ++j) raw[j] = ahead[j];
+            if (q + 1 < steps) fetch(row, q + 1);
+            else if (r + gridDim.x < M) fetch(Row<T>(logits, ld, r + gridDim.x, V), 0);
+#pragma unroll
+            for (int j = 0; j < kStreamLane; ++j) {
+                if (!(Row<T>::largest(raw[j], -INFINITY) >= thr)) continue;
                 float x[E];
-                Row<T>::unpack(raw, x);
+                Row<T>::unpack(raw[j], x);
 #pragma unroll
                 for (int e = 0; e < E; ++e)
                     if (x[e] >= thr && x[e] > -INFINITY) {
                         const uint32_t at = atomicAdd(&sh.cta_n, 1u);
-                        if (at < (uint32_t)kListMax) sh.list[at] = order_key(x[e], (q * kStreamVecs + i) * E + e - row.lead);
+                        if (at < (uint32_t)kListMax) sh.list[at] = order_key(x[e], (w0 + q * kStreamVecs + j * 32 + lane) * E + e - row.lead);
                     }
             }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&free_[slot]);
-            if (++slot == kStreamSlots) { slot = 0; phase ^= 1u; }
         }
-        if (__syncthreads_or(!ok)) { ok = false; break; }
+        __syncthreads();
         int n = sh.cta_n;
         if (n > kListMax) {                                                        // (thousands of equal logits: the K-th's key is searched for)
             const RowInMemory<T> all(row);
@@ -819,7 +768,6 @@ top_stream_kernel(const void* logits, long long ld, int V, int M, int pieces, in
         }
         __syncthreads();
     }
-    if (!ok) { set_status(status, SD_ERR_TIMEOUT); unwind_pause(); }
 }
 
 // ---------------------------------------------------------------- sampling and filtering
@@ -1452,11 +1400,8 @@ sd_status launch_top_logits(const void* logits, int dtype, long long ld, int M, 
     const TestKnobs knobs = test_knobs();
     if (K <= kFewK && M >= stream_rows(sm_count(dev))) {
         auto kern = dtype == SD_F32 ? top_stream_kernel<float> : top_stream_kernel<uint16_t>;
-        constexpr int smem = kStreamSlots * kStreamVecs * 16;
-        if (!allow_dynamic_smem(kern, smem)) return SD_ERR_CUDA;
-        const int ctas = 2 * sm_count(dev), pieces = (nvec + kStreamVecs - 1) / kStreamVecs;
-        return launch_dependent(kern, dim3((unsigned)(M < ctas ? M : ctas)), kThreads, smem, 1, st, logits, ld, V, M, pieces, K, inv_temp, values, index, lse,
-                                dev_status, knobs.withhold ? 16 : 0, knobs.wait_cycles);
+        const int ctas = 2 * sm_count(dev), steps = (nvec + kWarps * kStreamVecs - 1) / (kWarps * kStreamVecs);
+        return launch_dependent(kern, dim3((unsigned)(M < ctas ? M : ctas)), kThreads, 0, 1, st, logits, ld, V, M, steps, K, inv_temp, values, index, lse);
     }
     const int parts = parts_for(M, nvec, sm_count(dev)), smem = (nvec + parts - 1) / parts * 16;
     auto kern = dtype == SD_F32 ? top_kernel<float> : top_kernel<uint16_t>;
