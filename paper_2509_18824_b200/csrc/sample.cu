@@ -13,6 +13,7 @@
 // (Lists kept in a single pass over global memory, with a threshold that rises, took three times as long: their cutting and their
 // barriers, 12 of 30 us for one row, and for flat rows four passes through L2.)
 #include <limits.h>
+#include <type_traits>
 #include "rows.cuh"
 
 namespace sdv {
@@ -20,9 +21,11 @@ namespace rows {
 
 constexpr int kFewK = 112;             // of 128 groups: with k near 128 the threshold would be the least of them, and the list long
 constexpr int kGroups = 128;
+constexpr int kSomeK = 384;            // of 512 threads: 710 entries expected
 constexpr int kU = 4;                  // vectors per lane and chunk
-constexpr int kMaxChunks = 128;        // of a CTA
+constexpr int kMaxChunks = 544;        // of a CTA (a whole row of 2^18 f32: 16 warps' 33)
 constexpr int kBins = 1024;
+constexpr int kCopies = 8;             // of a row's bins' masses
 constexpr int kPieces = 4;             // copies of a slice: four warps' vectors each
 constexpr int kComparePairs = 96;      // kept entries up to which the draw compares all pairs instead of sorting again
 constexpr double kUnit = 8796093022208.0;          // 2^43: masses as whole numbers
@@ -54,6 +57,7 @@ struct RowShared {
     double cta_mid;
     int cta_count;
     double chunk[kMaxChunks];          // sums of this CTA's chunks
+    int chunk_ref[kMaxChunks];         // and what they are relative to, where every chunk has a power of its own
     uint64_t list[kListMax];
     union {
         struct { uint32_t count[kBins], mass[kBins]; } bins;     // of this CTA
@@ -65,12 +69,17 @@ struct RowShared {
     double total;
     // the row's, in every CTA: bins, or in the first one chunks or the list's masses, as inclusive sums
     union { double all[kListMax]; uint64_t all_u[kListMax]; };
-    uint32_t all_count[kBins];
+    __align__(16) uint32_t all_count[kBins];
     uint32_t scan_count[kWarps];
 };
 
 // ---------------------------------------------------------------- a slice of a row
-template <typename T>
+// HELD: in the CTA's shared memory.  Otherwise a whole row where it lies (parts = 1): passes over it come from L2, and load four vectors
+// ahead of those that they work on.
+struct Never {
+    __device__ __forceinline__ bool operator()() const { return false; }
+};
+template <typename T, bool HELD>
 struct Slice {
     static constexpr int E = Row<T>::kE;
     Row<T> row;
@@ -84,6 +93,73 @@ struct Slice {
         first = v0 * E - row.lead;
         seg = (per + kWarps - 1) / kWarps;                                         // a warp's consecutive vectors (the same in all parts)
         iters = (seg + 32 * kU - 1) / (32 * kU);                                   // its chunks
+    }
+    __device__ __forceinline__ uint4 load(int i) const {                           // vector i, or nothing where that is behind the slice
+        if constexpr (HELD) return i < nv ? data[i] : Row<T>::nothing();
+        else return i < nv ? row.load(i) : Row<T>::nothing();
+    }
+    // vectors i0 + lane, + 32, ..
+    __device__ __forceinline__ void load_four(int i0, int end, uint4 (&raw)[kU]) const {
+        const int lane = threadIdx.x & 31;
+        if (!HELD && i0 >= row.full0 && i0 + 32 * kU <= min(row.full1, end)) {
+#pragma unroll
+            for (int u = 0; u < kU; ++u) raw[u] = __ldcg(row.vec + i0 + u * 32 + lane);
+        } else {
+#pragma unroll
+            for (int u = 0; u < kU; ++u) raw[u] = i0 + u * 32 + lane < end ? load(i0 + u * 32 + lane) : Row<T>::nothing();
+        }
+    }
+    // f(vectors, index of the first one) for all of the warp's part, four vectors per lane at a time
+    template <typename F, typename G = Never>
+    __device__ __forceinline__ void each_four(F f, G stop = G()) const {
+        const int warp = threadIdx.x >> 5, w0 = min(nv, warp * seg), w1 = min(nv, w0 + seg);
+        uint4 raw[kU];
+        if constexpr (HELD) {
+            for (int i0 = w0; i0 < w1 && !stop(); i0 += 32 * kU) { load_four(i0, w1, raw); f(raw, i0); }
+        } else {
+            uint4 ahead[kU];
+            load_four(w0, w1, ahead);
+            for (int i0 = w0; i0 < w1 && !stop(); i0 += 32 * kU) {
+#pragma unroll
+                for (int u = 0; u < kU; ++u) raw[u] = ahead[u];
+                if (i0 + 32 * kU < w1) load_four(i0 + 32 * kU, w1, ahead);
+                f(raw, i0);
+            }
+        }
+    }
+    // f(vector, its index), for all of the warp's part, or until stop()
+    template <typename F, typename G = Never>
+    __device__ __forceinline__ void each_vector(F f, G stop = G()) const {
+        const int lane = threadIdx.x & 31;
+        if constexpr (HELD) {
+            const int warp = threadIdx.x >> 5, w0 = min(nv, warp * seg), w1 = min(nv, w0 + seg);
+#pragma unroll 2
+            for (int i = w0 + lane; i < w1 && !stop(); i += 32) f(data[i], i);
+        } else {
+            each_four([&](const uint4 (&raw)[kU], int i0) {
+#pragma unroll
+                for (int u = 0; u < kU; ++u) f(raw[u], i0 + u * 32 + lane);
+            }, stop);
+        }
+    }
+    // f(vector, its index) for all lanes of a warp, and end(chunk) behind each of its chunks: for passes with enough to do per vector
+    template <typename F, typename G>
+    __device__ __forceinline__ void each_chunk(F f, G end) const {
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, w0 = min(nv, warp * seg), w1 = min(nv, w0 + seg);
+        uint4 ahead = Row<T>::nothing();
+        if (!HELD && w0 + lane < w1) ahead = load(w0 + lane);
+        for (int c = 0; c < iters; ++c) {
+#pragma unroll 1
+            for (int u = 0; u < kU; ++u) {
+                const int i = w0 + (c * kU + u) * 32 + lane;
+                if (i - lane >= w1) break;
+                uint4 raw = ahead;
+                if constexpr (HELD) raw = i < w1 ? data[i] : Row<T>::nothing();
+                else ahead = i + 32 < w1 ? load(i + 32) : Row<T>::nothing();
+                f(raw, i);
+            }
+            end(c);
+        }
     }
     __device__ __forceinline__ void copy(RowShared& sh, int withheld) const {      // by the whole CTA; the caller's barrier settles the edges
         const int tid = threadIdx.x;
@@ -106,42 +182,31 @@ struct Slice {
     // f(logit, index) for every entry that is not masked
     template <typename F>
     __device__ __forceinline__ void each(F f) const {
-#pragma unroll 2
-        for (int i = (int)threadIdx.x; i < nv; i += kThreads) {
+        each_vector([&](const uint4& raw, int i) {
             float x[E];
-            Row<T>::unpack(data[i], x);
+            Row<T>::unpack(raw, x);
 #pragma unroll
             for (int e = 0; e < E; ++e)
                 if (x[e] > -INFINITY) f(x[e], first + i * E + e);
-        }
+        });
     }
     // f(logit, index) for every entry from `thr` on
-    template <typename F>
-    __device__ __forceinline__ void each_from(float thr, F f) const {
-#pragma unroll 4
-        for (int i = (int)threadIdx.x; i < nv; i += kThreads) {
-            if (!(Row<T>::largest(data[i], -INFINITY) >= thr)) continue;
+    template <typename F, typename G>
+    __device__ __forceinline__ void each_from(float thr, F f, G stop) const {
+        each_vector([&](const uint4& raw, int i) {
+            if (!(Row<T>::largest(raw, -INFINITY) >= thr)) return;
             float x[E];
-            Row<T>::unpack(data[i], x);
+            Row<T>::unpack(raw, x);
 #pragma unroll
             for (int e = 0; e < E; ++e)
                 if (x[e] >= thr && x[e] > -INFINITY) f(x[e], first + i * E + e);
-        }
+        }, stop);
     }
     // the chunk that entry `index` of the row belongs to, counted over the parts
     __device__ __forceinline__ int chunk_of(int index) const {
         const int v = (index + row.lead) / E, q = v / per, i = v - q * per, w = i / seg;
         return (q * kWarps + w) * iters + (i - w * seg) / (32 * kU);
     }
-};
-
-// A slice as the passes over it take it.  They are calls of their own: inlined, the kernel's many values left their loops without
-// registers (the pass over 19008 entries that sums up and lists 17000 cycles).
-struct Entries {
-    const uint4* data;
-    int nv, first, seg, iters;
-    template <typename T>
-    __device__ __forceinline__ explicit Entries(const Slice<T>& sl) : data(sl.data), nv(sl.nv), first(sl.first), seg(sl.seg), iters(sl.iters) {}
 };
 
 // ---------------------------------------------------------------- cutting a list down
@@ -219,15 +284,17 @@ __device__ __noinline__ void cut_list(RowShared& sh, uint64_t* buf, int n, int k
 // ---------------------------------------------------------------- largest logits
 // Waits for the slice; the largest logit of every group (4 * parts lanes) and of the CTA, and with LSE the sum of
 // 2^((x - cta_top) c).  Returns whether the copies came.
-template <typename T, bool LSE>
-__device__ __forceinline__ bool first_pass(RowShared& sh, const Slice<T>& sl, float c, long long wait_cycles) {
-    constexpr int E = Slice<T>::E;
+template <bool LSE, typename T, bool HELD>
+__device__ __forceinline__ bool first_pass(RowShared& sh, const Slice<T, HELD>& sl, float c, long long wait_cycles) {
+    constexpr int E = Row<T>::kE;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const bool ok = sm100::mbar_wait_warp(&sh.bar[warp / (kWarps / kPieces)], 0, &sh.abort_flag, wait_cycles);
-    const int w0 = min(sl.nv, warp * sl.seg), w1 = min(sl.nv, w0 + sl.seg);
+    bool ok = true;
+    if constexpr (HELD) ok = sm100::mbar_wait_warp(&sh.bar[warp / (kWarps / kPieces)], 0, &sh.abort_flag, wait_cycles);
     float top = -INFINITY;
-#pragma unroll 4
-    for (int i = w0 + lane; i < w1; i += 32) top = Row<T>::largest(sl.data[i], top);
+    sl.each_four([&](const uint4 (&raw)[kU], int) {
+#pragma unroll
+        for (int u = 0; u < kU; ++u) top = Row<T>::largest(raw[u], top);
+    });
     float g = top;
     for (int d = 1; d < 4 * sl.parts; d <<= 1) g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, d));
     if (lane % (4 * sl.parts) == 0) sh.group_top[tid / (4 * sl.parts)] = g;
@@ -236,16 +303,18 @@ __device__ __forceinline__ bool first_pass(RowShared& sh, const Slice<T>& sl, fl
     if constexpr (LSE) {
         const float from = top > -INFINITY ? top : 0.f;
         Pair a{0.f, 0.f}, b{0.f, 0.f};
-#pragma unroll 2
-        for (int i = w0 + lane; i < w1; i += 32) {
-            Pair x[E / 2];
-            Row<T>::pairs(sl.data[i], x);
+        sl.each_four([&](const uint4 (&raw)[kU], int) {
 #pragma unroll
-            for (int e = 0; e < E / 2; e += 2) {
-                a = add2(a, ex2(mul2(add2(Pair{fmaxf(x[e].x, -INFINITY), fmaxf(x[e].y, -INFINITY)}, Pair{-from, -from}), Pair{c, c})));
-                b = add2(b, ex2(mul2(add2(Pair{fmaxf(x[e + 1].x, -INFINITY), fmaxf(x[e + 1].y, -INFINITY)}, Pair{-from, -from}), Pair{c, c})));
+            for (int u = 0; u < kU; ++u) {
+                Pair x[E / 2];
+                Row<T>::pairs(Row<T>::without_nan(raw[u]), x);
+#pragma unroll
+                for (int e = 0; e < E / 2; e += 2) {
+                    a = add2(a, ex2(mul2(add2(x[e], Pair{-from, -from}), Pair{c, c})));
+                    b = add2(b, ex2(mul2(add2(x[e + 1], Pair{-from, -from}), Pair{c, c})));
+                }
             }
-        }
+        });
         s = warp_add((a.x + a.y) + (b.x + b.y));
     }
     if (lane == 0) { sh.wtop[warp] = top; sh.wsum[warp] = s; }
@@ -287,26 +356,42 @@ __device__ __forceinline__ float kth_group(RowShared& sh, int parts, int k) {
     return sh.thr;
 }
 
-// ---------------------------------------------------------------- lists
-// Entries that `wanted` names into this CTA's list; cta_n counts them, also those that find no room.
-template <typename T, typename F>
-__device__ __forceinline__ void list_entries(RowShared& sh, const Slice<T>& sl, F wanted) {
-    if (threadIdx.x == 0) sh.cta_n = 0;
+// The same of a row's 512 threads' largest logits, in its only CTA, k <= kSomeK
+__device__ __noinline__ float kth_thread(RowShared& sh, float mine, int k) {
+    float4* tops = reinterpret_cast<float4*>(sh.all_count);
+    const int tid = threadIdx.x;
+    reinterpret_cast<float*>(tops)[tid] = mine;
     __syncthreads();
-    sl.each([&](float x, int index) {
-        if (!wanted(x, index)) return;
-        const uint32_t at = atomicAdd(&sh.cta_n, 1u);
-        if (at < (uint32_t)kListMax) sh.list[at] = order_key(x, index);
-    });
+    int before = 0;
+#pragma unroll 4
+    for (int j = 0; j < kThreads / 4; ++j) {
+        const float4 t = tops[j];
+        const int at = 4 * j;
+        before += t.x > mine || (t.x == mine && at < tid);
+        before += t.y > mine || (t.y == mine && at + 1 < tid);
+        before += t.z > mine || (t.z == mine && at + 2 < tid);
+        before += t.w > mine || (t.w == mine && at + 3 < tid);
+    }
+    if (before == k - 1) sh.thr = mine;
+    __syncthreads();
+    return sh.thr;
 }
-template <typename T>
-__device__ __forceinline__ void list_from(RowShared& sh, const Slice<T>& sl, float thr) {
+
+// ---------------------------------------------------------------- lists
+// Entries from `thr` on that `wanted` names into this CTA's list; cta_n counts them, until they find no room.
+template <typename S, typename F>
+__device__ __forceinline__ void list_entries(RowShared& sh, const S& sl, float thr, F wanted) {
     if (threadIdx.x == 0) sh.cta_n = 0;
     __syncthreads();
     sl.each_from(thr, [&](float x, int index) {
+        if (!wanted(x, index)) return;
         const uint32_t at = atomicAdd(&sh.cta_n, 1u);
         if (at < (uint32_t)kListMax) sh.list[at] = order_key(x, index);
-    });
+    }, [&]() { return *(volatile uint32_t*)&sh.cta_n > (uint32_t)kListMax; });
+}
+template <typename S>
+__device__ __noinline__ void list_from(RowShared& sh, const S sl, float thr) {
+    list_entries(sh, sl, thr, [](float, int) { return true; });
 }
 // how many entries all parts have listed (behind a sync_parts)
 __device__ __forceinline__ uint32_t listed(RowShared& sh, int parts) {
@@ -406,13 +491,13 @@ struct LinearBins {
     }
 };
 
-template <typename T>
-__device__ __noinline__ void bin_entries(RowShared& sh, Entries en, bool counts, bool masses, LinearBins lin) {
+template <typename T, bool HELD>
+__device__ __noinline__ void bin_entries(RowShared& sh, const Slice<T, HELD> sl, bool counts, bool masses, const LinearBins lin) {
     constexpr int E = Row<T>::kE;
-#pragma unroll 2
-    for (int i = (int)threadIdx.x; i < en.nv; i += kThreads) {
+    uint32_t* mass = HELD ? sh.bins.mass : reinterpret_cast<uint32_t*>(sl.data) + (threadIdx.x / 32 % kCopies) * kBins;
+    sl.each_vector([&](const uint4& raw, int) {
         float x[E];
-        Row<T>::unpack(en.data[i], x);
+        Row<T>::unpack(raw, x);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             const float d = lin.distance(x[e]), b = floorf(d);
@@ -420,31 +505,46 @@ __device__ __noinline__ void bin_entries(RowShared& sh, Entries en, bool counts,
             const bool in = x[e] > -INFINITY && bin >= 0 && bin < kBins;
             // (a far entry of the last coarse bin: one unit, for its count)
             const uint32_t m = (uint32_t)fmaf(ex2(lin.window || bin < kBins - 1 ? (b - d) * lin.octaves : 0.f), 65536.f, 0.5f);
-            if (in && masses) atomicAdd(&sh.bins.mass[bin], m);
+            if (in && masses) atomicAdd(&mass[bin], m);
             if (in && counts) atomicAdd(&sh.bins.count[bin], 1u);
         }
-    }
+    });
 }
 
 // Counts or masses (or both) of the row's bins, in every CTA: all_count and all, inclusive sums that begin with the given ones; masses
-// as multiples of the largest entry's.  Without counts, all_count is what the masses allow at most.  A bin's mass is summed up in units of 2^-16 of its upper end, in 32 bits (a slice has at
-// most 40960 entries): to 2e-5 of it.  (The last coarse bin has none.)  Every CTA adds up its share of the bins over the parts
+// as multiples of the largest entry's.  Without counts, all_count is what the masses allow at most.  A bin's mass is summed up in units of 2^-16 of its upper end, in 32 bits (a slice in
+// shared memory has at most 40960 entries; a row elsewhere has kCopies sums for each bin, and two warps' 32784 entries in each): to 2e-5 of it.  (The last coarse bin has none.)  Every CTA adds up its share of the bins over the parts
 // and hands it to all.
-template <typename T>
-__device__ void fill_bins(RowShared& sh, const Slice<T>& sl, bool counts, bool masses, const LinearBins& lin, uint32_t count0, double mass0) {
+template <typename T, bool HELD>
+__device__ void fill_bins(RowShared& sh, const Slice<T, HELD>& sl, bool counts, bool masses, const LinearBins& lin, uint32_t count0, double mass0) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     for (int i = tid; i < kBins; i += kThreads) { sh.bins.count[i] = 0; sh.bins.mass[i] = 0; }
+    uint32_t* copies = reinterpret_cast<uint32_t*>(sl.data);
+    double* folded = reinterpret_cast<double*>(copies + kCopies * kBins);
+    if (!HELD && masses)
+        for (int i = tid; i < kCopies * kBins; i += kThreads) copies[i] = 0;
     __syncthreads();
-    bin_entries<T>(sh, Entries(sl), counts, masses, lin);
+    bin_entries(sh, sl, counts, masses, lin);
+    if (!HELD && masses) {
+        __syncthreads();
+        for (int i = tid; i < kBins; i += kThreads) {
+            double m = 0.0;
+#pragma unroll
+            for (int r = 0; r < kCopies; ++r) m += (double)copies[r * kBins + i];
+            folded[i] = m;
+        }
+    }
     sync_parts(sl.parts);
     const int share = kBins / sl.parts;
     for (int j = tid; j < share; j += kThreads) {
         const int i = sl.rank * share + j;
-        uint32_t c[8], m[8];
+        uint32_t c[8];
+        typename std::conditional<HELD, uint32_t, double>::type m[8];
 #pragma unroll
         for (int r = 0; r < 8; ++r) {
             c[r] = counts && r < sl.parts ? *of_rank(&sh.bins.count[i], r) : 0;
-            m[r] = masses && r < sl.parts ? *of_rank(&sh.bins.mass[i], r) : 0;
+            if constexpr (HELD) m[r] = masses && r < sl.parts ? *of_rank(&sh.bins.mass[i], r) : 0;
+            else m[r] = masses && r < sl.parts ? *of_rank(&folded[i], r) : 0.0;
         }
         uint32_t count = 0;
         double mass = 0.0;
@@ -543,11 +643,11 @@ top_kernel(const void* logits, long long ld, int V, int parts, int K, float inv_
     begin_dependent(logits, values, index, lse, status);
     const long long r = blockIdx.x / parts;
     const int rank = parts == 1 ? 0 : (int)sm100::cluster_ctarank();
-    const Slice<T> sl(logits, ld, r, V, parts, rank, data);
+    const Slice<T, true> sl(logits, ld, r, V, parts, rank, data);
     sl.copy(sh, withheld);
     __syncthreads();
     const float c = inv_temp * kLog2e;
-    const bool ok = first_pass<T, true>(sh, sl, c, wait_cycles);
+    const bool ok = first_pass<true>(sh, sl, c, wait_cycles);
     sync_parts(parts);
     const float top = top_of_parts(sh, parts);
     uint32_t n = kListMax + 1;
@@ -579,7 +679,7 @@ top_kernel(const void* logits, long long ld, int V, int parts, int K, float inv_
         if (sh.all_count[bin] - before > (uint32_t)kListMax) {
             if (n_all > (uint32_t)K) search_border(sh, sl, false, (uint64_t)K, -1.0, ~0ull, Scale(1.f), 0, &border);
             sync_parts(parts);
-            list_entries(sh, sl, [&](float x, int i) { return order_key(x, i) <= border; });
+            list_entries(sh, sl, -INFINITY, [&](float x, int i) { return order_key(x, i) <= border; });
         } else {
             if (tid == 0) { sh.cta_n = 0; sh.cta_m = 0; }
             __syncthreads();
@@ -712,6 +812,7 @@ top_stream_kernel(const void* logits, long long ld, int V, int M, int steps, int
         float g = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 2));
         if ((lane & 3) == 0) sh.group_top[tid >> 2] = g;
+        const float mine = top;
         const float sum = warp_add((a.x + a.y) + (b.x + b.y));
         top = warp_largest(top);
         if (lane == 0) { sh.wtop[warp] = top; sh.wsum[warp] = sum; sh.groups[warp] = from; }
@@ -724,7 +825,7 @@ top_stream_kernel(const void* logits, long long ld, int V, int M, int steps, int
             if (lane == 0) lse[r] = most > -INFINITY && most < INFINITY ? (float)((double)most * (double)inv_temp + log((double)s)) : most;
         }
         __syncthreads();                                                           // (groups is written again)
-        const float thr = kth_group(sh, 1, K);
+        const float thr = K <= kFewK ? kth_group(sh, 1, K) : kth_thread(sh, mine, K);
         // ---- the entries that reach the threshold
         for (int q = 0; q < steps; ++q) {
             uint4 raw[kStreamLane];
@@ -782,88 +883,128 @@ struct SampleCall {
 
 // Sums of the slice's chunks, relative to 2^ref: of all entries, or (LIST) of those from `above` on, while the entries from `end` to `above`
 // and from `end_k` to `above_k` are listed; returns the thread's share of the mass of the others from `above_k` on, and counts the ones above.
-template <typename T, bool LIST>
-__device__ __noinline__ double sum_chunks(RowShared& sh, Entries en, Scale sc, int ref, float above, float end, float above_k, float end_k, int* n_above) {
+template <bool LIST, typename T, bool HELD>
+__device__ __noinline__ double sum_chunks(RowShared& sh, const Slice<T, HELD> sl, const Scale sc, int ref, float above, float end, float above_k, float end_k,
+                                          int* n_above) {
     constexpr int E = Row<T>::kE;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int w0 = min(en.nv, warp * en.seg), w1 = min(en.nv, w0 + en.seg);
-    double mid = 0.0;
+    double mid = 0.0, s = 0.0, t = 0.0;
     int over = 0;
-    for (int c = 0; c < en.iters; ++c) {
-        double s = 0.0, t = 0.0;
-#pragma unroll 1
-        for (int u = 0; u < kU; ++u) {
-            const int i = w0 + (c * kU + u) * 32 + lane;
-            if (i - lane >= w1) break;
-            float x[E];
-            Row<T>::unpack(i < w1 ? en.data[i] : Row<T>::nothing(), x);
+    sl.each_chunk([&](const uint4& raw, int i) {
+        float x[E];
+        Row<T>::unpack(raw, x);
 #pragma unroll
-            for (int h = 0; h < E; h += 4) {
-                const float y[4] = {x[h], x[h + 1], x[h + 2], x[h + 3]};
-                double m[4];
-                sc.masses(y, ref, m);
+        for (int h = 0; h < E; h += 4) {
+            const float y[4] = {x[h], x[h + 1], x[h + 2], x[h + 3]};
+            double m[4];
+            sc.masses(y, ref, m);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if constexpr (LIST) {
-                        const bool up = y[e] >= above, here = !up && y[e] > -INFINITY && (y[e] >= end || (y[e] >= end_k && y[e] < above_k));
-                        over += up;
-                        (e & 1 ? t : s) += up ? m[e] : 0.0;
-                        mid += !up && !here && y[e] >= above_k ? m[e] : 0.0;
-                        if (here) {
-                            const uint32_t at = atomicAdd(&sh.cta_n, 1u);
-                            if (at < (uint32_t)kListMax) sh.list[at] = order_key(y[e], en.first + i * E + h + e);
-                        }
-                    } else {
-                        (e & 1 ? t : s) += m[e];
+            for (int e = 0; e < 4; ++e) {
+                if constexpr (LIST) {
+                    const bool up = y[e] >= above, here = !up && y[e] > -INFINITY && (y[e] >= end || (y[e] >= end_k && y[e] < above_k));
+                    over += up;
+                    (e & 1 ? t : s) += up ? m[e] : 0.0;
+                    mid += !up && !here && y[e] >= above_k ? m[e] : 0.0;
+                    if (here) {
+                        const uint32_t at = atomicAdd(&sh.cta_n, 1u);
+                        if (at < (uint32_t)kListMax) sh.list[at] = order_key(y[e], sl.first + i * E + h + e);
                     }
+                } else {
+                    (e & 1 ? t : s) += m[e];
                 }
             }
         }
+    }, [&](int c) {
         s = warp_add(s + t);
-        if (lane == 0) sh.chunk[warp * en.iters + c] = s;
-    }
+        if (lane == 0) sh.chunk[warp * sl.iters + c] = s;
+        s = t = 0.0;
+    });
     if constexpr (LIST) *n_above = over;
     return mid;
 }
-// The same of the entries up to the key `last` with a mass of at least `least`, counted in n_above
-template <typename T>
-__device__ __noinline__ void sum_kept(RowShared& sh, Entries en, Scale sc, int ref, uint64_t last, double least, int* kept) {
+// The same of all entries in a single pass, with the largest logit (cta_top): every chunk relative to a power of its own
+template <typename T, bool HELD>
+__device__ __noinline__ bool sum_all(RowShared& sh, const Slice<T, HELD> sl, const Scale sc, long long wait_cycles) {
     constexpr int E = Row<T>::kE;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int w0 = min(en.nv, warp * en.seg), w1 = min(en.nv, w0 + en.seg);
-    int cnt = 0;
-    for (int c = 0; c < en.iters; ++c) {
-        double s = 0.0;
-#pragma unroll 1
-        for (int u = 0; u < kU; ++u) {
-            const int i = w0 + (c * kU + u) * 32 + lane;
-            if (i - lane >= w1) break;
-            float x[E];
-            Row<T>::unpack(i < w1 ? en.data[i] : Row<T>::nothing(), x);
+    bool ok = true;
+    if constexpr (HELD) ok = sm100::mbar_wait_warp(&sh.bar[warp / (kWarps / kPieces)], 0, &sh.abort_flag, wait_cycles);
+    float top = -INFINITY;
+    int c = 0, cnt = 0;
+    for (int i = lane; i < sl.iters; i += 32) { sh.chunk[warp * sl.iters + i] = 0.0; sh.chunk_ref[warp * sl.iters + i] = INT_MIN; }
+    __syncwarp();
+    sl.each_four([&](const uint4 (&raw)[kU], int) {
+        float m = -INFINITY;
 #pragma unroll
-            for (int h = 0; h < E; h += 4) {
-                const float y[4] = {x[h], x[h + 1], x[h + 2], x[h + 3]};
-                double m[4];
-                sc.masses(y, ref, m);
+        for (int u = 0; u < kU; ++u) m = Row<T>::largest(raw[u], m);
+        m = warp_largest(m);
+        if (m > -INFINITY) {
+            const int ref = sc.whole(m);
+            double s = 0.0, t = 0.0;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const bool in = y[e] > -INFINITY && order_key(y[e], en.first + i * E + h + e) <= last && m[e] >= least;
-                    s += in ? m[e] : 0.0;
-                    cnt += in;
+            for (int u = 0; u < kU; ++u) {
+                float x[E];
+                Row<T>::unpack(raw[u], x);
+#pragma unroll
+                for (int h = 0; h < E; h += 4) {
+                    const float y[4] = {x[h], x[h + 1], x[h + 2], x[h + 3]};
+                    double w[4];
+                    sc.masses(y, ref, w);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) { (e & 1 ? t : s) += w[e]; cnt += y[e] > -INFINITY; }
                 }
             }
+            s = warp_add(s + t);
+            if (lane == 0) { sh.chunk[warp * sl.iters + c] = s; sh.chunk_ref[warp * sl.iters + c] = ref; }
+            top = fmaxf(top, m);
         }
-        s = warp_add(s);
-        if (lane == 0) sh.chunk[warp * en.iters + c] = s;
+        ++c;
+    });
+    cnt = __reduce_add_sync(0xffffffffu, cnt);
+    if (lane == 0) { sh.wtop[warp] = top; sh.wcnt[warp] = cnt; }
+    __syncthreads();
+    if (warp == 0) {
+        const float most = warp_largest(lane < kWarps ? sh.wtop[lane] : -INFINITY);
+        cnt = __reduce_add_sync(0xffffffffu, lane < kWarps ? sh.wcnt[lane] : 0);
+        if (lane == 0) { sh.cta_top = most; sh.cta_count = cnt; }
     }
+    return ok;
+}
+// The sums of the entries up to the key `last` with a mass of at least `least`, and (the thread's) how many there are
+template <typename T, bool HELD>
+__device__ __noinline__ void sum_kept(RowShared& sh, const Slice<T, HELD> sl, const Scale sc, int ref, uint64_t last, double least, int* kept) {
+    constexpr int E = Row<T>::kE;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    double s = 0.0;
+    int cnt = 0;
+    sl.each_chunk([&](const uint4& raw, int i) {
+        float x[E];
+        Row<T>::unpack(raw, x);
+#pragma unroll
+        for (int h = 0; h < E; h += 4) {
+            const float y[4] = {x[h], x[h + 1], x[h + 2], x[h + 3]};
+            double m[4];
+            sc.masses(y, ref, m);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const bool in = y[e] > -INFINITY && order_key(y[e], sl.first + i * E + h + e) <= last && m[e] >= least;
+                s += in ? m[e] : 0.0;
+                cnt += in;
+            }
+        }
+    }, [&](int c) {
+        s = warp_add(s);
+        if (lane == 0) sh.chunk[warp * sl.iters + c] = s;
+        s = 0.0;
+    });
     *kept = cnt;
 }
 
 // The entry of a chunk at which the mass in vocabulary order exceeds `over`; kept(x, index, mass): whether an entry counts.  A warp
 // calls it; the chunk may lie in another CTA's slice.  Sums that fall short by rounding end at the last entry with mass.
-template <typename T, typename F>
-__device__ int chunk_crossing(const Slice<T>& sl, int g, double over, const Scale& sc, int ref, F kept, double* its_mass) {
-    constexpr int E = Slice<T>::E;
+template <typename T, bool HELD, typename F>
+__device__ int chunk_crossing(const Slice<T, HELD>& sl, int g, double over, const Scale& sc, int ref, F kept, double* its_mass) {
+    constexpr int E = Row<T>::kE;
     const int lane = threadIdx.x & 31, per_part = kWarps * sl.iters, q = g / per_part, at = g - q * per_part, w = at / sl.iters, c = at - w * sl.iters;
     const uint4* data = sl.parts > 1 ? of_rank(sl.data, q) : sl.data;
     const int v0 = min(sl.row.nvec, q * sl.per), nv = min(sl.row.nvec, v0 + sl.per) - v0, first = v0 * E - sl.row.lead;
@@ -872,7 +1013,8 @@ __device__ int chunk_crossing(const Slice<T>& sl, int g, double over, const Scal
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
         const int i = w0 + (c * kU + u) * 32 + lane;
-        raw[u] = i < w1 ? data[i] : Row<T>::nothing();
+        if constexpr (HELD) raw[u] = i < w1 ? data[i] : Row<T>::nothing();
+        else raw[u] = i < w1 ? sl.load(i) : Row<T>::nothing();
     }
     const auto masses_of = [&](const uint4& now, int u, double (&m)[E]) {
         float x[E];
@@ -1011,7 +1153,7 @@ __device__ void draw_from_list(RowShared& sh, const SampleCall& a, long long r, 
     }
 }
 
-template <typename T>
+template <typename T, bool HELD>
 __global__ void __launch_bounds__(kThreads, 2)
 sample_kernel(SampleCall a) {
     extern __shared__ __align__(16) uint4 data[];
@@ -1027,8 +1169,8 @@ sample_kernel(SampleCall a) {
     const int parts = a.parts, V = a.V;
     const long long r = blockIdx.x / parts;
     const int rank = parts == 1 ? 0 : (int)sm100::cluster_ctarank();
-    const Slice<T> sl(a.logits, a.ld, r, V, parts, rank, data);
-    sl.copy(sh, a.withheld);
+    const Slice<T, HELD> sl(a.logits, a.ld, r, V, parts, rank, data);
+    if constexpr (HELD) sl.copy(sh, a.withheld);
 
     // ---- what the row asks for
     float it = a.inv_temp ? a.inv_temp[r] : 1.f;
@@ -1045,7 +1187,8 @@ sample_kernel(SampleCall a) {
     const Scale sc(it);
     __syncthreads();
 
-    const bool ok = first_pass<T, false>(sh, sl, 0.f, a.wait_cycles);
+    const bool all_stay = !by_k && !by_p && !by_mp;
+    const bool ok = all_stay ? sum_all(sh, sl, sc, a.wait_cycles) : first_pass<false>(sh, sl, 0.f, a.wait_cycles);
     sync_parts(parts);
     const float top = bad ? -INFINITY : top_of_parts(sh, parts);
     const int ref = top > -INFINITY ? sc.whole(top) : 0;
@@ -1129,9 +1272,9 @@ sample_kernel(SampleCall a) {
                 // everything down to the border is few: listed (with top-k and top-p, down to the k-th)
                 const int down = cut_k ? bk : end;
                 __syncthreads();
-                list_entries(sh, sl, [&](float x, int) { return lin.of(x) <= down; });
+                list_from(sh, sl, lin.edge(down));
                 if (!cut_k) {                                                      // top_p of the whole row: its mass
-                    sum_chunks<T, false>(sh, Entries(sl), sc, ref, 0.f, 0.f, 0.f, 0.f, nullptr);
+                    sum_chunks<false>(sh, sl, sc, ref, 0.f, 0.f, 0.f, 0.f, nullptr);
                     summed = true;
                 }
                 sync_parts(parts);
@@ -1153,7 +1296,7 @@ sample_kernel(SampleCall a) {
                         __syncthreads();
                         const float above_them = sh.edges[0], end_them = sh.edges[1], above_k_bin = sh.edges[2], end_k_bin = sh.edges[3];
                         // (without top-k, above_k_bin is minus infinity and nothing lies below it)
-                        double mid = sum_chunks<T, true>(sh, Entries(sl), sc, ref, above_them, end_them, above_k_bin, end_k_bin, &n_over);
+                        double mid = sum_chunks<true>(sh, sl, sc, ref, above_them, end_them, above_k_bin, end_k_bin, &n_over);
                         n_over = __reduce_add_sync(0xffffffffu, n_over);
                         if (lane == 0) sh.wcnt[warp] = n_over;
                         mid = warp_add(mid);
@@ -1238,7 +1381,7 @@ sample_kernel(SampleCall a) {
         } else if (!narrow && by_mp) {
             // min_p alone: the entries that stay, listed if they are few
             const float d = (float)(-log2((double)mp) * 1.0001 / sc.c), from = top - d - fabsf(top) * 1e-6f - d * 1e-4f;
-            list_entries(sh, sl, [&](float x, int) { return x >= from && sc.mass(x, ref) >= least; });
+            list_from(sh, sl, from);                                               // (the few that are too small are cut off below)
             sync_parts(parts);
             narrow = listed(sh, parts) <= (uint32_t)kListMax;
         }
@@ -1282,13 +1425,10 @@ sample_kernel(SampleCall a) {
             kind = kList;
         } else if (kind == kWide) {
             // ---- everything up to a border (or all, or by min_p): its mass chunk by chunk
-            int cnt = 0;
-            const uint64_t last = border;
-            if (last == ~0ull && !by_mp && !a.kept) {
-                sum_chunks<T, false>(sh, Entries(sl), sc, ref, 0.f, 0.f, 0.f, 0.f, nullptr);
-            } else {
-                sum_kept<T>(sh, Entries(sl), sc, ref, last, least, &cnt);
-                cnt = warp_add(cnt);
+            if (!all_stay) {
+                int cnt = 0;
+                sum_kept(sh, sl, sc, ref, border, least, &cnt);
+                cnt = __reduce_add_sync(0xffffffffu, cnt);
                 if (lane == 0) sh.wcnt[warp] = cnt;
                 __syncthreads();
                 if (tid == 0) {
@@ -1296,17 +1436,20 @@ sample_kernel(SampleCall a) {
                     sh.cta_count = cnt;
                 }
             }
-            sync_parts(parts);
+            if (!all_stay) sync_parts(parts);
             if (rank == 0) {
                 const int per_part = kWarps * sl.iters, chunks = parts * per_part;
-                for (int i = tid; i < chunks; i += kThreads) sh.all[i] = *of_rank(&sh.chunk[i % per_part], i / per_part);
-                block_scan(sh.all, chunks, sh.tmp_d);
-                if (tid == 0) {
-                    sh.total = sh.all[chunks - 1];
-                    cnt = 0;
-                    if (a.kept) for (int q = 0; q < parts; ++q) cnt += *of_rank(&sh.cta_count, q);
-                    sh.kept = cnt;
+                for (int i = tid; i < chunks; i += kThreads) {
+                    double m = *of_rank(&sh.chunk[i % per_part], i / per_part);
+                    if (all_stay) {
+                        const int e = *of_rank(&sh.chunk_ref[i % per_part], i / per_part);
+                        m = e == INT_MIN ? 0.0 : times_pow2(m, e - ref);
+                    }
+                    sh.all[i] = m;
                 }
+                block_scan(sh.all, chunks, sh.tmp_d);
+                const int cnt = __reduce_add_sync(0xffffffffu, of_parts(&sh.cta_count, parts));
+                if (tid == 0) { sh.total = sh.all[chunks - 1]; sh.kept = cnt; }
                 __syncthreads();
             }
         }
@@ -1363,14 +1506,43 @@ sample_kernel(SampleCall a) {
         }
         if (dense) {
             const float c32 = (float)sc.c, at_top = (float)(top_mass / total);
-            const T* entries = reinterpret_cast<const T*>(data);
-            const int lo = max(0, sl.first), hi = min(V, sl.first + sl.nv * Slice<T>::E);
-            for (int v = lo + tid; v < hi; v += kThreads) {
-                float x;
-                if constexpr (sizeof(T) == 4) x = (float)entries[v - sl.first];
-                else x = __uint_as_float((uint32_t)entries[v - sl.first] << 16);
-                const bool in = x > -INFINITY && order_key(x, v) <= border && (!by_mp || sc.mass(x, ref) >= least);
-                dense[v] = a.scaled ? (in ? scaled_logit(x, it) : -INFINITY) : (in ? at_top * exp2f((x - top) * c32) : 0.f);
+            constexpr int E = Row<T>::kE;
+            // the borders as logits; masses are compared where the distance in 32 bits leaves them open
+            const float border_at = border == ~0ull ? -INFINITY : key_logit(border);
+            const float d = by_mp ? (float)(-log2((double)mp) / sc.c) : 0.f, slack = fabsf(top) * 1e-6f + d * 1e-4f;
+            const float surely = by_mp ? top - d + slack : -INFINITY, never = by_mp ? top - d - slack : -INFINITY;
+            const auto value = [&](float x, int v) {
+                bool in = x > border_at || (x == border_at && border != ~0ull && order_key(x, v) <= border);
+                if (by_mp && !(x > surely)) in = in && x >= never && sc.mass(x, ref) >= least;
+                return a.scaled ? (in ? scaled_logit(x, it) : -INFINITY) : (in ? at_top * exp2f((x - top) * c32) : 0.f);
+            };
+            if (((reinterpret_cast<uintptr_t>(dense) + (uintptr_t)((long long)sl.first * 4)) & 15) == 0) {
+                sl.each_chunk([&](const uint4& raw, int i) {
+                    const int v = sl.first + i * E;
+                    if (i >= min(sl.nv, (warp + 1) * sl.seg)) return;
+                    float x[E];
+                    Row<T>::unpack(raw, x);
+                    if (v >= 0 && v + E <= V) {
+#pragma unroll
+                        for (int e = 0; e < E; e += 4)
+                            __stcs(reinterpret_cast<float4*>(dense + v + e), make_float4(value(x[e], v + e), value(x[e + 1], v + e + 1), value(x[e + 2], v + e + 2), value(x[e + 3], v + e + 3)));
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < E; ++e)
+                            if (v + e >= 0 && v + e < V) dense[v + e] = value(x[e], v + e);
+                    }
+                }, [](int) {});
+            } else {
+                const T* entries = reinterpret_cast<const T*>(data);
+                const int lo = max(0, sl.first), hi = min(V, sl.first + sl.nv * E);
+#pragma unroll 4
+                for (int v = lo + tid; v < hi; v += kThreads) {
+                    float x;
+                    if constexpr (!HELD) x = sl.row.at(v);
+                    else if constexpr (sizeof(T) == 4) x = (float)entries[v - sl.first];
+                    else x = __uint_as_float((uint32_t)entries[v - sl.first] << 16);
+                    dense[v] = value(x, v);
+                }
             }
         }
         __syncwarp();
@@ -1386,8 +1558,6 @@ static int parts_for(int M, int nvec, int sms) {
     return parts;
 }
 
-static int stream_rows(int sms) { return sms / 2; }
-
 }  // namespace rows
 
 using namespace rows;
@@ -1398,7 +1568,7 @@ sd_status launch_top_logits(const void* logits, int dtype, long long ld, int M, 
     if (cudaGetDevice(&dev) != cudaSuccess) return SD_ERR_CUDA;
     const int nvec = (int)(((long long)V * (dtype == SD_F32 ? 4 : 2) + 15) / 16) + 1;
     const TestKnobs knobs = test_knobs();
-    if (K <= kFewK && M >= stream_rows(sm_count(dev))) {
+    if (K <= kSomeK && M >= sm_count(dev) / 2) {
         auto kern = dtype == SD_F32 ? top_stream_kernel<float> : top_stream_kernel<uint16_t>;
         const int ctas = 2 * sm_count(dev), steps = (nvec + kWarps * kStreamVecs - 1) / (kWarps * kStreamVecs);
         return launch_dependent(kern, dim3((unsigned)(M < ctas ? M : ctas)), kThreads, 0, 1, st, logits, ld, V, M, steps, K, inv_temp, values, index, lse);
@@ -1415,8 +1585,17 @@ sd_status launch_sample(const void* logits, int dtype, long long ld, int M, int 
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return SD_ERR_CUDA;
     const int nvec = (int)(((long long)V * (dtype == SD_F32 ? 4 : 2) + 15) / 16) + 1;
-    const int parts = parts_for(M, nvec, sm_count(dev)), smem = (nvec + parts - 1) / parts * 16;
-    auto kern = dtype == SD_F32 ? sample_kernel<float> : sample_kernel<uint16_t>;
+    // One reading into shared memory where the SMs hold all clusters at once (and where one CTA holds a row).  Beyond that the waves of
+    // clusters wait for their own copies, and passes through L2 by CTAs of which more than one is resident are faster.  152064 f32, k = 50 /
+    // top_p: 64 rows 35 -> 20 / 107 -> 88 us, 256 rows 101 -> 52 / 368 -> 253 us; 32 rows 23 -> 19, but 57 -> 80 us.  Shares of a row: four
+    // or two keep the SMs busy (256 rows in one, two, four: 66, 52, 68 / 267, 253, 295 us), many rows need none (2048 rows, top_p: 1483 us
+    // in one, 1622 us in two).
+    const int fit = parts_for(M, nvec, sm_count(dev)), sms = sm_count(dev);
+    const bool held = nvec <= 5120 || (long long)M * fit <= 2 * sms;
+    const int parts = held ? fit : M < sms ? 4 : M < 6 * sms ? 2 : 1;
+    const int smem = held ? (nvec + parts - 1) / parts * 16 : kCopies * kBins * 4 + kBins * 8;
+    auto kern = dtype == SD_F32 ? (held ? sample_kernel<float, true> : sample_kernel<float, false>)
+                                : (held ? sample_kernel<uint16_t, true> : sample_kernel<uint16_t, false>);
     if (!allow_dynamic_smem(kern, smem)) return SD_ERR_CUDA;
     const TestKnobs knobs = test_knobs();
     const SampleCall call{logits, ld, V, parts, how.inv_temp, how.top_k, how.top_p, how.min_p, u, N, tokens, prob, dense, scaled, lse, kept, dev_status,
