@@ -486,7 +486,8 @@ sd_status sd_draft_feature_attention(const void *qp, const void *k, const void *
  * carry nearly all; Sec. 1: a tree's next level is grown from a node's best candidates), with the row's log-sum-exp.
  *   values : dev f32 [M][K], in order; minus infinity where a row has fewer unmasked entries
  *   index  : dev int32 [M][K], their places; -1 there
- *   lse    : NULL, or dev f32 [M]: log sum_v exp(logits[r][v] * inv_temp); minus infinity for a row without an unmasked entry
+ *   lse    : NULL, or dev f32 [M]: log sum_v exp(logits[r][v] * inv_temp) (products stop at f32's range); minus infinity for a row
+ *            without an unmasked entry
  *   1 <= K <= 1024, inv_temp > 0
  * Every logit is read once.
  */

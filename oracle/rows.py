@@ -26,7 +26,8 @@ def top(x: np.ndarray, K: int, inv_temp: float):
     o = in_order(x)[:K]
     values, index = np.full(K, -np.inf), np.full(K, -1, dtype=np.int64)
     values[:o.size], index[:o.size] = x[o], o
-    return values, index, lse(np.where(np.isnan(x), -np.inf, x) * inv_temp)
+    z = np.where(np.isnan(x), -np.inf, x) * inv_temp
+    return values, index, lse(np.where(np.isfinite(x), np.clip(z, -F32_MAX, F32_MAX), z))
 
 
 def keep(x: np.ndarray, inv_temp: float = 1.0, top_k: int = 0, top_p: float = 1.0, min_p: float = 0.0):

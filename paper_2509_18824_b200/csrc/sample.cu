@@ -96,14 +96,14 @@ struct Slice {
     }
     __device__ __forceinline__ uint4 load(int i) const {                           // vector i, or nothing where that is behind the slice
         if constexpr (HELD) return i < nv ? data[i] : Row<T>::nothing();
-        else return i < nv ? row.load(i) : Row<T>::nothing();
+        else return i < nv ? row.load(v0 + i) : Row<T>::nothing();
     }
     // vectors i0 + lane, + 32, ..
     __device__ __forceinline__ void load_four(int i0, int end, uint4 (&raw)[kU]) const {
         const int lane = threadIdx.x & 31;
-        if (!HELD && i0 >= row.full0 && i0 + 32 * kU <= min(row.full1, end)) {
+        if (!HELD && v0 + i0 >= row.full0 && v0 + i0 + 32 * kU <= row.full1 && i0 + 32 * kU <= end) {
 #pragma unroll
-            for (int u = 0; u < kU; ++u) raw[u] = __ldcg(row.vec + i0 + u * 32 + lane);
+            for (int u = 0; u < kU; ++u) raw[u] = __ldcg(row.vec + v0 + i0 + u * 32 + lane);
         } else {
 #pragma unroll
             for (int u = 0; u < kU; ++u) raw[u] = i0 + u * 32 + lane < end ? load(i0 + u * 32 + lane) : Row<T>::nothing();
@@ -627,6 +627,11 @@ __device__ __noinline__ void search_border(RowShared& sh, const S& sl, bool by_m
 }
 
 // ---------------------------------------------------------------- top logits
+// (the product stops at f32's range: minus infinity is a row without an entry)
+__device__ __forceinline__ float log_sum(float top, float inv_temp, float s) {
+    return (float)(fmin(fmax((double)top * (double)inv_temp, -3.4028234663852886e38), 3.4028234663852886e38) + log((double)s));
+}
+
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 2)
 top_kernel(const void* logits, long long ld, int V, int parts, int K, float inv_temp, float* values, int32_t* index, float* lse, int32_t* status,
@@ -716,7 +721,7 @@ top_kernel(const void* logits, long long ld, int V, int parts, int K, float inv_
                 const float t = *of_rank(&sh.cta_top, q);
                 if (t > -INFINITY) s += *of_rank(&sh.cta_sum, q) * ex2((t - top) * c);
             }
-            lse[r] = top > -INFINITY && top < INFINITY ? (float)((double)top * (double)inv_temp + log((double)s)) : top;
+            lse[r] = top > -INFINITY && top < INFINITY ? log_sum(top, inv_temp, s) : top;
         }
     }
     if (!ok) { set_status(status, SD_ERR_TIMEOUT); sm100::unwind_pause(); }
@@ -822,7 +827,7 @@ top_stream_kernel(const void* logits, long long ld, int V, int M, int steps, int
         if (lse && warp == kWarps - 1) {
             float s = lane < kWarps && wtop > -INFINITY ? sh.wsum[lane] * ex2((sh.groups[lane] - most) * c) : 0.f;
             s = warp_add(s);
-            if (lane == 0) lse[r] = most > -INFINITY && most < INFINITY ? (float)((double)most * (double)inv_temp + log((double)s)) : most;
+            if (lane == 0) lse[r] = most > -INFINITY && most < INFINITY ? log_sum(most, inv_temp, s) : most;
         }
         __syncthreads();                                                           // (groups is written again)
         const float thr = K <= kFewK ? kth_group(sh, 1, K) : kth_thread(sh, mine, K);
@@ -1006,7 +1011,7 @@ template <typename T, bool HELD, typename F>
 __device__ int chunk_crossing(const Slice<T, HELD>& sl, int g, double over, const Scale& sc, int ref, F kept, double* its_mass) {
     constexpr int E = Row<T>::kE;
     const int lane = threadIdx.x & 31, per_part = kWarps * sl.iters, q = g / per_part, at = g - q * per_part, w = at / sl.iters, c = at - w * sl.iters;
-    const uint4* data = sl.parts > 1 ? of_rank(sl.data, q) : sl.data;
+    const uint4* data = HELD && sl.parts > 1 ? of_rank(sl.data, q) : sl.data;
     const int v0 = min(sl.row.nvec, q * sl.per), nv = min(sl.row.nvec, v0 + sl.per) - v0, first = v0 * E - sl.row.lead;
     const int w0 = min(nv, w * sl.seg), w1 = min(nv, w0 + sl.seg);
     uint4 raw[kU];
@@ -1014,7 +1019,7 @@ __device__ int chunk_crossing(const Slice<T, HELD>& sl, int g, double over, cons
     for (int u = 0; u < kU; ++u) {
         const int i = w0 + (c * kU + u) * 32 + lane;
         if constexpr (HELD) raw[u] = i < w1 ? data[i] : Row<T>::nothing();
-        else raw[u] = i < w1 ? sl.load(i) : Row<T>::nothing();
+        else raw[u] = i < w1 ? sl.row.load(v0 + i) : Row<T>::nothing();
     }
     const auto masses_of = [&](const uint4& now, int u, double (&m)[E]) {
         float x[E];
@@ -1586,13 +1591,13 @@ sd_status launch_sample(const void* logits, int dtype, long long ld, int M, int 
     if (cudaGetDevice(&dev) != cudaSuccess) return SD_ERR_CUDA;
     const int nvec = (int)(((long long)V * (dtype == SD_F32 ? 4 : 2) + 15) / 16) + 1;
     // One reading into shared memory where the SMs hold all clusters at once (and where one CTA holds a row).  Beyond that the waves of
-    // clusters wait for their own copies, and passes through L2 by CTAs of which more than one is resident are faster.  152064 f32, k = 50 /
-    // top_p: 64 rows 35 -> 20 / 107 -> 88 us, 256 rows 101 -> 52 / 368 -> 253 us; 32 rows 23 -> 19, but 57 -> 80 us.  Shares of a row: four
-    // or two keep the SMs busy (256 rows in one, two, four: 66, 52, 68 / 267, 253, 295 us), many rows need none (2048 rows, top_p: 1483 us
-    // in one, 1622 us in two).
+    // clusters wait for their own copies, and passes through L2 by CTAs of which two are resident are faster.  152064 f32, k = 50 / top_p:
+    // 64 rows 36 -> 21 / 108 -> 90 us, 256 rows 101 -> 72 / 368 -> 270 us; 32 rows are as fast, but 57 -> 88 us.  A row's shares: as many
+    // as still run at once, and two where rows differ in what they ask for (256 rows, all kinds mixed: 235 us in one, 199 in two, 209 in
+    // four; 2048 rows: 920, 1026, 1309 us).
     const int fit = parts_for(M, nvec, sm_count(dev)), sms = sm_count(dev);
     const bool held = nvec <= 5120 || (long long)M * fit <= 2 * sms;
-    const int parts = held ? fit : M < sms ? 4 : M < 6 * sms ? 2 : 1;
+    const int parts = held ? fit : 4LL * M <= 2 * sms ? 4 : M <= 2 * sms ? 2 : 1;
     const int smem = held ? (nvec + parts - 1) / parts * 16 : kCopies * kBins * 4 + kBins * 8;
     auto kern = dtype == SD_F32 ? (held ? sample_kernel<float, true> : sample_kernel<float, false>)
                                 : (held ? sample_kernel<uint16_t, true> : sample_kernel<uint16_t, false>);

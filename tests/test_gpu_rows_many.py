@@ -1,0 +1,169 @@
+"""GPU: rows of logits in numbers at which a call reads them from memory more than once (or in shares of one, two and four CTAs), in
+place, in graphs and on two streams; copies that do not come."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import rows as ref
+from paper_2509_18824_b200 import binding as sd
+from rows_util import device_rows
+from test_gpu_rows_sampling import batch, check, filtered, parameters, sample, top
+
+pytestmark = pytest.mark.gpu
+
+
+# 152064 f32 of 40 to 74 rows: shares of a quarter; fewer than 297 rows: halves; beyond: whole rows (20600 f32 and 41000 bf16 are more than
+# a CTA's shared memory holds)
+@pytest.mark.parametrize("kind,M,V,ld,which", [("f32", 80, 41000, 41000, "kpm"), ("f32", 80, 41001, 41007, "p"), ("f32", 160, 20600, 20600, "kpmg"),
+                                               ("f32", 160, 20603, 20603, ""), ("f32", 900, 20600, 20601, "kpm"), ("f32", 80, 41000, 41000, "m"),
+                                               ("f32", 52, 152064, 152064, "kpm"), ("f32", 39, 152065, 152069, "p"), ("f32", 74, 82001, 82001, "m"), ("bf16", 74, 262143, 262144, "kpmg"),
+                                               ("bf16", 80, 82001, 82001, "kpm"), ("bf16", 160, 41000, 41000, "p"), ("bf16", 900, 41100, 41100, "kpmg"),
+                                               ("bf16", 160, 41003, 41011, "kp")])
+def test_many_rows(kind, M, V, ld, which):
+    t, x = batch(M, V, kind, M + V, ld=ld)
+    check(t, x, parameters(M, V, M + V, which), M, N=1)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_flat_rows_of_the_largest_vocabulary(kind):
+    """All mass in a few bins of a histogram, in a single one even: sums that 32 bits hold only in parts."""
+    M, V = 76, 262144
+    t, x = batch(M, V, kind, 3, patterns=("equal", "flat", "all_lowest", "bulk", "rising"))
+    it = np.ones(M, dtype=np.float32)
+    p = np.resize(np.array([0.5, 0.9, 0.999], dtype=np.float32), M)
+    k = np.resize(np.array([0, 0, 0, 0, 200000, 1500], dtype=np.int32), M)
+    # (equal logits at p = 0.5 have a border at exactly half of the entries: two patterns in five, one row in three, are left out)
+    check(t, x, (it, k, p, None), 1, N=1, decisive=1 - 2 / 15 - 0.05)
+
+
+@pytest.mark.parametrize("M,V", [(45, 100003), (80, 41000), (160, 20603), (900, 20600)])
+def test_filter_in_place_and_repeated(M, V):
+    t, x = batch(M, V, "f32", 8)
+    params = parameters(M, V, 8, "kpm")
+    first = filtered(t, params)
+    again = filtered(t, params)
+    copy = t.clone()
+    into = filtered(copy, params, out=copy)
+    for a, b, c in zip(first, again, into):
+        np.testing.assert_array_equal(a, b)
+        np.testing.assert_array_equal(a, c)
+
+
+def test_shares_of_a_row_do_not_change_what_stays():
+    """The same rows in calls of 20, 40, 80 and 400 rows."""
+    V = 90001
+    t, x = batch(20, V, "f32", 21)
+    params = parameters(20, V, 21, "kpm")
+    u = np.random.default_rng(2).random((20, 2)).astype(np.float32)
+    want = sample(t, params, u)
+    out = filtered(t, params)
+    for times in (2, 4, 20):
+        many = t.repeat(times, 1)
+        tiled = tuple(None if a is None else np.tile(a, times) for a in params)
+        tokens, prob, dense, lse, st = sample(many, tiled, np.tile(u, (times, 1)))
+        o, l, kept, fst = filtered(many, tiled)
+        assert st == 0 and fst == 0
+        for i in range(times):
+            s = slice(i * 20, i * 20 + 20)
+            np.testing.assert_array_equal(tokens[s], want[0])
+            np.testing.assert_array_equal(kept[s], out[2])
+            np.testing.assert_array_equal(o[s], out[0])
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("M,V,K,ld", [(80, 20000, 112, 20000), (80, 20000, 113, 20007), (149, 9001, 300, 9001), (149, 9001, 384, 9003), (149, 9001, 385, 9001),
+                                      (300, 700, 384, 701), (300, 50, 200, 50), (74, 3, 3, 3)])
+def test_top_logits_of_many_rows(kind, M, V, K, ld):
+    t, x = batch(M, V, kind, K, ld=ld)
+    values, index, lse = top(t, K, 1.25)
+    for r in range(M):
+        v, i, l = ref.top(x[r], K, 1.25)
+        np.testing.assert_array_equal(index[r], i, err_msg=str(r))
+        np.testing.assert_array_equal(values[r].astype(np.float64) + 0.0, v + 0.0)
+        # sums of V terms that are off by 2^-22 and an argument of at most 2^6 rounded to 2^-24 of it each, in 32 bits
+        assert lse[r] == l if np.isinf(l) else abs(lse[r] - l) <= 2e-5 + 2.0 ** -23 * abs(l)
+
+
+def calls(t, M, V, how, u):
+    """The three calls on t, as a function that enqueues them on the current stream, and what they write."""
+    f, i = (lambda *s: torch.zeros(s, device="cuda")), (lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda"))
+    out = dict(values=f(M, 20), index=i(M, 20), top_lse=f(M), tokens=i(M, 2), prob=f(M, 2), probs=f(M, V), lse=f(M), rows=f(M, V), flse=f(M), kept=i(M), st=sd.new_status())
+
+    def enqueue():
+        st = out["st"]
+        sd.sd_top_logits(t, 1.0, out["values"], out["index"], out["top_lse"], st)
+        sd.sd_sample_logits(t, how, u, out["tokens"], out["prob"], out["probs"], out["lse"], st)
+        sd.sd_filter_logits(t, how, out["rows"], out["flse"], out["kept"], st)
+    return enqueue, out
+
+
+@pytest.mark.parametrize("M,V", [(6, 30000), (80, 41000)])
+def test_calls_in_a_graph_on_new_rows_and_parameters(M, V):
+    t, _ = batch(M, V, "f32", 5)
+    how = sd.Sampling(*parameters(M, V, 5, "kpm"))
+    u = torch.rand((M, 2), device="cuda")
+    enqueue, out = calls(t, M, V, how, u)
+    enqueue()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        enqueue()
+    for seed in (6, 7):
+        t.copy_(batch(M, V, "f32", seed)[0])
+        new = sd.Sampling(*parameters(M, V, seed, "kpm"))
+        for a, b in ((how.inv_temp, new.inv_temp), (how.top_k, new.top_k), (how.top_p, new.top_p), (how.min_p, new.min_p)):
+            a.copy_(b)
+        u.uniform_()
+        u.clamp_(max=0.9999999)
+        graph.replay()
+        got = {k: v.clone() for k, v in out.items()}
+        for v in out.values():
+            v.zero_()
+        enqueue()
+        torch.cuda.synchronize()
+        for k in got:
+            assert torch.equal(got[k], out[k]), k
+    assert int(out["st"].item()) == 0
+
+
+def test_two_streams_at_once():
+    """Calls of few and of many rows side by side: nothing is shared between them."""
+    jobs = []
+    for M, V, seed in ((6, 152064, 11), (80, 41000, 12)):
+        t, _ = batch(M, V, "f32", seed)
+        jobs.append((calls(t, M, V, sd.Sampling(*parameters(M, V, seed, "kpm")), torch.rand((M, 2), device="cuda").clamp_(max=0.9999999)), torch.cuda.Stream()))
+    want = []
+    for (enqueue, out), _ in jobs:
+        enqueue()
+        torch.cuda.synchronize()
+        want.append({k: v.clone() for k, v in out.items()})
+        for v in out.values():
+            v.zero_()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for (enqueue, out), s in jobs:
+            with torch.cuda.stream(s):
+                enqueue()
+    torch.cuda.synchronize()
+    for ((_, out), _), w in zip(jobs, want):
+        for k in w:
+            assert torch.equal(out[k], w[k]), k
+        assert int(out["st"].item()) == 0
+
+
+def test_a_copy_that_does_not_come_is_reported(monkeypatch):
+    M, V = 4, 30000
+    t, x = batch(M, V, "f32", 9, patterns=("bulk", "peaks"))
+    params = parameters(M, V, 9, "kp")
+    u = np.full((M, 1), 0.5, dtype=np.float32)
+    monkeypatch.setenv("SDV_TEST_WAIT_CYCLES", "100000")
+    monkeypatch.setenv("SDV_TEST_WITHHOLD", "1")
+    assert sample(t, params, u)[4] == sd.SD_ERR_TIMEOUT
+    assert filtered(t, params)[3] == sd.SD_ERR_TIMEOUT
+    values, index, st = torch.zeros((M, 8), device="cuda"), torch.zeros((M, 8), dtype=torch.int32, device="cuda"), sd.new_status()
+    sd.sd_top_logits(t, 1.0, values, index, None, st)
+    torch.cuda.synchronize()
+    assert int(st.item()) == sd.SD_ERR_TIMEOUT
+    monkeypatch.delenv("SDV_TEST_WITHHOLD")
+    monkeypatch.delenv("SDV_TEST_WAIT_CYCLES")
+    check(t, x, params, 9, N=1)

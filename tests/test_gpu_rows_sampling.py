@@ -74,7 +74,7 @@ def close(got, want, rel, abs_=0.0):
     assert (np.abs(got[f] - want[f]) <= rel * np.abs(want[f]) + abs_).all()
 
 
-def check(t, x, params, seed, N=3, probs=True):
+def check(t, x, params, seed, N=3, probs=True, decisive=0.9):
     M, V = x.shape
     u = np.random.default_rng(seed).random((M, N)).astype(np.float32)
     u[0, 0] = 0.0
@@ -107,7 +107,7 @@ def check(t, x, params, seed, N=3, probs=True):
             decided += 1
             assert tokens[r, n] == want, (r, n, how)
             assert prob[r, n] == pytest.approx(p[want] if want >= 0 else 0.0, rel=2.0 ** -22)
-    assert decided >= 0.9 * M * N
+    assert decided >= decisive * M * N
 
 
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
