@@ -44,9 +44,9 @@ __device__ __forceinline__ bool sum_warps_or(bool v) {
 __device__ __forceinline__ float whole_power(float top, float c) { return top > -INFINITY ? rintf(top * c) : 0.f; }
 
 // What a CTA tells the others of its row: its largest logit and, with its R, the sums of 2^(x c - R) outside and among the
-// entries and of 2^(x log2 e - R1); its part of sum p z; the label's logit where it lies in its slice.
-struct __align__(16) Message { float top, label, rest, listed, sum1, pad; double entries; };
-static_assert(sizeof(Message) == 32, "two stores of 16 bytes");
+// entries and of 2^(x log2 e - R1); its entries' sums of p z, p and p log p; the label's logit where it lies in its slice.
+struct __align__(16) Message { float top, label, rest, sum1; double listed, entries, mass, plogp; };
+static_assert(sizeof(Message) == 48, "three stores of 16 bytes");
 
 // A place in the ring of slots and the phase of its barriers
 struct Turn {
@@ -56,11 +56,12 @@ struct Turn {
 };
 
 struct RowInfo {                       // prepared ahead
-    double mass, plogp;                // sums of p and p log p
+    double mass, plogp;                // sums of p and p log p over them
     float weight;                      // dloss
-    int label, any, count;             // count: entries that lie in this CTA's slice
+    int label, any, count;             // any: the row has entries; count: those that lie in this CTA's slice
 };
-struct RowFactors { float top, listed, tail, one; };           // what an exponential is multiplied with at the entries, elsewhere, for the cross-entropy
+// What an exponential is multiplied with at the entries, elsewhere, for the cross-entropy, and what the list's p are
+struct RowFactors { float top, listed, tail, one, p; };
 
 struct DistillShared {
     uint64_t full[kMaxSlots], picked[kMaxSlots], free_[kMaxSlots];
@@ -69,8 +70,8 @@ struct DistillShared {
     RowInfo info[kMaxLists];
     float label_z[kMaxLists];
     int dup[kMaxLists], label_listed[kMaxLists];
-    float4 sums[2][kSumWarps + 1];     // the warps' (largest logit, sum outside the entries, 0, sum at temperature 1); the listed entries'
-    double part[2];                    // sum of p z
+    float4 sums[2][kSumWarps + 1];     // the warps' (largest logit, sum outside the entries, 0, sum at temperature 1); the entries' (largest logit, 0, 0, sum at temperature 1)
+    double part[2], listed[2];         // sum of p z; the listed entries' sum of 2^(z c - R)
     Message msg[2][8];
     RowFactors row[2];
 };
@@ -111,6 +112,7 @@ struct Factors {
         per_p = g * a.kl_weight * a.inv_temp;
         listed = per_p * rf.listed;
         tail = per_p * rf.tail;
+        per_p *= rf.p;
         per_label = has_label ? g * a.ce_weight : 0.f;
         one = per_label != 0.f ? per_label * rf.one : 0.f;
         two = a.inv_temp != 1.f && one != 0.f;
@@ -170,50 +172,95 @@ struct RawList {
         weight = a.dloss ? __ldcg(a.dloss + r) : 1.f;
         t_lse = a.top_lse ? __ldcg(a.top_lse + r) : 0.f;
     }
-    __device__ __forceinline__ int index(int k) const { return k < 32 ? i0 : (k < 64 ? i1 : __ldcg(idx + k)); }
-    __device__ __forceinline__ float logit(int k) const { return k < 32 ? t0 : (k < 64 ? t1 : __ldcg(val + k)); }
+    // the entries from the 65th on, into the list's place (the lists in shared memory are written from their front, behind what is read)
+    __device__ __forceinline__ void stage(const Lists& li, int K) const {
+        const int lane = threadIdx.x & 31;
+        for (int k0 = 64 + lane; k0 < K; k0 += 128) {
+            int i[4];
+            float t[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int k = k0 + 32 * j;
+                i[j] = k < K ? __ldcg(idx + k) : -1;
+                t[j] = k < K ? __ldcg(val + k) : 0.f;
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (k0 + 32 * j < K) { li.at[k0 + 32 * j] = i[j]; li.z[k0 + 32 * j] = t[j]; }
+        }
+        __syncwarp();
+    }
+    __device__ __forceinline__ int index(const Lists& li, int k) const { return k < 32 ? i0 : (k < 64 ? i1 : li.at[k]); }
+    __device__ __forceinline__ float logit(const Lists& li, int k) const { return k < 32 ? t0 : (k < 64 ? t1 : li.z[k]); }
 };
 
-// By one warp: the entries of row r.
-template <typename T>
+// f(k, N values in a row of N * 32) for a list's entries: one each, where they are few, or four side by side (a chain of multiply-adds each)
+template <typename F>
+__device__ __forceinline__ void each_entry(int count, F f) {
+    const int lane = threadIdx.x & 31;
+    if (count <= 32) f(lane, std::integral_constant<int, 1>{});
+    else
+        for (int k = lane; k < count; k += 128) f(k, std::integral_constant<int, 4>{});
+}
+
+// By one warp: the entries of row r that lie in the slice (every CTA takes its own, and the join brings their sums together).  Without
+// top_lse their p are relative to the row's first one until then (in a launch for the gradient alone, where 32 bits do for p, at once).
+template <typename T, int MODE>
 __device__ __forceinline__ void prepare_entries(RowInfo& info, const Lists& li, const DistillCall& a, long long r, const RawList& raw, const SliceOf<T>& sl, bool report) {
     const int lane = threadIdx.x & 31;
     const int count = (sl.v1 - sl.v0) * SliceOf<T>::E;
-    double log_norm = (double)raw.t_lse;
+    raw.stage(li, a.K);
+    float top = -INFINITY, norm = 0.f;
     if (!a.top_lse) {                                                              // the entries' own soft-max
-        float top = -INFINITY;
         for (int k = lane; k < a.K; k += 32) {
-            const int i = raw.index(k);
-            if (i >= 0 && i < a.V) top = fmaxf(top, raw.logit(k));
+            const int i = raw.index(li, k);
+            if (i >= 0 && i < a.V) top = fmaxf(top, raw.logit(li, k));
         }
         top = warp_largest(top);
-        double norm = 0.0;
-        for (int k = lane; k < a.K; k += 32) {
-            const int i = raw.index(k);
-            if (i >= 0 && i < a.V) norm += exp(((double)raw.logit(k) - (double)top) * (double)a.inv_temp);
+        if constexpr (MODE == kGrad) {
+            for (int k = lane; k < a.K; k += 32) {
+                const int i = raw.index(li, k);
+                if (i >= 0 && i < a.V) norm += ex2((raw.logit(li, k) - top) * (a.inv_temp * kLog2e));
+            }
+            norm = warp_add(norm);
         }
-        norm = warp_add(norm);
-        log_norm = (double)top * (double)a.inv_temp + log(norm);
     }
-    double mass = 0.0, plogp = 0.0;
     bool any = false;
     int n = 0;
     for (int k0 = 0; k0 < a.K; k0 += 32) {
-        const int k = k0 + lane, i = k < a.K ? raw.index(k) : -1, at = i - sl.first;
+        const int k = k0 + lane, i = k < a.K ? raw.index(li, k) : -1, at = i - sl.first;
+        const float t = k < a.K ? raw.logit(li, k) : 0.f;
         const bool there = i >= 0 && i < a.V, here = there && at >= 0 && at < count;
-        const double log_p = there ? (double)raw.logit(k) * (double)a.inv_temp - log_norm : -INFINITY, p = exp(log_p);
-        mass += p;
-        if (p != 0.0) plogp += p * log_p;
-        const uint32_t all = __ballot_sync(0xffffffffu, here);
+        const uint32_t all = __ballot_sync(0xffffffffu, here);                     // (all have read their entry of this round)
         if (here) {
             const int to = n + __popc(all & ((1u << lane) - 1));
-            li.p[to] = p;
             li.at[to] = at;
+            li.z[to] = t;
         }
         n += __popc(all);
         any = any || there;
         if (i >= a.V && report) set_status(a.status, SD_ERR_BOUNDS);
     }
+    __syncwarp();
+    const double from = a.top_lse ? 0.0 : (double)top, off = a.top_lse ? (double)raw.t_lse : MODE == kGrad ? (double)logf(norm) : 0.0;
+    double mass = 0.0, plogp = 0.0;
+    each_entry(n, [&](int k0, auto side) {
+        constexpr int N = decltype(side)::value;
+        double log_p[N], t[N], p[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const int k = k0 + 32 * j;
+            log_p[j] = k < n ? ((double)li.z[k] - from) * (double)a.inv_temp - off : -INFINITY;
+            t[j] = log_p[j] * 1.4426950408889634074;
+        }
+        powers_of_two(t, p);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            if (k0 + 32 * j < n) li.p[k0 + 32 * j] = p[j];
+            mass += p[j];
+            if (p[j] != 0.0) plogp += p[j] * log_p[j];
+        }
+    });
     mass = warp_add(mass);
     plogp = warp_add(plogp);
     any = __any_sync(0xffffffffu, any);
@@ -269,7 +316,7 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
             const RawList raw(a, r);                                               // (under way while the place is waited for)
             ok = mbar_wait_warp(&sh.info_free[b], phase_of(n) ^ 1u, &sh.abort_flag, wait_cycles);
             if (!ok) break;
-            prepare_entries<T>(sh.info[b], lists_of(b), a, r, raw, sl, rank_of(u) == 0);
+            prepare_entries<T, MODE>(sh.info[b], lists_of(b), a, r, raw, sl, rank_of(u) == 0);
             if (lane == 0) mbar_arrive(&sh.info_full[b]);
         }
     } else if (warp == kCopyWarp) {
@@ -381,7 +428,9 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
             label_listed = __any_sync(0xffffffffu, label_listed);
             if constexpr (MODE != kGrad) {
                 // the listed entries' own sums, every index once
-                float top = -INFINITY, sum = 0.f, sum1 = 0.f;
+                // (in 64 bits: a draft that has learned is as near to the target as their rounding in 32)
+                float top = -INFINITY, sum1 = 0.f;
+                double sum = 0.0;
                 if (rest_too) {
                     const auto counts = [&](int k) { return k < 32 ? j0 >= 0 && !again0 : li.at[k] < kAgain; };
                     const auto logit = [&](int k) { return count <= 32 ? z0 : li.z[k]; };
@@ -389,18 +438,27 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
                     for (int k = lane; k < count; k += 32) if (counts(k)) top = fmaxf(top, logit(k));
                     top = warp_largest(top);
                     const float r_c = whole_power(top, c), r_e = whole_power(top, kLog2e);
-                    for (int k = lane; k < count; k += 32)
-                        if (counts(k)) {
-                            sum += ex2(fmaf(logit(k), c, -r_c));
-                            sum1 += ex2(fmaf(logit(k), kLog2e, -r_e));
+                    each_entry(count, [&](int k0, auto side) {
+                        constexpr int N = decltype(side)::value;
+                        double t[N], m[N];
+#pragma unroll
+                        for (int j = 0; j < N; ++j) {
+                            const int k = k0 + 32 * j;
+                            const float z = k < count && counts(k) ? logit(k) : -INFINITY;
+                            t[j] = fma((double)z, (double)c, -(double)r_c);
+                            sum1 += ex2(fmaf(z, kLog2e, -r_e));
                         }
+                        powers_of_two(t, m);
+#pragma unroll
+                        for (int j = 0; j < N; ++j) sum += m[j];
+                    });
                     sum = warp_add(sum);
                     sum1 = warp_add(sum1);
                 }
                 part = warp_add(part);
                 // (the loss alone: the sums of two rows before have been taken over)
                 ok = mbar_wait_warp(&sh.row_ready[h], (uint32_t)((n >> 1) & 1) ^ 1u, &sh.abort_flag, wait_cycles);
-                if (lane == 0) { sh.sums[h][kSumWarps] = make_float4(top, 0.f, sum, sum1); sh.part[h] = part; }
+                if (lane == 0) { sh.sums[h][kSumWarps] = make_float4(top, 0.f, 0.f, sum1); sh.part[h] = part; sh.listed[h] = sum; }
             }
             if (lane == 0) { sh.label_z[b] = label_z; sh.dup[b] = dup; sh.label_listed[b] = label_listed; }
             __syncwarp();
@@ -423,55 +481,63 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
             const int label = info.label;
             const bool has_label = label >= 0 && label < a.V, two = has_label && a.inv_temp != 1.f;
             const float4 w = lane <= kSumWarps ? sh.sums[h][lane] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
-            double entries = sh.part[h];
+            double entries = sh.part[h], listed = 0.0, mass = info.mass, plogp = info.plogp;
             float label_z = sh.label_z[b], most = warp_largest(w.x);
             const float f = weigh(w.x, most, c);
-            float rest = warp_add(w.y * f), listed = rest_too ? warp_add(w.z * f) : 0.f, sum1 = two ? warp_add(w.w * weigh(w.x, most, kLog2e)) : 0.f;
+            if (rest_too) listed = sh.listed[h] * (double)__shfl_sync(0xffffffffu, f, kSumWarps);
+            float rest = warp_add(w.y * f), sum1 = two ? warp_add(w.w * weigh(w.x, most, kLog2e)) : 0.f;
             if (talk) {
-                const Message mine{most, label_z, rest, listed, sum1, 0.f, entries};
+                const Message mine{most, label_z, rest, sum1, listed, entries, mass, plogp};
                 if (lane == rank) {
                     sh.msg[h][rank] = mine;
                     mbar_arrive_expect_tx(&sh.told[h], (parts - 1) * (uint32_t)sizeof(Message));
                 } else if (lane < parts) {
                     const uint32_t to = map_dsmem(smem_u32(&sh.msg[h][rank]), lane), bar = map_dsmem(smem_u32(&sh.told[h]), lane);
-                    st_async_v4(to, __float_as_uint(most), __float_as_uint(label_z), __float_as_uint(rest), __float_as_uint(listed), bar);
-                    st_async_v4(to + 16, __float_as_uint(sum1), 0u, (uint32_t)__double2loint(entries), (uint32_t)__double2hiint(entries), bar);
+                    st_async_v4(to, __float_as_uint(most), __float_as_uint(label_z), __float_as_uint(rest), __float_as_uint(sum1), bar);
+                    st_async_v4(to + 16, (uint32_t)__double2loint(listed), (uint32_t)__double2hiint(listed), (uint32_t)__double2loint(entries), (uint32_t)__double2hiint(entries), bar);
+                    st_async_v4(to + 32, (uint32_t)__double2loint(mass), (uint32_t)__double2hiint(mass), (uint32_t)__double2loint(plogp), (uint32_t)__double2hiint(plogp), bar);
                 }
                 ok = mbar_wait_cluster(&sh.told[h], ph, &sh.abort_flag, wait_cycles);
                 ok = __all_sync(0xffffffffu, ok);
-                Message o{-INFINITY, 0.f, 0.f, 0.f, 0.f, 0.f, 0.0};
+                Message o{-INFINITY, 0.f, 0.f, 0.f, 0.0, 0.0, 0.0, 0.0};
                 if (lane < parts) o = sh.msg[h][lane];
                 most = warp_largest(o.top);
                 const float g = weigh(o.top, most, c);
                 rest = warp_add(o.rest * g);
-                listed = rest_too ? warp_add(o.listed * g) : 0.f;
+                listed = rest_too ? warp_add(o.listed * (double)g) : 0.0;
                 if (two) sum1 = warp_add(o.sum1 * weigh(o.top, most, kLog2e));
                 entries = o.entries;
                 label_z = o.label;
+                mass = warp_add(o.mass);
+                plogp = o.plogp;
             }
-            const float sum = rest + listed;
+            const double p_unit = rest_too || !(mass > 0.0) ? 1.0 : 1.0 / mass;    // what the list's p are multiples of
+            const double total = (double)rest + listed;
+            const float sum = (float)total;
             if (!two) sum1 = sum;
-            const double p_rest = rest_too ? 1.0 - info.mass : 0.0;
+            const double p_rest = rest_too ? 1.0 - mass : 0.0;
             const bool has_rest = p_rest > 0.0 && rest > 0.f;
-            const float all_p = has_rest ? 1.f : (info.any ? (float)info.mass : 0.f);
+            const float all_p = has_rest ? 1.f : (info.any ? (rest_too ? (float)mass : 1.f) : 0.f);
             // tail / sum = (all_p - p_rest / s_rest) / sum with s_rest = rest / sum
             const float inv = 1.f / sum, tail = has_rest ? inv - (float)p_rest / rest : all_p * inv;
-            const RowFactors rf{most, all_p * inv, tail, two ? 1.f / sum1 : inv};
+            const RowFactors rf{most, all_p * inv, tail, two ? 1.f / sum1 : inv, (float)p_unit};
             if (lane == 0) { sh.row[h] = rf; mbar_arrive(&sh.row_ready[h]); }
             if (rank == 0) {
-                if (talk) { entries = warp_add(entries); label_z = warp_add(label_z); }
-                // lane 0: kl; lane 1: ce.  (R belongs to the power with c as 32 bits hold it: log sum = R ln 2 + log(sum), but for c's rounding)
-                const float cc = lane == 0 ? c : kLog2e;
-                const double it = lane == 0 ? (double)a.inv_temp : 1.0;
+                if (talk) { entries = warp_add(entries); label_z = warp_add(label_z); plogp = warp_add(plogp); }
+                if (!rest_too) { plogp = plogp * p_unit - log(mass); entries *= p_unit; mass = 1.0; }
+                // lane 0: kl; lane 1: ce.  R belongs to the power with c as 32 bits hold it.  Relative to the largest logit that is a slightly
+                // other temperature: ce takes it back at that logit; in kl the entries' logits stand at the same one, so that what is left
+                // of it counts by the difference of the two distributions.
+                constexpr double kLn2 = 0.69314718055994530942;
                 if (lane < 2) {
-                    const double lse = (double)most * it + log((double)(lane == 0 ? sum : sum1)) - ((double)most * (double)cc - (double)whole_power(most, cc)) * 0.69314718055994530942;
                     if (lane == 0) {
-                        double kl = info.any ? info.plogp - entries * it + info.mass * lse : 0.0;
-                        if (has_rest && info.any) kl += p_rest * log(p_rest * (double)sum / (double)rest);
+                        double kl = info.any ? plogp - entries * ((double)c * kLn2) + mass * (log(total) + (double)whole_power(most, c) * kLn2) : 0.0;
+                        if (has_rest && info.any) kl += p_rest * log(p_rest * total / (double)rest);
                         a.kl[r] = (float)kl;
                         if (a.stats) reinterpret_cast<float4*>(a.stats)[r] = make_float4(rf.top, rf.listed, rf.tail, rf.one);
                         if (label >= a.V) set_status(a.status, SD_ERR_BOUNDS);
                     } else if (a.ce) {
+                        const double lse = (double)most + log((double)sum1) - ((double)most * (double)kLog2e - (double)whole_power(most, kLog2e)) * kLn2;
                         a.ce[r] = has_label ? (float)(lse - (double)label_z) : 0.f;
                     }
                 }
@@ -568,7 +634,7 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
                 }
             } else {
                 const float4 st = __ldcg(reinterpret_cast<const float4*>(a.stats) + r);
-                rf = RowFactors{st.x, st.y, st.z, st.w};
+                rf = RowFactors{st.x, st.y, st.z, st.w, 1.f};
                 if (label >= a.V && tid == 0 && rank_of(u) == 0) set_status(a.status, SD_ERR_BOUNDS);
             }
 

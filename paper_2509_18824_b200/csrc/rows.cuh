@@ -176,6 +176,32 @@ struct Scale {
         return m[0];
     }
 };
+// 2^t, by the same series, N of them side by side; 0 below 2^-1000, NaN of NaN
+template <int N>
+__device__ __forceinline__ void powers_of_two(const double (&t)[N], double (&m)[N]) {
+    const double big = 6755399441055744.0;
+    constexpr double kC[10] = {1.0, 6.9314718055994531e-01, 2.4022650695910072e-01, 5.5504108664821580e-02, 9.6181291076284772e-03,
+                               1.3333558146428443e-03, 1.5403530393381609e-04, 1.5252733804059841e-05, 1.3215486790144309e-06,
+                               1.0178086009239699e-07};                            // (ln 2)^k / k!
+    double f[N];
+    int e[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const double x = fmin(fmax(t[j], -2000.0), 1000.0), r = x + big;
+        e[j] = __double2loint(r);
+        f[j] = x - (r - big);
+        m[j] = kC[9];
+    }
+#pragma unroll
+    for (int k = 8; k >= 0; --k)
+#pragma unroll
+        for (int j = 0; j < N; ++j) m[j] = fma(m[j], f[j], kC[k]);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const bool none = e[j] < -1000;
+        m[j] = t[j] != t[j] ? t[j] : __hiloint2double(none ? 0 : __double2hiint(m[j]) + (e[j] << 20), none ? 0 : __double2loint(m[j]));
+    }
+}
 // v * 2^e
 __device__ __forceinline__ double times_pow2(double v, int e) {
     if (e < -1000) return 0.0;

@@ -356,25 +356,20 @@ __device__ __forceinline__ float kth_group(RowShared& sh, int parts, int k) {
     return sh.thr;
 }
 
-// The same of a row's 512 threads' largest logits, in its only CTA, k <= kSomeK
+// A threshold that at least k of a row's 512 threads' largest logits reach, and hardly more, in its only CTA (k <= kSomeK): the range of
+// keys is halved until the count is near
 __device__ __noinline__ float kth_thread(RowShared& sh, float mine, int k) {
-    float4* tops = reinterpret_cast<float4*>(sh.all_count);
-    const int tid = threadIdx.x;
-    reinterpret_cast<float*>(tops)[tid] = mine;
-    __syncthreads();
-    int before = 0;
-#pragma unroll 4
-    for (int j = 0; j < kThreads / 4; ++j) {
-        const float4 t = tops[j];
-        const int at = 4 * j;
-        before += t.x > mine || (t.x == mine && at < tid);
-        before += t.y > mine || (t.y == mine && at + 1 < tid);
-        before += t.z > mine || (t.z == mine && at + 2 < tid);
-        before += t.w > mine || (t.w == mine && at + 3 < tid);
+    const uint32_t u = __float_as_uint(mine + 0.f), key = u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u);           // (upwards with the logit)
+    uint32_t lo = 0, hi = 0xffffffffu;                                             // all reach lo; fewer than k reach hi (no logit's key)
+    while (hi - lo > 1) {
+        const uint32_t mid = lo + (hi - lo) / 2;
+        const int n = __syncthreads_count(key >= mid);
+        if (n >= k) {
+            lo = mid;
+            if (n <= k + k / 16) break;
+        } else hi = mid;
     }
-    if (before == k - 1) sh.thr = mine;
-    __syncthreads();
-    return sh.thr;
+    return __uint_as_float(lo ^ ((lo >> 31) ? 0x80000000u : 0xffffffffu));
 }
 
 // ---------------------------------------------------------------- lists

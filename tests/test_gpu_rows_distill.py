@@ -233,3 +233,29 @@ def test_captured_and_replayed():
         for a, b in zip(got, (val, idx, lse, kl, ce, grad)):
             assert torch.equal(a, b)
     assert int(st.item()) == 0
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("V,K,inv_temp", [(4099, 16, 1.0), (20000, 40, 0.5), (152064, 64, 1.0), (3001, 427, 1.25)])
+def test_the_loss_of_a_draft_that_has_learned(kind, V, K, inv_temp):
+    """Small divergences, differences of sums that nearly agree."""
+    g = np.random.default_rng(V)
+    M = 9
+    t = device_rows((g.normal(size=(M, V)) * 3.0).astype(np.float32), kind)
+    z = exact_values(t)
+    teacher = z + 0.03 * g.normal(size=z.shape)
+    idx, val, t_lse = np.zeros((M, K), dtype=np.int32), np.zeros((M, K), dtype=np.float32), np.zeros(M, dtype=np.float32)
+    for r in range(M):
+        val[r], idx[r], t_lse[r] = ref.top(teacher[r], K, inv_temp)
+    kl, _, _ = loss(t, val, idx, t_lse, None, inv_temp, (1.0, 0.0))
+    for r in range(M):
+        want, _, _ = ref.distill(z[r], val[r].astype(np.float64), idx[r], float(t_lse[r]), -1, inv_temp, 1.0, 0.0)
+        s = np.exp(z[r] * inv_temp - ref.lse(z[r] * inv_temp))
+        p = np.exp(val[r].astype(np.float64) * inv_temp - float(t_lse[r]))
+        s_list = s[idx[r]].sum()
+        # kl = .. - sum p log s_k - p_rest log s_rest: the rest's sum is off by 2e-6 of itself (exponentials to 2^-22 and their arguments),
+        # which counts by s_rest - p_rest; the entries' are in 64 bits, of a temperature that 32 bits round (2^-24 of the logits' distance
+        # from the largest, by s - p); terms of up to 20 to 1e-11; one rounding of the result
+        change = np.abs(s[idx[r]] - p).sum() + abs((1 - s_list) - (1 - p.sum()))
+        far = inv_temp * (z[r].max() - z[r].min())
+        assert abs(kl[r] - want) <= 2e-6 * abs(s_list - p.sum()) + 2.0 ** -24 * far * change + 1e-9 + 2.0 ** -23 * abs(want), (r, kl[r], want)
