@@ -4,13 +4,18 @@
 // each CTA a slice of it, in pieces of 21 KB through a ring of slots.  Fourteen warps sum up the exponentials of a piece; what a row
 // needs but once is done by four more, so that it does not stand in their way:
 //   copy     issues the pieces' copies as slots become free
-//   entries  prepares the next row's list: probabilities, places in the slice
+//   entries  prepares the next rows' lists: the entries in this CTA's slice, their probabilities
 //   pick     takes the listed logits (and the label's) out of a piece that has arrived and puts minus infinity in their place: the others'
 //            sums are then those of the rest, without a question per entry (and without the cancellation of a difference)
 //   join     brings the warps' sums together, and with stores that report to a barrier the CTAs', and writes the losses
 // With the gradient a slice's pieces stay in their slots until the sums are known, the gradient is formed from there, and the next
 // row's pieces follow into the slots one by one; the listed entries' gradients (and the label's) are written over the others' afterwards.
-// (One row per cluster, all warps doing everything, a bitmap of the listed entries: 4096 rows of 152064 bf16 790 us.)
+// 1024 rows of 152064, K = 64: the loss of bf16 78 us (4.0 TB/s), of f32 118 (5.2 TB/s), loss and gradient of bf16 161 (3.9 TB/s read and
+// written), of f32 258 (4.8 TB/s).  bf16 is bound by instructions, 11 per 32 entries and pass (the exponentials' pipe at 50 %); f32 by HBM, of
+// which the time between a row's last piece and its gradient is lost.  Another temperature than 1 with a label costs a second exponential
+// per entry (bf16 115 and 235 us).
+// (One row per cluster, all warps doing everything, a bitmap of the listed entries: 4096 rows of bf16 790 us, now 640.  Every CTA preparing the
+// whole list: no slower at K = 64, but 60 % at K = 427 in short rows.  The exponentials of some entries by a polynomial: slower.)
 #include <type_traits>
 #include "rows.cuh"
 

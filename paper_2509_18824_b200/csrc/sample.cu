@@ -1,15 +1,21 @@
 // Top logits, filtered sampling and filtered logits of rows [M][V] (sd_top_logits, sd_sample_logits, sd_filter_logits).
 //
-// One cluster of `parts` CTAs per row, each with a slice of it in its shared memory (bulk copies; 152064 f32 are eight slices of
-// 76 KB, two of which share an SM): a row is read once, and passed over as often as it takes.  Which entries stay is decided on a
-// list of some hundred entries that the first CTA collects and sorts:
+// Which entries stay is decided on a list of some hundred entries that one CTA collects and sorts:
 //   top-k up to kFewK   entries that reach the k-th largest of 128 groups' largest logits
-//   other borders       histograms of the row in bins of a fraction of a factor of two below its largest logit, counts and (to 1e-4)
+//   other borders       histograms of the row in bins of a fraction of a factor of two below its largest logit, counts and (to 2e-5)
 //                       masses: the bins in which the borders lie are listed, and if there are few, all that is above them
 // With all kept entries listed, the borders are prefix lengths of the sorted list and the draws are among its entries.  Otherwise (flat
 // rows) the list gives the last entry that stays, and the mass above the listed bins is summed up, in 64 bits, chunk by chunk (32 * kU
 // consecutive vectors); a draw looks up the chunk and then the entry.  Lists that overflow (thousands of nearly equal logits) are
 // narrowed down by further histograms over the keys.
+//
+// Few rows: one cluster of up to eight CTAs per row, each with a slice of it in its shared memory (bulk copies; 152064 f32 are eight
+// slices of 76 KB, two of which share an SM), read once and passed over as often as it takes.  One such row: k = 50 13 us, any mixture
+// with top-p 42, all entries 17; latency bounds it (copy 3 us, then barriers of the cluster, sorting, the draw).
+// Many rows: passes over L2 with loads ahead in registers, a CTA or a small cluster per row.  Top logits then take one pass with the
+// log-sum-exp and one for the list: 2048 rows of 152064 bf16, K = 64 187 us, 3.3 TB/s, bound by instructions (63 % of the issue
+// slots, XU pipe 38 %) and by what follows a row's passes.  256 rows of 152064 f32: k = 50 72 us, everything 91 (its masses in 64 bits: the
+// fp64 pipe at 39 %), top-p 270 (the histograms' atomics).
 // (Lists kept in a single pass over global memory, with a threshold that rises, took three times as long: their cutting and their
 // barriers, 12 of 30 us for one row, and for flat rows four passes through L2.)
 #include <limits.h>
