@@ -508,7 +508,7 @@ sd_status sd_top_logits(const void *logits, int32_t dtype, int64_t ld, int32_t M
  *   probs     : dev f32 [M][V] or NULL: p of the whole row (sd_accept_tree_sampled_q's q_rows); not `logits`
  *   lse       : dev f32 [M] or NULL: log of the mass that stays
  *   1 <= N <= 64
- * An inv_temp below 1e-6 or NaN stores SD_ERR_INVALID_ARG (the row counts as masked).  Masses and their sums are held in 64 bits,
+ * An inv_temp below 1e-6 or NaN, or a logit of plus infinity, stores SD_ERR_INVALID_ARG (the row counts as masked).  Masses and their sums are held in 64 bits,
  * so that borders and draws are those of exact arithmetic but for sums within about 1e-10 of a border.  Scaled logits beyond
  * 2^29 count as 2^29.
  */
@@ -525,7 +525,7 @@ sd_status sd_sample_logits(const void *logits, int32_t dtype, int64_t ld, int32_
  *   lse  : dev f32 [M]: log sum exp of out's row (minus infinity if nothing is unmasked)
  *   kept : dev int32 [M] or NULL: how many entries stay
  * out and lse are what sd_accept_tree_sampled_q and sd_accept_chain_sampled take as logits and lse, with inv_temp = 1 there: the
- * temperatures, which may differ from row to row, are in them.  (An infinite inv_temp scales by 1.)
+ * temperatures, which may differ from row to row, are in them.  (An infinite inv_temp scales by 1.)  Errors as sd_sample_logits.
  */
 sd_status sd_filter_logits(const void *logits, int32_t dtype, int64_t ld, int32_t M, int32_t V,
                            const sd_sampling *how, float *out, float *lse, int32_t *kept,

@@ -1183,7 +1183,7 @@ sample_kernel(SampleCall a) {
     int k = a.top_k ? a.top_k[r] : 0;
     float p = a.top_p ? a.top_p[r] : 1.f;
     float mp = a.min_p ? a.min_p[r] : 0.f;
-    const bool bad = !(it >= 1e-6f);
+    bool bad = !(it >= 1e-6f);
     if (bad || it > 3.4e38f) { if (!bad) k = 1; it = 1.f; }                        // infinite: the first entry alone
     if (k >= V) k = 0;
     const bool by_k = k >= 1, by_p = p < 1.f, by_mp = mp > 0.f;
@@ -1196,7 +1196,9 @@ sample_kernel(SampleCall a) {
     const bool all_stay = !by_k && !by_p && !by_mp;
     const bool ok = all_stay ? sum_all(sh, sl, sc, a.wait_cycles) : first_pass<false>(sh, sl, 0.f, a.wait_cycles);
     sync_parts(parts);
-    const float top = bad ? -INFINITY : top_of_parts(sh, parts);
+    float top = top_of_parts(sh, parts);
+    bad = bad || top == INFINITY;                                                  // (no distribution)
+    if (bad) top = -INFINITY;
     const int ref = top > -INFINITY ? sc.whole(top) : 0;
     const double top_mass = sc.mass(top, ref), least = (double)mp * top_mass;
     float* dense = a.dense ? a.dense + r * (long long)V : nullptr;
@@ -1409,6 +1411,11 @@ sample_kernel(SampleCall a) {
                 }
                 // the other CTAs' parts of the output are filled, and they are not needed any more
                 sync_parts(parts);
+                if (n == 0) {                                                      // (a slice that did not come: what follows needs an entry)
+                    if (tid == 0) sh.list[0] = order_key(top, 0);
+                    n = 1;
+                    __syncthreads();
+                }
                 n = sort_list(sh, sh.list, n, by_k ? min(k, kListMax) : kListMax);
                 for (int i = tid; i < n; i += kThreads) sh.all[i] = sc.mass(key_logit(sh.list[i]), ref);
                 block_scan(sh.all, n, sh.tmp_d);

@@ -6,8 +6,8 @@ import torch
 
 from oracle import rows as ref
 from paper_2509_18824_b200 import binding as sd
-from rows_util import device_rows
-from test_gpu_rows_sampling import batch, check, filtered, parameters, sample, top
+from rows_util import margin
+from test_gpu_rows_sampling import BORDER, batch, check, filtered, of_row, parameters, sample, top
 
 pytestmark = pytest.mark.gpu
 
@@ -167,3 +167,63 @@ def test_a_copy_that_does_not_come_is_reported(monkeypatch):
     monkeypatch.delenv("SDV_TEST_WITHHOLD")
     monkeypatch.delenv("SDV_TEST_WAIT_CYCLES")
     check(t, x, params, 9, N=1)
+
+
+@pytest.mark.parametrize("M,V", [(6, 30000), (45, 100003)])
+def test_rows_with_infinity_are_reported_and_the_others_drawn(M, V):
+    t, x = batch(M, V, "f32", 13, patterns=("bulk", "peaks", "flat"))
+    t[1, 17] = np.inf
+    t[2, V - 1] = np.inf
+    t[2, 5] = np.inf
+    for which in ("kpm", "k", "p", "m", ""):
+        params = parameters(M, V, 13, which)
+        u = np.random.default_rng(1).random((M, 2)).astype(np.float32)
+        tokens, prob, dense, lse, st = sample(t, params, u)
+        out, flse, kept, fst = filtered(t, params)
+        assert st == sd.SD_ERR_INVALID_ARG and fst == sd.SD_ERR_INVALID_ARG
+        assert (tokens[1:3] == -1).all() and (prob[1:3] == 0).all() and (dense[1:3] == 0).all() and np.isneginf(lse[1:3]).all()
+        assert np.isneginf(out[1:3]).all() and np.isneginf(flse[1:3]).all() and (kept[1:3] == 0).all()
+        rest = [r for r in range(M) if r not in (1, 2)]
+        for r in rest:
+            how = of_row(params, r)
+            if margin(x[r], **how) < BORDER:
+                continue
+            assert kept[r] == ref.keep(x[r], **how)[0].size
+            assert (tokens[r] >= 0).all() and np.isfinite(out[r, tokens[r]]).all()
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_rows_beyond_offsets_of_32_bits(kind):
+    """The last rows of 2.3e9 logits end as they do in a call of their own (distillation: to its roundings)."""
+    M, V, n, K = 15200, 152064, 8, 16
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    t = torch.empty((M, V), dtype=torch.float32 if kind == "f32" else torch.bfloat16, device="cuda")
+    t[:1000].normal_(generator=g)
+    for at in range(1000, M, 1000):
+        t[at:at + 1000] = t[:min(1000, M - at)]
+    t[-n:].normal_(generator=g)
+    tail = t[-n:].clone()
+    f, i = (lambda *s: torch.zeros(s, device="cuda")), (lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda"))
+    res = []
+    for x in (t, tail):
+        rows = x.shape[0]
+        st = sd.new_status()
+        values, index, tokens, out, flse, kept, kl, ce = f(rows, K), i(rows, K), i(rows, 1), f(rows, V), f(rows), i(rows), f(rows), f(rows)
+        u = torch.full((rows, 1), 0.37, device="cuda")
+        how = sd.Sampling(None, torch.full((rows,), 40), None, None)
+        sd.sd_top_logits(x, 1.0, values, index, None, st)
+        sd.sd_sample_logits(x, how, u, tokens, None, None, None, st)
+        sd.sd_filter_logits(x, how, out, flse, kept, st)
+        grad = torch.zeros_like(x)
+        sd.sd_distill_loss(x, values, index, None, index[:, 3].contiguous(), 1.0, 1.0, 0.5, kl, ce, None, None, grad, st)
+        torch.cuda.synchronize()
+        assert int(st.item()) == 0
+        res.append([a[-n:].clone() for a in (values, index, tokens, out, kept, kl, ce, grad.float())])
+        del out, grad
+    for a, b in zip(res[0][:5], res[1][:5]):
+        assert torch.equal(a, b)
+    # two orders of summing 152064 exponentials in 32 bits, then (bf16) a rounding of the gradient each
+    for a, b in zip(res[0][5:7], res[1][5:7]):
+        assert (a - b).abs().max() <= 4e-6 + 2.0 ** -22 * b.abs().max()
+    assert ((res[0][7] - res[1][7]).abs() <= 8e-6 * (res[1][7].abs() + 1e-3) + (2.0 ** -7 * res[1][7].abs() if kind == "bf16" else 0)).all()
