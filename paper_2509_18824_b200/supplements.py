@@ -2,7 +2,7 @@
 the LM head at several row counts, and the bandwidth-regime cases (chain
 decoding, a compaction stress shape).  One JSON line per measurement.
 
-    python -m paper_2509_18824_b200.supplements [attention] [attention_layers] [lmhead] [lmhead480] [sampled] [draft] [compact]
+    python -m paper_2509_18824_b200.supplements [attention] [attention_layers] [lmhead] [lmhead480] [sampled] [draft] [compact] [rows]
                                                 [chain8] [compact512]        (small cases for profiler captures)
 
 Timing: CUDA events on the launching stream, >= 3 warm-up calls, inputs rotated
@@ -248,6 +248,41 @@ def draft(S=4096, L=28, Q=4, H=28):
                           "frac_hbm_nominal_8TBs": nbytes / ms / 1e6 / 8000.0, "bytes": nbytes, "peaks": src}))
 
 
+def rows(M=480, V=152064, K=64, train=4096):
+    """The calls on rows of logits: the verify step's 480 rows (and one) of the LM head's f32, a training step's 4096 of bf16."""
+    hbm, _, src = _peaks()
+    g = torch.Generator(device="cuda"); g.manual_seed(0)
+    f, i = (lambda *s: torch.empty(s, device="cuda")), (lambda *s: torch.empty(s, dtype=torch.int32, device="cuda"))
+    st = sd.new_status()
+
+    def report(call, workload, ms, nbytes):
+        print(json.dumps({"call": call, "workload": workload, "us": ms * 1e3, "gbs": nbytes / ms / 1e6,
+                          "frac_hbm": nbytes / ms / 1e6 / hbm, "bytes": nbytes, "peaks": src, "status": int(st.item())}))
+
+    for m in (1, M):
+        x = torch.randn((m, V), device="cuda", generator=g) * 2.5
+        one = lambda a, t=torch.float32: torch.full((m,), a, dtype=t, device="cuda")
+        u = torch.rand((m, 1), device="cuda", generator=g).clamp_(max=0.9999999)
+        tokens, prob, out, lse = i(m, 1), f(m, 1), f(m, V), f(m)
+        for name, how in (("top-k 50, top-p 0.95", sd.Sampling(one(1.1), one(50, torch.int32), one(0.95))), ("top-p 0.9", sd.Sampling(None, None, one(0.9))),
+                          ("min-p 0.05", sd.Sampling(None, None, None, one(0.05))), ("all entries", sd.Sampling(one(1.0)))):
+            report("sd_sample_logits", f"{m} x {V} f32, {name}",
+                   _time(lambda: sd.sd_sample_logits(x, how, u, tokens, prob, None, lse, st), 10), m * V * 4)
+            report("sd_filter_logits", f"{m} x {V} f32, {name}",
+                   _time(lambda: sd.sd_filter_logits(x, how, out, lse, None, st), 10), m * V * 8)
+        del x, out
+    t, x = ((torch.randn((train, V), device="cuda", generator=g) * 2.5).bfloat16() for _ in range(2))
+    val, idx, t_lse, kl, ce, stats, grad = f(train, K), i(train, K), f(train), f(train), f(train), f(train, 4), torch.empty_like(x)
+    nbytes = train * V * 2
+    report("sd_top_logits", f"{train} x {V} bf16, K = {K}", _time(lambda: sd.sd_top_logits(t, 1.0, val, idx, t_lse, st), 10), nbytes)
+    label = idx[:, 0].contiguous()
+    args = (x, val, idx, t_lse, label, 1.0, 1.0, 0.1)
+    report("sd_distill_loss", f"{train} x {V} bf16, K = {K}", _time(lambda: sd.sd_distill_loss(*args, kl, ce, stats, None, None, st), 10), nbytes)
+    report("sd_distill_grad", f"{train} x {V} bf16, K = {K}", _time(lambda: sd.sd_distill_grad(*args, stats, None, grad, st), 10), 2 * nbytes)
+    report("sd_distill_loss", f"{train} x {V} bf16, K = {K}, with its gradient",
+           _time(lambda: sd.sd_distill_loss(*args, kl, ce, None, None, grad, st), 10), 2 * nbytes)
+
+
 def compact(**kw):
     print(json.dumps(measure_compact(**kw)))
 
@@ -282,7 +317,7 @@ def measure_compact(B=1024, L=8, T=64, Hkv=4, D=128):
 
 
 if __name__ == "__main__":
-    what = sys.argv[1:] or ["attention", "attention_layers", "lmhead", "sampled", "draft", "compact"]
+    what = sys.argv[1:] or ["attention", "attention_layers", "lmhead", "sampled", "draft", "compact", "rows"]
     if "attention" in what:
         attention()
     if "attention_layers" in what:
@@ -299,6 +334,8 @@ if __name__ == "__main__":
         draft()
     if "compact" in what:
         compact()
+    if "rows" in what:
+        rows()
     if "chain8" in what:                   # chain decoding, 8 layers in one call (0.55 GB of K/V)
         for r in measure_attention_layers(("chain11",), L=8, reps=3):
             print(json.dumps(r))
