@@ -633,7 +633,7 @@ __device__ __forceinline__ float log_sum(float top, float inv_temp, float s) {
     return (float)(fmin(fmax((double)top * (double)inv_temp, -3.4028234663852886e38), 3.4028234663852886e38) + log((double)s));
 }
 
-template <typename T>
+template <typename T, bool HELD>
 __global__ void __launch_bounds__(kThreads, 2)
 top_kernel(const void* logits, long long ld, int V, int parts, int K, float inv_temp, float* values, int32_t* index, float* lse, int32_t* status,
            int withheld, long long wait_cycles) {
@@ -649,8 +649,8 @@ top_kernel(const void* logits, long long ld, int V, int parts, int K, float inv_
     begin_dependent(logits, values, index, lse, status);
     const long long r = blockIdx.x / parts;
     const int rank = parts == 1 ? 0 : (int)sm100::cluster_ctarank();
-    const Slice<T, true> sl(logits, ld, r, V, parts, rank, data);
-    sl.copy(sh, withheld);
+    const Slice<T, HELD> sl(logits, ld, r, V, parts, rank, data);
+    if constexpr (HELD) sl.copy(sh, withheld);
     __syncthreads();
     const float c = inv_temp * kLog2e;
     const bool ok = first_pass<true>(sh, sl, c, wait_cycles);
@@ -1564,6 +1564,10 @@ sample_kernel(SampleCall a) {
     if (!ok) { set_status(a.status, SD_ERR_TIMEOUT); sm100::unwind_pause(); }
 }
 
+// A row's shares where it lies in memory: as many as still run at once, and two where rows differ in what they ask for (256 rows, all
+// kinds mixed: 235 us in one, 199 in two, 209 in four; 2048 rows: 920, 1026, 1309 us).
+static int shares_of(int M, int sms) { return 4LL * M <= 2 * sms ? 4 : M <= 2 * sms ? 2 : 1; }
+
 // CTAs per row: slices of at most 80 KB while eight are enough for that, and more of them while all run at once, two on an SM, and a warp's
 // lanes have a vector each (80 rows of 32003 bf16, top-p: 79 us in one, 60 in two)
 static int parts_for(int M, int nvec, int sms) {
@@ -1582,13 +1586,22 @@ sd_status launch_top_logits(const void* logits, int dtype, long long ld, int M, 
     if (cudaGetDevice(&dev) != cudaSuccess) return SD_ERR_CUDA;
     const int nvec = (int)(((long long)V * (dtype == SD_F32 ? 4 : 2) + 15) / 16) + 1;
     const TestKnobs knobs = test_knobs();
-    if (K <= kSomeK && M >= sm_count(dev) / 2) {
+    const int sms = sm_count(dev), fit = parts_for(M, nvec, sms);
+    // (GPCs whose SMs are no multiple of a cluster's leave some: 33 clusters of eight run at once, 71 of four)
+    const bool all_at_once = (long long)M * fit <= 2 * sms - 32;
+    if (K <= kSomeK && (M >= sms / 2 || !all_at_once)) {
         auto kern = dtype == SD_F32 ? top_stream_kernel<float> : top_stream_kernel<uint16_t>;
-        const int ctas = 2 * sm_count(dev), steps = (nvec + kWarps * kStreamVecs - 1) / (kWarps * kStreamVecs);
-        return launch_dependent(kern, dim3((unsigned)(M < ctas ? M : ctas)), kThreads, 0, 1, st, logits, ld, V, M, steps, K, inv_temp, values, index, lse);
+        // (up to one row per SM: so much shared memory that no SM takes two; 80 rows of f32 27 -> 20 us)
+        const int ctas = 2 * sms, steps = (nvec + kWarps * kStreamVecs - 1) / (kWarps * kStreamVecs), alone = M <= sms ? 96 * 1024 : 0;
+        if (!allow_dynamic_smem(kern, 96 * 1024)) return SD_ERR_CUDA;
+        return launch_dependent(kern, dim3((unsigned)(M < ctas ? M : ctas)), kThreads, alone, 1, st, logits, ld, V, M, steps, K, inv_temp, values, index, lse);
     }
-    const int parts = parts_for(M, nvec, sm_count(dev)), smem = (nvec + parts - 1) / parts * 16;
-    auto kern = dtype == SD_F32 ? top_kernel<float> : top_kernel<uint16_t>;
+    // (long lists: as sampled rows, below; K = 1000 of 148 rows of 152064 f32 136 -> 76 us, of 2048 1697 -> 950)
+    const bool held = nvec <= 5120 || all_at_once;
+    const int parts = held ? fit : shares_of(M, sms);
+    const int smem = held ? (nvec + parts - 1) / parts * 16 : kCopies * kBins * 4 + kBins * 8;
+    auto kern = dtype == SD_F32 ? (held ? top_kernel<float, true> : top_kernel<float, false>)
+                                : (held ? top_kernel<uint16_t, true> : top_kernel<uint16_t, false>);
     if (!allow_dynamic_smem(kern, smem)) return SD_ERR_CUDA;
     return launch_dependent(kern, dim3((unsigned)M * parts), kThreads, smem, parts, st, logits, ld, V, parts, K, inv_temp, values, index, lse, dev_status,
                             knobs.withhold ? 16 : 0, knobs.wait_cycles);
@@ -1601,12 +1614,10 @@ sd_status launch_sample(const void* logits, int dtype, long long ld, int M, int 
     const int nvec = (int)(((long long)V * (dtype == SD_F32 ? 4 : 2) + 15) / 16) + 1;
     // One reading into shared memory where the SMs hold all clusters at once (and where one CTA holds a row).  Beyond that the waves of
     // clusters wait for their own copies, and passes through L2 by CTAs of which two are resident are faster.  152064 f32, k = 50 / top_p:
-    // 64 rows 36 -> 21 / 108 -> 90 us, 256 rows 101 -> 72 / 368 -> 270 us; 32 rows are as fast, but 57 -> 88 us.  A row's shares: as many
-    // as still run at once, and two where rows differ in what they ask for (256 rows, all kinds mixed: 235 us in one, 199 in two, 209 in
-    // four; 2048 rows: 920, 1026, 1309 us).
+    // 64 rows 36 -> 21 / 108 -> 90 us, 256 rows 101 -> 72 / 368 -> 270 us; 32 rows are as fast, but 57 -> 88 us.
     const int fit = parts_for(M, nvec, sm_count(dev)), sms = sm_count(dev);
     const bool held = nvec <= 5120 || (long long)M * fit <= 2 * sms;
-    const int parts = held ? fit : 4LL * M <= 2 * sms ? 4 : M <= 2 * sms ? 2 : 1;
+    const int parts = held ? fit : shares_of(M, sms);
     const int smem = held ? (nvec + parts - 1) / parts * 16 : kCopies * kBins * 4 + kBins * 8;
     auto kern = dtype == SD_F32 ? (held ? sample_kernel<float, true> : sample_kernel<float, false>)
                                 : (held ? sample_kernel<uint16_t, true> : sample_kernel<uint16_t, false>);
