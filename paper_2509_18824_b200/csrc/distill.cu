@@ -75,7 +75,7 @@ struct DistillShared {
     RowInfo info[kMaxLists];
     float label_z[kMaxLists];
     int dup[kMaxLists], label_listed[kMaxLists];
-    float4 sums[2][kSumWarps + 1];     // the warps' (largest logit, sum outside the entries, 0, sum at temperature 1); the entries' (largest logit, 0, 0, sum at temperature 1)
+    float4 sums[2][kSumWarps + 1];     // the warps' (largest logit, sum outside the entries, 0, sum at temperature 1); the entries' last
     double part[2], listed[2];         // sum of p z; the listed entries' sum of 2^(z c - R)
     Message msg[2][8];
     RowFactors row[2];
@@ -211,7 +211,8 @@ __device__ __forceinline__ void each_entry(int count, F f) {
 // By one warp: the entries of row r that lie in the slice (every CTA takes its own, and the join brings their sums together).  Without
 // top_lse their p are relative to the row's first one until then (in a launch for the gradient alone, where 32 bits do for p, at once).
 template <typename T, int MODE>
-__device__ __forceinline__ void prepare_entries(RowInfo& info, const Lists& li, const DistillCall& a, long long r, const RawList& raw, const SliceOf<T>& sl, bool report) {
+__device__ __forceinline__ void prepare_entries(RowInfo& info, const Lists& li, const DistillCall& a, long long r, const RawList& raw,
+                                                const SliceOf<T>& sl, bool report) {
     const int lane = threadIdx.x & 31;
     const int count = (sl.v1 - sl.v0) * SliceOf<T>::E;
     raw.stage(li, a.K);
@@ -286,7 +287,11 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
     if (tid == 0) {
         sh.abort_flag = 0;
         for (int q = 0; q < slots; ++q) { mbar_init(&sh.full[q], 1); mbar_init(&sh.picked[q], 1); mbar_init(&sh.free_[q], kSumWarps); }
-        for (int q = 0; q < kMaxLists; ++q) { mbar_init(&sh.info_full[q], 1); mbar_init(&sh.info_free[q], kSumWarps + 1 + (MODE != kGrad)); mbar_init(&sh.sums_full[q], MODE == kGrad ? 1 : kSumWarps + 1); }
+        for (int q = 0; q < kMaxLists; ++q) {
+            mbar_init(&sh.info_full[q], 1);
+            mbar_init(&sh.info_free[q], kSumWarps + 1 + (MODE != kGrad));
+            mbar_init(&sh.sums_full[q], MODE == kGrad ? 1 : kSumWarps + 1);
+        }
         for (int q = 0; q < 2; ++q) { mbar_init(&sh.told[q], 1); mbar_init(&sh.row_ready[q], 1); }
         fence_barrier_init();
     }
@@ -480,7 +485,8 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
         for (long long r = start; r < units && ok; r += step, ++n) {
             const int b = list_of(n), h = (int)(n & 1);
             const uint32_t ph = (uint32_t)((n >> 1) & 1);
-            ok = mbar_wait_warp(&sh.info_full[b], phase_of(n), &sh.abort_flag, wait_cycles) && mbar_wait_warp(&sh.sums_full[b], phase_of(n), &sh.abort_flag, wait_cycles);
+            ok = mbar_wait_warp(&sh.info_full[b], phase_of(n), &sh.abort_flag, wait_cycles) &&
+                 mbar_wait_warp(&sh.sums_full[b], phase_of(n), &sh.abort_flag, wait_cycles);
             if (!ok) break;
             const RowInfo& info = sh.info[b];
             const int label = info.label;
@@ -499,8 +505,11 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
                 } else if (lane < parts) {
                     const uint32_t to = map_dsmem(smem_u32(&sh.msg[h][rank]), lane), bar = map_dsmem(smem_u32(&sh.told[h]), lane);
                     st_async_v4(to, __float_as_uint(most), __float_as_uint(label_z), __float_as_uint(rest), __float_as_uint(sum1), bar);
-                    st_async_v4(to + 16, (uint32_t)__double2loint(listed), (uint32_t)__double2hiint(listed), (uint32_t)__double2loint(entries), (uint32_t)__double2hiint(entries), bar);
-                    st_async_v4(to + 32, (uint32_t)__double2loint(mass), (uint32_t)__double2hiint(mass), (uint32_t)__double2loint(plogp), (uint32_t)__double2hiint(plogp), bar);
+                    const auto two_doubles = [&](uint32_t at, double x, double y) {
+                        st_async_v4(at, (uint32_t)__double2loint(x), (uint32_t)__double2hiint(x), (uint32_t)__double2loint(y), (uint32_t)__double2hiint(y), bar);
+                    };
+                    two_doubles(to + 16, listed, entries);
+                    two_doubles(to + 32, mass, plogp);
                 }
                 ok = mbar_wait_cluster(&sh.told[h], ph, &sh.abort_flag, wait_cycles);
                 ok = __all_sync(0xffffffffu, ok);

@@ -513,9 +513,10 @@ __device__ __noinline__ void bin_entries(RowShared& sh, const Slice<T, HELD> sl,
 }
 
 // Counts or masses (or both) of the row's bins, in every CTA: all_count and all, inclusive sums that begin with the given ones; masses
-// as multiples of the largest entry's.  Without counts, all_count is what the masses allow at most.  A bin's mass is summed up in units of 2^-16 of its upper end, in 32 bits (a slice in
-// shared memory has at most 40960 entries; a row elsewhere has kCopies sums for each bin, and two warps' 32784 entries in each): to 2e-5 of it.  (The last coarse bin has none.)  Every CTA adds up its share of the bins over the parts
-// and hands it to all.
+// as multiples of the largest entry's.  Without counts, all_count is what the masses allow at most.  A bin's mass is summed up in units
+// of 2^-16 of its upper end, in 32 bits, to 2e-5 of it: a slice in shared memory has at most 40960 entries; a row elsewhere has kCopies sums
+// for each bin, and two warps' 32784 entries in each.  (The last coarse bin has none.)  Every CTA adds up its share of the bins over the
+// parts and hands it to all.
 template <typename T, bool HELD>
 __device__ void fill_bins(RowShared& sh, const Slice<T, HELD>& sl, bool counts, bool masses, const LinearBins& lin, uint32_t count0, double mass0) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -734,7 +735,8 @@ top_kernel(const void* logits, long long ld, int V, int parts, int K, float inv_
 // Where there are enough rows to fill the GPU, a CTA takes one at a time, twice over: first for the groups' largest logits and the
 // sum, then, mostly from L2, for the entries that reach the threshold.  Every warp has a sixteenth of the row and loads four vectors per
 // lane ahead of those that it works on, the next pass's and row's first ones too: no warp waits for another within a pass.  (Clusters
-// that hold a row in shared memory, 4096 rows of 152064 bf16: 740 us; a ring of copies for all warps of a CTA 580; one for every warp 850.)
+// that hold a row in shared memory, 4096 rows of 152064 bf16: 740 us; a ring of copies for all warps of a CTA 580; one for every warp 850;
+// so 370.)
 constexpr int kStreamLane = 4;                     // vectors per lane and step
 constexpr int kStreamVecs = kStreamLane * 32;
 
@@ -1366,7 +1368,8 @@ sample_kernel(SampleCall a) {
                                 for (int i = tid; i < stays; i += kThreads) {
                                     const int id = sl.chunk_of(key_index(sh.list[i]));
                                     if (id >= 0 && id < chunks)
-                                        atomicAdd(reinterpret_cast<unsigned long long*>(&sh.other[id]), (unsigned long long)(sc.mass(key_logit(sh.list[i]), ref) * kUnit + 0.5));
+                                        atomicAdd(reinterpret_cast<unsigned long long*>(&sh.other[id]),
+                                                  (unsigned long long)(sc.mass(key_logit(sh.list[i]), ref) * kUnit + 0.5));
                                     else set_status(a.status, SD_ERR_BOUNDS);
                                 }
                                 __syncthreads();
@@ -1377,7 +1380,7 @@ sample_kernel(SampleCall a) {
                         }
                         sync_parts(parts);
                         border = *of_rank(&sh.border, 0);
-                                        total = *of_rank(&sh.total, 0);
+                        total = *of_rank(&sh.total, 0);
                         kind = -1;                                                 // (done: borders, count and mass are known)
                     } else {
                         // more than a list holds in the borders' bins
@@ -1538,7 +1541,8 @@ sample_kernel(SampleCall a) {
                     if (v >= 0 && v + E <= V) {
 #pragma unroll
                         for (int e = 0; e < E; e += 4)
-                            __stcs(reinterpret_cast<float4*>(dense + v + e), make_float4(value(x[e], v + e), value(x[e + 1], v + e + 1), value(x[e + 2], v + e + 2), value(x[e + 3], v + e + 3)));
+                            __stcs(reinterpret_cast<float4*>(dense + v + e), make_float4(value(x[e], v + e), value(x[e + 1], v + e + 1),
+                                                                                         value(x[e + 2], v + e + 2), value(x[e + 3], v + e + 3)));
                     } else {
 #pragma unroll
                         for (int e = 0; e < E; ++e)
