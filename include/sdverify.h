@@ -95,7 +95,7 @@ typedef enum { SD_F32 = 0, SD_BF16 = 1 } sd_dtype;
 
 /* Sampling parameters of M rows; every pointer is a dev array [M] or NULL (nobody uses it). */
 typedef struct {
-    const float *inv_temp;       /* 1 / temperature, at least 1e-6; +infinity: the first entry alone (NULL: 1) */
+    const float *inv_temp;       /* 1 / temperature, at least 1e-6; above 1e30: the first entry alone (NULL: 1) */
     const int32_t *top_k;        /* the k first entries; below 1 or above V - 1: all                           */
     const float *top_p;          /* shortest prefix with this share of their mass; 1 and above: all            */
     const float *min_p;          /* entries with this share of the largest probability; 0 and below: all       */
@@ -509,8 +509,7 @@ sd_status sd_top_logits(const void *logits, int32_t dtype, int64_t ld, int32_t M
  *   lse       : dev f32 [M] or NULL: log of the mass that stays
  *   1 <= N <= 64
  * An inv_temp below 1e-6 or NaN, or a logit of plus infinity, stores SD_ERR_INVALID_ARG (the row counts as masked).  Masses and their sums are held in 64 bits,
- * so that borders and draws are those of exact arithmetic but for sums within about 1e-10 of a border.  Scaled logits beyond
- * 2^29 count as 2^29.
+ * so that borders and draws are those of exact arithmetic but for sums within about 1e-10 of a border.
  */
 sd_status sd_sample_logits(const void *logits, int32_t dtype, int64_t ld, int32_t M, int32_t V,
                            const sd_sampling *how, const float *u, int32_t N,
@@ -525,7 +524,7 @@ sd_status sd_sample_logits(const void *logits, int32_t dtype, int64_t ld, int32_
  *   lse  : dev f32 [M]: log sum exp of out's row (minus infinity if nothing is unmasked)
  *   kept : dev int32 [M] or NULL: how many entries stay
  * out and lse are what sd_accept_tree_sampled_q and sd_accept_chain_sampled take as logits and lse, with inv_temp = 1 there: the
- * temperatures, which may differ from row to row, are in them.  (An infinite inv_temp scales by 1.)  Errors as sd_sample_logits.
+ * temperatures, which may differ from row to row, are in them.  (An inv_temp above 1e30 scales by 1.)  Errors as sd_sample_logits.
  */
 sd_status sd_filter_logits(const void *logits, int32_t dtype, int64_t ld, int32_t M, int32_t V,
                            const sd_sampling *how, float *out, float *lse, int32_t *kept,

@@ -32,7 +32,7 @@ def top(x: np.ndarray, K: int, inv_temp: float):
 
 def keep(x: np.ndarray, inv_temp: float = 1.0, top_k: int = 0, top_p: float = 1.0, min_p: float = 0.0):
     """(kept indices in order, scaled logits z [V]): top-k, then top-p of their mass, then min-p of the largest probability."""
-    if np.isinf(inv_temp):
+    if inv_temp > np.float32(1e30):                           # the first entry alone
         inv_temp, top_k = 1.0, 1
     z = np.where(x > -np.inf, np.clip(x * inv_temp, -F32_MAX, F32_MAX), -np.inf)
     o = in_order(x)

@@ -133,14 +133,17 @@ struct Row {
 // mass(x) = 2^(x c - ref) with c = inv_temp log2 e and a whole number ref, in 64 bits: which token a uniform number falls on, and
 // where a sum passes top_p of another, must not depend on the rounding of single masses (with 2^-24 in each of 152064 equal masses
 // one draw in forty thousand would).  2^f for |f| <= 1/2 is its Taylor series up to f^9 (the rest is below 7e-12 of it); ref
-// being whole, sums taken with different ones are brought together exactly.  Scaled logits beyond 2^29 count as 2^29.
+// being whole, sums taken with different ones are brought together exactly. (So far as they stay below
+// 2^28: beyond, logits are taken relative to the largest one.)
 struct Scale {
     double c;
-    float lim;
-    __device__ __forceinline__ explicit Scale(float inv_temp) : c((double)inv_temp * 1.4426950408889634073599) {
+    float lim, base;                   // base: what logits are relative to
+    __device__ __forceinline__ explicit Scale(float inv_temp) : c((double)inv_temp * 1.4426950408889634073599), base(0.f) {
         lim = (float)fmin(536870912.0 / c, 3.4028234663852886e38);
     }
-    __device__ __forceinline__ double clamped(float x) const { return __dmul_rn((double)fminf(fmaxf(x, -lim), lim), c); }
+    __device__ __forceinline__ double clamped(float x) const { return __dmul_rn((double)fminf(fmaxf(__fsub_rn(x, base), -lim), lim), c); }
+    // Where exponents would leave 2^28, logits count from the largest one.  (Differences of nearby ones are exact, the others' masses 0.)
+    __device__ __forceinline__ void from(float top) { base = fabs((double)top * c) > 268435456.0 ? top : 0.f; }
     __device__ __forceinline__ int whole(float x) const { return __double2int_rn(clamped(x)); }
     // N masses side by side: their chains of multiply-adds hide one another's latency
     template <int N>

@@ -1186,21 +1186,23 @@ sample_kernel(SampleCall a) {
     float p = a.top_p ? a.top_p[r] : 1.f;
     float mp = a.min_p ? a.min_p[r] : 0.f;
     bool bad = !(it >= 1e-6f);
-    if (bad || it > 3.4e38f) { if (!bad) k = 1; it = 1.f; }                        // infinite: the first entry alone
+    if (bad || it > 1e30f) { if (!bad) k = 1; it = 1.f; }                          // infinite: the first entry alone
     if (k >= V) k = 0;
     const bool by_k = k >= 1, by_p = p < 1.f, by_mp = mp > 0.f;
     p = fmaxf(p, 0.f);
     mp = by_mp ? fminf(mp, 1.f) : 0.f;
     if (tid < a.N) sh.u[tid] = a.u[r * a.N + tid];
-    const Scale sc(it);
+    Scale sc(it);
     __syncthreads();
 
-    const bool all_stay = !by_k && !by_p && !by_mp;
+    bool all_stay = !by_k && !by_p && !by_mp;
     const bool ok = all_stay ? sum_all(sh, sl, sc, a.wait_cycles) : first_pass<false>(sh, sl, 0.f, a.wait_cycles);
     sync_parts(parts);
     float top = top_of_parts(sh, parts);
     bad = bad || top == INFINITY;                                                  // (no distribution)
     if (bad) top = -INFINITY;
+    if (top > -INFINITY) sc.from(top);
+    if (sc.base != 0.f) all_stay = false;                                          // (its sums are with another base)
     const int ref = top > -INFINITY ? sc.whole(top) : 0;
     const double top_mass = sc.mass(top, ref), least = (double)mp * top_mass;
     float* dense = a.dense ? a.dense + r * (long long)V : nullptr;
@@ -1521,7 +1523,7 @@ sample_kernel(SampleCall a) {
             }
         }
         if (dense) {
-            const float c32 = (float)sc.c, at_top = (float)(top_mass / total);
+            const float c32 = (float)fmin(sc.c, 3.4028234663852886e38), at_top = (float)(top_mass / total);
             constexpr int E = Row<T>::kE;
             // the borders as logits; masses are compared where the distance in 32 bits leaves them open
             const float border_at = border == ~0ull ? -INFINITY : key_logit(border);

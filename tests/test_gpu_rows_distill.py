@@ -1,4 +1,4 @@
-"""GPU: the draft's training loss and its gradient against the 64-bit checker."""
+"""GPU: the draft's training loss and its gradient against the 64-bit oracle."""
 import os
 
 import numpy as np

@@ -6,7 +6,7 @@ import torch
 
 from oracle import rows as ref
 from paper_2509_18824_b200 import binding as sd
-from rows_util import margin
+from rows_util import LOWEST, margin
 from test_gpu_rows_sampling import BORDER, batch, check, filtered, of_row, parameters, sample, top
 
 pytestmark = pytest.mark.gpu
@@ -227,3 +227,44 @@ def test_rows_beyond_offsets_of_32_bits(kind):
     for a, b in zip(res[0][5:7], res[1][5:7]):
         assert (a - b).abs().max() <= 4e-6 + 2.0 ** -22 * b.abs().max()
     assert ((res[0][7] - res[1][7]).abs() <= 8e-6 * (res[1][7].abs() + 1e-3) + (2.0 ** -7 * res[1][7].abs() if kind == "bf16" else 0)).all()
+
+
+@pytest.mark.parametrize("M,V", [(12, 20000), (45, 100003), (320, 20600)])
+@pytest.mark.parametrize("which", ["kpm", "p", "m", ""])
+def test_extreme_temperatures_and_logits(M, V, which):
+    """Exponents far beyond what a mass can have, in every part of the range: distributions of the nearest ones, or flat ones."""
+    t, _ = batch(M, V, "f32", 31, patterns=("bulk", "peaks", "equal", "lowest", "all_lowest"))
+    it, k, p, mp = parameters(M, V, 31, which)
+    it = np.resize(np.array([1e-6, 1.0, 1e5, 1e9, 1e30, 3e38, np.inf], dtype=np.float32), M)
+    scale = np.resize(np.array([1.0, 1e6, 1e30], dtype=np.float32), M)
+    x = t.cpu().numpy()
+    with np.errstate(over="ignore"):
+        x = np.clip(x * scale[:, None], LOWEST["f32"], -LOWEST["f32"])
+    t.copy_(torch.from_numpy(x))
+    x = x.astype(np.float64)
+    u = np.random.default_rng(5).random((M, 2)).astype(np.float32)
+    tokens, prob, dense, lse, st = sample(t, (it, k, p, mp), u)
+    out, flse, kept, fst = filtered(t, (it, k, p, mp))
+    assert st == 0 and fst == 0
+    decided = 0
+    for r in range(M):
+        how = of_row((it, k, p, mp), r)
+        # the oracle's scaled logits stop at f32's range, which is not where masses come from: relative ones here
+        top = x[r].max()
+        with np.errstate(over="ignore"):
+            rel = np.where(x[r] - top > -1e38, x[r] - top, -1e38)
+        if margin(rel, **how) < BORDER:
+            continue
+        o, z = ref.keep(rel, **how)
+        assert kept[r] == o.size, (r, how)
+        stays = np.zeros(V, dtype=bool)
+        stays[o] = True
+        np.testing.assert_array_equal(np.isfinite(out[r]), stays)
+        q = ref.probabilities(rel, **how)
+        assert (np.abs(dense[r] - q) <= 1e-5 * q + 1e-24).all(), (r, how)
+        for n in range(2):
+            want, far = ref.draw(q, float(u[r, n]))
+            if far >= BORDER or o.size == 1:
+                decided += 1
+                assert tokens[r, n] == want, (r, n, how)
+    assert decided >= M

@@ -1,4 +1,4 @@
-"""GPU: top logits, sampling and filtering of rows of logits against the 64-bit checker."""
+"""GPU: top logits, sampling and filtering of rows of logits against the 64-bit oracle."""
 import numpy as np
 import pytest
 import torch
