@@ -549,7 +549,7 @@ sd_status sd_filter_logits(const void *logits, int32_t dtype, int64_t ld, int32_
  * grad      : NULL (the loss alone), or dev [M][V] of the logits' type, rows grad_ld apart; may be `logits` itself (grad_ld = ld)
  * A row without entries has kl 0.  An index or label of V or more stores SD_ERR_BOUNDS and is left out.  Logits of minus infinity
  * are allowed (kl is infinite where the target gives one mass); NaN, a row of minus infinity alone, or one whose
- * largest |logit * inv_temp| is beyond 1e38 gives NaN.  With the gradient
+ * largest |logit * inv_temp| (for ce, |logit|) is beyond 1e8 gives NaN.  With the gradient
  * in the same call the logits are read once.
  */
 sd_status sd_distill_loss(const void *logits, int32_t dtype, int64_t ld, int32_t M, int32_t V,

@@ -533,8 +533,10 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
             const bool has_rest = p_rest > 0.0 && rest > 0.f;
             const float all_p = has_rest ? 1.f : (info.any ? (rest_too ? (float)mass : 1.f) : 0.f);
             // tail / sum = (all_p - p_rest / s_rest) / sum with s_rest = rest / sum
-            const float inv = 1.f / sum, tail = has_rest ? inv - (float)p_rest / rest : all_p * inv;
-            const RowFactors rf{most, all_p * inv, tail, two ? 1.f / sum1 : inv, (float)p_unit};
+            // (beyond 2^28, powers with R as 32 bits hold it are no longer near 1 at the largest logit: such a row has no loss)
+            const bool far = !(fabsf(most * c) <= 268435456.f), far1 = !(fabsf(most * kLog2e) <= 268435456.f);
+            const float inv = far ? __int_as_float(0x7fffffff) : 1.f / sum, tail = has_rest ? inv - (float)p_rest / rest : all_p * inv;
+            const RowFactors rf{most, all_p * inv, tail, two ? (far1 ? __int_as_float(0x7fffffff) : 1.f / sum1) : inv, (float)p_unit};
             if (lane == 0) { sh.row[h] = rf; mbar_arrive(&sh.row_ready[h]); }
             if (rank == 0) {
                 if (talk) { entries = warp_add(entries); label_z = warp_add(label_z); plogp = warp_add(plogp); }
@@ -547,12 +549,12 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
                     if (lane == 0) {
                         double kl = info.any ? plogp - entries * ((double)c * kLn2) + mass * (log(total) + (double)whole_power(most, c) * kLn2) : 0.0;
                         if (has_rest && info.any) kl += p_rest * log(p_rest * total / (double)rest);
-                        a.kl[r] = (float)kl;
+                        a.kl[r] = far ? inv : (float)kl;
                         if (a.stats) reinterpret_cast<float4*>(a.stats)[r] = make_float4(rf.top, rf.listed, rf.tail, rf.one);
                         if (label >= a.V) set_status(a.status, SD_ERR_BOUNDS);
                     } else if (a.ce) {
                         const double lse = (double)most + log((double)sum1) - ((double)most * (double)kLog2e - (double)whole_power(most, kLog2e)) * kLn2;
-                        a.ce[r] = has_label ? (float)(lse - (double)label_z) : 0.f;
+                        a.ce[r] = !has_label ? 0.f : far1 ? __int_as_float(0x7fffffff) : (float)(lse - (double)label_z);
                     }
                 }
             }

@@ -259,3 +259,34 @@ def test_the_loss_of_a_draft_that_has_learned(kind, V, K, inv_temp):
         change = np.abs(s[idx[r]] - p).sum() + abs((1 - s_list) - (1 - p.sum()))
         far = inv_temp * (z[r].max() - z[r].min())
         assert abs(kl[r] - want) <= 2e-6 * abs(s_list - p.sum()) + 2.0 ** -24 * far * change + 1e-9 + 2.0 ** -23 * abs(want), (r, kl[r], want)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [300, 4099, 40000])
+def test_logits_of_any_size(kind, V):
+    """Up to |logit * inv_temp| of 1e8 the losses are those of the formula; beyond, NaN (never a number that is wrong)."""
+    g = np.random.default_rng(V)
+    K, size = 8, np.array([1e-3, 1.0, 1e3, 1e6, 1e7, 2e9, 1e12, 1e20, 1e37])
+    M = size.size
+    x = g.normal(size=(M, V))
+    x = np.clip(x, -4.0, 4.0) * size[:, None]
+    t = device_rows(x.astype(np.float32), kind)
+    z = exact_values(t)
+    teacher = np.clip(g.normal(size=(M, V)), -4.0, 4.0) * np.minimum(size, 1e7)[:, None]
+    for inv_temp in (0.5, 1.0, 1.25):
+        idx, val, label = np.zeros((M, K), dtype=np.int32), np.zeros((M, K), dtype=np.float32), g.integers(0, V, M).astype(np.int32)
+        for r in range(M):
+            val[r], idx[r], _ = ref.top(teacher[r], K, inv_temp)
+        grad = torch.zeros_like(t)
+        kl, ce, _ = loss(t, val, idx, None, label, inv_temp, (1.0, 0.5), None, grad)
+        gr = grad.double().cpu().numpy()
+        for r in range(M):
+            if size[r] > 1e8:
+                assert np.isnan(kl[r]) and np.isnan(ce[r]) and np.isnan(gr[r]).any()
+                continue
+            a, b, want = ref.distill(z[r], val[r].astype(np.float64), idx[r], None, int(label[r]), inv_temp, 1.0, 0.5)
+            # a temperature that 32 bits round (2^-24 of the logits' distance), sums to 2e-6, one rounding
+            far = inv_temp * (z[r].max() - z[r].min())
+            assert abs(kl[r] - a) <= 2.0 ** -24 * 2 * far + 2e-6 + 2.0 ** -23 * abs(a), (size[r], kl[r], a)
+            assert abs(ce[r] - b) <= 2.0 ** -24 * 2 * (z[r].max() - z[r].min()) + 2e-6 + 2.0 ** -23 * abs(b), (size[r], ce[r], b)
+            assert np.isfinite(gr[r]).all()
