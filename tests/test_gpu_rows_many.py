@@ -268,3 +268,52 @@ def test_extreme_temperatures_and_logits(M, V, which):
                 decided += 1
                 assert tokens[r, n] == want, (r, n, how)
     assert decided >= M
+
+
+@pytest.mark.parametrize("which", ["", "p", "kp", "m"])
+@pytest.mark.parametrize("kind,M,V", [("f32", 45, 100003), ("bf16", 310, 41111)])
+def test_many_draws_of_many_rows(kind, M, V, which):
+    t, x = batch(M, V, kind, 41)
+    check(t, x, parameters(M, V, 41, which), 41, N=64, probs=False)
+
+
+@pytest.mark.parametrize("M,V", [(5, 30001), (80, 41000)])
+def test_small_arrays_at_any_place_and_outputs_left_out(M, V):
+    """The arrays with a few values per row need the alignment of their elements only; what may be missing is."""
+    t, x = batch(M, V, "f32", 51)
+    params = parameters(M, V, 51, "kpm")
+    u = np.random.default_rng(1).random((M, 3)).astype(np.float32)
+    want = sample(t, params, u)
+    kept_rows = filtered(t, params)
+
+    def odd(a):
+        whole = torch.full((a.numel() + 2,), 7, dtype=a.dtype, device="cuda")
+        whole[1:-1] = a.reshape(-1)
+        return whole, whole[1:-1].view(a.shape)
+    how = sd.Sampling(*params)
+    for name in ("inv_temp", "top_k", "top_p", "min_p"):
+        setattr(how, name, odd(getattr(how, name))[1])
+    how.c = sd.sd_sampling(how.inv_temp.data_ptr(), how.top_k.data_ptr(), how.top_p.data_ptr(), how.min_p.data_ptr())
+    ut = odd(torch.from_numpy(u).cuda())[1]
+    st = sd.new_status()
+    tokens_at, tokens = odd(torch.zeros((M, 3), dtype=torch.int32, device="cuda"))
+    prob_at, prob = odd(torch.zeros((M, 3), device="cuda"))
+    lse_at, lse = odd(torch.zeros(M, device="cuda"))
+    sd.sd_sample_logits(t, how, ut, tokens, prob, None, lse, st)
+    only = torch.zeros((M, 3), dtype=torch.int32, device="cuda")
+    sd.sd_sample_logits(t, how, ut, only, None, None, None, st)
+    out = torch.empty((M, V), device="cuda")
+    flse_at, flse = odd(torch.zeros(M, device="cuda"))
+    sd.sd_filter_logits(t, how, out, flse, None, st)
+    values_at, values = odd(torch.zeros((M, 5), device="cuda"))
+    index_at, index = odd(torch.zeros((M, 5), dtype=torch.int32, device="cuda"))
+    sd.sd_top_logits(t, 1.0, values, index, None, st)
+    torch.cuda.synchronize()
+    assert int(st.item()) == 0
+    for got, expect in ((tokens, want[0]), (prob, want[1]), (lse, want[3]), (only, want[0]), (out, kept_rows[0]), (flse, kept_rows[1])):
+        np.testing.assert_array_equal(got.cpu().numpy(), expect)
+    v, i, _ = top(t, 5, 1.0)
+    np.testing.assert_array_equal(index.cpu().numpy(), i)
+    np.testing.assert_array_equal(values.cpu().numpy(), v)
+    for whole in (tokens_at, prob_at, lse_at, flse_at, values_at, index_at):                # nothing beside them is written
+        assert float(whole[0]) == 7 and float(whole[-1]) == 7
