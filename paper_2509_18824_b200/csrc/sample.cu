@@ -733,10 +733,11 @@ top_kernel(const void* logits, long long ld, int V, int parts, int K, float inv_
 
 // ---------------------------------------------------------------- top logits of many rows
 // Where there are enough rows to fill the GPU, a CTA takes one at a time, twice over: first for the groups' largest logits and the
-// sum, then, mostly from L2, for the entries that reach the threshold.  Every warp has a sixteenth of the row and loads four vectors per
-// lane ahead of those that it works on, the next pass's and row's first ones too: no warp waits for another within a pass.  (Clusters
-// that hold a row in shared memory, 4096 rows of 152064 bf16: 740 us; a ring of copies for all warps of a CTA 580; one for every warp 850;
-// so 370.)
+// sum, then, mostly from L2, for the entries that reach the threshold.  A thread loads four vectors ahead of those that it works on, the
+// next pass's and row's first ones too: no warp waits for another within a pass.  Neighbours in the row belong to different threads, and
+// so to different groups: vocabularies have their frequent tokens side by side.  (With a sixteenth of the row for every warp, 512 rows of bf16
+// whose logits fall along the row took 4900 us, and 59 where they do not.  Clusters that hold a row in shared memory, 4096 rows of 152064
+// bf16: 740 us; a ring of copies for all warps of a CTA 580; one for every warp 850; so 370.)
 constexpr int kStreamLane = 4;                     // vectors per lane and step
 constexpr int kStreamVecs = kStreamLane * 32;
 
@@ -759,6 +760,19 @@ struct RowInMemory {
     }
 };
 
+// The logit of the K-th of a full list, K <= kSomeK
+__device__ __noinline__ float kth_listed(RowShared& sh, int K) {
+    const int tid = threadIdx.x;
+    cut_list(sh, sh.list, kListMax, K);
+    uint64_t last = tid < K ? sh.list[tid] : 0;
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1) last = max(last, __shfl_xor_sync(0xffffffffu, last, d));
+    if ((tid & 31) == 0) sh.hi[tid >> 5] = last;
+    __syncthreads();
+    for (int w = 0; w < kWarps; ++w) last = max(last, sh.hi[w]);
+    return key_logit(last);
+}
+
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 2)
 top_stream_kernel(const void* logits, long long ld, int V, int M, int steps, int K, float inv_temp, float* values, int32_t* index, float* lse) {
@@ -767,16 +781,15 @@ top_stream_kernel(const void* logits, long long ld, int V, int M, int steps, int
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     begin_dependent(logits, values, index, lse);
     const float c = inv_temp * kLog2e;
-    const int w0 = warp * steps * kStreamVecs;                                     // the warp's first vector
     uint4 ahead[kStreamLane];
-    const auto fetch = [&](const Row<T>& row, int q) {                             // step q of the warp's part
-        const int i0 = w0 + q * kStreamVecs;
-        if (i0 >= row.full0 && i0 + kStreamVecs <= row.full1) {
+    const auto place = [&](int q, int j) { return (q * kStreamLane + j) * kThreads + tid; };         // the thread's vectors of step q
+    const auto fetch = [&](const Row<T>& row, int q) {
+        if (place(q, 0) - lane >= row.full0 && place(q, kStreamLane - 1) - lane + 32 <= row.full1) {
 #pragma unroll
-            for (int j = 0; j < kStreamLane; ++j) ahead[j] = __ldcg(row.vec + i0 + j * 32 + lane);
+            for (int j = 0; j < kStreamLane; ++j) ahead[j] = __ldcg(row.vec + place(q, j));
         } else {
 #pragma unroll
-            for (int j = 0; j < kStreamLane; ++j) ahead[j] = i0 + j * 32 + lane < row.nvec ? row.load(i0 + j * 32 + lane) : Row<T>::nothing();
+            for (int j = 0; j < kStreamLane; ++j) ahead[j] = place(q, j) < row.nvec ? row.load(place(q, j)) : Row<T>::nothing();
         }
     };
     if (blockIdx.x < M) fetch(Row<T>(logits, ld, blockIdx.x, V), 0);
@@ -807,7 +820,7 @@ top_stream_kernel(const void* logits, long long ld, int V, int M, int steps, int
             top = fmaxf(top, m);
 #pragma unroll
             for (int j = 0; j < kStreamLane; ++j) {
-                if (w0 + q * kStreamVecs + j * 32 >= row.nvec) break;
+                if (place(q, j) - lane >= row.nvec) break;
                 Pair x[E / 2];
                 Row<T>::pairs(Row<T>::without_nan(raw[j]), x);
 #pragma unroll
@@ -833,35 +846,45 @@ top_stream_kernel(const void* logits, long long ld, int V, int M, int steps, int
             if (lane == 0) lse[r] = most > -INFINITY && most < INFINITY ? log_sum(most, inv_temp, s) : most;
         }
         __syncthreads();                                                           // (groups is written again)
-        const float thr = K <= kFewK ? kth_group(sh, 1, K) : kth_thread(sh, mine, K);
+        float thr = K <= kFewK ? kth_group(sh, 1, K) : kth_thread(sh, mine, K);
+        uint32_t n;
         // ---- the entries that reach the threshold
-        for (int q = 0; q < steps; ++q) {
-            uint4 raw[kStreamLane];
+        while (true) {
+            for (int q = 0; q < steps; ++q) {
+                uint4 raw[kStreamLane];
 #pragma unroll
-            for (int j = 0; j < kStreamLane; ++j) raw[j] = ahead[j];
-            if (q + 1 < steps) fetch(row, q + 1);
-            else if (r + gridDim.x < M) fetch(Row<T>(logits, ld, r + gridDim.x, V), 0);
+                for (int j = 0; j < kStreamLane; ++j) raw[j] = ahead[j];
+                if (q + 1 < steps) fetch(row, q + 1);
+                else if (r + gridDim.x < M) fetch(Row<T>(logits, ld, r + gridDim.x, V), 0);
 #pragma unroll
-            for (int j = 0; j < kStreamLane; ++j) {
-                if (!(Row<T>::largest(raw[j], -INFINITY) >= thr)) continue;
-                float x[E];
-                Row<T>::unpack(raw[j], x);
+                for (int j = 0; j < kStreamLane; ++j) {
+                    if (!(Row<T>::largest(raw[j], -INFINITY) >= thr)) continue;
+                    float x[E];
+                    Row<T>::unpack(raw[j], x);
 #pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (x[e] >= thr && x[e] > -INFINITY) {
-                        const uint32_t at = atomicAdd(&sh.cta_n, 1u);
-                        if (at < (uint32_t)kListMax) sh.list[at] = order_key(x[e], (w0 + q * kStreamVecs + j * 32 + lane) * E + e - row.lead);
-                    }
+                    for (int e = 0; e < E; ++e)
+                        if (x[e] >= thr && x[e] > -INFINITY) {
+                            const uint32_t at = atomicAdd(&sh.cta_n, 1u);
+                            if (at < (uint32_t)kListMax) sh.list[at] = order_key(x[e], place(q, j) * E + e - row.lead);
+                        }
+                }
             }
-        }
-        __syncthreads();
-        int n = sh.cta_n;
-        if (n > kListMax) {                                                        // (thousands of equal logits: the K-th's key is searched for)
+            __syncthreads();
+            n = sh.cta_n;
+            if (n <= (uint32_t)kListMax) break;
+            // Too many.  Where the largest logits stand side by side, the K-th of those listed is a better threshold; behind thousands of
+            // equal ones the K-th's key is searched for.
+            const float better = kth_listed(sh, K);
+            if (tid == 0) sh.cta_n = 0;
+            __syncthreads();
+            if (better > thr) {
+                thr = better;
+                fetch(row, 0);
+                continue;
+            }
             const RowInMemory<T> all(row);
             uint64_t border = ~0ull;
             search_border(sh, all, false, (uint64_t)K, -1.0, ~0ull, Scale(1.f), 0, &border);
-            if (tid == 0) sh.cta_n = 0;
-            __syncthreads();
             all.each([&](float x, int i) {
                 if (order_key(x, i) > border) return;
                 const uint32_t at = atomicAdd(&sh.cta_n, 1u);
@@ -869,6 +892,7 @@ top_stream_kernel(const void* logits, long long ld, int V, int M, int steps, int
             });
             __syncthreads();
             n = min(sh.cta_n, (uint32_t)kListMax);
+            break;
         }
         n = sort_list(sh, sh.list, n, K);
         for (int i = tid; i < K; i += kThreads) {

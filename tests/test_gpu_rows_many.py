@@ -6,7 +6,7 @@ import torch
 
 from oracle import rows as ref
 from paper_2509_18824_b200 import binding as sd
-from rows_util import LOWEST, margin
+from rows_util import LOWEST, device_rows, exact_values, margin
 from test_gpu_rows_sampling import BORDER, batch, check, filtered, of_row, parameters, sample, top
 
 pytestmark = pytest.mark.gpu
@@ -317,3 +317,25 @@ def test_small_arrays_at_any_place_and_outputs_left_out(M, V):
     np.testing.assert_array_equal(values.cpu().numpy(), v)
     for whole in (tokens_at, prob_at, lse_at, flse_at, values_at, index_at):                # nothing beside them is written
         assert float(whole[0]) == 7 and float(whole[-1]) == 7
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("M,V,K", [(3, 60000, 64), (76, 60001, 64), (149, 20000, 300), (149, 60000, 10), (330, 30011, 384)])
+def test_top_logits_that_stand_side_by_side(M, V, K, kind):
+    """Vocabularies with their frequent tokens at one end: rows that fall, rise, or have a high stretch."""
+    g = np.random.default_rng(M + K)
+    at = np.arange(V) / V
+    shapes = (12.0 * (1 - at), 12.0 * at, 8.0 * np.exp(-at * 50), np.where(np.abs(at - 0.4) < 0.02, 9.0, 0.0), 40.0 * at)
+    x = np.stack([g.normal(size=V) * 2.0 + shapes[r % 5] for r in range(M)])
+    x[4::10] = np.sort(x[4::10], axis=1)
+    t = device_rows(x.astype(np.float32), kind)
+    x = exact_values(t)
+    values, index, lse = top(t, K, 1.0)
+    for r in range(M):
+        v, i, l = ref.top(x[r], K, 1.0)
+        np.testing.assert_array_equal(index[r], i, err_msg=str(r))
+        np.testing.assert_array_equal(values[r].astype(np.float64), v)
+        # as above: terms to 2^-22, arguments of at most 2^6 to 2^-24 of them
+        assert abs(lse[r] - l) <= 2e-5 + 2.0 ** -23 * abs(l)
+    params = (np.ones(M, np.float32), np.resize([50, 5, 0], M).astype(np.int32), np.resize([1.0, 0.9], M).astype(np.float32), None)
+    check(t, x, params, 3, N=1)
