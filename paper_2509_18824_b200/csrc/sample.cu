@@ -13,7 +13,7 @@
 // slices of 76 KB, two of which share an SM), read once and passed over as often as it takes.  One such row: k = 50 13 us, any mixture
 // with top-p 42, all entries 17; latency bounds it (copy 3 us, then barriers of the cluster, sorting, the draw).
 // Many rows: passes over L2 with loads ahead in registers, a CTA or a small cluster per row.  Top logits then take one pass with the
-// log-sum-exp and one for the list: 2048 rows of 152064 bf16, K = 64 187 us, 3.3 TB/s, bound by instructions (63 % of the issue
+// log-sum-exp and one for the list: 2048 rows of 152064 bf16, K = 64 192 us, 3.2 TB/s, bound by instructions (63 % of the issue
 // slots, XU pipe 38 %) and by what follows a row's passes.  256 rows of 152064 f32: k = 50 72 us, everything 91 (its masses in 64 bits: the
 // fp64 pipe at 39 %), top-p 270 (the histograms' atomics).
 // (Lists kept in a single pass over global memory, with a threshold that rises, took three times as long: their cutting and their
@@ -737,7 +737,7 @@ top_kernel(const void* logits, long long ld, int V, int parts, int K, float inv_
 // next pass's and row's first ones too: no warp waits for another within a pass.  Neighbours in the row belong to different threads, and
 // so to different groups: vocabularies have their frequent tokens side by side.  (With a sixteenth of the row for every warp, 512 rows of bf16
 // whose logits fall along the row took 4900 us, and 59 where they do not.  Clusters that hold a row in shared memory, 4096 rows of 152064
-// bf16: 740 us; a ring of copies for all warps of a CTA 580; one for every warp 850; so 370.)
+// bf16: 740 us; a ring of copies for all warps of a CTA 580; one for every warp 850; so 380.)
 constexpr int kStreamLane = 4;                     // vectors per lane and step
 constexpr int kStreamVecs = kStreamLane * 32;
 
@@ -1621,12 +1621,12 @@ sd_status launch_top_logits(const void* logits, int dtype, long long ld, int M, 
     const bool all_at_once = (long long)M * fit <= 2 * sms - 32;
     if (K <= kSomeK && (M >= sms / 2 || !all_at_once)) {
         auto kern = dtype == SD_F32 ? top_stream_kernel<float> : top_stream_kernel<uint16_t>;
-        // (up to one row per SM: so much shared memory that no SM takes two; 80 rows of f32 27 -> 20 us)
+        // (up to one row per SM: so much shared memory that no SM takes two; 80 rows of f32 27 -> 21 us)
         const int ctas = 2 * sms, steps = (nvec + kWarps * kStreamVecs - 1) / (kWarps * kStreamVecs), alone = M <= sms ? 96 * 1024 : 0;
         if (!allow_dynamic_smem(kern, 96 * 1024)) return SD_ERR_CUDA;
         return launch_dependent(kern, dim3((unsigned)(M < ctas ? M : ctas)), kThreads, alone, 1, st, logits, ld, V, M, steps, K, inv_temp, values, index, lse);
     }
-    // (long lists: as sampled rows, below; K = 1000 of 148 rows of 152064 f32 136 -> 76 us, of 2048 1697 -> 950)
+    // (long lists: as sampled rows, below; K = 1000 of 148 rows of 152064 f32 136 -> 76 us, of 2048 1697 -> 892)
     const bool held = nvec <= 5120 || all_at_once;
     const int parts = held ? fit : shares_of(M, sms);
     const int smem = held ? (nvec + parts - 1) / parts * 16 : kCopies * kBins * 4 + kBins * 8;
