@@ -45,8 +45,10 @@ __device__ __forceinline__ bool sum_warps_or(bool v) {
 }
 
 // Exponentials are taken as 2^(x c - R) with R = rint(top c), a whole number: x c - R is one instruction with one rounding (of a small
-// number where it matters), and sums with different R are brought together exactly.
-__device__ __forceinline__ float whole_power(float top, float c) { return top > -INFINITY ? rintf(top * c) : 0.f; }
+// number where it matters), and sums with different R are brought together exactly.  R stays above -2^28: what is further down (a
+// mask's lowest value, whose R would be minus infinity, and the difference from it NaN) has a power of 0 with any other R.
+constexpr float kFar = 268435456.f;    // 2^28: up to here 32 bits hold R as near to the logit's power as exponents need
+__device__ __forceinline__ float whole_power(float top, float c) { return top > -INFINITY ? fmaxf(rintf(top * c), -kFar) : 0.f; }
 
 // What a CTA tells the others of its row: its largest logit and, with its R, the sums of 2^(x c - R) outside and among the
 // entries and of 2^(x log2 e - R1); its entries' sums of p z, p and p log p; the label's logit where it lies in its slice.
@@ -534,7 +536,7 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
             const float all_p = has_rest ? 1.f : (info.any ? (rest_too ? (float)mass : 1.f) : 0.f);
             // tail / sum = (all_p - p_rest / s_rest) / sum with s_rest = rest / sum
             // (beyond 2^28, powers with R as 32 bits hold it are no longer near 1 at the largest logit: such a row has no loss)
-            const bool far = !(fabsf(most * c) <= 268435456.f), far1 = !(fabsf(most * kLog2e) <= 268435456.f);
+            const bool far = !(fabsf(most * c) <= kFar), far1 = !(fabsf(most * kLog2e) <= kFar);
             const float inv = far ? __int_as_float(0x7fffffff) : 1.f / sum, tail = has_rest ? inv - (float)p_rest / rest : all_p * inv;
             const RowFactors rf{most, all_p * inv, tail, two ? (far1 ? __int_as_float(0x7fffffff) : 1.f / sum1) : inv, (float)p_unit};
             if (lane == 0) { sh.row[h] = rf; mbar_arrive(&sh.row_ready[h]); }
