@@ -8,6 +8,7 @@ from __future__ import annotations
 import numpy as np
 
 F32_MAX = float(np.finfo(np.float32).max)                     # where scaled logits of unmasked entries stop
+REST_IS_NONE = -2.0 ** 28 * np.log(2.0)                       # scaled logits below this are masks: no mass outside a student's entries
 
 
 def in_order(x: np.ndarray) -> np.ndarray:
@@ -87,11 +88,11 @@ def distill(z: np.ndarray, top_val, top_idx, top_lse, label: int, inv_temp: floa
         outside[i] = False
         g = s * p.sum() - dist
         if top_lse is not None:
-            p_rest, s_rest = 1.0 - p.sum(), s[outside].sum()
-            if p_rest > 0 and s_rest > 0:
-                kl += float(p_rest * (np.log(p_rest) - np.log(s_rest)))
-                g = s - dist
-                g[outside] -= p_rest * s[outside] / s_rest
+            p_rest, rest = 1.0 - p.sum(), np.where(outside, z * inv_temp, -np.inf)
+            log_rest = lse(rest)                              # (of the student's mass outside the entries, however small that is)
+            if p_rest > 0 and log_rest > REST_IS_NONE:
+                kl += float(p_rest * (np.log(p_rest) - log_rest + lse(z * inv_temp)))
+                g = s - dist - p_rest * np.exp(rest - log_rest)
         g *= inv_temp
     g = kl_weight * g
     if 0 <= label < V:

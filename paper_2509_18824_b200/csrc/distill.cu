@@ -46,13 +46,15 @@ __device__ __forceinline__ bool sum_warps_or(bool v) {
 
 // Exponentials are taken as 2^(x c - R) with R = rint(top c), a whole number: x c - R is one instruction with one rounding (of a small
 // number where it matters), and sums with different R are brought together exactly.  R stays above -2^28: what is further down (a
-// mask's lowest value, whose R would be minus infinity, and the difference from it NaN) has a power of 0 with any other R.
+// mask's lowest value, whose R would be minus infinity, and the difference from it NaN) has a power of 0 there.
+constexpr double kLn2 = 0.69314718055994530942;
 constexpr float kFar = 268435456.f;    // 2^28: up to here 32 bits hold R as near to the logit's power as exponents need
-__device__ __forceinline__ float whole_power(float top, float c) { return top > -INFINITY ? fmaxf(rintf(top * c), -kFar) : 0.f; }
+__device__ __forceinline__ float whole_power(float top, float c) { return fmaxf(rintf(top * c), -kFar); }
 
-// What a CTA tells the others of its row: its largest logit and, with its R, the sums of 2^(x c - R) outside and among the
-// entries and of 2^(x log2 e - R1); its entries' sums of p z, p and p log p; the label's logit where it lies in its slice.
-struct __align__(16) Message { float top, label, rest, sum1; double listed, entries, mass, plogp; };
+// What a CTA tells the others of its row: its largest logit and, with its R, the sums of 2^(x c - R) among the entries and of
+// 2^(x log2 e - R1); the largest logit outside the entries and, with the R of that, the sum there (a student may be surer of an entry than
+// 32 bits have exponents); its entries' sums of p and of p (log p - z c ln 2); the label's logit where it lies in its slice.
+struct __align__(16) Message { float top, label, rest, sum1, top_rest, none; double listed, mass, own; };
 static_assert(sizeof(Message) == 48, "three stores of 16 bytes");
 
 // A place in the ring of slots and the phase of its barriers
@@ -67,8 +69,9 @@ struct RowInfo {                       // prepared ahead
     float weight;                      // dloss
     int label, any, count;             // any: the row has entries; count: those that lie in this CTA's slice
 };
-// What an exponential is multiplied with at the entries, elsewhere, for the cross-entropy, and what the list's p are
-struct RowFactors { float top, listed, tail, one, p; };
+// What 2^(x c - r_c) is multiplied with at the entries, 2^(x c - r_rest) elsewhere, 2^(x log2 e - r_e) for the cross-entropy, and what
+// the list's p are
+struct RowFactors { float r_c, r_rest, r_e, listed, tail, one, p; };
 
 struct DistillShared {
     uint64_t full[kMaxSlots], picked[kMaxSlots], free_[kMaxSlots];
@@ -78,7 +81,7 @@ struct DistillShared {
     float label_z[kMaxLists];
     int dup[kMaxLists], label_listed[kMaxLists];
     float4 sums[2][kSumWarps + 1];     // the warps' (largest logit, sum outside the entries, 0, sum at temperature 1); the entries' last
-    double part[2], listed[2];         // sum of p z; the listed entries' sum of 2^(z c - R)
+    double own[2], listed[2];          // sum of p (log p - z c ln 2); the listed entries' sum of 2^(z c - R)
     Message msg[2][8];
     RowFactors row[2];
 };
@@ -105,17 +108,62 @@ __device__ __forceinline__ uint4 pack(const float (&g)[Row<T>::kE]) {
 }
 
 
-// Gradient factors of a row, with dloss and the weights: an entry x outside the list gets tail * 2^(x c - R) + one *
-// 2^(x log2 e - R1), at temperature 1 in one term.
+// RowFactors between two calls, in the four floats that a row has there.  As a rule r_rest is r_c, and that and r_e follow from the row's
+// largest logit: (it, listed, tail, one).  Where the entries outside the list lie so far below that their sum has an R of its own (kOwnPower),
+// seven numbers in 16 bytes, told by the second one's sign: r_c (r_e at a label and inv_temp < 1; one follows from the other)
+// and its distance from r_rest as multiples of 128 in 23 bits each, listed, -tail and one as floats without sign and last four bits (kNoOne:
+// no cross-entropy to be had).  Any R near a logit's power will do, with the factors adjusted.
+constexpr float kOwnPower = 64.f;      // up to here r_c serves both: factors reach 2^64, what is lost is below 2^-62 of p_rest
+constexpr float kStepR = 128.f;
+constexpr uint32_t kNoOne = 0x7ffffffu;
+__device__ __forceinline__ uint32_t short_float(float x) { return ((__float_as_uint(x) & 0x7fffffffu) + 8u) >> 4; }
+__device__ __forceinline__ float long_float(uint32_t u) { return __uint_as_float((u & 0x7ffffffu) << 4); }
+__device__ __forceinline__ void stats_powers(float step, bool by_e, float inv_temp, float& r_c, float& r_e) {
+    const float r = step * kStepR;
+    r_c = by_e ? rintf(r * inv_temp) : r;
+    r_e = by_e ? r : rintf(__fdividef(r, inv_temp));
+}
+__device__ __noinline__ float4 pack_stats(const RowFactors& rf, bool by_e, float inv_temp) {
+    const bool none = rf.one != rf.one;
+    by_e = by_e && !none;
+    const float step = rintf((by_e ? rf.r_e : rf.r_c) / kStepR);
+    float r_c, r_e;
+    stats_powers(step, by_e, inv_temp, r_c, r_e);
+    const int down = (int)rintf((r_c - rf.r_rest) / kStepR);
+    const float r_rest = r_c - (float)down * kStepR;
+    const uint32_t listed = short_float(rf.listed * ex2(r_c - rf.r_c)), tail = short_float(fmaxf(-rf.tail, 0.f) * ex2(r_rest - rf.r_rest)),
+                   one = none ? kNoOne : short_float(rf.one * ex2(r_e - rf.r_e)), at = (uint32_t)(int)step & 0x7fffffu, d = (uint32_t)down;
+    return make_float4(__uint_as_float(listed | d << 27), __uint_as_float(0x80000000u | tail | (d >> 5 & 15u) << 27),
+                       __uint_as_float(one | (d >> 9 & 31u) << 27), __uint_as_float(at | (d >> 14) << 23));
+}
+__device__ __forceinline__ RowFactors unpack_stats(const float4& st, bool by_e, float inv_temp) {
+    const uint32_t a = __float_as_uint(st.x), b = __float_as_uint(st.y), e = __float_as_uint(st.z), w = __float_as_uint(st.w);
+    RowFactors rf{0.f, 0.f, 0.f, st.y, st.z, st.w, 1.f};
+    if (!(b >> 31)) {
+        rf.r_c = rf.r_rest = whole_power(st.x, inv_temp * kLog2e);
+        rf.r_e = whole_power(st.x, kLog2e);
+        return rf;
+    }
+    stats_powers((float)((int)(w << 9) >> 9), by_e && (e & kNoOne) != kNoOne, inv_temp, rf.r_c, rf.r_e);
+    rf.r_rest = rf.r_c - (float)(a >> 27 | (b >> 27 & 15u) << 5 | e >> 27 << 9 | w >> 23 << 14) * kStepR;
+    rf.listed = long_float(a);
+    rf.tail = -long_float(b);
+    rf.one = long_float(e);
+    return rf;
+}
+
+// Gradient factors of a row, with dloss and the weights: an entry x outside the list gets tail * 2^(x c - r_rest) + one *
+// 2^(x log2 e - r_e), at temperature 1 in one term.
 struct Factors {
-    float r_c, r_e, c;                 // R, R1
-    float listed, tail, one;           // `listed` stands for `tail` at the listed entries
+    float r_c, r_rest, r_e, c;
+    float listed, tail, one;           // `listed` stands for `tail`, and r_c for r_rest, at the listed entries
     float per_p, per_label;            // what a listed entry's p, and the label, take away
     bool two;
     __device__ __forceinline__ Factors(const DistillCall& a, const RowFactors& rf, float g, bool has_label) {
         c = a.inv_temp * kLog2e;
-        r_c = whole_power(rf.top, c);
-        r_e = whole_power(rf.top, kLog2e);
+        r_c = rf.r_c;
+        r_rest = rf.r_rest;
+        r_e = rf.r_e;
         per_p = g * a.kl_weight * a.inv_temp;
         listed = per_p * rf.listed;
         tail = per_p * rf.tail;
@@ -123,10 +171,10 @@ struct Factors {
         per_label = has_label ? g * a.ce_weight : 0.f;
         one = per_label != 0.f ? per_label * rf.one : 0.f;
         two = a.inv_temp != 1.f && one != 0.f;
-        if (!two) { listed += one; tail += one; }
+        if (!two) { listed += one; tail += one * ex2(r_rest - r_c); }
     }
-    __device__ __forceinline__ float at(float x, float factor) const {
-        const float e = factor * ex2(fmaf(x, c, -r_c));
+    __device__ __forceinline__ float at(float x, float factor, float r) const {
+        const float e = factor * ex2(fmaf(x, c, -r));
         return two ? fmaf(one, ex2(fmaf(x, kLog2e, -r_e)), e) : e;
     }
     template <typename T, bool TWO>
@@ -135,7 +183,7 @@ struct Factors {
         Row<T>::pairs(raw, x);
 #pragma unroll
         for (int e = 0; e < Row<T>::kE / 2; ++e) {
-            const Pair w = ex2(fma2(x[e], Pair{c, c}, Pair{-r_c, -r_c}));
+            const Pair w = ex2(fma2(x[e], Pair{c, c}, Pair{-r_rest, -r_rest}));
             Pair o{tail * w.x, tail * w.y};
             if constexpr (TWO) o = fma2(Pair{one, one}, ex2(fma2(x[e], Pair{kLog2e, kLog2e}, Pair{-r_e, -r_e})), o);
             g[2 * e] = o.x;
@@ -470,7 +518,7 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
                 part = warp_add(part);
                 // (the loss alone: the sums of two rows before have been taken over)
                 ok = mbar_wait_warp(&sh.row_ready[h], (uint32_t)((n >> 1) & 1) ^ 1u, &sh.abort_flag, wait_cycles);
-                if (lane == 0) { sh.sums[h][kSumWarps] = make_float4(top, 0.f, 0.f, sum1); sh.part[h] = part; sh.listed[h] = sum; }
+                if (lane == 0) { sh.sums[h][kSumWarps] = make_float4(top, 0.f, 0.f, sum1); sh.own[h] = sh.info[b].plogp - part * ((double)c * kLn2); sh.listed[h] = sum; }
             }
             if (lane == 0) { sh.label_z[b] = label_z; sh.dup[b] = dup; sh.label_listed[b] = label_listed; }
             __syncwarp();
@@ -480,7 +528,7 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
         const float c = a.inv_temp * kLog2e;
         const bool rest_too = a.top_lse != nullptr;
         const auto weigh = [](float own, float all, float cc) {                    // 2^(R - the row's R)
-            return own > -INFINITY ? ex2(whole_power(own, cc) - whole_power(all, cc)) : 1.f;
+            return ex2(whole_power(own, cc) - whole_power(all, cc));
         };
         long long n = 0;
         if constexpr (MODE != kGrad)
@@ -494,68 +542,76 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
             const int label = info.label;
             const bool has_label = label >= 0 && label < a.V, two = has_label && a.inv_temp != 1.f;
             const float4 w = lane <= kSumWarps ? sh.sums[h][lane] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
-            double entries = sh.part[h], listed = 0.0, mass = info.mass, plogp = info.plogp;
-            float label_z = sh.label_z[b], most = warp_largest(w.x);
-            const float f = weigh(w.x, most, c);
-            if (rest_too) listed = sh.listed[h] * (double)__shfl_sync(0xffffffffu, f, kSumWarps);
-            float rest = warp_add(w.y * f), sum1 = two ? warp_add(w.w * weigh(w.x, most, kLog2e)) : 0.f;
+            double listed = 0.0, mass = info.mass, own = sh.own[h];
+            const float top_rest = lane < kSumWarps ? w.x : -INFINITY, top_listed = __shfl_sync(0xffffffffu, w.x, kSumWarps);
+            float label_z = sh.label_z[b], most_rest = warp_largest(top_rest), most = fmaxf(most_rest, top_listed);
+            if (rest_too) listed = sh.listed[h] * (double)weigh(top_listed, most, c);
+            float rest = warp_add(w.y * weigh(top_rest, most_rest, c)), sum1 = two ? warp_add(w.w * weigh(w.x, most, kLog2e)) : 0.f;
             if (talk) {
-                const Message mine{most, label_z, rest, sum1, listed, entries, mass, plogp};
+                const Message mine{most, label_z, rest, sum1, most_rest, 0.f, listed, mass, own};
                 if (lane == rank) {
                     sh.msg[h][rank] = mine;
                     mbar_arrive_expect_tx(&sh.told[h], (parts - 1) * (uint32_t)sizeof(Message));
                 } else if (lane < parts) {
                     const uint32_t to = map_dsmem(smem_u32(&sh.msg[h][rank]), lane), bar = map_dsmem(smem_u32(&sh.told[h]), lane);
+                    const auto low = [](double x) { return (uint32_t)__double2loint(x); };
+                    const auto high = [](double x) { return (uint32_t)__double2hiint(x); };
                     st_async_v4(to, __float_as_uint(most), __float_as_uint(label_z), __float_as_uint(rest), __float_as_uint(sum1), bar);
-                    const auto two_doubles = [&](uint32_t at, double x, double y) {
-                        st_async_v4(at, (uint32_t)__double2loint(x), (uint32_t)__double2hiint(x), (uint32_t)__double2loint(y), (uint32_t)__double2hiint(y), bar);
-                    };
-                    two_doubles(to + 16, listed, entries);
-                    two_doubles(to + 32, mass, plogp);
+                    st_async_v4(to + 16, __float_as_uint(most_rest), 0u, low(listed), high(listed), bar);
+                    st_async_v4(to + 32, low(mass), high(mass), low(own), high(own), bar);
                 }
                 ok = mbar_wait_cluster(&sh.told[h], ph, &sh.abort_flag, wait_cycles);
                 ok = __all_sync(0xffffffffu, ok);
-                Message o{-INFINITY, 0.f, 0.f, 0.f, 0.0, 0.0, 0.0, 0.0};
+                Message o{-INFINITY, 0.f, 0.f, 0.f, -INFINITY, 0.f, 0.0, 0.0, 0.0};
                 if (lane < parts) o = sh.msg[h][lane];
                 most = warp_largest(o.top);
-                const float g = weigh(o.top, most, c);
-                rest = warp_add(o.rest * g);
-                listed = rest_too ? warp_add(o.listed * (double)g) : 0.0;
+                most_rest = warp_largest(o.top_rest);
+                rest = warp_add(o.rest * weigh(o.top_rest, most_rest, c));
+                listed = rest_too ? warp_add(o.listed * (double)weigh(o.top, most, c)) : 0.0;
                 if (two) sum1 = warp_add(o.sum1 * weigh(o.top, most, kLog2e));
-                entries = o.entries;
+                own = o.own;
                 label_z = o.label;
                 mass = warp_add(o.mass);
-                plogp = o.plogp;
             }
             const double p_unit = rest_too || !(mass > 0.0) ? 1.0 : 1.0 / mass;    // what the list's p are multiples of
-            const double total = (double)rest + listed;
-            const float sum = (float)total;
-            if (!two) sum1 = sum;
             const double p_rest = rest_too ? 1.0 - mass : 0.0;
             const bool has_rest = p_rest > 0.0 && rest > 0.f;
-            const float all_p = has_rest ? 1.f : (info.any ? (rest_too ? (float)mass : 1.f) : 0.f);
-            // tail / sum = (all_p - p_rest / s_rest) / sum with s_rest = rest / sum
             // (beyond 2^28, powers with R as 32 bits hold it are no longer near 1 at the largest logit: such a row has no loss)
             const bool far = !(fabsf(most * c) <= kFar), far1 = !(fabsf(most * kLog2e) <= kFar);
-            const float inv = far ? __int_as_float(0x7fffffff) : 1.f / sum, tail = has_rest ? inv - (float)p_rest / rest : all_p * inv;
-            const RowFactors rf{most, all_p * inv, tail, two ? (far1 ? __int_as_float(0x7fffffff) : 1.f / sum1) : inv, (float)p_unit};
+            // the rest has an R of its own where it lies too far below the largest logit, else that one's
+            const float r_c = whole_power(most, c), r_e = whole_power(most, kLog2e), r_own = whole_power(most_rest, c);
+            const float at_c = ex2(r_own - r_c);
+            const bool apart = has_rest && r_c - r_own > kOwnPower && !far;
+            const double total = (double)(rest * at_c) + listed;
+            const float sum = (float)total;
+            if (!apart) rest *= at_c;
+            if (!two) sum1 = sum;
+            const float all_p = has_rest ? 1.f : (info.any ? (rest_too ? (float)mass : 1.f) : 0.f);
+            // tail / sum = (all_p - p_rest / s_rest) / sum with s_rest = rest / sum
+            const float inv = far ? __int_as_float(0x7fffffff) : 1.f / sum, tail = has_rest ? (apart ? inv * at_c : inv) - (float)p_rest / rest : all_p * inv;
+            const RowFactors rf{r_c, apart ? r_own : r_c, r_e, all_p * inv, tail, two ? (far1 ? __int_as_float(0x7fffffff) : 1.f / sum1) : inv, (float)p_unit};
             if (lane == 0) { sh.row[h] = rf; mbar_arrive(&sh.row_ready[h]); }
             if (rank == 0) {
-                if (talk) { entries = warp_add(entries); label_z = warp_add(label_z); plogp = warp_add(plogp); }
-                if (!rest_too) { plogp = plogp * p_unit - log(mass); entries *= p_unit; mass = 1.0; }
-                // lane 0: kl; lane 1: ce.  R belongs to the power with c as 32 bits hold it.  Relative to the largest logit that is a slightly
-                // other temperature: ce takes it back at that logit; in kl the entries' logits stand at the same one, so that what is left
-                // of it counts by the difference of the two distributions.
-                constexpr double kLn2 = 0.69314718055994530942;
-                if (lane < 2) {
+                if (talk) { own = warp_add(own); label_z = warp_add(label_z); }
+                // R belongs to the power with c as 32 bits hold it.  Relative to the largest logit that is a slightly other temperature: ce takes
+                // it back at that logit; in kl the entries' logits stand at the same one, so that what is left of it counts by the difference
+                // of the two distributions.
+                // A logarithm per lane, of one call (four in a row would not stay in the instruction caches from row to row)
+                const double log_of = log(lane == 0 ? total : lane == 1 ? (double)sum1 : lane == 2 ? p_rest * total : lane == 3 ? (double)rest : mass);
+                const double log_total = __shfl_sync(0xffffffffu, log_of, 0), log_p = __shfl_sync(0xffffffffu, log_of, 2) - __shfl_sync(0xffffffffu, log_of, 3),
+                             log_mass = __shfl_sync(0xffffffffu, log_of, 4);
+                if (!rest_too) { own = own * p_unit - log_mass; mass = 1.0; }
+                if (lane < 2) {                                                    // lane 0: kl; lane 1: ce
                     if (lane == 0) {
-                        double kl = info.any ? plogp - entries * ((double)c * kLn2) + mass * (log(total) + (double)whole_power(most, c) * kLn2) : 0.0;
-                        if (has_rest && info.any) kl += p_rest * log(p_rest * total / (double)rest);
+                        double kl = info.any ? own + mass * (log_total + (double)r_c * kLn2) : 0.0;
+                        if (has_rest && info.any) kl += p_rest * (log_p + ((double)r_c - (double)rf.r_rest) * kLn2);
                         a.kl[r] = far ? inv : (float)kl;
-                        if (a.stats) reinterpret_cast<float4*>(a.stats)[r] = make_float4(rf.top, rf.listed, rf.tail, rf.one);
+                        if (a.stats)
+                            reinterpret_cast<float4*>(a.stats)[r] = apart ? pack_stats(rf, two && a.inv_temp < 1.f, a.inv_temp)
+                                                                          : make_float4(most, rf.listed, rf.tail, rf.one);
                         if (label >= a.V) set_status(a.status, SD_ERR_BOUNDS);
                     } else if (a.ce) {
-                        const double lse = (double)most + log((double)sum1) - ((double)most * (double)kLog2e - (double)whole_power(most, kLog2e)) * kLn2;
+                        const double lse = (double)most + log_of - ((double)most * (double)kLog2e - (double)r_e) * kLn2;
                         a.ce[r] = !has_label ? 0.f : far1 ? __int_as_float(0x7fffffff) : (float)(lse - (double)label_z);
                     }
                 }
@@ -581,9 +637,8 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
             const Turn at0 = at;
 
             // ---- sums of the pieces as they come in
-            float top = -INFINITY, r_c = 0.f, r_e = 0.f;                           // top: of the lane's entries; the R's are the warp's
+            float top = -INFINITY, r_c = -kFar, r_e = -kFar;                        // top: of the lane's entries; the R's are the warp's
             Pair s{0.f, 0.f}, t{0.f, 0.f}, s1{0.f, 0.f};
-            bool begun = false;
             for (int q = 0; MODE != kGrad && q < sl.pieces; ++q, at.next(slots)) {
                 const int slot = at.slot;
                 ok = mbar_wait(&sh.picked[slot], at.phase, &sh.abort_flag, wait_cycles) && ok;
@@ -599,14 +654,15 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
                 }
                 // R is that of the first pieces' largest logit until one comes that is 2^32 times as much (exponentials of up to that
                 // size are added as exactly)
-                if (__any_sync(0xffffffffu, m > -INFINITY && (!begun || m * c - r_c > 32.f || m * kLog2e - r_e > 32.f))) {
+                if (__any_sync(0xffffffffu, m * c - r_c > 32.f || m * kLog2e - r_e > 32.f)) {
                     const float most = warp_largest(fmaxf(top, m));
                     const float n_c = whole_power(most, c), n_e = whole_power(most, kLog2e);
                     const float f = ex2(r_c - n_c), f1 = ex2(r_e - n_e);
-                    if (begun) { s = Pair{s.x * f, s.y * f}; t = Pair{t.x * f, t.y * f}; s1 = Pair{s1.x * f1, s1.y * f1}; }
+                    s = Pair{s.x * f, s.y * f};
+                    t = Pair{t.x * f, t.y * f};
+                    s1 = Pair{s1.x * f1, s1.y * f1};
                     r_c = n_c;
                     r_e = n_e;
-                    begun = true;
                 }
                 top = fmaxf(top, m);
                 const Pair from_c{-r_c, -r_c}, from_e{-r_e, -r_e};
@@ -652,7 +708,7 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
                 }
             } else {
                 const float4 st = __ldcg(reinterpret_cast<const float4*>(a.stats) + r);
-                rf = RowFactors{st.x, st.y, st.z, st.w, 1.f};
+                rf = unpack_stats(st, has_label && a.inv_temp < 1.f, a.inv_temp);
                 if (label >= a.V && tid == 0 && rank_of(u) == 0) set_status(a.status, SD_ERR_BOUNDS);
             }
 
@@ -711,13 +767,13 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
                             p = 0.0;
                             for (int x = 0; x < info.count; ++x) p += (li.at[x] & ~kAgain) == j ? li.p[x] : 0.0;
                         }
-                        float g = f.at(li.z[k], f.listed) - f.per_p * (float)p;
+                        float g = f.at(li.z[k], f.listed, f.r_c) - f.per_p * (float)p;
                         if (j + sl.first == label) g -= f.per_label;
                         store_one<T>(grad, j + sl.first, g);
                     }
                     const int lj = label - sl.first;
                     if (tid == kSumThreads - 1 && has_label && !sh.label_listed[b] && lj >= 0 && lj < (sl.v1 - sl.v0) * E)
-                        store_one<T>(grad, label, f.at(sh.label_z[b], f.tail) - f.per_label);
+                        store_one<T>(grad, label, f.at(sh.label_z[b], f.tail, f.r_rest) - f.per_label);
                 }
             }
             __syncwarp();
