@@ -536,7 +536,9 @@ sd_status sd_filter_logits(const void *logits, int32_t dtype, int64_t ld, int32_
  *   top_lse NULL : p = softmax of t * inv_temp over the row's entries;  kl[r] = sum_k p_k (log p_k - log s[i_k])
  *   top_lse given: p_k = exp(t_k * inv_temp - top_lse[r]), and what is missing from 1, p_rest, stands against the student's mass outside
  *                  the entries, s_rest:  kl[r] = sum_k p_k (log p_k - log s[i_k]) + p_rest (log p_rest - log s_rest)
- *                  (no such term where p_rest <= 0 or s_rest = 0)
+ *                  (no such term where p_rest <= 0).  A student that masks everything outside the entries, with minus infinity or logits
+ *                  below -1.86e8 behind inv_temp, has s_rest = 0: kl[r] is infinite, but where p_rest is at most 4e-5 + 2^-22
+ *                  |top_lse[r]|, what a log-sum-exp in 32 bits may leave of a target that masks the same: no such term then
  *   ce[r] = log sum_v exp z[v] - z[label[r]]                                                    (at temperature 1)
  *   grad[r][v] = dloss[r] * d(kl_weight * kl[r] + ce_weight * ce[r]) / d z[v]
  * top_val, top_idx : dev f32, int32 [M][K], 1 <= K <= 1024, as sd_top_logits leaves them.  An index below 0 is no entry (a

@@ -93,6 +93,8 @@ def distill(z: np.ndarray, top_val, top_idx, top_lse, label: int, inv_temp: floa
             if p_rest > 0 and log_rest > REST_IS_NONE:
                 kl += float(p_rest * (np.log(p_rest) - log_rest + lse(z * inv_temp)))
                 g = s - dist - p_rest * np.exp(rest - log_rest)
+            elif p_rest > 4e-5 + 2.0 ** -22 * abs(top_lse):   # (less is what a log-sum-exp in 32 bits leaves)
+                kl, g = np.inf, s - dist
         g *= inv_temp
     g = kl_weight * g
     if 0 <= label < V:

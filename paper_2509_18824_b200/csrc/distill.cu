@@ -66,7 +66,7 @@ struct Turn {
 
 struct RowInfo {                       // prepared ahead
     double mass, plogp;                // sums of p and p log p over them
-    float weight;                      // dloss
+    float weight, rounding;            // dloss; what top_lse in 32 bits may leave of a p_rest that is 0
     int label, any, count;             // any: the row has entries; count: those that lie in this CTA's slice
 };
 // What 2^(x c - r_c) is multiplied with at the entries, 2^(x c - r_rest) elsewhere, 2^(x log2 e - r_e) for the cross-entropy, and what
@@ -320,7 +320,7 @@ __device__ __forceinline__ void prepare_entries(RowInfo& info, const Lists& li, 
     mass = warp_add(mass);
     plogp = warp_add(plogp);
     any = __any_sync(0xffffffffu, any);
-    if (lane == 0) info = RowInfo{mass, plogp, raw.weight, raw.label, any, n};
+    if (lane == 0) info = RowInfo{mass, plogp, raw.weight, fmaf(fabsf(raw.t_lse), 0x1p-22f, 4e-5f), raw.label, any, n};
     __syncwarp();
 }
 
@@ -576,6 +576,7 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
             const double p_unit = rest_too || !(mass > 0.0) ? 1.0 : 1.0 / mass;    // what the list's p are multiples of
             const double p_rest = rest_too ? 1.0 - mass : 0.0;
             const bool has_rest = p_rest > 0.0 && rest > 0.f;
+            const bool masked_rest = info.any && rest == 0.f && p_rest > info.rounding;              // mass that the student can have nowhere
             // (beyond 2^28, powers with R as 32 bits hold it are no longer near 1 at the largest logit: such a row has no loss)
             const bool far = !(fabsf(most * c) <= kFar), far1 = !(fabsf(most * kLog2e) <= kFar);
             // the rest has an R of its own where it lies too far below the largest logit, else that one's
@@ -586,7 +587,7 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
             const float sum = (float)total;
             if (!apart) rest *= at_c;
             if (!two) sum1 = sum;
-            const float all_p = has_rest ? 1.f : (info.any ? (rest_too ? (float)mass : 1.f) : 0.f);
+            const float all_p = has_rest || masked_rest ? 1.f : (info.any ? (rest_too ? (float)mass : 1.f) : 0.f);
             // tail / sum = (all_p - p_rest / s_rest) / sum with s_rest = rest / sum
             const float inv = far ? __int_as_float(0x7fffffff) : 1.f / sum, tail = has_rest ? (apart ? inv * at_c : inv) - (float)p_rest / rest : all_p * inv;
             const RowFactors rf{r_c, apart ? r_own : r_c, r_e, all_p * inv, tail, two ? (far1 ? __int_as_float(0x7fffffff) : 1.f / sum1) : inv, (float)p_unit};
@@ -605,7 +606,7 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
                     if (lane == 0) {
                         double kl = info.any ? own + mass * (log_total + (double)r_c * kLn2) : 0.0;
                         if (has_rest && info.any) kl += p_rest * (log_p + ((double)r_c - (double)rf.r_rest) * kLn2);
-                        a.kl[r] = far ? inv : (float)kl;
+                        a.kl[r] = far ? inv : masked_rest ? INFINITY : (float)kl;
                         if (a.stats)
                             reinterpret_cast<float4*>(a.stats)[r] = apart ? pack_stats(rf, two && a.inv_temp < 1.f, a.inv_temp)
                                                                           : make_float4(most, rf.listed, rf.tail, rf.one);

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from oracle import rows as ref
-from rows_util import TYPES, device_rows, exact_values
+from rows_util import LOWEST, TYPES, device_rows, exact_values
 from test_gpu_rows_distill import grad_alone, loss
 
 pytestmark = pytest.mark.gpu
@@ -104,3 +104,33 @@ def test_in_the_logits_place(kind):
     loss(one, val, idx, t_lse, label, 1.25, (1.0, 0.25), dloss, one)
     grad_alone(two, val, idx, t_lse, label, 1.25, (1.0, 0.25), stats, dloss, two)
     assert torch.equal(one, want) and torch.equal(two, apart)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("mask", ["infinity", "lowest", "far"])
+@pytest.mark.parametrize("M,V", [(6, 40000), (200, 999)])
+def test_a_student_that_masks_everything_outside_the_entries(kind, mask, M, V):
+    """A target that masks the same: its p_rest is a rounding, and no loss.  One that gives the rest half of its mass: an infinite loss, as of
+    a listed token that the student masks."""
+    g = np.random.default_rng(V)
+    K, w, inv_temp = 12, (1.0, 0.25), 1.25
+    x = np.full((M, V), {"infinity": -np.inf, "lowest": LOWEST[kind], "far": -1e9}[mask])
+    idx = np.stack([g.permutation(V)[:K] for _ in range(M)]).astype(np.int32)
+    np.put_along_axis(x, idx.astype(np.int64), g.normal(size=(M, K)) * 2.0, axis=1)
+    t = device_rows(x.astype(np.float32), kind)
+    z = exact_values(t)
+    val, label, dloss = (g.normal(size=(M, K)) * 2.0).astype(np.float32), idx[:, 3].copy(), np.ones(M, dtype=np.float32)
+    t_lse = np.array([ref.lse(v * inv_temp) for v in val.astype(np.float64)], dtype=np.float32)
+    for rest, lse in (("none", t_lse), ("half", t_lse + np.float32(np.log(2.0)))):
+        fused, apart = torch.zeros_like(t), torch.zeros_like(t)
+        kl, ce, stats = loss(t, val, idx, lse, label, inv_temp, w, dloss, fused)
+        grad_alone(t, val, idx, lse, label, inv_temp, w, stats, dloss, apart)
+        want = [ref.distill(z[r], val[r].astype(np.float64), idx[r], float(lse[r]), int(label[r]), inv_temp, *w) for r in range(M)]
+        assert np.isposinf([a for a, _, _ in want]).all() == (rest == "half")
+        # as for the formula's other rows: sums to 2e-6 and one rounding; a gradient's terms to 8e-6 of at most 1, and its rounding
+        for r, (a, b, grad) in enumerate(want):
+            assert kl[r] == a if np.isinf(a) else abs(kl[r] - a) <= 2e-6 + 2.0 ** -23 * abs(a), (rest, r, kl[r], a)
+            assert abs(ce[r] - b) <= 2e-6 + 2.0 ** -23 * abs(b)
+            for got in (fused, apart):
+                got = exact_values(got)[r]
+                assert (np.abs(got - grad) <= torch.finfo(TYPES[kind]).eps / 2 * np.abs(grad) + 2 * 8e-6 * (grad != 0)).all(), (rest, r)

@@ -59,3 +59,18 @@ def test_divergence_of_equal_distributions_is_zero():
     o = rows.in_order(z)[:6]
     kl, ce, g = rows.distill(z, z[o], o, rows.lse(z), -1, 1.0, 1.0, 1.0)
     assert abs(kl) < 1e-14 and ce == 0 and np.abs(g).max() < 1e-15
+
+
+def test_a_student_that_masks_the_rest():
+    """Infinite where the target has mass there, no term where that is a rounding's; a share of any smallness by its logarithm."""
+    z = np.array([1.0, 0.0, -np.inf, -np.inf])
+    idx, val = np.array([0, 1]), np.log(np.array([0.25, 0.25]))
+    kl, _, g = rows.distill(z, val, idx, 0.0, -1, 1.0, 1.0, 0.0)
+    s = np.exp(z[:2]) / np.exp(z[:2]).sum()
+    assert np.isposinf(kl) and g == pytest.approx([s[0] - 0.25, s[1] - 0.25, 0, 0])
+    t_lse = np.float32(rows.lse(val))
+    kl, _, g = rows.distill(z, val, idx, float(t_lse), -1, 1.0, 1.0, 0.0)
+    assert kl == pytest.approx(np.log(0.5) - 0.5 * np.log(s).sum(), abs=1e-6) and g == pytest.approx([s[0] - 0.5, s[1] - 0.5, 0, 0], abs=1e-6)
+    z = np.array([2000.0, 0.0, 0.0])
+    kl, _, g = rows.distill(z, np.log(np.array([0.5])), np.array([0]), 0.0, -1, 1.0, 1.0, 0.0)
+    assert kl == pytest.approx(np.log(0.5) + 0.5 * (2000 - np.log(2))) and g == pytest.approx([0.5, -0.25, -0.25])
