@@ -2,6 +2,7 @@
 #include "common.cuh"
 
 #include <atomic>
+#include <mutex>
 #include <math.h>
 #include <stdlib.h>
 #include <string.h>
@@ -20,6 +21,14 @@ int sm_count(int dev) {
     if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms <= 0) return 148;
     if (cached) cache[dev].store(sms, std::memory_order_relaxed);
     return sms;
+}
+
+bool raise_dynamic_smem(const void* kern, int bytes) {
+    static std::mutex lock;
+    const std::lock_guard<std::mutex> hold(lock);
+    cudaFuncAttributes now;
+    if (cudaFuncGetAttributes(&now, kern) != cudaSuccess) return false;
+    return now.maxDynamicSharedSizeBytes >= bytes || cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess;
 }
 
 // (One pass over the environment: three getenv calls took 0.35 us with 200 variables, a tenth of what the smallest

@@ -26,18 +26,23 @@ inline sd_status cuda_ok(cudaError_t e) { return e == cudaSuccess ? SD_OK : SD_E
 // SM count of device `dev` (asked once per device)
 int sm_count(int dev);
 
-// Opts a kernel into `bytes` of dynamic shared memory, once per kernel and device (the attribute stays set)
+// Opts a kernel into `bytes` of dynamic shared memory.  The limit belongs to the process: raised only, under a lock, so that what one
+// thread has seen to be enough stays enough whatever sizes the others launch.
+bool raise_dynamic_smem(const void* kern, int bytes);
 template <typename Kernel>
 inline bool allow_dynamic_smem(Kernel* kern, int bytes) {
     struct Done { const void* kern; int dev, bytes; };
-    static thread_local Done done[16];                     // (a thread's own, so that no lock is needed)
+    static thread_local Done done[16];                     // (a thread's own: a call that has been made needs no lock)
     static thread_local int next = 0;
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return false;
-    for (const Done& d : done)
-        if (d.kern == reinterpret_cast<const void*>(kern) && d.dev == dev && d.bytes >= bytes) return true;
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
-    done[next++ % 16] = Done{reinterpret_cast<const void*>(kern), dev, bytes};
+    Done* known = nullptr;
+    for (Done& d : done)
+        if (d.kern == reinterpret_cast<const void*>(kern) && d.dev == dev) known = &d;
+    if (known && known->bytes >= bytes) return true;
+    if (!raise_dynamic_smem(reinterpret_cast<const void*>(kern), bytes)) return false;
+    if (!known) known = &done[next++ % 16];
+    *known = Done{reinterpret_cast<const void*>(kern), dev, bytes};
     return true;
 }
 
