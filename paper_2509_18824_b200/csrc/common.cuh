@@ -71,8 +71,8 @@ inline sd_status launch_dependent(void (*kern)(P...), dim3 grid, int threads, si
 
 // Start of such a kernel's work on global memory.  The pointers pass through the asm so that no load from
 // them, read-only ones included, can be moved in front of the wait.  (The read-only path, __ldg, is for what no kernel
-// writes that may still run when this one begins: a caller's inputs, and what the LM-head tiles leave, which let
-// nobody begin early.)
+// writes that may still run when this one begins: block tables, weights and hidden states, and what the LM-head tiles leave, which let
+// nobody begin early.  Logits, draft distributions and log-sum-exps may come from sd_filter_logits and sd_sample_logits: through L2.)
 template <typename Ptr>
 __device__ __forceinline__ void settle(Ptr& p) { asm volatile("" : "+l"(p)); }
 __device__ __forceinline__ void settle(sd_batch& bt) {

@@ -266,7 +266,7 @@ residual_blocksum_kernel(int V, const int32_t* __restrict__ n_excl, const int32_
     if (t < V) {
         if (logits) {
             const int row = stop_row[b];
-            m = __expf(__ldg(logits + (size_t)row * V + t) * inv_temp - lse[row]);
+            m = __expf(__ldcg(logits + (size_t)row * V + t) * inv_temp - lse[row]);
             if (!q_rows || !n_excl[b]) mass[(size_t)b * V + t] = m;
         } else {
             m = mass[(size_t)b * V + t];
@@ -274,7 +274,7 @@ residual_blocksum_kernel(int V, const int32_t* __restrict__ n_excl, const int32_
         const int ne = n_excl[b];
         if (q_rows) {
             if (ne) {
-                m = fmaxf(m - __ldg(q_rows + (size_t)stop_row[b] * V + t), 0.f);
+                m = fmaxf(m - __ldcg(q_rows + (size_t)stop_row[b] * V + t), 0.f);
                 mass[(size_t)b * V + t] = m;
             }
         } else {

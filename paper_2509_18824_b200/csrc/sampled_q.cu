@@ -77,8 +77,8 @@ struct VocabSlice {
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
             const int i = k * kQThreads + tid;
-            p[k] = i < len ? __ldg(logits + i) : -INFINITY;
-            q[k] = (qrow && i < len) ? __ldg(qrow + i) : 0.f;
+            p[k] = i < len ? __ldcg(logits + i) : -INFINITY;
+            q[k] = (qrow && i < len) ? __ldcg(qrow + i) : 0.f;
         }
 #pragma unroll
         for (int k = 0; k < PER; ++k) p[k] = __expf(p[k] * inv_temp - lse);
@@ -254,8 +254,8 @@ tree_walk_q_kernel(sd_batch bt, int V, float inv_temp, const float* lse, const f
         const float* qrow = q_rows + row * V;
         v.load(lrow + v0, qrow + v0, inv_temp, row_lse, tid);
         if (tid < n && sh.par[tid] == cur) {           // p and q of the children's tokens, together with the slices
-            sh.px[tid] = __expf(__ldg(lrow + sh.tok[tid]) * inv_temp - row_lse);
-            sh.qx[tid] = __ldg(qrow + sh.tok[tid]);
+            sh.px[tid] = __expf(__ldcg(lrow + sh.tok[tid]) * inv_temp - row_lse);
+            sh.qx[tid] = __ldcg(qrow + sh.tok[tid]);
         }
         uint64_t kids = ((uint64_t)__ballot_sync(0xffffffffu, par1 == cur) << 32) | __ballot_sync(0xffffffffu, par0 == cur);
         __syncthreads();
@@ -325,7 +325,7 @@ chain_walk_q_logits_kernel(sd_batch bt, int V, float inv_temp, const float* lse,
             const int p = bt.parents[at], x = draft[at];
             const float uq = u[at], qt = q_tok[at], plse = tid > 0 ? lse[at - 1] : 0.f;
             const bool x_ok = x >= 0 && x < V;
-            const float px = tid > 0 && x_ok ? __expf(__ldg(logits + (at - 1) * V + x) * inv_temp - plse) : 0.f;
+            const float px = tid > 0 && x_ok ? __expf(__ldcg(logits + (at - 1) * V + x) * inv_temp - plse) : 0.f;
             sh.tok[tid] = x;
             if (n_ok && tid < n) {
                 if (tid == 0 ? (p != -1) : (p < 0 || p >= tid)) sh.bad = SD_ERR_INVALID_TREE;
