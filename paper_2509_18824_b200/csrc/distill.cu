@@ -688,7 +688,7 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
                 else add(std::false_type{});
                 if (MODE == kLoss) {
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&sh.free_[slot]);
+                    if (lane == 0 && ok) mbar_arrive(&sh.free_[slot]);             // (a copy that has not come is still expected there)
                 }
             }
 
@@ -722,7 +722,8 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
                 const bool same = ((reinterpret_cast<uintptr_t>(grad) ^ reinterpret_cast<uintptr_t>(sl.row.p)) & 15) == 0;
                 uint4* out = reinterpret_cast<uint4*>(reinterpret_cast<uintptr_t>(grad) & ~(uintptr_t)15);
                 at = at0;
-                for (int q = 0; q < sl.pieces; ++q, at.next(slots)) {
+                const int pieces = MODE == kGrad || __all_sync(0xffffffffu, ok) ? sl.pieces : 0;
+                for (int q = 0; q < pieces; ++q, at.next(slots)) {
                     const int slot = at.slot;
                     if (MODE == kGrad) ok = mbar_wait(&sh.picked[slot], at.phase, &sh.abort_flag, wait_cycles) && ok;
                     const uint4* src = ring + slot * kPieceVecs;
@@ -754,7 +755,7 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
                     else if (f.two) all(std::integral_constant<int, 2>{});
                     else all(std::integral_constant<int, 1>{});
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&sh.free_[slot]);
+                    if (lane == 0 && (MODE == kLossGrad || ok)) mbar_arrive(&sh.free_[slot]);
                 }
                 // over what has just been written
                 if (MODE == kGrad) ok = mbar_wait(&sh.sums_full[b], phase_of(n), &sh.abort_flag, wait_cycles) && ok;
