@@ -780,6 +780,7 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(&sh.info_free[b]);
+            if (MODE == kLoss) ok = __all_sync(0xffffffffu, ok);                   // (a warp goes on, or leaves, as one: the bound may run out between its lanes)
             if (!ok) break;
         }
     }

@@ -50,3 +50,13 @@ def test_loss_and_gradient(kind, M, V, withheld):
     assert (beside() == 5.0).all()
     kl, ce, _ = loss(t, val, idx, t_lse, label, 1.0, W, dloss, grad)
     check_few(kind, p, kl, ce, [grad])
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("M,V", SHAPES)
+def test_the_loss_alone(kind, M, V, withheld):
+    p = t, _, val, idx, t_lse, label, _ = problem(M, V, 16, kind, 4, True, 1.0)
+    with withheld:
+        loss(t, val, idx, t_lse, label, 1.0, W, status=sd.SD_ERR_TIMEOUT)
+    kl, ce, _ = loss(t, val, idx, t_lse, label, 1.0, W)
+    check_few(kind, p, kl, ce, [])
