@@ -760,18 +760,18 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
                 // over what has just been written
                 if (MODE == kGrad) ok = mbar_wait(&sh.sums_full[b], phase_of(n), &sh.abort_flag, wait_cycles) && ok;
                 ok = !sum_warps_or(!ok);                                           // (all fourteen come here in every row, whatever they waited for)
-                if (!zero) {
+                if (ok && !zero) {                                                 // (else the list may be another row's)
                     for (int k = tid; k < info.count; k += kSumThreads) {
-                        const int j = li.at[k];
-                        if (j >= kAgain) continue;
+                        const int j = li.at[k], v = j + sl.first;
+                        if (j >= kAgain || v < 0 || v >= a.V) continue;
                         double p = li.p[k];
                         if (sh.dup[b]) {                                           // the same index twice somewhere: all of its masses
                             p = 0.0;
                             for (int x = 0; x < info.count; ++x) p += (li.at[x] & ~kAgain) == j ? li.p[x] : 0.0;
                         }
                         float g = f.at(li.z[k], f.listed, f.r_c) - f.per_p * (float)p;
-                        if (j + sl.first == label) g -= f.per_label;
-                        store_one<T>(grad, j + sl.first, g);
+                        if (v == label) g -= f.per_label;
+                        store_one<T>(grad, v, g);
                     }
                     const int lj = label - sl.first;
                     if (tid == kSumThreads - 1 && has_label && !sh.label_listed[b] && lj >= 0 && lj < (sl.v1 - sl.v0) * E)

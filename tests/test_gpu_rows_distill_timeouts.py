@@ -5,7 +5,7 @@ import torch
 
 from paper_2509_18824_b200 import binding as sd
 from rows_util import TYPES
-from test_gpu_rows_distill import check_rows, loss, problem
+from test_gpu_rows_distill import check_rows, grad_alone, loss, problem
 
 pytestmark = pytest.mark.gpu
 W = (1.0, 0.1)
@@ -60,3 +60,16 @@ def test_the_loss_alone(kind, M, V, withheld):
         loss(t, val, idx, t_lse, label, 1.0, W, status=sd.SD_ERR_TIMEOUT)
     kl, ce, _ = loss(t, val, idx, t_lse, label, 1.0, W)
     check_few(kind, p, kl, ce, [])
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("M,V", SHAPES)
+def test_the_gradient_alone(kind, M, V, withheld):
+    p = t, _, val, idx, t_lse, label, dloss = problem(M, V, 16, kind, 4, True, 1.0)
+    kl, ce, stats = loss(t, val, idx, t_lse, label, 1.0, W)
+    grad, beside = with_gaps(M, V, kind)
+    with withheld:
+        grad_alone(t, val, idx, t_lse, label, 1.0, W, stats, dloss, grad, status=sd.SD_ERR_TIMEOUT)
+    assert (beside() == 5.0).all()
+    grad_alone(t, val, idx, t_lse, label, 1.0, W, stats, dloss, grad)
+    check_few(kind, p, kl, ce, [grad])
