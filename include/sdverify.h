@@ -93,12 +93,15 @@ typedef struct {
 /* Element type of a matrix of logits. */
 typedef enum { SD_F32 = 0, SD_BF16 = 1 } sd_dtype;
 
-/* Sampling parameters of M rows; every pointer is a dev array [M] or NULL (nobody uses it). */
+/* Sampling parameters of M rows; every pointer is a dev array ([M], n_used apart) or NULL (nobody uses it).  Zero what is not set. */
 typedef struct {
     const float *inv_temp;       /* 1 / temperature, at least 1e-6; above 1e30: the first entry alone (NULL: 1) */
     const int32_t *top_k;        /* the k first entries; below 1 or above V - 1: all                           */
     const float *top_p;          /* shortest prefix with this share of their mass; 1 and above: all            */
     const float *min_p;          /* entries with this share of the largest probability; 0 and below: all       */
+    const int32_t *n_used;       /* [M / per]: of every `per` rows the first n_used ones (an sd_batch's n_nodes, with T_max); the others
+                                    count as masked whatever stands in them, their parameters and their uniforms, and are not reported */
+    int32_t per;                 /* at least 1 with n_used                                                      */
 } sd_sampling;
 
 /* Library version (major*100 + minor). */

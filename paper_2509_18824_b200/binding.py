@@ -7,6 +7,7 @@ cannot be loaded, importing this module raises.
 """
 from __future__ import annotations
 
+import copy
 import ctypes as C
 import os
 from typing import List, Optional, Sequence
@@ -56,7 +57,8 @@ class sd_batch(C.Structure):
 
 
 class sd_sampling(C.Structure):
-    _fields_ = [("inv_temp", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p), ("min_p", C.c_void_p)]
+    _fields_ = [("inv_temp", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p), ("min_p", C.c_void_p),
+                ("n_used", C.c_void_p), ("per", C.c_int32)]
 
 
 def _load(path: str = LIB_PATH) -> C.CDLL:
@@ -410,6 +412,14 @@ class Sampling:
         assert all(t.dim() == 1 and t.shape == have[0].shape for t in have), "one value per row in each array"
         self.M = have[0].numel() if have else None
         self.c = sd_sampling(_ptr(self.inv_temp), _ptr(self.top_k), _ptr(self.top_p), _ptr(self.min_p))
+
+    def for_nodes(self, batch: Batch) -> "Sampling":
+        """The same for the B * T_max rows of a batch: rows that no node uses count as masked, and nothing is reported of them."""
+        assert self.M is None or self.M == batch.B * batch.T_max, "one set of sampling parameters per row"
+        of = copy.copy(self)
+        of.batch = batch
+        of.c = sd_sampling(self.c.inv_temp, self.c.top_k, self.c.top_p, self.c.min_p, _ptr(batch.n_nodes), batch.T_max)
+        return of
 
 
 def sd_top_logits(logits, inv_temp: float, values, index, lse, status, stream=None) -> None:

@@ -78,7 +78,8 @@ sd_status check_rows(const void* logits, int32_t dtype, int64_t ld, int32_t M, i
     return SD_OK;
 }
 bool ok_sampling(const sd_sampling* how) {
-    return how && ok_4(how->inv_temp) && ok_4(how->top_k) && ok_4(how->top_p) && ok_4(how->min_p);
+    return how && ok_4(how->inv_temp) && ok_4(how->top_k) && ok_4(how->top_p) && ok_4(how->min_p) && ok_4(how->n_used) &&
+           (!how->n_used || how->per >= 1);
 }
 // the arguments that the two distillation calls share
 sd_status check_distill(const void* logits, int32_t dtype, int64_t ld, int32_t M, int32_t V, const float* top_val, const int32_t* top_idx,

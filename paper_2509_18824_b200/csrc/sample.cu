@@ -906,7 +906,7 @@ top_stream_kernel(const void* logits, long long ld, int V, int M, int steps, int
 // ---------------------------------------------------------------- sampling and filtering
 struct SampleCall {
     const void* logits; long long ld; int V, parts;
-    const float* inv_temp; const int32_t* top_k; const float* top_p; const float* min_p;
+    const float* inv_temp; const int32_t* top_k; const float* top_p; const float* min_p; const int32_t* n_used; int per_used;
     const float* u; int N; int32_t* tokens; float* prob;       // draws (N = 0: none)
     float* dense; bool scaled;                                 // [M][V]: probabilities, or (scaled) the kept logits times inv_temp
     float* lse; int32_t* kept; int32_t* status;
@@ -1197,7 +1197,7 @@ sample_kernel(SampleCall a) {
         sm100::fence_barrier_init();
     }
     __syncthreads();
-    begin_dependent(a.logits, a.inv_temp, a.top_k, a.top_p, a.min_p, a.u, a.tokens, a.prob, a.dense, a.lse, a.kept, a.status);
+    begin_dependent(a.logits, a.inv_temp, a.top_k, a.top_p, a.min_p, a.n_used, a.u, a.tokens, a.prob, a.dense, a.lse, a.kept, a.status);
     const int parts = a.parts, V = a.V;
     const long long r = blockIdx.x / parts;
     const int rank = parts == 1 ? 0 : (int)sm100::cluster_ctarank();
@@ -1209,6 +1209,8 @@ sample_kernel(SampleCall a) {
     int k = a.top_k ? a.top_k[r] : 0;
     float p = a.top_p ? a.top_p[r] : 1.f;
     float mp = a.min_p ? a.min_p[r] : 0.f;
+    const bool used = !a.n_used || (int)(r % a.per_used) < a.n_used[r / a.per_used];
+    if (!used) it = 1.f;
     bool bad = !(it >= 1e-6f);
     if (bad || it > 1e30f) { if (!bad) k = 1; it = 1.f; }                          // infinite: the first entry alone
     if (k >= V) k = 0;
@@ -1223,8 +1225,8 @@ sample_kernel(SampleCall a) {
     const bool ok = all_stay ? sum_all(sh, sl, sc, a.wait_cycles) : first_pass<false>(sh, sl, 0.f, a.wait_cycles);
     sync_parts(parts);
     float top = top_of_parts(sh, parts);
-    bad = bad || top == INFINITY;                                                  // (no distribution)
-    if (bad) top = -INFINITY;
+    bad = bad || (used && top == INFINITY);                                        // (no distribution)
+    if (bad || !used) top = -INFINITY;
     if (top > -INFINITY) sc.from(top);
     if (sc.base != 0.f) all_stay = false;                                          // (its sums are with another base)
     const int ref = top > -INFINITY ? sc.whole(top) : 0;
@@ -1653,7 +1655,7 @@ sd_status launch_sample(const void* logits, int dtype, long long ld, int M, int 
                                 : (held ? sample_kernel<uint16_t, true> : sample_kernel<uint16_t, false>);
     if (!allow_dynamic_smem(kern, smem)) return SD_ERR_CUDA;
     const TestKnobs knobs = test_knobs();
-    const SampleCall call{logits, ld, V, parts, how.inv_temp, how.top_k, how.top_p, how.min_p, u, N, tokens, prob, dense, scaled, lse, kept, dev_status,
+    const SampleCall call{logits, ld, V, parts, how.inv_temp, how.top_k, how.top_p, how.min_p, how.n_used, how.per, u, N, tokens, prob, dense, scaled, lse, kept, dev_status,
                           knobs.withhold ? 16 : 0, knobs.wait_cycles};
     return launch_dependent(kern, dim3((unsigned)M * parts), kThreads, smem, parts, st, call);
 }

@@ -192,14 +192,14 @@ class VerifyStep:
         """The tail for trees whose children were sampled from q_rows [B,T,V], against the target as it would be sampled
         itself: LM head with its logits kept, `how` (temperature, top-k, top-p, min-p; values for the B * T rows) applied to
         them in place, the rejection walk child after child with the given uniforms (u [B,T], w [B]), then compaction.
-        Behind it self.logits holds the filtered rows and self.lse_filtered their log-sum-exp."""
+        Behind it self.logits holds the filtered rows and self.lse_filtered their log-sum-exp (masked rows where no node is)."""
         M, V = self.w.B * self.w.T_max, self.w.V
         if getattr(self, "logits", None) is None:
             f = dict(dtype=torch.float32, device=self.device)
             self.logits, self.lse_filtered, self.lse_kept = torch.zeros((M, V), **f), torch.zeros(M, **f), torch.zeros(M, **f)
         sd.sd_lmhead_stats_logits(self.hidden, self.W, 1.0, None, None, self.lse_kept, self.logits, self.workspace,
                                   self.status, stream)
-        sd.sd_filter_logits(self.logits, how, self.logits, self.lse_filtered, None, self.status, stream)
+        sd.sd_filter_logits(self.logits, how.for_nodes(self.batch), self.logits, self.lse_filtered, None, self.status, stream)
         sd.sd_accept_tree_sampled_q(self.batch, 1.0, self.lse_filtered, self.logits, self.draft_tok, q_rows, u, w,
                                     self.n_acc, self.path, self.out_tok, self.new_len, self.status, stream)
         self.compact(stream)
