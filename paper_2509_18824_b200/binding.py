@@ -401,17 +401,47 @@ def _shaped(t, shape, dtype=torch.float32):
         assert t.shape == shape and t.dtype == dtype, f"expected {dtype} {shape}, got {t.dtype} {tuple(t.shape)}"
 
 
+def _raw_stream(stream) -> int:
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) if stream is None else int(getattr(stream, "cuda_stream", stream))
+
+
 class Sampling:
-    """Owns the per-row arrays named by the C struct ``sd_sampling`` (each a sequence or tensor of M values, or None)."""
+    """Owns the per-row arrays named by the C struct ``sd_sampling`` (each a sequence or tensor of M values, or None).  Arrays that are
+    made here, on the current stream, are ready for calls on any other; a tensor that can be taken as it is stays the caller's."""
 
     def __init__(self, inv_temp=None, top_k=None, top_p=None, min_p=None, device="cuda"):
-        to = lambda a, t: None if a is None else torch.as_tensor(a, dtype=t).contiguous().to(torch.device(device))
+        self._made, self._event = [], None
+
+        def to(a, t):
+            if a is None:
+                return None
+            got = torch.as_tensor(a, dtype=t).contiguous().to(torch.device(device))
+            if got is not a:
+                self._made.append(got)
+                self._event = self._event or (torch.cuda.Event() if torch.is_tensor(a) and a.is_cuda else None)
+            return got
         self.inv_temp, self.top_p, self.min_p = to(inv_temp, torch.float32), to(top_p, torch.float32), to(min_p, torch.float32)
         self.top_k = to(top_k, torch.int32)
         have = [t for t in (self.inv_temp, self.top_k, self.top_p, self.min_p) if t is not None]
         assert all(t.dim() == 1 and t.shape == have[0].shape for t in have), "one value per row in each array"
         self.M = have[0].numel() if have else None
+        self._streams = {_raw_stream(None)} if self._made and self._made[0].is_cuda else set()
+        if self._event is not None:
+            self._event.record()
         self.c = sd_sampling(_ptr(self.inv_temp), _ptr(self.top_k), _ptr(self.top_p), _ptr(self.min_p))
+
+    def on(self, stream) -> int:
+        """The struct's address for a call on `stream` (None: the current one)."""
+        raw = _raw_stream(stream) if self._made else None
+        if raw is not None and raw not in self._streams:
+            self._streams.add(raw)
+            other = torch.cuda.ExternalStream(raw)
+            with torch.cuda.stream(other):
+                if self._event is not None and not torch.cuda.is_current_stream_capturing():       # (a capture begins behind a synchronisation)
+                    other.wait_event(self._event)
+            for t in self._made:
+                t.record_stream(other)
+        return _at(self.c)
 
     def for_nodes(self, batch: Batch) -> "Sampling":
         """The same for the B * T_max rows of a batch: rows that no node uses count as masked, and nothing is reported of them."""
@@ -443,7 +473,7 @@ def sd_sample_logits(logits, how: Sampling, u, tokens, prob, probs, lse, status,
     _shaped(prob, (M, N))
     _shaped(probs, (M, V))
     _shaped(lse, (M,))
-    _check(_n.sd_sample_logits(x, dtype, ld, M, V, _at(how.c), u, N, tokens, prob, probs, lse, status, stream))
+    _check(_n.sd_sample_logits(x, dtype, ld, M, V, how.on(stream), u, N, tokens, prob, probs, lse, status, stream))
 
 
 def sd_filter_logits(logits, how: Sampling, out, lse, kept, status, stream=None) -> None:
@@ -454,7 +484,7 @@ def sd_filter_logits(logits, how: Sampling, out, lse, kept, status, stream=None)
     _shaped(out, (M, V))
     _shaped(lse, (M,))
     _shaped(kept, (M,), torch.int32)
-    _check(_n.sd_filter_logits(x, dtype, ld, M, V, _at(how.c), out, lse, kept, status, stream))
+    _check(_n.sd_filter_logits(x, dtype, ld, M, V, how.on(stream), out, lse, kept, status, stream))
 
 
 def _distill_args(logits, top_val, top_idx, top_lse, label, dloss, grad, stats):
