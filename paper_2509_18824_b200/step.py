@@ -8,6 +8,7 @@ tree K/V and the final hidden states are inputs.)
 """
 from __future__ import annotations
 
+import contextlib
 from typing import List, Optional
 
 import numpy as np
@@ -196,7 +197,9 @@ class VerifyStep:
         M, V = self.w.B * self.w.T_max, self.w.V
         if getattr(self, "logits", None) is None:
             f = dict(dtype=torch.float32, device=self.device)
-            self.logits, self.lse_filtered, self.lse_kept = torch.zeros((M, V), **f), torch.zeros(M, **f), torch.zeros(M, **f)
+            # (on the calls' stream, and not filled: the current one's fill could come behind what they write)
+            with contextlib.nullcontext() if stream is None else torch.cuda.stream(torch.cuda.ExternalStream(getattr(stream, "cuda_stream", stream))):
+                self.logits, self.lse_filtered, self.lse_kept = torch.empty((M, V), **f), torch.empty(M, **f), torch.empty(M, **f)
         sd.sd_lmhead_stats_logits(self.hidden, self.W, 1.0, None, None, self.lse_kept, self.logits, self.workspace,
                                   self.status, stream)
         sd.sd_filter_logits(self.logits, how.for_nodes(self.batch), self.logits, self.lse_filtered, None, self.status, stream)

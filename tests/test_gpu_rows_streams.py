@@ -67,3 +67,24 @@ def test_tensors_that_can_be_taken_as_they_are_stay_the_callers():
     it = torch.ones(3, device="cuda")
     how = sd.Sampling(it, np.full(3, 5))
     assert how.inv_temp is it and how.c.inv_temp == it.data_ptr() and how.top_k.dtype == torch.int32
+
+
+def test_a_step_s_first_call_on_another_stream():
+    """The buffers that the first call makes are not filled behind what it writes."""
+    from paper_2509_18824_b200 import workloads as wl
+    from paper_2509_18824_b200.step import VerifyStep
+    w = wl.make("c5", hidden_gain=12.0, B=3, L=1, V=8192, Hd=128, prefix=100)
+    M = w.B * w.T_max
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    q = torch.softmax(torch.randn((w.B, w.T_max, w.V), device="cuda", generator=g), dim=-1)
+    u, wv = torch.rand((w.B, w.T_max), device="cuda", generator=g), torch.rand(w.B, device="cuda", generator=g)
+    how = sd.Sampling(np.full(M, 0.9), np.full(M, 100))
+    one, two, side = VerifyStep(w), VerifyStep(w), torch.cuda.Stream()
+    one.tail_filtered(how, q, u, wv)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(BUSY)
+    two.tail_filtered(how, q, u, wv, stream=side)
+    torch.cuda.synchronize()
+    for name in ("logits", "lse_filtered", "n_acc", "path", "out_tok", "new_len"):
+        assert torch.equal(getattr(one, name), getattr(two, name)), name
