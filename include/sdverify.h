@@ -481,7 +481,7 @@ sd_status sd_draft_feature_attention(const void *qp, const void *k, const void *
  *            or of a larger matrix; only the base has to be 16-byte aligned), 1 <= V <= 262144
  * Entries of a row stand in the order (logit descending, index ascending).  Entries of minus infinity, and NaN, are masked: they are
  * in no list and have no mass.  A mask's lowest finite value is an ordinary logit.  M rows, up to 2^24; M = 0 does nothing.
- * The small arrays of these calls (one or a few values per row) need the alignment of their elements only.
+ * The small arrays of these calls (one or a few values per row) need the alignment of their elements only (sd_distill_loss's stats: 16 bytes).
  */
 
 /*
@@ -492,7 +492,7 @@ sd_status sd_draft_feature_attention(const void *qp, const void *k, const void *
  *   lse    : NULL, or dev f32 [M]: log sum_v exp(logits[r][v] * inv_temp) (products stop at f32's range); minus infinity for a row
  *            without an unmasked entry
  *   1 <= K <= 1024, inv_temp > 0
- * Every logit is read once.
+ * A row crosses HBM about once; it is passed over again in shared memory, or where rows are many, in L2.
  */
 sd_status sd_top_logits(const void *logits, int32_t dtype, int64_t ld, int32_t M, int32_t V, int32_t K,
                         float inv_temp, float *values, int32_t *index, float *lse,
@@ -511,8 +511,10 @@ sd_status sd_top_logits(const void *logits, int32_t dtype, int64_t ld, int32_t M
  *   probs     : dev f32 [M][V] or NULL: p of the whole row (sd_accept_tree_sampled_q's q_rows); not `logits`
  *   lse       : dev f32 [M] or NULL: log of the mass that stays
  *   1 <= N <= 64
- * An inv_temp below 1e-6 or NaN, or a logit of plus infinity, stores SD_ERR_INVALID_ARG (the row counts as masked).  Masses and their sums are held in 64 bits,
- * so that borders and draws are those of exact arithmetic but for sums within about 1e-10 of a border.
+ * An inv_temp below 1e-6 or NaN, or a logit of plus infinity, stores SD_ERR_INVALID_ARG (the row counts as masked).  Masses and their sums
+ * are held in 64 bits, so that borders and draws are those of exact arithmetic but for sums within about 1e-10 of a border; so are prob and lse,
+ * rounded once.  probs, where thousands of entries stay, come from exponentials in 32 bits: to 1e-5 of themselves, so that a token's may
+ * differ from its prob by as much.
  */
 sd_status sd_sample_logits(const void *logits, int32_t dtype, int64_t ld, int32_t M, int32_t V,
                            const sd_sampling *how, const float *u, int32_t N,
@@ -549,12 +551,12 @@ sd_status sd_filter_logits(const void *logits, int32_t dtype, int64_t ld, int32_
  * top_lse   : dev f32 [M] or NULL, with the same inv_temp
  * label     : dev int32 [M] or NULL; below 0: the row has no cross-entropy (ce 0)
  * kl, ce    : dev f32 [M]; ce may be NULL where label is
- * stats     : NULL, or dev f32 [M][4] that sd_distill_grad reads
+ * stats     : NULL, or dev f32 [M][4], 16-byte aligned, that sd_distill_grad reads
  * dloss     : NULL (1), or dev f32 [M], the rows' weights in what is minimised; a row of weight 0 has gradient 0
  * grad      : NULL (the loss alone), or dev [M][V] of the logits' type, rows grad_ld apart; may be `logits` itself (grad_ld = ld)
  * A row without entries has kl 0.  An index or label of V or more stores SD_ERR_BOUNDS and is left out.  Logits of minus infinity
  * are allowed (kl is infinite where the target gives one mass); NaN, a row of minus infinity alone, or one whose
- * largest |logit * inv_temp| (for ce, |logit|) is beyond 1e8 gives NaN.  With the gradient
+ * largest logit times inv_temp (for ce, largest logit) is beyond 1.86e8 (2^28 ln 2) in size gives NaN.  With the gradient
  * in the same call the logits are read once.
  */
 sd_status sd_distill_loss(const void *logits, int32_t dtype, int64_t ld, int32_t M, int32_t V,

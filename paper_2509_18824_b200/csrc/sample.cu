@@ -80,8 +80,8 @@ struct RowShared {
 };
 
 // ---------------------------------------------------------------- a slice of a row
-// HELD: in the CTA's shared memory.  Otherwise a whole row where it lies (parts = 1): passes over it come from L2, and load four vectors
-// ahead of those that they work on.
+// HELD: in the CTA's shared memory.  Otherwise where the row lies (its share of one, two or four): passes over it come from L2, as far as the
+// resident rows fit there, and load four vectors ahead of those that they work on.
 struct Never {
     __device__ __forceinline__ bool operator()() const { return false; }
 };
