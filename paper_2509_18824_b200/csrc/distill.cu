@@ -10,10 +10,12 @@
 //   join     brings the warps' sums together, and with stores that report to a barrier the CTAs', and writes the losses
 // With the gradient a slice's pieces stay in their slots until the sums are known, the gradient is formed from there, and the next
 // row's pieces follow into the slots one by one; the listed entries' gradients (and the label's) are written over the others' afterwards.
-// 1024 rows of 152064, K = 64: the loss of bf16 78 us (4.0 TB/s), of f32 118 (5.2 TB/s), loss and gradient of bf16 161 (3.9 TB/s read and
-// written), of f32 258 (4.8 TB/s).  bf16 is bound by instructions, 11 per 32 entries and pass (the exponentials' pipe at 50 %); f32 by HBM, of
-// which the time between a row's last piece and its gradient is lost.  Another temperature than 1 with a label costs a second exponential
-// per entry (bf16 115 and 235 us).
+// 1024 rows of 152064, K = 64: the loss of bf16 80 us (3.9 TB/s), of f32 124 (5.0 TB/s), loss and gradient of bf16 161 (3.9 TB/s read and
+// written), of f32 257 (4.8 TB/s), the gradient alone of bf16 111 (5.6 TB/s), of f32 214 (5.8 TB/s).  The loss of bf16 takes 11 instructions per 32
+// entries (the exponentials' pipe at 50 %), its gradient as many again, of which the arithmetic is about four and control the likely rest; f32 is bound by
+// HBM, of which the time between a row's last piece and its gradient is lost.  Another temperature than 1 with a label costs a second
+// exponential per entry (bf16 129 and 255 us).  The join's code is met once a row and has to stay short: 600 cycles of it more, by the instruction
+// caches, took 5 % of the loss.
 // (One row per cluster, all warps doing everything, a bitmap of the listed entries: 4096 rows of bf16 790 us, now 640.  Every CTA preparing the
 // whole list: no slower at K = 64, but 60 % at K = 427 in short rows.  The exponentials of some entries by a polynomial: slower.)
 #include <type_traits>
@@ -790,7 +792,8 @@ distill_kernel(DistillCall a, long long units, int parts, int per, int slots, in
     if (!ok || *reinterpret_cast<volatile int*>(&sh.abort_flag)) unwind_pause();
 }
 
-// CTAs per row: slices of at most four pieces (a slot is left for the next row) where eight CTAs are enough for that, and more of them where the rows leave SMs idle
+// CTAs per row: slices of at most four pieces (a slot is left for the next row) where eight CTAs are enough for that (172 032 f32; five to
+// seven pieces in as many slots beyond), and more of them where the rows leave SMs idle
 static int distill_parts(int M, int nvec, int sms) {
     int parts = 1;
     while (parts < 8 && ((nvec + parts - 1) / parts > (kSlots - 1) * kPieceVecs || ((long long)M * parts <= sms && nvec / (parts * 2) >= kSumThreads))) parts *= 2;

@@ -10,12 +10,15 @@
 // narrowed down by further histograms over the keys.
 //
 // Few rows: one cluster of up to eight CTAs per row, each with a slice of it in its shared memory (bulk copies; 152064 f32 are eight
-// slices of 76 KB, two of which share an SM), read once and passed over as often as it takes.  One such row: k = 50 13 us, any mixture
-// with top-p 42, all entries 17; latency bounds it (copy 3 us, then barriers of the cluster, sorting, the draw).
-// Many rows: passes over L2 with loads ahead in registers, a CTA or a small cluster per row.  Top logits then take one pass with the
-// log-sum-exp and one for the list: 2048 rows of 152064 bf16, K = 64 192 us, 3.2 TB/s, bound by instructions (63 % of the issue
-// slots, XU pipe 38 %) and by what follows a row's passes.  256 rows of 152064 f32: k = 50 72 us, everything 91 (its masses in 64 bits: the
-// fp64 pipe at 39 %), top-p 270 (the histograms' atomics).
+// slices of 76 KB, two of which share an SM; of more than 4812 vectors, vocabularies above 154 000 f32, an SM holds one), read once and passed
+// over as often as it takes.  One such row, which L2 still holds (from HBM): k = 50 14 us (16), top-p 40 (55), all entries 16 (23); latency bounds it
+// (copy 3 us, then barriers of the cluster, sorting, the draw).  The threshold's 128 groups are stretches of the row there: where the large logits
+// stand side by side, the list overflows and a k = 50 takes the histograms' time.
+// Many rows: passes over L2, as far as the resident rows fit there, with loads ahead in registers, a CTA or a small cluster per row.  Top
+// logits then take one pass with the log-sum-exp and one for the list: 2048 rows of 152064 bf16, K = 64 191 us, 3.3 TB/s, of f32 364, 3.4 TB/s
+// (its resident rows are 180 MB, more than L2: both passes come from HBM); bound by instructions (63 % of the issue slots, XU pipe 38 %) and by what follows
+// a row's passes.  256 rows of 152064 f32: k = 50 70 us, everything 90 (its masses in 64 bits: the fp64 pipe at 39 %), top-p 272 (the
+// histograms' atomics).
 // (Lists kept in a single pass over global memory, with a threshold that rises, took three times as long: their cutting and their
 // barriers, 12 of 30 us for one row, and for flat rows four passes through L2.)
 #include <limits.h>
@@ -737,7 +740,7 @@ top_kernel(const void* logits, long long ld, int V, int parts, int K, float inv_
 // next pass's and row's first ones too: no warp waits for another within a pass.  Neighbours in the row belong to different threads, and
 // so to different groups: vocabularies have their frequent tokens side by side.  (With a sixteenth of the row for every warp, 512 rows of bf16
 // whose logits fall along the row took 4900 us, and 59 where they do not.  Clusters that hold a row in shared memory, 4096 rows of 152064
-// bf16: 740 us; a ring of copies for all warps of a CTA 580; one for every warp 850; so 380.)
+// bf16: 740 us; a ring of copies for all warps of a CTA 580; one for every warp 850; so 377 to 399, by the rows.)
 constexpr int kStreamLane = 4;                     // vectors per lane and step
 constexpr int kStreamVecs = kStreamLane * 32;
 
@@ -1600,7 +1603,7 @@ sample_kernel(SampleCall a) {
 // kinds mixed: 235 us in one, 199 in two, 209 in four; 2048 rows: 920, 1026, 1309 us).
 static int shares_of(int M, int sms) { return 4LL * M <= 2 * sms ? 4 : M <= 2 * sms ? 2 : 1; }
 
-// CTAs per row: slices of at most 80 KB while eight are enough for that, and more of them while all run at once, two on an SM, and a warp's
+// CTAs per row: slices of at most 80 KB while eight are enough for that, and more of them while all run at once, and a warp's
 // lanes have a vector each (80 rows of 32003 bf16, top-p: 79 us in one, 60 in two)
 static int parts_for(int M, int nvec, int sms) {
     int parts = 1;
@@ -1623,7 +1626,7 @@ sd_status launch_top_logits(const void* logits, int dtype, long long ld, int M, 
     const bool all_at_once = (long long)M * fit <= 2 * sms - 32;
     if (K <= kSomeK && (M >= sms / 2 || !all_at_once)) {
         auto kern = dtype == SD_F32 ? top_stream_kernel<float> : top_stream_kernel<uint16_t>;
-        // (up to one row per SM: so much shared memory that no SM takes two; 80 rows of f32 27 -> 21 us)
+        // (up to one row per SM: so much shared memory that no SM takes two; 80 rows of f32 27 -> 20 to 25 us, by the rows)
         const int ctas = 2 * sms, steps = (nvec + kWarps * kStreamVecs - 1) / (kWarps * kStreamVecs), alone = M <= sms ? 96 * 1024 : 0;
         if (!allow_dynamic_smem(kern, 96 * 1024)) return SD_ERR_CUDA;
         return launch_dependent(kern, dim3((unsigned)(M < ctas ? M : ctas)), kThreads, alone, 1, st, logits, ld, V, M, steps, K, inv_temp, values, index, lse);
@@ -1644,7 +1647,8 @@ sd_status launch_sample(const void* logits, int dtype, long long ld, int M, int 
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return SD_ERR_CUDA;
     const int nvec = (int)(((long long)V * (dtype == SD_F32 ? 4 : 2) + 15) / 16) + 1;
-    // One reading into shared memory where the SMs hold all clusters at once (and where one CTA holds a row).  Beyond that the waves of
+    // One reading into shared memory where the SMs hold all clusters at once, two CTAs each (slices above 77 KB, of which an SM holds one, then take
+    // two waves), and where one CTA holds a row.  Beyond that the waves of
     // clusters wait for their own copies, and passes through L2 by CTAs of which two are resident are faster.  152064 f32, k = 50 / top_p:
     // 64 rows 36 -> 21 / 108 -> 90 us, 256 rows 101 -> 72 / 368 -> 270 us; 32 rows are as fast, but 57 -> 88 us.
     const int fit = parts_for(M, nvec, sm_count(dev)), sms = sm_count(dev);
