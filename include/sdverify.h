@@ -99,7 +99,7 @@ typedef struct {
     const int32_t *top_k;        /* the k first entries; below 1 or above V - 1: all                           */
     const float *top_p;          /* shortest prefix with this share of their mass; 1 and above: all            */
     const float *min_p;          /* entries with this share of the largest probability; 0 and below: all       */
-    const int32_t *n_used;       /* [M / per]: of every `per` rows the first n_used ones (an sd_batch's n_nodes, with T_max); the others
+    const int32_t *n_used;       /* [M / per, rounded up]: of every `per` rows the first n_used ones (an sd_batch's n_nodes, with T_max); the others
                                     count as masked whatever stands in them, their parameters and their uniforms, and are not reported */
     int32_t per;                 /* at least 1 with n_used                                                      */
 } sd_sampling;

@@ -405,6 +405,12 @@ def _raw_stream(stream) -> int:
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) if stream is None else int(getattr(stream, "cuda_stream", stream))
 
 
+def stream_of(stream) -> "torch.cuda.Stream":
+    """The stream behind an argument, a torch stream or a handle (0: the default stream)."""
+    raw = _raw_stream(stream)
+    return torch.cuda.ExternalStream(raw) if raw else torch.cuda.default_stream()
+
+
 class Sampling:
     """Owns the per-row arrays named by the C struct ``sd_sampling`` (each a sequence or tensor of M values, or None).  Arrays that are
     made here, on the current stream, are ready for calls on any other; a tensor that can be taken as it is stays the caller's."""
@@ -435,7 +441,7 @@ class Sampling:
         raw = _raw_stream(stream) if self._made else None
         if raw is not None and raw not in self._streams:
             self._streams.add(raw)
-            other = torch.cuda.ExternalStream(raw)
+            other = stream_of(raw)
             with torch.cuda.stream(other):
                 if self._event is not None and not torch.cuda.is_current_stream_capturing():       # (a capture begins behind a synchronisation)
                     other.wait_event(self._event)

@@ -198,7 +198,7 @@ class VerifyStep:
         if getattr(self, "logits", None) is None:
             f = dict(dtype=torch.float32, device=self.device)
             # (on the calls' stream, and not filled: the current one's fill could come behind what they write)
-            with contextlib.nullcontext() if stream is None else torch.cuda.stream(torch.cuda.ExternalStream(getattr(stream, "cuda_stream", stream))):
+            with contextlib.nullcontext() if stream is None else torch.cuda.stream(sd.stream_of(stream)):
                 self.logits, self.lse_filtered, self.lse_kept = torch.empty((M, V), **f), torch.empty(M, **f), torch.empty(M, **f)
         sd.sd_lmhead_stats_logits(self.hidden, self.W, 1.0, None, None, self.lse_kept, self.logits, self.workspace,
                                   self.status, stream)

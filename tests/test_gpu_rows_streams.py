@@ -44,6 +44,28 @@ def test_parameters_that_are_converted_on_a_busy_stream(as_argument):
             assert torch.equal(a, b)
 
 
+def test_parameters_that_are_converted_on_a_busy_side_stream():
+    """And read on the default one."""
+    M, V = 12, 5000
+    t, _ = batch(M, V, "f32", 3)
+    params = parameters(M, V, 3, "kpm")
+    want = outputs(M, V)
+    sd.sd_filter_logits(t, sd.Sampling(*params), *want)
+    given = [torch.from_numpy(a).cuda().to(d) for a, d in zip(params, (torch.float64, torch.int64, torch.float64, torch.float64))]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for stream in (None, 0, torch.cuda.default_stream()):
+        got = outputs(M, V)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(BUSY)
+            how = sd.Sampling(*given)
+        sd.sd_filter_logits(t, how, *got, stream=stream)
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+
+
 def test_parameters_outlive_a_call_on_another_stream():
     """Arrays from the host, dropped behind a call that has not begun."""
     M, V = 12, 5000
