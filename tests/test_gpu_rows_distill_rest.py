@@ -134,3 +134,20 @@ def test_a_student_that_masks_everything_outside_the_entries(kind, mask, M, V):
             for got in (fused, apart):
                 got = exact_values(got)[r]
                 assert (np.abs(got - grad) <= torch.finfo(TYPES[kind]).eps / 2 * np.abs(grad) + 2 * 8e-6 * (grad != 0)).all(), (rest, r)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_a_label_whose_cross_entropy_is_out_of_range_and_counts_for_nothing(kind):
+    """Logits whose size a flat temperature brings back in range: the cross-entropy at temperature 1 has none, kl and its gradient are as ever."""
+    M, V, inv_temp, w = 24, 1003, 0.1, (1.0, 0.0)
+    t, z, val, idx, t_lse, label = sure_students(M, V, kind, inv_temp, 11)
+    dloss = np.ones(M, dtype=np.float32)
+    fused, apart = torch.zeros_like(t), torch.zeros_like(t)
+    kl, ce, stats = loss(t, val, idx, t_lse, label, inv_temp, w, dloss, fused)
+    grad_alone(t, val, idx, t_lse, label, inv_temp, w, stats, dloss, apart)
+    far = (z.max(axis=1) > 2.0 ** 28 * np.log(2.0)) & (label >= 0)
+    assert far.any() and not far.all()
+    np.testing.assert_array_equal(np.isnan(ce), far)
+    for r in np.flatnonzero(far):
+        ce[r] = ref.distill(z[r], val[r].astype(np.float64), idx[r], float(t_lse[r]), int(label[r]), inv_temp, *w)[1]
+    check(kind, z, val, idx, t_lse, label, dloss, inv_temp, w, kl, ce, [fused, apart])
