@@ -90,6 +90,33 @@ typedef struct {
                                     i itself or an ancestor of i (sd_tree_prepare)   */
 } sd_batch;
 
+/* Blocks that no request holds: a stack, its top at free_blocks[*n_free - 1]. */
+typedef struct {
+    int32_t *free_blocks;        /* dev [num_blocks]                                 */
+    int32_t *n_free;             /* dev [1]                                          */
+    int32_t num_blocks;          /* blocks of the caches, at most 2^25               */
+} sd_block_pool;
+
+/* New tokens of B requests in packed rows: those of request b from row start[b] on, in order; n_new may be 0.  Scalars are host values;
+ * pointers are dev arrays owned by the caller. */
+typedef struct {
+    int32_t B;                   /* requests, at most 8192                           */
+    int32_t N;                   /* rows of the packed arrays, at least the sum of n_new; at most 2^24.  The rest belongs to nobody */
+    int32_t Hq, Hkv, D;          /* query heads, KV heads, head dim (128)            */
+    int32_t block_size;          /* 64                                               */
+    int32_t max_blocks_per_seq;  /* row stride of block_table                        */
+    int32_t num_blocks;          /* blocks of every cache that the calls are given   */
+    const int32_t *block_table;  /* dev [B][max_blocks_per_seq]                      */
+    const int32_t *n_blocks;     /* dev [B] entries of the table that each request holds, or NULL: all of them.  A request whose blocks
+                                    do not cover len + n_new tokens is left out: its slots are -1, its rows of outputs are not written */
+    const int32_t *len;          /* dev [B] tokens cached in front of the new ones   */
+    const int32_t *n_new;        /* dev [B] new tokens                               */
+    int32_t *start;              /* dev [B + 1] (sd_prompt_prepare)                  */
+    int32_t *slot;               /* dev [N] 64 x block + offset of the row's token, or -1 (sd_prompt_prepare) */
+    int32_t *position;           /* dev [N] its place in its sequence (sd_prompt_prepare); 0 in rows of nobody */
+    void *plan;                  /* dev, sd_prompt_plan_bytes: the attention's work (sd_prompt_prepare); 16-byte aligned */
+} sd_prompts;
+
 /* Element type of a matrix of logits. */
 typedef enum { SD_F32 = 0, SD_BF16 = 1 } sd_dtype;
 
@@ -574,6 +601,64 @@ sd_status sd_distill_grad(const void *logits, int32_t dtype, int64_t ld, int32_t
                           const int32_t *label, float inv_temp, float kl_weight, float ce_weight,
                           const float *stats, const float *dloss, void *grad, int64_t grad_ld,
                           int32_t *dev_status, void *stream);
+
+/*
+ * From requests to a filled cache.  Verification runs over a context (Sec. 4.1: the KV cache is the running context; Sec. 2, long
+ * interleaved prompts of text and images); the calls below build it: blocks for the requests' lengths, the prompts' K and V in them, and
+ * the prompts' own attention.  Lengths stay on the device, so that a step can follow acceptance without the host.  The small int32 arrays
+ * of these calls need the alignment of their elements only.
+ */
+
+/*
+ * Block tables that cover len[b] + n_new[b] tokens, no more and no fewer: requests that hold more blocks give the last ones back, requests
+ * that hold fewer take new ones.  Blocks given back are taken first, in the order of the requests and of their tables, then the stack's from
+ * the top; what is left of the former is pushed so that the first of it comes out first.  So taking and giving back the same leaves the
+ * stack as it was.  Where the supply ends, the first request that it does not suffice for and all behind it that need any get none.
+ *   block_table : dev [B][max_blocks_per_seq], entries beyond n_blocks may hold anything; they are left as they are
+ *   n_blocks    : dev [B], in and out
+ *   len, n_new  : dev [B] (an sd_batch's len and n_nodes for the trees of a step; both 0 for a request that is done)
+ *   granted     : dev [B] or NULL: 1, or 0 for requests that got none
+ * 1 <= B <= 8192.  A negative length stores SD_ERR_INVALID_ARG; more tokens than the table's row holds, or n_blocks or *n_free out of
+ * range, SD_ERR_BOUNDS: that request keeps what it has (with *n_free out of range the stack counts as empty).  The arrays must not overlap.
+ */
+sd_status sd_assign_blocks(const sd_block_pool *pool, int32_t B, int32_t max_blocks_per_seq, int32_t *block_table,
+                           int32_t *n_blocks, const int32_t *len, const int32_t *n_new, int32_t *granted,
+                           int32_t *dev_status, void *stream);
+
+/*
+ * First rows, slots and positions of the packed tokens (start, slot, position), and the plan of their attention, once for all layers of
+ * a step.  To be called again when len, n_new, n_blocks or the tables have changed.  A negative len or n_new stores SD_ERR_INVALID_ARG, a
+ * sum of n_new above N, a table entry outside [0, num_blocks), or without n_blocks a request longer than its row of the table, SD_ERR_BOUNDS.
+ */
+size_t sd_prompt_plan_bytes(const sd_prompts *prompts);
+sd_status sd_prompt_prepare(const sd_prompts *prompts, int32_t *dev_status, void *stream);
+
+/*
+ * K and V of the packed tokens into one layer's cache, byte for byte, at the slots of sd_prompt_prepare.  Rows of nobody and of requests
+ * that were left out are not read.
+ *   k, v : dev bf16, head h of row r at element r * ld + h * 128 (ld >= Hkv * 128, a multiple of 8: views of a projection's output);
+ *          must not overlap the cache
+ */
+sd_status sd_append_kv(const sd_prompts *prompts, const sd_kv_layer *cache, const void *k, int64_t ldk,
+                       const void *v, int64_t ldv, int32_t *dev_status, void *stream);
+
+/*
+ * Causal GQA attention of the packed tokens of one layer (their K and V are in the cache, sd_append_kv): for token i of request b and query
+ * head h   out = softmax(scale * q . K^T) V  over the cached keys t <= len[b] + i.  From one token a request (decoding) to whole prompts,
+ * with or without tokens in front, mixed in any way.
+ *   q, out    : dev bf16, head h of row r at element r * ld + h * 128 (ld >= Hq * 128, a multiple of 8); out must not overlap q
+ *   lse       : dev f32 [N][Hq] or NULL; natural-log sum of exp of the scaled scores
+ *   workspace : dev scratch of at least sd_prompt_workspace_bytes(prompts); calls that may run at the same time need one each
+ * Rows of nobody and of requests that were left out are not written.  Slots behind a request's last token may hold any bit pattern.
+ * Arithmetic: bf16 inputs, fp32 accumulation, weights rounded to bf16 in front of the product with V, bf16 output.  Range as
+ * sd_verify_attention; K and V of the request's own tokens have to be finite.
+ * Errors: SD_ERR_INVALID_ARG, SD_ERR_UNSUPPORTED, SD_ERR_WORKSPACE on the host; SD_ERR_BOUNDS (table entry outside [0, num_blocks)) or
+ * SD_ERR_TIMEOUT through *dev_status.
+ */
+size_t sd_prompt_workspace_bytes(const sd_prompts *prompts);
+sd_status sd_prompt_attention(const sd_prompts *prompts, const sd_kv_layer *cache, const void *q, int64_t ldq,
+                              float scale, void *out, int64_t ldo, float *lse,
+                              void *workspace, size_t workspace_bytes, int32_t *dev_status, void *stream);
 
 #ifdef __cplusplus
 }

@@ -42,7 +42,8 @@ EXPORTS = ["sd_version", "sd_status_string", "sd_workspace_bytes", "sd_tree_prep
            "sd_verify_attention", "sd_verify_attention_layers", "sd_lmhead_argmax", "sd_lmhead_argmax_static", "sd_accept_tree",
            "sd_compact_kv", "sd_lmhead_accept_compact", "sd_lmhead_stats", "sd_accept_tree_sampled", "sd_lmhead_accept_sampled_compact", "sd_accept_chain_sampled", "sd_lmhead_stats_logits", "sd_accept_tree_sampled_q",
            "sd_draft_feature_attention",
-           "sd_top_logits", "sd_sample_logits", "sd_filter_logits", "sd_distill_loss", "sd_distill_grad"]
+           "sd_top_logits", "sd_sample_logits", "sd_filter_logits", "sd_distill_loss", "sd_distill_grad",
+           "sd_assign_blocks", "sd_prompt_plan_bytes", "sd_prompt_prepare", "sd_append_kv", "sd_prompt_workspace_bytes", "sd_prompt_attention"]
 
 
 class sd_kv_layer(C.Structure):
@@ -59,6 +60,17 @@ class sd_batch(C.Structure):
 class sd_sampling(C.Structure):
     _fields_ = [("inv_temp", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p), ("min_p", C.c_void_p),
                 ("n_used", C.c_void_p), ("per", C.c_int32)]
+
+
+class sd_block_pool(C.Structure):
+    _fields_ = [("free_blocks", C.c_void_p), ("n_free", C.c_void_p), ("num_blocks", C.c_int32)]
+
+
+class sd_prompts(C.Structure):
+    _fields_ = [("B", C.c_int32), ("N", C.c_int32), ("Hq", C.c_int32), ("Hkv", C.c_int32), ("D", C.c_int32), ("block_size", C.c_int32),
+                ("max_blocks_per_seq", C.c_int32), ("num_blocks", C.c_int32), ("block_table", C.c_void_p), ("n_blocks", C.c_void_p),
+                ("len", C.c_void_p), ("n_new", C.c_void_p), ("start", C.c_void_p), ("slot", C.c_void_p), ("position", C.c_void_p),
+                ("plan", C.c_void_p)]
 
 
 def _load(path: str = LIB_PATH) -> C.CDLL:
@@ -140,6 +152,18 @@ def _load(path: str = LIB_PATH) -> C.CDLL:
     lib.sd_distill_loss.argtypes = rows + teacher + [C.c_void_p] * 5 + [C.c_int64, C.c_void_p, C.c_void_p]
     lib.sd_distill_grad.restype = C.c_int
     lib.sd_distill_grad.argtypes = rows + teacher + [C.c_void_p] * 3 + [C.c_int64, C.c_void_p, C.c_void_p]
+    lib.sd_assign_blocks.restype = C.c_int
+    lib.sd_assign_blocks.argtypes = [C.c_void_p, C.c_int32, C.c_int32] + [C.c_void_p] * 7
+    lib.sd_prompt_prepare.restype = C.c_int
+    lib.sd_prompt_prepare.argtypes = [C.c_void_p] * 3
+    for sized in (lib.sd_prompt_plan_bytes, lib.sd_prompt_workspace_bytes):
+        sized.restype = C.c_size_t
+        sized.argtypes = [C.c_void_p]
+    lib.sd_append_kv.restype = C.c_int
+    lib.sd_append_kv.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]
+    lib.sd_prompt_attention.restype = C.c_int
+    lib.sd_prompt_attention.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_float, C.c_void_p, C.c_int64, C.c_void_p,
+                                        C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
     return lib
 
 
@@ -527,3 +551,111 @@ def sd_distill_grad(logits, top_val, top_idx, top_lse, label, inv_temp: float, k
     x, dtype, ld, M, V, K, g, g_ld = _distill_args(logits, top_val, top_idx, top_lse, label, dloss, grad, stats)
     _check(_n.sd_distill_grad(x, dtype, ld, M, V, top_val, top_idx, K, top_lse, label, inv_temp, kl_weight, ce_weight, stats, dloss,
                               g, g_ld, status, stream))
+
+
+# ------------------------------------------------------------------ packed new tokens
+def _ints(t, shape, what):
+    assert t.is_cuda and t.dtype == torch.int32 and tuple(t.shape) == shape and t.is_contiguous(), f"{what}: contiguous int32 CUDA tensor {shape}"
+    assert t.get_device() == torch.cuda.current_device(), f"{what} lies on another device than the current one"
+    return t
+
+
+def _heads(t, rows, heads, what):
+    """(address, row stride) of bf16 rows of heads [rows, heads, 128]; rows may lie further apart (a view of a projection's output)."""
+    assert t.is_cuda and t.dtype in (torch.bfloat16, torch.int16, torch.uint16), f"{what}: bf16 CUDA tensor"
+    assert t.get_device() == torch.cuda.current_device(), f"{what} lies on another device than the current one"
+    assert tuple(t.shape) == (rows, heads, 128), f"{what}: expected {(rows, heads, 128)}, got {tuple(t.shape)}"
+    assert t.stride(2) == 1 and (heads == 1 or t.stride(1) == 128), f"{what}: the heads of a row must be contiguous"
+    ld = t.stride(0) if rows > 1 else heads * 128
+    assert ld >= heads * 128, f"{what}: rows must not overlap"
+    return t.data_ptr(), ld
+
+
+class BlockPool:
+    """Owns the arrays named by the C struct ``sd_block_pool``: all blocks free, block 0 on top, or the caller's own stack."""
+
+    def __init__(self, num_blocks: int, free_blocks: Optional[torch.Tensor] = None, n_free: Optional[torch.Tensor] = None, device="cuda"):
+        self.num_blocks = int(num_blocks)
+        if free_blocks is None:
+            free_blocks = torch.arange(self.num_blocks - 1, -1, -1, dtype=torch.int32, device=device)
+            n_free = torch.full((1,), self.num_blocks, dtype=torch.int32, device=device)
+        self.free_blocks = _ints(free_blocks, (self.num_blocks,), "free_blocks")
+        self.n_free = _ints(n_free, (1,), "n_free")
+        self.c = sd_block_pool(self.free_blocks.data_ptr(), self.n_free.data_ptr(), self.num_blocks)
+
+
+def sd_assign_blocks(pool: BlockPool, block_table, n_blocks, lens, n_new, granted, status, stream=None) -> None:
+    """Makes the tables [B, max_blocks] cover lens + n_new tokens (each [B]): n_blocks [B] and the pool are brought up to date,
+    granted [B] (or None) is 0 for requests that the pool did not suffice for."""
+    B, W = block_table.shape
+    _ints(block_table, (B, W), "block_table")
+    _ints(n_blocks, (B,), "n_blocks")
+    _ints(lens, (B,), "lens")
+    _ints(n_new, (B,), "n_new")
+    if granted is not None:
+        _ints(granted, (B,), "granted")
+    _check(_n.sd_assign_blocks(_at(pool.c), B, W, block_table, n_blocks, lens, n_new, granted, status, stream))
+
+
+class Prompts:
+    """New tokens of B requests in N packed rows: owns the arrays named by the C struct ``sd_prompts``.  Tensors that are int32 on
+    the device are taken as they are and may change between calls (sd_prompt_prepare then comes again); others are copied there."""
+
+    def __init__(self, N, Hq, Hkv, D, block_table, lens, n_new, n_blocks=None, num_blocks=None, block_size=64, device="cuda"):
+        dev = torch.device(device)
+        to = lambda a: torch.as_tensor(a, dtype=torch.int32).contiguous().to(dev)
+        self.N, self.Hq, self.Hkv, self.D = int(N), int(Hq), int(Hkv), int(D)
+        self.len, self.n_new = to(lens), to(n_new)
+        self.B = int(self.len.numel())
+        self.block_table = to(block_table).reshape(self.B, -1)
+        self.n_blocks = None if n_blocks is None else to(n_blocks)
+        self.max_blocks, self.num_blocks = int(self.block_table.shape[1]), int(num_blocks)
+        for t in (self.len, self.n_new, self.n_blocks):
+            if t is not None:
+                _ints(t, (self.B,), "lens, n_new and n_blocks")
+        rows = lambda n: torch.empty(max(n, 1), dtype=torch.int32, device=dev)[:n]
+        self.c = sd_prompts(self.B, self.N, self.Hq, self.Hkv, self.D, int(block_size), self.max_blocks, self.num_blocks,
+                            self.block_table.data_ptr(), _ptr(self.n_blocks), self.len.data_ptr(), self.n_new.data_ptr())
+        self.plan = torch.empty(max(int(lib.sd_prompt_plan_bytes(self.ref())), 16), dtype=torch.uint8, device=dev)
+        self.c.plan = self.plan.data_ptr()
+        self.use(rows(self.B + 1), rows(self.N), rows(self.N))
+
+    def use(self, start, slot, position) -> "Prompts":
+        """Puts what sd_prompt_prepare makes into the caller's arrays: start [B + 1], slot and position [N]."""
+        self.start, self.slot, self.position = (_ints(t, (n,), "start, slot and position") for t, n in
+                                                ((start, self.B + 1), (slot, self.N), (position, self.N)))
+        at = lambda t, other: t.data_ptr() or other.data_ptr()                   # (an empty tensor has no address)
+        self.c.start, self.c.slot, self.c.position = start.data_ptr(), at(slot, start), at(position, start)
+        return self
+
+    def ref(self):
+        return C.byref(self.c)
+
+
+def sd_prompt_plan_bytes(prompts: Prompts) -> int:
+    return int(lib.sd_prompt_plan_bytes(prompts.ref()))
+
+
+def sd_prompt_workspace_bytes(prompts: Prompts) -> int:
+    return int(lib.sd_prompt_workspace_bytes(prompts.ref()))
+
+
+def sd_prompt_prepare(prompts: Prompts, status, stream=None) -> None:
+    """First rows, slots and positions of the packed tokens, and the plan of their attention; once for all layers of a step."""
+    _check(_n.sd_prompt_prepare(_at(prompts.c), status, stream))
+
+
+def sd_append_kv(prompts: Prompts, cache: sd_kv_layer, k, v, status, stream=None) -> None:
+    """K and V of the packed tokens, [N, Hkv, 128] each (rows may be strided), into one layer's cache."""
+    k, ldk = _heads(k, prompts.N, prompts.Hkv, "k")
+    v, ldv = _heads(v, prompts.N, prompts.Hkv, "v")
+    _check(_n.sd_append_kv(_at(prompts.c), _at(cache), k, ldk, v, ldv, status, stream))
+
+
+def sd_prompt_attention(prompts: Prompts, cache: sd_kv_layer, q, scale: float, out, lse, workspace, status, stream=None) -> None:
+    """Causal attention of the packed tokens over one layer's cache, which holds their own K and V: q, out [N, Hq, 128] (rows may be
+    strided), lse [N, Hq] f32 or None."""
+    q, ldq = _heads(q, prompts.N, prompts.Hq, "q")
+    out, ldo = _heads(out, prompts.N, prompts.Hq, "out")
+    _shaped(lse, (prompts.N, prompts.Hq))
+    _check(_n.sd_prompt_attention(_at(prompts.c), _at(cache), q, ldq, scale, out, ldo, lse, workspace, workspace, status, stream))

@@ -1,5 +1,6 @@
 // C-ABI entry points: argument validation, then the kernel launchers.
 #include "common.cuh"
+#include "prompt_plan.cuh"
 
 #include <atomic>
 #include <mutex>
@@ -96,6 +97,23 @@ sd_status check_distill(const void* logits, int32_t dtype, int64_t ld, int32_t M
     if (grad == logits && grad_ld != ld) return SD_ERR_INVALID_ARG;
     return SD_OK;
 }
+
+sd_status check_prompts(const sd_prompts* p, bool need_pointers) {
+    if (!p) return SD_ERR_INVALID_ARG;
+    if (p->B < 1 || p->N < 0 || p->Hq < 1 || p->Hkv < 1 || p->max_blocks_per_seq < 1 || p->num_blocks < 1) return SD_ERR_INVALID_ARG;
+    if (p->D != kD || p->block_size != kBlock || p->B > kMaxRequests || p->N > (1 << 24) || p->num_blocks > kMaxPoolBlocks)
+        return SD_ERR_UNSUPPORTED;
+    if (p->Hq % p->Hkv != 0 || p->Hq / p->Hkv > 8 || p->Hq > 1024) return SD_ERR_UNSUPPORTED;
+    if (need_pointers) {
+        if (!p->block_table || !p->len || !p->n_new || !p->start || !p->slot || !p->position || !ok_ptr(p->plan)) return SD_ERR_INVALID_ARG;
+        if (!ok_4(p->block_table) || !ok_4(p->n_blocks) || !ok_4(p->len) || !ok_4(p->n_new) || !ok_4(p->start) || !ok_4(p->slot) ||
+            !ok_4(p->position))
+            return SD_ERR_INVALID_ARG;
+    }
+    return SD_OK;
+}
+// rows of `heads` heads, ld elements apart
+bool ok_heads(const void* x, int64_t ld, int heads) { return ok_ptr(x) && ld >= (int64_t)heads * kD && ld % 8 == 0 && ld < (1ll << 31); }
 
 }  // namespace
 
@@ -389,6 +407,54 @@ sd_status sd_distill_grad(const void* logits, int32_t dtype, int64_t ld, int32_t
     if (!grad || !ok_ptr(stats)) return SD_ERR_INVALID_ARG;
     return launch_distill_grad(DistillCall{logits, ld, V, top_val, top_idx, K, top_lse, label, inv_temp, kl_weight, ce_weight, nullptr, nullptr,
                                            const_cast<float*>(stats), dloss, grad, grad_ld, dev_status}, dtype, M, static_cast<cudaStream_t>(stream));
+}
+
+sd_status sd_assign_blocks(const sd_block_pool* pool, int32_t B, int32_t max_blocks_per_seq, int32_t* block_table,
+                           int32_t* n_blocks, const int32_t* len, const int32_t* n_new, int32_t* granted,
+                           int32_t* dev_status, void* stream) {
+    if (!pool || B < 1 || max_blocks_per_seq < 1 || pool->num_blocks < 1) return SD_ERR_INVALID_ARG;
+    if (B > kMaxRequests || pool->num_blocks > kMaxPoolBlocks) return SD_ERR_UNSUPPORTED;
+    if (!pool->free_blocks || !pool->n_free || !block_table || !n_blocks || !len || !n_new || !dev_status) return SD_ERR_INVALID_ARG;
+    if (!ok_4(pool->free_blocks) || !ok_4(pool->n_free) || !ok_4(block_table) || !ok_4(n_blocks) || !ok_4(len) || !ok_4(n_new) || !ok_4(granted))
+        return SD_ERR_INVALID_ARG;
+    return launch_assign_blocks(*pool, B, max_blocks_per_seq, block_table, n_blocks, len, n_new, granted, dev_status,
+                                static_cast<cudaStream_t>(stream));
+}
+
+size_t sd_prompt_plan_bytes(const sd_prompts* prompts) { return check_prompts(prompts, false) == SD_OK ? prompt_plan_bytes(*prompts) : 0; }
+size_t sd_prompt_workspace_bytes(const sd_prompts* prompts) {
+    return check_prompts(prompts, false) == SD_OK ? prompt_workspace_bytes(*prompts) : 0;
+}
+
+sd_status sd_prompt_prepare(const sd_prompts* prompts, int32_t* dev_status, void* stream) {
+    const sd_status s = check_prompts(prompts, true);
+    if (s != SD_OK) return s;
+    if (!dev_status) return SD_ERR_INVALID_ARG;
+    return launch_prompt_prepare(*prompts, dev_status, static_cast<cudaStream_t>(stream));
+}
+
+sd_status sd_append_kv(const sd_prompts* prompts, const sd_kv_layer* cache, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                       int32_t* dev_status, void* stream) {
+    const sd_status s = check_prompts(prompts, true);
+    if (s != SD_OK) return s;
+    if (!cache || !ok_ptr(cache->k) || !ok_ptr(cache->v) || cache->num_blocks != prompts->num_blocks || !dev_status) return SD_ERR_INVALID_ARG;
+    if (prompts->N == 0) return SD_OK;
+    if (!ok_heads(k, ldk, prompts->Hkv) || !ok_heads(v, ldv, prompts->Hkv)) return SD_ERR_INVALID_ARG;
+    return launch_append_kv(*prompts, *cache, k, ldk, v, ldv, dev_status, static_cast<cudaStream_t>(stream));
+}
+
+sd_status sd_prompt_attention(const sd_prompts* prompts, const sd_kv_layer* cache, const void* q, int64_t ldq, float scale,
+                              void* out, int64_t ldo, float* lse, void* workspace, size_t workspace_bytes,
+                              int32_t* dev_status, void* stream) {
+    const sd_status s = check_prompts(prompts, true);
+    if (s != SD_OK) return s;
+    if (!cache || !ok_ptr(cache->k) || !ok_ptr(cache->v) || cache->num_blocks != prompts->num_blocks || !dev_status) return SD_ERR_INVALID_ARG;
+    if (!(scale > 0.f) || !(scale < INFINITY) || !ok_4(lse) || !ok_ptr(workspace)) return SD_ERR_INVALID_ARG;
+    if (workspace_bytes < prompt_workspace_bytes(*prompts)) return SD_ERR_WORKSPACE;
+    if (prompts->N == 0) return SD_OK;
+    if (!ok_heads(q, ldq, prompts->Hq) || !ok_heads(out, ldo, prompts->Hq) || out == q) return SD_ERR_INVALID_ARG;
+    return launch_prompt_attention(*prompts, *cache, q, ldq, scale, out, ldo, lse, workspace, dev_status,
+                                   static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

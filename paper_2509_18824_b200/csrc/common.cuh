@@ -177,4 +177,15 @@ struct DistillCall {
 sd_status launch_distill_loss(const DistillCall& call, int dtype, int M, cudaStream_t st);
 sd_status launch_distill_grad(const DistillCall& call, int dtype, int M, cudaStream_t st);
 
+// packed new tokens (pages.cu, prompt.cu)
+sd_status launch_assign_blocks(const sd_block_pool& pool, int B, int W, int32_t* table, int32_t* n_blocks, const int32_t* len,
+                               const int32_t* n_new, int32_t* granted, int32_t* dev_status, cudaStream_t st);
+size_t prompt_plan_bytes(const sd_prompts& p);
+size_t prompt_workspace_bytes(const sd_prompts& p);
+sd_status launch_prompt_prepare(const sd_prompts& p, int32_t* dev_status, cudaStream_t st);
+sd_status launch_append_kv(const sd_prompts& p, const sd_kv_layer& cache, const void* k, long long ldk, const void* v, long long ldv,
+                           int32_t* dev_status, cudaStream_t st);
+sd_status launch_prompt_attention(const sd_prompts& p, const sd_kv_layer& cache, const void* q, long long ldq, float scale, void* out,
+                                  long long ldo, float* lse, void* ws, int32_t* dev_status, cudaStream_t st);
+
 }  // namespace sdv

@@ -116,7 +116,8 @@ PyMethodDef kMethods[] = {
     SD_METHOD(sd_lmhead_accept_compact), SD_METHOD(sd_lmhead_stats), SD_METHOD(sd_lmhead_stats_logits),
     SD_METHOD(sd_accept_tree_sampled), SD_METHOD(sd_accept_chain_sampled), SD_METHOD(sd_accept_tree_sampled_q),
     SD_METHOD(sd_lmhead_accept_sampled_compact), SD_METHOD(sd_draft_feature_attention), SD_METHOD(sd_top_logits),
-    SD_METHOD(sd_sample_logits), SD_METHOD(sd_filter_logits), SD_METHOD(sd_distill_loss), SD_METHOD(sd_distill_grad), {nullptr, nullptr, 0, nullptr}};
+    SD_METHOD(sd_sample_logits), SD_METHOD(sd_filter_logits), SD_METHOD(sd_distill_loss), SD_METHOD(sd_distill_grad),
+    SD_METHOD(sd_assign_blocks), SD_METHOD(sd_prompt_prepare), SD_METHOD(sd_append_kv), SD_METHOD(sd_prompt_attention), {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_sdnative", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
