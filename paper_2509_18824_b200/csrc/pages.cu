@@ -143,22 +143,31 @@ sd_status launch_assign_blocks(const sd_block_pool& pool, int B, int W, int32_t*
                             granted, dev_status);
 }
 
-// First rows of the requests, and slot and position of each packed row.
+// First rows of the requests; slot and position of each packed row (all CTAs but the first); the attention's entries (the first).
+namespace {
+constexpr int kOrderBins = 1024;
+constexpr int kEntryTiles = 2;                 // what an entry costs beside its key tiles, in key tiles
+constexpr int kChunkMin = 2;                   // key tiles of the shortest chunk
+}  // namespace
+
 __global__ void __launch_bounds__(kPageThreads)
-prompt_prepare_kernel(sd_prompts p, int32_t* status) {
+prompt_prepare_kernel(sd_prompts p, PromptGeom geom, int32_t* status) {
     extern __shared__ int page_smem[];
     int* const start = page_smem;              // [B + 1]
+    int* const first_entry = page_smem + p.B + 1;        // [B + 1] (the first CTA)
     __shared__ Pair warp_sums[32];
-    begin_dependent(p.block_table, p.n_blocks, p.len, p.n_new, p.start, p.slot, p.position);
+    __shared__ int bins[kOrderBins];
+    __shared__ int n_splits, n_slots, n_entries;
+    begin_dependent(p.block_table, p.n_blocks, p.len, p.n_new, p.start, p.slot, p.position, p.plan);
     const int B = p.B, W = p.max_blocks_per_seq;
-    const bool first = blockIdx.x == 0;
+    const bool planner = blockIdx.x == 0;
     Pair sum{0, 0};
     for (int b0 = 0; b0 < B; b0 += kPageThreads) {
         const int b = b0 + (int)threadIdx.x;
         Pair mine{0, 0};
         if (b < B) {
             const int n = __ldcg(p.n_new + b), l = __ldcg(p.len + b);
-            if ((n < 0 || l < 0) && first) set_status(status, SD_ERR_INVALID_ARG);
+            if ((n < 0 || l < 0) && planner) set_status(status, SD_ERR_INVALID_ARG);
             mine.a = max(n, 0);
         }
         Pair all;
@@ -167,36 +176,122 @@ prompt_prepare_kernel(sd_prompts p, int32_t* status) {
         sum.a += all.a;
     }
     if (threadIdx.x == 0) start[B] = (int)min(sum.a, (long long)p.N);
-    if (first && threadIdx.x == 0 && sum.a > p.N) set_status(status, SD_ERR_BOUNDS);
+    if (planner && threadIdx.x == 0 && sum.a > p.N) set_status(status, SD_ERR_BOUNDS);
     __syncthreads();
-    if (first)
-        for (int b = threadIdx.x; b <= B; b += kPageThreads) p.start[b] = start[b];
-    const int total = start[B];
-    const int r1 = min((int)(blockIdx.x + 1) * kSlotRows, p.N);
-    for (int r = blockIdx.x * kSlotRows + (int)threadIdx.x; r < r1; r += kPageThreads) {
-        int slot = -1, position = 0;
-        if (r < total) {
-            const int b = last_at_most(start, B, r);
-            const RequestSpan q = request_span(p, b, start[b], start[b + 1]);
-            position = max(q.len, 0) + r - start[b];
-            if (q.covered) {
-                const int block = __ldcg(p.block_table + (size_t)b * W + position / kBlock);
-                if (block >= 0 && block < p.num_blocks) slot = block * kBlock + position % kBlock;
-                else set_status(status, SD_ERR_BOUNDS);
-            } else if (!p.n_blocks) {
-                set_status(status, SD_ERR_BOUNDS);
+    if (!planner) {
+        const int total = start[B];
+        const int r0 = ((int)blockIdx.x - 1) * kSlotRows, r1 = min(r0 + kSlotRows, p.N);
+        for (int r = r0 + (int)threadIdx.x; r < r1; r += kPageThreads) {
+            int slot = -1, position = 0;
+            if (r < total) {
+                const int b = last_at_most(start, B, r);
+                const RequestSpan q = request_span(p, b, start[b], start[b + 1]);
+                position = max(q.len, 0) + r - start[b];
+                if (q.covered) {
+                    const int block = __ldcg(p.block_table + (size_t)b * W + position / kBlock);
+                    if (block >= 0 && block < p.num_blocks) slot = block * kBlock + position % kBlock;
+                    else set_status(status, SD_ERR_BOUNDS);
+                } else if (!p.n_blocks) {
+                    set_status(status, SD_ERR_BOUNDS);
+                }
             }
+            p.slot[r] = slot;
+            p.position[r] = position;
         }
-        p.slot[r] = slot;
-        p.position[r] = position;
+        return;
     }
+    // ------------------------------------------------------------ entries
+    const int pair = 2 * geom.tokens;
+    int at = 0;
+    for (int b0 = 0; b0 < B; b0 += kPageThreads) {
+        const int b = b0 + (int)threadIdx.x;
+        Pair mine{0, 0};
+        if (b < B) {
+            p.start[b] = start[b];
+            const RequestSpan q = request_span(p, b, start[b], start[b + 1]);
+            if (q.covered) mine.a = (q.n + pair - 1) / pair;
+        }
+        Pair all;
+        const Pair before = block_scan(mine, warp_sums, &all);
+        if (b < B) first_entry[b] = at + (int)before.a;
+        at += (int)all.a;
+    }
+    if (threadIdx.x == 0) {
+        p.start[B] = start[B];
+        first_entry[B] = at;
+        n_splits = n_slots = n_entries = 0;
+    }
+    for (int i = threadIdx.x; i < kOrderBins; i += kPageThreads) bins[i] = 0;
+    __syncthreads();
+    const int total = min(at, geom.cap_entries);
+    // entry e with all its keys
+    const auto whole = [&](int e) {
+        PromptEntry x;
+        x.b = last_at_most(first_entry, B, e);
+        const int len = __ldcg(p.len + x.b), n = start[x.b + 1] - start[x.b], t0 = (e - first_entry[x.b]) * pair;
+        x.row0 = start[x.b] + t0;
+        x.pos0 = len + t0;
+        x.tokens = min(pair, n - t0);
+        x.kb0 = 0;
+        x.kb1 = (x.pos0 + x.tokens + kBlock - 1) / kBlock;
+        x.end = len + n;
+        x.slot = -1;
+        return x;
+    };
+    Pair cost{0, 0};
+    for (int e = threadIdx.x; e < total; e += kPageThreads) cost.a += (whole(e).kb1 + 1) / 2 + kEntryTiles;
+    Pair all;
+    block_scan(cost, warp_sums, &all);
+    // An entry is cut where it is longer than a CTA's share of all of them; into chunks of half a share, so that what the CTAs take adds
+    // up more evenly.
+    const long long share = (all.a * p.Hkv + 2 * geom.sms - 1) / (2 * geom.sms);
+    const int chunk = (int)min(max(share, (long long)kChunkMin), 1ll << 24);
+    const auto chunks_of = [&](int tiles) { return tiles >= 2 * chunk ? (tiles + chunk - 1) / chunk : 1; };
+    const auto bin_of = [&](int tiles) { return kOrderBins - 1 - min(tiles, kOrderBins - 1); };
+    for (int e = threadIdx.x; e < total; e += kPageThreads) {
+        const int tiles = (whole(e).kb1 + 1) / 2, n = chunks_of(tiles), per = (tiles + n - 1) / n;
+        for (int c = 0; c < n; ++c) atomicAdd(&bins[bin_of(min(per, tiles - c * per))], 1);
+    }
+    __syncthreads();
+    {
+        static_assert(kOrderBins == kPageThreads, "");
+        const Pair here{bins[threadIdx.x], 0};
+        const Pair before = block_scan(here, warp_sums, &all);
+        bins[threadIdx.x] = (int)before.a;
+    }
+    __syncthreads();
+    PromptEntry* const entries = plan_entries(p.plan);
+    PromptSplit* const splits = plan_splits(p.plan, geom.cap_entries);
+    for (int e = threadIdx.x; e < total; e += kPageThreads) {
+        PromptEntry x = whole(e);
+        const int tiles = (x.kb1 + 1) / 2, n = chunks_of(tiles), per = (tiles + n - 1) / n, last = x.kb1;
+        int slot = -1;
+        if (n > 1) {
+            slot = atomicAdd(&n_slots, n * p.Hkv);
+            splits[atomicAdd(&n_splits, 1)] = PromptSplit{x.row0, x.tokens, slot, n};
+        }
+        for (int c = 0; c < n; ++c) {
+            x.kb0 = 2 * c * per;
+            x.kb1 = min(2 * (c + 1) * per, last);
+            x.slot = n > 1 ? slot + c * p.Hkv : -1;
+            entries[atomicAdd(&bins[bin_of(min(per, tiles - c * per))], 1)] = x;
+            atomicAdd(&n_entries, 1);
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) *plan_header(p.plan) = PromptHeader{n_entries, n_splits, n_slots, 0};
+}
+
+size_t prompt_plan_bytes(const sd_prompts& p) {
+    const PromptGeom g = prompt_geom(p, current_sms());
+    return sizeof(PromptHeader) + (size_t)g.cap_entries * sizeof(PromptEntry) + (size_t)g.cap_splits * sizeof(PromptSplit);
 }
 
 sd_status launch_prompt_prepare(const sd_prompts& p, int32_t* dev_status, cudaStream_t st) {
-    const int smem = (p.B + 1) * 4;
+    const int smem = 2 * (p.B + 1) * 4;
     if (!allow_dynamic_smem(prompt_prepare_kernel, smem)) return SD_ERR_CUDA;
-    const int ctas = p.N <= kSlotRows ? 1 : (p.N + kSlotRows - 1) / kSlotRows;
-    return launch_dependent(prompt_prepare_kernel, dim3(ctas), kPageThreads, smem, 1, st, p, dev_status);
+    return launch_dependent(prompt_prepare_kernel, dim3(1 + (p.N + kSlotRows - 1) / kSlotRows), kPageThreads, smem, 1, st, p,
+                            prompt_geom(p, current_sms()), dev_status);
 }
 
 // A token's K and V rows of all KV heads (256 bytes a head) into its slot; unit of work = one 16-byte vector of each.
