@@ -201,7 +201,6 @@ prompt_prepare_kernel(sd_prompts p, PromptGeom geom, int32_t* status) {
         return;
     }
     // ------------------------------------------------------------ entries
-    const int pair = 2 * geom.tokens;
     int at = 0;
     for (int b0 = 0; b0 < B; b0 += kPageThreads) {
         const int b = b0 + (int)threadIdx.x;
@@ -209,7 +208,7 @@ prompt_prepare_kernel(sd_prompts p, PromptGeom geom, int32_t* status) {
         if (b < B) {
             p.start[b] = start[b];
             const RequestSpan q = request_span(p, b, start[b], start[b + 1]);
-            if (q.covered) mine.a = (q.n + pair - 1) / pair;
+            if (q.covered) mine.a = (q.n + geom.tokens - 1) / geom.tokens;
         }
         Pair all;
         const Pair before = block_scan(mine, warp_sums, &all);
@@ -228,10 +227,10 @@ prompt_prepare_kernel(sd_prompts p, PromptGeom geom, int32_t* status) {
     const auto whole = [&](int e) {
         PromptEntry x;
         x.b = last_at_most(first_entry, B, e);
-        const int len = __ldcg(p.len + x.b), n = start[x.b + 1] - start[x.b], t0 = (e - first_entry[x.b]) * pair;
+        const int len = __ldcg(p.len + x.b), n = start[x.b + 1] - start[x.b], t0 = (e - first_entry[x.b]) * geom.tokens;
         x.row0 = start[x.b] + t0;
         x.pos0 = len + t0;
-        x.tokens = min(pair, n - t0);
+        x.tokens = min(geom.tokens, n - t0);
         x.kb0 = 0;
         x.kb1 = (x.pos0 + x.tokens + kBlock - 1) / kBlock;
         x.end = len + n;

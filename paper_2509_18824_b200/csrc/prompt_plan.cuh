@@ -20,13 +20,13 @@ __device__ __forceinline__ RequestSpan request_span(const sd_prompts& p, int b, 
 }
 
 // ---------------------------------------------------------------- the attention's work
-// A row tile is the query heads of one KV head for whole tokens, at most 128 rows; an entry is a pair of row tiles (or one, where a request
-// has no more tokens) and the key tiles [kt0, kt1) of its request; every KV head has the same entries.  Entries are in order of their
-// length, the longest first; CTA c of the attention's grid takes number c, then 2 G - 1 - c, 2 G + c, ...
+// A row tile is the query heads of one KV head for whole tokens, at most 128 rows; an entry is a row tile and the key blocks [kb0, kb1) of
+// its request; every KV head has the same entries.  Entries are in order of their length, the longest first; CTA c of the attention's grid
+// takes number c, then 2 G - 1 - c, 2 G + c, ...
 constexpr int kPromptTile = 128;               // keys per tile: two cache blocks
 struct alignas(16) PromptEntry {
     int row0, pos0;        // packed row and place in the sequence of the entry's first token
-    int tokens;            // of up to two row tiles
+    int tokens;
     int b;
     int kb0, kb1;          // key blocks (kb0 even)
     int end;               // len + n_new of the request
@@ -39,11 +39,11 @@ struct PromptGeom {
     int G;                 // query heads of a KV head
     int tokens;            // of a row tile
     int cap_entries, cap_splits, cap_slots;
-    int tiles, rows;       // row tiles, and rows of each, of a partial result
+    int rows;              // of a partial result
     int sms;
     int g_magic;           // ceil(65536 / G): row / G for rows below 128
     __host__ __device__ __forceinline__ int token_of(int row) const { return (row * g_magic) >> 16; }
-    __host__ __device__ __forceinline__ size_t slot_floats() const { return (size_t)tiles * rows * (kD + 2); }
+    __host__ __device__ __forceinline__ size_t slot_floats() const { return (size_t)rows * (kD + 2); }
 };
 inline PromptGeom prompt_geom(const sd_prompts& p, int sms) {
     PromptGeom g;
@@ -54,9 +54,8 @@ inline PromptGeom prompt_geom(const sd_prompts& p, int sms) {
     // (chunk_tiles: a chunk is at least a 2 sms-th of all key tiles of all heads, and what is cut at least two of them long)
     g.cap_slots = 4 * sms + p.Hkv;
     g.cap_splits = 2 * sms / p.Hkv + 2;
-    g.cap_entries = p.N / (2 * g.tokens) + (p.B < p.N ? p.B : p.N) + 4 * sms / p.Hkv + 4;
+    g.cap_entries = p.N / g.tokens + (p.B < p.N ? p.B : p.N) + 4 * sms / p.Hkv + 4;
     const long long rows = (long long)p.N * g.G;
-    g.tiles = p.N > g.tokens ? 2 : 1;
     g.rows = rows >= 128 ? 128 : (int)((rows + 7) / 8 * 8);
     return g;
 }
