@@ -16,8 +16,8 @@
 namespace sdv {
 
 namespace {
-constexpr int kPThreads = 480;                 // warps 0-3, 4-7 soft-max, 8-11 results, 12 products, 13 K and Q copies, 14 V copies
-constexpr int kPMmaWarp = 12, kPKeyWarp = 13, kPValueWarp = 14;
+constexpr int kPThreads = 512;                 // warps 0-3, 4-7 soft-max, 8-11 results, 12 scores, 13 products with V, 14 K and Q copies, 15 V copies
+constexpr int kPScoreWarp = 12, kPProductWarp = 13, kPKeyWarp = 14, kPValueWarp = 15;
 constexpr int kPStages = 3;                    // K and V ring slots, score buffers
 constexpr int kPWorks = 4;                     // pieces of work that are known ahead
 constexpr int kPHalf = kPromptTile * 128;      // bytes of one D-half of a key tile: [128 keys][64] bf16, swizzled (16 KiB)
@@ -25,10 +25,7 @@ constexpr int kPStage = 2 * kPHalf;
 constexpr int kPQBytes = 2 * kRowTile * 128;
 constexpr int kPBars = 512;                    // barriers, two words and the pieces of work
 constexpr int kPSmem = kPQBytes + 2 * kPStages * kPStage + kPBars + 5 * kRowTile * 4;
-#ifndef POLY
-#define POLY 4
-#endif
-constexpr int kPolyPairs = POLY;
+constexpr int kSoftmaxRegs = 152, kOtherRegs = 104;        // registers of a thread: 8 warps x 152 + 8 x 104 = 16 x 128, what the launch has
 constexpr int kMergeThreads = 256;
 
 struct PromptShared {
@@ -46,8 +43,8 @@ struct PromptShared {
     uint64_t* o_empty;      // results -> MMA, soft-max: O, references and sums have been read
     uint64_t* sum_full;     // [2] soft-max group -> results: references and sums
     uint64_t* work_full;    // [4] K copies -> the others: a piece of work
-    uint64_t* work_empty;   // [4] the others (14 warps) -> K copies: it has been read
-    uint64_t* unwound;      // MMA: every product that was issued has completed
+    uint64_t* work_empty;   // [4] the others (15 warps) -> K copies: it has been read
+    uint64_t* unwound;      // [2] MMA: everything that either warp has issued has completed
     uint32_t* tmem_slot;
     int* abort_flag;
     int* works;             // [4][10]
@@ -63,8 +60,8 @@ struct PromptShared {
         k_full = bars; v_full = bars + 3; s_full = bars + 6; v_empty = bars + 9; p_full = bars + 12; commit = bars + 15; ref_full = bars + 19;
         q_full = bars + 27; q_empty = bars + 28; o_full = bars + 29; o_empty = bars + 30; sum_full = bars + 31;
         work_full = bars + 33; work_empty = bars + 37; unwound = bars + 41;
-        tmem_slot = reinterpret_cast<uint32_t*>(bars + 42);
-        abort_flag = reinterpret_cast<int*>(bars + 42) + 1;
+        tmem_slot = reinterpret_cast<uint32_t*>(bars + 43);
+        abort_flag = reinterpret_cast<int*>(bars + 43) + 1;
         works = reinterpret_cast<int*>(bars + 44);
         static_assert(44 * 8 + kPWorks * 40 <= kPBars, "");
         refs = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(bars) + kPBars);
@@ -80,8 +77,8 @@ struct PromptShared {
         for (int i = 0; i < 4; ++i) { mbar_init(&commit[i], 1); mbar_init(&ref_full[i], 1); mbar_init(&ref_full[4 + i], 1); }
         mbar_init(q_full, 1); mbar_init(q_empty, 1); mbar_init(o_full, 1); mbar_init(o_empty, 4);
         mbar_init(&sum_full[0], 4); mbar_init(&sum_full[1], 4);
-        for (int i = 0; i < kPWorks; ++i) { mbar_init(&work_full[i], 1); mbar_init(&work_empty[i], 14); }
-        mbar_init(unwound, 1);
+        for (int i = 0; i < kPWorks; ++i) { mbar_init(&work_full[i], 1); mbar_init(&work_empty[i], 15); }
+        mbar_init(&unwound[0], 1); mbar_init(&unwound[1], 1);
     }
 };
 static_assert(kPSmem <= 227 * 1024, "");
@@ -144,56 +141,11 @@ __device__ __forceinline__ void done_with_work(const PromptShared& sh, RingAt<kP
     at.next();
 }
 
-__device__ __forceinline__ void halves(uint64_t x, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(x)); }
 __device__ __forceinline__ uint64_t twice(float c) { return pack_f32x2(c, c); }
-__device__ __forceinline__ float min3(float a, float b, float c) {
-    float d;
-    asm("min.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-    return d;
-}
-
-// 32 raw scores of a row -> 2^(score * scale - reference), packed to bf16 in pairs, and added to the sums.  kPolyPairs of the sixteen pairs go
-// through the multiply-add units: x = n + f with n whole and f in [-1/2, 1/2], n by adding 1.5 x 2^23 (Cody and Waite's reduction; the
-// reference is a whole number, so that one multiply-add gives it), 2^f by its minimax polynomial of degree 4 (least relative error, 2.6e-6,
-// by reweighted least squares), n added to the exponent's bits.  That is right for |n| <= 126; lo, hi: the smallest and largest 1.5 x 2^23 + n.
-constexpr float kShift = 12582912.f;
-__device__ __forceinline__ void exp_block(const uint32_t (&r)[32], uint64_t scale2, float m, uint32_t* pk, uint64_t (&ps)[2], float& lo, float& hi) {
-    const uint64_t neg_m2 = twice(-m), shift = twice(kShift - m);
-#pragma unroll
-    for (int c = 0; c < 16; ++c) {
-        const uint64_t s = pack_f32x2(__uint_as_float(r[2 * c]), __uint_as_float(r[2 * c + 1]));
-        float y0, y1;
-        if (c * kPolyPairs / 16 != (c + 1) * kPolyPairs / 16) {
-            const uint64_t t = fma_f32x2(s, scale2, shift);
-            const uint64_t f = fma_f32x2(s, scale2, fma_f32x2(t, twice(-1.f), shift));
-            uint64_t q = fma_f32x2(f, twice(0x1.3997d4p-7f), twice(0x1.ca1440p-5f));
-            q = fma_f32x2(q, f, twice(0x1.ec06dap-3f));
-            q = fma_f32x2(q, f, twice(0x1.62e0dcp-1f));
-            q = fma_f32x2(q, f, twice(0x1.ffffe8p-1f));
-            float t0, t1, q0, q1;
-            halves(t, t0, t1);
-            halves(q, q0, q1);
-            lo = min3(lo, t0, t1);
-            hi = max3(hi, t0, t1);
-            y0 = __uint_as_float(__float_as_uint(q0) + (__float_as_uint(t0) << 23));
-            y1 = __uint_as_float(__float_as_uint(q1) + (__float_as_uint(t1) << 23));
-        } else {
-            float x0, x1;
-            halves(fma_f32x2(s, scale2, neg_m2), x0, x1);
-            y0 = ex2_approx(x0);
-            y1 = ex2_approx(x1);
-        }
-        ps[c & 1] = add_f32x2(ps[c & 1], pack_f32x2(y0, y1));
-        const __nv_bfloat162 h = __floats2bfloat162_rn(y0, y1);
-        pk[c] = *reinterpret_cast<const uint32_t*>(&h);
-    }
-}
-
 // What the soft-max of a row hands from tile to tile.
 struct RowState {
     float m, l;             // reference (a whole number) and sum of the weights relative to it
     float raised;           // what this tile has scaled the row by
-    int usual;              // every reference of the warp is small enough for exp_block
     int ok;                 // no wait ran out
 };
 struct TileAt {
@@ -201,19 +153,18 @@ struct TileAt {
     int vis;                // keys of the tile that this row sees
     int blocks;             // of 64 keys, 1 or 2
     int first;              // the first tile of an entry
-    uint64_t *ref_full, *commit, *o_done;
-    uint32_t commit_phase, o_phase;
-    int begun;              // there is a tile before this one in the stream
+    uint64_t* o_done;       // O updated by the tile before
+    uint32_t o_phase;
     int row_ok;
 };
-// A tile from block hb on, looked at before anything is weighed: masks, the reference of an entry's first tile, references that have to be
-// raised (by the largest score, where that is more than 2^32 above), and what exp_block does not take.  (A call: in line it made the usual
-// tile's code slower.)
+// A tile from block hb on (the tile before it is final), looked at before anything is weighed: the reference that another tile has raised since, and
+// references that have to be raised (to the largest score, where that is more than 2^32 above).  (A call: in line it made the usual tile's
+// code slower.)
 __device__ __noinline__ RowState careful_tile(RowState st, const TileAt t, int hb, float scale_log2, volatile float* my_ref, int* abort_flag,
                                               long long limit) {
     const uint64_t scale2 = twice(scale_log2);
-    const int lane = threadIdx.x & 31;
-    tmem_ld_wait();
+    const float ref = *my_ref;
+    if (ref != st.m) { st.l *= exp2f(st.m - ref); st.m = ref; }
 #pragma unroll 1
     for (; hb < t.blocks; ++hb) {
         const uint32_t tb = t.ts + hb * kBlock;
@@ -230,18 +181,6 @@ __device__ __noinline__ RowState careful_tile(RowState st, const TileAt t, int h
             for (int x = 0; x < 32; x += 2) mt = max3(mt, __uint_as_float(s[x]), __uint_as_float(s[x + 1]));
         }
         mt = t.row_ok ? rintf(mt * scale_log2) : -INFINITY;
-        if (hb == 0) {
-            if (t.first) {
-                st.m = mt > -INFINITY ? mt : 0.f;          // (no key: the row has no weight here)
-                *my_ref = st.m;
-                __syncwarp();
-                if (lane == 0) mbar_arrive(t.ref_full);
-            }
-            // the tile before is final, and so is its reference
-            if (t.begun && !mbar_wait_warp(t.commit, t.commit_phase, abort_flag, limit)) { st.ok = 0; return st; }
-            const float ref = *my_ref;
-            if (ref != st.m) { st.l *= exp2f(st.m - ref); st.m = ref; }
-        }
         const bool raise = mt > st.m + kRaiseAbove;
         if (__any_sync(0xffffffffu, raise)) {
             const float alpha = raise ? exp2f(st.m - mt) : 1.f;                // (a power of two: weights of the first block stay exact)
@@ -288,7 +227,6 @@ __device__ __noinline__ RowState careful_tile(RowState st, const TileAt t, int h
         st.l += sum_f32x2(add_f32x2(ps[0], ps[1]));
         tmem_st_wait();
     }
-    st.usual = !__any_sync(0xffffffffu, !(fabsf(st.m) < 2097152.f));
     return st;
 }
 }  // namespace
@@ -328,6 +266,9 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
     const uint32_t tmem_s = tmem + kD;
     griddep_wait();                                        // global memory from here on
 
+    bool ok = true;                                        // no wait has run out
+    if (warp >= 12) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     if (warp == kPKeyWarp || warp == kPValueWarp) {
         // ------------------------------------------------------------ copies (whole warps in uniform control flow)
         const bool keys = warp == kPKeyWarp;
@@ -338,7 +279,6 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
         RingAt<kPStages> at;
         RingAt<kPWorks> work_at;
         uint32_t q_phase = 1u;                             // (empty at first)
-        bool ok = true;
         RawWork raw;
         int entries = 0;
         if (keys) {
@@ -401,92 +341,77 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
                 }
             }
         }
-        if (!ok) {
-            if (lane == 0) set_status(status, SD_ERR_TIMEOUT);
-            unwind_pause();
-        }
-    } else if (warp == kPMmaWarp) {
-        // ------------------------------------------------------------ products (a whole warp in uniform control flow)
-        const uint32_t idesc_s = make_idesc_bf16(kRowTile, kPromptTile, false, false), idesc_s_half = make_idesc_bf16(kRowTile, kBlock, false, false);
-        const uint32_t idesc_o = make_idesc_bf16(kRowTile, kD, false, true);
-        const uint64_t q_desc = make_smem_desc(smem_u32(sh.q_smem), 16, 1024, 128);
-        const uint64_t k_desc = make_smem_desc(smem_u32(sh.k_smem), 16, 1024, 128);
-        const uint64_t v_desc = make_smem_desc(smem_u32(sh.v_smem), kPHalf, 1024, 128);   // [key][d]: N (= d) contiguous
-        RingAt<kPStages> s_at, o_at;
-        RingAt<kPWorks> s_work, o_work;                    // the scores may be two entries ahead of the products with V
-        uint32_t q_phase = 0u, o_phase = 1u;
-        int s_nb = 0, s_j = 0, o_nb = 0, o_j = 0;          // blocks and next tile of the entry that either is in
-        bool ok = true, more = true;
-        PromptWork w;
-        const auto scores = [&] {
-            if (2 * s_j >= s_nb) {
-                if (!(ok = see_work(sh, s_work, w, limit))) return;
-                s_work.next();
-                s_nb = w.nb;
-                s_j = 0;
-                if (s_nb == 0) { more = false; return; }
-                if (!(ok = mbar_wait_warp(sh.q_full, q_phase, abort_flag, limit))) return;
-                q_phase ^= 1u;
-            }
-            if (!(ok = mbar_wait_warp(&sh.k_full[s_at.slot], s_at.phase, abort_flag, limit))) return;
-            tc_fence_after_sync();
-            const uint64_t kd = k_desc + (uint64_t)(s_at.slot * (kPStage >> 4));
-            const uint32_t d = tmem_s + s_at.slot * kPromptTile;
-            const uint32_t idesc = 2 * s_j + 1 < s_nb ? idesc_s : idesc_s_half;
-            ++s_j;
-            if (elect_one()) {
-#pragma unroll
-                for (int k = 0; k < kD / 16; ++k)
-                    mma_ss(d, q_desc + (uint64_t)((k >> 2) * ((kRowTile * 128) >> 4) + (k & 3) * 2),
-                           kd + (uint64_t)((k >> 2) * (kPHalf >> 4) + (k & 3) * 2), idesc, k != 0 ? 1u : 0u);
-                mma_commit(&sh.s_full[s_at.slot]);
-                if (2 * s_j >= s_nb) mma_commit(sh.q_empty);
-            }
-            __syncwarp();
-            s_at.next();
-        };
-        scores();
-        if (ok && more) scores();
+    } else {
+        // ------------------------------------------------------------ products (whole warps in uniform control flow, one lane elected around
+        // the instructions).  Eight instructions take about 400 cycles to issue, so that one warp for both products was what the others
+        // waited for.
+        const bool is_scores = warp == kPScoreWarp;
+        RingAt<kPStages> at;
+        RingAt<kPWorks> work_at;
+        uint32_t entry_phase = 0u;
         while (ok) {
-            // scores two tiles ahead: their buffer held the weights of the tile before this one, whose product was issued before
-            if (more) scores();
-            if (!ok) break;
-            if (2 * o_j >= o_nb) {
-                if (o_nb) done_with_work(sh, o_work, lane);
-                if (!(ok = see_work(sh, o_work, w, limit))) break;
-                o_nb = w.nb;
-                o_j = 0;
-                if (o_nb == 0) break;
-                if (!(ok = mbar_wait_warp(sh.o_empty, o_phase, abort_flag, limit))) break;      // the entry before has left O
-                o_phase ^= 1u;
-            }
-            if (!(ok = mbar_wait_warp(&sh.p_full[o_at.slot], o_at.phase, abort_flag, limit))) break;
-            if (!(ok = mbar_wait_warp(&sh.v_full[o_at.slot], o_at.phase, abort_flag, limit))) break;
-            tc_fence_after_sync();
-            const uint64_t vd = v_desc + (uint64_t)(o_at.slot * (kPStage >> 4));
-            const uint32_t pa = tmem_s + o_at.slot * kPromptTile;                      // 16 keys = 8 columns
-            const uint32_t first = o_j ? 1u : 0u;
-            const bool two = 2 * o_j + 1 < o_nb;
-            ++o_j;
-            if (elect_one()) {
+            PromptWork w;
+            if (!(ok = see_work(sh, work_at, w, limit))) break;
+            done_with_work(sh, work_at, lane);
+            if (w.nb == 0) break;
+            // Q is there; or the entry before has left O
+            if (!(ok = is_scores ? mbar_wait_warp(sh.q_full, entry_phase, abort_flag, limit) : mbar_wait_warp(sh.o_empty, entry_phase ^ 1u, abort_flag, limit))) break;
+            entry_phase ^= 1u;
+            if (is_scores) {
+                const uint32_t idesc_s = make_idesc_bf16(kRowTile, kPromptTile, false, false), idesc_half = make_idesc_bf16(kRowTile, kBlock, false, false);
+                const uint64_t q_desc = make_smem_desc(smem_u32(sh.q_smem), 16, 1024, 128);
+                const uint64_t k_desc = make_smem_desc(smem_u32(sh.k_smem), 16, 1024, 128);
+                for (int j = 0; 2 * j < w.nb; ++j) {
+                    if (!(ok = mbar_wait_warp(&sh.k_full[at.slot], at.phase, abort_flag, limit))) break;
+                    // the buffer held the weights of three tiles before
+                    if (!(ok = mbar_wait_warp(&sh.v_empty[at.slot], at.phase ^ 1u, abort_flag, limit))) break;
+                    tc_fence_after_sync();
+                    const uint64_t kd = k_desc + (uint64_t)(at.slot * (kPStage >> 4));
+                    const uint32_t d = tmem_s + at.slot * kPromptTile;
+                    const uint32_t idesc = 2 * j + 1 < w.nb ? idesc_s : idesc_half;
+                    if (elect_one()) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) mma_ts(tmem, pa + i * 8, vd + (uint64_t)(i * (2048 >> 4)), idesc_o, i ? 1u : first);
-                if (two) {
-#pragma unroll
-                    for (int i = 4; i < 8; ++i) mma_ts(tmem, pa + i * 8, vd + (uint64_t)(i * (2048 >> 4)), idesc_o, 1u);
+                        for (int k = 0; k < kD / 16; ++k)
+                            mma_ss(d, q_desc + (uint64_t)((k >> 2) * ((kRowTile * 128) >> 4) + (k & 3) * 2),
+                                   kd + (uint64_t)((k >> 2) * (kPHalf >> 4) + (k & 3) * 2), idesc, k != 0 ? 1u : 0u);
+                        mma_commit(&sh.s_full[at.slot]);
+                        if (2 * (j + 1) >= w.nb) mma_commit(sh.q_empty);
+                    }
+                    __syncwarp();
+                    at.next();
                 }
-                mma_commit(&sh.v_empty[o_at.slot]);
-                if (2 * o_j >= o_nb) mma_commit(sh.o_full);
+            } else {
+                const uint32_t idesc_o = make_idesc_bf16(kRowTile, kD, false, true);
+                const uint64_t v_desc = make_smem_desc(smem_u32(sh.v_smem), kPHalf, 1024, 128);   // [key][d]: N (= d) contiguous
+                for (int j = 0; 2 * j < w.nb; ++j) {
+                    if (!(ok = mbar_wait_warp(&sh.v_full[at.slot], at.phase, abort_flag, limit))) break;
+                    if (!(ok = mbar_wait_warp(&sh.p_full[at.slot], at.phase, abort_flag, limit))) break;
+                    tc_fence_after_sync();
+                    const uint64_t vd = v_desc + (uint64_t)(at.slot * (kPStage >> 4));
+                    const uint32_t pa = tmem_s + at.slot * kPromptTile;                // 16 keys = 8 columns
+                    const uint32_t first = j ? 1u : 0u;
+                    if (elect_one()) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) mma_ts(tmem, pa + i * 8, vd + (uint64_t)(i * (2048 >> 4)), idesc_o, i ? 1u : first);
+                        if (2 * j + 1 < w.nb) {
+#pragma unroll
+                            for (int i = 4; i < 8; ++i) mma_ts(tmem, pa + i * 8, vd + (uint64_t)(i * (2048 >> 4)), idesc_o, 1u);
+                        }
+                        mma_commit(&sh.v_empty[at.slot]);
+                        if (2 * (j + 1) >= w.nb) mma_commit(sh.o_full);
+                    }
+                    __syncwarp();
+                    at.next();
+                }
             }
-            __syncwarp();
-            o_at.next();
         }
-        if (elect_one()) mma_commit(sh.unwound);
+        uint64_t* const mine = &sh.unwound[is_scores ? 0 : 1];
+        if (elect_one()) mma_commit(mine);
         __syncwarp();
-        if (!ok && lane == 0) set_status(status, SD_ERR_TIMEOUT);
-        mbar_wait_plain(sh.unwound, 0, limit);             // (nothing gives tensor memory back while a product runs)
-        if (!ok) unwind_pause();
+        mbar_wait_plain(mine, 0, limit);                   // (nothing gives tensor memory back while a product runs)
+    }
     } else if (warp < 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
         // ------------------------------------------------------------ soft-max: one thread per row and group
         const int group = warp >> 2, quad = warp & 3;
         const int r = quad * 32 + lane;                    // TMEM lane, row of the tile
@@ -497,7 +422,6 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
         RingAt<kPStages> at;                               // the stream's next tile
         RingAt<kPWorks> work_at;
         uint32_t n = 0, entry = 0;                         // tiles and entries so far
-        bool ok = true;
         while (ok) {
             PromptWork w;
             if (!(ok = see_work(sh, work_at, w, limit))) break;
@@ -510,70 +434,84 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
             volatile float* const my_ref = sh.refs + (entry & 1) * kRowTile + r;
             uint64_t* const ref_full = sh.ref_full + (entry & 1) * 4 + quad;
             const int nt = w.tiles();
-            RowState st{0.f, 0.f, 1.f, 1, 1};
+            RowState st{0.f, 0.f, 1.f, 1};
             for (int j = 0; j < nt; ++j, ++n, at.next()) {
                 if ((int)(n & 1u) != group) continue;
                 const uint32_t ts = tmem_s + lanes + at.slot * kPromptTile;
                 if (j == 1) {                              // the reference that the other group found in the first tile
                     if (!(ok = mbar_wait_warp(ref_full, (entry >> 1) & 1u, abort_flag, limit))) break;
                     st.m = *my_ref;
-                    st.usual = !__any_sync(0xffffffffu, !(fabsf(st.m) < 2097152.f));
                 }
                 if (!(ok = mbar_wait_warp(&sh.s_full[at.slot], at.phase, abort_flag, limit))) break;
                 tc_fence_after_sync();
+                const int blocks = 2 * j + 1 == w.nb ? 1 : 2;
+                const bool masked = all_see < (j + 1) * kPromptTile;           // some row does not see some key (or there is one block)
+                // V rows behind the request's last token carry weight 0, but 0 x NaN would still reach O: cleared before P.V reads them
+                if (filled < j * kPromptTile + blocks * kBlock) {
+                    if (!(ok = mbar_wait_warp(&sh.v_full[at.slot], at.phase, abort_flag, limit))) break;
+                    if (r >= filled - j * kPromptTile) {
+                        uint4* z = reinterpret_cast<uint4*>(sh.v_smem + at.slot * kPStage + r * 128);
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) z[c] = z[c + kPHalf / 16] = make_uint4(0, 0, 0, 0);
+                        fence_proxy_async_smem();
+                    }
+                }
+                const int vis = row_ok ? seen - j * kPromptTile : kPromptTile; // keys of the tile that this row sees
                 int hb = 0;                                // blocks that are done
                 st.raised = 1.f;
-                if (j > 0 && all_see >= (j + 1) * kPromptTile && st.usual) {
-                    // ---------------------------------------- the usual tile: all keys are visible
+                const auto weigh = [&]() -> bool {
                     uint32_t ra[32], rb[32], pk[32];
-                    const auto out_of_range = [&](float psum, float lo, float hi) {
-                        return row_ok && (!(psum <= kSumLimit) || lo < kShift - 126.f || hi > kShift + 126.f);
-                    };
                     uint64_t ps[2] = {0ull, 0ull};
-                    float lo = kShift, hi = kShift;
+                    const auto hide = [&](uint32_t (&x)[32], int c) {
+                        if (masked) mask_scores(x, vis >= c + 32 ? ~0u : (1u << max(vis - c, 0)) - 1u);
+                    };
                     tmem_ld32(ts, ra);
                     tmem_ld_wait();
                     tmem_ld32(ts + 32, rb);                // (the next scores are on their way)
-                    exp_block(ra, scale2, st.m, pk, ps, lo, hi);
+                    hide(ra, 0);
+                    if (j == 0) {                          // the reference: the largest of the first 32 scores that the row sees, as a whole number
+                        float mt = fmaxf(__uint_as_float(ra[0]), __uint_as_float(ra[1]));
+#pragma unroll
+                        for (int c = 2; c < 32; c += 2) mt = max3(mt, __uint_as_float(ra[c]), __uint_as_float(ra[c + 1]));
+                        st.m = row_ok && mt > -INFINITY ? rintf(mt * a.scale_log2) : 0.f;      // (no key: the row has no weight here)
+                        *my_ref = st.m;
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(ref_full);
+                    }
+                    const uint64_t neg_m2 = twice(-st.m);
+                    exp_pack(ra, scale2, neg_m2, pk, ps);
                     tmem_ld_wait();
-                    tmem_ld32(ts + 64, ra);
-                    exp_block(rb, scale2, st.m, pk + 16, ps, lo, hi);
+                    if (blocks == 2) tmem_ld32(ts + 64, ra);
+                    hide(rb, 32);
+                    exp_pack(rb, scale2, neg_m2, pk + 16, ps);
                     float psum = sum_f32x2(add_f32x2(ps[0], ps[1]));
                     // the tile before is final, and its reference still the one used here
-                    if (!(ok = mbar_wait_warp(commit, (n - 1u) & 1u, abort_flag, limit))) break;
-                    if (!__any_sync(0xffffffffu, out_of_range(psum, lo, hi) || *my_ref != st.m)) {
-                        tmem_st32(ts, pk);                 // over scores that have been read
-                        st.l += psum;
-                        hb = 1;
-                        ps[0] = ps[1] = 0ull;
-                        tmem_ld_wait();
-                        tmem_ld32(ts + 96, rb);
-                        exp_block(ra, scale2, st.m, pk, ps, lo, hi);
-                        tmem_ld_wait();
-                        exp_block(rb, scale2, st.m, pk + 16, ps, lo, hi);
-                        psum = sum_f32x2(add_f32x2(ps[0], ps[1]));
-                        if (!__any_sync(0xffffffffu, out_of_range(psum, lo, hi))) {
-                            tmem_st32(ts + 32, pk);
-                            st.l += psum;
-                            hb = 2;
-                        }
-                    }
-                }
-                const int blocks = 2 * j + 1 == w.nb ? 1 : 2;
+                    if (n > 0 && !mbar_wait_warp(commit, (n - 1u) & 1u, abort_flag, limit)) return false;
+                    const bool moved = j > 0 && *my_ref != st.m;
+                    tmem_ld_wait();
+                    if (__any_sync(0xffffffffu, row_ok && (moved || !(psum <= kSumLimit)))) return true;
+                    tmem_st32(ts, pk);                     // over scores that have been read
+                    st.l += psum;
+                    hb = 1;
+                    if (blocks == 1) return true;
+                    ps[0] = ps[1] = 0ull;
+                    tmem_ld32(ts + 96, rb);
+                    hide(ra, 64);
+                    exp_pack(ra, scale2, neg_m2, pk, ps);
+                    tmem_ld_wait();
+                    hide(rb, 96);
+                    exp_pack(rb, scale2, neg_m2, pk + 16, ps);
+                    psum = sum_f32x2(add_f32x2(ps[0], ps[1]));
+                    if (__any_sync(0xffffffffu, row_ok && !(psum <= kSumLimit))) return true;
+                    tmem_st32(ts + 32, pk);
+                    st.l += psum;
+                    hb = 2;
+                    return true;
+                };
+                if (!(ok = weigh())) break;
                 if (hb < blocks) {
-                    // V rows behind the request's last token carry weight 0, but 0 x NaN would still reach O: cleared before P.V reads them
-                    if (filled < j * kPromptTile + blocks * kBlock) {
-                        if (!(ok = mbar_wait_warp(&sh.v_full[at.slot], at.phase, abort_flag, limit))) break;
-                        if (r >= filled - j * kPromptTile) {
-                            uint4* z = reinterpret_cast<uint4*>(sh.v_smem + at.slot * kPStage + r * 128);
-#pragma unroll
-                            for (int c = 0; c < 8; ++c) z[c] = z[c + kPHalf / 16] = make_uint4(0, 0, 0, 0);
-                            fence_proxy_async_smem();
-                        }
-                    }
                     const int last = at.slot == 0 ? kPStages - 1 : at.slot - 1;
-                    const TileAt t{ts, tmem + lanes, row_ok ? seen - j * kPromptTile : kPromptTile, blocks, j == 0, ref_full, commit, &sh.v_empty[last],
-                                   (n - 1u) & 1u, at.slot == 0 ? at.phase ^ 1u : at.phase, n > 0, row_ok};
+                    const TileAt t{ts, tmem + lanes, vis, blocks, j == 0, &sh.v_empty[last], at.slot == 0 ? at.phase ^ 1u : at.phase, row_ok};
                     st = careful_tile(st, t, hb, a.scale_log2, my_ref, abort_flag, limit);
                     if (!(ok = st.ok)) break;
                 }
@@ -593,18 +531,14 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
             __syncwarp();
             if (lane == 0) mbar_arrive(&sh.sum_full[group]);
         }
-        if (!ok) {
-            if (lane == 0) set_status(status, SD_ERR_TIMEOUT);
-            unwind_pause();
-        }
-    } else if (warp < 12) {
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         // ------------------------------------------------------------ results: one thread per row
         const int quad = warp & 3, r = quad * 32 + lane;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         const int token = a.g.token_of(r), head = r - token * a.g.G;
         uint32_t phase = 0u, sum_phase[2] = {0u, 0u}, n = 0, entry = 0;
         RingAt<kPWorks> work_at;
-        bool ok = true;
         while (ok) {
             PromptWork w;
             if (!(ok = see_work(sh, work_at, w, limit))) break;
@@ -665,10 +599,10 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
             if (row_ok && part) reinterpret_cast<float2*>(part + (size_t)a.g.rows * kD)[r] = make_float2(m, l);
             if (row_ok && !part && a.lse) a.lse[row * a.p.Hq + h] = (m + log2f(l)) * 0.6931471805599453f;
         }
-        if (!ok) {
-            if (lane == 0) set_status(status, SD_ERR_TIMEOUT);
-            unwind_pause();
-        }
+    }
+    if (!ok) {
+        if (lane == 0) set_status(status, SD_ERR_TIMEOUT);
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);  // (as unwind_pause: copies on their way land first; a call would bind every role's registers)
     }
     tc_fence_before_sync();
     __syncthreads();
