@@ -142,6 +142,7 @@ __device__ __forceinline__ void done_with_work(const PromptShared& sh, RingAt<kP
 }
 
 __device__ __forceinline__ uint64_t twice(float c) { return pack_f32x2(c, c); }
+
 // What the soft-max of a row hands from tile to tile.
 struct RowState {
     float m, l;             // reference (a whole number) and sum of the weights relative to it
@@ -435,37 +436,31 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
             uint64_t* const ref_full = sh.ref_full + (entry & 1) * 4 + quad;
             const int nt = w.tiles();
             RowState st{0.f, 0.f, 1.f, 1};
-            for (int j = 0; j < nt; ++j, ++n, at.next()) {
-                if ((int)(n & 1u) != group) continue;
-                const uint32_t ts = tmem_s + lanes + at.slot * kPromptTile;
+            const int j0 = (int)(n & 1u) ^ group;          // this group's tiles: every second one of the stream
+            RingAt<kPStages> s_at = at;
+            if (j0) s_at.next();
+            for (int j = j0; j < nt; j += 2, s_at.next(), s_at.next()) {
+                const uint32_t ts = tmem_s + lanes + s_at.slot * kPromptTile;
+                const bool begun = j > 0 || n > 0;         // there is a tile before this one in the stream
+                const uint32_t commit_phase = (n + (uint32_t)j - 1u) & 1u;
                 if (j == 1) {                              // the reference that the other group found in the first tile
                     if (!(ok = mbar_wait_warp(ref_full, (entry >> 1) & 1u, abort_flag, limit))) break;
                     st.m = *my_ref;
                 }
-                if (!(ok = mbar_wait_warp(&sh.s_full[at.slot], at.phase, abort_flag, limit))) break;
+                if (!(ok = mbar_wait_warp(&sh.s_full[s_at.slot], s_at.phase, abort_flag, limit))) break;
                 tc_fence_after_sync();
-                const int blocks = 2 * j + 1 == w.nb ? 1 : 2;
                 const bool masked = all_see < (j + 1) * kPromptTile;           // some row does not see some key (or there is one block)
-                // V rows behind the request's last token carry weight 0, but 0 x NaN would still reach O: cleared before P.V reads them
-                if (filled < j * kPromptTile + blocks * kBlock) {
-                    if (!(ok = mbar_wait_warp(&sh.v_full[at.slot], at.phase, abort_flag, limit))) break;
-                    if (r >= filled - j * kPromptTile) {
-                        uint4* z = reinterpret_cast<uint4*>(sh.v_smem + at.slot * kPStage + r * 128);
-#pragma unroll
-                        for (int c = 0; c < 8; ++c) z[c] = z[c + kPHalf / 16] = make_uint4(0, 0, 0, 0);
-                        fence_proxy_async_smem();
-                    }
-                }
-                const int vis = row_ok ? seen - j * kPromptTile : kPromptTile; // keys of the tile that this row sees
-                int hb = 0;                                // blocks that are done
-                st.raised = 1.f;
-                const auto weigh = [&]() -> bool {
+                int hb = 0, blocks = 2;                    // blocks that are done, of how many
+                int vis = kPromptTile;                     // keys of the tile that this row sees
+                const auto weigh = [&](auto with_mask) -> bool {
+                    constexpr bool kMasked = decltype(with_mask)::value;
                     uint32_t ra[32], rb[32], pk[32];
                     uint64_t ps[2] = {0ull, 0ull};
-                    const auto hide = [&](uint32_t (&x)[32], int c) {
-                        if (masked) mask_scores(x, vis >= c + 32 ? ~0u : (1u << max(vis - c, 0)) - 1u);
-                    };
                     tmem_ld32(ts, ra);
+                    const auto hide = [&](uint32_t (&x)[32], int c) {
+                        if (kMasked) mask_scores(x, vis >= c + 32 ? ~0u : (1u << max(vis - c, 0)) - 1u);
+                    };
+                    st.raised = 1.f;
                     tmem_ld_wait();
                     tmem_ld32(ts + 32, rb);                // (the next scores are on their way)
                     hide(ra, 0);
@@ -477,23 +472,23 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
                         *my_ref = st.m;
                         __syncwarp();
                         if (lane == 0) mbar_arrive(ref_full);
-                    }
+                        }
                     const uint64_t neg_m2 = twice(-st.m);
                     exp_pack(ra, scale2, neg_m2, pk, ps);
                     tmem_ld_wait();
-                    if (blocks == 2) tmem_ld32(ts + 64, ra);
+                    if (!kMasked || blocks == 2) tmem_ld32(ts + 64, ra);
                     hide(rb, 32);
                     exp_pack(rb, scale2, neg_m2, pk + 16, ps);
                     float psum = sum_f32x2(add_f32x2(ps[0], ps[1]));
                     // the tile before is final, and its reference still the one used here
-                    if (n > 0 && !mbar_wait_warp(commit, (n - 1u) & 1u, abort_flag, limit)) return false;
-                    const bool moved = j > 0 && *my_ref != st.m;
+                    if (begun && !mbar_wait_warp(commit, commit_phase, abort_flag, limit)) return false;
+                    const float ref = *my_ref;
                     tmem_ld_wait();
-                    if (__any_sync(0xffffffffu, row_ok && (moved || !(psum <= kSumLimit)))) return true;
+                    if (__any_sync(0xffffffffu, row_ok && (ref != st.m || !(psum <= kSumLimit)))) return true;
                     tmem_st32(ts, pk);                     // over scores that have been read
                     st.l += psum;
                     hb = 1;
-                    if (blocks == 1) return true;
+                    if (kMasked && blocks == 1) return true;
                     ps[0] = ps[1] = 0ull;
                     tmem_ld32(ts + 96, rb);
                     hide(ra, 64);
@@ -508,17 +503,40 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
                     hb = 2;
                     return true;
                 };
-                if (!(ok = weigh())) break;
+                if (!masked) {
+                    ok = weigh(std::false_type{});
+                } else {
+                    vis = row_ok ? seen - j * kPromptTile : kPromptTile;
+                    blocks = 2 * j + 1 == w.nb ? 1 : 2;
+                    // V rows behind the request's last token carry weight 0, but 0 x NaN would still reach O: cleared before P.V reads them
+                    if (filled < j * kPromptTile + blocks * kBlock) {
+                        if (!(ok = mbar_wait_warp(&sh.v_full[s_at.slot], s_at.phase, abort_flag, limit))) break;
+                        if (r >= filled - j * kPromptTile) {
+                            uint4* z = reinterpret_cast<uint4*>(sh.v_smem + s_at.slot * kPStage + r * 128);
+#pragma unroll
+                            for (int c = 0; c < 8; ++c) z[c] = z[c + kPHalf / 16] = make_uint4(0, 0, 0, 0);
+                            fence_proxy_async_smem();
+                        }
+                    }
+                    ok = weigh(std::true_type{});
+                }
+                if (!ok) break;
                 if (hb < blocks) {
-                    const int last = at.slot == 0 ? kPStages - 1 : at.slot - 1;
-                    const TileAt t{ts, tmem + lanes, vis, blocks, j == 0, &sh.v_empty[last], at.slot == 0 ? at.phase ^ 1u : at.phase, row_ok};
+                    const int last = s_at.slot == 0 ? kPStages - 1 : s_at.slot - 1;
+                    const TileAt t{ts, tmem + lanes, vis, blocks, j == 0, &sh.v_empty[last], s_at.slot == 0 ? s_at.phase ^ 1u : s_at.phase, row_ok};
                     st = careful_tile(st, t, hb, a.scale_log2, my_ref, abort_flag, limit);
                     if (!(ok = st.ok)) break;
                 }
                 tmem_st_wait();
                 tc_fence_before_sync();
                 __syncwarp();
-                if (lane == 0 && !a.withhold) { mbar_arrive(&sh.p_full[at.slot]); mbar_arrive(commit); }
+                if (lane == 0 && !a.withhold) { mbar_arrive(&sh.p_full[s_at.slot]); mbar_arrive(commit); }
+            }
+            n += (uint32_t)nt;
+            {                                              // at += nt
+                const int slot = at.slot + nt % kPStages, rounds = nt / kPStages + (slot >= kPStages ? 1 : 0);
+                at.slot = slot >= kPStages ? slot - kPStages : slot;
+                at.phase ^= (uint32_t)(rounds & 1);
             }
             if (!ok) break;
             // the entry before has been read (phase entry - 1)
@@ -566,33 +584,65 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
             tc_fence_after_sync();
             float* const part = w.slot < 0 ? nullptr : a.partial + (size_t)w.slot * a.g.slot_floats();
             const size_t row = (size_t)(w.row0 + token), h = (size_t)w.h * a.g.G + head;
-            __nv_bfloat16* const dst = a.out + row * a.ldo + h * kD;
             const float inv = 1.f / l;
+            const auto leave = [&] {                       // O has been read: the next entry's first product waits for this
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(sh.o_empty);
+            };
+            if (part) {
 #pragma unroll 1
-            for (int c = 0; c < 4; ++c) {
-                uint32_t o[32];
-                tmem_ld32(tmem + lanes + c * 32, o);
-                tmem_ld_wait();
-                if (c == 3) {
-                    tc_fence_before_sync();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(sh.o_empty);
-                }
-                if (!row_ok) continue;
-                if (part) {                                // [16-byte piece][row]: a warp's stores are whole lines
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t o[32];
+                    tmem_ld32(tmem + lanes + c * 32, o);
+                    tmem_ld_wait();
+                    if (c == 3) leave();
+                    if (!row_ok) continue;
 #pragma unroll
-                    for (int x = 0; x < 8; ++x)
+                    for (int x = 0; x < 8; ++x)            // [16-byte piece][row]: a warp's stores are whole lines
                         reinterpret_cast<uint4*>(part)[(c * 8 + x) * a.g.rows + r] = make_uint4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
-                } else {
+                }
+            } else {
+                // Eight rows at a time, 64 bytes of each: a row per thread would make 32 lines of every store, whose passes through the
+                // load-store unit hold up the other warps' barriers.
+                const int q4 = lane & 3;
+#pragma unroll 1
+                for (int up = 0; up < 2; ++up) {           // rows 0-15 and 16-31 of the quadrant
+                    __nv_bfloat16* to[2];
+                    float by[2];
+                    bool there[2];
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        uint32_t u[4];
+                    for (int x = 0; x < 2; ++x) {
+                        const int rr = up * 16 + x * 8 + (lane >> 2), t_row = a.g.token_of(quad * 32 + rr), hd = quad * 32 + rr - t_row * a.g.G;
+                        by[x] = __shfl_sync(0xffffffffu, inv, rr);
+                        there[x] = t_row < w.tokens;
+                        to[x] = a.out + (size_t)(w.row0 + t_row) * a.ldo + ((size_t)w.h * a.g.G + hd) * kD + q4 * 8;
+                    }
 #pragma unroll
-                        for (int y = 0; y < 4; ++y) {
-                            const __nv_bfloat162 hh = __floats2bfloat162_rn(__uint_as_float(o[8 * x + 2 * y]) * inv, __uint_as_float(o[8 * x + 2 * y + 1]) * inv);
-                            u[y] = *reinterpret_cast<const uint32_t*>(&hh);
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t o[16];
+                        tmem_ld_16x256b_x4(tmem + lanes + ((uint32_t)(up * 16) << 16) + c * 32, o);
+                        tmem_ld_wait();
+                        if (up == 1 && c == 3) leave();
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            uint32_t u[4];                 // this thread's two columns of four eights; then its eight columns
+#pragma unroll
+                            for (int y = 0; y < 4; ++y) {
+                                const __nv_bfloat162 hh = __floats2bfloat162_rn(__uint_as_float(o[4 * y + 2 * x]) * by[x], __uint_as_float(o[4 * y + 2 * x + 1]) * by[x]);
+                                u[y] = *reinterpret_cast<const uint32_t*>(&hh);
+                            }
+#pragma unroll
+                            for (int d = 1; d < 4; d <<= 1)
+#pragma unroll
+                                for (int y = 0; y < 4; ++y) {
+                                    if (y & d) continue;
+                                    const bool odd = (q4 & d) != 0;
+                                    const uint32_t got = __shfl_xor_sync(0xffffffffu, odd ? u[y] : u[y | d], d);
+                                    if (odd) u[y] = got; else u[y | d] = got;
+                                }
+                            if (there[x]) *reinterpret_cast<uint4*>(to[x] + c * 32) = make_uint4(u[0], u[1], u[2], u[3]);
                         }
-                        reinterpret_cast<uint4*>(dst)[c * 4 + x] = make_uint4(u[0], u[1], u[2], u[3]);
                     }
                 }
             }
