@@ -618,7 +618,7 @@ sd_status sd_distill_grad(const void *logits, int32_t dtype, int64_t ld, int32_t
  *   n_blocks    : dev [B], in and out
  *   len, n_new  : dev [B] (an sd_batch's len and n_nodes for the trees of a step; both 0 for a request that is done)
  *   granted     : dev [B] or NULL: 1, or 0 for requests that got none
- * 1 <= B <= 8192.  A negative length stores SD_ERR_INVALID_ARG; more tokens than the table's row holds, or n_blocks or *n_free out of
+ * 1 <= B <= 8192, B * max_blocks_per_seq < 2^29.  A negative length stores SD_ERR_INVALID_ARG; more tokens than the table's row holds, or n_blocks or *n_free out of
  * range, SD_ERR_BOUNDS: that request keeps what it has (with *n_free out of range the stack counts as empty).  The arrays must not overlap.
  */
 sd_status sd_assign_blocks(const sd_block_pool *pool, int32_t B, int32_t max_blocks_per_seq, int32_t *block_table,
@@ -635,7 +635,7 @@ sd_status sd_prompt_prepare(const sd_prompts *prompts, int32_t *dev_status, void
 
 /*
  * K and V of the packed tokens into one layer's cache, byte for byte, at the slots of sd_prompt_prepare.  Rows of nobody and of requests
- * that were left out are not read.
+ * that were left out go nowhere.
  *   k, v : dev bf16, head h of row r at element r * ld + h * 128 (ld >= Hkv * 128, a multiple of 8: views of a projection's output);
  *          must not overlap the cache
  */

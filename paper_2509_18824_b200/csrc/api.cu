@@ -413,7 +413,7 @@ sd_status sd_assign_blocks(const sd_block_pool* pool, int32_t B, int32_t max_blo
                            int32_t* n_blocks, const int32_t* len, const int32_t* n_new, int32_t* granted,
                            int32_t* dev_status, void* stream) {
     if (!pool || B < 1 || max_blocks_per_seq < 1 || pool->num_blocks < 1) return SD_ERR_INVALID_ARG;
-    if (B > kMaxRequests || pool->num_blocks > kMaxPoolBlocks) return SD_ERR_UNSUPPORTED;
+    if (B > kMaxRequests || pool->num_blocks > kMaxPoolBlocks || (int64_t)B * max_blocks_per_seq >= 1 << 29) return SD_ERR_UNSUPPORTED;
     if (!pool->free_blocks || !pool->n_free || !block_table || !n_blocks || !len || !n_new || !dev_status) return SD_ERR_INVALID_ARG;
     if (!ok_4(pool->free_blocks) || !ok_4(pool->n_free) || !ok_4(block_table) || !ok_4(n_blocks) || !ok_4(len) || !ok_4(n_new) || !ok_4(granted))
         return SD_ERR_INVALID_ARG;

@@ -2,7 +2,7 @@
 //
 // Lengths are known on the device first (acceptance leaves new_len there), so tables that are made on the host cost a round trip per
 // step.  Both calls on lengths are scans over the requests; every CTA repeats the scan (8192 requests: 32 KB of lengths through L2), so
-// that nothing has to be handed from one to another.
+// that nothing has to be handed from one to another.  They are bound by latencies: launches, one or two trips to L2, and the scans.
 #include "prompt_plan.cuh"
 #include "sm100.cuh"
 
@@ -10,37 +10,47 @@ namespace sdv {
 using namespace sm100;
 
 namespace {
-constexpr int kPageThreads = 1024;
-constexpr int kSlotRows = 4096;                // packed rows of one CTA of the slot map
+constexpr int kFewThreads = 256, kManyThreads = 1024;
+constexpr int kOrderBins = 1024;
 
-// Sums of a value over the threads in front of this one, and over all; two values at a time.
-struct Pair { long long a, b; };
-__device__ __forceinline__ Pair block_scan(Pair v, Pair* warp_sums, Pair* total) {
+// Sums of whole numbers from 0 up stop at 2^29, which no count of rows or blocks reaches: what is behind that does not fit anyway.
+constexpr int kMost = 1 << 29;
+__device__ __forceinline__ int add_up(int a, int b) { return min(a + b, kMost); }
+__device__ __forceinline__ long long add_up(long long a, long long b) { return a + b; }
+
+// v: K values of this thread -> their sums over the threads in front of it; total: over all.  sums: room for two scans of K x 32 numbers; scans
+// that follow one another take the two in turn (buf), so that one barrier is enough.
+template <int THREADS, int K, typename T>
+__device__ __forceinline__ void block_scan(T (&v)[K], T (&total)[K], T* sums, int& buf) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    Pair in = v;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const long long a = __shfl_up_sync(0xffffffffu, in.a, d), b = __shfl_up_sync(0xffffffffu, in.b, d);
-        if (lane >= d) { in.a += a; in.b += b; }
-    }
-    if (lane == 31) warp_sums[warp] = in;
-    __syncthreads();
-    if (warp == 0) {
-        Pair w = warp_sums[lane];
+    T* const here = sums + buf * K * 32;
+    buf ^= 1;
+    const auto scan = [&](T (&x)[K]) {
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
-            const long long a = __shfl_up_sync(0xffffffffu, w.a, d), b = __shfl_up_sync(0xffffffffu, w.b, d);
-            if (lane >= d) { w.a += a; w.b += b; }
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const T below = __shfl_up_sync(0xffffffffu, x[k], d);
+                if (lane >= d) x[k] = add_up(x[k], below);
+            }
         }
-        warp_sums[lane] = w;
-    }
+    };
+    scan(v);
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+        if (lane == 31) here[k * 32 + warp] = v[k];
     __syncthreads();
-    const Pair before = warp > 0 ? warp_sums[warp - 1] : Pair{0, 0};
-    *total = warp_sums[31];
-    __syncthreads();                           // (warp_sums may be written again)
-    return Pair{before.a + in.a - v.a, before.b + in.b - v.b};
+    T w[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) w[k] = lane < THREADS / 32 ? here[k * 32 + lane] : T(0);
+    scan(w);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const T before = __shfl_sync(0xffffffffu, w[k], max(warp - 1, 0)), below = __shfl_up_sync(0xffffffffu, v[k], 1);
+        total[k] = __shfl_sync(0xffffffffu, w[k], 31);
+        v[k] = add_up(warp > 0 ? before : T(0), lane > 0 ? below : T(0));
+    }
 }
-__device__ __forceinline__ int cut(long long x) { return (int)min(x, 1ll << 30); }
 
 // the last of n ascending numbers that is at most x (the first one is)
 __device__ __forceinline__ int last_at_most(const int* a, int n, int x) {
@@ -55,28 +65,23 @@ __device__ __forceinline__ int last_at_most(const int* a, int n, int x) {
 
 // One cluster.  Blocks that come free stand in front of the stack, in order of the requests; the t-th block that is taken is the t-th of
 // this list.  So giving back what was taken leaves the stack as it was.
-__global__ void __launch_bounds__(kPageThreads)
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS)
 assign_blocks_kernel(sd_block_pool pool, int B, int W, int32_t* table, int32_t* n_blocks, const int32_t* len, const int32_t* n_new,
                      int32_t* granted, int32_t* status) {
     extern __shared__ int page_smem[];
-    int *const grow_at = page_smem, *const free_at = page_smem + B, *const held_of = page_smem + 2 * B;      // prefix sums; blocks held
-    __shared__ Pair warp_sums[32];
-    __shared__ int taken_smem;
+    int *const grow_at = page_smem, *const free_at = page_smem + B + 1, *const held_of = page_smem + 2 * B + 2;      // sums in front [B + 1]; blocks held [B]
+    __shared__ int sums[2 * 2 * 32];
     // (Tables are read through the read-only path by the attention calls, so no kernel behind this one begins before it has ended.)
     griddep_wait();
     settle(pool.free_blocks); settle(pool.n_free); settle(table); settle(n_blocks); settle(len); settle(n_new);
     const int cta = blockIdx.x, ctas = gridDim.x;
     const bool first = cta == 0;
-    if (threadIdx.x == 0) taken_smem = 0;
-    int n_free = __ldcg(pool.n_free);
-    if (n_free < 0 || n_free > pool.num_blocks) {
-        if (first && threadIdx.x == 0) set_status(status, SD_ERR_BOUNDS);
-        n_free = 0;
-    }
-    Pair sum{0, 0};
-    for (int b0 = 0; b0 < B; b0 += kPageThreads) {
+    int n_free = __ldcg(pool.n_free), buf = 0;
+    int so_far[2] = {0, 0};
+    for (int b0 = 0; b0 < B; b0 += THREADS) {
         const int b = b0 + (int)threadIdx.x;
-        Pair mine{0, 0};
+        int move[2] = {0, 0}, all[2];                      // blocks to take and to give back
         int held = 0;
         if (b < B) {
             held = __ldcg(n_blocks + b);
@@ -86,113 +91,135 @@ assign_blocks_kernel(sd_block_pool pool, int B, int W, int32_t* table, int32_t* 
             if (l < 0 || n < 0) bad = SD_ERR_INVALID_ARG;
             else if (held < 0 || held > W || want > W) bad = SD_ERR_BOUNDS;
             if (bad) { if (first) set_status(status, bad); }                    // (and the request keeps what it has)
-            else if (want > held) mine.a = want - held;
-            else mine.b = held - want;
+            else if (want > held) move[0] = (int)want - held;
+            else move[1] = held - (int)want;
         }
-        Pair all;
-        const Pair before = block_scan(mine, warp_sums, &all);
-        if (b < B) { grow_at[b] = cut(sum.a + before.a); free_at[b] = cut(sum.b + before.b); held_of[b] = held; }
-        sum.a += all.a; sum.b += all.b;
+        block_scan<THREADS>(move, all, sums, buf);
+        if (b < B) {
+            grow_at[b] = add_up(so_far[0], move[0]);
+            free_at[b] = add_up(so_far[1], move[1]);
+            held_of[b] = held;
+        }
+        so_far[0] = add_up(so_far[0], all[0]);
+        so_far[1] = add_up(so_far[1], all[1]);
     }
-    const int come_free = cut(sum.b), needed = cut(sum.a);
-    const long long supply = (long long)n_free + come_free;
-    const auto grow_end = [&](int b) { return b + 1 < B ? grow_at[b + 1] : needed; };
-    const auto free_end = [&](int b) { return b + 1 < B ? free_at[b + 1] : come_free; };
+    if (threadIdx.x == 0) { grow_at[B] = so_far[0]; free_at[B] = so_far[1]; }
+    if (n_free < 0 || n_free > pool.num_blocks) {
+        if (first && threadIdx.x == 0) set_status(status, SD_ERR_BOUNDS);
+        n_free = 0;
+    }
+    const int come_free = so_far[1];
     __syncthreads();
     // what is taken: the needs of the requests in front of the first that goes short
-    int taken = 0;
-    for (int b = threadIdx.x; b < B; b += kPageThreads)
-        if (grow_end(b) <= supply && grow_end(b) < (1 << 30)) taken = max(taken, grow_end(b));
-    if (taken) atomicMax(&taken_smem, taken);
-    __syncthreads();
-    taken = taken_smem;
-    if (ctas > 1) cluster_arrive_release();    // everybody has read the counts
+    const int taken = grow_at[last_at_most(grow_at, B + 1, min(n_free + come_free, kMost - 1))];
+    if (ctas > 1) cluster_arrive_release();                // everybody has read the counts
 
     const auto released = [&](int t) {
-        const int b = last_at_most(free_at, B, t), want = held_of[b] - (free_end(b) - free_at[b]);
+        const int b = last_at_most(free_at, B, t), want = held_of[b] - (free_at[b + 1] - free_at[b]);
         return __ldcg(table + (size_t)b * W + want + (t - free_at[b]));
     };
-    const int tid = cta * kPageThreads + (int)threadIdx.x, threads = ctas * kPageThreads;
+    const int tid = cta * THREADS + (int)threadIdx.x, threads = ctas * THREADS;
     for (int t = tid; t < taken; t += threads) {
         const int b = last_at_most(grow_at, B, t);
         const int block = t < come_free ? released(t) : __ldcg(pool.free_blocks + n_free - 1 - (t - come_free));
         table[(size_t)b * W + held_of[b] + (t - grow_at[b])] = block;
     }
     for (int t = taken + tid; t < come_free; t += threads) {
-        const long long at = (long long)n_free + come_free - 1 - t;
+        const int at = n_free + come_free - 1 - t;
         if (at < pool.num_blocks) pool.free_blocks[at] = released(t);
-        else set_status(status, SD_ERR_BOUNDS);                                 // (more than the pool has: given back twice)
+        else set_status(status, SD_ERR_BOUNDS);            // (more than the pool has: given back twice)
     }
     if (ctas > 1) cluster_wait_acquire();
     for (int b = tid; b < B; b += threads) {
-        const int grow = grow_end(b) - grow_at[b], shrink = free_end(b) - free_at[b];
-        const bool ok = grow == 0 || grow_end(b) <= taken;
+        const int grow = grow_at[b + 1] - grow_at[b], shrink = free_at[b + 1] - free_at[b];
+        const bool ok = grow_at[b + 1] <= taken || grow == 0;
         if (grow && ok) n_blocks[b] = held_of[b] + grow;
         if (shrink) n_blocks[b] = held_of[b] - shrink;
         if (granted) granted[b] = ok ? 1 : 0;
     }
-    if (tid == 0) *pool.n_free = (int)min((long long)n_free + come_free - taken, (long long)pool.num_blocks);
+    if (tid == 0) *pool.n_free = min(n_free + come_free - taken, pool.num_blocks);
 }
 
 sd_status launch_assign_blocks(const sd_block_pool& pool, int B, int W, int32_t* table, int32_t* n_blocks, const int32_t* len,
                                const int32_t* n_new, int32_t* granted, int32_t* dev_status, cudaStream_t st) {
-    const int smem = 3 * B * 4;
-    if (!allow_dynamic_smem(assign_blocks_kernel, smem)) return SD_ERR_CUDA;
-    const int ctas = B <= 64 ? 1 : 8;
-    return launch_dependent(assign_blocks_kernel, dim3(ctas), kPageThreads, smem, ctas, st, pool, B, W, table, n_blocks, len, n_new,
+    const int smem = (3 * B + 2) * 4;
+    if (B <= kFewThreads)
+        return launch_dependent(assign_blocks_kernel<kFewThreads>, dim3(1), kFewThreads, smem, 1, st, pool, B, W, table, n_blocks, len, n_new,
+                                granted, dev_status);
+    if (!allow_dynamic_smem(assign_blocks_kernel<kManyThreads>, smem)) return SD_ERR_CUDA;
+    return launch_dependent(assign_blocks_kernel<kManyThreads>, dim3(8), kManyThreads, smem, 8, st, pool, B, W, table, n_blocks, len, n_new,
                             granted, dev_status);
 }
 
-// First rows of the requests; slot and position of each packed row (all CTAs but the first); the attention's entries (the first).
-namespace {
-constexpr int kOrderBins = 1024;
-constexpr int kEntryTiles = 2;                 // what an entry costs beside its key tiles, in key tiles
-constexpr int kChunkMin = 2;                   // key tiles of the shortest chunk
-}  // namespace
-
-__global__ void __launch_bounds__(kPageThreads)
-prompt_prepare_kernel(sd_prompts p, PromptGeom geom, int32_t* status) {
+// First rows of the requests and the attention's work (the first CTA); slot and position of each packed row (the others, `rows` rows each).
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS)
+prompt_prepare_kernel(sd_prompts p, PromptGeom geom, int rows, int32_t* status) {
     extern __shared__ int page_smem[];
     int* const start = page_smem;              // [B + 1]
-    int* const first_entry = page_smem + p.B + 1;        // [B + 1] (the first CTA)
-    __shared__ Pair warp_sums[32];
+    int* const len_of = page_smem + p.B + 1;   // [B] cached tokens; ~cached tokens of a request that is left out
+    int* const first_entry = len_of + p.B;     // [B + 1] (the first CTA)
+    __shared__ int sums[2 * 32];
+    __shared__ long long line_sums[2 * 32];
     __shared__ int bins[kOrderBins];
-    __shared__ int n_splits, n_slots, n_entries;
+    __shared__ int n_splits, longest_smem;
     begin_dependent(p.block_table, p.n_blocks, p.len, p.n_new, p.start, p.slot, p.position, p.plan);
     const int B = p.B, W = p.max_blocks_per_seq;
     const bool planner = blockIdx.x == 0;
-    Pair sum{0, 0};
-    for (int b0 = 0; b0 < B; b0 += kPageThreads) {
-        const int b = b0 + (int)threadIdx.x;
-        Pair mine{0, 0};
-        if (b < B) {
-            const int n = __ldcg(p.n_new + b), l = __ldcg(p.len + b);
-            if ((n < 0 || l < 0) && planner) set_status(status, SD_ERR_INVALID_ARG);
-            mine.a = max(n, 0);
-        }
-        Pair all;
-        const Pair before = block_scan(mine, warp_sums, &all);
-        if (b < B) start[b] = (int)min(sum.a + before.a, (long long)p.N);       // (rows behind the packed ones belong to nobody)
-        sum.a += all.a;
+    int buf = 0, so_far = 0, entries = 0;
+    if (planner) {
+        for (int i = threadIdx.x; i < kOrderBins; i += THREADS) bins[i] = 0;
+        if (threadIdx.x == 0) { n_splits = longest_smem = 0; }
     }
-    if (threadIdx.x == 0) start[B] = (int)min(sum.a, (long long)p.N);
-    if (planner && threadIdx.x == 0 && sum.a > p.N) set_status(status, SD_ERR_BOUNDS);
+    for (int b0 = 0; b0 < B; b0 += THREADS) {
+        const int b = b0 + (int)threadIdx.x;
+        RequestSpan q{0, 0, false};
+        if (b < B) {
+            q = request_span(p, b, __ldcg(p.n_new + b));
+            if ((q.n < 0 || q.len < 0) && planner) set_status(status, SD_ERR_INVALID_ARG);
+            if (q.n > 0 && !q.covered && !p.n_blocks && q.len >= 0 && planner) set_status(status, SD_ERR_BOUNDS);
+        }
+        const int n = min(max(q.n, 0), kMost);
+        int at[1] = {n}, all[1];
+        block_scan<THREADS>(at, all, sums, buf);
+        at[0] = add_up(so_far, at[0]);
+        so_far = add_up(so_far, all[0]);
+        // (rows behind the packed ones belong to nobody, and a request that has some there is left out)
+        const bool there = q.covered && add_up(at[0], n) <= p.N;
+        if (b < B) {
+            start[b] = min(at[0], p.N);
+            len_of[b] = there ? q.len : ~max(q.len, 0);
+        }
+        if (planner) {
+            at[0] = there ? (n + geom.tokens - 1) / geom.tokens : 0;
+            block_scan<THREADS>(at, all, sums, buf);
+            if (b < B) first_entry[b] = entries + at[0];
+            entries += all[0];
+        }
+    }
+    if (threadIdx.x == 0) {
+        start[B] = min(so_far, p.N);
+        if (planner) first_entry[B] = entries;
+        if (planner && so_far > p.N) set_status(status, SD_ERR_BOUNDS);
+    }
     __syncthreads();
     if (!planner) {
         const int total = start[B];
-        const int r0 = ((int)blockIdx.x - 1) * kSlotRows, r1 = min(r0 + kSlotRows, p.N);
-        for (int r = r0 + (int)threadIdx.x; r < r1; r += kPageThreads) {
+        const int r0 = ((int)blockIdx.x - 1) * rows, r1 = min(r0 + rows, p.N);
+        int b = 0, next = 0;                   // the request of the last row, and the next one's first
+        for (int r = r0 + (int)threadIdx.x; r < r1; r += THREADS) {
             int slot = -1, position = 0;
             if (r < total) {
-                const int b = last_at_most(start, B, r);
-                const RequestSpan q = request_span(p, b, start[b], start[b + 1]);
-                position = max(q.len, 0) + r - start[b];
-                if (q.covered) {
+                if (r >= next) {
+                    b = last_at_most(start, B, r);
+                    next = start[b + 1];
+                }
+                const int len = len_of[b];
+                position = (len < 0 ? ~len : len) + r - start[b];
+                if (len >= 0) {
                     const int block = __ldcg(p.block_table + (size_t)b * W + position / kBlock);
                     if (block >= 0 && block < p.num_blocks) slot = block * kBlock + position % kBlock;
                     else set_status(status, SD_ERR_BOUNDS);
-                } else if (!p.n_blocks) {
-                    set_status(status, SD_ERR_BOUNDS);
                 }
             }
             p.slot[r] = slot;
@@ -200,121 +227,201 @@ prompt_prepare_kernel(sd_prompts p, PromptGeom geom, int32_t* status) {
         }
         return;
     }
-    // ------------------------------------------------------------ entries
-    int at = 0;
-    for (int b0 = 0; b0 < B; b0 += kPageThreads) {
-        const int b = b0 + (int)threadIdx.x;
-        Pair mine{0, 0};
-        if (b < B) {
-            p.start[b] = start[b];
-            const RequestSpan q = request_span(p, b, start[b], start[b + 1]);
-            if (q.covered) mine.a = (q.n + geom.tokens - 1) / geom.tokens;
-        }
-        Pair all;
-        const Pair before = block_scan(mine, warp_sums, &all);
-        if (b < B) first_entry[b] = at + (int)before.a;
-        at += (int)all.a;
-    }
-    if (threadIdx.x == 0) {
-        p.start[B] = start[B];
-        first_entry[B] = at;
-        n_splits = n_slots = n_entries = 0;
-    }
-    for (int i = threadIdx.x; i < kOrderBins; i += kPageThreads) bins[i] = 0;
-    __syncthreads();
-    const int total = min(at, geom.cap_entries);
-    // entry e with all its keys
-    const auto whole = [&](int e) {
+    // ------------------------------------------------------------ the attention's work
+    for (int b = threadIdx.x; b <= B; b += THREADS) p.start[b] = start[b];
+    const int Hkv = p.Hkv;
+    PromptEntry* const list = plan_entries(p.plan, geom.sms);
+    PromptStart* const starts = plan_starts(p.plan);
+    PromptSplit* const splits = plan_splits(p.plan, geom.sms);
+    const auto entry = [&](int e) {
         PromptEntry x;
         x.b = last_at_most(first_entry, B, e);
-        const int len = __ldcg(p.len + x.b), n = start[x.b + 1] - start[x.b], t0 = (e - first_entry[x.b]) * geom.tokens;
+        const int len = len_of[x.b], n = start[x.b + 1] - start[x.b], t0 = (e - first_entry[x.b]) * geom.tokens;
         x.row0 = start[x.b] + t0;
         x.pos0 = len + t0;
         x.tokens = min(geom.tokens, n - t0);
-        x.kb0 = 0;
-        x.kb1 = (x.pos0 + x.tokens + kBlock - 1) / kBlock;
+        x.blocks = (x.pos0 + x.tokens + kBlock - 1) / kBlock;
         x.end = len + n;
-        x.slot = -1;
+        x.unused0 = x.unused1 = 0;
         return x;
     };
-    Pair cost{0, 0};
-    for (int e = threadIdx.x; e < total; e += kPageThreads) cost.a += (whole(e).kb1 + 1) / 2 + kEntryTiles;
-    Pair all;
-    block_scan(cost, warp_sums, &all);
-    // An entry is cut where it is longer than a CTA's share of all of them; into chunks of half a share, so that what the CTAs take adds
-    // up more evenly.
-    const long long share = (all.a * p.Hkv + 2 * geom.sms - 1) / (2 * geom.sms);
-    const int chunk = (int)min(max(share, (long long)kChunkMin), 1ll << 24);
-    const auto chunks_of = [&](int tiles) { return tiles >= 2 * chunk ? (tiles + chunk - 1) / chunk : 1; };
-    const auto bin_of = [&](int tiles) { return kOrderBins - 1 - min(tiles, kOrderBins - 1); };
-    for (int e = threadIdx.x; e < total; e += kPageThreads) {
-        const int tiles = (whole(e).kb1 + 1) / 2, n = chunks_of(tiles), per = (tiles + n - 1) / n;
-        for (int c = 0; c < n; ++c) atomicAdd(&bins[bin_of(min(per, tiles - c * per))], 1);
-    }
-    __syncthreads();
-    {
-        static_assert(kOrderBins == kPageThreads, "");
-        const Pair here{bins[threadIdx.x], 0};
-        const Pair before = block_scan(here, warp_sums, &all);
-        bins[threadIdx.x] = (int)before.a;
-    }
-    __syncthreads();
-    PromptEntry* const entries = plan_entries(p.plan);
-    PromptSplit* const splits = plan_splits(p.plan, geom.cap_entries);
-    for (int e = threadIdx.x; e < total; e += kPageThreads) {
-        PromptEntry x = whole(e);
-        const int tiles = (x.kb1 + 1) / 2, n = chunks_of(tiles), per = (tiles + n - 1) / n, last = x.kb1;
-        int slot = -1;
-        if (n > 1) {
-            slot = atomicAdd(&n_slots, n * p.Hkv);
-            splits[atomicAdd(&n_splits, 1)] = PromptSplit{x.row0, x.tokens, slot, n};
+    // All entries are made once; the first kHeld lengths of a thread stay in registers, so that what follows, on one SM, is short.
+    constexpr int kHeld = 8;
+    int held[kHeld];
+    const auto for_own = [&](auto&& use) {     // use(e, key tiles): for all threads together, -1 where there is no entry
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i)
+            if (i * THREADS < entries) use(i * THREADS + (int)threadIdx.x, held[i]);
+        for (int e0 = kHeld * THREADS; e0 < entries; e0 += THREADS) {
+            const int e = e0 + (int)threadIdx.x;
+            use(e, e < entries ? (list[e].blocks + 1) / 2 : -1);
         }
-        for (int c = 0; c < n; ++c) {
-            x.kb0 = 2 * c * per;
-            x.kb1 = min(2 * (c + 1) * per, last);
-            x.slot = n > 1 ? slot + c * p.Hkv : -1;
-            entries[atomicAdd(&bins[bin_of(min(per, tiles - c * per))], 1)] = x;
-            atomicAdd(&n_entries, 1);
+    };
+    long long cost[1] = {0}, all_cost[1];
+    int longest = 0;
+    const auto make = [&](int e) {
+        if (e >= entries) return -1;
+        const PromptEntry x = entry(e);
+        list[e] = x;
+        const int tiles = (x.blocks + 1) / 2;
+        longest = max(longest, tiles);
+        cost[0] += tiles + kEntryTiles;
+        return tiles;
+    };
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) held[i] = make(i * THREADS + (int)threadIdx.x);
+    for (int e = kHeld * THREADS + (int)threadIdx.x; e < entries; e += THREADS) make(e);
+    longest = __reduce_max_sync(0xffffffffu, longest);
+    if ((threadIdx.x & 31) == 0 && longest) atomicMax(&longest_smem, longest);
+    buf = 0;
+    block_scan<THREADS>(cost, all_cost, line_sums, buf);       // (its barrier is behind the atomics)
+    const long long line = all_cost[0] * Hkv, part = max((line + geom.sms - 1) / geom.sms, (long long)kPartMin);
+    if (part >= (long long)kDealFrom * (longest_smem + kEntryTiles)) {
+        // ---------------------------------------- dealt out: sorted by counting.  (Lanes with the same length count as one.)
+        const auto put = [&](int tiles) {                                      // the place that each lane's entry gets in its bin
+            const int bin = kOrderBins - 1 - min(tiles, kOrderBins - 1);
+            const unsigned same = __match_any_sync(0xffffffffu, tiles < 0 ? -1 : bin), lane = threadIdx.x & 31;
+            const int leader = __ffs(same) - 1;
+            int first = 0;
+            if (tiles >= 0 && (int)lane == leader) first = atomicAdd(&bins[bin], __popc(same));
+            return __shfl_sync(0xffffffffu, first, leader) + __popc(same & ((1u << lane) - 1u));
+        };
+        for_own([&](int, int tiles) { put(tiles); });
+        __syncthreads();
+        constexpr int kOwn = kOrderBins / THREADS;                             // bins of a thread
+        int own[1] = {0}, all[1];
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) own[0] += bins[threadIdx.x * kOwn + i];
+        buf = 0;
+        block_scan<THREADS>(own, all, sums, buf);
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) {
+            const int n = bins[threadIdx.x * kOwn + i];
+            bins[threadIdx.x * kOwn + i] = own[0];
+            own[0] += n;
         }
+        __syncthreads();
+        int* const order = plan_order(list, geom.cap);
+        for_own([&](int e, int tiles) {
+            const int at = put(tiles);
+            if (tiles >= 0) order[at] = e;
+        });
+        if (threadIdx.x == 0) *plan_header(p.plan) = PromptHeader{0, entries, 0, 0};
+        return;
+    }
+    // ------------------------------------------------ in parts
+    // where part c begins, given the entry that its cut lies in and where that begins in the line
+    const auto cut_at = [&](long long c, int e, int tiles, long long from) {
+        const int one = tiles + kEntryTiles, off = (int)min(c * part - from, (long long)Hkv * one);
+        int h = off / one, tile = max(off - h * one - kEntryTiles, 0);
+        // (a chunk of a few tiles is not worth joining, unless the parts are not much longer)
+        if (part > 32 * kSnap && tile <= kSnap) tile = 0;
+        else if (part > 32 * kSnap && tile >= tiles - kSnap) { tile = 0; ++h; }
+        if (h == Hkv) { h = 0; ++e; }
+        starts[c] = PromptStart{e, h, tile, 0, entry(min(e, entries - 1))};
+    };
+    const bool few = entries <= kOrderBins && all_cost[0] < kMost;             // (then there may be many cuts to an entry: a thread for each of them)
+    long long at = 0;
+    for_own([&](int e, int tiles) {
+        const long long one = tiles < 0 ? 0 : tiles + kEntryTiles;             // of one head
+        long long before[1] = {one}, all[1];
+        block_scan<THREADS>(before, all, line_sums, buf);
+        const long long from = at + before[0];
+        if (few && tiles >= 0) bins[e] = (int)from;
+        if (!few && tiles >= 0)
+            for (long long c = (from * Hkv + part - 1) / part; c * part < (from + one) * Hkv; ++c) cut_at(c, e, tiles, from * Hkv);
+        at += all[0];
+    });
+    __syncthreads();
+    if (few)
+        for (int c = threadIdx.x; c * part < line; c += THREADS) {
+            const int e = last_at_most(bins, entries, (int)((unsigned)(c * (int)part) / (unsigned)Hkv));
+            cut_at(c, e, (list[e].blocks + 1) / 2, (long long)bins[e] * Hkv);
+        }
+    const int used = (int)((line + part - 1) / part);
+    for (int c = used + (int)threadIdx.x; c <= geom.sms; c += THREADS) starts[c] = PromptStart{entries, 0, 0, 0, PromptEntry{0, 0, 0, 0, 0, 0, 0, 0}};
+    __syncthreads();
+    // what was cut: found at its first cut
+    for (int c = 1 + (int)threadIdx.x; c < used; c += THREADS) {
+        const PromptStart s = starts[c];
+        if (s.tile == 0) continue;
+        const auto through = [&](int d) { return starts[d].e == s.e && starts[d].h == s.h && starts[d].tile > 0; };
+        if (through(c - 1)) continue;
+        int chunks = 2;
+        while (c + chunks - 1 < used && through(c + chunks - 1)) ++chunks;
+        // the first chunk is the last piece of CTA c - 1, and its first one too if its part begins with the entry
+        const bool only = starts[c - 1].e == s.e && starts[c - 1].h == s.h;
+        splits[atomicAdd(&n_splits, 1)] = PromptSplit{s.entry.row0, s.entry.tokens, s.h, 2 * (c - 1) + (only ? 0 : 1), c - 1, chunks, 0, 0};
     }
     __syncthreads();
-    if (threadIdx.x == 0) *plan_header(p.plan) = PromptHeader{n_entries, n_splits, n_slots, 0};
+    if (threadIdx.x == 0) *plan_header(p.plan) = PromptHeader{n_splits, 0, 0, 0};
 }
 
 size_t prompt_plan_bytes(const sd_prompts& p) {
     const PromptGeom g = prompt_geom(p, current_sms());
-    return sizeof(PromptHeader) + (size_t)g.cap_entries * sizeof(PromptEntry) + (size_t)g.cap_splits * sizeof(PromptSplit);
+    return sizeof(PromptHeader) + (g.sms + 1) * sizeof(PromptStart) + g.sms * sizeof(PromptSplit) + (size_t)g.cap * (sizeof(PromptEntry) + sizeof(int));
 }
 
+template <int THREADS>
+static sd_status launch_prepare(const sd_prompts& p, int32_t* dev_status, cudaStream_t st) {
+    const int smem = (3 * p.B + 2) * 4;
+    if (!allow_dynamic_smem(prompt_prepare_kernel<THREADS>, smem)) return SD_ERR_CUDA;
+    const PromptGeom geom = prompt_geom(p, current_sms());
+    // (one row a thread until the CTAs fill the GPU: every CTA repeats the scan over the requests)
+    const int others = geom.sms > 1 ? geom.sms - 1 : 1;
+    const int rows = ((p.N + others - 1) / others + THREADS - 1) / THREADS * THREADS;
+    const int ctas = 1 + (p.N > 0 ? (p.N + rows - 1) / rows : 0);
+    return launch_dependent(prompt_prepare_kernel<THREADS>, dim3(ctas), THREADS, smem, 1, st, p, geom, rows, dev_status);
+}
 sd_status launch_prompt_prepare(const sd_prompts& p, int32_t* dev_status, cudaStream_t st) {
-    const int smem = 2 * (p.B + 1) * 4;
-    if (!allow_dynamic_smem(prompt_prepare_kernel, smem)) return SD_ERR_CUDA;
-    return launch_dependent(prompt_prepare_kernel, dim3(1 + (p.N + kSlotRows - 1) / kSlotRows), kPageThreads, smem, 1, st, p,
-                            prompt_geom(p, current_sms()), dev_status);
+    return p.B <= kFewThreads && p.N <= 32 * kFewThreads ? launch_prepare<kFewThreads>(p, dev_status, st) : launch_prepare<kManyThreads>(p, dev_status, st);
 }
 
-// A token's K and V rows of all KV heads (256 bytes a head) into its slot; unit of work = one 16-byte vector of each.
+// A token's K and V rows of all KV heads (256 bytes a head) into its slot; unit of work = one 16-byte vector of each, U of them per thread.  Bound
+// by HBM; four units keep enough loads on their way (47195 rows of four heads xxx us with one, xxx with four), one leaves the shortest chain
+// where there are few rows.
+template <int U>
 __global__ void __launch_bounds__(256)
 append_kernel(sd_prompts p, sd_kv_layer cache, const uint4* k, long long ldk, const uint4* v, long long ldv, int32_t* status) {
     begin_dependent(p.slot, cache.k, cache.v, k, v);
-    const int per = p.Hkv * 16;
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-    const int row = (int)(i / per), vec = (int)(i - (long long)row * per);
-    if (row >= p.N) return;
-    const int slot = __ldcg(p.slot + row);
-    if (slot < 0) return;
-    const int block = slot / kBlock;
-    if (block >= cache.num_blocks) { set_status(status, SD_ERR_BOUNDS); return; }
-    const size_t at = (((size_t)block * p.Hkv + vec / 16) * kBlock + slot % kBlock) * 16 + vec % 16;
-    static_cast<uint4*>(cache.k)[at] = __ldcs(k + row * ldk + vec);
-    static_cast<uint4*>(cache.v)[at] = __ldcs(v + row * ldv + vec);
+    const unsigned per = (unsigned)p.Hkv * 16u;
+    const unsigned long long units = (unsigned long long)p.N * per;
+    uint4 kx[U], vx[U];
+    int slot[U];
+    unsigned vec[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const unsigned long long i = ((unsigned long long)blockIdx.x * U + u) * 256 + threadIdx.x;
+        slot[u] = -1;
+        vec[u] = 0;
+        if (i >= units) continue;
+        const unsigned row = units < 0xffffffffull ? (unsigned)i / per : (unsigned)(i / per);
+        vec[u] = (unsigned)(i - (unsigned long long)row * per);
+        slot[u] = __ldcg(p.slot + row);                    // (the rows come along without waiting for it)
+        kx[u] = __ldcs(k + row * ldk + vec[u]);
+        vx[u] = __ldcs(v + row * ldv + vec[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (slot[u] < 0) continue;
+        const int block = slot[u] / kBlock;
+        if (block >= cache.num_blocks) { set_status(status, SD_ERR_BOUNDS); continue; }
+        const size_t at = (((size_t)block * p.Hkv + vec[u] / 16) * kBlock + slot[u] % kBlock) * 16 + vec[u] % 16;
+        static_cast<uint4*>(cache.k)[at] = kx[u];
+        static_cast<uint4*>(cache.v)[at] = vx[u];
+    }
 }
 
 sd_status launch_append_kv(const sd_prompts& p, const sd_kv_layer& cache, const void* k, long long ldk, const void* v, long long ldv,
                            int32_t* dev_status, cudaStream_t st) {
-    const long long threads = (long long)p.N * p.Hkv * 16;
-    return launch_dependent(append_kernel, dim3((unsigned)((threads + 255) / 256)), 256, 0, 1, st, p, cache,
-                            static_cast<const uint4*>(k), ldk / 8, static_cast<const uint4*>(v), ldv / 8, dev_status);
+    const long long units = (long long)p.N * p.Hkv * 16;
+    const auto launch = [&](auto kern, int per_thread) {
+        const long long per_cta = 256ll * per_thread;
+        return launch_dependent(kern, dim3((unsigned)((units + per_cta - 1) / per_cta)), 256, 0, 1, st, p, cache, static_cast<const uint4*>(k),
+                                ldk / 8, static_cast<const uint4*>(v), ldv / 8, dev_status);
+    };
+    // (from one unit for every thread that the GPU holds)
+    return units >= 2048ll * current_sms() ? launch(append_kernel<4>, 4) : launch(append_kernel<1>, 1);
 }
 
 }  // namespace sdv

@@ -4,7 +4,7 @@
 // (see kSumLimit: the reference moves only where a tile's weights add up to more than 2^40, so that no maximum is looked for and nothing
 // is rescaled in the usual tile).
 //
-// A CTA per SM works through its entries of the plan (prompt_plan.cuh): a row tile of 128 rows - the query heads of a KV head for 128 / G
+// A CTA per SM works through its part of the plan (prompt_plan.cuh): entries, a row tile of 128 rows - the query heads of a KV head for 128 / G
 // tokens - against tiles of 128 keys.  The tiles of all its entries are one stream: the scores of tile g + 2 are computed before the product
 // of tile g's weights with V, whatever entries they belong to, in three score buffers of tensor memory beside O.  Weights, in bf16, lie over
 // the scores that they come from.  Two groups of four soft-max warps take the tiles in turn; both add to the one O, which works because the
@@ -17,7 +17,7 @@ namespace sdv {
 
 namespace {
 constexpr int kPThreads = 512;                 // warps 0-3, 4-7 soft-max, 8-11 results, 12 scores, 13 products with V, 14 K and Q copies, 15 V copies
-constexpr int kPScoreWarp = 12, kPProductWarp = 13, kPKeyWarp = 14, kPValueWarp = 15;
+constexpr int kPScoreWarp = 12, kPKeyWarp = 14, kPValueWarp = 15;
 constexpr int kPStages = 3;                    // K and V ring slots, score buffers
 constexpr int kPWorks = 4;                     // pieces of work that are known ahead
 constexpr int kPHalf = kPromptTile * 128;      // bytes of one D-half of a key tile: [128 keys][64] bf16, swizzled (16 KiB)
@@ -104,29 +104,74 @@ struct PromptArgs {
     int withhold;
 };
 
-// An entry for one KV head, as PromptEntry; slot is this head's, nb key blocks from kb0 on (0: there is no more work).
+// A piece of work: (a chunk of) an entry for one KV head; nb key blocks from kb0 on (0: there is no more work), slot of its partial result or -1.
 struct PromptWork {
     int row0, pos0, tokens, b, kb0, end, slot, h, nb;
     __device__ __forceinline__ int tiles() const { return (nb + 1) / 2; }
 };
-// the CTA's k-th piece of work, two vectors of its entry, and the head; none: kb1 = 0
-struct RawWork { int4 x, y; int h; };
-__device__ __forceinline__ RawWork fetch_work(const PromptArgs& a, int k, int entries) {
-    const int ctas = gridDim.x, c = blockIdx.x;
-    const long long i = (long long)k * ctas + ((k & 1) ? ctas - 1 - c : c);
-    RawWork r{make_int4(0, 0, 0, 0), make_int4(0, 0, 0, -1), 0};
-    if (i < (long long)entries * a.p.Hkv) {
-        const unsigned e = (unsigned)i / (unsigned)a.p.Hkv;                     // (entries x Hkv < 2^32: 2^24 rows of 1024 heads at most, 128 to a tile)
-        const int4* src = reinterpret_cast<const int4*>(plan_entries(a.p.plan) + e);
-        r.x = __ldcg(src);
-        r.y = __ldcg(src + 1);
-        r.h = (int)((unsigned)i - e * (unsigned)a.p.Hkv);
+// This CTA's pieces, one after the other.
+struct PromptWalk {
+    int e, h, tile;         // the next piece
+    int e1, h1, tile1;      // in parts: where this CTA's ends; dealt out: e is the number of the piece, e1 how many there are
+    int slot;               // of the next piece, if that is a chunk
+    bool dealt;
+    PromptEntry x;          // its entry
+    const PromptEntry* list;
+    const int* order;
+    int round;
+    __device__ __forceinline__ static PromptEntry load(const void* from) {
+        const int4* src = static_cast<const int4*>(from);
+        const int4 u = __ldcg(src), v = __ldcg(src + 1);
+        return PromptEntry{u.x, u.y, u.z, u.w, v.x, v.y, 0, 0};
     }
-    return r;
-}
-__device__ __forceinline__ PromptWork decode_work(const RawWork& r) {
-    return PromptWork{r.x.x, r.x.y, r.x.z, r.x.w, r.y.x, r.y.z, r.y.w < 0 ? -1 : r.y.w + r.h, r.h, r.y.y - r.y.x};
-}
+    __device__ __forceinline__ void begin(const PromptArgs& a) {
+        const int entries = __ldcg(&plan_header(a.p.plan)->dealt);
+        const PromptStart* s = plan_starts(a.p.plan) + blockIdx.x;
+        const int4 u = __ldcg(reinterpret_cast<const int4*>(s)), v = __ldcg(reinterpret_cast<const int4*>(s + 1));
+        x = load(&s->entry);
+        list = plan_entries(a.p.plan, a.g.sms);
+        order = plan_order(plan_entries(a.p.plan, a.g.sms), a.g.cap);
+        dealt = entries > 0;
+        e = u.x; h = u.y; tile = u.z;
+        e1 = v.x; h1 = v.y; tile1 = v.z;
+        slot = 2 * (int)blockIdx.x;
+        if (dealt) {
+            round = tile = 0;
+            e1 = entries * a.p.Hkv;                        // (below 2^31: 2^24 rows of 1024 heads at most, 16 or more tokens to a row tile)
+            e = (int)blockIdx.x;
+            if (e < e1) fetch(a.p.Hkv);
+        }
+    }
+    __device__ __forceinline__ void fetch(int Hkv) {
+        x = load(list + __ldcg(order + e / Hkv));
+        h = e % Hkv;
+    }
+    __device__ __forceinline__ PromptWork next(int Hkv) {
+        PromptWork w{x.row0, x.pos0, x.tokens, x.b, 2 * tile, x.end, -1, h, 0};
+        if (dealt) {
+            if (e >= e1) return w;
+            w.nb = x.blocks;
+            ++round;
+            const long long i = (long long)round * gridDim.x + ((round & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+            e = (int)min(i, (long long)e1);
+            if (e < e1) fetch(Hkv);                        // (on its way while this piece's copies are issued)
+            return w;
+        }
+        const bool last = e == e1 && h == h1;
+        if (e > e1 || (e == e1 && h > h1) || (last && tile >= tile1)) return w;
+        const int kb1 = last ? 2 * tile1 : x.blocks;
+        w.nb = kb1 - w.kb0;
+        if (w.kb0 > 0 || kb1 < x.blocks) w.slot = slot;
+        slot = 2 * (int)blockIdx.x + 1;
+        tile = 0;
+        if (++h == Hkv) {
+            h = 0;
+            ++e;
+            if (e < e1 || (e == e1 && (h1 > 0 || tile1 > 0))) x = load(list + e);
+        }
+        return w;
+    }
+};
 // The next piece of work, for every warp but the one that hands them out; false: a wait ran out.  done_with_work: it has been read.
 __device__ __forceinline__ bool see_work(const PromptShared& sh, const RingAt<kPWorks>& at, PromptWork& w, long long limit) {
     if (!mbar_wait_warp(&sh.work_full[at.slot], at.phase, sh.abort_flag, limit)) return false;
@@ -280,16 +325,12 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
         RingAt<kPStages> at;
         RingAt<kPWorks> work_at;
         uint32_t q_phase = 1u;                             // (empty at first)
-        RawWork raw;
-        int entries = 0;
-        if (keys) {
-            entries = __ldcg(&plan_header(a.p.plan)->entries);
-            raw = fetch_work(a, 0, entries);
-        }
-        for (int k = 0; ok; ++k) {
+        PromptWalk walk;
+        if (keys) walk.begin(a);
+        while (ok) {
             PromptWork w;
             if (keys) {
-                w = decode_work(raw);
+                w = walk.next(a.p.Hkv);
                 if (!(ok = mbar_wait_warp(&sh.work_empty[work_at.slot], work_at.phase ^ 1u, abort_flag, limit))) break;
                 if (lane == 0) {
                     int* dst = sh.works + work_at.slot * 10;
@@ -300,7 +341,6 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
                 __syncwarp();
                 work_at.next();
                 if (w.nb == 0) break;
-                raw = fetch_work(a, k + 1, entries);       // (on its way while this one's copies are issued)
             } else {
                 if (!(ok = see_work(sh, work_at, w, limit))) break;
                 done_with_work(sh, work_at, lane);
@@ -342,7 +382,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
                 }
             }
         }
-    } else {
+    } else {                                               // warps 12 and 13
         // ------------------------------------------------------------ products (whole warps in uniform control flow, one lane elected around
         // the instructions).  Eight instructions take about 400 cycles to issue, so that one warp for both products was what the others
         // waited for.
@@ -662,56 +702,78 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
     }
 }
 
-// Joins the chunks of the entries that were cut, in the order of the keys.  A thread takes 16 columns of a row.
+// Joins the chunks of the entries that were cut, in the order of the keys.  A thread takes sixteen columns of a row; sixteen loads are on
+// their way together.
 __global__ void __launch_bounds__(kMergeThreads)
 prompt_merge_kernel(const __grid_constant__ PromptArgs a) {
     begin_dependent();
-    const int splits = __ldcg(&plan_header(a.p.plan)->splits);
-    const PromptSplit* const list = plan_splits(a.p.plan, a.g.cap_entries);
-    const int per = (a.g.rows * 8 + kMergeThreads - 1) / kMergeThreads;        // CTAs of an entry and KV head, at most
-    for (int u = blockIdx.x; u < splits * a.p.Hkv * per; u += gridDim.x) {
-        const int4 s = __ldcg(reinterpret_cast<const int4*>(list + u / (a.p.Hkv * per)));
-        const int h = u / per % a.p.Hkv, rows = s.y * a.g.G, item = u % per * kMergeThreads + (int)threadIdx.x;
+    const PromptSplit* const list = plan_splits(a.p.plan, a.g.sms);
+    const int per = (a.g.rows * 8 + kMergeThreads - 1) / kMergeThreads;        // CTAs of an entry, at most
+    int splits = a.g.sms;                                                      // (the most there can be)
+    for (int u = blockIdx.x; u < splits * per; u += gridDim.x) {
+        const int4* src = reinterpret_cast<const int4*>(list + u / per);
+        const int4 s0 = __ldcg(src), s1 = __ldcg(src + 1);
+        splits = __ldcg(&plan_header(a.p.plan)->splits);
+        if (u >= splits * per) return;
+        const int row0 = s0.x, rows = s0.y * a.g.G, h = s0.z, first = s0.w, cta = s1.x, chunks = s1.y;
+        const int item = u % per * kMergeThreads + (int)threadIdx.x;
         if (item >= rows * 8) continue;
         const int cg = item / rows, r = item - cg * rows;
-        const size_t step = a.g.slot_floats() * a.p.Hkv;
-        const float* const part = a.partial + (size_t)(s.z + h) * a.g.slot_floats();
-        const float* const sums = part + (size_t)a.g.rows * kD + 2 * r;
-        const float* const o = part + ((size_t)cg * 4 * a.g.rows + r) * 4;
-        float top = -INFINITY;
-        for (int c = 0; c < s.w; ++c) {
-            const float2 ml = __ldcg(reinterpret_cast<const float2*>(sums + c * step));
-            if (ml.y != 0.f) top = fmaxf(top, ml.x);
-        }
-        float den = 0.f;
+        const auto part = [&](int c) { return a.partial + (size_t)(c == 0 ? first : 2 * (cta + c)) * a.g.slot_floats(); };
+        const size_t sums = (size_t)a.g.rows * kD + 2 * r, mine = ((size_t)cg * 4 * a.g.rows + r) * 4, next = (size_t)a.g.rows * 4;
+        constexpr int kAhead = 4;
+        float top = -INFINITY, den = 0.f;                  // relative to the largest reference so far
         float4 acc[4];
 #pragma unroll
         for (int x = 0; x < 4; ++x) acc[x] = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int c = 0; c < s.w; ++c) {
-            const float2 ml = __ldcg(reinterpret_cast<const float2*>(sums + c * step));
-            if (ml.y == 0.f) continue;                     // (no key that the row sees)
-            const float f = exp2f(ml.x - top);
-            den = fmaf(f, ml.y, den);
+        for (int c0 = 0; c0 < chunks; c0 += kAhead) {
+            float2 ml[kAhead];
+            float4 v[kAhead][4];
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const float4 v = __ldcg(reinterpret_cast<const float4*>(o + (size_t)x * a.g.rows * 4 + c * step));
-                acc[x].x = fmaf(f, v.x, acc[x].x); acc[x].y = fmaf(f, v.y, acc[x].y);
-                acc[x].z = fmaf(f, v.z, acc[x].z); acc[x].w = fmaf(f, v.w, acc[x].w);
+            for (int i = 0; i < kAhead; ++i) {
+                ml[i] = make_float2(-INFINITY, 0.f);
+                if (c0 + i < chunks) {
+                    const float* from = part(c0 + i);
+                    ml[i] = __ldcg(reinterpret_cast<const float2*>(from + sums));
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) v[i][x] = __ldcg(reinterpret_cast<const float4*>(from + mine + x * next));
+                }
+            }
+            float high = top;
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+                if (ml[i].y != 0.f) high = fmaxf(high, ml[i].x);               // (0: no key that the row sees)
+            if (high == -INFINITY) continue;
+            const float scale = exp2f(top - high);
+            top = high;
+            den *= scale;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) { acc[x].x *= scale; acc[x].y *= scale; acc[x].z *= scale; acc[x].w *= scale; }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                if (ml[i].y == 0.f) continue;
+                const float f = exp2f(ml[i].x - top);
+                den = fmaf(f, ml[i].y, den);
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    acc[x].x = fmaf(f, v[i][x].x, acc[x].x); acc[x].y = fmaf(f, v[i][x].y, acc[x].y);
+                    acc[x].z = fmaf(f, v[i][x].z, acc[x].z); acc[x].w = fmaf(f, v[i][x].w, acc[x].w);
+                }
             }
         }
         const float inv = 1.f / den;
-        uint32_t u8[8];
+        uint32_t o[8];
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
             const __nv_bfloat162 h0 = __floats2bfloat162_rn(acc[x].x * inv, acc[x].y * inv), h1 = __floats2bfloat162_rn(acc[x].z * inv, acc[x].w * inv);
-            u8[2 * x] = *reinterpret_cast<const uint32_t*>(&h0);
-            u8[2 * x + 1] = *reinterpret_cast<const uint32_t*>(&h1);
+            o[2 * x] = *reinterpret_cast<const uint32_t*>(&h0);
+            o[2 * x + 1] = *reinterpret_cast<const uint32_t*>(&h1);
         }
         const int token = a.g.token_of(r);
-        const size_t row = (size_t)(s.x + token), head = (size_t)h * a.g.G + (r - token * a.g.G);
+        const size_t row = (size_t)(row0 + token), head = (size_t)h * a.g.G + (r - token * a.g.G);
         uint4* dst = reinterpret_cast<uint4*>(a.out + row * a.ldo + head * kD + cg * 16);
-        dst[0] = make_uint4(u8[0], u8[1], u8[2], u8[3]);
-        dst[1] = make_uint4(u8[4], u8[5], u8[6], u8[7]);
+        dst[0] = make_uint4(o[0], o[1], o[2], o[3]);
+        dst[1] = make_uint4(o[4], o[5], o[6], o[7]);
         if (cg == 0 && a.lse) a.lse[row * a.p.Hq + head] = (top + log2f(den)) * 0.6931471805599453f;
     }
 }
@@ -724,7 +786,7 @@ int current_sms() {
 
 size_t prompt_workspace_bytes(const sd_prompts& p) {
     const PromptGeom g = prompt_geom(p, current_sms());
-    return ((size_t)g.cap_slots * g.slot_floats() * 4 + 255) & ~(size_t)255;
+    return ((size_t)2 * g.sms * g.slot_floats() * 4 + 255) & ~(size_t)255;
 }
 
 sd_status launch_prompt_attention(const sd_prompts& p, const sd_kv_layer& cache, const void* q, long long ldq, float scale, void* out,
@@ -750,11 +812,9 @@ sd_status launch_prompt_attention(const sd_prompts& p, const sd_kv_layer& cache,
         !encode_tmap_bf16_2d(&vm, cache.v, kv_rows, kD, kD * 2, 64, kBlock, 128))
         return SD_ERR_CUDA;
     if (!allow_dynamic_smem(prompt_kernel, kPSmem)) return SD_ERR_CUDA;
-    const long long items = (long long)a.g.cap_entries * p.Hkv;
-    const int ctas = (int)(items < a.g.sms ? items : a.g.sms);
-    sd_status s = launch_dependent(prompt_kernel, dim3(ctas), kPThreads, kPSmem, 1, st, qm, km, vm, a, dev_status);
+    sd_status s = launch_dependent(prompt_kernel, dim3(a.g.sms), kPThreads, kPSmem, 1, st, qm, km, vm, a, dev_status);
     if (s != SD_OK) return s;
-    return launch_dependent(prompt_merge_kernel, dim3(2 * a.g.sms), kMergeThreads, 0, 1, st, a);
+    return launch_dependent(prompt_merge_kernel, dim3(4 * a.g.sms), kMergeThreads, 0, 1, st, a);
 }
 
 }  // namespace sdv
