@@ -652,8 +652,8 @@ sd_status sd_append_kv(const sd_prompts *prompts, const sd_kv_layer *cache, cons
  * Rows of nobody and of requests that were left out are not written.  Slots behind a request's last token may hold any bit pattern.
  * Arithmetic: bf16 inputs, fp32 accumulation, weights rounded to bf16 in front of the product with V, bf16 output.  Range as
  * sd_verify_attention; K and V of the request's own tokens have to be finite.
- * Errors: SD_ERR_INVALID_ARG, SD_ERR_UNSUPPORTED, SD_ERR_WORKSPACE on the host; SD_ERR_BOUNDS (table entry outside [0, num_blocks)) or
- * SD_ERR_TIMEOUT through *dev_status.
+ * Errors: SD_ERR_INVALID_ARG, SD_ERR_UNSUPPORTED, SD_ERR_WORKSPACE on the host; SD_ERR_BOUNDS (table entry outside [0, num_blocks)),
+ * SD_ERR_INVALID_ARG (no plan that sd_prompt_prepare has made for these sizes) or SD_ERR_TIMEOUT through *dev_status.
  */
 size_t sd_prompt_workspace_bytes(const sd_prompts *prompts);
 sd_status sd_prompt_attention(const sd_prompts *prompts, const sd_kv_layer *cache, const void *q, int64_t ldq,

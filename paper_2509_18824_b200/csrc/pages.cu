@@ -306,7 +306,7 @@ prompt_prepare_kernel(sd_prompts p, PromptGeom geom, int rows, int32_t* status) 
             const int at = put(tiles);
             if (tiles >= 0) order[at] = e;
         });
-        if (threadIdx.x == 0) *plan_header(p.plan) = PromptHeader{0, entries, 0, 0};
+        if (threadIdx.x == 0) *plan_header(p.plan) = PromptHeader{0, entries, plan_stamp(p, geom), 0};
         return;
     }
     // ------------------------------------------------ in parts
@@ -354,7 +354,7 @@ prompt_prepare_kernel(sd_prompts p, PromptGeom geom, int rows, int32_t* status) 
         splits[atomicAdd(&n_splits, 1)] = PromptSplit{s.entry.row0, s.entry.tokens, s.h, 2 * (c - 1) + (only ? 0 : 1), c - 1, chunks, 0, 0};
     }
     __syncthreads();
-    if (threadIdx.x == 0) *plan_header(p.plan) = PromptHeader{n_splits, 0, 0, 0};
+    if (threadIdx.x == 0) *plan_header(p.plan) = PromptHeader{n_splits, 0, plan_stamp(p, geom), 0};
 }
 
 size_t prompt_plan_bytes(const sd_prompts& p) {

@@ -41,7 +41,8 @@ struct PromptShared {
     uint64_t* q_empty;      // MMA -> TMA: the entry's last scores are there
     uint64_t* o_full;       // MMA -> results: O updated by the entry's last tile
     uint64_t* o_empty;      // results -> MMA, soft-max: O, references and sums have been read
-    uint64_t* sum_full;     // [2] soft-max group -> results: references and sums
+    uint64_t* other_full;   // soft-max group without an entry's last tile -> results (the other group): its sums
+    uint64_t* sum_full;     // soft-max group with an entry's last tile -> results: references and sums
     uint64_t* work_full;    // [4] K copies -> the others: a piece of work
     uint64_t* work_empty;   // [4] the others (15 warps) -> K copies: it has been read
     uint64_t* unwound;      // [2] MMA: everything that either warp has issued has completed
@@ -49,8 +50,8 @@ struct PromptShared {
     int* abort_flag;
     int* works;             // [4][10]
     float* refs;            // [2][128] reference of a row, entries in turn
-    float* sums;            // [2][128] sum of a row over a group's tiles
-    float* raised;          // [128] what the entry's last tile has scaled the row by
+    float* others;          // [128] sum of a row over the tiles of the group without the entry's last one
+    float2* sums;           // [128] last reference of an entry's row, and its sum
 
     __device__ __forceinline__ explicit PromptShared(uint8_t* smem) {
         q_smem = smem;
@@ -58,15 +59,15 @@ struct PromptShared {
         v_smem = k_smem + kPStages * kPStage;
         uint64_t* bars = reinterpret_cast<uint64_t*>(v_smem + kPStages * kPStage);
         k_full = bars; v_full = bars + 3; s_full = bars + 6; v_empty = bars + 9; p_full = bars + 12; commit = bars + 15; ref_full = bars + 19;
-        q_full = bars + 27; q_empty = bars + 28; o_full = bars + 29; o_empty = bars + 30; sum_full = bars + 31;
+        q_full = bars + 27; q_empty = bars + 28; o_full = bars + 29; o_empty = bars + 30; other_full = bars + 31; sum_full = bars + 32;
         work_full = bars + 33; work_empty = bars + 37; unwound = bars + 41;
         tmem_slot = reinterpret_cast<uint32_t*>(bars + 43);
         abort_flag = reinterpret_cast<int*>(bars + 43) + 1;
         works = reinterpret_cast<int*>(bars + 44);
         static_assert(44 * 8 + kPWorks * 40 <= kPBars, "");
         refs = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(bars) + kPBars);
-        sums = refs + 2 * kRowTile;
-        raised = sums + 2 * kRowTile;
+        others = refs + 2 * kRowTile;
+        sums = reinterpret_cast<float2*>(others + kRowTile);
     }
     // (one thread)
     __device__ __forceinline__ void init_barriers() const {
@@ -76,7 +77,7 @@ struct PromptShared {
         }
         for (int i = 0; i < 4; ++i) { mbar_init(&commit[i], 1); mbar_init(&ref_full[i], 1); mbar_init(&ref_full[4 + i], 1); }
         mbar_init(q_full, 1); mbar_init(q_empty, 1); mbar_init(o_full, 1); mbar_init(o_empty, 4);
-        mbar_init(&sum_full[0], 4); mbar_init(&sum_full[1], 4);
+        mbar_init(other_full, 4); mbar_init(sum_full, 4);
         for (int i = 0; i < kPWorks; ++i) { mbar_init(&work_full[i], 1); mbar_init(&work_empty[i], 15); }
         mbar_init(&unwound[0], 1); mbar_init(&unwound[1], 1);
     }
@@ -114,7 +115,7 @@ struct PromptWalk {
     int e, h, tile;         // the next piece
     int e1, h1, tile1;      // in parts: where this CTA's ends; dealt out: e is the number of the piece, e1 how many there are
     int slot;               // of the next piece, if that is a chunk
-    bool dealt;
+    bool dealt, made;       // how; whether sd_prompt_prepare has made the plan of these prompts
     PromptEntry x;          // its entry
     const PromptEntry* list;
     const int* order;
@@ -125,12 +126,19 @@ struct PromptWalk {
         return PromptEntry{u.x, u.y, u.z, u.w, v.x, v.y, 0, 0};
     }
     __device__ __forceinline__ void begin(const PromptArgs& a) {
-        const int entries = __ldcg(&plan_header(a.p.plan)->dealt);
+        const int4 head = __ldcg(reinterpret_cast<const int4*>(plan_header(a.p.plan)));
+        const int entries = head.y;
         const PromptStart* s = plan_starts(a.p.plan) + blockIdx.x;
         const int4 u = __ldcg(reinterpret_cast<const int4*>(s)), v = __ldcg(reinterpret_cast<const int4*>(s + 1));
-        x = load(&s->entry);
+        x = load(&s->entry);                               // (within the plan whatever stands there)
         list = plan_entries(a.p.plan, a.g.sms);
         order = plan_order(plan_entries(a.p.plan, a.g.sms), a.g.cap);
+        made = head.z == plan_stamp(a.p, a.g);
+        if (!made) {                                       // (nothing of it is looked at)
+            dealt = false;
+            e = e1 = h = h1 = tile = tile1 = 0;
+            return;
+        }
         dealt = entries > 0;
         e = u.x; h = u.y; tile = u.z;
         e1 = v.x; h1 = v.y; tile1 = v.z;
@@ -327,6 +335,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
         uint32_t q_phase = 1u;                             // (empty at first)
         PromptWalk walk;
         if (keys) walk.begin(a);
+        if (keys && !walk.made && lane == 0) set_status(status, SD_ERR_INVALID_ARG);
         while (ok) {
             PromptWork w;
             if (keys) {
@@ -579,15 +588,22 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
                 at.phase ^= (uint32_t)(rounds & 1);
             }
             if (!ok) break;
-            // the entry before has been read (phase entry - 1)
-            if (!(ok = mbar_wait_warp(sh.o_empty, (entry & 1u) ^ 1u, abort_flag, limit))) break;
+            // Both groups leave their sums.  The other's is relative to the reference in front of the last tile: where that tile has raised it, the last
+            // tile's group adds them up itself.  Every warp waits here for the entry before to have been read, and reports, whether it had a
+            // tile of this one or not: nobody is ever two phases away from these barriers, whose waits tell only odd phases from even ones.
+            const bool has_last = (int)((n - 1u) & 1u) == group, both = nt > 1;
+            const uint32_t phase = entry & 1u;
             ++entry;
-            const bool has_last = (int)((n - 1u) & 1u) == group;
-            if (nt == 1 && !has_last) continue;            // (no tile of the entry was this group's)
-            sh.sums[group * kRowTile + r] = st.l;
-            if (has_last) sh.raised[r] = st.raised;
+            if (!(ok = mbar_wait_warp(sh.o_empty, phase ^ 1u, abort_flag, limit))) break;
+            if (!has_last) sh.others[r] = both ? st.l : 0.f;
+            if (has_last && __any_sync(0xffffffffu, both && st.raised != 1.f)) {
+                if (!(ok = mbar_wait_warp(sh.other_full, phase, abort_flag, limit))) break;
+                st.l = fmaf(sh.others[r], st.raised, st.l);
+                sh.others[r] = 0.f;
+            }
+            if (has_last) sh.sums[r] = make_float2(st.m, st.l);
             __syncwarp();
-            if (lane == 0) mbar_arrive(&sh.sum_full[group]);
+            if (lane == 0) mbar_arrive(has_last ? sh.sum_full : sh.other_full);
         }
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
@@ -595,30 +611,17 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
         const int quad = warp & 3, r = quad * 32 + lane;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         const int token = a.g.token_of(r), head = r - token * a.g.G;
-        uint32_t phase = 0u, sum_phase[2] = {0u, 0u}, n = 0, entry = 0;
+        uint32_t phase = 0u;
         RingAt<kPWorks> work_at;
         while (ok) {
             PromptWork w;
             if (!(ok = see_work(sh, work_at, w, limit))) break;
             done_with_work(sh, work_at, lane);
             if (w.nb == 0) break;
-            const int nt = w.tiles();
-            n += (uint32_t)nt;
             const bool row_ok = token < w.tokens;
-            // the sum of the last tile's group is relative to the entry's last reference, the other's to the one before that tile
-            float sum[2] = {0.f, 0.f};
-#pragma unroll
-            for (int g = 0; g < 2; ++g) {
-                const bool last = (int)((n - 1u) & 1u) == g;
-                if (!ok || (nt == 1 && !last)) continue;
-                ok = mbar_wait_warp(&sh.sum_full[g], sum_phase[g], abort_flag, limit);
-                sum_phase[g] ^= 1u;
-                sum[g] = sh.sums[g * kRowTile + r];
-            }
-            if (!ok) break;
-            const int last = (int)((n - 1u) & 1u);
-            const float l = (last ? sum[1] : sum[0]) + (nt > 1 ? (last ? sum[0] : sum[1]) * sh.raised[r] : 0.f);
-            const float m = sh.refs[(entry++ & 1) * kRowTile + r];
+            if (!(ok = mbar_wait_warp(sh.sum_full, phase, abort_flag, limit))) break;
+            if (!(ok = mbar_wait_warp(sh.other_full, phase, abort_flag, limit))) break;
+            const float m = sh.sums[r].x, l = sh.sums[r].y + sh.others[r];
             if (!(ok = mbar_wait_warp(sh.o_full, phase, abort_flag, limit))) break;
             phase ^= 1u;
             tc_fence_after_sync();
@@ -713,8 +716,9 @@ prompt_merge_kernel(const __grid_constant__ PromptArgs a) {
     for (int u = blockIdx.x; u < splits * per; u += gridDim.x) {
         const int4* src = reinterpret_cast<const int4*>(list + u / per);
         const int4 s0 = __ldcg(src), s1 = __ldcg(src + 1);
-        splits = __ldcg(&plan_header(a.p.plan)->splits);
-        if (u >= splits * per) return;
+        const int4 of = __ldcg(reinterpret_cast<const int4*>(plan_header(a.p.plan)));
+        splits = of.x;
+        if (of.z != plan_stamp(a.p, a.g) || u >= splits * per) return;
         const int row0 = s0.x, rows = s0.y * a.g.G, h = s0.z, first = s0.w, cta = s1.x, chunks = s1.y;
         const int item = u % per * kMergeThreads + (int)threadIdx.x;
         if (item >= rows * 8) continue;

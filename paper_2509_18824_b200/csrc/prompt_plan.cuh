@@ -49,7 +49,7 @@ struct alignas(16) PromptSplit {
     int slot, cta, chunks;                     // partial results: slot, then 2 (cta + 1), 2 (cta + 2) ..
     int unused0, unused1;
 };
-struct alignas(16) PromptHeader { int splits, dealt, unused0, unused1; };       // dealt: how many entries, 0: in parts
+struct alignas(16) PromptHeader { int splits, dealt, stamp, unused; };          // dealt: how many entries, 0: in parts
 
 struct PromptGeom {
     int G;                 // query heads of a KV head
@@ -71,6 +71,12 @@ inline PromptGeom prompt_geom(const sd_prompts& p, int sms) {
     g.rows = rows >= 128 ? 128 : (int)((rows + 7) / 8 * 8);
     g.cap = p.N / g.tokens + (p.B < p.N ? p.B : p.N) + 1;
     return g;
+}
+// Tells a plan that sd_prompt_prepare has made for these sizes from other memory.
+__host__ __device__ __forceinline__ int plan_stamp(const sd_prompts& p, const PromptGeom& g) {
+    uint32_t x = 0x9e3779b9u;
+    for (const int v : {p.B, p.N, p.Hq, p.Hkv, p.max_blocks_per_seq, p.num_blocks, g.sms}) x = (x ^ (uint32_t)v) * 0x01000193u + 0x7f4a7c15u;
+    return (int)x;
 }
 // the plan: header, starts [sms + 1], splits [sms], entries [cap], and for entries that are dealt out their order [cap]
 __host__ __device__ __forceinline__ PromptHeader* plan_header(void* plan) { return static_cast<PromptHeader*>(plan); }

@@ -211,3 +211,55 @@ def test_nothing_to_do():
     sd.sd_prompt_attention(empty, r.cache, none, r.scale, none, None, r.work, r.status)
     torch.cuda.synchronize()
     assert int(r.status.item()) == 0 and empty.start.tolist() == [0, 0, 0]
+
+
+@pytest.mark.parametrize("heads", [(4, 4), (7, 1)], ids=str)
+def test_many_entries_of_one_tile(heads):
+    """Thousands of entries that only one of the soft-max groups has a tile of, beside some of two and three."""
+    g = np.random.default_rng(17)
+    lens = [(1, int(c)) for c in g.integers(0, 64, 2000)] + [(1, int(c)) for c in g.integers(128, 300, 100)] + [(140, 0), (2, 127)]
+    order = g.permutation(len(lens))
+    r = Requests([lens[i] for i in order], *heads, seed=12)
+    r.prepare()
+    r.append()
+    r.attend()
+    r.check()
+
+
+def test_a_plan_that_was_not_made_is_reported():
+    r = Requests([(40, 100), (1, 300)], 7, 1, seed=4)
+    r.prepare()
+    r.append()
+    torch.cuda.synchronize()
+    for fill in (0, 255, 77):
+        r.prompts.plan.fill_(fill)
+        r.attend()
+        torch.cuda.synchronize()
+        assert int(r.status.item()) == sd.SD_ERR_INVALID_ARG and (r.out == 7.0).all() and (r.lse == 7.0).all()
+        r.status.zero_()
+    other = sd.Prompts(r.N - 2, 7, 1, 128, r.table, r.len, r.new, r.held, num_blocks=r.num_blocks)      # made for other sizes
+    sd.sd_prompt_prepare(other, r.status)
+    torch.cuda.synchronize()
+    r.status.zero_()
+    r.prompts.plan[:other.plan.numel()].copy_(other.plan)
+    r.attend()
+    torch.cuda.synchronize()
+    assert int(r.status.item()) == sd.SD_ERR_INVALID_ARG and (r.out == 7.0).all()
+
+
+@pytest.mark.parametrize("lens", [[(200, 3000)], [(1, 500)], [(30, 0), (1, 9)]], ids=str)
+def test_waits_that_run_out_are_reported(lens, monkeypatch):
+    r = Requests(lens, 7, 1, seed=4)
+    r.prepare()
+    r.append()
+    torch.cuda.synchronize()
+    monkeypatch.setenv("SDV_TEST_WITHHOLD", "1")
+    monkeypatch.setenv("SDV_TEST_WAIT_CYCLES", "200000")
+    r.attend()
+    torch.cuda.synchronize()
+    assert int(r.status.item()) == sd.SD_ERR_TIMEOUT
+    monkeypatch.delenv("SDV_TEST_WITHHOLD")
+    monkeypatch.delenv("SDV_TEST_WAIT_CYCLES")
+    r.status.zero_()
+    r.attend()                                               # and the next call finds everything as it should be
+    r.check()
