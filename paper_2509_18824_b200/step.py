@@ -309,7 +309,51 @@ class VerifyStep:
             self._ev_done[slot] = torch.cuda.Event()
         self._ev_done[slot].record(main)
 
+    def prompts(self, N: int, n_new, pool: Optional["sd.BlockPool"] = None, n_blocks: Optional[torch.Tensor] = None) -> "PromptStep":
+        """What brings prompts (or the next pieces of them) into this step's caches, see PromptStep."""
+        return PromptStep(self, N, n_new, pool, n_blocks)
+
     def check_status(self):
         code = int(self.status.item())
         if code != 0:
             raise sd.SdError(code)
+
+
+class PromptStep:
+    """New tokens of a VerifyStep's sequences in N packed rows, n_new [B] of each: blocks for them, their K and V in the caches of all
+    layers, and their own causal attention.  begin() once, layer() for every layer as its q, k and v exist, end().
+
+    pool, n_blocks [B]: the blocks that no sequence holds, and how many each holds, where the tables are to follow the lengths; sequences
+    that the pool does not suffice for are left out (granted 0) and keep what they have.  Without them the tables are the caller's."""
+
+    def __init__(self, step: VerifyStep, N: int, n_new, pool: Optional["sd.BlockPool"] = None, n_blocks: Optional[torch.Tensor] = None):
+        assert (pool is None) == (n_blocks is None), "a pool of blocks goes with the counts that it is kept for"
+        self.step, self.pool = step, pool
+        b, w = step.batch, step.w
+        self.prompts = sd.Prompts(N, b.Hq, b.Hkv, b.D, b.block_table, b.len, n_new, n_blocks, num_blocks=int(step.k_cache[0].shape[0]),
+                                  device=step.device)
+        self.granted = torch.ones(b.B, dtype=torch.int32, device=step.device)
+        self.workspace = torch.empty(sd.sd_prompt_workspace_bytes(self.prompts), dtype=torch.uint8, device=step.device)
+
+    def begin(self, stream=None):
+        """Tables, slots and positions (self.prompts.position: what a decoder rotates q and k by), and the attention's plan."""
+        p, status = self.prompts, self.step.status
+        if self.pool is not None:
+            sd.sd_assign_blocks(self.pool, p.block_table, p.n_blocks, p.len, p.n_new, self.granted, status, stream)
+        sd.sd_prompt_prepare(p, status, stream)
+
+    def layer(self, l: int, q, k, v, out, lse=None, stream=None):
+        """K and V [N, Hkv, 128] of the new tokens into layer l's cache, then their attention: q, out [N, Hq, 128], lse [N, Hq] or None."""
+        st = self.step
+        sd.sd_append_kv(self.prompts, st.caches[l], k, v, st.status, stream)
+        sd.sd_prompt_attention(self.prompts, st.caches[l], q, st.scale, out, lse, self.workspace, st.status, stream)
+
+    def end(self, stream=None):
+        """The new tokens count as cached from here on (of sequences that were not left out)."""
+        with contextlib.nullcontext() if stream is None else torch.cuda.stream(sd.stream_of(stream)):
+            self.prompts.len.addcmul_(self.prompts.n_new, self.granted)
+
+    def reserve_trees(self, stream=None):
+        """Blocks for the trees of the next verification (or what behind it is not needed, given back): tables that cover len + n_nodes."""
+        p, b = self.prompts, self.step.batch
+        sd.sd_assign_blocks(self.pool, p.block_table, p.n_blocks, b.len, b.n_nodes, self.granted, self.step.status, stream)

@@ -2,7 +2,7 @@
 the LM head at several row counts, and the bandwidth-regime cases (chain
 decoding, a compaction stress shape).  One JSON line per measurement.
 
-    python -m paper_2509_18824_b200.supplements [attention] [attention_layers] [lmhead] [lmhead480] [sampled] [draft] [compact] [rows]
+    python -m paper_2509_18824_b200.supplements [attention] [attention_layers] [lmhead] [lmhead480] [sampled] [draft] [compact] [rows] [prompts]
                                                 [chain8] [compact512]        (small cases for profiler captures)
 
 Timing: CUDA events on the launching stream, >= 3 warm-up calls, inputs rotated
@@ -283,6 +283,38 @@ def rows(M=480, V=152064, K=64, train=4096):
            _time(lambda: sd.sd_distill_loss(*args, kl, ce, None, None, grad, st), 10), 2 * nbytes)
 
 
+def prompts(Hq=28, Hkv=4):
+    """Blocks, copies into the cache and attention of packed new tokens; the caches of two calls in turn are larger than L2 together."""
+    hbm, tens, src = _peaks()
+    for what, new, cached in (("prompts of 4096 tokens", [4096] * 8, [0] * 8), ("one prompt of 32768", [32768], [0]),
+                              ("ragged prompts", list(range(64, 2049, 128)), [0] * 16),
+                              ("1024 tokens behind 8192", [1024], [8192]), ("one token each behind 4096", [1] * 32, [4096] * 32)):
+        B, N = len(new), sum(new)
+        held = [-(-(n + c) // 64) for n, c in zip(new, cached)]
+        total = sum(held)
+        order = torch.randperm(total, device="cuda").int()
+        table = torch.zeros((B, max(held)), dtype=torch.int32, device="cuda")
+        table[torch.arange(max(held), device="cuda")[None] < torch.tensor(held, device="cuda")[:, None]] = order
+        k, v = (torch.randn((total, Hkv, 64, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        qkv = torch.randn((N, Hq + 2 * Hkv, 128), dtype=torch.bfloat16, device="cuda")
+        out, st = torch.empty((N, Hq, 128), dtype=torch.bfloat16, device="cuda"), sd.new_status()
+        p = sd.Prompts(N, Hq, Hkv, 128, table, cached, new, held, num_blocks=total)
+        ws = torch.empty(sd.sd_prompt_workspace_bytes(p), dtype=torch.uint8, device="cuda")
+        cache = sd.kv_layer(k, v)
+        ms = {"sd_prompt_prepare": _time(lambda: sd.sd_prompt_prepare(p, st), 20),
+              "sd_append_kv": _time(lambda: sd.sd_append_kv(p, cache, qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:], st), 20),
+              "sd_prompt_attention": _time(lambda: sd.sd_prompt_attention(p, cache, qkv[:, :Hq], 128 ** -0.5, out, None, ws, st), 20)}
+        seen = sum(n * c + n * (n + 1) // 2 for n, c in zip(new, cached))
+        flops, nbytes = 4.0 * 128 * Hq * seen, {"sd_append_kv": 8.0 * N * Hkv * 128, "sd_prompt_attention": 4.0 * 128 * (N * Hq + Hkv * 64 * total)}
+        for call, t in ms.items():
+            line = {"call": call, "workload": what, "us": t * 1e3, "peaks": src, "status": int(st.item())}
+            if call in nbytes:
+                line.update(gbs=nbytes[call] / t / 1e6, frac_hbm=nbytes[call] / t / 1e6 / hbm)
+            if call == "sd_prompt_attention":
+                line.update(tflops=flops / t / 1e9, frac_tensor=flops / t / 1e9 / tens)
+            print(json.dumps(line))
+
+
 def compact(**kw):
     print(json.dumps(measure_compact(**kw)))
 
@@ -317,7 +349,7 @@ def measure_compact(B=1024, L=8, T=64, Hkv=4, D=128):
 
 
 if __name__ == "__main__":
-    what = sys.argv[1:] or ["attention", "attention_layers", "lmhead", "sampled", "draft", "compact", "rows"]
+    what = sys.argv[1:] or ["attention", "attention_layers", "lmhead", "sampled", "draft", "compact", "rows", "prompts"]
     if "attention" in what:
         attention()
     if "attention_layers" in what:
@@ -336,6 +368,8 @@ if __name__ == "__main__":
         compact()
     if "rows" in what:
         rows()
+    if "prompts" in what:
+        prompts()
     if "chain8" in what:                   # chain decoding, 8 layers in one call (0.55 GB of K/V)
         for r in measure_attention_layers(("chain11",), L=8, reps=3):
             print(json.dumps(r))
