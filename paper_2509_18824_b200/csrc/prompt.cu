@@ -18,53 +18,64 @@ namespace sdv {
 namespace {
 constexpr int kPThreads = 512;                 // warps 0-3, 4-7 soft-max, 8-11 results, 12 scores, 13 products with V, 14 K and Q copies, 15 V copies
 constexpr int kPScoreWarp = 12, kPKeyWarp = 14, kPValueWarp = 15;
-constexpr int kPStages = 3;                    // K and V ring slots, score buffers
-constexpr int kPWorks = 4;                     // pieces of work that are known ahead
+constexpr int kPStages = 3;                    // V ring slots, score buffers
+constexpr int kPKeyStages = 2, kPQueryStages = 2;          // K ring slots, and entries whose Q is there
+constexpr int kPWorks = 3;                     // pieces of work that are known ahead
 constexpr int kPHalf = kPromptTile * 128;      // bytes of one D-half of a key tile: [128 keys][64] bf16, swizzled (16 KiB)
 constexpr int kPStage = 2 * kPHalf;
 constexpr int kPQBytes = 2 * kRowTile * 128;
 constexpr int kPBars = 512;                    // barriers, two words and the pieces of work
-constexpr int kPSmem = kPQBytes + 2 * kPStages * kPStage + kPBars + 5 * kRowTile * 4;
-constexpr int kSoftmaxRegs = 152, kOtherRegs = 104;        // registers of a thread: 8 warps x 152 + 8 x 104 = 16 x 128, what the launch has
+constexpr int kPSmem = kPQueryStages * kPQBytes + (kPKeyStages + kPStages) * kPStage + kPBars + 5 * kRowTile * 4;
+#ifndef RS
+#define RS 152
+#define RO 104
+#endif
+constexpr int kSoftmaxRegs = RS, kOtherRegs = RO;        // registers of a thread: 8 warps x 152 + 8 x 104 = 16 x 128, what the launch has
 constexpr int kMergeThreads = 256;
 
 struct PromptShared {
     uint8_t *q_smem, *k_smem, *v_smem;
-    uint64_t* k_full;       // [3] TMA -> MMA
+    uint64_t* k_full;       // [2] TMA -> MMA
+    uint64_t* k_empty;      // [2] MMA -> TMA
     uint64_t* v_full;       // [3] TMA -> MMA (and whoever clears V rows)
-    uint64_t* s_full;       // [3] MMA -> soft-max, TMA: scores of tile g in buffer g % 3, K slot g % 3 read
+    uint64_t* s_full;       // [3] MMA -> soft-max: scores of tile g in buffer g % 3
     uint64_t* v_empty;      // [3] MMA -> TMA (and whoever raises a reference): O updated by tile g, V slot g % 3 read
     uint64_t* p_full;       // [3] soft-max -> MMA: weights of tile g written over its scores
     uint64_t* commit;       // [4] per TMEM quadrant: tile g's soft-max is final (phase g)
     uint64_t* ref_full;     // [2][4] per TMEM quadrant: the reference that an entry's first tile sets, entries in turn
-    uint64_t* q_full;       // TMA -> MMA
-    uint64_t* q_empty;      // MMA -> TMA: the entry's last scores are there
+    uint64_t* q_full;       // [2] TMA -> MMA, entries in turn
+    uint64_t* q_empty;      // [2] MMA -> TMA: the entry's last scores are there
     uint64_t* o_full;       // MMA -> results: O updated by the entry's last tile
     uint64_t* o_empty;      // results -> MMA, soft-max: O, references and sums have been read
     uint64_t* other_full;   // soft-max group without an entry's last tile -> results (the other group): its sums
     uint64_t* sum_full;     // soft-max group with an entry's last tile -> results: references and sums
-    uint64_t* work_full;    // [4] K copies -> the others: a piece of work
-    uint64_t* work_empty;   // [4] the others (15 warps) -> K copies: it has been read
+    uint64_t* work_full;    // [3] K copies -> the others: a piece of work
+    uint64_t* work_empty;   // [3] the others (15 warps) -> K copies: it has been read
     uint64_t* unwound;      // [2] MMA: everything that either warp has issued has completed
     uint32_t* tmem_slot;
     int* abort_flag;
-    int* works;             // [4][10]
+    int* works;             // [3][9]
     float* refs;            // [2][128] reference of a row, entries in turn
     float* others;          // [128] sum of a row over the tiles of the group without the entry's last one
     float2* sums;           // [128] last reference of an entry's row, and its sum
 
     __device__ __forceinline__ explicit PromptShared(uint8_t* smem) {
         q_smem = smem;
-        k_smem = smem + kPQBytes;
-        v_smem = k_smem + kPStages * kPStage;
-        uint64_t* bars = reinterpret_cast<uint64_t*>(v_smem + kPStages * kPStage);
-        k_full = bars; v_full = bars + 3; s_full = bars + 6; v_empty = bars + 9; p_full = bars + 12; commit = bars + 15; ref_full = bars + 19;
-        q_full = bars + 27; q_empty = bars + 28; o_full = bars + 29; o_empty = bars + 30; other_full = bars + 31; sum_full = bars + 32;
-        work_full = bars + 33; work_empty = bars + 37; unwound = bars + 41;
-        tmem_slot = reinterpret_cast<uint32_t*>(bars + 43);
-        abort_flag = reinterpret_cast<int*>(bars + 43) + 1;
-        works = reinterpret_cast<int*>(bars + 44);
-        static_assert(44 * 8 + kPWorks * 40 <= kPBars, "");
+        k_smem = smem + kPQueryStages * kPQBytes;
+        v_smem = k_smem + kPKeyStages * kPStage;
+        uint64_t* const bars = reinterpret_cast<uint64_t*>(v_smem + kPStages * kPStage);
+        uint64_t* at = bars;
+        const auto take = [&](int n) { uint64_t* const got = at; at += n; return got; };
+        k_full = take(kPKeyStages); k_empty = take(kPKeyStages);
+        v_full = take(kPStages); v_empty = take(kPStages); s_full = take(kPStages); p_full = take(kPStages);
+        commit = take(4); ref_full = take(8);
+        q_full = take(kPQueryStages); q_empty = take(kPQueryStages);
+        o_full = take(1); o_empty = take(1); other_full = take(1); sum_full = take(1);
+        work_full = take(kPWorks); work_empty = take(kPWorks); unwound = take(2);
+        tmem_slot = reinterpret_cast<uint32_t*>(take(1));
+        abort_flag = reinterpret_cast<int*>(tmem_slot) + 1;
+        works = reinterpret_cast<int*>(at);
+        static_assert((2 * kPKeyStages + 4 * kPStages + 12 + 2 * kPQueryStages + 4 + 2 * kPWorks + 3) * 8 + kPWorks * 36 <= kPBars, "");
         refs = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(bars) + kPBars);
         others = refs + 2 * kRowTile;
         sums = reinterpret_cast<float2*>(others + kRowTile);
@@ -72,11 +83,13 @@ struct PromptShared {
     // (one thread)
     __device__ __forceinline__ void init_barriers() const {
         *abort_flag = 0;
+        for (int i = 0; i < kPKeyStages; ++i) { mbar_init(&k_full[i], 1); mbar_init(&k_empty[i], 1); }
+        for (int i = 0; i < kPQueryStages; ++i) { mbar_init(&q_full[i], 1); mbar_init(&q_empty[i], 1); }
         for (int i = 0; i < kPStages; ++i) {
-            mbar_init(&k_full[i], 1); mbar_init(&v_full[i], 1); mbar_init(&s_full[i], 1); mbar_init(&v_empty[i], 1); mbar_init(&p_full[i], 4);
+            mbar_init(&v_full[i], 1); mbar_init(&s_full[i], 1); mbar_init(&v_empty[i], 1); mbar_init(&p_full[i], 4);
         }
         for (int i = 0; i < 4; ++i) { mbar_init(&commit[i], 1); mbar_init(&ref_full[i], 1); mbar_init(&ref_full[4 + i], 1); }
-        mbar_init(q_full, 1); mbar_init(q_empty, 1); mbar_init(o_full, 1); mbar_init(o_empty, 4);
+        mbar_init(o_full, 1); mbar_init(o_empty, 4);
         mbar_init(other_full, 4); mbar_init(sum_full, 4);
         for (int i = 0; i < kPWorks; ++i) { mbar_init(&work_full[i], 1); mbar_init(&work_empty[i], 15); }
         mbar_init(&unwound[0], 1); mbar_init(&unwound[1], 1);
@@ -183,7 +196,7 @@ struct PromptWalk {
 // The next piece of work, for every warp but the one that hands them out; false: a wait ran out.  done_with_work: it has been read.
 __device__ __forceinline__ bool see_work(const PromptShared& sh, const RingAt<kPWorks>& at, PromptWork& w, long long limit) {
     if (!mbar_wait_warp(&sh.work_full[at.slot], at.phase, sh.abort_flag, limit)) return false;
-    const volatile int* src = sh.works + at.slot * 10;
+    const volatile int* src = sh.works + at.slot * 9;
     w.row0 = src[0]; w.pos0 = src[1]; w.tokens = src[2]; w.b = src[3]; w.kb0 = src[4]; w.end = src[5]; w.slot = src[6]; w.h = src[7];
     w.nb = src[8];
     return true;
@@ -328,11 +341,13 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
         const bool keys = warp == kPKeyWarp;
         const CUtensorMap* const map = keys ? &k_map : &v_map;
         uint8_t* const ring = keys ? sh.k_smem : sh.v_smem;
-        uint64_t *const full = keys ? sh.k_full : sh.v_full, *const empty = keys ? sh.s_full : sh.v_empty;
+        uint64_t *const full = keys ? sh.k_full : sh.v_full, *const empty = keys ? sh.k_empty : sh.v_empty;
+        const int stages = keys ? kPKeyStages : kPStages;
         const uint64_t keep = policy_evict_last(), once = policy_evict_first();
-        RingAt<kPStages> at;
+        int slot = 0;                                      // of the next K or V
+        uint32_t slot_phase = 1u;                          // (empty at first)
+        RingAt<kPQueryStages> q_at;
         RingAt<kPWorks> work_at;
-        uint32_t q_phase = 1u;                             // (empty at first)
         PromptWalk walk;
         if (keys) walk.begin(a);
         if (keys && !walk.made && lane == 0) set_status(status, SD_ERR_INVALID_ARG);
@@ -342,7 +357,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
                 w = walk.next(a.p.Hkv);
                 if (!(ok = mbar_wait_warp(&sh.work_empty[work_at.slot], work_at.phase ^ 1u, abort_flag, limit))) break;
                 if (lane == 0) {
-                    int* dst = sh.works + work_at.slot * 10;
+                    int* dst = sh.works + work_at.slot * 9;
                     dst[0] = w.row0; dst[1] = w.pos0; dst[2] = w.tokens; dst[3] = w.b; dst[4] = w.kb0; dst[5] = w.end; dst[6] = w.slot; dst[7] = w.h;
                     dst[8] = w.nb;
                     mbar_arrive(&sh.work_full[work_at.slot]);
@@ -366,28 +381,29 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
                 if ((j & 15) == 0) held = 2 * j + lane < w.nb ? __ldcg(table + 2 * j + lane) : 0;
                 const bool two = 2 * j + 1 < w.nb;
                 const int y0 = (block_of(2 * j) * a.p.Hkv + w.h) * kBlock, y1 = two ? (block_of(2 * j + 1) * a.p.Hkv + w.h) * kBlock : 0;
-                if (!(ok = mbar_wait_warp(&empty[at.slot], at.phase ^ 1u, abort_flag, limit))) break;
-                uint8_t* dst = ring + at.slot * kPStage;
+                if (!(ok = mbar_wait_warp(&empty[slot], slot_phase, abort_flag, limit))) break;
+                uint8_t* dst = ring + slot * kPStage;
                 if (elect_one()) {
-                    mbar_arrive_expect_tx(&full[at.slot], two ? kPStage : kPStage / 2);
-                    tma_load_2d(dst, map, 0, y0, &full[at.slot], keep);
-                    tma_load_2d(dst + kPHalf, map, 64, y0, &full[at.slot], keep);
+                    mbar_arrive_expect_tx(&full[slot], two ? kPStage : kPStage / 2);
+                    tma_load_2d(dst, map, 0, y0, &full[slot], keep);
+                    tma_load_2d(dst + kPHalf, map, 64, y0, &full[slot], keep);
                     if (two) {
-                        tma_load_2d(dst + kPHalf / 2, map, 0, y1, &full[at.slot], keep);
-                        tma_load_2d(dst + kPHalf + kPHalf / 2, map, 64, y1, &full[at.slot], keep);
+                        tma_load_2d(dst + kPHalf / 2, map, 0, y1, &full[slot], keep);
+                        tma_load_2d(dst + kPHalf + kPHalf / 2, map, 64, y1, &full[slot], keep);
                     }
                 }
                 __syncwarp();
-                at.next();
+                if (++slot == stages) { slot = 0; slot_phase ^= 1u; }
                 if (j == 0 && keys) {
-                    if (!(ok = mbar_wait_warp(sh.q_empty, q_phase, abort_flag, limit))) break;
-                    q_phase ^= 1u;
+                    if (!(ok = mbar_wait_warp(&sh.q_empty[q_at.slot], q_at.phase ^ 1u, abort_flag, limit))) break;
                     if (elect_one()) {
-                        mbar_arrive_expect_tx(sh.q_full, (uint32_t)(a.g.tokens * a.g.G) * kD * 2);
-                        tma_load_3d(sh.q_smem, &q_map, 0, w.h * a.g.G, w.row0, sh.q_full, once);
-                        tma_load_3d(sh.q_smem + kRowTile * 128, &q_map, 64, w.h * a.g.G, w.row0, sh.q_full, once);
+                        uint8_t* to = sh.q_smem + q_at.slot * kPQBytes;
+                        mbar_arrive_expect_tx(&sh.q_full[q_at.slot], (uint32_t)(a.g.tokens * a.g.G) * kD * 2);
+                        tma_load_3d(to, &q_map, 0, w.h * a.g.G, w.row0, &sh.q_full[q_at.slot], once);
+                        tma_load_3d(to + kRowTile * 128, &q_map, 64, w.h * a.g.G, w.row0, &sh.q_full[q_at.slot], once);
                     }
                     __syncwarp();
+                    q_at.next();
                 }
             }
         }
@@ -397,26 +413,28 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
         // waited for.
         const bool is_scores = warp == kPScoreWarp;
         RingAt<kPStages> at;
+        RingAt<kPKeyStages> k_at;
+        RingAt<kPQueryStages> q_at;
         RingAt<kPWorks> work_at;
-        uint32_t entry_phase = 0u;
+        uint32_t entry_phase = 1u;
         while (ok) {
             PromptWork w;
             if (!(ok = see_work(sh, work_at, w, limit))) break;
             done_with_work(sh, work_at, lane);
             if (w.nb == 0) break;
             // Q is there; or the entry before has left O
-            if (!(ok = is_scores ? mbar_wait_warp(sh.q_full, entry_phase, abort_flag, limit) : mbar_wait_warp(sh.o_empty, entry_phase ^ 1u, abort_flag, limit))) break;
+            if (!(ok = is_scores ? mbar_wait_warp(&sh.q_full[q_at.slot], q_at.phase, abort_flag, limit) : mbar_wait_warp(sh.o_empty, entry_phase, abort_flag, limit))) break;
             entry_phase ^= 1u;
             if (is_scores) {
                 const uint32_t idesc_s = make_idesc_bf16(kRowTile, kPromptTile, false, false), idesc_half = make_idesc_bf16(kRowTile, kBlock, false, false);
-                const uint64_t q_desc = make_smem_desc(smem_u32(sh.q_smem), 16, 1024, 128);
+                const uint64_t q_desc = make_smem_desc(smem_u32(sh.q_smem + q_at.slot * kPQBytes), 16, 1024, 128);
                 const uint64_t k_desc = make_smem_desc(smem_u32(sh.k_smem), 16, 1024, 128);
                 for (int j = 0; 2 * j < w.nb; ++j) {
-                    if (!(ok = mbar_wait_warp(&sh.k_full[at.slot], at.phase, abort_flag, limit))) break;
+                    if (!(ok = mbar_wait_warp(&sh.k_full[k_at.slot], k_at.phase, abort_flag, limit))) break;
                     // the buffer held the weights of three tiles before
                     if (!(ok = mbar_wait_warp(&sh.v_empty[at.slot], at.phase ^ 1u, abort_flag, limit))) break;
                     tc_fence_after_sync();
-                    const uint64_t kd = k_desc + (uint64_t)(at.slot * (kPStage >> 4));
+                    const uint64_t kd = k_desc + (uint64_t)(k_at.slot * (kPStage >> 4));
                     const uint32_t d = tmem_s + at.slot * kPromptTile;
                     const uint32_t idesc = 2 * j + 1 < w.nb ? idesc_s : idesc_half;
                     if (elect_one()) {
@@ -425,11 +443,14 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
                             mma_ss(d, q_desc + (uint64_t)((k >> 2) * ((kRowTile * 128) >> 4) + (k & 3) * 2),
                                    kd + (uint64_t)((k >> 2) * (kPHalf >> 4) + (k & 3) * 2), idesc, k != 0 ? 1u : 0u);
                         mma_commit(&sh.s_full[at.slot]);
-                        if (2 * (j + 1) >= w.nb) mma_commit(sh.q_empty);
+                        mma_commit(&sh.k_empty[k_at.slot]);
+                        if (2 * (j + 1) >= w.nb) mma_commit(&sh.q_empty[q_at.slot]);
                     }
                     __syncwarp();
                     at.next();
+                    k_at.next();
                 }
+                q_at.next();
             } else {
                 const uint32_t idesc_o = make_idesc_bf16(kRowTile, kD, false, true);
                 const uint64_t v_desc = make_smem_desc(smem_u32(sh.v_smem), kPHalf, 1024, 128);   // [key][d]: N (= d) contiguous
@@ -478,6 +499,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
             done_with_work(sh, work_at, lane);
             if (w.nb == 0) break;
             const bool row_ok = token < w.tokens;
+            const bool idle = !__any_sync(0xffffffffu, row_ok);                // (single tokens: three warps of four)
             const int seen = row_ok ? w.pos0 + token + 1 - w.kb0 * kBlock : 0x7fffffff;     // keys from kb0 on that this row sees
             const int all_see = min(w.pos0 + 1 - w.kb0 * kBlock, w.nb * kBlock);            // ... that every row of the tile sees
             const int filled = w.end - w.kb0 * kBlock;     // ... that have been written
@@ -552,7 +574,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
                     hb = 2;
                     return true;
                 };
-                if (!masked) {
+                if (!masked && !idle) {
                     ok = weigh(std::false_type{});
                 } else {
                     vis = row_ok ? seen - j * kPromptTile : kPromptTile;
@@ -567,7 +589,13 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
                             fence_proxy_async_smem();
                         }
                     }
-                    ok = weigh(std::true_type{});
+                    if (!idle) {
+                        ok = weigh(std::true_type{});
+                    } else {                               // none of the warp's rows is read: it keeps its place among the barriers
+                        if (j == 0 && lane == 0) mbar_arrive(ref_full);
+                        if (begun) ok = mbar_wait_warp(commit, commit_phase, abort_flag, limit);
+                        hb = blocks;
+                    }
                 }
                 if (!ok) break;
                 if (hb < blocks) {
@@ -654,6 +682,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
                     __nv_bfloat16* to[2];
                     float by[2];
                     bool there[2];
+                    uint32_t o[2][16];
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
                         const int rr = up * 16 + x * 8 + (lane >> 2), t_row = a.g.token_of(quad * 32 + rr), hd = quad * 32 + rr - t_row * a.g.G;
@@ -663,16 +692,18 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
                     }
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        uint32_t o[16];
-                        tmem_ld_16x256b_x4(tmem + lanes + ((uint32_t)(up * 16) << 16) + c * 32, o);
-                        tmem_ld_wait();
-                        if (up == 1 && c == 3) leave();
+                        if ((c & 1) == 0) {                // two loads on their way together
+                            tmem_ld_16x256b_x4(tmem + lanes + ((uint32_t)(up * 16) << 16) + c * 32, o[0]);
+                            tmem_ld_16x256b_x4(tmem + lanes + ((uint32_t)(up * 16) << 16) + c * 32 + 32, o[1]);
+                            tmem_ld_wait();
+                            if (up == 1 && c == 2) leave();
+                        }
 #pragma unroll
                         for (int x = 0; x < 2; ++x) {
                             uint32_t u[4];                 // this thread's two columns of four eights; then its eight columns
 #pragma unroll
                             for (int y = 0; y < 4; ++y) {
-                                const __nv_bfloat162 hh = __floats2bfloat162_rn(__uint_as_float(o[4 * y + 2 * x]) * by[x], __uint_as_float(o[4 * y + 2 * x + 1]) * by[x]);
+                                const __nv_bfloat162 hh = __floats2bfloat162_rn(__uint_as_float(o[c & 1][4 * y + 2 * x]) * by[x], __uint_as_float(o[c & 1][4 * y + 2 * x + 1]) * by[x]);
                                 u[y] = *reinterpret_cast<const uint32_t*>(&hh);
                             }
 #pragma unroll
