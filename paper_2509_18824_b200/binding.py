@@ -554,56 +554,95 @@ def sd_distill_grad(logits, top_val, top_idx, top_lse, label, inv_temp: float, k
 
 
 # ------------------------------------------------------------------ packed new tokens
-def _ints(t, shape, what):
-    assert t.is_cuda and t.dtype == torch.int32 and tuple(t.shape) == shape and t.is_contiguous(), f"{what}: contiguous int32 CUDA tensor {shape}"
-    assert t.get_device() == torch.cuda.current_device(), f"{what} lies on another device than the current one"
+_here = torch._C._cuda_getDevice           # (torch.cuda.current_device() takes 0.4 us, a tenth of a small call)
+_BF16 = (torch.bfloat16, torch.int16, torch.uint16)
+
+
+def _ints(t, n, what, here=None):
+    """A contiguous int32 tensor of shape n on the current device."""
+    if t.dtype is not torch.int32 or t.shape != n or not t.is_contiguous() or t.get_device() != (_here() if here is None else here):
+        raise AssertionError(f"{what}: expected a contiguous int32 tensor {n} on the current device, got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t
 
 
-def _heads(t, rows, heads, what):
+def _heads(t, rows, heads, what, here):
     """(address, row stride) of bf16 rows of heads [rows, heads, 128]; rows may lie further apart (a view of a projection's output)."""
-    assert t.is_cuda and t.dtype in (torch.bfloat16, torch.int16, torch.uint16), f"{what}: bf16 CUDA tensor"
-    assert t.get_device() == torch.cuda.current_device(), f"{what} lies on another device than the current one"
-    assert tuple(t.shape) == (rows, heads, 128), f"{what}: expected {(rows, heads, 128)}, got {tuple(t.shape)}"
-    assert t.stride(2) == 1 and (heads == 1 or t.stride(1) == 128), f"{what}: the heads of a row must be contiguous"
-    ld = t.stride(0) if rows > 1 else heads * 128
-    assert ld >= heads * 128, f"{what}: rows must not overlap"
+    if t.dtype not in _BF16 or t.shape != (rows, heads, 128) or t.get_device() != here:
+        raise AssertionError(f"{what}: expected bf16 {(rows, heads, 128)} on the current device, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    ld, between, one = t.stride()
+    if rows < 2:
+        ld = heads * 128
+    if one != 1 or (heads > 1 and between != 128) or ld < heads * 128:
+        raise AssertionError(f"{what}: the heads of a row must be contiguous, rows must not overlap (strides {t.stride()})")
     return t.data_ptr(), ld
 
 
-class BlockPool:
+class _OnAnyStream:
+    """The arrays that an object makes, on the current stream, are ready for calls on any other and outlive them."""
+
+    def _makes(self, *tensors):
+        self._made = [t for t in tensors if t is not None]
+        self._streams = set()
+        if self._made:
+            self._streams.add(torch._C._cuda_getCurrentRawStream(_here()))
+            self._event = torch.cuda.Event()
+            self._event.record()
+
+    def on(self, stream) -> int:
+        """The struct's address for a call on `stream` (None: the current one)."""
+        if self._made:
+            raw = torch._C._cuda_getCurrentRawStream(_here()) if stream is None else _raw_stream(stream)
+            if raw not in self._streams:
+                self._streams.add(raw)
+                other = stream_of(raw)
+                if not torch.cuda.is_current_stream_capturing():               # (a capture begins behind a synchronisation)
+                    other.wait_event(self._event)
+                for t in self._made:
+                    t.record_stream(other)
+        return _at(self.c)
+
+
+class BlockPool(_OnAnyStream):
     """Owns the arrays named by the C struct ``sd_block_pool``: all blocks free, block 0 on top, or the caller's own stack."""
 
     def __init__(self, num_blocks: int, free_blocks: Optional[torch.Tensor] = None, n_free: Optional[torch.Tensor] = None, device="cuda"):
         self.num_blocks = int(num_blocks)
-        if free_blocks is None:
+        own = free_blocks is None
+        if own:
             free_blocks = torch.arange(self.num_blocks - 1, -1, -1, dtype=torch.int32, device=device)
             n_free = torch.full((1,), self.num_blocks, dtype=torch.int32, device=device)
         self.free_blocks = _ints(free_blocks, (self.num_blocks,), "free_blocks")
         self.n_free = _ints(n_free, (1,), "n_free")
         self.c = sd_block_pool(self.free_blocks.data_ptr(), self.n_free.data_ptr(), self.num_blocks)
+        self._makes(*((self.free_blocks, self.n_free) if own else ()))
 
 
 def sd_assign_blocks(pool: BlockPool, block_table, n_blocks, lens, n_new, granted, status, stream=None) -> None:
     """Makes the tables [B, max_blocks] cover lens + n_new tokens (each [B]): n_blocks [B] and the pool are brought up to date,
     granted [B] (or None) is 0 for requests that the pool did not suffice for."""
     B, W = block_table.shape
-    _ints(block_table, (B, W), "block_table")
-    _ints(n_blocks, (B,), "n_blocks")
-    _ints(lens, (B,), "lens")
-    _ints(n_new, (B,), "n_new")
+    here, n = _here(), (B,)
+    _ints(block_table, (B, W), "block_table", here)
+    _ints(n_blocks, n, "n_blocks", here)
+    _ints(lens, n, "lens", here)
+    _ints(n_new, n, "n_new", here)
     if granted is not None:
-        _ints(granted, (B,), "granted")
-    _check(_n.sd_assign_blocks(_at(pool.c), B, W, block_table, n_blocks, lens, n_new, granted, status, stream))
+        _ints(granted, n, "granted", here)
+    _check(_n.sd_assign_blocks(pool.on(stream), B, W, block_table, n_blocks, lens, n_new, granted, status, stream))
 
 
-class Prompts:
+class Prompts(_OnAnyStream):
     """New tokens of B requests in N packed rows: owns the arrays named by the C struct ``sd_prompts``.  Tensors that are int32 on
     the device are taken as they are and may change between calls (sd_prompt_prepare then comes again); others are copied there."""
 
-    def __init__(self, N, Hq, Hkv, D, block_table, lens, n_new, n_blocks=None, num_blocks=None, block_size=64, device="cuda"):
-        dev = torch.device(device)
-        to = lambda a: torch.as_tensor(a, dtype=torch.int32).contiguous().to(dev)
+    def __init__(self, N, Hq, Hkv, D, block_table, lens, n_new, n_blocks=None, *, num_blocks, block_size=64, device="cuda"):
+        dev, made = torch.device(device), []
+
+        def to(a):
+            got = torch.as_tensor(a, dtype=torch.int32).contiguous().to(dev)
+            if got is not a:
+                made.append(got)
+            return got
         self.N, self.Hq, self.Hkv, self.D = int(N), int(Hq), int(Hkv), int(D)
         self.len, self.n_new = to(lens), to(n_new)
         self.B = int(self.len.numel())
@@ -618,7 +657,9 @@ class Prompts:
                             self.block_table.data_ptr(), _ptr(self.n_blocks), self.len.data_ptr(), self.n_new.data_ptr())
         self.plan = torch.empty(max(int(lib.sd_prompt_plan_bytes(self.ref())), 16), dtype=torch.uint8, device=dev)
         self.c.plan = self.plan.data_ptr()
-        self.use(rows(self.B + 1), rows(self.N), rows(self.N))
+        own = rows(self.B + 1), rows(self.N), rows(self.N)
+        self.use(*own)
+        self._makes(self.plan, *own, *made)
 
     def use(self, start, slot, position) -> "Prompts":
         """Puts what sd_prompt_prepare makes into the caller's arrays: start [B + 1], slot and position [N]."""
@@ -642,20 +683,22 @@ def sd_prompt_workspace_bytes(prompts: Prompts) -> int:
 
 def sd_prompt_prepare(prompts: Prompts, status, stream=None) -> None:
     """First rows, slots and positions of the packed tokens, and the plan of their attention; once for all layers of a step."""
-    _check(_n.sd_prompt_prepare(_at(prompts.c), status, stream))
+    _check(_n.sd_prompt_prepare(prompts.on(stream), status, stream))
 
 
 def sd_append_kv(prompts: Prompts, cache: sd_kv_layer, k, v, status, stream=None) -> None:
     """K and V of the packed tokens, [N, Hkv, 128] each (rows may be strided), into one layer's cache."""
-    k, ldk = _heads(k, prompts.N, prompts.Hkv, "k")
-    v, ldv = _heads(v, prompts.N, prompts.Hkv, "v")
-    _check(_n.sd_append_kv(_at(prompts.c), _at(cache), k, ldk, v, ldv, status, stream))
+    here = _here()
+    k, ldk = _heads(k, prompts.N, prompts.Hkv, "k", here)
+    v, ldv = _heads(v, prompts.N, prompts.Hkv, "v", here)
+    _check(_n.sd_append_kv(prompts.on(stream), _at(cache), k, ldk, v, ldv, status, stream))
 
 
 def sd_prompt_attention(prompts: Prompts, cache: sd_kv_layer, q, scale: float, out, lse, workspace, status, stream=None) -> None:
     """Causal attention of the packed tokens over one layer's cache, which holds their own K and V: q, out [N, Hq, 128] (rows may be
     strided), lse [N, Hq] f32 or None."""
-    q, ldq = _heads(q, prompts.N, prompts.Hq, "q")
-    out, ldo = _heads(out, prompts.N, prompts.Hq, "out")
+    here = _here()
+    q, ldq = _heads(q, prompts.N, prompts.Hq, "q", here)
+    out, ldo = _heads(out, prompts.N, prompts.Hq, "out", here)
     _shaped(lse, (prompts.N, prompts.Hq))
-    _check(_n.sd_prompt_attention(_at(prompts.c), _at(cache), q, ldq, scale, out, ldo, lse, workspace, workspace, status, stream))
+    _check(_n.sd_prompt_attention(prompts.on(stream), _at(cache), q, ldq, scale, out, ldo, lse, workspace, workspace, status, stream))

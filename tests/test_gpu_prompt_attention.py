@@ -263,3 +263,64 @@ def test_waits_that_run_out_are_reported(lens, monkeypatch):
     r.status.zero_()
     r.attend()                                               # and the next call finds everything as it should be
     r.check()
+
+
+def test_objects_made_here_are_ready_on_any_stream():
+    """Arrays that Prompts and BlockPool make on a busy stream, used at once on another, and dropped while that still runs."""
+    side = torch.cuda.Stream()
+    keep = Requests([(60, 10), (1, 90)], 7, 1, seed=6)
+    torch.cuda.synchronize()
+    for _ in range(5):
+        torch.cuda._sleep(20000000)                          # the current stream is busy for some ten milliseconds
+        p = sd.Prompts(keep.N, 7, 1, 128, keep.table.tolist(), keep.len.tolist(), keep.new.tolist(), keep.held.tolist(), num_blocks=keep.num_blocks)
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(1000000)
+        sd.sd_prompt_prepare(p, keep.status, side)
+        sd.sd_append_kv(p, keep.cache, keep.k, keep.v, keep.status, side)
+        sd.sd_prompt_attention(p, keep.cache, keep.q, keep.scale, keep.out, keep.lse, keep.work, keep.status, side)
+        del p
+        junk = [torch.full((1 << 16,), 2 ** 30, dtype=torch.int32, device="cuda") for _ in range(8)]
+        torch.cuda.synchronize()
+        del junk
+        keep.check()
+        keep.out.fill_(7.0)
+        keep.lse.fill_(7.0)
+    pool = sd.BlockPool(64)
+    table, held, lens, new = (torch.zeros(s, dtype=torch.int32, device="cuda") for s in ((2, 8), (2,), (2,), (2,)))
+    new += 100
+    torch.cuda.synchronize()
+    torch.cuda._sleep(20000000)
+    pool = sd.BlockPool(64)
+    sd.sd_assign_blocks(pool, table, held, lens, new, None, keep.status, side)
+    torch.cuda.synchronize()
+    assert table[:, :2].tolist() == [[0, 1], [2, 3]] and int(pool.n_free.item()) == 60
+
+
+def test_arguments_that_do_not_fit_are_refused():
+    r = Requests([(5, 3), (2, 0)], 4, 2, seed=1, extra_rows=0)
+    r.prepare()
+    bad = lambda **over: pytest.raises(AssertionError, r.attend, **over)
+    bad(out=r.out[:, :3])
+    bad(out=r.out.float())
+    bad(lse=r.lse[:3])
+    bad(out=torch.empty((r.N, 128, 4), dtype=torch.bfloat16, device="cuda").transpose(1, 2))
+    bad(out=torch.empty((1, 4, 128), dtype=torch.bfloat16, device="cuda").expand(r.N, 4, 128))
+    with pytest.raises(sd.SdError):
+        r.attend(work=r.work[:-1])
+    with pytest.raises(AssertionError):
+        sd.sd_append_kv(r.prompts, r.cache, r.q, r.v, r.status)
+    wide = torch.empty((r.N, 4, 132), dtype=torch.bfloat16, device="cuda")           # heads 132 apart, rows no multiple of 8
+    with pytest.raises(AssertionError):
+        r.attend(out=wide[:, :, :128])
+    odd = torch.empty((r.N * 516 + 8,), dtype=torch.bfloat16, device="cuda")[:r.N * 516].view(r.N, 516)[:, :512].view(r.N, 4, 128)
+    with pytest.raises(sd.SdError) as e:
+        r.attend(out=odd)
+    assert e.value.code == sd.SD_ERR_INVALID_ARG
+    with pytest.raises(AssertionError):
+        r.prompts.use(r.prompts.start, r.prompts.slot[:-1], r.prompts.position)
+    with pytest.raises(AssertionError):
+        r.prompts.use(r.prompts.start.long(), r.prompts.slot, r.prompts.position)
+    with pytest.raises(AssertionError):
+        sd.sd_assign_blocks(sd.BlockPool(8), r.prompts.block_table, r.prompts.n_blocks[:1], r.prompts.len, r.prompts.n_new, None, r.status)
+    torch.cuda.synchronize()
+    assert int(r.status.item()) == 0
