@@ -378,7 +378,7 @@ sd_status launch_prompt_prepare(const sd_prompts& p, int32_t* dev_status, cudaSt
 }
 
 // A token's K and V rows of all KV heads (256 bytes a head) into its slot; unit of work = one 16-byte vector of each, U of them per thread.  Bound
-// by HBM; four units keep enough loads on their way (47195 rows of four heads xxx us with one, xxx with four), one leaves the shortest chain
+// by HBM; four units keep enough loads on their way (47195 rows of four heads 36.9 us with one, 32.8 with four, 5.9 TB/s), one leaves the shortest chain
 // where there are few rows.
 template <int U>
 __global__ void __launch_bounds__(256)

@@ -1,4 +1,4 @@
-// Causal GQA attention of packed new tokens over the paged cache.
+// Causal GQA attention of packed new tokens over the paged cache.  (The first half of this comment says what is done, the second what bounds it.)
 //
 // out = softmax(scale q . K^T) V over the keys t <= len + i, a pass over the keys with a row's weights relative to one of its first scores
 // (see kSumLimit: the reference moves only where a tile's weights add up to more than 2^40, so that no maximum is looked for and nothing
@@ -10,6 +10,16 @@
 // the scores that they come from.  Two groups of four soft-max warps take the tiles in turn; both add to the one O, which works because the
 // reference stays (the rare tile that raises it is serialised through a barrier that every tile passes, commit).  Four more warps normalise
 // and store an entry's rows while the next one's tiles are under way.
+//
+// Eight prompts of 4096 tokens (28 query, 4 KV heads): 811 us, 1187 TFLOP/s, in a few calls; 941 us, 1022 TFLOP/s, in many, because the GPU is at its
+// power cap then (1000 W, 1.49 GHz; a large matrix product sustains 1407 TFLOP/s at 1.36).  A tile of 128 x 128 takes about 1500 cycles of which
+// the tensor pipe is busy for 1024: what passes through shared memory (Q, K and V for the products and the copies, 160 KiB) takes 1280, the
+// exponentials (four a cycle and quarter of the SM) 1024 of both groups' time, and a soft-max warp's tile about 2900 cycles, half of them latencies.
+// Steps, us for those prompts: two row tiles in a CTA that share K and V and wait for each other 935; this stream 892; scores and products
+// with V issued by a warp each (eight instructions take 400 cycles to issue) 862; registers moved to the soft-max warps 842; results
+// stored eight rows at a time (a row a thread made thirty-two lines of every store and held up the barriers) 811.  A quarter to a third of the
+// exponentials as polynomials on the multiply-add units: 2 % off to 8 % on, left out.
+#include <atomic>
 #include "attention_shared.cuh"
 #include "prompt_plan.cuh"
 
@@ -26,11 +36,9 @@ constexpr int kPStage = 2 * kPHalf;
 constexpr int kPQBytes = 2 * kRowTile * 128;
 constexpr int kPBars = 512;                    // barriers, two words and the pieces of work
 constexpr int kPSmem = kPQueryStages * kPQBytes + (kPKeyStages + kPStages) * kPStage + kPBars + 5 * kRowTile * 4;
-#ifndef RS
-#define RS 152
-#define RO 104
-#endif
-constexpr int kSoftmaxRegs = RS, kOtherRegs = RO;        // registers of a thread: 8 warps x 152 + 8 x 104 = 16 x 128, what the launch has
+constexpr int kSoftmaxRegs = 152, kOtherRegs = 104;        // registers of a thread of the eight soft-max warps and the eight others, see setmaxnreg
+constexpr int kLaunchRegs = 128;               // ... that the launch brings: 8 x 152 + 8 x 104 = 16 x 128
+static_assert(kPThreads / 2 * (kSoftmaxRegs + kOtherRegs) <= kPThreads * kLaunchRegs, "");
 constexpr int kMergeThreads = 256;
 
 struct PromptShared {
@@ -370,6 +378,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
                 done_with_work(sh, work_at, lane);
                 if (w.nb == 0) break;
             }
+            const uint64_t hint = w.tokens * a.g.G <= 16 ? once : keep;
             const int32_t* table = a.p.block_table + (size_t)w.b * a.p.max_blocks_per_seq + w.kb0;
             int held = 0;                                  // 32 entries of the table
             const auto block_of = [&](int i) {
@@ -385,11 +394,11 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
                 uint8_t* dst = ring + slot * kPStage;
                 if (elect_one()) {
                     mbar_arrive_expect_tx(&full[slot], two ? kPStage : kPStage / 2);
-                    tma_load_2d(dst, map, 0, y0, &full[slot], keep);
-                    tma_load_2d(dst + kPHalf, map, 64, y0, &full[slot], keep);
+                    tma_load_2d(dst, map, 0, y0, &full[slot], hint);
+                    tma_load_2d(dst + kPHalf, map, 64, y0, &full[slot], hint);
                     if (two) {
-                        tma_load_2d(dst + kPHalf / 2, map, 0, y1, &full[slot], keep);
-                        tma_load_2d(dst + kPHalf + kPHalf / 2, map, 64, y1, &full[slot], keep);
+                        tma_load_2d(dst + kPHalf / 2, map, 0, y1, &full[slot], hint);
+                        tma_load_2d(dst + kPHalf + kPHalf / 2, map, 64, y1, &full[slot], hint);
                     }
                 }
                 __syncwarp();
@@ -425,8 +434,11 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
             // Q is there; or the entry before has left O
             if (!(ok = is_scores ? mbar_wait_warp(&sh.q_full[q_at.slot], q_at.phase, abort_flag, limit) : mbar_wait_warp(sh.o_empty, entry_phase, abort_flag, limit))) break;
             entry_phase ^= 1u;
+            // Products of 64 rows have sixteen in each TMEM quadrant: the first sixteen lie where they do in those of 128.  (Under the power cap what
+            // idle rows do costs time: 32 single tokens behind 512 to 16384 100.2 us at 1.46 GHz, 96.7 at 1.64.)
+            const bool few = w.tokens * a.g.G <= 16;
             if (is_scores) {
-                const uint32_t idesc_s = make_idesc_bf16(kRowTile, kPromptTile, false, false), idesc_half = make_idesc_bf16(kRowTile, kBlock, false, false);
+                const uint32_t idesc_s = make_idesc_bf16(few ? 64 : kRowTile, kPromptTile, false, false), idesc_half = make_idesc_bf16(few ? 64 : kRowTile, kBlock, false, false);
                 const uint64_t q_desc = make_smem_desc(smem_u32(sh.q_smem + q_at.slot * kPQBytes), 16, 1024, 128);
                 const uint64_t k_desc = make_smem_desc(smem_u32(sh.k_smem), 16, 1024, 128);
                 for (int j = 0; 2 * j < w.nb; ++j) {
@@ -452,7 +464,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
                 }
                 q_at.next();
             } else {
-                const uint32_t idesc_o = make_idesc_bf16(kRowTile, kD, false, true);
+                const uint32_t idesc_o = make_idesc_bf16(few ? 64 : kRowTile, kD, false, true);
                 const uint64_t v_desc = make_smem_desc(smem_u32(sh.v_smem), kPHalf, 1024, 128);   // [key][d]: N (= d) contiguous
                 for (int j = 0; 2 * j < w.nb; ++j) {
                     if (!(ok = mbar_wait_warp(&sh.v_full[at.slot], at.phase, abort_flag, limit))) break;
@@ -847,6 +859,14 @@ sd_status launch_prompt_attention(const sd_prompts& p, const sd_kv_layer& cache,
         !encode_tmap_bf16_2d(&vm, cache.v, kv_rows, kD, kD * 2, 64, kBlock, 128))
         return SD_ERR_CUDA;
     if (!allow_dynamic_smem(prompt_kernel, kPSmem)) return SD_ERR_CUDA;
+    // (with fewer registers a thread than the split counts on, setmaxnreg would wait for good)
+    static std::atomic<int> regs{0};
+    if (regs.load(std::memory_order_relaxed) == 0) {
+        cudaFuncAttributes f;
+        if (cudaFuncGetAttributes(&f, prompt_kernel) != cudaSuccess) return SD_ERR_CUDA;
+        regs.store(f.numRegs, std::memory_order_relaxed);
+    }
+    if (regs.load(std::memory_order_relaxed) != kLaunchRegs) return SD_ERR_UNSUPPORTED;
     sd_status s = launch_dependent(prompt_kernel, dim3(a.g.sms), kPThreads, kPSmem, 1, st, qm, km, vm, a, dev_status);
     if (s != SD_OK) return s;
     return launch_dependent(prompt_merge_kernel, dim3(4 * a.g.sms), kMergeThreads, 0, 1, st, a);

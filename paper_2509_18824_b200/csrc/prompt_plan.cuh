@@ -29,7 +29,8 @@ __device__ __forceinline__ RequestSpan request_span(const sd_prompts& p, int b, 
 // Parts are even, but their ends have to be joined (about 6 us), and what an entry costs beside its tiles is not known well (it overlaps its
 // neighbours); dealt out, every CTA has as many entries as the others.  So entries are dealt out where every CTA gets kDealFrom times the
 // longest.  Us, dealt out and in parts: 16 prompts of up to 2048 tokens 135 and 165, three of up to 6000 with twelve heads 190 and 201, eight of
-// 4096 811 and 821; 1000 tokens behind 7000 beside 24 single ones xxx, 32 single tokens behind 512 to 16384 xxx and 96, one behind 2047 xxx and 11.
+// 4096 811 and 821; with entries cut at half a CTA's share and then dealt out, and in parts: one token behind 2047 17 and 11, 32 behind 512 to
+// 16384 117 and 94, 61 behind 16000 41 and 28.
 constexpr int kPromptTile = 128;               // keys per tile: two cache blocks
 constexpr int kEntryTiles = 2;                 // what an entry costs beside its key tiles, in key tiles
 constexpr int kPartMin = 2;                    // the shortest part of a CTA
