@@ -617,9 +617,11 @@ sd_status sd_distill_grad(const void *logits, int32_t dtype, int64_t ld, int32_t
  *   block_table : dev [B][max_blocks_per_seq], entries beyond n_blocks may hold anything; they are left as they are
  *   n_blocks    : dev [B], in and out
  *   len, n_new  : dev [B] (an sd_batch's len and n_nodes for the trees of a step; both 0 for a request that is done)
- *   granted     : dev [B] or NULL: 1, or 0 for requests that got none
+ *   granted     : dev [B] or NULL: 1, or 0 for requests that got none or whose numbers are out of range
+ * A block is one request's or the stack's: tables that share blocks are not for this call.
  * 1 <= B <= 8192, B * max_blocks_per_seq < 2^29.  A negative length stores SD_ERR_INVALID_ARG; more tokens than the table's row holds, or n_blocks or *n_free out of
- * range, SD_ERR_BOUNDS: that request keeps what it has (with *n_free out of range the stack counts as empty).  The arrays must not overlap.
+ * range, SD_ERR_BOUNDS: that request keeps what it has (with *n_free out of range the stack counts as empty).  A block outside [0, num_blocks)
+ * that is given back or taken stores SD_ERR_BOUNDS as well.  The arrays must not overlap.
  */
 sd_status sd_assign_blocks(const sd_block_pool *pool, int32_t B, int32_t max_blocks_per_seq, int32_t *block_table,
                            int32_t *n_blocks, const int32_t *len, const int32_t *n_new, int32_t *granted,
@@ -649,6 +651,7 @@ sd_status sd_append_kv(const sd_prompts *prompts, const sd_kv_layer *cache, cons
  *   q, out    : dev bf16, head h of row r at element r * ld + h * 128 (ld >= Hq * 128, a multiple of 8); out must not overlap q
  *   lse       : dev f32 [N][Hq] or NULL; natural-log sum of exp of the scaled scores
  *   workspace : dev scratch of at least sd_prompt_workspace_bytes(prompts); calls that may run at the same time need one each
+ * num_blocks * Hkv < 2^25.  Tables may share blocks that are only read.
  * Rows of nobody and of requests that were left out are not written.  Slots behind a request's last token may hold any bit pattern.
  * Arithmetic: bf16 inputs, fp32 accumulation, weights rounded to bf16 in front of the product with V, bf16 output.  Range as
  * sd_verify_attention; K and V of the request's own tokens have to be finite.

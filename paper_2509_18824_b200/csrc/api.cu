@@ -453,6 +453,7 @@ sd_status sd_prompt_attention(const sd_prompts* prompts, const sd_kv_layer* cach
     if (workspace_bytes < prompt_workspace_bytes(*prompts)) return SD_ERR_WORKSPACE;
     if (prompts->N == 0) return SD_OK;
     if (!ok_heads(q, ldq, prompts->Hq) || !ok_heads(out, ldo, prompts->Hq) || out == q) return SD_ERR_INVALID_ARG;
+    if ((int64_t)cache->num_blocks * prompts->Hkv * kBlock > INT32_MAX) return SD_ERR_UNSUPPORTED;             // (rows of the copies' coordinates)
     return launch_prompt_attention(*prompts, *cache, q, ldq, scale, out, ldo, lse, workspace, dev_status,
                                    static_cast<cudaStream_t>(stream));
 }

@@ -12,6 +12,7 @@ using namespace sm100;
 namespace {
 constexpr int kFewThreads = 256, kManyThreads = 1024;
 constexpr int kOrderBins = 1024;
+constexpr int kNotHeld = -1;                   // in place of the blocks of a request whose numbers are out of range
 
 // Sums of whole numbers from 0 up stop at 2^29, which no count of rows or blocks reaches: what is behind that does not fit anyway.
 constexpr int kMost = 1 << 29;
@@ -90,7 +91,10 @@ assign_blocks_kernel(sd_block_pool pool, int B, int W, int32_t* table, int32_t* 
             int bad = 0;
             if (l < 0 || n < 0) bad = SD_ERR_INVALID_ARG;
             else if (held < 0 || held > W || want > W) bad = SD_ERR_BOUNDS;
-            if (bad) { if (first) set_status(status, bad); }                    // (and the request keeps what it has)
+            if (bad) {                                                          // (and the request keeps what it has)
+                if (first) set_status(status, bad);
+                held = kNotHeld;
+            }
             else if (want > held) move[0] = (int)want - held;
             else move[1] = held - (int)want;
         }
@@ -123,16 +127,18 @@ assign_blocks_kernel(sd_block_pool pool, int B, int W, int32_t* table, int32_t* 
         const int b = last_at_most(grow_at, B, t);
         const int block = t < come_free ? released(t) : __ldcg(pool.free_blocks + n_free - 1 - (t - come_free));
         table[(size_t)b * W + held_of[b] + (t - grow_at[b])] = block;
+        if (block < 0 || block >= pool.num_blocks) set_status(status, SD_ERR_BOUNDS);
     }
     for (int t = taken + tid; t < come_free; t += threads) {
         const int at = n_free + come_free - 1 - t;
-        if (at < pool.num_blocks) pool.free_blocks[at] = released(t);
-        else set_status(status, SD_ERR_BOUNDS);            // (more than the pool has: given back twice)
+        const int block = released(t);
+        if (at < pool.num_blocks) pool.free_blocks[at] = block;
+        if (at >= pool.num_blocks || block < 0 || block >= pool.num_blocks) set_status(status, SD_ERR_BOUNDS);     // (more than the pool has: given back twice)
     }
     if (ctas > 1) cluster_wait_acquire();
     for (int b = tid; b < B; b += threads) {
         const int grow = grow_at[b + 1] - grow_at[b], shrink = free_at[b + 1] - free_at[b];
-        const bool ok = grow_at[b + 1] <= taken || grow == 0;
+        const bool ok = held_of[b] != kNotHeld && (grow_at[b + 1] <= taken || grow == 0);
         if (grow && ok) n_blocks[b] = held_of[b] + grow;
         if (shrink) n_blocks[b] = held_of[b] - shrink;
         if (granted) granted[b] = ok ? 1 : 0;
@@ -312,15 +318,16 @@ prompt_prepare_kernel(sd_prompts p, PromptGeom geom, int rows, int32_t* status) 
     // ------------------------------------------------ in parts
     // where part c begins, given the entry that its cut lies in and where that begins in the line
     const auto cut_at = [&](long long c, int e, int tiles, long long from) {
-        const int one = tiles + kEntryTiles, off = (int)min(c * part - from, (long long)Hkv * one);
-        int h = off / one, tile = max(off - h * one - kEntryTiles, 0);
+        const int one = tiles + kEntryTiles;
+        const long long off = min(c * part - from, (long long)Hkv * one);
+        int h = off < kMost ? (int)off / one : (int)(off / one), tile = max((int)(off - (long long)h * one) - kEntryTiles, 0);
         // (a chunk of a few tiles is not worth joining, unless the parts are not much longer)
         if (part > 32 * kSnap && tile <= kSnap) tile = 0;
         else if (part > 32 * kSnap && tile >= tiles - kSnap) { tile = 0; ++h; }
         if (h == Hkv) { h = 0; ++e; }
         starts[c] = PromptStart{e, h, tile, 0, entry(min(e, entries - 1))};
     };
-    const bool few = entries <= kOrderBins && all_cost[0] < kMost;             // (then there may be many cuts to an entry: a thread for each of them)
+    const bool few = entries <= kOrderBins && line < kMost;                    // (then there may be many cuts to an entry: a thread for each of them)
     long long at = 0;
     for_own([&](int e, int tiles) {
         const long long one = tiles < 0 ? 0 : tiles + kEntryTiles;             // of one head

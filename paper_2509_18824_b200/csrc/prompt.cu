@@ -20,6 +20,7 @@
 // stored eight rows at a time (a row a thread made thirty-two lines of every store and held up the barriers) 811.  A quarter to a third of the
 // exponentials as polynomials on the multiply-add units: 2 % off to 8 % on, left out.
 #include <atomic>
+#include <type_traits>
 #include "attention_shared.cuh"
 #include "prompt_plan.cuh"
 

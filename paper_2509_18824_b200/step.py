@@ -355,5 +355,6 @@ class PromptStep:
 
     def reserve_trees(self, stream=None):
         """Blocks for the trees of the next verification (or what behind it is not needed, given back): tables that cover len + n_nodes."""
+        assert self.pool is not None, "the tables are the caller's: there is no pool to take blocks from"
         p, b = self.prompts, self.step.batch
         sd.sd_assign_blocks(self.pool, p.block_table, p.n_blocks, b.len, b.n_nodes, self.granted, self.step.status, stream)

@@ -180,3 +180,71 @@ def test_rows_reach_their_slots_and_nothing_else_changes(heads, strided):
     assert int(r.status.item()) == 0
     for cache, w in zip((r.k_cache, r.v_cache), want):
         np.testing.assert_array_equal(cache.view(torch.int16).cpu().numpy(), w)
+
+
+@pytest.mark.parametrize("B", [3, 400])
+def test_requests_out_of_range_are_not_granted(B):
+    p = Pages([100] * B, 6, 20, seed=4)
+    lens, new = np.full(B, 100), np.zeros(B, dtype=np.int64)
+    lens[1], new[0] = 400, 100                               # seven blocks of six; four
+    p.call(lens, new)
+    torch.cuda.synchronize()
+    assert int(p.status.item()) == sd.SD_ERR_BOUNDS
+    assert p.granted.tolist() == [1, 0] + [1] * (B - 2) and p.d_held.tolist() == [4] + [2] * (B - 1)
+
+
+@pytest.mark.parametrize("bad", [-1, 24, 2 ** 30])
+def test_blocks_out_of_range_that_change_hands_are_reported(bad):
+    p = Pages([100, 100], 6, 20, seed=4)
+    p.d_table[1, 1] = bad                                    # given back
+    p.call(np.array([100, 0]), np.zeros(2))
+    torch.cuda.synchronize()
+    assert int(p.status.item()) == sd.SD_ERR_BOUNDS and int(p.pool.n_free.item()) == 22
+    p.status.zero_()
+    p.call(np.array([100, 100]), np.zeros(2))                # and taken
+    torch.cuda.synchronize()
+    assert int(p.status.item()) == sd.SD_ERR_BOUNDS and p.d_table[1, 1].item() == bad
+
+
+def test_the_most_requests():
+    B = 8192
+    g = np.random.default_rng(9)
+    lens, new = g.integers(0, 300, B), g.integers(0, 4, B)
+    p = Pages(lens, 8, 12000, seed=9)
+    p.call(lens, new)
+    p.check(lens, new)
+    N = int(new.sum()) + 5
+    q = sd.Prompts(N, 2, 1, 128, p.d_table, lens, new, p.d_held, num_blocks=p.num_blocks)
+    sd.sd_prompt_prepare(q, p.status)
+    torch.cuda.synchronize()
+    assert int(p.status.item()) == 0
+    for got, want in zip((q.start, q.slot, q.position), ref.slots(p.table, p.held, lens, new, N)):
+        np.testing.assert_array_equal(got.cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("B, Hkv, tokens", [(40, 8, 100000), (3, 64, 2 ** 24), (1500, 4, 2 ** 19), (1, 2, 10 ** 6)])
+def test_parts_are_equal_however_long(B, Hkv, tokens):
+    """Single tokens behind long contexts: where the CTAs' parts begin, as the plan's words say it (entries of key tiles and two more)."""
+    g = np.random.default_rng(B)
+    lens = tokens - g.integers(0, tokens // 2, B) - 1
+    if B > 1000:
+        lens[1:] = g.integers(0, 200, B - 1)                 # (that many of one length would be dealt out)
+    W = blocks(tokens)
+    q = sd.Prompts(B, Hkv, Hkv, 128, torch.zeros((B, W), dtype=torch.int32, device="cuda"), lens, np.ones(B, dtype=np.int32), num_blocks=1)
+    st = sd.new_status()
+    sd.sd_prompt_prepare(q, st)
+    torch.cuda.synchronize()
+    assert int(st.item()) == 0
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    words = q.plan.cpu().numpy()[:16 + 48 * (sms + 1)].view(np.int32)
+    assert words[1] == 0                                     # in parts
+    starts = words[4:].reshape(sms + 1, 12)[:, :3].astype(np.int64)
+    one = -(-(lens // 64 + 1) // 2) + 2
+    before = np.concatenate([[0], np.cumsum(one)]) * Hkv
+    line = int(before[-1])
+    part = -(-line // sms)
+    e, h, tile = starts.T
+    assert tuple(starts[-1]) == (B, 0, 0)
+    at = before[e] + h * np.append(one, 0)[e] + np.where(tile > 0, tile + 2, 0)
+    want = np.minimum(np.arange(sms + 1) * part, line)
+    assert np.abs(at - want).max() <= 6 and (np.diff(at) > 0).all()

@@ -324,3 +324,44 @@ def test_arguments_that_do_not_fit_are_refused():
         sd.sd_assign_blocks(sd.BlockPool(8), r.prompts.block_table, r.prompts.n_blocks[:1], r.prompts.len, r.prompts.n_new, None, r.status)
     torch.cuda.synchronize()
     assert int(r.status.item()) == 0
+
+
+def test_two_calls_at_once():
+    """Two layers on two streams, one plan, a workspace each: entries that are cut, joined by both."""
+    a, c = (Requests([(1, 3000), (60, 900), (1, 17), (300, 0)], 14, 2, seed=8, gain=gain) for gain in (1.0, 3.0))
+    a.prepare()
+    torch.cuda.synchronize()
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(20):
+        for r, s in zip((a, c), streams):
+            sd.sd_append_kv(a.prompts, r.cache, r.k, r.v, r.status, s)
+            sd.sd_prompt_attention(a.prompts, r.cache, r.q, r.scale, r.out, r.lse, r.work, r.status, s)
+    a.check()
+    c.check()
+
+
+def test_two_captured_steps_share_a_workspace_one_after_the_other():
+    a, c = (Requests([(1, 2000), (33, 500)], 7, 1, seed=s) for s in (1, 2))
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    for r, g in ((a, graphs[0]), (c, graphs[1])):
+        torch.cuda.synchronize()
+        with torch.cuda.graph(g):
+            r.prepare()
+            r.append()
+            r.attend(work=a.work)
+    for g in graphs * 3:
+        g.replay()
+    a.check()
+    c.check()
+
+
+def test_a_prefix_that_requests_share():
+    """Blocks that several tables name are read by all of them."""
+    r = Requests([(5, 256), (70, 300), (1, 700)], 8, 2, seed=6)
+    r.table[1, :4] = r.table[0, :4]
+    r.table[2, :4] = r.table[0, :4]
+    r.prompts.block_table.copy_(torch.from_numpy(r.table))
+    r.prepare()
+    r.append()
+    r.attend()
+    r.check()

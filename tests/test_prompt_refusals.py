@@ -67,6 +67,11 @@ def test_tables():
     assert assign(blocks=(1 << 25) + 1) == b.SD_ERR_UNSUPPORTED
 
 
+def test_caches_whose_rows_pass_32_bits():
+    many = dict(Hq=64, Hkv=64, ldq=8192, ldo=8192, blocks=1 << 19, cache=(ok, ok, 1 << 19))
+    assert attend(**many) == b.SD_ERR_UNSUPPORTED
+
+
 def test_sizes_of_refused_geometries_are_zero():
     assert b.lib.sd_prompt_plan_bytes(ctypes.byref(prompts())) > 0
     for bad in (dict(D=64), dict(B=0), dict(Hq=9)):
