@@ -20,7 +20,6 @@
 // stored eight rows at a time (a row a thread made thirty-two lines of every store and held up the barriers) 811.  A quarter to a third of the
 // exponentials as polynomials on the multiply-add units: 2 % off to 8 % on, left out.
 #include <atomic>
-#include <type_traits>
 #include "attention_shared.cuh"
 #include "prompt_plan.cuh"
 
@@ -217,6 +216,17 @@ __device__ __forceinline__ void done_with_work(const PromptShared& sh, RingAt<kP
 }
 
 __device__ __forceinline__ uint64_t twice(float c) { return pack_f32x2(c, c); }
+__device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t pack_bf16x2(uint64_t a) {
+    float lo, hi;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(a));
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
 
 // What the soft-max of a row hands from tile to tile.
 struct RowState {
@@ -536,18 +546,13 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
                 const bool masked = all_see < (j + 1) * kPromptTile;           // some row does not see some key (or there is one block)
                 int hb = 0, blocks = 2;                    // blocks that are done, of how many
                 int vis = kPromptTile;                     // keys of the tile that this row sees
-                const auto weigh = [&](auto with_mask) -> bool {
-                    constexpr bool kMasked = decltype(with_mask)::value;
+                const auto weigh = [&]() -> bool {
                     uint32_t ra[32], rb[32], pk[32];
                     uint64_t ps[2] = {0ull, 0ull};
                     tmem_ld32(ts, ra);
-                    const auto hide = [&](uint32_t (&x)[32], int c) {
-                        if (kMasked) mask_scores(x, vis >= c + 32 ? ~0u : (1u << max(vis - c, 0)) - 1u);
-                    };
                     st.raised = 1.f;
                     tmem_ld_wait();
                     tmem_ld32(ts + 32, rb);                // (the next scores are on their way)
-                    hide(ra, 0);
                     if (j == 0) {                          // the reference: the largest of the first 32 scores that the row sees, as a whole number
                         float mt = fmaxf(__uint_as_float(ra[0]), __uint_as_float(ra[1]));
 #pragma unroll
@@ -560,8 +565,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
                     const uint64_t neg_m2 = twice(-st.m);
                     exp_pack(ra, scale2, neg_m2, pk, ps);
                     tmem_ld_wait();
-                    if (!kMasked || blocks == 2) tmem_ld32(ts + 64, ra);
-                    hide(rb, 32);
+                    if (blocks == 2) tmem_ld32(ts + 64, ra);
                     exp_pack(rb, scale2, neg_m2, pk + 16, ps);
                     float psum = sum_f32x2(add_f32x2(ps[0], ps[1]));
                     // the tile before is final, and its reference still the one used here
@@ -572,13 +576,11 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
                     tmem_st32(ts, pk);                     // over scores that have been read
                     st.l += psum;
                     hb = 1;
-                    if (kMasked && blocks == 1) return true;
+                    if (blocks == 1) return true;
                     ps[0] = ps[1] = 0ull;
                     tmem_ld32(ts + 96, rb);
-                    hide(ra, 64);
                     exp_pack(ra, scale2, neg_m2, pk, ps);
                     tmem_ld_wait();
-                    hide(rb, 96);
                     exp_pack(rb, scale2, neg_m2, pk + 16, ps);
                     psum = sum_f32x2(add_f32x2(ps[0], ps[1]));
                     if (__any_sync(0xffffffffu, row_ok && !(psum <= kSumLimit))) return true;
@@ -587,9 +589,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
                     hb = 2;
                     return true;
                 };
-                if (!masked && !idle) {
-                    ok = weigh(std::false_type{});
-                } else {
+                if (masked || idle) {
                     vis = row_ok ? seen - j * kPromptTile : kPromptTile;
                     blocks = 2 * j + 1 == w.nb ? 1 : 2;
                     // V rows behind the request's last token carry weight 0, but 0 x NaN would still reach O: cleared before P.V reads them
@@ -602,13 +602,25 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
                             fence_proxy_async_smem();
                         }
                     }
-                    if (!idle) {
-                        ok = weigh(std::true_type{});
-                    } else {                               // none of the warp's rows is read: it keeps its place among the barriers
-                        if (j == 0 && lane == 0) mbar_arrive(ref_full);
-                        if (begun) ok = mbar_wait_warp(commit, commit_phase, abort_flag, limit);
-                        hb = blocks;
+                    // Hidden scores become -inf where they stand, 32 keys at a time where some row does not see them all.  (Sixteen ragged prompts of
+                    // up to 2048 tokens 153 us with the masks in a second copy of what follows, 141 so.)
+                    const int c0 = __reduce_min_sync(0xffffffffu, vis) & ~31;
+#pragma unroll 1
+                    for (int c = max(c0, 0); c < blocks * kBlock; c += 32) {
+                        uint32_t x[32];
+                        tmem_ld32(ts + c, x);
+                        tmem_ld_wait();
+                        mask_scores(x, vis >= c + 32 ? ~0u : (1u << max(vis - c, 0)) - 1u);
+                        tmem_st32(ts + c, x);
                     }
+                    tmem_st_wait();
+                }
+                if (!idle) {
+                    ok = weigh();
+                } else {                                   // none of the warp's rows is read: it keeps its place among the barriers
+                    if (j == 0 && lane == 0) mbar_arrive(ref_full);
+                    if (begun) ok = mbar_wait_warp(commit, commit_phase, abort_flag, limit);
+                    hb = blocks;
                 }
                 if (!ok) break;
                 if (hb < blocks) {
@@ -687,49 +699,37 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
                         reinterpret_cast<uint4*>(part)[(c * 8 + x) * a.g.rows + r] = make_uint4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
                 }
             } else {
-                // Eight rows at a time, 64 bytes of each: a row per thread would make 32 lines of every store, whose passes through the
-                // load-store unit hold up the other warps' barriers.
+                // A row per thread would make 32 lines of every store, whose passes through the load-store unit hold up the other warps' barriers;
+                // so the rows go back to tensor memory in bf16, over columns of O that have been read, and are loaded as eight rows of 32 bytes.
+                // (Transposed among four threads instead, with 64 shuffles: 140 us for those prompts, 136 so.  Leaving O with all of it in registers: 153,
+                // the soft-max warps spill.)
+                const uint64_t inv2 = twice(inv);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t o[32], pk[16];
+                    tmem_ld32(tmem + lanes + c * 32, o);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) pk[x] = pack_bf16x2(mul_f32x2(pack_f32x2(__uint_as_float(o[2 * x]), __uint_as_float(o[2 * x + 1])), inv2));
+                    tmem_st16(tmem + lanes + c * 16, pk);
+                }
+                tmem_st_wait();
                 const int q4 = lane & 3;
-#pragma unroll 1
+#pragma unroll
                 for (int up = 0; up < 2; ++up) {           // rows 0-15 and 16-31 of the quadrant
-                    __nv_bfloat16* to[2];
-                    float by[2];
-                    bool there[2];
                     uint32_t o[2][16];
+                    tmem_ld_16x256b_x4(tmem + lanes + ((uint32_t)(up * 16) << 16), o[0]);
+                    tmem_ld_16x256b_x4(tmem + lanes + ((uint32_t)(up * 16) << 16) + 32, o[1]);
+                    tmem_ld_wait();
+                    if (up == 1) leave();
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
-                        const int rr = up * 16 + x * 8 + (lane >> 2), t_row = a.g.token_of(quad * 32 + rr), hd = quad * 32 + rr - t_row * a.g.G;
-                        by[x] = __shfl_sync(0xffffffffu, inv, rr);
-                        there[x] = t_row < w.tokens;
-                        to[x] = a.out + (size_t)(w.row0 + t_row) * a.ldo + ((size_t)w.h * a.g.G + hd) * kD + q4 * 8;
-                    }
+                        const int rr = quad * 32 + up * 16 + x * 8 + (lane >> 2), t_row = a.g.token_of(rr);
+                        if (t_row >= w.tokens) continue;
+                        __nv_bfloat16* const to = a.out + (size_t)(w.row0 + t_row) * a.ldo + ((size_t)w.h * a.g.G + (rr - t_row * a.g.G)) * kD + q4 * 4;
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        if ((c & 1) == 0) {                // two loads on their way together
-                            tmem_ld_16x256b_x4(tmem + lanes + ((uint32_t)(up * 16) << 16) + c * 32, o[0]);
-                            tmem_ld_16x256b_x4(tmem + lanes + ((uint32_t)(up * 16) << 16) + c * 32 + 32, o[1]);
-                            tmem_ld_wait();
-                            if (up == 1 && c == 2) leave();
-                        }
-#pragma unroll
-                        for (int x = 0; x < 2; ++x) {
-                            uint32_t u[4];                 // this thread's two columns of four eights; then its eight columns
-#pragma unroll
-                            for (int y = 0; y < 4; ++y) {
-                                const __nv_bfloat162 hh = __floats2bfloat162_rn(__uint_as_float(o[c & 1][4 * y + 2 * x]) * by[x], __uint_as_float(o[c & 1][4 * y + 2 * x + 1]) * by[x]);
-                                u[y] = *reinterpret_cast<const uint32_t*>(&hh);
-                            }
-#pragma unroll
-                            for (int d = 1; d < 4; d <<= 1)
-#pragma unroll
-                                for (int y = 0; y < 4; ++y) {
-                                    if (y & d) continue;
-                                    const bool odd = (q4 & d) != 0;
-                                    const uint32_t got = __shfl_xor_sync(0xffffffffu, odd ? u[y] : u[y | d], d);
-                                    if (odd) u[y] = got; else u[y | d] = got;
-                                }
-                            if (there[x]) *reinterpret_cast<uint4*>(to[x] + c * 32) = make_uint4(u[0], u[1], u[2], u[3]);
-                        }
+                        for (int c = 0; c < 8; ++c)
+                            *reinterpret_cast<uint2*>(to + c * 16) = make_uint2(o[c >> 2][4 * (c & 3) + 2 * x], o[c >> 2][4 * (c & 3) + 2 * x + 1]);
                     }
                 }
             }
