@@ -243,14 +243,33 @@ struct TileAt {
     uint32_t o_phase;
     int row_ok;
 };
-// A tile from block hb on (the tile before it is final), looked at before anything is weighed: the reference that another tile has raised since, and
-// references that have to be raised (to the largest score, where that is more than 2^32 above).  (A call: in line it made the usual tile's
-// code slower.)
+// A tile whose blocks in front of hb have been weighed (the tile before it is final).  Those get the reference that another tile has raised
+// since; the others are looked at before they are weighed, and references raised where they have to be (to the largest score, where that is more than
+// 2^32 above).  (A call: in line it made the usual tile's code slower.)
 __device__ __noinline__ RowState careful_tile(RowState st, const TileAt t, int hb, float scale_log2, volatile float* my_ref, int* abort_flag,
                                               long long limit) {
     const uint64_t scale2 = twice(scale_log2);
-    const float ref = *my_ref;
-    if (ref != st.m) { st.l *= exp2f(st.m - ref); st.m = ref; }
+    const auto scale_weights = [&](int block, float by) {
+        uint32_t o[32];
+        tmem_ld32(t.ts + block * 32, o);
+        tmem_ld_wait();
+#pragma unroll
+        for (int x = 0; x < 32; ++x) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(bf16lo(o[x]) * by, bf16hi(o[x]) * by);
+            o[x] = *reinterpret_cast<const uint32_t*>(&h);
+        }
+        tmem_st32(t.ts + block * 32, o);
+        tmem_st_wait();
+    };
+    tmem_st_wait();
+    const float ref = t.row_ok ? *my_ref : st.m;
+    if (__any_sync(0xffffffffu, ref != st.m)) {            // (by whole powers of two: the weights' digits stay)
+        const float by = ref != st.m ? exp2f(st.m - ref) : 1.f;
+#pragma unroll 1
+        for (int i = 0; i < hb; ++i) scale_weights(i, by);
+        st.l *= by;
+        st.m = ref;
+    }
 #pragma unroll 1
     for (; hb < t.blocks; ++hb) {
         const uint32_t tb = t.ts + hb * kBlock;
@@ -283,17 +302,7 @@ __device__ __noinline__ RowState careful_tile(RowState st, const TileAt t, int h
                     tmem_st32(t.to + c * 32, o);
                 }
             }
-            if (hb > 0) {
-                uint32_t o[32];
-                tmem_ld32(t.ts, o);
-                tmem_ld_wait();
-#pragma unroll
-                for (int x = 0; x < 32; ++x) {
-                    const __nv_bfloat162 h = __floats2bfloat162_rn(bf16lo(o[x]) * alpha, bf16hi(o[x]) * alpha);
-                    o[x] = *reinterpret_cast<const uint32_t*>(&h);
-                }
-                tmem_st32(t.ts, o);
-            }
+            if (hb > 0) scale_weights(0, alpha);
             tmem_st_wait();
             st.l *= alpha;
             st.raised *= alpha;
@@ -546,7 +555,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
                 const bool masked = all_see < (j + 1) * kPromptTile;           // some row does not see some key (or there is one block)
                 int hb = 0, blocks = 2;                    // blocks that are done, of how many
                 int vis = kPromptTile;                     // keys of the tile that this row sees
-                const auto weigh = [&]() -> bool {
+                const auto weigh = [&] {
                     uint32_t ra[32], rb[32], pk[32];
                     uint64_t ps[2] = {0ull, 0ull};
                     tmem_ld32(ts, ra);
@@ -568,26 +577,22 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
                     if (blocks == 2) tmem_ld32(ts + 64, ra);
                     exp_pack(rb, scale2, neg_m2, pk + 16, ps);
                     float psum = sum_f32x2(add_f32x2(ps[0], ps[1]));
-                    // the tile before is final, and its reference still the one used here
-                    if (begun && !mbar_wait_warp(commit, commit_phase, abort_flag, limit)) return false;
-                    const float ref = *my_ref;
                     tmem_ld_wait();
-                    if (__any_sync(0xffffffffu, row_ok && (ref != st.m || !(psum <= kSumLimit)))) return true;
+                    if (__any_sync(0xffffffffu, row_ok && !(psum <= kSumLimit))) return;
                     tmem_st32(ts, pk);                     // over scores that have been read
                     st.l += psum;
                     hb = 1;
-                    if (blocks == 1) return true;
+                    if (blocks == 1) return;
                     ps[0] = ps[1] = 0ull;
                     tmem_ld32(ts + 96, rb);
                     exp_pack(ra, scale2, neg_m2, pk, ps);
                     tmem_ld_wait();
                     exp_pack(rb, scale2, neg_m2, pk + 16, ps);
                     psum = sum_f32x2(add_f32x2(ps[0], ps[1]));
-                    if (__any_sync(0xffffffffu, row_ok && !(psum <= kSumLimit))) return true;
+                    if (__any_sync(0xffffffffu, row_ok && !(psum <= kSumLimit))) return;
                     tmem_st32(ts + 32, pk);
                     st.l += psum;
                     hb = 2;
-                    return true;
                 };
                 if (masked || idle) {
                     vis = row_ok ? seen - j * kPromptTile : kPromptTile;
@@ -615,15 +620,15 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
                     }
                     tmem_st_wait();
                 }
-                if (!idle) {
-                    ok = weigh();
-                } else {                                   // none of the warp's rows is read: it keeps its place among the barriers
+                if (!idle) weigh();                        // (rows that nobody reads only keep their place among the barriers)
+                else {
                     if (j == 0 && lane == 0) mbar_arrive(ref_full);
-                    if (begun) ok = mbar_wait_warp(commit, commit_phase, abort_flag, limit);
                     hb = blocks;
                 }
-                if (!ok) break;
-                if (hb < blocks) {
+                // The tile before is final: is its reference still the one used here?  (Looked at behind the weights, not in front of them, so that the groups
+                // wait for one another as little as can be.)
+                if (begun && !(ok = mbar_wait_warp(commit, commit_phase, abort_flag, limit))) break;
+                if (__any_sync(0xffffffffu, hb < blocks || (row_ok && *my_ref != st.m))) {
                     const int last = s_at.slot == 0 ? kPStages - 1 : s_at.slot - 1;
                     const TileAt t{ts, tmem + lanes, vis, blocks, j == 0, &sh.v_empty[last], s_at.slot == 0 ? s_at.phase ^ 1u : s_at.phase, row_ok};
                     st = careful_tile(st, t, hb, a.scale_log2, my_ref, abort_flag, limit);
