@@ -312,6 +312,9 @@ prompt_prepare_kernel(sd_prompts p, PromptGeom geom, int rows, int32_t* status) 
             const int at = put(tiles);
             if (tiles >= 0) order[at] = e;
         });
+        __syncthreads();
+        // every CTA's first piece, so that it need not look for it
+        for (int c = threadIdx.x; c < geom.sms && c < (long long)entries * Hkv; c += THREADS) starts[c] = PromptStart{c, c % Hkv, 0, 0, list[order[c / Hkv]]};
         if (threadIdx.x == 0) *plan_header(p.plan) = PromptHeader{0, entries, plan_stamp(p, geom), 0};
         return;
     }

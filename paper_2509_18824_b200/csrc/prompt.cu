@@ -167,8 +167,7 @@ struct PromptWalk {
         if (dealt) {
             round = tile = 0;
             e1 = entries * a.p.Hkv;                        // (below 2^31: 2^24 rows of 1024 heads at most, 16 or more tokens to a row tile)
-            e = (int)blockIdx.x;
-            if (e < e1) fetch(a.p.Hkv);
+            e = (int)blockIdx.x;                           // (its entry stands in the start)
         }
     }
     __device__ __forceinline__ void fetch(int Hkv) {

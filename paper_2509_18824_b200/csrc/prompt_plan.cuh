@@ -28,11 +28,11 @@ __device__ __forceinline__ RequestSpan request_span(const sd_prompts& p, int b, 
 //   CTA has at most two such chunks, its first and its last piece.
 // Parts are even, but their ends have to be joined (about 6 us), and what an entry costs beside its tiles is not known well (it overlaps its
 // neighbours); dealt out, every CTA has as many entries as the others.  So entries are dealt out where every CTA gets kDealFrom times the
-// longest.  Us, dealt out and in parts: 16 prompts of up to 2048 tokens 135 and 165, three of up to 6000 with twelve heads 190 and 201, eight of
-// 4096 811 and 821; with entries cut at half a CTA's share and then dealt out, and in parts: one token behind 2047 17 and 11, 32 behind 512 to
+// longest.  Us, dealt out and in parts (when a tile took a tenth longer than now): 16 prompts of up to 2048 tokens 135 and 165, three of up to 6000
+// with twelve heads 190 and 201, eight of 4096 811 and 821; with entries cut at half a CTA's share and then dealt out, and in parts: one token behind 2047 17 and 11, 32 behind 512 to
 // 16384 117 and 94, 61 behind 16000 41 and 28.
 constexpr int kPromptTile = 128;               // keys per tile: two cache blocks
-constexpr int kEntryTiles = 2;                 // what an entry costs beside its key tiles, in key tiles
+constexpr int kEntryTiles = 2;                 // what an entry costs beside its key tiles, in key tiles (1 and 3: the same within 1 %)
 constexpr int kPartMin = 2;                    // the shortest part of a CTA
 constexpr int kDealFrom = 4;
 constexpr int kSnap = 3;                       // a cut so few key tiles from an entry's end is made there
@@ -44,7 +44,7 @@ struct alignas(16) PromptEntry {
     int end;               // len + n_new of the request
     int unused0, unused1;
 };
-struct alignas(16) PromptStart { int e, h, tile, unused; PromptEntry entry; };  // where a CTA's part begins (and the one's before ends)
+struct alignas(16) PromptStart { int e, h, tile, unused; PromptEntry entry; };  // where a CTA's part begins (and the one's before ends); dealt out: its first piece
 struct alignas(16) PromptSplit {
     int row0, tokens, h;
     int slot, cta, chunks;                     // partial results: slot, then 2 (cta + 1), 2 (cta + 2) ..
