@@ -10,6 +10,9 @@ namespace sdv {
 using namespace sm100;
 
 namespace {
+// Threads of a CTA: a pass of the scans is shorter with few, and with many there are fewer passes.  Us, 256 threads and 1024 (blocks: in a cluster
+// of eight), blocks / slots and plan: 64 requests of 60 new tokens 3.4 and 4.2 / 6.4 and 7.2, 256 of one 3.6 and 4.4 / 6.8 and 7.5, 256 of 60 (15360 rows) 3.8
+// and 4.6 / 7.5 and 7.0, 400 of 30 4.5 and 4.5 / 8.7 and 7.3, 2000 of 50 15.5 and 6.7 / 39 and 19.
 constexpr int kFewThreads = 256, kManyThreads = 1024;
 constexpr int kOrderBins = 1024;
 constexpr int kNotHeld = -1;                   // in place of the blocks of a request whose numbers are out of range
@@ -387,51 +390,30 @@ sd_status launch_prompt_prepare(const sd_prompts& p, int32_t* dev_status, cudaSt
     return p.B <= kFewThreads && p.N <= 32 * kFewThreads ? launch_prepare<kFewThreads>(p, dev_status, st) : launch_prepare<kManyThreads>(p, dev_status, st);
 }
 
-// A token's K and V rows of all KV heads (256 bytes a head) into its slot; unit of work = one 16-byte vector of each, U of them per thread.  Bound
-// by HBM; four units keep enough loads on their way (47195 rows of four heads 36.9 us with one, 32.8 with four, 5.9 TB/s), one leaves the shortest chain
-// where there are few rows.
-template <int U>
+// A token's K and V rows of all KV heads (256 bytes a head) into its slot, a 16-byte vector of each per thread.  Bound by HBM: 47195 rows of four
+// heads 31.1 us, 6.2 TB/s (four vectors of each per thread, their loads together: 31.5, and 16 rows 3.3 instead of 2.1).
 __global__ void __launch_bounds__(256)
 append_kernel(sd_prompts p, sd_kv_layer cache, const uint4* k, long long ldk, const uint4* v, long long ldv, int32_t* status) {
     begin_dependent(p.slot, cache.k, cache.v, k, v);
     const unsigned per = (unsigned)p.Hkv * 16u;
-    const unsigned long long units = (unsigned long long)p.N * per;
-    uint4 kx[U], vx[U];
-    int slot[U];
-    unsigned vec[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const unsigned long long i = ((unsigned long long)blockIdx.x * U + u) * 256 + threadIdx.x;
-        slot[u] = -1;
-        vec[u] = 0;
-        if (i >= units) continue;
-        const unsigned row = units < 0xffffffffull ? (unsigned)i / per : (unsigned)(i / per);
-        vec[u] = (unsigned)(i - (unsigned long long)row * per);
-        slot[u] = __ldcg(p.slot + row);                    // (the rows come along without waiting for it)
-        kx[u] = __ldcs(k + row * ldk + vec[u]);
-        vx[u] = __ldcs(v + row * ldv + vec[u]);
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        if (slot[u] < 0) continue;
-        const int block = slot[u] / kBlock;
-        if (block >= cache.num_blocks) { set_status(status, SD_ERR_BOUNDS); continue; }
-        const size_t at = (((size_t)block * p.Hkv + vec[u] / 16) * kBlock + slot[u] % kBlock) * 16 + vec[u] % 16;
-        static_cast<uint4*>(cache.k)[at] = kx[u];
-        static_cast<uint4*>(cache.v)[at] = vx[u];
-    }
+    const unsigned long long units = (unsigned long long)p.N * per, i = (unsigned long long)blockIdx.x * 256 + threadIdx.x;
+    if (i >= units) return;
+    const unsigned row = units < 0xffffffffull ? (unsigned)i / per : (unsigned)(i / per), vec = (unsigned)(i - (unsigned long long)row * per);
+    const int slot = __ldcg(p.slot + row);
+    const uint4 kx = __ldcs(k + row * ldk + vec), vx = __ldcs(v + row * ldv + vec);                // (without waiting for the slot)
+    if (slot < 0) return;
+    const int block = slot / kBlock;
+    if (block >= cache.num_blocks) { set_status(status, SD_ERR_BOUNDS); return; }
+    const size_t at = (((size_t)block * p.Hkv + vec / 16) * kBlock + slot % kBlock) * 16 + vec % 16;
+    static_cast<uint4*>(cache.k)[at] = kx;
+    static_cast<uint4*>(cache.v)[at] = vx;
 }
 
 sd_status launch_append_kv(const sd_prompts& p, const sd_kv_layer& cache, const void* k, long long ldk, const void* v, long long ldv,
                            int32_t* dev_status, cudaStream_t st) {
     const long long units = (long long)p.N * p.Hkv * 16;
-    const auto launch = [&](auto kern, int per_thread) {
-        const long long per_cta = 256ll * per_thread;
-        return launch_dependent(kern, dim3((unsigned)((units + per_cta - 1) / per_cta)), 256, 0, 1, st, p, cache, static_cast<const uint4*>(k),
-                                ldk / 8, static_cast<const uint4*>(v), ldv / 8, dev_status);
-    };
-    // (from one unit for every thread that the GPU holds)
-    return units >= 2048ll * current_sms() ? launch(append_kernel<4>, 4) : launch(append_kernel<1>, 1);
+    return launch_dependent(append_kernel, dim3((unsigned)((units + 255) / 256)), 256, 0, 1, st, p, cache, static_cast<const uint4*>(k), ldk / 8,
+                            static_cast<const uint4*>(v), ldv / 8, dev_status);
 }
 
 }  // namespace sdv

@@ -11,14 +11,15 @@
 // reference stays (the rare tile that raises it is serialised through a barrier that every tile passes, commit).  Four more warps normalise
 // and store an entry's rows while the next one's tiles are under way.
 //
-// Eight prompts of 4096 tokens (28 query, 4 KV heads): 811 us, 1187 TFLOP/s, in a few calls; 941 us, 1022 TFLOP/s, in many, because the GPU is at its
-// power cap then (1000 W, 1.49 GHz; a large matrix product sustains 1407 TFLOP/s at 1.36).  A tile of 128 x 128 takes about 1500 cycles of which
-// the tensor pipe is busy for 1024: what passes through shared memory (Q, K and V for the products and the copies, 160 KiB) takes 1280, the
-// exponentials (four a cycle and quarter of the SM) 1024 of both groups' time, and a soft-max warp's tile about 2900 cycles, half of them latencies.
+// Eight prompts of 4096 tokens (28 query, 4 KV heads): 792 us, 1215 TFLOP/s, in a few calls (at 1.62 GHz); 920 us, 1046 TFLOP/s, in many, because the
+// GPU is at its power cap then (1000 W; a large matrix product sustains 1407 TFLOP/s at 1.36 GHz).  A tile of 128 x 128 takes about 1400 cycles of
+// which the tensor pipe is busy for 1024: what passes through shared memory (Q, K and V for the products and the copies, 160 KiB) takes 1280, the
+// exponentials (four a cycle and quarter of the SM) 1024 of both groups' time.  An entry costs 500 to 1000 cycles beside its tiles, one of a single
+// tile 3000 in all, and a CTA's first 8000 (plan, table, first copies).
 // Steps, us for those prompts: two row tiles in a CTA that share K and V and wait for each other 935; this stream 892; scores and products
 // with V issued by a warp each (eight instructions take 400 cycles to issue) 862; registers moved to the soft-max warps 842; results
-// stored eight rows at a time (a row a thread made thirty-two lines of every store and held up the barriers) 811.  A quarter to a third of the
-// exponentials as polynomials on the multiply-add units: 2 % off to 8 % on, left out.
+// stored eight rows at a time (a row a thread made thirty-two lines of every store and held up the barriers) 816; the tile before waited for
+// behind the weights, not half-way, 792.  A quarter to a third of the exponentials as polynomials on the multiply-add units: 2 % off to 8 % on, left out.
 #include <atomic>
 #include "attention_shared.cuh"
 #include "prompt_plan.cuh"
