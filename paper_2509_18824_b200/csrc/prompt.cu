@@ -2,7 +2,9 @@
 //
 // out = softmax(scale q . K^T) V over the keys t <= len + i, a pass over the keys with a row's weights relative to one of its first scores
 // (see kSumLimit: the reference moves only where a tile's weights add up to more than 2^40, so that no maximum is looked for and nothing
-// is rescaled in the usual tile).
+// is rescaled in the usual tile).  Scores, sums and O are in 32 bits.  A weight is rounded to bf16 (half a step, 2^-8) because V is bf16 and both operands
+// of a product have one type; sums are of the weights as they were before.  The output is then 0.0023 of its norm off, 0.0016 with its own rounding alone.
+// (Weights of few rows as the sum of two bf16: 0.0017, and 32 single tokens 93 instead of 88 us, a prompt's piece beside single tokens 141 instead of 112.)
 //
 // A CTA per SM works through its part of the plan (prompt_plan.cuh): entries, a row tile of 128 rows - the query heads of a KV head for 128 / G
 // tokens - against tiles of 128 keys.  The tiles of all its entries are one stream: the scores of tile g + 2 are computed before the product
