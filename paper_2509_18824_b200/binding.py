@@ -639,6 +639,8 @@ class Prompts(_OnAnyStream):
         dev, made = torch.device(device), []
 
         def to(a):
+            if isinstance(a, torch.Tensor) and a.is_cuda and a.dtype is torch.int32 and not a.is_contiguous():
+                raise AssertionError("int32 tensors on the device are taken as they are and have to be contiguous")
             got = torch.as_tensor(a, dtype=torch.int32).contiguous().to(dev)
             if got is not a:
                 made.append(got)
@@ -646,7 +648,9 @@ class Prompts(_OnAnyStream):
         self.N, self.Hq, self.Hkv, self.D = int(N), int(Hq), int(Hkv), int(D)
         self.len, self.n_new = to(lens), to(n_new)
         self.B = int(self.len.numel())
-        self.block_table = to(block_table).reshape(self.B, -1)
+        self.block_table = to(block_table)
+        if self.block_table.dim() != 2 or self.block_table.shape[0] != self.B:
+            raise AssertionError(f"block_table: expected [{self.B}, max_blocks], got {tuple(self.block_table.shape)}")
         self.n_blocks = None if n_blocks is None else to(n_blocks)
         self.max_blocks, self.num_blocks = int(self.block_table.shape[1]), int(num_blocks)
         for t in (self.len, self.n_new, self.n_blocks):

@@ -365,3 +365,13 @@ def test_a_prefix_that_requests_share():
     r.append()
     r.attend()
     r.check()
+
+
+def test_tables_that_would_be_taken_wrongly_are_refused():
+    make = lambda table, lens=(1, 2): sd.Prompts(3, 4, 2, 128, table, list(lens), [1, 2], num_blocks=8)
+    wide = torch.zeros((2, 6), dtype=torch.int32, device="cuda")
+    for bad in (wide[:, :4], wide.reshape(4, 3), wide.reshape(12)):          # a copy would not follow; four sequences; no rows
+        with pytest.raises(AssertionError):
+            make(bad)
+    assert make(wide).block_table is wide
+    assert make(wide[:, :4].long()).max_blocks == 4                          # (another type: copied in any case)
