@@ -11,8 +11,8 @@ using namespace sm100;
 
 namespace {
 // Threads of a CTA: a pass of the scans is shorter with few, and with many there are fewer passes.  Us, 256 threads and 1024 (blocks: in a cluster
-// of eight), blocks / slots and plan: 64 requests of 60 new tokens 3.4 and 4.2 / 6.4 and 7.2, 256 of one 3.6 and 4.4 / 6.8 and 7.5, 256 of 60 (15360 rows) 3.8
-// and 4.6 / 7.5 and 7.0, 400 of 30 4.5 and 4.5 / 8.7 and 7.3, 2000 of 50 15.5 and 6.7 / 39 and 19.
+// of eight), blocks / slots and plan: 64 requests of 60 new tokens 3.4 and 4.2 / 6.1 and 7.4, 256 of one 3.6 and 4.5 / 6.4 and 7.7, 256 of 60 (15360 rows) 3.8
+// and 4.7 / 7.8 and 6.8, 400 of 30 4.5 and 4.5 / 8.7 and 6.5, 2000 of 50 15.4 and 6.7 / 39 and 16.5.
 constexpr int kFewThreads = 256, kManyThreads = 1024;
 constexpr int kOrderBins = 1024;
 constexpr int kNotHeld = -1;                   // in place of the blocks of a request whose numbers are out of range
@@ -64,6 +64,29 @@ __device__ __forceinline__ int last_at_most(const int* a, int n, int x) {
         if (a[m] <= x) lo = m; else hi = m;
     }
     return lo;
+}
+// The same for the 32 lanes of a warp, whose x follow one another: thirty-two numbers are looked at together.  (A search per lane is eleven steps for 2000
+// numbers, each with bank conflicts: searching and writing 6000 row tiles of 2000 requests took 15200 cycles, 13200 so.)
+__device__ __forceinline__ int last_at_most_warp(const int* a, int n, int x) {
+    const int lane = threadIdx.x & 31, x0 = x - lane;
+    int lo = 0;
+    for (int left = n; left > 1;) {                        // of lane 0
+        const int step = (left + 31) / 32, at = lane * step;
+        const int k = __popc(__ballot_sync(0xffffffffu, at < left && a[lo + min(at, left - 1)] <= x0)) - 1;    // (a[lo] is at most x0)
+        lo += k * step;
+        left = min(step, left - k * step);
+    }
+    int mine = lo;
+    for (int base = lo + 1;; base += 32) {                 // and how many of those behind it each lane passes
+        const int next = base + lane < n ? a[base + lane] : 0x7fffffff;
+        int c = 0;
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1)
+            if (__shfl_sync(0xffffffffu, next, c + d - 1) <= x) c += d;
+        if (__shfl_sync(0xffffffffu, next, c) <= x) ++c;
+        mine += c;
+        if (!__any_sync(0xffffffffu, c == 32)) return mine;
+    }
 }
 }  // namespace
 
@@ -242,9 +265,9 @@ prompt_prepare_kernel(sd_prompts p, PromptGeom geom, int rows, int32_t* status) 
     PromptEntry* const list = plan_entries(p.plan, geom.sms);
     PromptStart* const starts = plan_starts(p.plan);
     PromptSplit* const splits = plan_splits(p.plan, geom.sms);
-    const auto entry = [&](int e) {
+    const auto entry_of = [&](int b, int e) {
         PromptEntry x;
-        x.b = last_at_most(first_entry, B, e);
+        x.b = b;
         const int len = len_of[x.b], n = start[x.b + 1] - start[x.b], t0 = (e - first_entry[x.b]) * geom.tokens;
         x.row0 = start[x.b] + t0;
         x.pos0 = len + t0;
@@ -254,46 +277,50 @@ prompt_prepare_kernel(sd_prompts p, PromptGeom geom, int rows, int32_t* status) 
         x.unused0 = x.unused1 = 0;
         return x;
     };
-    // All entries are made once; the first kHeld lengths of a thread stay in registers, so that what follows, on one SM, is short.
+    const auto entry = [&](int e) { return entry_of(last_at_most(first_entry, B, e), e); };
+    // All entries are made once; the first lengths of each thread stay in shared memory.  (In registers the loops below have to be written out, and one
+    // CTA's cold code is slower than its loads: a request 6.3 us, 5.7 so; 2000 of 50 tokens 15.2, 16.5 so.)
     constexpr int kHeld = 8;
-    int held[kHeld];
+    __shared__ int held[kHeld * THREADS];
     const auto for_own = [&](auto&& use) {     // use(e, key tiles): for all threads together, -1 where there is no entry
-#pragma unroll
-        for (int i = 0; i < kHeld; ++i)
-            if (i * THREADS < entries) use(i * THREADS + (int)threadIdx.x, held[i]);
-        for (int e0 = kHeld * THREADS; e0 < entries; e0 += THREADS) {
+#pragma unroll 1
+        for (int e0 = 0; e0 < entries; e0 += THREADS) {
             const int e = e0 + (int)threadIdx.x;
-            use(e, e < entries ? (list[e].blocks + 1) / 2 : -1);
+            use(e, e >= entries ? -1 : e < kHeld * THREADS ? held[e] : (list[e].blocks + 1) / 2);
         }
     };
     long long cost[1] = {0}, all_cost[1];
     int longest = 0;
-    const auto make = [&](int e) {
+    const auto make = [&](int e) {             // (whole warps)
+        if (e - (int)(threadIdx.x & 31) >= entries) return -1;
+        const int b = last_at_most_warp(first_entry, B, e);
         if (e >= entries) return -1;
-        const PromptEntry x = entry(e);
+        const PromptEntry x = entry_of(b, e);
         list[e] = x;
         const int tiles = (x.blocks + 1) / 2;
         longest = max(longest, tiles);
         cost[0] += tiles + kEntryTiles;
         return tiles;
     };
-#pragma unroll
-    for (int i = 0; i < kHeld; ++i) held[i] = make(i * THREADS + (int)threadIdx.x);
-    for (int e = kHeld * THREADS + (int)threadIdx.x; e < entries; e += THREADS) make(e);
+#pragma unroll 1
+    for (int e0 = 0; e0 < entries; e0 += THREADS) {
+        const int e = e0 + (int)threadIdx.x, tiles = make(e);
+        if (e < kHeld * THREADS) held[e] = tiles;
+    }
     longest = __reduce_max_sync(0xffffffffu, longest);
     if ((threadIdx.x & 31) == 0 && longest) atomicMax(&longest_smem, longest);
     buf = 0;
     block_scan<THREADS>(cost, all_cost, line_sums, buf);       // (its barrier is behind the atomics)
     const long long line = all_cost[0] * Hkv, part = max((line + geom.sms - 1) / geom.sms, (long long)kPartMin);
     if (part >= (long long)kDealFrom * (longest_smem + kEntryTiles)) {
-        // ---------------------------------------- dealt out: sorted by counting.  (Lanes with the same length count as one.)
+        // ---------------------------------------- dealt out: sorted by counting.  (A warp of one length counts as one.)
         const auto put = [&](int tiles) {                                      // the place that each lane's entry gets in its bin
-            const int bin = kOrderBins - 1 - min(tiles, kOrderBins - 1);
-            const unsigned same = __match_any_sync(0xffffffffu, tiles < 0 ? -1 : bin), lane = threadIdx.x & 31;
-            const int leader = __ffs(same) - 1;
-            int first = 0;
-            if (tiles >= 0 && (int)lane == leader) first = atomicAdd(&bins[bin], __popc(same));
-            return __shfl_sync(0xffffffffu, first, leader) + __popc(same & ((1u << lane) - 1u));
+            const int bin = tiles < 0 ? -1 : kOrderBins - 1 - min(tiles, kOrderBins - 1), lane = threadIdx.x & 31;
+            int alike = 0, first = 0;
+            __match_all_sync(0xffffffffu, bin, &alike);
+            if (!alike) return bin < 0 ? 0 : atomicAdd(&bins[bin], 1);
+            if (lane == 0 && bin >= 0) first = atomicAdd(&bins[bin], 32);
+            return __shfl_sync(0xffffffffu, first, 0) + lane;
         };
         for_own([&](int, int tiles) { put(tiles); });
         __syncthreads();
