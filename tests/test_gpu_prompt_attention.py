@@ -375,3 +375,33 @@ def test_tables_that_would_be_taken_wrongly_are_refused():
             make(bad)
     assert make(wide).block_table is wide
     assert make(wide[:, :4].long()).max_blocks == 4                          # (another type: copied in any case)
+
+
+@pytest.mark.parametrize("heads", [(64, 64), (128, 64), (4, 2)], ids=str)
+def test_spikes_and_plateaus(heads):
+    """Single keys that tower over all others, and stretches just below them: weights that were relative to the reference before the spike, in the tile
+    behind it and in the other half of its own, are brought to the one after it.  (So many heads that a CTA has whole entries; few, and they are cut.)"""
+    g = np.random.default_rng(21)
+    r = Requests([(20, 900), (3, 700), (1, 1200), (129, 500), (20, 640), (64, 300), (20, 128), (1, 2000), (33, 1000), (20, 1100)], *heads, seed=21)
+    r.prepare()
+    r.append()
+    r.q[:r.rows] = 1.0
+    for b, (n, c) in enumerate(r.lens):
+        level = g.normal(0.0, 1.0, n + c)                                       # in powers of two
+        for t0 in range(0, n + c, 64):
+            stretch = slice(t0, min(t0 + 64, n + c))
+            level[stretch] += g.choice([0.0, 0.0, 20.0, 31.0])
+            if g.random() < 0.4:
+                level[g.integers(t0, min(t0 + 64, n + c))] = g.choice([35.0, 45.0, 80.0, 120.0]) + 3.0 * b
+        values = torch.from_numpy((level * np.log(2.0) * np.sqrt(128.0) / 128.0).astype(np.float32)).to(torch.bfloat16).cuda()
+        t = torch.arange(n + c, device="cuda")
+        block = torch.from_numpy(r.table[b]).cuda().long()[t // 64]
+        r.k_cache[block, :, t % 64] = values[:, None, None].expand(-1, heads[1], 128)
+    r.attend()
+    torch.cuda.synchronize()
+    assert int(r.status.item()) == 0
+    out, lse, spread, size = r.expect()
+    got = r.out[:r.rows].double().cpu().numpy()
+    slack = 2.0 ** -17 * size[..., None] * 2.0
+    assert (np.abs(got - out) <= (2.0 ** -8 + 2.0 ** -10 + slack) * spread + (2.0 ** -8 + slack) * np.abs(out)).all()
+    assert (np.abs(r.lse[:r.rows].double().cpu().numpy() - lse) <= 2.0 ** -17 * size + 2.0 ** -22 * np.abs(lse) + 2.0 ** -14).all()

@@ -151,3 +151,21 @@ def test_a_step_on_another_stream():
     p.layer(0, qkv[:, :28], qkv[:, 28:32], qkv[:, 32:], here)
     torch.cuda.synchronize()
     assert torch.equal(out.view(torch.int16), here.view(torch.int16)) and out.any()
+
+
+def test_without_a_pool_the_tables_are_the_callers():
+    w = wl.make("c5", B=2, L=1, V=1024, Hd=128, prefix=200, T=8)
+    vs = VerifyStep(w)
+    vs.batch.len.zero_()
+    before = vs.batch.block_table.clone()
+    p = vs.prompts(90, [60, 30])
+    qkv = torch.randn((90, 36, 128), device="cuda").to(torch.bfloat16)
+    out = torch.zeros((90, 28, 128), dtype=torch.bfloat16, device="cuda")
+    p.begin()
+    p.layer(0, qkv[:, :28], qkv[:, 28:32], qkv[:, 32:], out)
+    p.end()
+    torch.cuda.synchronize()
+    vs.check_status()
+    assert vs.batch.len.tolist() == [60, 30] and torch.equal(before, vs.batch.block_table) and out.any(dim=2).all()
+    with pytest.raises(AssertionError):
+        p.reserve_trees()
