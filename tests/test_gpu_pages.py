@@ -248,3 +248,37 @@ def test_parts_are_equal_however_long(B, Hkv, tokens):
     at = before[e] + h * np.append(one, 0)[e] + np.where(tile > 0, tile + 2, 0)
     want = np.minimum(np.arange(sms + 1) * part, line)
     assert np.abs(at - want).max() <= 6 and (np.diff(at) > 0).all()
+
+
+@pytest.mark.parametrize("B, new, heads", [(200, 2000, (8, 1)), (300, 40, (28, 4)), (2000, 50, (28, 4)), (8, 4096, (28, 4)), (700, 1, (64, 64))], ids=str)
+def test_entries_that_are_dealt_out_stand_in_order(B, new, heads):
+    """Every row tile once, the longest first, and each CTA's first piece in its start."""
+    g = np.random.default_rng(B)
+    lens, n = g.integers(0, 3000, B), g.integers(0, new + 1, B)
+    n[0] = new
+    W, N = blocks(3000 + new), int(n.sum())
+    q = sd.Prompts(N, *heads, 128, torch.zeros((B, W), dtype=torch.int32, device="cuda"), lens, n, num_blocks=1)
+    st = sd.new_status()
+    sd.sd_prompt_prepare(q, st)
+    torch.cuda.synchronize()
+    assert int(st.item()) == 0
+    tokens = 128 // (heads[0] // heads[1])
+    row0 = np.concatenate([[0], np.cumsum(n)])
+    want = [(row0[b] + i, lens[b] + i, min(tokens, n[b] - i), b, blocks(int(lens[b] + min(i + tokens, n[b]))), lens[b] + n[b])
+            for b in range(B) for i in range(0, int(n[b]), tokens)]
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    raw = q.plan.cpu().numpy()
+    words = lambda at, count: raw[at:at + 4 * count].view(np.int32)
+    entries = int(words(0, 4)[1])
+    assert entries == len(want)
+    starts, at = words(16, 12 * (sms + 1)).reshape(-1, 12), 16 + 48 * (sms + 1) + 32 * sms
+    cap = N // tokens + min(B, N) + 1
+    got = words(at, 8 * entries).reshape(-1, 8)[:, :6]
+    np.testing.assert_array_equal(got, np.array(want))
+    order = words(at + 32 * cap, entries)
+    assert np.array_equal(np.sort(order), np.arange(entries))
+    tiles = (got[:, 4] + 1) // 2
+    assert (np.diff(tiles[order]) <= 0).all()
+    for c in range(min(sms, entries * heads[1])):
+        assert tuple(starts[c, :2]) == (c, c % heads[1])
+        np.testing.assert_array_equal(starts[c, 4:10], got[order[c // heads[1]]])
