@@ -84,7 +84,9 @@ typedef struct {
     int32_t max_blocks_per_seq;  /* row stride of block_table                        */
     const int32_t *block_table;  /* dev [B][max_blocks_per_seq]; covers len+n_nodes  */
     const int32_t *len;          /* dev [B] cached prefix length of each sequence    */
-    const int32_t *n_nodes;      /* dev [B] nodes in each tree, 1..T_max             */
+    const int32_t *n_nodes;      /* dev [B] nodes in each tree, 1..T_max.  0, or minus the nodes of a tree that waits (down to -T_max): the
+                                    sequence takes no part in the step.  Its n_acc is 0, its new_len = len, its path and out_tok
+                                    -1, its rows of the attention's outputs zero; no cache is written for it, and nothing reported */
     const int32_t *parents;      /* dev [B][T_max]                                   */
     uint64_t *anc_mask;          /* dev [B][T_max]; bit j of [b][i] set iff node j is
                                     i itself or an ancestor of i (sd_tree_prepare)   */
@@ -148,8 +150,9 @@ size_t sd_workspace_bytes(const sd_batch *geom, int32_t M, int32_t V);
 /*
  * Ancestor masks of the draft trees (Sec. 1: the speculative tokens are
  * validated together; a node may attend only to its own root path).
- * Validates parents (root -1, parent < child, n_nodes in 1..T_max) and fills
- * batch->anc_mask.  A bad tree stores SD_ERR_INVALID_TREE into *dev_status.
+ * Validates parents (root -1, parent < child, n_nodes in -T_max..T_max) and fills
+ * batch->anc_mask, for trees that wait (n_nodes < 0) too.  A bad tree stores
+ * SD_ERR_INVALID_TREE into *dev_status.
  */
 sd_status sd_tree_prepare(const sd_batch *batch, int32_t *dev_status, void *stream);
 
@@ -617,7 +620,9 @@ sd_status sd_distill_grad(const void *logits, int32_t dtype, int64_t ld, int32_t
  *   block_table : dev [B][max_blocks_per_seq], entries beyond n_blocks may hold anything; they are left as they are
  *   n_blocks    : dev [B], in and out
  *   len, n_new  : dev [B] (an sd_batch's len and n_nodes for the trees of a step; both 0 for a request that is done)
- *   granted     : dev [B] or NULL: 1, or 0 for requests that got none or whose numbers are out of range
+ *   granted     : dev [B] or NULL: 1, or 0 for requests that got none or whose numbers are out of range.  What such a request's table names
+ *                 behind n_blocks may be another one's by now: where n_new are the nodes of a step's trees, its n_nodes has to be made
+ *                 0 or negative before the step (see sd_batch)
  * A block is one request's or the stack's: tables that share blocks are not for this call.
  * 1 <= B <= 8192, B * max_blocks_per_seq < 2^29.  A negative length stores SD_ERR_INVALID_ARG; more tokens than the table's row holds, or n_blocks or *n_free out of
  * range, SD_ERR_BOUNDS: that request keeps what it has (with *n_free out of range the stack counts as empty).  A block outside [0, num_blocks)

@@ -154,7 +154,7 @@ child_prob_kernel(sd_batch bt, const uint16_t* __restrict__ hidden, const uint16
 // The rejection walk of one sequence, by one warp.  Results go where `o` points (global or shared
 // memory): the accepted path and the drafted tokens along it (entries beyond: -1; the slot of the
 // token still to be drawn: -1), the drafted tokens of the stop node's children and their
-// probabilities.  Returns, in every lane: accepted nodes (0: bad tree, reported, nothing written), the
+// probabilities.  Returns, in every lane: accepted nodes (0: bad tree, reported, or one that waits; nothing written), the
 // stop node, the number of its children, the residual mass left there.
 struct WalkOut { int32_t* path; int32_t* out_tok; int32_t* excl; float* excl_p; };
 struct WalkEnd { int na, stop, n_excl; float R; };
@@ -162,6 +162,7 @@ struct WalkEnd { int na, stop, n_excl; float R; };
 // n nodes of at most T; par, dt, p_child, u: the sequence's own (global or shared memory).
 __device__ __forceinline__ WalkEnd sampled_walk(int n, int T, int lane, const int32_t* par, const int32_t* dt, const float* p_child,
                                                 const float* u, const WalkOut& o, int32_t* status) {
+    if (sits_out(n, T)) return WalkEnd{0, 0, 0, 0.f};
     bool bad = (n < 1 || n > T);
     if (!bad)
         for (int i = lane; i < n; i += 32) {
@@ -231,6 +232,7 @@ __global__ void sampled_walk_kernel(sd_batch bt, const int32_t* __restrict__ dra
         resid[b] = e.R;
         if (e.na > 0) new_len[b] = bt.len[b] + e.na;
     }
+    if (sits_out(bt.n_nodes[b], T)) leave_out(T, b, lane, 32, bt.len[b], n_acc, path, out_tok, new_len);
 }
 
 // hidden rows (and their lse) of the stop nodes, gathered into a dense [B][Hd] matrix for the LM-head kernel
@@ -306,7 +308,7 @@ residual_pick_kernel(sd_batch bt, int V, const float* __restrict__ w, const floa
     begin_dependent(bt, w, mass, block_sum, n_acc);
     const int b = blockIdx.x;
     const int na = n_acc[b];
-    if (na < 1 || na > bt.T_max) return;                               // bad tree: already reported
+    if (na < 1 || na > bt.T_max) return;                               // bad tree: already reported; or one that waits
     const int lane = threadIdx.x & 31;
     const float* bs = block_sum + (size_t)b * n_blocks;
     for (int k = threadIdx.x; k < n_blocks; k += blockDim.x) s_bs[k] = bs[k];
@@ -538,7 +540,7 @@ residual_pick_groups_kernel(sd_batch bt, const uint16_t* __restrict__ hidden, co
     begin_dependent(bt, hidden, W, lse, group_stats, w, stop_row, n_excl, excl, excl_p, n_acc);
     const int b = blockIdx.x;
     const int na = n_acc[b];
-    if (na < 1 || na > bt.T_max) return;                               // bad tree: already reported
+    if (na < 1 || na > bt.T_max) return;                               // bad tree: already reported; or one that waits
     const int row = stop_row[b];
     residual_pick_groups<1>(hidden, W, Hd, V, inv_temp, lse[row], bt.B * bt.T_max, row, group_stats, n_groups, w[b], n_excl[b],
                             excl + (size_t)b * 64, excl_p + (size_t)b * 64, out_tok + (size_t)b * bt.T_max + na - 1, status, [] {});
@@ -568,8 +570,10 @@ __global__ void chain_walk_q_kernel(sd_batch bt, const int32_t* __restrict__ dra
     bad = __any_sync(0xffffffffu, bad);
     branching = __any_sync(0xffffffffu, branching);
     if (bad || branching) {
+        const bool waits = sits_out(n, T);
+        if (waits) leave_out(T, b, lane, 32, bt.len[b], n_acc, path, out_tok, new_len);
         if (lane == 0) {
-            set_status(status, bad ? SD_ERR_INVALID_TREE : SD_ERR_UNSUPPORTED);
+            if (!waits) set_status(status, bad ? SD_ERR_INVALID_TREE : SD_ERR_UNSUPPORTED);
             n_acc[b] = 0; stop_row[b] = b * T; rejected[b] = 0;
         }
         return;
@@ -729,6 +733,8 @@ sampled_tail_kernel(sd_batch bt, const __grid_constant__ CompactLayers ly, int L
         residual_pick_groups<kTailCluster>(hidden, W, Hd, V, inv_temp, s_lse[e.stop], bt.B * T, row, group_stats, n_groups, w[b],
                                            e.n_excl, s_excl, s_excl_p, out_tok + (size_t)b * T + e.na - 1, status,
                                            [&] { copy_layers(4); });
+    } else if (rank == 0 && sits_out(n, T)) {
+        leave_out(T, b, threadIdx.x, blockDim.x, bt.len[b], n_acc, path, out_tok, new_len);
     }
     if (rank != 0) copy_layers(L);
 }

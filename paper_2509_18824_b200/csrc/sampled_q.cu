@@ -238,7 +238,8 @@ tree_walk_q_kernel(sd_batch bt, int V, float inv_temp, const float* lse, const f
     __syncthreads();
     const int bad = n_ok ? sh.bad : (int)SD_ERR_INVALID_TREE;
     if (bad != 0) {                                    // (the same in every CTA)
-        if (rank == 0 && tid == 0) { set_status(status, bad); n_acc[b] = 0; }
+        if (rank == 0 && sits_out(n, T)) leave_out(T, b, tid, kQThreads, bt.len[b], n_acc, path, out_tok, new_len);
+        else if (rank == 0 && tid == 0) { set_status(status, bad); n_acc[b] = 0; }
         q_end(sh);
         return;
     }
@@ -340,7 +341,8 @@ chain_walk_q_logits_kernel(sd_batch bt, int V, float inv_temp, const float* lse,
     __syncthreads();
     const int bad = n_ok ? sh.bad : (int)SD_ERR_INVALID_TREE;
     if (bad != 0) {                                    // (the same in every CTA)
-        if (rank == 0 && tid == 0) { set_status(status, bad); n_acc[b] = 0; }
+        if (rank == 0 && sits_out(n, T)) leave_out(T, b, tid, kQThreads, bt.len[b], n_acc, path, out_tok, new_len);
+        else if (rank == 0 && tid == 0) { set_status(status, bad); n_acc[b] = 0; }
         q_end(sh);
         return;
     }

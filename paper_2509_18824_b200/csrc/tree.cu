@@ -10,10 +10,10 @@ __global__ void tree_prepare_kernel(sd_batch bt, int32_t* status) {
     const int b = blockIdx.x;
     const int lane = threadIdx.x;
     const int T = bt.T_max;
-    const int n = bt.n_nodes[b];
+    const int n = sits_out(bt.n_nodes[b], T) ? -bt.n_nodes[b] : bt.n_nodes[b];     // (of a tree that waits too)
     const int32_t* par = bt.parents + (size_t)b * T;
     uint64_t* am = bt.anc_mask + (size_t)b * T;
-    if (n < 1 || n > T) {
+    if (n < 0 || n > T) {
         if (lane == 0) set_status(status, SD_ERR_INVALID_TREE);
         return;
     }

@@ -195,15 +195,31 @@ __device__ __forceinline__ int warp_find_crossing(const float* v, int n, float t
     }
 }
 
+// A sequence without a tree, or whose tree of -n nodes waits, takes no part in the step.
+__device__ __forceinline__ bool sits_out(int n, int T) { return n <= 0 && n >= -T; }
+// ... and what the acceptance calls leave of it.
+__device__ __forceinline__ void leave_out(int T, int b, int tid, int threads, int len, int32_t* n_acc, int32_t* path, int32_t* out_tok,
+                                          int32_t* new_len) {
+    for (int k = tid; k < T; k += threads) path[(size_t)b * T + k] = out_tok[(size_t)b * T + k] = -1;
+    if (tid == 0) {
+        n_acc[b] = 0;
+        new_len[b] = len;
+    }
+}
+
 // Greedy acceptance for one sequence of n nodes and len cached tokens, executed by one warp.  par/dt/tg: the
 // sequence's parents, draft tokens and target arg-max, in global or shared memory (in the tail kernel, where they can be
 // brought there meanwhile, 2.9 -> 2.4 us; the stand-alone kernel, which would wait for them, takes 3.6 instead of 4.0 without).  Returns the number of
-// accepted nodes (0 for a bad tree, which is reported through *status) and, in lane 0, has written
+// accepted nodes (0 for a bad tree, which is reported through *status, and for one that waits) and, in lane 0, has written
 // n_acc, new_len, path and out_tok; `path_out` (nullable, e.g. shared memory) receives the path too.
 __device__ __forceinline__ int accept_sequence(int T, int b, int lane, int n, int len, const int32_t* par,
                                                const int32_t* dt, const int32_t* tg,
                                                int32_t* n_acc, int32_t* path, int32_t* out_tok, int32_t* new_len,
                                                int32_t* path_out, int32_t* status) {
+    if (sits_out(n, T)) {
+        leave_out(T, b, lane, 32, len, n_acc, path, out_tok, new_len);
+        return 0;
+    }
     bool bad = (n < 1 || n > T);
     if (!bad)
         for (int i = lane; i < n; i += 32) {

@@ -67,6 +67,10 @@ class VerifyStep:
         self.path = torch.zeros((B, T), dtype=torch.int32, device=d)
         self.out_tok = torch.zeros((B, T), dtype=torch.int32, device=d)
         self.new_len = torch.zeros(B, dtype=torch.int32, device=d)
+        # tables that follow a pool of blocks (PromptStep): the pool, the counts that it is kept for, what is asked of it for the
+        # trees, and whom it suffices for
+        self._pool = None
+        self._asked, self.trees_granted = (torch.ones(B, dtype=torch.int32, device=d) for _ in range(2))
         nbytes = sd.sd_workspace_bytes(self.batch, M if self.W is not None else 0, w.V if self.W is not None else 0)
         self.workspace = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=d)
         self.caches = [sd.kv_layer(k, v) for k, v in zip(self.k_cache, self.v_cache)]
@@ -291,6 +295,8 @@ class VerifyStep:
             ev_last.record(cs)
         main.wait_event(self._ev_small[slot])
         sd.sd_tree_prepare(self.batch, self.status)
+        if self._pool is not None:
+            self._reserve_trees()       # (the trees' sizes have come just now)
         for l0 in range(0, self.L, group):
             l1 = min(l0 + group, self.L)
             main.wait_event(self._ev_layer[slot][l1 - 1])
@@ -313,6 +319,18 @@ class VerifyStep:
         """What brings prompts (or the next pieces of them) into this step's caches, see PromptStep."""
         return PromptStep(self, N, n_new, pool, n_blocks)
 
+    def _reserve_trees(self, stream=None):
+        """Tables that cover len + n_nodes.  A sequence that the pool does not suffice for gets minus its n_nodes, so that it takes no
+        part in the step: its table may name blocks that are another one's by now."""
+        b, (pool, n_blocks) = self.batch, self._pool
+        with contextlib.nullcontext() if stream is None else torch.cuda.stream(sd.stream_of(stream)):
+            torch.abs(b.n_nodes, out=self._asked)
+            sd.sd_assign_blocks(pool, b.block_table, n_blocks, b.len, self._asked, self.trees_granted, self.status, stream)
+            torch.neg(self._asked, out=b.n_nodes)
+            b.n_nodes.addcmul_(self._asked, self.trees_granted, value=2)
+            if self._copy_stream is not None and not torch.cuda.is_current_stream_capturing():
+                self._copy_stream.wait_stream(torch.cuda.current_stream())     # (it brings the next trees into the same array)
+
     def check_status(self):
         code = int(self.status.item())
         if code != 0:
@@ -329,6 +347,8 @@ class PromptStep:
     def __init__(self, step: VerifyStep, N: int, n_new, pool: Optional["sd.BlockPool"] = None, n_blocks: Optional[torch.Tensor] = None):
         assert (pool is None) == (n_blocks is None), "a pool of blocks goes with the counts that it is kept for"
         self.step, self.pool = step, pool
+        if pool is not None:
+            step._pool = pool, n_blocks
         b, w = step.batch, step.w
         self.prompts = sd.Prompts(N, b.Hq, b.Hkv, b.D, b.block_table, b.len, n_new, n_blocks, num_blocks=int(step.k_cache[0].shape[0]),
                                   device=step.device)
@@ -354,7 +374,8 @@ class PromptStep:
             self.prompts.len.addcmul_(self.prompts.n_new, self.granted)
 
     def reserve_trees(self, stream=None):
-        """Blocks for the trees of the next verification (or what behind it is not needed, given back): tables that cover len + n_nodes."""
+        """Blocks for the trees of the next verification (or what behind it is not needed, given back): tables that cover len + n_nodes.
+        A sequence that the pool does not suffice for (the step's trees_granted 0) keeps what it has and waits: its n_nodes becomes negative, and
+        the step leaves it out (n_acc 0) until a later call finds blocks for it.  run_from_host() does this by itself, once its trees are there."""
         assert self.pool is not None, "the tables are the caller's: there is no pool to take blocks from"
-        p, b = self.prompts, self.step.batch
-        sd.sd_assign_blocks(self.pool, p.block_table, p.n_blocks, b.len, b.n_nodes, self.granted, self.step.status, stream)
+        self.step._reserve_trees(stream)
