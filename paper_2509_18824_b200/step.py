@@ -98,9 +98,10 @@ class VerifyStep:
                 out_tok=torch.zeros((B, T), dtype=torch.int32).pin_memory(),
                 new_len=torch.zeros(B, dtype=torch.int32).pin_memory())
             # The end-to-end path double-buffers the per-step inputs on the device, so that the next
-            # step's copies run while this step still computes.  Slot 0 is the set built above.
+            # step's copies run while this step still computes.  Slot 0 is the set built above.  Tables and lengths are
+            # the caches' and exist once: whatever changes them holds for every step.
             self._slots = [self._slot_state()]
-            self.batch = sd.Batch.of(w, device=d)
+            self.batch = sd.Batch(w.B, w.T_max, w.Hq, w.Hkv, w.D, self.batch.block_table, self.batch.len, w.n_nodes, w.parents, device=d)
             self._in_dev = torch.empty_like(self._in_dev)
             self.q, self.k_tree, self.v_tree = self._layer_views(self._in_dev, w)
             self.hidden, self.draft_tok = torch.empty_like(self.hidden), torch.empty_like(self.draft_tok)

@@ -1,0 +1,82 @@
+"""GPU: prompts brought into a verify step's caches in the ways that a serving program calls them: input sets that alternate, streams that
+are not the constructor's, objects dropped early, pieces that do not fit."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2509_18824_b200 import binding as sd
+from paper_2509_18824_b200.step import VerifyStep
+from test_gpu_prompt_waiting import T, agreeable, bf, expected, fill, same, short_of_blocks, workload
+
+pytestmark = pytest.mark.gpu
+
+
+def host_step(B, **over):
+    vs = VerifyStep(workload(B, **over), keep_host_inputs=True)
+    tok = agreeable(vs)
+    vs.host["draft_tok"].copy_(tok)
+    torch.cuda.synchronize()
+    return vs
+
+
+def test_prompts_and_steps_from_the_host():
+    """The step's inputs exist twice; its tables and lengths once."""
+    vs = host_step(2)
+    pool, held = sd.BlockPool(8), torch.zeros(2, dtype=torch.int32, device="cuda")
+    vs.batch.len.zero_()
+    p = vs.prompts(173, [130, 43], pool, held)
+    fill(vs, p, 3)
+    lens = [130, 43]
+    for step in range(4):
+        torch.cuda.synchronize()
+        before = [c.clone() for c in vs.k_cache + vs.v_cache]
+        if step == 3:                                        # another piece in between
+            more = vs.prompts(30, [0, 30], pool, held)
+            fill(vs, more, 4)
+            lens[1] += 30
+            torch.cuda.synchronize()
+            before = [c.clone() for c in vs.k_cache + vs.v_cache]
+        vs.run_from_host()
+        torch.cuda.synchronize()
+        vs.check_status()
+        assert vs.host_out["n_acc"].tolist() == [T, T] and vs.host_out["new_len"].tolist() == [n + T for n in lens], step
+        assert held.tolist() == [-(-(n + T) // 64) for n in lens]
+        want = expected(vs, expected(vs, before, 0, lens[0]), 1, lens[1])
+        assert same(vs.k_cache + vs.v_cache, want), step
+        vs.batch.len.copy_(vs.new_len)
+        lens = [n + T for n in lens]
+    table = vs.batch.block_table.cpu().numpy()
+    owned = np.concatenate([table[b, :int(held[b])] for b in range(2)])
+    assert np.unique(owned).size == owned.size
+
+
+def test_steps_from_the_host_let_sequences_wait():
+    vs = host_step(2)
+    p, held = short_of_blocks(vs)
+    for _ in range(3):
+        torch.cuda.synchronize()
+        at = int(vs.batch.len[1])
+        before = [c.clone() for c in vs.k_cache + vs.v_cache]
+        vs.run_from_host()
+        torch.cuda.synchronize()
+        vs.check_status()
+        assert vs.host_out["n_acc"].tolist() == [0, T] and vs.host_out["new_len"].tolist() == [60, at + T]
+        assert same(vs.k_cache + vs.v_cache, expected(vs, before, 1, at))
+        vs.batch.len.copy_(vs.new_len)
+    assert held.tolist() == [1, 2]
+
+
+def test_tables_and_lengths_exist_once():
+    vs = host_step(2)
+    a, b = (s["batch"] for s in vs._slots)
+    assert a.len is b.len and a.block_table.data_ptr() == b.block_table.data_ptr() and a.c.len == b.c.len and a.c.block_table == b.c.block_table
+    assert a.n_nodes.data_ptr() != b.n_nodes.data_ptr() and a.parents.data_ptr() != b.parents.data_ptr() and a.anc_mask.data_ptr() != b.anc_mask.data_ptr()
+
+
+def test_without_prompts_steps_from_the_host_keep_their_lengths():
+    vs = host_step(2)
+    for _ in range(3):
+        vs.run_from_host()
+    torch.cuda.synchronize()
+    vs.check_status()
+    assert vs.host_out["new_len"].tolist() == [int(n) + T for n in vs.w.len]
