@@ -588,8 +588,8 @@ class _OnAnyStream:
             self._event = torch.cuda.Event()
             self._event.record()
 
-    def on(self, stream) -> int:
-        """The struct's address for a call on `stream` (None: the current one)."""
+    def _ready(self, stream) -> None:
+        """In front of a call on `stream` (None: the current one)."""
         if self._made:
             raw = torch._C._cuda_getCurrentRawStream(_here()) if stream is None else _raw_stream(stream)
             if raw not in self._streams:
@@ -599,6 +599,10 @@ class _OnAnyStream:
                     other.wait_event(self._event)
                 for t in self._made:
                     t.record_stream(other)
+
+    def on(self, stream) -> int:
+        """The struct's address for a call on `stream`."""
+        self._ready(stream)
         return _at(self.c)
 
 

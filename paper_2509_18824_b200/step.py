@@ -338,7 +338,7 @@ class VerifyStep:
             raise sd.SdError(code)
 
 
-class PromptStep:
+class PromptStep(sd._OnAnyStream):
     """New tokens of a VerifyStep's sequences in N packed rows, n_new [B] of each: blocks for them, their K and V in the caches of all
     layers, and their own causal attention.  begin() once, layer() for every layer as its q, k and v exist, end().
 
@@ -355,10 +355,16 @@ class PromptStep:
                                   device=step.device)
         self.granted = torch.ones(b.B, dtype=torch.int32, device=step.device)
         self.workspace = torch.empty(sd.sd_prompt_workspace_bytes(self.prompts), dtype=torch.uint8, device=step.device)
+        self._makes(self.granted, self.workspace)
+
+    def _ready(self, stream):
+        super()._ready(stream)
+        self.prompts._ready(stream)
 
     def begin(self, stream=None):
         """Tables, slots and positions (self.prompts.position: what a decoder rotates q and k by), and the attention's plan."""
         p, status = self.prompts, self.step.status
+        self._ready(stream)
         if self.pool is not None:
             sd.sd_assign_blocks(self.pool, p.block_table, p.n_blocks, p.len, p.n_new, self.granted, status, stream)
         sd.sd_prompt_prepare(p, status, stream)
@@ -366,11 +372,13 @@ class PromptStep:
     def layer(self, l: int, q, k, v, out, lse=None, stream=None):
         """K and V [N, Hkv, 128] of the new tokens into layer l's cache, then their attention: q, out [N, Hq, 128], lse [N, Hq] or None."""
         st = self.step
+        self._ready(stream)
         sd.sd_append_kv(self.prompts, st.caches[l], k, v, st.status, stream)
         sd.sd_prompt_attention(self.prompts, st.caches[l], q, st.scale, out, lse, self.workspace, st.status, stream)
 
     def end(self, stream=None):
         """The new tokens count as cached from here on (of sequences that were not left out)."""
+        self._ready(stream)
         with contextlib.nullcontext() if stream is None else torch.cuda.stream(sd.stream_of(stream)):
             self.prompts.len.addcmul_(self.prompts.n_new, self.granted)
 

@@ -80,3 +80,59 @@ def test_without_prompts_steps_from_the_host_keep_their_lengths():
     torch.cuda.synchronize()
     vs.check_status()
     assert vs.host_out["new_len"].tolist() == [int(n) + T for n in vs.w.len]
+
+
+@pytest.mark.parametrize("given", ["int32", "int64"])
+def test_a_step_made_while_its_stream_is_busy(given):
+    """Everything that the object makes is ready on the stream of its calls."""
+    w = workload(3, L=1)
+    vs = VerifyStep(w)
+    pool, held = sd.BlockPool(3), torch.zeros(3, dtype=torch.int32, device="cuda")       # of 2, 2 and 1 blocks that are needed
+    new = torch.tensor([100, 100, 30], dtype=getattr(torch, given), device="cuda")
+    qkv = torch.randn((230, 36, 128), device="cuda").to(bf)
+    out = torch.full((230, 28, 128), 5.0, dtype=bf, device="cuda")
+    vs.batch.len.zero_()
+    vs.prompts(230, new, pool, held).begin()                 # (loads the kernels; takes blocks that the next begin finds held)
+    torch.cuda.synchronize()
+    assert held.tolist() == [2, 0, 0]
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        vs.batch.len.zero_()
+        out.fill_(5.0)
+        torch.cuda.synchronize()
+        torch.cuda._sleep(50000000)                          # the current stream is busy for some 25 milliseconds
+        p = vs.prompts(230, new, pool, held)
+        p.begin(side)
+        p.layer(0, qkv[:, :28], qkv[:, 28:32], qkv[:, 32:], out, stream=side)
+        p.end(side)
+        torch.cuda.synchronize()
+        vs.check_status()
+        assert p.granted.tolist() == [1, 0, 0] and vs.batch.len.tolist() == [100, 0, 0] and held.tolist() == [2, 0, 0]
+        assert (out[100:] == 5.0).all() and not (out[:100] == 5.0).all(dim=2).any()
+
+
+def test_memory_of_a_step_that_is_dropped_is_not_given_away_while_it_runs():
+    w = workload(2, L=1)
+    vs = VerifyStep(w)
+    vs.batch.len.zero_()
+    pool, held = sd.BlockPool(8), torch.zeros(2, dtype=torch.int32, device="cuda")
+    qkv = torch.randn((90, 36, 128), device="cuda").to(bf)
+    out = torch.zeros((90, 28, 128), dtype=bf, device="cuda")
+    new = torch.tensor([60, 30], dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    p = vs.prompts(90, new, pool, held)
+    taken = {t.data_ptr(): t.numel() * t.element_size() for t in (p.workspace, p.granted)}
+    sizes = list(taken.values())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100000000)
+    p.begin(side)
+    p.layer(0, qkv[:, :28], qkv[:, 28:32], qkv[:, 32:], out, stream=side)
+    p.end(side)
+    del p
+    got = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(6)]
+    assert not side.query()                                  # (it still runs)
+    assert not any(t.data_ptr() in taken for t in got)
+    torch.cuda.synchronize()
+    vs.check_status()
+    assert vs.batch.len.tolist() == [60, 30]
