@@ -449,9 +449,10 @@ sd_status sd_prompt_attention(const sd_prompts* prompts, const sd_kv_layer* cach
     const sd_status s = check_prompts(prompts, true);
     if (s != SD_OK) return s;
     if (!cache || !ok_ptr(cache->k) || !ok_ptr(cache->v) || cache->num_blocks != prompts->num_blocks || !dev_status) return SD_ERR_INVALID_ARG;
-    if (!(scale > 0.f) || !(scale < INFINITY) || !ok_4(lse) || !ok_ptr(workspace)) return SD_ERR_INVALID_ARG;
+    if (!(scale > 0.f) || !(scale < INFINITY) || !ok_4(lse)) return SD_ERR_INVALID_ARG;
+    if (prompts->N == 0) return SD_OK;                     // (which needs no scratch either)
+    if (!ok_ptr(workspace)) return SD_ERR_INVALID_ARG;
     if (workspace_bytes < prompt_workspace_bytes(*prompts)) return SD_ERR_WORKSPACE;
-    if (prompts->N == 0) return SD_OK;
     if (!ok_heads(q, ldq, prompts->Hq) || !ok_heads(out, ldo, prompts->Hq) || out == q) return SD_ERR_INVALID_ARG;
     if ((int64_t)cache->num_blocks * prompts->Hkv * kBlock > INT32_MAX) return SD_ERR_UNSUPPORTED;             // (rows of the copies' coordinates)
     return launch_prompt_attention(*prompts, *cache, q, ldq, scale, out, ldo, lse, workspace, dev_status,
