@@ -356,6 +356,7 @@ class PromptStep(sd._OnAnyStream):
         self.granted = torch.ones(b.B, dtype=torch.int32, device=step.device)
         self.workspace = torch.empty(sd.sd_prompt_workspace_bytes(self.prompts), dtype=torch.uint8, device=step.device)
         self._makes(self.granted, self.workspace)
+        self._begun = False                                    # between begin() and end()
 
     def _ready(self, stream):
         super()._ready(stream)
@@ -365,6 +366,7 @@ class PromptStep(sd._OnAnyStream):
         """Tables, slots and positions (self.prompts.position: what a decoder rotates q and k by), and the attention's plan."""
         p, status = self.prompts, self.step.status
         self._ready(stream)
+        self._begun = True
         if self.pool is not None:
             sd.sd_assign_blocks(self.pool, p.block_table, p.n_blocks, p.len, p.n_new, self.granted, status, stream)
         sd.sd_prompt_prepare(p, status, stream)
@@ -379,12 +381,26 @@ class PromptStep(sd._OnAnyStream):
     def end(self, stream=None):
         """The new tokens count as cached from here on (of sequences that were not left out)."""
         self._ready(stream)
+        self._begun = False
+        p = self.prompts
+        if p.N == 0:                                           # (no rows: nobody's tokens were taken in)
+            return
         with contextlib.nullcontext() if stream is None else torch.cuda.stream(sd.stream_of(stream)):
-            self.prompts.len.addcmul_(self.prompts.n_new, self.granted)
+            # whom sd_prompt_prepare has left out, by the pool, its table or the rows that there are, has no slots; who has no
+            # room for a first row either starts where the rows end
+            first = p.start[:-1]
+            taken = (p.slot.index_select(0, first.clamp(max=p.N - 1)) >= 0).logical_and_(first < p.N)
+            p.len.addcmul_(p.n_new.clamp(min=0), taken.to(torch.int32))
+
+    @property
+    def trees_granted(self) -> torch.Tensor:
+        """[B]: 0 for sequences that the last reserve_trees() had no blocks for."""
+        return self.step.trees_granted
 
     def reserve_trees(self, stream=None):
         """Blocks for the trees of the next verification (or what behind it is not needed, given back): tables that cover len + n_nodes.
-        A sequence that the pool does not suffice for (the step's trees_granted 0) keeps what it has and waits: its n_nodes becomes negative, and
+        A sequence that the pool does not suffice for (trees_granted 0) keeps what it has and waits: its n_nodes becomes negative, and
         the step leaves it out (n_acc 0) until a later call finds blocks for it.  run_from_host() does this by itself, once its trees are there."""
         assert self.pool is not None, "the tables are the caller's: there is no pool to take blocks from"
+        assert not self._begun, "blocks for trees come behind end(): until then the new tokens' own would be given back"
         self.step._reserve_trees(stream)

@@ -122,6 +122,14 @@ def test_memory_of_a_step_that_is_dropped_is_not_given_away_while_it_runs():
     torch.cuda.synchronize()
     side = torch.cuda.Stream()
     p = vs.prompts(90, new, pool, held)
+    for _ in range(2):                                       # (the first time loads the kernels, which takes as long as the pause below)
+        p.begin(side)
+        p.layer(0, qkv[:, :28], qkv[:, 28:32], qkv[:, 32:], out, stream=side)
+        p.end(side)
+    torch.cuda.synchronize()
+    vs.batch.len.zero_()
+    torch.cuda.synchronize()
+    p = vs.prompts(90, new, pool, held)
     taken = {t.data_ptr(): t.numel() * t.element_size() for t in (p.workspace, p.granted)}
     sizes = list(taken.values())
     with torch.cuda.stream(side):
@@ -136,3 +144,52 @@ def test_memory_of_a_step_that_is_dropped_is_not_given_away_while_it_runs():
     torch.cuda.synchronize()
     vs.check_status()
     assert vs.batch.len.tolist() == [60, 30]
+
+
+def pieces(vs, p, N):
+    qkv = torch.randn((N, 36, 128), device="cuda").to(bf)
+    out = torch.zeros((N, 28, 128), dtype=bf, device="cuda")
+    p.begin()
+    for l in range(vs.L):
+        p.layer(l, qkv[:, :28], qkv[:, 28:32], qkv[:, 32:], out)
+    p.end()
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("pooled", [True, False])
+def test_tokens_that_had_no_rows_do_not_count_as_cached(pooled):
+    vs = VerifyStep(workload(4, L=1))
+    vs.batch.len.zero_()
+    with_pool = (sd.BlockPool(int(vs.k_cache[0].shape[0])), torch.zeros(4, dtype=torch.int32, device="cuda")) if pooled else ()
+    for N, want in ((120, [60, 60, 0, 0]), (130, [60, 60, 0, 0]), (119, [60, 0, 0, 0]), (0, [0, 0, 0, 0])):      # of 60, 60, 30 and 5
+        vs.batch.len.zero_()
+        vs.status.zero_()
+        pieces(vs, vs.prompts(N, [60, 60, 30, 5], *with_pool), N)
+        assert int(vs.status.item()) == sd.SD_ERR_BOUNDS
+        assert vs.batch.len.tolist() == want, N
+
+
+def test_tokens_that_the_table_has_no_room_for_do_not_count_as_cached():
+    vs = VerifyStep(workload(3, L=1))
+    room = 64 * vs.batch.max_blocks
+    vs.batch.len.copy_(torch.tensor([10, 7, room - 20], dtype=torch.int32))
+    pieces(vs, vs.prompts(room + 50, [room, 20, 21]), room + 50)
+    assert int(vs.status.item()) == sd.SD_ERR_BOUNDS and vs.batch.len.tolist() == [10, 27, room - 20]
+    vs.status.zero_()
+    pieces(vs, vs.prompts(50, [-5, 20, 20]), 50)
+    assert int(vs.status.item()) == sd.SD_ERR_INVALID_ARG and vs.batch.len.tolist() == [10, 47, room]
+
+
+def test_blocks_for_trees_come_behind_the_prompts():
+    vs = VerifyStep(workload(2, L=1))
+    vs.batch.len.zero_()
+    pool, held = sd.BlockPool(3), torch.zeros(2, dtype=torch.int32, device="cuda")
+    p = vs.prompts(120, [60, 60], pool, held)
+    p.begin()
+    with pytest.raises(AssertionError):                      # (it would take the blocks of the new tokens back)
+        p.reserve_trees()
+    p.end()
+    p.reserve_trees()
+    torch.cuda.synchronize()
+    vs.check_status()
+    assert p.granted.tolist() == [1, 1] and p.trees_granted.tolist() == [1, 0] and held.tolist() == [2, 1] and vs.batch.len.tolist() == [60, 60]
