@@ -54,6 +54,7 @@ struct PromptShared {
     uint64_t* p_full;       // [3] soft-max -> MMA: weights of tile g written over its scores
     uint64_t* commit;       // [4] per TMEM quadrant: tile g's soft-max is final (phase g)
     uint64_t* ref_full;     // [2][4] per TMEM quadrant: the reference that an entry's first tile sets, entries in turn
+    uint64_t* ref_seen;     // [4] per TMEM quadrant: the group without an entry's first tile has read that reference (phase: the entry)
     uint64_t* q_full;       // [2] TMA -> MMA, entries in turn
     uint64_t* q_empty;      // [2] MMA -> TMA: the entry's last scores are there
     uint64_t* o_full;       // MMA -> results: O updated by the entry's last tile
@@ -79,14 +80,14 @@ struct PromptShared {
         const auto take = [&](int n) { uint64_t* const got = at; at += n; return got; };
         k_full = take(kPKeyStages); k_empty = take(kPKeyStages);
         v_full = take(kPStages); v_empty = take(kPStages); s_full = take(kPStages); p_full = take(kPStages);
-        commit = take(4); ref_full = take(8);
+        commit = take(4); ref_full = take(8); ref_seen = take(4);
         q_full = take(kPQueryStages); q_empty = take(kPQueryStages);
         o_full = take(1); o_empty = take(1); other_full = take(1); sum_full = take(1);
         work_full = take(kPWorks); work_empty = take(kPWorks); unwound = take(2);
         tmem_slot = reinterpret_cast<uint32_t*>(take(1));
         abort_flag = reinterpret_cast<int*>(tmem_slot) + 1;
         works = reinterpret_cast<int*>(at);
-        static_assert((2 * kPKeyStages + 4 * kPStages + 12 + 2 * kPQueryStages + 4 + 2 * kPWorks + 3) * 8 + kPWorks * 36 <= kPBars, "");
+        static_assert((2 * kPKeyStages + 4 * kPStages + 16 + 2 * kPQueryStages + 4 + 2 * kPWorks + 3) * 8 + kPWorks * 36 <= kPBars, "");
         refs = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(bars) + kPBars);
         others = refs + 2 * kRowTile;
         sums = reinterpret_cast<float2*>(others + kRowTile);
@@ -99,7 +100,9 @@ struct PromptShared {
         for (int i = 0; i < kPStages; ++i) {
             mbar_init(&v_full[i], 1); mbar_init(&s_full[i], 1); mbar_init(&v_empty[i], 1); mbar_init(&p_full[i], 4);
         }
-        for (int i = 0; i < 4; ++i) { mbar_init(&commit[i], 1); mbar_init(&ref_full[i], 1); mbar_init(&ref_full[4 + i], 1); }
+        for (int i = 0; i < 4; ++i) {
+            mbar_init(&commit[i], 1); mbar_init(&ref_full[i], 1); mbar_init(&ref_full[4 + i], 1); mbar_init(&ref_seen[i], 1);
+        }
         mbar_init(o_full, 1); mbar_init(o_empty, 4);
         mbar_init(other_full, 4); mbar_init(sum_full, 4);
         for (int i = 0; i < kPWorks; ++i) { mbar_init(&work_full[i], 1); mbar_init(&work_empty[i], 15); }
@@ -241,8 +244,8 @@ struct TileAt {
     int vis;                // keys of the tile that this row sees
     int blocks;             // of 64 keys, 1 or 2
     int first;              // the first tile of an entry
-    uint64_t* o_done;       // O updated by the tile before
-    uint32_t o_phase;
+    uint64_t* hold;         // what a reference is raised behind: O updated by the tile before; for an entry's first tile, if it has more: its
+    uint32_t hold_phase;    // reference read by the other group, which would otherwise see it before or after, as it happens
     int row_ok;
 };
 // A tile whose blocks in front of hb have been weighed (the tile before it is final).  Those get the reference that another tile has raised
@@ -291,8 +294,8 @@ __device__ __noinline__ RowState careful_tile(RowState st, const TileAt t, int h
         const bool raise = mt > st.m + kRaiseAbove;
         if (__any_sync(0xffffffffu, raise)) {
             const float alpha = raise ? exp2f(st.m - mt) : 1.f;                // (a power of two: weights of the first block stay exact)
+            if (t.hold && !mbar_wait_warp(t.hold, t.hold_phase, abort_flag, limit)) { st.ok = 0; return st; }
             if (!t.first) {                                // (nothing has been added to O before an entry's first tile)
-                if (!mbar_wait_warp(t.o_done, t.o_phase, abort_flag, limit)) { st.ok = 0; return st; }
                 tc_fence_after_sync();
 #pragma unroll 1
                 for (int c = 0; c < 4; ++c) {
@@ -542,6 +545,8 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
             const int nt = w.tiles();
             RowState st{0.f, 0.f, 1.f, 1};
             const int j0 = (int)(n & 1u) ^ group;          // this group's tiles: every second one of the stream
+            uint64_t* const ref_seen = sh.ref_seen + quad;
+            if (j0 >= nt && lane == 0) mbar_arrive(ref_seen);                  // (nothing to read)
             RingAt<kPStages> s_at = at;
             if (j0) s_at.next();
             for (int j = j0; j < nt; j += 2, s_at.next(), s_at.next()) {
@@ -551,6 +556,8 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
                 if (j == 1) {                              // the reference that the other group found in the first tile
                     if (!(ok = mbar_wait_warp(ref_full, (entry >> 1) & 1u, abort_flag, limit))) break;
                     st.m = *my_ref;
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(ref_seen);
                 }
                 if (!(ok = mbar_wait_warp(&sh.s_full[s_at.slot], s_at.phase, abort_flag, limit))) break;
                 tc_fence_after_sync();
@@ -632,7 +639,8 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
                 if (begun && !(ok = mbar_wait_warp(commit, commit_phase, abort_flag, limit))) break;
                 if (__any_sync(0xffffffffu, hb < blocks || (row_ok && *my_ref != st.m))) {
                     const int last = s_at.slot == 0 ? kPStages - 1 : s_at.slot - 1;
-                    const TileAt t{ts, tmem + lanes, vis, blocks, j == 0, &sh.v_empty[last], s_at.slot == 0 ? s_at.phase ^ 1u : s_at.phase, row_ok};
+                    const TileAt t{ts, tmem + lanes, vis, blocks, j == 0, j > 0 ? &sh.v_empty[last] : nt > 1 ? ref_seen : nullptr,
+                                   j == 0 ? entry & 1u : s_at.slot == 0 ? s_at.phase ^ 1u : s_at.phase, row_ok};
                     st = careful_tile(st, t, hb, a.scale_log2, my_ref, abort_flag, limit);
                     if (!(ok = st.ok)) break;
                 }
