@@ -25,6 +25,7 @@ struct WideShared {
     uint64_t* p_full;       // [3] softmax -> MMA: P of tile j written over its scores
     uint64_t* commit;       // [4] per TMEM quadrant: tile j's softmax is final (phase j)
     uint64_t* ref_full;     // [4] per TMEM quadrant: the first tile's reference is known
+    uint64_t* ref_seen;     // [4] per TMEM quadrant: the other group has read it
     uint64_t* o_full;       // MMA -> softmax: every MMA of a row tile has completed
     uint64_t* q_full;       // TMA -> MMA
     uint64_t* x_full;       // the other chunks' rows have arrived
@@ -42,8 +43,10 @@ struct WideShared {
         k_full = bars; v_full = bars + 3; s_full = bars + 6; v_empty = bars + 9; p_full = bars + 12; commit = bars + 15;
         o_full = bars + 19; q_full = bars + 20; x_full = bars + 21; ref_full = bars + 22;
         tmem_slot = reinterpret_cast<uint32_t*>(bars + 26);
-        abort_flag = reinterpret_cast<int*>(bars + 27);
-        seq = reinterpret_cast<int*>(bars + 28);
+        abort_flag = reinterpret_cast<int*>(bars + 26) + 1;
+        seq = reinterpret_cast<int*>(bars + 27);
+        ref_seen = bars + 28;
+        static_assert(32 * 8 <= kWBars, "");
         ref_smem = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(bars) + kWBars);
         sum_smem = ref_smem + kRowTile;
     }
@@ -54,7 +57,7 @@ struct WideShared {
             mbar_init(&k_full[i], 1); mbar_init(&v_full[i], 1); mbar_init(&s_full[i], 1);
             mbar_init(&v_empty[i], 1); mbar_init(&p_full[i], 4);
         }
-        for (int i = 0; i < 4; ++i) { mbar_init(&commit[i], 1); mbar_init(&ref_full[i], 1); }
+        for (int i = 0; i < 4; ++i) { mbar_init(&commit[i], 1); mbar_init(&ref_full[i], 1); mbar_init(&ref_seen[i], 1); }
         mbar_init(o_full, 1); mbar_init(q_full, 1); mbar_init(x_full, 1);
     }
 };
@@ -173,6 +176,8 @@ __device__ __forceinline__ bool wide_softmax(const AttnPlan& plan, const WideSha
             if (!mbar_wait(&sh.ref_full[quad], 0, sh.abort_flag, plan.wait_cycles)) return false;
             m_used = *my_ref;
             neg_m2 = pack_f32x2(-m_used, -m_used);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh.ref_seen[quad]);
         }
         uint32_t mask[4] = {~0u, ~0u, ~0u, ~0u};           // visible keys of the four 32-key quarters
         if (!mbar_wait(&sh.s_full[s], ph, sh.abort_flag, plan.wait_cycles)) return false;
@@ -248,6 +253,9 @@ __device__ __forceinline__ bool wide_softmax(const AttnPlan& plan, const WideSha
             tmem_st_wait();
             l *= alpha;
         }
+        // (what tile 0 raises is raised behind the other group's reading of its first reference: seen before or after, as it
+        // happened, it would decide what that group's first tile does)
+        if (j == 0 && w.nt > 1 && !mbar_wait(&sh.ref_seen[quad], 0, sh.abort_flag, plan.wait_cycles)) return false;
         if (raise) m_used = mt;
         *my_ref = m_used;
         neg_m2 = pack_f32x2(-m_used, -m_used);
