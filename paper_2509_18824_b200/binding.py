@@ -583,6 +583,7 @@ class _OnAnyStream:
     def _makes(self, *tensors):
         self._made = [t for t in tensors if t is not None]
         self._streams = set()
+        self._device = _here()                             # (where its arrays lie: _ints)
         if self._made:
             self._streams.add(torch._C._cuda_getCurrentRawStream(_here()))
             self._event = torch.cuda.Event()
@@ -590,8 +591,11 @@ class _OnAnyStream:
 
     def _ready(self, stream) -> None:
         """In front of a call on `stream` (None: the current one)."""
+        here = _here()
+        if here != self._device:
+            raise AssertionError(f"arrays on device {self._device}, the current one is {here}")
         if self._made:
-            raw = torch._C._cuda_getCurrentRawStream(_here()) if stream is None else _raw_stream(stream)
+            raw = torch._C._cuda_getCurrentRawStream(here) if stream is None else _raw_stream(stream)
             if raw not in self._streams:
                 self._streams.add(raw)
                 other = stream_of(raw)
