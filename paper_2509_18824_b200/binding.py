@@ -586,8 +586,10 @@ class _OnAnyStream:
         self._device = _here()                             # (where its arrays lie: _ints)
         if self._made:
             self._streams.add(torch._C._cuda_getCurrentRawStream(_here()))
-            self._event = torch.cuda.Event()
-            self._event.record()
+            self._event = None
+            if not torch.cuda.is_current_stream_capturing():                   # (nothing outside of a capture can wait for an event in it)
+                self._event = torch.cuda.Event()
+                self._event.record()
 
     def _ready(self, stream) -> None:
         """In front of a call on `stream` (None: the current one)."""
@@ -599,8 +601,9 @@ class _OnAnyStream:
             if raw not in self._streams:
                 self._streams.add(raw)
                 other = stream_of(raw)
-                if not torch.cuda.is_current_stream_capturing():               # (a capture begins behind a synchronisation)
-                    other.wait_event(self._event)
+                with torch.cuda.stream(other):
+                    if self._event is not None and not torch.cuda.is_current_stream_capturing():       # (a capture begins behind a synchronisation)
+                        other.wait_event(self._event)
                 for t in self._made:
                     t.record_stream(other)
 
