@@ -176,12 +176,14 @@ class VerifyStep:
         given uniforms (u [B,T], w [B], device f32), the residual draw, then compaction; through the one
         fused call, or (fused=False) as the three separate calls it stands for."""
         if getattr(self, "lse_rows", None) is None:
-            self.lse_rows = torch.zeros(self.w.B * self.w.T_max, dtype=torch.float32, device=self.device)
-            self.group_stats = torch.zeros(sd.group_stats_shape(self.w.B * self.w.T_max, self.w.V),
-                                           dtype=torch.float32, device=self.device)
-            need = sd.sd_workspace_bytes(self.batch, self.w.B * self.w.T_max, self.w.V)
-            if self.workspace.numel() < need:
-                self.workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
+            # (on the calls' stream, and not filled, as in tail_filtered)
+            with contextlib.nullcontext() if stream is None else torch.cuda.stream(sd.stream_of(stream)):
+                self.lse_rows = torch.empty(self.w.B * self.w.T_max, dtype=torch.float32, device=self.device)
+                self.group_stats = torch.empty(sd.group_stats_shape(self.w.B * self.w.T_max, self.w.V),
+                                               dtype=torch.float32, device=self.device)
+                need = sd.sd_workspace_bytes(self.batch, self.w.B * self.w.T_max, self.w.V)
+                if self.workspace.numel() < need:
+                    self.workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
         if fused:
             sd.sd_lmhead_accept_sampled_compact(self.batch, self.hidden, self.W, inv_temp, self.draft_tok, u, w,
                                                 self.layerset, self.lse_rows, self.group_stats, self.n_acc, self.path,
