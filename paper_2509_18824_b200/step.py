@@ -71,6 +71,7 @@ class VerifyStep:
         # trees, and whom it suffices for
         self._pool = None
         self._asked, self.trees_granted = (torch.ones(B, dtype=torch.int32, device=d) for _ in range(2))
+        self._columns = torch.arange(self.batch.max_blocks, dtype=torch.int32, device=d)
         nbytes = sd.sd_workspace_bytes(self.batch, M if self.W is not None else 0, w.V if self.W is not None else 0)
         self.workspace = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=d)
         self.caches = [sd.kv_layer(k, v) for k, v in zip(self.k_cache, self.v_cache)]
@@ -319,16 +320,25 @@ class VerifyStep:
         self._ev_done[slot].record(main)
 
     def prompts(self, N: int, n_new, pool: Optional["sd.BlockPool"] = None, n_blocks: Optional[torch.Tensor] = None) -> "PromptStep":
-        """What brings prompts (or the next pieces of them) into this step's caches, see PromptStep."""
+        """What brings prompts (or the next pieces of them) into this step's caches, see PromptStep.  From its first begin() with a pool on
+        the step's tables follow that pool: before each run() reserve_trees() finds blocks for the trees (run_from_host() does it by itself)."""
         return PromptStep(self, N, n_new, pool, n_blocks)
+
+    def _cover(self, n, granted, stream):
+        """Tables that cover len + n.  Entries behind a sequence's blocks name none: the blocks that stood there may be another one's by
+        now, and what is written there by mistake has to be reported."""
+        b, (pool, n_blocks) = self.batch, self._pool
+        sd.sd_assign_blocks(pool, b.block_table, n_blocks, b.len, n, granted, self.status, stream)
+        with contextlib.nullcontext() if stream is None else torch.cuda.stream(sd.stream_of(stream)):
+            b.block_table.masked_fill_(self._columns >= n_blocks[:, None], -1)
 
     def _reserve_trees(self, stream=None):
         """Tables that cover len + n_nodes.  A sequence that the pool does not suffice for gets minus its n_nodes, so that it takes no
-        part in the step: its table may name blocks that are another one's by now."""
-        b, (pool, n_blocks) = self.batch, self._pool
+        part in the step."""
+        b = self.batch
         with contextlib.nullcontext() if stream is None else torch.cuda.stream(sd.stream_of(stream)):
             torch.abs(b.n_nodes, out=self._asked)
-            sd.sd_assign_blocks(pool, b.block_table, n_blocks, b.len, self._asked, self.trees_granted, self.status, stream)
+            self._cover(self._asked, self.trees_granted, stream)
             torch.neg(self._asked, out=b.n_nodes)
             b.n_nodes.addcmul_(self._asked, self.trees_granted, value=2)
             if self._copy_stream is not None and not torch.cuda.is_current_stream_capturing():
@@ -350,8 +360,6 @@ class PromptStep(sd._OnAnyStream):
     def __init__(self, step: VerifyStep, N: int, n_new, pool: Optional["sd.BlockPool"] = None, n_blocks: Optional[torch.Tensor] = None):
         assert (pool is None) == (n_blocks is None), "a pool of blocks goes with the counts that it is kept for"
         self.step, self.pool = step, pool
-        if pool is not None:
-            step._pool = pool, n_blocks
         b, w = step.batch, step.w
         self.prompts = sd.Prompts(N, b.Hq, b.Hkv, b.D, b.block_table, b.len, n_new, n_blocks, num_blocks=int(step.k_cache[0].shape[0]),
                                   device=step.device)
@@ -370,7 +378,8 @@ class PromptStep(sd._OnAnyStream):
         self._ready(stream)
         self._begun = True
         if self.pool is not None:
-            sd.sd_assign_blocks(self.pool, p.block_table, p.n_blocks, p.len, p.n_new, self.granted, status, stream)
+            self.step._pool = self.pool, p.n_blocks
+            self.step._cover(p.n_new, self.granted, stream)
         sd.sd_prompt_prepare(p, status, stream)
 
     def layer(self, l: int, q, k, v, out, lse=None, stream=None):
@@ -405,4 +414,6 @@ class PromptStep(sd._OnAnyStream):
         the step leaves it out (n_acc 0) until a later call finds blocks for it.  run_from_host() does this by itself, once its trees are there."""
         assert self.pool is not None, "the tables are the caller's: there is no pool to take blocks from"
         assert not self._begun, "blocks for trees come behind end(): until then the new tokens' own would be given back"
+        self._ready(stream)
+        self.step._pool = self.pool, self.prompts.n_blocks
         self.step._reserve_trees(stream)

@@ -54,18 +54,24 @@ def tails(vs):
 
 def short_of_blocks(vs):
     """Three blocks: sequence 0 has 60 tokens and gave the block of its tree back, sequence 1 has taken it for its prompt."""
+    p, held, given_back = take_all_blocks(vs)
+    table = vs.batch.block_table.cpu().numpy()
+    assert held.tolist() == [1, 2] and vs.batch.len.tolist() == [60, 100] and given_back in table[1, :2]
+    vs.check_status()
+    return p, held
+
+
+def take_all_blocks(vs):
     pool, held = sd.BlockPool(3), torch.zeros(2, dtype=torch.int32, device="cuda")
     vs.batch.len.zero_()
     p = vs.prompts(60, [60, 0], pool, held)
     fill(vs, p, 1)
     p.reserve_trees()
     assert held.tolist() == [2, 1]
+    given_back = int(vs.batch.block_table[0, 1])
     p = vs.prompts(100, [0, 100], pool, held)
     fill(vs, p, 2)
-    table = vs.batch.block_table.cpu().numpy()
-    assert held.tolist() == [1, 2] and vs.batch.len.tolist() == [60, 100] and table[0, 1] in table[1, :2]
-    vs.check_status()
-    return p, held
+    return p, held, given_back
 
 
 def expected(vs, before, who, at):
@@ -200,3 +206,36 @@ def test_masks_of_a_tree_that_waits_are_made():
     torch.cuda.synchronize()
     vs.check_status()
     assert torch.equal(vs.batch.anc_mask, want)
+
+
+@pytest.mark.parametrize("tail", ["fused", "sampled", "filtered"])
+def test_a_step_whose_trees_have_no_blocks_is_reported(tail):
+    """Blocks for the trees have not been reserved: nothing goes to blocks that were given back."""
+    vs = VerifyStep(workload(2))
+    agreeable(vs)
+    _, held = short_of_blocks(vs)
+    before = [c.clone() for c in vs.k_cache + vs.v_cache]
+    vs.attention_layers()
+    tails(vs)[tail]()
+    torch.cuda.synchronize()
+    assert int(vs.status.item()) == sd.SD_ERR_BOUNDS
+    # what fits into the blocks that they hold is there, and nothing else
+    row, want = vs.batch.block_table.cpu().numpy(), [c.clone() for c in before]
+    for c, tree in zip(want, vs.k_tree + vs.v_tree):
+        for b, at in ((0, 60), (1, 100)):
+            for i in range(T):
+                if at + i < 64 * int(held[b]):
+                    c[int(row[b, (at + i) // 64]), :, (at + i) % 64] = tree[b, i]
+    assert same(vs.k_cache + vs.v_cache, want)
+
+
+def test_table_entries_behind_a_sequences_blocks_name_none():
+    vs = VerifyStep(workload(2))
+    vs.batch.block_table.fill_(5)
+    p, held = short_of_blocks(vs)
+    p.reserve_trees()
+    torch.cuda.synchronize()
+    vs.check_status()
+    table = vs.batch.block_table.cpu().numpy()
+    for b in range(2):
+        assert (table[b, :int(held[b])] >= 0).all() and (table[b, int(held[b]):] == -1).all()
