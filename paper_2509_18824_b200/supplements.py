@@ -284,8 +284,10 @@ def rows(M=480, V=152064, K=64, train=4096):
 
 
 def prompts(Hq=28, Hkv=4):
-    """Blocks, copies into the cache and attention of packed new tokens; the caches of two calls in turn are larger than L2 together."""
+    """Copies into the cache and attention of packed new tokens, and their plan.  Rows and caches of several layers take turns; rates are given
+    where what a call moves is twice the size of L2 before it comes again (a few rows' copies are not)."""
     hbm, tens, src = _peaks()
+    twice_l2 = 2 * torch.cuda.get_device_properties(0).L2_cache_size
     for what, new, cached in (("prompts of 4096 tokens", [4096] * 8, [0] * 8), ("one prompt of 32768", [32768], [0]),
                               ("ragged prompts", list(range(64, 2049, 128)), [0] * 16),
                               ("1024 tokens behind 8192", [1024], [8192]), ("one token each behind 4096", [1] * 32, [4096] * 32)):
@@ -295,20 +297,30 @@ def prompts(Hq=28, Hkv=4):
         order = torch.randperm(total, device="cuda").int()
         table = torch.zeros((B, max(held)), dtype=torch.int32, device="cuda")
         table[torch.arange(max(held), device="cuda")[None] < torch.tensor(held, device="cuda")[:, None]] = order
-        k, v = (torch.randn((total, Hkv, 64, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
-        qkv = torch.randn((N, Hq + 2 * Hkv, 128), dtype=torch.bfloat16, device="cuda")
-        out, st = torch.empty((N, Hq, 128), dtype=torch.bfloat16, device="cuda"), sd.new_status()
-        p = sd.Prompts(N, Hq, Hkv, 128, table, cached, new, held, num_blocks=total)
-        ws = torch.empty(sd.sd_prompt_workspace_bytes(p), dtype=torch.uint8, device="cuda")
-        cache = sd.kv_layer(k, v)
-        ms = {"sd_prompt_prepare": _time(lambda: sd.sd_prompt_prepare(p, st), 20),
-              "sd_append_kv": _time(lambda: sd.sd_append_kv(p, cache, qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:], st), 20),
-              "sd_prompt_attention": _time(lambda: sd.sd_prompt_attention(p, cache, qkv[:, :Hq], 128 ** -0.5, out, None, ws, st), 20)}
         seen = sum(n * c + n * (n + 1) // 2 for n, c in zip(new, cached))
         flops, nbytes = 4.0 * 128 * Hq * seen, {"sd_append_kv": 8.0 * N * Hkv * 128, "sd_prompt_attention": 4.0 * 128 * (N * Hq + Hkv * 64 * total)}
+        # as many layers as that takes, in 8 GB at most
+        L = int(max(2, min(-(-twice_l2 // min(nbytes.values())), 8e9 // (nbytes["sd_append_kv"] + nbytes["sd_prompt_attention"]))))
+        st, p = sd.new_status(), sd.Prompts(N, Hq, Hkv, 128, table, cached, new, held, num_blocks=total)
+        ws = torch.empty(sd.sd_prompt_workspace_bytes(p), dtype=torch.uint8, device="cuda")
+        layers = []
+        for _ in range(L):
+            k, v = (torch.randn((total, Hkv, 64, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+            qkv = torch.randn((N, Hq + 2 * Hkv, 128), dtype=torch.bfloat16, device="cuda")
+            layers.append((sd.kv_layer(k, v), qkv[:, :Hq], qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:], torch.empty((N, Hq, 128), dtype=torch.bfloat16, device="cuda")))
+
+        def append():
+            for cache, _, k, v, _ in layers:
+                sd.sd_append_kv(p, cache, k, v, st)
+
+        def attend():
+            for cache, q, _, _, out in layers:
+                sd.sd_prompt_attention(p, cache, q, 128 ** -0.5, out, None, ws, st)
+        ms = {"sd_prompt_prepare": _time(lambda: sd.sd_prompt_prepare(p, st), 20), "sd_append_kv": _time(append, -(-20 // L)) / L,
+              "sd_prompt_attention": _time(attend, -(-20 // L)) / L}
         for call, t in ms.items():
-            line = {"call": call, "workload": what, "us": t * 1e3, "peaks": src, "status": int(st.item())}
-            if call in nbytes:
+            line = {"call": call, "workload": what, "us": t * 1e3, "layers": L, "peaks": src, "status": int(st.item())}
+            if L * nbytes.get(call, 0) >= twice_l2:
                 line.update(gbs=nbytes[call] / t / 1e6, frac_hbm=nbytes[call] / t / 1e6 / hbm)
             if call == "sd_prompt_attention":
                 line.update(tflops=flops / t / 1e9, frac_tensor=flops / t / 1e9 / tens)
