@@ -369,155 +369,155 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
     bool ok = true;                                        // no wait has run out
     if (warp >= 12) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-    if (warp == kPKeyWarp || warp == kPValueWarp) {
-        // ------------------------------------------------------------ copies (whole warps in uniform control flow)
-        const bool keys = warp == kPKeyWarp;
-        const CUtensorMap* const map = keys ? &k_map : &v_map;
-        uint8_t* const ring = keys ? sh.k_smem : sh.v_smem;
-        uint64_t *const full = keys ? sh.k_full : sh.v_full, *const empty = keys ? sh.k_empty : sh.v_empty;
-        const int stages = keys ? kPKeyStages : kPStages;
-        const uint64_t keep = policy_evict_last(), once = policy_evict_first();
-        int slot = 0;                                      // of the next K or V
-        uint32_t slot_phase = 1u;                          // (empty at first)
-        RingAt<kPQueryStages> q_at;
-        RingAt<kPWorks> work_at;
-        PromptWalk walk;
-        if (keys) walk.begin(a);
-        if (keys && !walk.made && lane == 0) set_status(status, SD_ERR_INVALID_ARG);
-        while (ok) {
-            PromptWork w;
-            if (keys) {
-                w = walk.next(a.p.Hkv);
-                if (!(ok = mbar_wait_warp(&sh.work_empty[work_at.slot], work_at.phase ^ 1u, abort_flag, limit))) break;
-                if (lane == 0) {
-                    int* dst = sh.works + work_at.slot * 9;
-                    dst[0] = w.row0; dst[1] = w.pos0; dst[2] = w.tokens; dst[3] = w.b; dst[4] = w.kb0; dst[5] = w.end; dst[6] = w.slot; dst[7] = w.h;
-                    dst[8] = w.nb;
-                    mbar_arrive(&sh.work_full[work_at.slot]);
+        if (warp == kPKeyWarp || warp == kPValueWarp) {
+            // ------------------------------------------------------------ copies (whole warps in uniform control flow)
+            const bool keys = warp == kPKeyWarp;
+            const CUtensorMap* const map = keys ? &k_map : &v_map;
+            uint8_t* const ring = keys ? sh.k_smem : sh.v_smem;
+            uint64_t *const full = keys ? sh.k_full : sh.v_full, *const empty = keys ? sh.k_empty : sh.v_empty;
+            const int stages = keys ? kPKeyStages : kPStages;
+            const uint64_t keep = policy_evict_last(), once = policy_evict_first();
+            int slot = 0;                                      // of the next K or V
+            uint32_t slot_phase = 1u;                          // (empty at first)
+            RingAt<kPQueryStages> q_at;
+            RingAt<kPWorks> work_at;
+            PromptWalk walk;
+            if (keys) walk.begin(a);
+            if (keys && !walk.made && lane == 0) set_status(status, SD_ERR_INVALID_ARG);
+            while (ok) {
+                PromptWork w;
+                if (keys) {
+                    w = walk.next(a.p.Hkv);
+                    if (!(ok = mbar_wait_warp(&sh.work_empty[work_at.slot], work_at.phase ^ 1u, abort_flag, limit))) break;
+                    if (lane == 0) {
+                        int* dst = sh.works + work_at.slot * 9;
+                        dst[0] = w.row0; dst[1] = w.pos0; dst[2] = w.tokens; dst[3] = w.b; dst[4] = w.kb0; dst[5] = w.end; dst[6] = w.slot; dst[7] = w.h;
+                        dst[8] = w.nb;
+                        mbar_arrive(&sh.work_full[work_at.slot]);
+                    }
+                    __syncwarp();
+                    work_at.next();
+                    if (w.nb == 0) break;
+                } else {
+                    if (!(ok = see_work(sh, work_at, w, limit))) break;
+                    done_with_work(sh, work_at, lane);
+                    if (w.nb == 0) break;
                 }
-                __syncwarp();
-                work_at.next();
-                if (w.nb == 0) break;
-            } else {
+                const uint64_t hint = w.tokens * a.g.G <= 16 ? once : keep;
+                const int32_t* table = a.p.block_table + (size_t)w.b * a.p.max_blocks_per_seq + w.kb0;
+                int held = 0;                                  // 32 entries of the table
+                const auto block_of = [&](int i) {
+                    int blk = __shfl_sync(0xffffffffu, held, i & 31);
+                    if (blk < 0 || blk >= a.num_blocks) { if (lane == 0) set_status(status, SD_ERR_BOUNDS); blk = 0; }
+                    return blk;
+                };
+                for (int j = 0; ok && 2 * j < w.nb; ++j) {
+                    if ((j & 15) == 0) held = 2 * j + lane < w.nb ? __ldcg(table + 2 * j + lane) : 0;
+                    const bool two = 2 * j + 1 < w.nb;
+                    const int y0 = (block_of(2 * j) * a.p.Hkv + w.h) * kBlock, y1 = two ? (block_of(2 * j + 1) * a.p.Hkv + w.h) * kBlock : 0;
+                    if (!(ok = mbar_wait_warp(&empty[slot], slot_phase, abort_flag, limit))) break;
+                    uint8_t* dst = ring + slot * kPStage;
+                    if (elect_one()) {
+                        mbar_arrive_expect_tx(&full[slot], two ? kPStage : kPStage / 2);
+                        tma_load_2d(dst, map, 0, y0, &full[slot], hint);
+                        tma_load_2d(dst + kPHalf, map, 64, y0, &full[slot], hint);
+                        if (two) {
+                            tma_load_2d(dst + kPHalf / 2, map, 0, y1, &full[slot], hint);
+                            tma_load_2d(dst + kPHalf + kPHalf / 2, map, 64, y1, &full[slot], hint);
+                        }
+                    }
+                    __syncwarp();
+                    if (++slot == stages) { slot = 0; slot_phase ^= 1u; }
+                    if (j == 0 && keys) {
+                        if (!(ok = mbar_wait_warp(&sh.q_empty[q_at.slot], q_at.phase ^ 1u, abort_flag, limit))) break;
+                        if (elect_one()) {
+                            uint8_t* to = sh.q_smem + q_at.slot * kPQBytes;
+                            mbar_arrive_expect_tx(&sh.q_full[q_at.slot], (uint32_t)(a.g.tokens * a.g.G) * kD * 2);
+                            tma_load_3d(to, &q_map, 0, w.h * a.g.G, w.row0, &sh.q_full[q_at.slot], once);
+                            tma_load_3d(to + kRowTile * 128, &q_map, 64, w.h * a.g.G, w.row0, &sh.q_full[q_at.slot], once);
+                        }
+                        __syncwarp();
+                        q_at.next();
+                    }
+                }
+            }
+        } else {                                               // warps 12 and 13
+            // ------------------------------------------------------------ products (whole warps in uniform control flow, one lane elected around
+            // the instructions).  Eight instructions take about 400 cycles to issue, so that one warp for both products was what the others
+            // waited for.
+            const bool is_scores = warp == kPScoreWarp;
+            RingAt<kPStages> at;
+            RingAt<kPKeyStages> k_at;
+            RingAt<kPQueryStages> q_at;
+            RingAt<kPWorks> work_at;
+            uint32_t entry_phase = 1u;
+            while (ok) {
+                PromptWork w;
                 if (!(ok = see_work(sh, work_at, w, limit))) break;
                 done_with_work(sh, work_at, lane);
                 if (w.nb == 0) break;
-            }
-            const uint64_t hint = w.tokens * a.g.G <= 16 ? once : keep;
-            const int32_t* table = a.p.block_table + (size_t)w.b * a.p.max_blocks_per_seq + w.kb0;
-            int held = 0;                                  // 32 entries of the table
-            const auto block_of = [&](int i) {
-                int blk = __shfl_sync(0xffffffffu, held, i & 31);
-                if (blk < 0 || blk >= a.num_blocks) { if (lane == 0) set_status(status, SD_ERR_BOUNDS); blk = 0; }
-                return blk;
-            };
-            for (int j = 0; ok && 2 * j < w.nb; ++j) {
-                if ((j & 15) == 0) held = 2 * j + lane < w.nb ? __ldcg(table + 2 * j + lane) : 0;
-                const bool two = 2 * j + 1 < w.nb;
-                const int y0 = (block_of(2 * j) * a.p.Hkv + w.h) * kBlock, y1 = two ? (block_of(2 * j + 1) * a.p.Hkv + w.h) * kBlock : 0;
-                if (!(ok = mbar_wait_warp(&empty[slot], slot_phase, abort_flag, limit))) break;
-                uint8_t* dst = ring + slot * kPStage;
-                if (elect_one()) {
-                    mbar_arrive_expect_tx(&full[slot], two ? kPStage : kPStage / 2);
-                    tma_load_2d(dst, map, 0, y0, &full[slot], hint);
-                    tma_load_2d(dst + kPHalf, map, 64, y0, &full[slot], hint);
-                    if (two) {
-                        tma_load_2d(dst + kPHalf / 2, map, 0, y1, &full[slot], hint);
-                        tma_load_2d(dst + kPHalf + kPHalf / 2, map, 64, y1, &full[slot], hint);
-                    }
-                }
-                __syncwarp();
-                if (++slot == stages) { slot = 0; slot_phase ^= 1u; }
-                if (j == 0 && keys) {
-                    if (!(ok = mbar_wait_warp(&sh.q_empty[q_at.slot], q_at.phase ^ 1u, abort_flag, limit))) break;
-                    if (elect_one()) {
-                        uint8_t* to = sh.q_smem + q_at.slot * kPQBytes;
-                        mbar_arrive_expect_tx(&sh.q_full[q_at.slot], (uint32_t)(a.g.tokens * a.g.G) * kD * 2);
-                        tma_load_3d(to, &q_map, 0, w.h * a.g.G, w.row0, &sh.q_full[q_at.slot], once);
-                        tma_load_3d(to + kRowTile * 128, &q_map, 64, w.h * a.g.G, w.row0, &sh.q_full[q_at.slot], once);
-                    }
-                    __syncwarp();
-                    q_at.next();
-                }
-            }
-        }
-    } else {                                               // warps 12 and 13
-        // ------------------------------------------------------------ products (whole warps in uniform control flow, one lane elected around
-        // the instructions).  Eight instructions take about 400 cycles to issue, so that one warp for both products was what the others
-        // waited for.
-        const bool is_scores = warp == kPScoreWarp;
-        RingAt<kPStages> at;
-        RingAt<kPKeyStages> k_at;
-        RingAt<kPQueryStages> q_at;
-        RingAt<kPWorks> work_at;
-        uint32_t entry_phase = 1u;
-        while (ok) {
-            PromptWork w;
-            if (!(ok = see_work(sh, work_at, w, limit))) break;
-            done_with_work(sh, work_at, lane);
-            if (w.nb == 0) break;
-            // Q is there; or the entry before has left O
-            if (!(ok = is_scores ? mbar_wait_warp(&sh.q_full[q_at.slot], q_at.phase, abort_flag, limit) : mbar_wait_warp(sh.o_empty, entry_phase, abort_flag, limit))) break;
-            entry_phase ^= 1u;
-            // Products of 64 rows have sixteen in each TMEM quadrant: the first sixteen lie where they do in those of 128.  (Under the power cap what
-            // idle rows do costs time: 32 single tokens behind 512 to 16384 100.2 us at 1.46 GHz, 96.7 at 1.64.)
-            const bool few = w.tokens * a.g.G <= 16;
-            if (is_scores) {
-                const uint32_t idesc_s = make_idesc_bf16(few ? 64 : kRowTile, kPromptTile, false, false), idesc_half = make_idesc_bf16(few ? 64 : kRowTile, kBlock, false, false);
-                const uint64_t q_desc = make_smem_desc(smem_u32(sh.q_smem + q_at.slot * kPQBytes), 16, 1024, 128);
-                const uint64_t k_desc = make_smem_desc(smem_u32(sh.k_smem), 16, 1024, 128);
-                for (int j = 0; 2 * j < w.nb; ++j) {
-                    if (!(ok = mbar_wait_warp(&sh.k_full[k_at.slot], k_at.phase, abort_flag, limit))) break;
-                    // the buffer held the weights of three tiles before
-                    if (!(ok = mbar_wait_warp(&sh.v_empty[at.slot], at.phase ^ 1u, abort_flag, limit))) break;
-                    tc_fence_after_sync();
-                    const uint64_t kd = k_desc + (uint64_t)(k_at.slot * (kPStage >> 4));
-                    const uint32_t d = tmem_s + at.slot * kPromptTile;
-                    const uint32_t idesc = 2 * j + 1 < w.nb ? idesc_s : idesc_half;
-                    if (elect_one()) {
+                // Q is there; or the entry before has left O
+                if (!(ok = is_scores ? mbar_wait_warp(&sh.q_full[q_at.slot], q_at.phase, abort_flag, limit) : mbar_wait_warp(sh.o_empty, entry_phase, abort_flag, limit))) break;
+                entry_phase ^= 1u;
+                // Products of 64 rows have sixteen in each TMEM quadrant: the first sixteen lie where they do in those of 128.  (Under the power cap what
+                // idle rows do costs time: 32 single tokens behind 512 to 16384 100.2 us at 1.46 GHz, 96.7 at 1.64.)
+                const bool few = w.tokens * a.g.G <= 16;
+                if (is_scores) {
+                    const uint32_t idesc_s = make_idesc_bf16(few ? 64 : kRowTile, kPromptTile, false, false), idesc_half = make_idesc_bf16(few ? 64 : kRowTile, kBlock, false, false);
+                    const uint64_t q_desc = make_smem_desc(smem_u32(sh.q_smem + q_at.slot * kPQBytes), 16, 1024, 128);
+                    const uint64_t k_desc = make_smem_desc(smem_u32(sh.k_smem), 16, 1024, 128);
+                    for (int j = 0; 2 * j < w.nb; ++j) {
+                        if (!(ok = mbar_wait_warp(&sh.k_full[k_at.slot], k_at.phase, abort_flag, limit))) break;
+                        // the buffer held the weights of three tiles before
+                        if (!(ok = mbar_wait_warp(&sh.v_empty[at.slot], at.phase ^ 1u, abort_flag, limit))) break;
+                        tc_fence_after_sync();
+                        const uint64_t kd = k_desc + (uint64_t)(k_at.slot * (kPStage >> 4));
+                        const uint32_t d = tmem_s + at.slot * kPromptTile;
+                        const uint32_t idesc = 2 * j + 1 < w.nb ? idesc_s : idesc_half;
+                        if (elect_one()) {
 #pragma unroll
-                        for (int k = 0; k < kD / 16; ++k)
-                            mma_ss(d, q_desc + (uint64_t)((k >> 2) * ((kRowTile * 128) >> 4) + (k & 3) * 2),
-                                   kd + (uint64_t)((k >> 2) * (kPHalf >> 4) + (k & 3) * 2), idesc, k != 0 ? 1u : 0u);
-                        mma_commit(&sh.s_full[at.slot]);
-                        mma_commit(&sh.k_empty[k_at.slot]);
-                        if (2 * (j + 1) >= w.nb) mma_commit(&sh.q_empty[q_at.slot]);
-                    }
-                    __syncwarp();
-                    at.next();
-                    k_at.next();
-                }
-                q_at.next();
-            } else {
-                const uint32_t idesc_o = make_idesc_bf16(few ? 64 : kRowTile, kD, false, true);
-                const uint64_t v_desc = make_smem_desc(smem_u32(sh.v_smem), kPHalf, 1024, 128);   // [key][d]: N (= d) contiguous
-                for (int j = 0; 2 * j < w.nb; ++j) {
-                    if (!(ok = mbar_wait_warp(&sh.v_full[at.slot], at.phase, abort_flag, limit))) break;
-                    if (!(ok = mbar_wait_warp(&sh.p_full[at.slot], at.phase, abort_flag, limit))) break;
-                    tc_fence_after_sync();
-                    const uint64_t vd = v_desc + (uint64_t)(at.slot * (kPStage >> 4));
-                    const uint32_t pa = tmem_s + at.slot * kPromptTile;                // 16 keys = 8 columns
-                    const uint32_t first = j ? 1u : 0u;
-                    if (elect_one()) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) mma_ts(tmem, pa + i * 8, vd + (uint64_t)(i * (2048 >> 4)), idesc_o, i ? 1u : first);
-                        if (2 * j + 1 < w.nb) {
-#pragma unroll
-                            for (int i = 4; i < 8; ++i) mma_ts(tmem, pa + i * 8, vd + (uint64_t)(i * (2048 >> 4)), idesc_o, 1u);
+                            for (int k = 0; k < kD / 16; ++k)
+                                mma_ss(d, q_desc + (uint64_t)((k >> 2) * ((kRowTile * 128) >> 4) + (k & 3) * 2),
+                                       kd + (uint64_t)((k >> 2) * (kPHalf >> 4) + (k & 3) * 2), idesc, k != 0 ? 1u : 0u);
+                            mma_commit(&sh.s_full[at.slot]);
+                            mma_commit(&sh.k_empty[k_at.slot]);
+                            if (2 * (j + 1) >= w.nb) mma_commit(&sh.q_empty[q_at.slot]);
                         }
-                        mma_commit(&sh.v_empty[at.slot]);
-                        if (2 * (j + 1) >= w.nb) mma_commit(sh.o_full);
+                        __syncwarp();
+                        at.next();
+                        k_at.next();
                     }
-                    __syncwarp();
-                    at.next();
+                    q_at.next();
+                } else {
+                    const uint32_t idesc_o = make_idesc_bf16(few ? 64 : kRowTile, kD, false, true);
+                    const uint64_t v_desc = make_smem_desc(smem_u32(sh.v_smem), kPHalf, 1024, 128);   // [key][d]: N (= d) contiguous
+                    for (int j = 0; 2 * j < w.nb; ++j) {
+                        if (!(ok = mbar_wait_warp(&sh.v_full[at.slot], at.phase, abort_flag, limit))) break;
+                        if (!(ok = mbar_wait_warp(&sh.p_full[at.slot], at.phase, abort_flag, limit))) break;
+                        tc_fence_after_sync();
+                        const uint64_t vd = v_desc + (uint64_t)(at.slot * (kPStage >> 4));
+                        const uint32_t pa = tmem_s + at.slot * kPromptTile;                // 16 keys = 8 columns
+                        const uint32_t first = j ? 1u : 0u;
+                        if (elect_one()) {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) mma_ts(tmem, pa + i * 8, vd + (uint64_t)(i * (2048 >> 4)), idesc_o, i ? 1u : first);
+                            if (2 * j + 1 < w.nb) {
+#pragma unroll
+                                for (int i = 4; i < 8; ++i) mma_ts(tmem, pa + i * 8, vd + (uint64_t)(i * (2048 >> 4)), idesc_o, 1u);
+                            }
+                            mma_commit(&sh.v_empty[at.slot]);
+                            if (2 * (j + 1) >= w.nb) mma_commit(sh.o_full);
+                        }
+                        __syncwarp();
+                        at.next();
+                    }
                 }
             }
+            uint64_t* const mine = &sh.unwound[is_scores ? 0 : 1];
+            if (elect_one()) mma_commit(mine);
+            __syncwarp();
+            mbar_wait_plain(mine, 0, limit);                   // (nothing gives tensor memory back while a product runs)
         }
-        uint64_t* const mine = &sh.unwound[is_scores ? 0 : 1];
-        if (elect_one()) mma_commit(mine);
-        __syncwarp();
-        mbar_wait_plain(mine, 0, limit);                   // (nothing gives tensor memory back while a product runs)
-    }
     } else if (warp < 8) {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
         // ------------------------------------------------------------ soft-max: one thread per row and group
@@ -579,7 +579,7 @@ prompt_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__
                         *my_ref = st.m;
                         __syncwarp();
                         if (lane == 0) mbar_arrive(ref_full);
-                        }
+                    }
                     const uint64_t neg_m2 = twice(-st.m);
                     exp_pack(ra, scale2, neg_m2, pk, ps);
                     tmem_ld_wait();

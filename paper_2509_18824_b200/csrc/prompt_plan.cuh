@@ -26,11 +26,11 @@ __device__ __forceinline__ RequestSpan request_span(const sd_prompts& p, int b, 
 //   In parts: all entries of all heads stand in one line, entry by entry and head by head, each as long as its key tiles and kEntryTiles; the
 //   line is cut into G equal parts.  An entry that a cut goes through is computed in chunks of whole key tiles and joined.  Every
 //   CTA has at most two such chunks, its first and its last piece.
-// Parts are even, but their ends have to be joined (about 6 us), and what an entry costs beside its tiles is not known well (it overlaps its
+// Parts are even, but their ends have to be joined (about 5 us), and what an entry costs beside its tiles is not known well (it overlaps its
 // neighbours); dealt out, every CTA has as many entries as the others.  So entries are dealt out where every CTA gets kDealFrom times the
-// longest.  Us, dealt out and in parts (when a tile took a tenth longer than now): 16 prompts of up to 2048 tokens 135 and 165, three of up to 6000
-// with twelve heads 190 and 201, eight of 4096 811 and 821; with entries cut at half a CTA's share and then dealt out, and in parts: one token behind 2047 17 and 11, 32 behind 512 to
-// 16384 117 and 94, 61 behind 16000 41 and 28.
+// longest.  Us, dealt out and in parts (28 query, 4 KV heads): 16 prompts of up to 2048 tokens 137 and 148, three of up to 6000 with twelve heads 189 and
+// 198, eight of 4096 799 and 811, one of 32749 5660 and 5735; in parts by the rule: 1000 tokens behind 7000 beside 24 single ones 112 and 114, 32 single
+// tokens behind 512 to 16384 121 and 94, one behind 2047 20 and 12, 61 tokens behind 16000 104 and 30.
 constexpr int kPromptTile = 128;               // keys per tile: two cache blocks
 constexpr int kEntryTiles = 2;                 // what an entry costs beside its key tiles, in key tiles (1 and 3: the same within 1 %)
 constexpr int kPartMin = 2;                    // the shortest part of a CTA
