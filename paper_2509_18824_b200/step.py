@@ -376,11 +376,11 @@ class PromptStep(sd._OnAnyStream):
         """Tables, slots and positions (self.prompts.position: what a decoder rotates q and k by), and the attention's plan."""
         p, status = self.prompts, self.step.status
         self._ready(stream)
-        self._begun = True
         if self.pool is not None:
             self.step._pool = self.pool, p.n_blocks
             self.step._cover(p.n_new, self.granted, stream)
         sd.sd_prompt_prepare(p, status, stream)
+        self._begun = True
 
     def layer(self, l: int, q, k, v, out, lse=None, stream=None):
         """K and V [N, Hkv, 128] of the new tokens into layer l's cache, then their attention: q, out [N, Hq, 128], lse [N, Hq] or None."""

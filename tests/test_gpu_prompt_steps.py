@@ -193,3 +193,21 @@ def test_blocks_for_trees_come_behind_the_prompts():
     torch.cuda.synchronize()
     vs.check_status()
     assert p.granted.tolist() == [1, 1] and p.trees_granted.tolist() == [1, 0] and held.tolist() == [2, 1] and vs.batch.len.tolist() == [60, 60]
+
+
+def test_a_begin_that_failed_leaves_the_trees_their_blocks(monkeypatch):
+    vs = VerifyStep(workload(2, L=1))
+    vs.batch.len.zero_()
+    pool, held = sd.BlockPool(8), torch.zeros(2, dtype=torch.int32, device="cuda")
+    p = vs.prompts(120, [60, 60], pool, held)
+
+    def refused(*_):
+        raise sd.SdError(sd.SD_ERR_UNSUPPORTED)
+    monkeypatch.setattr(sd, "sd_prompt_prepare", refused)
+    with pytest.raises(sd.SdError):
+        p.begin()
+    monkeypatch.undo()
+    p.reserve_trees()
+    torch.cuda.synchronize()
+    vs.check_status()
+    assert held.tolist() == [1, 1] and p.trees_granted.tolist() == [1, 1] and vs.batch.len.tolist() == [0, 0]
