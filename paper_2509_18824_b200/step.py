@@ -2,7 +2,8 @@
 
 Per layer: tree attention; then once: LM-head arg-max, greedy acceptance and
 KV compaction over all layers.  This file only moves tensors to the device and
-issues the C-ABI calls in order; it computes nothing itself.  (The layers'
+issues the C-ABI calls in order; beside counts of tokens and marks of
+sequences that wait it computes nothing itself.  (The layers'
 projections, MLPs and norms of a real decoder are outside this library: q,
 tree K/V and the final hidden states are inputs.)
 """
